@@ -12,6 +12,9 @@
  *     < D, "distant" is >= D), applied per point together with visibility;
  *   - the dispatch of points and features into contiguous per-expert buffers,
  *     indexed by prefix sums (Sec. 3.6).
+ * Beside it stand the learned operators that an expert applies to those rows
+ * first, forward and backward (Sec. 3.3, 3.4): rows of a table by id, layer norm
+ * and a gated feed-forward block with weights per expert.
  *
  * General rules
  *   - Every pointer named d_* is DEVICE memory on the handle's device, owned by
@@ -305,6 +308,59 @@ int emc2_occlusion(emc2_bridge_t* bridge, int32_t B, int32_t N, const float* d_p
  * Enqueues one small kernel on `cuda_stream`. */
 int emc2_scene_route(emc2_bridge_t* bridge, int32_t B, const int32_t* d_offsets, const uint8_t* priority,
                      int32_t min_points, int32_t* d_scene_expert, void* cuda_stream);
+
+/* ---- Operators on dispatched rows, for the experts and their training (Sec. 3.3, 3.4; the paper's own layers are not
+ * given, these are the usual forms).  Rules beyond the general ones:
+ *   - Rows are [B, N, channels] as emc2_route_dispatch leaves them: frame b's rows of expert e are
+ *     d_offsets[b][e] .. d_offsets[b][e+1] - 1 (int32 [B, E+1], E of the handle's configuration).  Rows before
+ *     d_offsets[b][0] and from d_offsets[b][E] on belong to no expert: they are not read into any result, and the
+ *     output rows there are left untouched.  d_offsets NULL: one expert (E = 1) owns every row.  Offsets that do not
+ *     ascend within 0 .. N make EMC2_ERR_INVALID_ARG sticky; they are then taken as the nearest that do.
+ *   - The number of channels is the call's own, not the configuration's feat_c.
+ *   - Weights and their gradients have one entry per expert, the expert first; the gradient of an expert without rows is
+ *     zero.  Gradients are written, not added to.
+ *   - Outputs must not alias inputs.  Results are the same on every run, bit for bit.
+ *   - Calls marked (scratch) use the area that emc2_rows_reserve allocates, and return EMC2_ERR_TOO_LARGE if it was not
+ *     reserved for that many channels. */
+typedef enum { EMC2_F32 = 0, EMC2_BF16 = 1, EMC2_F16 = 2 } emc2_type_t;
+
+/* Allocates the scratch of the calls marked (scratch) for up to max_channels channels (4 .. 1024) and
+ * any batch the handle takes; max_hidden >= 0 is the largest hidden width of emc2_expert_ffn and its gradient.  A
+ * later call can ask for more: the first area then stays allocated until the handle is destroyed, so that graphs
+ * captured with it stay valid.  Call it outside any stream capture. */
+int emc2_rows_reserve(emc2_bridge_t* bridge, int32_t max_channels, int32_t max_hidden);
+
+/* Rows of a table by id: d_out[i] = scale * d_table[d_ids[i]], zeros where d_ids[i] is negative, as d_point_voxel and
+ * d_cam mark points without a voxel or camera.  For voxel rows brought back to their points, or learned rows by
+ * expert, camera or ring.
+ *   d_ids    int32 [n], n <= max_batch * max_points     d_table  type [rows, channels]     d_out  type [n, channels]
+ * channels is a multiple of 4 up to 1024.  The product is rounded once.  An id >= rows makes EMC2_ERR_INVALID_ARG
+ * sticky and gives zeros. */
+int emc2_row_lookup(emc2_bridge_t* bridge, int32_t n, int32_t rows, int32_t channels, int32_t type, const int32_t* d_ids,
+                    const void* d_table, float scale, void* d_out, void* cuda_stream);
+
+/* Its gradient (scratch): d_grad_table[v] = scale * the sum of d_grad_out[i] over d_ids[i] = v, zeros where no id names v.
+ * Sums are held in fp32 and rounded once.  An id >= rows makes EMC2_ERR_INVALID_ARG sticky and counts nowhere.
+ *   d_grad_out  type [n, channels]     d_grad_table  type [rows, channels], every row written */
+int emc2_row_lookup_grad(emc2_bridge_t* bridge, int32_t n, int32_t rows, int32_t channels, int32_t type, const int32_t* d_ids,
+                         const void* d_grad_out, float scale, void* d_grad_table, void* cuda_stream);
+
+/* Layer norm with a weight and a bias per expert: d_y = (x - mean) * rstd * weight[e] + bias[e] per row, with
+ * rstd = 1 / sqrt(mean((x - mean)^2) + eps).  fp32 throughout, rounded once to type_y.
+ *   d_x     type_x [B, N, channels]     d_y  type_y [B, N, channels]; channels a multiple of 4 up to 1024
+ *   d_weight, d_bias  float [E, channels]; d_bias may be NULL
+ *   d_mean, d_rstd    float [B, N], for the gradient; either may be NULL
+ * eps >= 0. */
+int emc2_expert_norm(emc2_bridge_t* bridge, int32_t B, int32_t N, int32_t channels, int32_t type_x, int32_t type_y, const void* d_x,
+                     const int32_t* d_offsets, const float* d_weight, const float* d_bias, float eps, void* d_y, float* d_mean,
+                     float* d_rstd, void* cuda_stream);
+
+/* Its gradients (scratch) for d_grad_y, type_y [B, N, channels], and the d_mean and d_rstd that the forward call left:
+ *   d_grad_x  type_x [B, N, channels]     d_grad_weight, d_grad_bias  float [E, channels]; d_grad_bias may be NULL */
+int emc2_expert_norm_grad(emc2_bridge_t* bridge, int32_t B, int32_t N, int32_t channels, int32_t type_x, int32_t type_y,
+                          const void* d_x, const int32_t* d_offsets, const float* d_weight, const float* d_mean,
+                          const float* d_rstd, const void* d_grad_y, void* d_grad_x, float* d_grad_weight, float* d_grad_bias,
+                          void* cuda_stream);
 
 /* Turns the handle's own streams in emc2_bridge_run off (0) or on (non-zero, the default).  Off, every
  * kernel of the call is enqueued on `cuda_stream` itself, one after another: for callers that

@@ -37,7 +37,11 @@ ABI_SYMBOLS = (
     "emc2_features_channels_last",
     "emc2_voxel_image", "emc2_voxel_image_sampled", "emc2_occlusion", "emc2_rulebook",
     "emc2_bridge_set_tuning", "emc2_bridge_profile_timeline", "emc2_voxel_image_pooled",
+    "emc2_rows_reserve", "emc2_row_lookup", "emc2_row_lookup_grad", "emc2_expert_norm", "emc2_expert_norm_grad",
 )
+
+# emc2_type_t
+ROW_TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 
 # emc2_tuning_t
 TUNE_ROW_STORE = 0
@@ -106,6 +110,12 @@ def load_library() -> ctypes.CDLL:
     lib.emc2_bridge_set_overlap.argtypes = [vp, ctypes.c_int]
     lib.emc2_bridge_set_tuning.argtypes = [vp, i32, i32]
     lib.emc2_bridge_profile_timeline.argtypes = [vp, P(i32), P(ctypes.c_float), P(ctypes.c_float), i32]
+    f32 = ctypes.c_float
+    lib.emc2_rows_reserve.argtypes = [vp, i32, i32]
+    lib.emc2_row_lookup.argtypes = [vp, i32, i32, i32, i32, vp, vp, f32, vp, vp]
+    lib.emc2_row_lookup_grad.argtypes = [vp, i32, i32, i32, i32, vp, vp, f32, vp, vp]
+    lib.emc2_expert_norm.argtypes = [vp] + [i32] * 5 + [vp] * 4 + [f32] + [vp] * 4
+    lib.emc2_expert_norm_grad.argtypes = [vp] + [i32] * 5 + [vp] * 10
     lib.emc2_bridge_destroy.argtypes = [vp]
     lib.emc2_status_string.argtypes = [ctypes.c_int]
     lib.emc2_status_string.restype = ctypes.c_char_p
@@ -459,6 +469,103 @@ class Bridge:
         rc = self.lib.emc2_scene_route(self._h, B, offsets.data_ptr(), pr, int(min_points), out.data_ptr(),
                                        self._stream())
         self._raise(rc, "emc2_scene_route")
+        return out
+
+    # ------------------------------------------------------------------ operators on dispatched rows
+    def reserve_rows(self, channels: int, hidden: int = 0) -> None:
+        """emc2_rows_reserve: scratch of the gradient calls below for rows of up to ``channels`` channels."""
+        self._raise(self.lib.emc2_rows_reserve(self._h, int(channels), int(hidden)), "emc2_rows_reserve")
+
+    def _row_type(self, t: torch.Tensor, name: str) -> int:
+        if t.dtype not in ROW_TYPES:
+            raise ValueError(f"{name}: expected float32, bfloat16 or float16, got {t.dtype}")
+        return ROW_TYPES[t.dtype]
+
+    def _experts(self, offsets: Optional[torch.Tensor], B: int) -> int:
+        if offsets is None:
+            return 1
+        _check(offsets, torch.int32, (B, self.cfg.num_experts + 1), "offsets", self.device)
+        return self.cfg.num_experts
+
+    def row_lookup(self, ids: torch.Tensor, table: torch.Tensor, scale: float = 1.0,
+                   out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """emc2_row_lookup: ``scale * table[ids]`` with zero rows where an id is negative; ids of any shape."""
+        rows, C = table.shape
+        kind = self._row_type(table, "table")
+        _check(ids, torch.int32, ids.shape, "ids", self.device)
+        _check(table, table.dtype, (rows, C), "table", self.device)
+        shape = (*ids.shape, C)
+        if out is None:
+            out = torch.empty(shape, dtype=table.dtype, device=self.device)
+        _check(out, table.dtype, shape, "out", self.device)
+        rc = self.lib.emc2_row_lookup(self._h, ids.numel(), rows, C, kind, ids.data_ptr(), table.data_ptr(), float(scale),
+                                      out.data_ptr(), self._stream())
+        self._raise(rc, "emc2_row_lookup")
+        return out
+
+    def row_lookup_grad(self, ids: torch.Tensor, grad_out: torch.Tensor, rows: int, scale: float = 1.0,
+                        out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """emc2_row_lookup_grad: gradient [rows, channels] of the table of :meth:`row_lookup` (needs :meth:`reserve_rows`)."""
+        C = grad_out.shape[-1]
+        kind = self._row_type(grad_out, "grad_out")
+        _check(ids, torch.int32, ids.shape, "ids", self.device)
+        _check(grad_out, grad_out.dtype, (*ids.shape, C), "grad_out", self.device)
+        if out is None:
+            out = torch.empty((int(rows), C), dtype=grad_out.dtype, device=self.device)
+        _check(out, grad_out.dtype, (int(rows), C), "out", self.device)
+        rc = self.lib.emc2_row_lookup_grad(self._h, ids.numel(), int(rows), C, kind, ids.data_ptr(), grad_out.data_ptr(),
+                                           float(scale), out.data_ptr(), self._stream())
+        self._raise(rc, "emc2_row_lookup_grad")
+        return out
+
+    def expert_norm(self, x: torch.Tensor, offsets: Optional[torch.Tensor], weight: torch.Tensor,
+                    bias: Optional[torch.Tensor] = None, eps: float = 1e-5, out_dtype: Optional[torch.dtype] = None,
+                    out: Optional[Dict[str, Optional[torch.Tensor]]] = None) -> Dict[str, Optional[torch.Tensor]]:
+        """emc2_expert_norm: ``y``, and the ``mean`` and ``rstd`` of every row for the gradient (None in ``out``: not stored).
+        Rows of no expert are left as they are in ``out``; without ``out`` they are unspecified."""
+        B, N, C = x.shape
+        E = self._experts(offsets, B)
+        _check(x, x.dtype, (B, N, C), "x", self.device)
+        _check(weight, torch.float32, (E, C), "weight", self.device)
+        if bias is not None:
+            _check(bias, torch.float32, (E, C), "bias", self.device)
+        if out is None:
+            out = {"y": torch.empty((B, N, C), dtype=out_dtype or x.dtype, device=self.device),
+                   "mean": torch.empty((B, N), dtype=torch.float32, device=self.device),
+                   "rstd": torch.empty((B, N), dtype=torch.float32, device=self.device)}
+        y = out["y"]
+        _check(y, out_dtype or y.dtype, (B, N, C), "y", self.device)
+        for k in ("mean", "rstd"):
+            if out.get(k) is not None:
+                _check(out[k], torch.float32, (B, N), k, self.device)
+        rc = self.lib.emc2_expert_norm(self._h, B, N, C, self._row_type(x, "x"), self._row_type(y, "y"), x.data_ptr(),
+                                       _ptr(offsets), weight.data_ptr(), _ptr(bias), float(eps), y.data_ptr(),
+                                       _ptr(out.get("mean")), _ptr(out.get("rstd")), self._stream())
+        self._raise(rc, "emc2_expert_norm")
+        return out
+
+    def expert_norm_grad(self, x: torch.Tensor, offsets: Optional[torch.Tensor], weight: torch.Tensor, mean: torch.Tensor,
+                         rstd: torch.Tensor, grad_y: torch.Tensor,
+                         out: Optional[Dict[str, Optional[torch.Tensor]]] = None) -> Dict[str, Optional[torch.Tensor]]:
+        """emc2_expert_norm_grad: ``grad_x``, ``grad_weight``, ``grad_bias`` (needs :meth:`reserve_rows`)."""
+        B, N, C = x.shape
+        E = self._experts(offsets, B)
+        _check(x, x.dtype, (B, N, C), "x", self.device)
+        _check(weight, torch.float32, (E, C), "weight", self.device)
+        _check(mean, torch.float32, (B, N), "mean", self.device)
+        _check(rstd, torch.float32, (B, N), "rstd", self.device)
+        _check(grad_y, grad_y.dtype, (B, N, C), "grad_y", self.device)
+        if out is None:
+            out = {"grad_x": torch.empty_like(x), "grad_weight": torch.empty_like(weight), "grad_bias": torch.empty_like(weight)}
+        _check(out["grad_x"], x.dtype, (B, N, C), "grad_x", self.device)
+        _check(out["grad_weight"], torch.float32, (E, C), "grad_weight", self.device)
+        if out.get("grad_bias") is not None:
+            _check(out["grad_bias"], torch.float32, (E, C), "grad_bias", self.device)
+        rc = self.lib.emc2_expert_norm_grad(self._h, B, N, C, self._row_type(x, "x"), self._row_type(grad_y, "grad_y"),
+                                            x.data_ptr(), _ptr(offsets), weight.data_ptr(), mean.data_ptr(), rstd.data_ptr(),
+                                            grad_y.data_ptr(), out["grad_x"].data_ptr(), out["grad_weight"].data_ptr(),
+                                            _ptr(out.get("grad_bias")), self._stream())
+        self._raise(rc, "emc2_expert_norm_grad")
         return out
 
     def set_overlap(self, enable: bool) -> None:

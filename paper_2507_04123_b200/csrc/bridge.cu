@@ -1,9 +1,10 @@
 // Handle management and the extern "C" entry points of the bridge library.
+#include <algorithm>
 #include <cmath>
 #include <cstring>
 #include <new>
 
-#include "bridge_internal.cuh"
+#include "rows.cuh"
 
 namespace emc2 {
 
@@ -11,7 +12,8 @@ static const char* const kKernelNames[K_KINDS] = {
     "vox_mark", "vox_count", "vox_rank", "vox_accum", "vox_over_find", "vox_over_fill", "vox_finalize", "arm_keys", "arm_sort", "arm_hash", "arm_rank",
     "project_gather", "project_route", "gather_scatter", "route_hist", "route_scan", "dispatch_scatter", "scene_route", "pool_features",
     "vif_scan", "vif_fill", "vif_mean", "vif_sample", "occl_fill", "occl_splat", "occl_test",
-    "channels_last", "rb_mark", "rb_count", "rb_scan", "rb_fill", "rb_clear"};
+    "channels_last", "rb_mark", "rb_count", "rb_scan", "rb_fill", "rb_clear",
+    "row_lookup", "lookup_sort", "lookup_sum", "lookup_join", "norm", "norm_grad", "norm_sum"};
 
 int check_cuda(emc2_bridge* h, cudaError_t e) {
     if (e == cudaSuccess) return EMC2_OK;
@@ -645,6 +647,29 @@ int emc2_bridge_set_tuning(emc2_bridge_t* h, int32_t knob, int32_t value) {
     return EMC2_OK;
 }
 
+int emc2_rows_reserve(emc2_bridge_t* h, int32_t max_channels, int32_t max_hidden) {
+    if (!h || max_channels < 4 || max_channels > kMaxRowChannels || max_hidden < 0) return EMC2_ERR_INVALID_ARG;
+    RowsScratch& r = h->rows_scratch;
+    if (r.slab && max_channels <= r.max_channels && max_hidden <= r.max_hidden) return EMC2_OK;
+    const int channels = std::max(max_channels, r.max_channels), hidden = std::max(max_hidden, r.max_hidden);
+    const size_t bytes = std::max(norm_scratch_bytes(h, channels), lookup_scratch_bytes(h, channels));
+    DeviceGuard guard(h->cfg.device);
+    if (!guard.ok) return EMC2_ERR_CUDA;
+    if (!r.slab || bytes > r.bytes) {
+        // Room for the old area's place in the list first: a failure must not lose it.
+        try { r.outgrown.reserve(r.outgrown.size() + 1); } catch (...) { return EMC2_ERR_INTERNAL; }
+        void* p = nullptr;
+        const cudaError_t e = cudaMalloc(&p, bytes);
+        if (e != cudaSuccess) { cudaGetLastError(); return check_cuda(h, e); }
+        if (r.slab) { r.outgrown.push_back(r.slab); r.outgrown_bytes += r.bytes; }
+        r.slab = p;
+        r.bytes = bytes;
+    }
+    r.max_channels = channels;
+    r.max_hidden = hidden;
+    return EMC2_OK;
+}
+
 int emc2_bridge_status(emc2_bridge_t* h, void* cuda_stream) {
     if (!h) return EMC2_ERR_INVALID_ARG;
     DeviceGuard guard(h->cfg.device);
@@ -677,6 +702,9 @@ int emc2_bridge_destroy(emc2_bridge_t* h) {
     if (h->rows) cudaStreamDestroy(h->rows);
     if (h->slab && cudaFree(h->slab) != cudaSuccess) rc = EMC2_ERR_CUDA;
     if (h->arm.slab && cudaFree(h->arm.slab) != cudaSuccess) rc = EMC2_ERR_CUDA;
+    if (h->rows_scratch.slab && cudaFree(h->rows_scratch.slab) != cudaSuccess) rc = EMC2_ERR_CUDA;
+    for (void* p : h->rows_scratch.outgrown)
+        if (cudaFree(p) != cudaSuccess) rc = EMC2_ERR_CUDA;
     delete h;
     return rc;
 }
@@ -696,7 +724,7 @@ const char* emc2_status_string(int status) {
 }
 
 int emc2_bridge_last_cuda_error(const emc2_bridge_t* h) { return h ? h->last_cuda_error : 0; }
-size_t emc2_bridge_scratch_bytes(const emc2_bridge_t* h) { return h ? h->slab_bytes + h->arm.bytes : 0; }
+size_t emc2_bridge_scratch_bytes(const emc2_bridge_t* h) { return h ? h->slab_bytes + h->arm.bytes + h->rows_scratch.bytes + h->rows_scratch.outgrown_bytes : 0; }
 
 int emc2_bridge_kernel_kinds(void) { return K_KINDS; }
 const char* emc2_bridge_kernel_name(int kind) { return kind >= 0 && kind < K_KINDS ? kKernelNames[kind] : ""; }

@@ -71,6 +71,13 @@ enum KernelKind {
     K_RB_SCAN,
     K_RB_FILL,
     K_RB_CLEAR,
+    K_ROW_LOOKUP,
+    K_LOOKUP_SORT,
+    K_LOOKUP_SUM,
+    K_LOOKUP_JOIN,
+    K_NORM,
+    K_NORM_GRAD,
+    K_NORM_SUM,
     K_KINDS
 };
 
@@ -185,6 +192,15 @@ struct DedupArm {
     uint32_t slots = 0;
 };
 
+// Scratch of the operators on dispatched rows (emc2_rows_reserve).  Each call lays it out for itself.
+struct RowsScratch {
+    void* slab = nullptr;
+    size_t bytes = 0;
+    int max_channels = 0, max_hidden = 0;
+    std::vector<void*> outgrown;                // smaller ones that captured graphs may still use
+    size_t outgrown_bytes = 0;
+};
+
 struct ProfRec {
     int kind;
     cudaEvent_t a, b;
@@ -214,6 +230,7 @@ struct emc2_bridge {
     int max_tiles = 0;
     int tune[EMC2_TUNE_KNOBS] = {0, 1, 0, 0, 0};   // emc2_bridge_set_tuning
     emc2::DedupArm arm;
+    emc2::RowsScratch rows_scratch;
     int num_sms = 0;               // multiprocessors of the handle's device
     bool overlap = true;           // emc2_bridge_run uses `side` and `rows`
     cudaStream_t side = nullptr;   // stream of stage 1 inside emc2_bridge_run ...
@@ -249,6 +266,14 @@ int launch_voxelize(emc2_bridge* h, int B, int N, const float* d_points, int32_t
                     const int32_t capacity[2], int32_t* d_num_voxels, float* d_bev, cudaStream_t st,
                     bool marked = false, bool chained = false);
 int dedup_arm_alloc(emc2_bridge* h);
+// Sorts n (key, value) pairs by the low `bits` bits of the key, stably; returns which buffer holds the result.  counts:
+// [256][sort_tiles(n)], row_tot: [256].  `kind`: the kernel kind that the launches count as.
+int sort_tiles(size_t n);
+int radix_sort(emc2_bridge* h, int kind, int n, int bits, uint32_t* const keys[2], uint32_t* const vals[2], bool with_vals, int* counts,
+               int* row_tot, cudaStream_t st);
+// Scratch that the operators on rows of up to max_channels channels need on this handle.
+size_t norm_scratch_bytes(const emc2_bridge* h, int max_channels);
+size_t lookup_scratch_bytes(const emc2_bridge* h, int max_channels);
 int launch_dedup_arm(emc2_bridge* h, int s, int design, int B, int N, const float* d_points, int capacity,
                      int32_t* d_num_voxels, cudaStream_t st);
 int launch_project_gather(emc2_bridge* h, int B, int N, const float* d_points, const float* d_proj,

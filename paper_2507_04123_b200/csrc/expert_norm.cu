@@ -1,0 +1,354 @@
+// Layer norm of dispatched rows with a weight and a bias per expert, and its gradients.
+//
+//   m = mean(x), r = 1 / sqrt(mean((x - m)^2) + eps), h = (x - m) r, y = h w_e + b_e
+//   g = dy w_e:  dx = r (g - mean(g) - h mean(g h)),  dw_e = sum dy h,  db_e = sum dy   over the expert's rows
+//
+// Bound by memory: a row is read once, held in the registers of a group of lanes (see row_split), and written once.
+// Sums, means and gradients of the parameters are held in fp32; y and dx are rounded once.
+#include <algorithm>
+
+#include "rows.cuh"
+
+namespace emc2 {
+namespace {
+
+constexpr int kNormThreads = 256;
+
+struct NormArgs {
+    RowSegments seg;
+    FastDiv frame;               // division by N
+    const void* x;
+    const float* weight;
+    const float* bias;           // or null
+    void* y;
+    float* mean;                 // or null
+    float* rstd;                 // or null
+    float eps, inv_c;
+    int nvec, log, type_x, type_y;
+};
+
+// Rows in the caller's order, one per group of lanes and step.  The weights of the expert whose rows a group is at stay
+// in its registers.
+template <int K>
+__global__ void __launch_bounds__(kNormThreads) norm_kernel(NormArgs a) {
+    __shared__ int bounds[kMaxBounds];
+    load_bounds(a.seg, bounds);
+    const int lane = threadIdx.x & ((1 << a.log) - 1);
+    const uint32_t rows = (uint32_t)a.seg.B * a.seg.N, groups = (gridDim.x * kNormThreads) >> a.log;
+    const uint32_t sub = (threadIdx.x & 31) >> a.log, first = (blockIdx.x * kNormThreads + threadIdx.x) >> a.log;
+    const int E = a.seg.E;
+    float4 w[K], bias[K];
+    int have = -1;
+    // All groups of a warp make the same number of steps: the sums are taken by the whole warp.
+    for (uint32_t r0 = first - sub; r0 < rows; r0 += groups) {
+        const uint32_t row = r0 + sub;
+        int e = E;
+        if (row < rows) {
+            uint32_t b, j;
+            a.frame.divmod(row, b, j);
+            const int* of = bounds + b * (E + 1);
+            if ((int)j >= of[0]) {
+                e = 0;
+                while (e < E && (int)j >= of[e + 1]) ++e;
+            }
+        }
+        const bool in = e < E;
+        float4 x[K];
+        load_row<K>(x, a.x, (size_t)row * a.nvec, lane, a.log, in ? a.nvec : 0, a.type_x);
+        if (in && e != have) {
+            have = e;
+#pragma unroll
+            for (int i = 0; i < K; ++i) {
+                const int v = lane + (i << a.log);
+                const float4 zero = make_float4(0.f, 0.f, 0.f, 0.f);
+                w[i] = v < a.nvec ? __ldg(reinterpret_cast<const float4*>(a.weight) + e * a.nvec + v) : zero;
+                bias[i] = a.bias && v < a.nvec ? __ldg(reinterpret_cast<const float4*>(a.bias) + e * a.nvec + v) : zero;
+            }
+        }
+        float s = 0.f;
+#pragma unroll
+        for (int i = 0; i < K; ++i) s += (x[i].x + x[i].y) + (x[i].z + x[i].w);
+        const float m = group_sum(s, a.log) * a.inv_c;
+        // The variance from the differences: the squares of values far from zero would lose it.
+        float q = 0.f;
+#pragma unroll
+        for (int i = 0; i < K; ++i) {
+            if (lane + (i << a.log) >= a.nvec) continue;
+            x[i].x -= m; x[i].y -= m; x[i].z -= m; x[i].w -= m;
+            q += (x[i].x * x[i].x + x[i].y * x[i].y) + (x[i].z * x[i].z + x[i].w * x[i].w);
+        }
+        const float r = rsqrtf(group_sum(q, a.log) * a.inv_c + a.eps);
+        if (!in) continue;
+#pragma unroll
+        for (int i = 0; i < K; ++i) {
+            const int v = lane + (i << a.log);
+            if (v >= a.nvec) continue;
+            const float4 o = make_float4(x[i].x * r * w[i].x + bias[i].x, x[i].y * r * w[i].y + bias[i].y,
+                                         x[i].z * r * w[i].z + bias[i].z, x[i].w * r * w[i].w + bias[i].w);
+            store_row4(a.y, (size_t)row * a.nvec + v, o, a.type_y);
+        }
+        if (lane == 0) {
+            if (a.mean) a.mean[row] = m;
+            if (a.rstd) a.rstd[row] = r;
+        }
+    }
+}
+
+struct NormGradArgs {
+    RowSegments seg;
+    const void* x;
+    const void* dy;
+    const float* weight;
+    const float* mean;
+    const float* rstd;
+    void* dx;
+    float* part;                 // [gridDim.x + E][2][C]: sums of dw and db of a CTA's rows of an expert
+    float inv_c;
+    int nvec, log, type_x, type_y;
+};
+
+// The rows are taken expert by expert, an equal run of them per CTA: a CTA meets few experts, and sums the parameters'
+// gradients of each in registers.  Entry i + e of `part` holds those of CTA i and expert e: along the run of all rows
+// either i or e goes up, so no two share an entry.
+template <int K>
+__global__ void __launch_bounds__(kNormThreads, 1) norm_grad_kernel(NormGradArgs a) {
+    __shared__ int bounds[kMaxBounds];
+    __shared__ int start[kMaxSegments + 1];
+    extern __shared__ float4 sums[];             // [warps][2][nvec]
+    load_bounds(a.seg, bounds);
+    segment_starts(a.seg, bounds, 1, start);
+    const int B = a.seg.B, E = a.seg.E, total = start[B * E];
+    const int lo = (int)((long long)total * blockIdx.x / gridDim.x), hi = (int)((long long)total * (blockIdx.x + 1) / gridDim.x);
+    const int lanes = 1 << a.log, lane = threadIdx.x & (lanes - 1), warp = threadIdx.x >> 5;
+    const int per_warp = 32 >> a.log, sub = (threadIdx.x & 31) >> a.log, step = kNormThreads >> a.log;
+    if (lo >= hi) return;
+    for (int e = segment_of(start, B * E, lo) / B; e < E && start[e * B] < hi; ++e) {
+        const int from = max(lo, start[e * B]), to = min(hi, start[(e + 1) * B]);
+        if (from >= to) continue;
+        float4 w[K], dw[K], db[K];
+#pragma unroll
+        for (int i = 0; i < K; ++i) {
+            const int v = lane + (i << a.log);
+            w[i] = v < a.nvec ? __ldg(reinterpret_cast<const float4*>(a.weight) + e * a.nvec + v) : make_float4(0.f, 0.f, 0.f, 0.f);
+            dw[i] = db[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+        int q = e * B;
+        for (int p0 = from + warp * per_warp; p0 < to; p0 += step) {
+            const int p = p0 + sub;
+            const bool in = p < to;
+            size_t row = 0;
+            if (in) {
+                while (p >= start[q + 1]) ++q;                    // p < start[(e + 1) * B]
+                const int b = q - e * B;
+                row = (size_t)b * a.seg.N + bounds[b * (E + 1) + e] + (p - start[q]);
+            }
+            const float m = in ? __ldg(a.mean + row) : 0.f, r = in ? __ldg(a.rstd + row) : 0.f;
+            float4 x[K], g[K];
+            load_row<K>(x, a.x, row * a.nvec, lane, a.log, in ? a.nvec : 0, a.type_x);
+            load_row<K>(g, a.dy, row * a.nvec, lane, a.log, in ? a.nvec : 0, a.type_y);
+            float s = 0.f, t = 0.f;
+#pragma unroll
+            for (int i = 0; i < K; ++i) {
+                if (!in || lane + (i << a.log) >= a.nvec) continue;
+                x[i].x = (x[i].x - m) * r; x[i].y = (x[i].y - m) * r; x[i].z = (x[i].z - m) * r; x[i].w = (x[i].w - m) * r;
+                dw[i].x += g[i].x * x[i].x; dw[i].y += g[i].y * x[i].y; dw[i].z += g[i].z * x[i].z; dw[i].w += g[i].w * x[i].w;
+                db[i].x += g[i].x; db[i].y += g[i].y; db[i].z += g[i].z; db[i].w += g[i].w;
+                g[i].x *= w[i].x; g[i].y *= w[i].y; g[i].z *= w[i].z; g[i].w *= w[i].w;
+                s += (g[i].x + g[i].y) + (g[i].z + g[i].w);
+                t += (g[i].x * x[i].x + g[i].y * x[i].y) + (g[i].z * x[i].z + g[i].w * x[i].w);
+            }
+            s = group_sum(s, a.log) * a.inv_c;
+            t = group_sum(t, a.log) * a.inv_c;
+            if (!in) continue;
+#pragma unroll
+            for (int i = 0; i < K; ++i) {
+                const int v = lane + (i << a.log);
+                if (v >= a.nvec) continue;
+                const float4 o = make_float4(r * (g[i].x - s - x[i].x * t), r * (g[i].y - s - x[i].y * t),
+                                             r * (g[i].z - s - x[i].z * t), r * (g[i].w - s - x[i].w * t));
+                store_row4(a.dx, row * a.nvec + v, o, a.type_x);
+            }
+        }
+        // The groups of a warp hold the same columns in the same lanes, then the warps' sums in their order.
+#pragma unroll
+        for (int i = 0; i < K; ++i) {
+            float* f = &dw[i].x;
+            float* h = &db[i].x;
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+                for (int d = lanes; d < 32; d <<= 1) {
+                    f[c] += __shfl_xor_sync(0xFFFFFFFFu, f[c], d);
+                    h[c] += __shfl_xor_sync(0xFFFFFFFFu, h[c], d);
+                }
+            const int v = lane + (i << a.log);
+            if (sub == 0 && v < a.nvec) {
+                sums[(warp * 2 + 0) * a.nvec + v] = dw[i];
+                sums[(warp * 2 + 1) * a.nvec + v] = db[i];
+            }
+        }
+        __syncthreads();
+        float4* part = reinterpret_cast<float4*>(a.part) + (size_t)(blockIdx.x + e) * 2 * a.nvec;
+        for (int v = threadIdx.x; v < 2 * a.nvec; v += kNormThreads) {
+            float4 o = sums[v];
+            for (int k = 1; k < kNormThreads / 32; ++k) {
+                const float4 y = sums[k * 2 * a.nvec + v];
+                o.x += y.x; o.y += y.y; o.z += y.z; o.w += y.w;
+            }
+            part[v] = o;
+        }
+        __syncthreads();
+    }
+}
+
+struct NormSumArgs {
+    RowSegments seg;
+    const float* part;
+    float* dweight;
+    float* dbias;                // or null
+    int ctas, C;                 // of norm_grad_kernel
+};
+
+// dw_e and db_e: the entries of the CTAs that had rows of expert e, in their order; 32 columns per CTA.
+__global__ void __launch_bounds__(kNormThreads) norm_sum_kernel(NormSumArgs a) {
+    constexpr int kWarps = kNormThreads / 32;
+    __shared__ int bounds[kMaxBounds];
+    __shared__ int start[kMaxSegments + 1];
+    __shared__ float sum[kWarps][32];
+    load_bounds(a.seg, bounds);
+    segment_starts(a.seg, bounds, 1, start);
+    const int e = blockIdx.y, B = a.seg.B, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const long long total = start[B * a.seg.E], from = start[e * B], to = start[(e + 1) * B];
+    const int c = blockIdx.x * 32 + lane;                                  // column of [dw | db]
+    float s = 0.f;
+    if (from < to && c < 2 * a.C) {
+        // CTA i has rows total * i / ctas .. total * (i + 1) / ctas - 1: those of the first and of the last row.
+        const int i0 = (int)(((from + 1) * a.ctas - 1) / total), i1 = (int)((to * a.ctas - 1) / total);
+        for (int i = i0 + warp; i <= i1; i += kWarps) {
+            if (total * i / a.ctas == total * (i + 1) / a.ctas) continue;  // more CTAs than rows: it had none
+            s += a.part[(size_t)(i + e) * 2 * a.C + c];
+        }
+    }
+    sum[warp][lane] = s;
+    __syncthreads();
+    if (warp == 0 && c < 2 * a.C) {
+        for (int k = 1; k < kWarps; ++k) s += sum[k][lane];
+        if (c < a.C) a.dweight[e * a.C + c] = s;
+        else if (a.dbias) a.dbias[e * a.C + c - a.C] = s;
+    }
+}
+
+template <template <int> class F, typename... A>
+void by_vectors(int per, const A&... args) {
+    switch (per) {
+        case 1: F<1>::go(args...); break;
+        case 2: F<2>::go(args...); break;
+        case 3: F<3>::go(args...); break;
+        case 4: F<4>::go(args...); break;
+        case 5: F<5>::go(args...); break;
+        case 6: F<6>::go(args...); break;
+        case 7: F<7>::go(args...); break;
+        default: F<8>::go(args...); break;
+    }
+}
+
+template <int K>
+struct Norm {
+    static void go(const NormArgs& a, int ctas, cudaStream_t st) { norm_kernel<K><<<ctas, kNormThreads, 0, st>>>(a); }
+};
+template <int K>
+struct NormGrad {
+    static void go(const NormGradArgs& a, int ctas, size_t shared, cudaStream_t st) {
+        if (shared > 32 * 1024)
+            cudaFuncSetAttribute(norm_grad_kernel<K>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)shared);
+        norm_grad_kernel<K><<<ctas, kNormThreads, shared, st>>>(a);
+    }
+};
+
+int norm_grad_ctas(const emc2_bridge* h) { return 2 * h->num_sms; }
+
+int check_norm(const emc2_bridge* h, int B, int N, int channels, int type_x, int type_y, const void* x, const int32_t* offsets,
+               const float* weight) {
+    if (!h || B < 0 || N < 0 || B > h->cfg.max_batch || N > h->cfg.max_points) return EMC2_ERR_INVALID_ARG;
+    if (channels < 4 || channels > kMaxRowChannels || (channels & 3) || !is_type(type_x) || !is_type(type_y)) return EMC2_ERR_INVALID_ARG;
+    if (!weight || !on_16_bytes(weight) || !on_16_bytes(x)) return EMC2_ERR_INVALID_ARG;
+    if (B > 0 && N > 0 && !x) return EMC2_ERR_INVALID_ARG;
+    if (reinterpret_cast<uintptr_t>(offsets) & 3) return EMC2_ERR_INVALID_ARG;
+    return EMC2_OK;
+}
+
+}  // namespace
+
+size_t norm_scratch_bytes(const emc2_bridge* h, int max_channels) {
+    return (size_t)(norm_grad_ctas(h) + EMC2_MAX_EXPERTS) * 2 * max_channels * sizeof(float);
+}
+
+}  // namespace emc2
+
+using namespace emc2;
+
+extern "C" int emc2_expert_norm(emc2_bridge_t* h, int32_t B, int32_t N, int32_t channels, int32_t type_x, int32_t type_y,
+                                const void* d_x, const int32_t* d_offsets, const float* d_weight, const float* d_bias, float eps,
+                                void* d_y, float* d_mean, float* d_rstd, void* cuda_stream) {
+    const int rc = check_norm(h, B, N, channels, type_x, type_y, d_x, d_offsets, d_weight);
+    if (rc != EMC2_OK) return rc;
+    if (!on_16_bytes(d_bias) || !on_16_bytes(d_y) || !(eps >= 0.0f)) return EMC2_ERR_INVALID_ARG;
+    if (B == 0 || N == 0) return EMC2_OK;
+    if (!d_y || d_y == d_x) return EMC2_ERR_INVALID_ARG;
+    RowsDevice device(h->cfg.device);
+    if (!device.ok) return EMC2_ERR_CUDA;
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    NormArgs a;
+    a.seg = row_segments(h, B, N, d_offsets);
+    a.frame = make_fast_div((uint32_t)N);
+    a.x = d_x; a.weight = d_weight; a.bias = d_bias; a.y = d_y; a.mean = d_mean; a.rstd = d_rstd;
+    a.eps = eps; a.inv_c = 1.0f / (float)channels; a.nvec = channels / 4; a.type_x = type_x; a.type_y = type_y;
+    const RowSplit split = row_split(a.nvec);
+    a.log = split.log;
+    const long long rows = (long long)B * N, per_cta = kNormThreads >> split.log;
+    const int ctas = (int)std::min<long long>((rows + per_cta - 1) / per_cta, 8LL * h->num_sms);
+    LaunchScope ls(h, K_NORM, st);
+    by_vectors<Norm>(split.per, a, ctas, st);
+    return check_cuda(h, cudaGetLastError());
+}
+
+extern "C" int emc2_expert_norm_grad(emc2_bridge_t* h, int32_t B, int32_t N, int32_t channels, int32_t type_x, int32_t type_y,
+                                     const void* d_x, const int32_t* d_offsets, const float* d_weight, const float* d_mean,
+                                     const float* d_rstd, const void* d_grad_y, void* d_grad_x, float* d_grad_weight,
+                                     float* d_grad_bias, void* cuda_stream) {
+    const int rc = check_norm(h, B, N, channels, type_x, type_y, d_x, d_offsets, d_weight);
+    if (rc != EMC2_OK) return rc;
+    if (!d_grad_weight || !on_16_bytes(d_grad_y) || !on_16_bytes(d_grad_x)) return EMC2_ERR_INVALID_ARG;
+    const bool empty = B == 0 || N == 0;
+    if (!empty && (!d_mean || !d_rstd || !d_grad_y || !d_grad_x || d_grad_x == d_x || d_grad_x == d_grad_y)) return EMC2_ERR_INVALID_ARG;
+    if (!h->rows_scratch.slab || channels > h->rows_scratch.max_channels) return EMC2_ERR_TOO_LARGE;
+    RowsDevice device(h->cfg.device);
+    if (!device.ok) return EMC2_ERR_CUDA;
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    NormSumArgs t;
+    t.seg = row_segments(h, B, N, d_offsets);
+    if (empty) {
+        const size_t bytes = (size_t)t.seg.E * channels * sizeof(float);
+        cudaError_t e = cudaMemsetAsync(d_grad_weight, 0, bytes, st);
+        if (e == cudaSuccess && d_grad_bias) e = cudaMemsetAsync(d_grad_bias, 0, bytes, st);
+        return check_cuda(h, e);
+    }
+    NormGradArgs a;
+    a.seg = t.seg;
+    a.x = d_x; a.dy = d_grad_y; a.weight = d_weight; a.mean = d_mean; a.rstd = d_rstd; a.dx = d_grad_x;
+    a.part = static_cast<float*>(h->rows_scratch.slab);
+    a.inv_c = 1.0f / (float)channels; a.nvec = channels / 4; a.type_x = type_x; a.type_y = type_y;
+    const RowSplit split = row_split(a.nvec);
+    a.log = split.log;
+    const long long rows = (long long)B * N, per_cta = kNormThreads >> split.log;
+    t.ctas = (int)std::min<long long>((rows + per_cta - 1) / per_cta, norm_grad_ctas(h));
+    t.part = a.part; t.dweight = d_grad_weight; t.dbias = d_grad_bias; t.C = channels;
+    {
+        LaunchScope ls(h, K_NORM_GRAD, st);
+        by_vectors<NormGrad>(split.per, a, t.ctas, (size_t)(kNormThreads / 32) * 2 * a.nvec * sizeof(float4), st);
+    }
+    {
+        LaunchScope ls(h, K_NORM_SUM, st);
+        norm_sum_kernel<<<dim3((2 * channels + 31) / 32, t.seg.E), kNormThreads, 0, st>>>(t);
+    }
+    return check_cuda(h, cudaGetLastError());
+}
