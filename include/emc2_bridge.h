@@ -52,8 +52,9 @@ typedef enum {
     EMC2_ERR_BAD_CONFIG = -2,  /* emc2_config_t rejected by emc2_bridge_create */
     EMC2_ERR_CUDA = -3,        /* a CUDA runtime call failed; see emc2_bridge_last_cuda_error */
     EMC2_ERR_CAPACITY = -4,    /* more unique voxels than capacity[s] (device-detected, sticky) */
-    EMC2_ERR_TIMEOUT = -5,     /* reserved: a bounded device-side wait gave up.  No kernel of this library
-                                  waits for another CTA, so it is never returned at present */
+    EMC2_ERR_TIMEOUT = -5,     /* from emc2_bridge_status: a bounded device-side wait gave up, and the outputs of that
+                                  call are void.  Kernels of this library wait for their own copies and products
+                                  only, never for another CTA, so it is not expected */
     EMC2_ERR_INTERNAL = -6,    /* from emc2_bridge_status: a call found the handle's scratch in use, or cells
                                   marked that none of its points lies in (two calls on one handle at once);
                                   that call's voxel outputs are void and the handle should be destroyed.  Not
@@ -361,6 +362,27 @@ int emc2_expert_norm_grad(emc2_bridge_t* bridge, int32_t B, int32_t N, int32_t c
                           const void* d_x, const int32_t* d_offsets, const float* d_weight, const float* d_mean,
                           const float* d_rstd, const void* d_grad_y, void* d_grad_x, float* d_grad_weight, float* d_grad_bias,
                           void* cuda_stream);
+
+/* Gated feed-forward block with weights per expert: with g = x w_gate[e]^T and u = x w_up[e]^T,
+ * d_y = (act(g) * u) w_down[e]^T per row.  act: SiLU, g / (1 + exp(-g)), or GELU, g Phi(g) with the normal distribution.
+ *   d_x, d_y       type [B, N, channels], type EMC2_BF16 or EMC2_F16 (emc2_expert_norm brings fp32 rows to either)
+ *   d_w_gate, d_w_up  type [E, hidden, channels]     d_w_down  type [E, channels, hidden]
+ * channels and hidden are multiples of 8, channels up to 256, hidden up to 8192.  Products are summed in fp32; act(g) * u is
+ * rounded to the type before the last product (in EMC2_F16 it has to stay below 65504), the result once. */
+typedef enum { EMC2_ACT_SILU = 0, EMC2_ACT_GELU = 1 } emc2_act_t;
+int emc2_expert_ffn(emc2_bridge_t* bridge, int32_t B, int32_t N, int32_t channels, int32_t hidden, int32_t type, int32_t act,
+                    const void* d_x, const int32_t* d_offsets, const void* d_w_gate, const void* d_w_up, const void* d_w_down,
+                    void* d_y, void* cuda_stream);
+
+/* Its gradients (scratch, reserved for that many channels and hidden units) for d_grad_y, type [B, N, channels]:
+ *   d_grad_x  type [B, N, channels]     d_grad_gate, d_grad_up  type [E, hidden, channels]
+ *   d_grad_down  type [E, channels, hidden]
+ * The gradients at g and u, and act(g) * u, are rounded to the type before their products; sums over the rows are held in
+ * fp32 and rounded once. */
+int emc2_expert_ffn_grad(emc2_bridge_t* bridge, int32_t B, int32_t N, int32_t channels, int32_t hidden, int32_t type, int32_t act,
+                         const void* d_x, const int32_t* d_offsets, const void* d_w_gate, const void* d_w_up,
+                         const void* d_w_down, const void* d_grad_y, void* d_grad_x, void* d_grad_gate, void* d_grad_up,
+                         void* d_grad_down, void* cuda_stream);
 
 /* Turns the handle's own streams in emc2_bridge_run off (0) or on (non-zero, the default).  Off, every
  * kernel of the call is enqueued on `cuda_stream` itself, one after another: for callers that

@@ -38,10 +38,13 @@ ABI_SYMBOLS = (
     "emc2_voxel_image", "emc2_voxel_image_sampled", "emc2_occlusion", "emc2_rulebook",
     "emc2_bridge_set_tuning", "emc2_bridge_profile_timeline", "emc2_voxel_image_pooled",
     "emc2_rows_reserve", "emc2_row_lookup", "emc2_row_lookup_grad", "emc2_expert_norm", "emc2_expert_norm_grad",
+    "emc2_expert_ffn", "emc2_expert_ffn_grad",
 )
 
 # emc2_type_t
 ROW_TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+# emc2_act_t
+ACTIVATIONS = {"silu": 0, "gelu": 1}
 
 # emc2_tuning_t
 TUNE_ROW_STORE = 0
@@ -116,6 +119,8 @@ def load_library() -> ctypes.CDLL:
     lib.emc2_row_lookup_grad.argtypes = [vp, i32, i32, i32, i32, vp, vp, f32, vp, vp]
     lib.emc2_expert_norm.argtypes = [vp] + [i32] * 5 + [vp] * 4 + [f32] + [vp] * 4
     lib.emc2_expert_norm_grad.argtypes = [vp] + [i32] * 5 + [vp] * 10
+    lib.emc2_expert_ffn.argtypes = [vp] + [i32] * 6 + [vp] * 7
+    lib.emc2_expert_ffn_grad.argtypes = [vp] + [i32] * 6 + [vp] * 11
     lib.emc2_bridge_destroy.argtypes = [vp]
     lib.emc2_status_string.argtypes = [ctypes.c_int]
     lib.emc2_status_string.restype = ctypes.c_char_p
@@ -566,6 +571,51 @@ class Bridge:
                                             grad_y.data_ptr(), out["grad_x"].data_ptr(), out["grad_weight"].data_ptr(),
                                             _ptr(out.get("grad_bias")), self._stream())
         self._raise(rc, "emc2_expert_norm_grad")
+        return out
+
+    def _check_ffn(self, x, offsets, w_gate, w_up, w_down, act):
+        B, N, C = x.shape
+        E = self._experts(offsets, B)
+        H = w_gate.shape[1]
+        if act not in ACTIVATIONS:
+            raise ValueError(f"act: expected one of {sorted(ACTIVATIONS)}, got {act!r}")
+        if x.dtype not in (torch.bfloat16, torch.float16):
+            raise ValueError(f"x: expected bfloat16 or float16, got {x.dtype}")
+        _check(x, x.dtype, (B, N, C), "x", self.device)
+        _check(w_gate, x.dtype, (E, H, C), "w_gate", self.device)
+        _check(w_up, x.dtype, (E, H, C), "w_up", self.device)
+        _check(w_down, x.dtype, (E, C, H), "w_down", self.device)
+        return B, N, C, H
+
+    def expert_ffn(self, x: torch.Tensor, offsets: Optional[torch.Tensor], w_gate: torch.Tensor, w_up: torch.Tensor,
+                   w_down: torch.Tensor, act: str = "silu", out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """emc2_expert_ffn: ``(act(x w_gate^T) * (x w_up^T)) w_down^T`` with the weights of each row's expert.  Rows of no
+        expert are left as they are in ``out``; without ``out`` they are unspecified."""
+        B, N, C, H = self._check_ffn(x, offsets, w_gate, w_up, w_down, act)
+        if out is None:
+            out = torch.empty_like(x)
+        _check(out, x.dtype, (B, N, C), "out", self.device)
+        rc = self.lib.emc2_expert_ffn(self._h, B, N, C, H, ROW_TYPES[x.dtype], ACTIVATIONS[act], x.data_ptr(), _ptr(offsets),
+                                      w_gate.data_ptr(), w_up.data_ptr(), w_down.data_ptr(), out.data_ptr(), self._stream())
+        self._raise(rc, "emc2_expert_ffn")
+        return out
+
+    def expert_ffn_grad(self, x: torch.Tensor, offsets: Optional[torch.Tensor], w_gate: torch.Tensor, w_up: torch.Tensor,
+                        w_down: torch.Tensor, grad_y: torch.Tensor, act: str = "silu",
+                        out: Optional[Dict[str, torch.Tensor]] = None) -> Dict[str, torch.Tensor]:
+        """emc2_expert_ffn_grad: ``grad_x``, ``grad_gate``, ``grad_up``, ``grad_down`` (needs :meth:`reserve_rows`)."""
+        B, N, C, H = self._check_ffn(x, offsets, w_gate, w_up, w_down, act)
+        _check(grad_y, x.dtype, (B, N, C), "grad_y", self.device)
+        if out is None:
+            out = {"grad_x": torch.empty_like(x), "grad_gate": torch.empty_like(w_gate), "grad_up": torch.empty_like(w_up),
+                   "grad_down": torch.empty_like(w_down)}
+        for k, like in (("grad_x", x), ("grad_gate", w_gate), ("grad_up", w_up), ("grad_down", w_down)):
+            _check(out[k], x.dtype, like.shape, k, self.device)
+        rc = self.lib.emc2_expert_ffn_grad(self._h, B, N, C, H, ROW_TYPES[x.dtype], ACTIVATIONS[act], x.data_ptr(), _ptr(offsets),
+                                           w_gate.data_ptr(), w_up.data_ptr(), w_down.data_ptr(), grad_y.data_ptr(),
+                                           out["grad_x"].data_ptr(), out["grad_gate"].data_ptr(), out["grad_up"].data_ptr(),
+                                           out["grad_down"].data_ptr(), self._stream())
+        self._raise(rc, "emc2_expert_ffn_grad")
         return out
 
     def set_overlap(self, enable: bool) -> None:

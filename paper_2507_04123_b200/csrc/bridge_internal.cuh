@@ -78,6 +78,10 @@ enum KernelKind {
     K_NORM,
     K_NORM_GRAD,
     K_NORM_SUM,
+    K_FFN,
+    K_FFN_GRAD_X,
+    K_FFN_GRAD_W,
+    K_FFN_SUM,
     K_KINDS
 };
 
@@ -274,6 +278,7 @@ int radix_sort(emc2_bridge* h, int kind, int n, int bits, uint32_t* const keys[2
 // Scratch that the operators on rows of up to max_channels channels need on this handle.
 size_t norm_scratch_bytes(const emc2_bridge* h, int max_channels);
 size_t lookup_scratch_bytes(const emc2_bridge* h, int max_channels);
+size_t ffn_scratch_bytes(const emc2_bridge* h, int max_channels, int max_hidden);
 int launch_dedup_arm(emc2_bridge* h, int s, int design, int B, int N, const float* d_points, int capacity,
                      int32_t* d_num_voxels, cudaStream_t st);
 int launch_project_gather(emc2_bridge* h, int B, int N, const float* d_points, const float* d_proj,

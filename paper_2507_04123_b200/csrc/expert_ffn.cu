@@ -1,0 +1,835 @@
+// Gated feed-forward block on dispatched rows, with weights per expert, and its gradients.
+//
+//   g = x Wg^T, u = x Wu^T, h = act(g) u, y = h Wd^T                       rows [., C], hidden width H
+//   dh = dy Wd, dg = dh u act'(g), du = dh act(g), dx = dg Wg + du Wu
+//   dWg = dg^T x, dWu = du^T x, dWd = dy^T h                               sums over the expert's rows
+//
+// All products run on the tensor cores (tcgen05, fp32 accumulators in TMEM).  Nothing of width H reaches device memory:
+// tiles of 128 rows stay in shared memory while the hidden units pass by in chunks, whose weights are copied in beside the
+// products.  What lies between the two products of a chunk (h, or dg and du) is rounded to the rows' type, as the tensor
+// cores take it; all sums are held in fp32, results are rounded once.
+//
+// Three kinds of warps pass tiles along with mbarriers: one thread copies (tiled bulk copies), one issues products, eight
+// warps apply the activation from TMEM to shared memory, four per accumulator so that one is filled while the other is read.
+#include <algorithm>
+
+#include "rows.cuh"
+#include "umma.cuh"
+
+namespace emc2 {
+namespace {
+
+constexpr int kTileRows = 128;
+constexpr int kBlockBytes = kTileRows * 128;     // a tile's 64 columns
+constexpr int kCopyWarp = 8, kProductWarp = 9, kFixWarp = 10;
+constexpr int kRowThreads = 320, kWeightThreads = 352;
+constexpr int kTmemColumns = 512;
+constexpr int kMaxFfnChannels = 256, kMaxFfnHidden = 8192;
+constexpr int kMaxStages = 4;
+constexpr size_t kMaxShared = 232448 - 1024;     // what a CTA can have, less the kernels' static part
+
+enum { FORWARD = 0, GRAD_X = 1 };
+
+// ---------------------------------------------------------------- a walk over the tiles, expert by expert
+// Tiles hold up to 128 * NT rows of one (expert, frame) segment.
+struct TileWalk {
+    int q;              // segment e * B + b
+    int row;            // first row of the tile in [B * N]
+    int left;           // rows of the segment from there on
+};
+
+__device__ __forceinline__ void segment_rows(const RowSegments& s, int q, int& lo, int& hi) {
+    const int e = q / s.B, b = q - e * s.B;
+    if (!s.offsets) { lo = 0; hi = s.N; return; }
+    const int32_t* of = s.offsets + b * (s.E + 1);
+    int at = 0;
+    for (int k = 0; k <= e; ++k) at = max(at, min(__ldg(of + k), s.N));
+    lo = at;
+    hi = max(at, min(__ldg(of + e + 1), s.N));
+}
+
+// From the tables of load_bounds and segment_starts.
+__device__ __forceinline__ TileWalk tile_at(const RowSegments& s, const int* bounds, const int* start, int tile, int tile_rows) {
+    TileWalk w;
+    w.q = segment_of(start, s.B * s.E, tile);
+    const int e = w.q / s.B, b = w.q - e * s.B, skip = (tile - start[w.q]) * tile_rows;
+    const int* of = bounds + b * (s.E + 1) + e;
+    w.row = b * s.N + of[0] + skip;
+    w.left = of[1] - of[0] - skip;
+    return w;
+}
+
+__device__ __forceinline__ void next_tile(const RowSegments& s, TileWalk& w, int tile_rows) {
+    w.row += tile_rows;
+    w.left -= tile_rows;
+    while (w.left <= 0 && ++w.q < s.B * s.E) {
+        int lo, hi;
+        segment_rows(s, w.q, lo, hi);
+        w.row = (w.q % s.B) * s.N + lo;
+        w.left = hi - lo;
+    }
+}
+
+// ---------------------------------------------------------------- activations
+template <int ACT>
+__device__ __forceinline__ float activation(float g) {
+    if (ACT == EMC2_ACT_SILU) return __fdividef(g, 1.0f + __expf(-g));
+    return 0.5f * g * (1.0f + erff(g * 0.70710678118654752f));
+}
+template <int ACT>
+__device__ __forceinline__ void activation_grad(float g, float& a, float& da) {
+    if (ACT == EMC2_ACT_SILU) {
+        const float s = __fdividef(1.0f, 1.0f + __expf(-g));
+        a = g * s;
+        da = s + a * (1.0f - s);
+    } else {
+        const float phi = 0.5f + 0.5f * erff(g * 0.70710678118654752f);
+        a = g * phi;
+        da = phi + g * 0.39894228040143268f * __expf(-0.5f * g * g);
+    }
+}
+
+template <bool BF16>
+__device__ __forceinline__ uint32_t pack(float a, float b) { return as_halves(a, b, BF16 ? EMC2_BF16 : EMC2_F16); }
+
+__device__ __forceinline__ void store_shared(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+
+// 16-byte piece `piece` of row r in a block of rows of HC 16-bit values, with the swizzle that its width has.
+template <int HC>
+__device__ __forceinline__ uint32_t swizzled(int r, int piece) {
+    return HC == 64 ? r * 128 + ((piece ^ (r & 7)) << 4) : r * 64 + ((piece ^ ((r >> 1) & 3)) << 4);
+}
+
+// Columns c .. c + 7 of a chunk, at j of the arrays: the values that go on to the second product, a 16-byte piece of row r.
+template <int MODE, int HC, int ACT, bool BF16, bool WITH_H, int W>
+__device__ __forceinline__ void hidden8(const uint32_t (&g)[W], const uint32_t (&u)[W], const uint32_t (&dh)[W], int j0, uint32_t to, int r, int c) {
+    constexpr uint32_t kBlock = kTileRows * HC * 2;
+    uint32_t p[4], q[4], t[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int j = j0 + 2 * i;
+        const float g0 = __uint_as_float(g[j]), g1 = __uint_as_float(g[j + 1]), u0 = __uint_as_float(u[j]), u1 = __uint_as_float(u[j + 1]);
+        if (MODE == FORWARD) {
+            p[i] = pack<BF16>(activation<ACT>(g0) * u0, activation<ACT>(g1) * u1);
+        } else {
+            const float d0 = __uint_as_float(dh[j]), d1 = __uint_as_float(dh[j + 1]);
+            float a0, a1, da0, da1;
+            activation_grad<ACT>(g0, a0, da0);
+            activation_grad<ACT>(g1, a1, da1);
+            p[i] = pack<BF16>(d0 * u0 * da0, d1 * u1 * da1);
+            q[i] = pack<BF16>(d0 * a0, d1 * a1);
+            if (WITH_H) t[i] = pack<BF16>(a0 * u0, a1 * u1);
+        }
+    }
+    const uint32_t at = to + swizzled<HC>(r, c / 8);
+    store_shared(at, p[0], p[1], p[2], p[3]);
+    if (MODE == GRAD_X) {
+        store_shared(at + kBlock, q[0], q[1], q[2], q[3]);
+        if (WITH_H) store_shared(at + 2 * kBlock, t[0], t[1], t[2], t[3]);
+    }
+}
+
+// The activation of one chunk of one tile: accumulators at `acc` (g, u and, for the gradients, dh, HC columns each) of
+// the warp's 32 rows into the blocks at `to`.  Eight columns at a time where more would not fit in the registers.
+template <int MODE, int HC, int ACT, bool BF16, bool WITH_H>
+__device__ __forceinline__ void hidden_chunk(uint32_t acc, uint32_t to, int r) {
+    constexpr int W = MODE == GRAD_X && ACT == EMC2_ACT_GELU ? 8 : 16;
+    uint32_t g[W], u[W], dh[W];
+#pragma unroll
+    for (int c = 0; c < HC; c += W) {
+        tmem_load(g, acc + c);
+        tmem_load(u, acc + HC + c);
+        if (MODE == GRAD_X) tmem_load(dh, acc + 2 * HC + c);
+        tmem_wait(g);
+        tmem_wait(u);
+        if (MODE == GRAD_X) tmem_wait(dh);
+#pragma unroll
+        for (int j = 0; j < W; j += 8) hidden8<MODE, HC, ACT, BF16, WITH_H>(g, u, dh, j, to, r, c + j);
+    }
+}
+
+// ---------------------------------------------------------------- rows: y, or dx
+struct RowArgs {
+    RowSegments seg;
+    void* out;
+    int C, H, c16, blocks, chunks;          // c16: C rounded up to 16; blocks of 64 columns; chunks of HC hidden units
+    int xn, gn, dn, hn;                     // stages of the rows' tiles, of Wg and Wu, of Wd, of the hidden values
+    uint32_t off_g, off_d, off_h;           // in the dynamic shared memory, behind the rows' tiles
+    uint32_t x_bytes, g_bytes, d_bytes, h_bytes;   // of a stage
+};
+struct Maps {
+    CUtensorMap x, dy, gate, up, down;
+};
+
+template <int MODE, int HC, int NT, int ACT, bool BF16>
+__global__ void __launch_bounds__(kRowThreads, 1) ffn_rows_kernel(const RowArgs a, const __grid_constant__ Maps maps) {
+    constexpr int kAcc = (MODE == FORWARD ? 2 : 3) * HC;               // columns of an accumulator
+    constexpr int kHidBlock = kTileRows * HC * 2;
+    extern __shared__ uint8_t dynamic[];
+    __shared__ __align__(8) uint64_t bars[4 * kMaxStages * 2 + 16];
+    __shared__ uint32_t tmem_at;
+    __shared__ int gave_up;
+    const uint32_t base = (smem_u32(dynamic) + 1023u) & ~1023u;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t bar0 = smem_u32(bars);
+    auto x_full = [&](int s) { return bar0 + 8 * s; };
+    auto x_empty = [&](int s) { return bar0 + 8 * (4 + s); };
+    auto g_full = [&](int s) { return bar0 + 8 * (8 + s); };
+    auto g_empty = [&](int s) { return bar0 + 8 * (12 + s); };
+    auto d_full = [&](int s) { return bar0 + 8 * (16 + s); };
+    auto d_empty = [&](int s) { return bar0 + 8 * (20 + s); };
+    auto acc_full = [&](int s) { return bar0 + 8 * (24 + s); };
+    auto acc_empty = [&](int s) { return bar0 + 8 * (26 + s); };
+    auto hid_full = [&](int s) { return bar0 + 8 * (28 + s); };
+    auto hid_empty = [&](int s) { return bar0 + 8 * (30 + s); };
+    auto out_full = [&](int t) { return bar0 + 8 * (32 + t); };
+    auto out_empty = [&](int t) { return bar0 + 8 * (34 + t); };
+
+    // The tables lie where the tiles come later.
+    int* bounds = reinterpret_cast<int*>(dynamic + (base - smem_u32(dynamic)));
+    int* start = bounds + kMaxBounds;
+    load_bounds(a.seg, bounds);
+    segment_starts(a.seg, bounds, kTileRows * NT, start);
+    const int total = start[a.seg.B * a.seg.E];
+    const int lo = (int)((long long)total * blockIdx.x / gridDim.x), hi = (int)((long long)total * (blockIdx.x + 1) / gridDim.x);
+    if (lo >= hi) return;
+    TileWalk walk = tile_at(a.seg, bounds, start, lo, kTileRows * NT);
+    if (threadIdx.x == 0) {
+        gave_up = 0;
+        for (int s = 0; s < kMaxStages; ++s) {
+            bar_init(x_full(s), 1); bar_init(x_empty(s), 1);
+            bar_init(g_full(s), 1); bar_init(g_empty(s), 1);
+            bar_init(d_full(s), 1); bar_init(d_empty(s), 1);
+        }
+        for (int s = 0; s < 2; ++s) {
+            bar_init(acc_full(s), 1); bar_init(acc_empty(s), 128);
+            bar_init(hid_full(s), 128); bar_init(hid_empty(s), 1);
+            bar_init(out_full(s), 1); bar_init(out_empty(s), NT == 2 ? 128 : 256);
+        }
+        fence_bar_init();
+    }
+    if (warp == 0) tmem_alloc(smem_u32(&tmem_at), kTmemColumns);
+    fence_async_shared();
+    tmem_fence_before();
+    __syncthreads();
+    tmem_fence_after();
+    const uint32_t tmem = tmem_at;
+    const uint32_t acc0 = tmem + NT * a.c16;                           // behind the output's accumulators
+    const int items = hi - lo, units = items * a.chunks * NT;
+#define WAIT(bar, parity) bar_wait(bar, parity, &gave_up, a.seg.status)
+
+    if (warp == kCopyWarp) {
+        if (lane == 0) {
+            int xc = 0, wc = 0;                                        // tiles and chunks copied so far
+            for (int it = 0; it < items; ++it, next_tile(a.seg, walk, kTileRows * NT)) {
+                const int e = walk.q / a.seg.B;
+                bool ok = true;
+                for (int t = 0; ok && t < NT; ++t, ++xc) {
+                    const int s = xc % a.xn;
+                    if (!(ok = WAIT(x_empty(s), (xc / a.xn & 1) ^ 1))) break;
+                    bar_expect(x_full(s), a.x_bytes);
+                    const uint32_t to = base + s * a.x_bytes;
+                    for (int b = 0; b < a.blocks; ++b) {
+                        copy_tile(to + b * kBlockBytes, &maps.x, 64 * b, walk.row + t * kTileRows, x_full(s));
+                        if (MODE == GRAD_X) copy_tile(to + (a.blocks + b) * kBlockBytes, &maps.dy, 64 * b, walk.row + t * kTileRows, x_full(s));
+                    }
+                }
+                for (int j = 0; ok && j < a.chunks; ++j, ++wc) {
+                    const int s = wc % a.gn, d = wc % a.dn;
+                    if (!(ok = WAIT(g_empty(s), (wc / a.gn & 1) ^ 1))) break;
+                    bar_expect(g_full(s), a.g_bytes);
+                    for (int b = 0; b < a.blocks; ++b) {
+                        const uint32_t to = base + a.off_g + s * a.g_bytes + b * (2 * HC * 128);
+                        copy_tile(to, &maps.gate, 64 * b, j * HC, e, g_full(s));
+                        copy_tile(to + HC * 128, &maps.up, 64 * b, j * HC, e, g_full(s));
+                    }
+                    if (!(ok = WAIT(d_empty(d), (wc / a.dn & 1) ^ 1))) break;
+                    bar_expect(d_full(d), a.d_bytes);
+                    copy_tile(base + a.off_d + d * a.d_bytes, &maps.down, j * HC, 0, e, d_full(d));
+                }
+                if (!ok) break;
+            }
+        }
+    } else if (warp == kProductWarp) {
+        if (lane == 0) {
+            const uint32_t kind_gu = product_kind(2 * HC, BF16, false, false), kind_dh = product_kind(HC, BF16, false, true);
+            const uint32_t kind_out = product_kind(a.c16, BF16, false, MODE == GRAD_X);
+            int item = 0, j = 0, t = 0, pitem = 0, pj = 0, pt = 0;
+            // Unit n is chunk j of tile t of an item; the second product of a unit follows the first one of the next.
+            for (int n = 0; n <= units; ++n) {
+                if (n < units) {
+                    const int xc = item * NT + t, xs = xc % a.xn, wc = item * a.chunks + j, gs = wc % a.gn, ds = wc % a.dn;
+                    if (t == 0 && !WAIT(g_full(gs), wc / a.gn & 1)) break;
+                    if (MODE == GRAD_X && !WAIT(d_full(ds), wc / a.dn & 1)) break;
+                    if (j == 0 && !WAIT(x_full(xs), xc / a.xn & 1)) break;
+                    if (!WAIT(acc_empty(n & 1), (n >> 1 & 1) ^ 1)) break;
+                    tmem_fence_after();
+                    const uint32_t d = acc0 + (n & 1) * kAcc, x = base + xs * a.x_bytes, w = base + a.off_g + gs * a.g_bytes;
+                    for (int k = 0; k < a.c16 / 16; ++k)
+                        product(d, operand(x + (k >> 2) * kBlockBytes + (k & 3) * 32, 128, 0),
+                                operand(w + (k >> 2) * (2 * HC * 128) + (k & 3) * 32, 128, 0), kind_gu, k > 0);
+                    if (MODE == GRAD_X) {
+                        const uint32_t dy = x + a.blocks * kBlockBytes, wd = base + a.off_d + ds * a.d_bytes;
+                        for (int k = 0; k < a.c16 / 16; ++k)
+                            product(d + 2 * HC, operand(dy + (k >> 2) * kBlockBytes + (k & 3) * 32, 128, 0),
+                                    operand(wd + k * 16 * HC * 2, HC * 2, 0), kind_dh, k > 0);
+                    }
+                    products_done(acc_full(n & 1));
+                    if (MODE == FORWARD && t == NT - 1) products_done(g_empty(gs));
+                    if (MODE == GRAD_X) products_done(d_empty(ds));
+                    if (j == a.chunks - 1) products_done(x_empty(xs));
+                    if (++t == NT) { t = 0; if (++j == a.chunks) { j = 0; ++item; } }
+                }
+                if (n > 0) {
+                    const int v = n - 1, hs = v % a.hn, wc = pitem * a.chunks + pj, gs = wc % a.gn, ds = wc % a.dn;
+                    if (!WAIT(hid_full(hs), v / a.hn & 1)) break;
+                    if (pj == 0 && !WAIT(out_empty(pt), (pitem & 1) ^ 1)) break;
+                    if (MODE == FORWARD && pt == 0 && !WAIT(d_full(ds), wc / a.dn & 1)) break;
+                    tmem_fence_after();
+                    const uint32_t d = tmem + pt * a.c16, hid = base + a.off_h + hs * a.h_bytes;
+                    if (MODE == FORWARD) {
+                        const uint32_t wd = base + a.off_d + ds * a.d_bytes;
+                        for (int k = 0; k < HC / 16; ++k)
+                            product(d, operand(hid + k * 32, HC * 2, 0), operand(wd + k * 32, HC * 2, 0), kind_out, pj > 0 || k > 0);
+                    } else {
+                        const uint32_t w = base + a.off_g + gs * a.g_bytes;
+                        for (int k = 0; k < 2 * HC / 16; ++k)
+                            product(d, operand(hid + k / (HC / 16) * kHidBlock + k % (HC / 16) * 32, HC * 2, 0),
+                                    operand(w + k * 16 * 128, 128, 2 * HC * 128), kind_out, pj > 0 || k > 0);
+                    }
+                    products_done(hid_empty(hs));
+                    if (MODE == FORWARD && pt == NT - 1) products_done(d_empty(ds));
+                    if (MODE == GRAD_X) products_done(g_empty(gs));
+                    if (pj == a.chunks - 1) products_done(out_full(pt));
+                    if (++pt == NT) { pt = 0; if (++pj == a.chunks) { pj = 0; ++pitem; } }
+                }
+            }
+        }
+    } else {
+        const int group = warp >> 2, quarter = warp & 3, r = quarter * 32 + lane;
+        const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
+        bool ok = true;
+        int n = 0;
+        for (int it = 0; ok && it < items; ++it, next_tile(a.seg, walk, kTileRows * NT)) {
+            for (int k = 0; ok && k < a.chunks * NT; ++k, ++n) {
+                if ((n & 1) != group) continue;
+                const int hs = n % a.hn;
+                if (!(ok = WAIT(acc_full(group), n >> 1 & 1))) break;
+                if (!(ok = WAIT(hid_empty(hs), (n / a.hn & 1) ^ 1))) break;
+                tmem_fence_after();
+                hidden_chunk<MODE, HC, ACT, BF16, false>(acc0 + group * kAcc + lanes, base + a.off_h + hs * a.h_bytes, r);
+                tmem_fence_before();
+                bar_arrive(acc_empty(group));
+                fence_async_shared();
+                bar_arrive(hid_full(hs));
+            }
+            if (!ok) break;
+            const int t = NT == 2 ? group : 0;
+            if (!(ok = WAIT(out_full(t), it & 1))) break;
+            tmem_fence_after();
+            const bool mine = t * kTileRows + r < walk.left;
+            uint16_t* to = static_cast<uint16_t*>(a.out) + (size_t)(walk.row + t * kTileRows + r) * a.C;
+            for (int c = NT == 2 ? 0 : 16 * group; c < a.c16; c += NT == 2 ? 16 : 32) {
+                uint32_t v[16];
+                tmem_load(v, tmem + t * a.c16 + c + lanes);
+                tmem_wait(v);
+#pragma unroll
+                for (int k = 0; k < 16; k += 8)
+                    if (mine && c + k < a.C)
+                        *reinterpret_cast<uint4*>(to + c + k) = make_uint4(
+                            pack<BF16>(__uint_as_float(v[k]), __uint_as_float(v[k + 1])), pack<BF16>(__uint_as_float(v[k + 2]), __uint_as_float(v[k + 3])),
+                            pack<BF16>(__uint_as_float(v[k + 4]), __uint_as_float(v[k + 5])), pack<BF16>(__uint_as_float(v[k + 6]), __uint_as_float(v[k + 7])));
+            }
+            tmem_fence_before();
+            bar_arrive(out_empty(t));
+        }
+    }
+    __syncwarp();
+    leave_after_timeout(&gave_up);
+    tmem_fence_before();
+    __syncthreads();
+    tmem_fence_after();
+    if (warp == 0) tmem_free(tmem, kTmemColumns);
+}
+
+// ---------------------------------------------------------------- weights: dWg, dWu, dWd
+constexpr int kSlice = 32;                  // hidden units whose weights a CTA holds
+
+struct WeightArgs {
+    RowSegments seg;
+    float* part;                            // [ranges + E][slices][3 * kSlice][C]
+    int C, H, c16, blocks, slices, ranges;
+    int xn, hn;
+    uint32_t off_w, off_h;
+    uint32_t x_bytes, w_bytes, h_bytes;
+};
+
+// Zeros in rows `rows` .. 127 of the blocks of a tile (one warp): they belong to other experts, and whatever they hold,
+// infinities and NaN too, must not reach the sums.
+__device__ __forceinline__ void clear_rows(uint32_t tile, int blocks, int rows, int lane) {
+    const int pieces = (kTileRows - rows) * 8;
+    for (int b = 0; b < blocks; ++b)
+        for (int i = lane; i < pieces; i += 32) store_shared(tile + b * kBlockBytes + rows * 128 + i * 16, 0u, 0u, 0u, 0u);
+}
+
+// A unit of work is a slice of hidden units and a range of the tiles, with accumulators for the three gradients of the
+// slice, [C, kSlice] each (the channels in the lanes).  All slices of a range are taken at about the same time, so that its
+// tiles are read from device memory once.  A range that meets several experts has a part of the result for each: entry
+// r + e of `part`, which along the run of all tiles no other pair of range and expert has.
+template <int ACT, bool BF16>
+__global__ void __launch_bounds__(kWeightThreads, 1) ffn_weights_kernel(const WeightArgs a, const __grid_constant__ Maps maps) {
+    constexpr int HC = kSlice, kAcc = 3 * HC, kHidBlock = kTileRows * HC * 2;
+    extern __shared__ uint8_t dynamic[];
+    __shared__ __align__(8) uint64_t bars[32];
+    __shared__ int bounds[kMaxBounds];
+    __shared__ int start[kMaxSegments + 1];
+    __shared__ uint32_t tmem_at;
+    __shared__ int gave_up;
+    const uint32_t base = (smem_u32(dynamic) + 1023u) & ~1023u;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t bar0 = smem_u32(bars);
+    auto x_land = [&](int s) { return bar0 + 8 * s; };
+    auto x_full = [&](int s) { return bar0 + 8 * (4 + s); };
+    auto x_empty = [&](int s) { return bar0 + 8 * (8 + s); };
+    auto acc_full = [&](int s) { return bar0 + 8 * (12 + s); };
+    auto acc_empty = [&](int s) { return bar0 + 8 * (14 + s); };
+    auto hid_full = [&](int s) { return bar0 + 8 * (16 + s); };
+    auto hid_empty = [&](int s) { return bar0 + 8 * (18 + s); };
+    const uint32_t w_full = bar0 + 8 * 20, w_empty = bar0 + 8 * 21, out_full = bar0 + 8 * 22, out_empty = bar0 + 8 * 23;
+
+    load_bounds(a.seg, bounds);
+    segment_starts(a.seg, bounds, kTileRows, start);
+    const int total = start[a.seg.B * a.seg.E], work = a.ranges * a.slices;
+    if (total == 0) return;
+    if (threadIdx.x == 0) {
+        gave_up = 0;
+        for (int s = 0; s < kMaxStages; ++s) { bar_init(x_land(s), 1); bar_init(x_full(s), 1); bar_init(x_empty(s), 1); }
+        for (int s = 0; s < 2; ++s) {
+            bar_init(acc_full(s), 1); bar_init(acc_empty(s), 128);
+            bar_init(hid_full(s), 128); bar_init(hid_empty(s), 1);
+        }
+        bar_init(w_full, 1); bar_init(w_empty, 1); bar_init(out_full, 1); bar_init(out_empty, 256);
+        fence_bar_init();
+    }
+    if (warp == 0) tmem_alloc(smem_u32(&tmem_at), kTmemColumns);
+    fence_async_shared();
+    tmem_fence_before();
+    __syncthreads();
+    tmem_fence_after();
+    const uint32_t tmem = tmem_at;
+    const int halves = (a.c16 + 127) / 128;                            // of the channels, 128 lanes each
+    const uint32_t acc0 = tmem + 2 * kAcc;
+    // Every role makes the same walk: for each unit of work its tiles, a piece for each expert.
+    auto first_tile = [&](int r) { return (int)((long long)total * r / a.ranges); };
+
+    if (warp == kCopyWarp) {
+        if (lane == 0) {
+            int n = 0, piece = 0;
+            bool ok = true;
+            for (int k = blockIdx.x; ok && k < work; k += gridDim.x) {
+                const int r = k / a.slices, c = k - r * a.slices, lo = first_tile(r), hi = first_tile(r + 1);
+                if (lo >= hi) continue;
+                TileWalk walk = tile_at(a.seg, bounds, start, lo, kTileRows);
+                int e = -1;
+                for (int i = lo; ok && i < hi; ++i, ++n, next_tile(a.seg, walk, kTileRows)) {
+                    if (walk.q / a.seg.B != e) {
+                        e = walk.q / a.seg.B;
+                        if (!(ok = WAIT(w_empty, (piece & 1) ^ 1))) break;
+                        bar_expect(w_full, a.w_bytes);
+                        for (int b = 0; b < a.blocks; ++b) {
+                            const uint32_t to = base + a.off_w + b * (2 * HC * 128);
+                            copy_tile(to, &maps.gate, 64 * b, c * HC, e, w_full);
+                            copy_tile(to + HC * 128, &maps.up, 64 * b, c * HC, e, w_full);
+                        }
+                        copy_tile(base + a.off_w + a.blocks * (2 * HC * 128), &maps.down, c * HC, 0, e, w_full);
+                        ++piece;
+                    }
+                    const int s = n % a.xn;
+                    if (!(ok = WAIT(x_empty(s), (n / a.xn & 1) ^ 1))) break;
+                    bar_expect(x_land(s), a.x_bytes);
+                    const uint32_t to = base + s * a.x_bytes;
+                    for (int b = 0; b < a.blocks; ++b) {
+                        copy_tile(to + b * kBlockBytes, &maps.x, 64 * b, walk.row, x_land(s));
+                        copy_tile(to + (a.blocks + b) * kBlockBytes, &maps.dy, 64 * b, walk.row, x_land(s));
+                    }
+                }
+            }
+        }
+    } else if (warp == kFixWarp) {
+        int n = 0;
+        bool ok = true;
+        for (int k = blockIdx.x; ok && k < work; k += gridDim.x) {
+            const int r = k / a.slices, lo = first_tile(r), hi = first_tile(r + 1);
+            if (lo >= hi) continue;
+            TileWalk walk = tile_at(a.seg, bounds, start, lo, kTileRows);
+            for (int i = lo; i < hi; ++i, ++n, next_tile(a.seg, walk, kTileRows)) {
+                const int s = n % a.xn;
+                if (!(ok = WAIT(x_land(s), n / a.xn & 1))) break;
+                if (walk.left < kTileRows) {
+                    clear_rows(base + s * a.x_bytes, 2 * a.blocks, walk.left, lane);
+                    fence_async_shared();
+                }
+                __syncwarp();
+                if (lane == 0) bar_arrive(x_full(s));
+            }
+        }
+    } else if (warp == kProductWarp) {
+        if (lane == 0) {
+            const uint32_t kind_gu = product_kind(2 * HC, BF16, false, false), kind_dh = product_kind(HC, BF16, false, true);
+            const uint32_t kind_w2 = product_kind(2 * HC, BF16, true, true), kind_w1 = product_kind(HC, BF16, true, true);
+            int n = 0, piece = 0;
+            bool ok = true, pfirst = false, plast = false;
+            // The gradients' products of unit v, which is not before the unit behind it has begun.
+            auto second = [&](int v, int pc) {
+                const int hs = v % a.hn, s = v % a.xn;
+                if (!WAIT(hid_full(hs), v / a.hn & 1)) return false;
+                if (pfirst && !WAIT(out_empty, (pc & 1) ^ 1)) return false;
+                tmem_fence_after();
+                const uint32_t x = base + s * a.x_bytes, dy = x + a.blocks * kBlockBytes, hid = base + a.off_h + hs * a.h_bytes;
+                for (int m = 0; m < halves; ++m)
+                    for (int k = 0; k < kTileRows / 16; ++k) {
+                        const uint32_t at = 2 * m * kBlockBytes + k * 16 * 128;
+                        product(tmem + m * kAcc, operand(x + at, 128, kBlockBytes), operand(hid + k * 16 * HC * 2, HC * 2, kHidBlock), kind_w2,
+                                !pfirst || k > 0);
+                        product(tmem + m * kAcc + 2 * HC, operand(dy + at, 128, kBlockBytes), operand(hid + 2 * kHidBlock + k * 16 * HC * 2, HC * 2, kHidBlock),
+                                kind_w1, !pfirst || k > 0);
+                    }
+                products_done(hid_empty(hs));
+                products_done(x_empty(s));
+                if (plast) products_done(out_full);
+                return true;
+            };
+            for (int k = blockIdx.x; ok && k < work; k += gridDim.x) {
+                const int r = k / a.slices, lo = first_tile(r), hi = first_tile(r + 1);
+                if (lo >= hi) continue;
+                TileWalk walk = tile_at(a.seg, bounds, start, lo, kTileRows);
+                int e = -1;
+                for (int i = lo; i < hi; ++i, ++n) {
+                    const bool first = walk.q / a.seg.B != e;
+                    e = walk.q / a.seg.B;
+                    TileWalk after = walk;
+                    next_tile(a.seg, after, kTileRows);
+                    const bool last = i + 1 == hi || after.q / a.seg.B != e;
+                    walk = after;
+                    const int s = n % a.xn;
+                    if (first) {
+                        if (!(ok = WAIT(w_full, piece & 1))) break;
+                        ++piece;
+                    }
+                    if (!(ok = WAIT(x_full(s), n / a.xn & 1))) break;
+                    if (!(ok = WAIT(acc_empty(n & 1), (n >> 1 & 1) ^ 1))) break;
+                    tmem_fence_after();
+                    const uint32_t d = acc0 + (n & 1) * kAcc, x = base + s * a.x_bytes, dy = x + a.blocks * kBlockBytes;
+                    const uint32_t w = base + a.off_w, wd = w + a.blocks * (2 * HC * 128);
+                    for (int q = 0; q < a.c16 / 16; ++q)
+                        product(d, operand(x + (q >> 2) * kBlockBytes + (q & 3) * 32, 128, 0), operand(w + (q >> 2) * (2 * HC * 128) + (q & 3) * 32, 128, 0),
+                                kind_gu, q > 0);
+                    for (int q = 0; q < a.c16 / 16; ++q)
+                        product(d + 2 * HC, operand(dy + (q >> 2) * kBlockBytes + (q & 3) * 32, 128, 0), operand(wd + q * 16 * HC * 2, HC * 2, 0), kind_dh, q > 0);
+                    products_done(acc_full(n & 1));
+                    if (last) products_done(w_empty);
+                    // With one stage of tiles the next unit cannot begin before this one's second products.
+                    if (a.xn > 1 && n > 0 && !(ok = second(n - 1, piece - 1 - (first ? 1 : 0)))) break;
+                    pfirst = first;
+                    plast = last;
+                    if (a.xn == 1 && !(ok = second(n, piece - 1))) break;
+                }
+            }
+            if (ok && a.xn > 1 && n > 0) second(n - 1, piece - 1);
+        }
+    } else {
+        const int group = warp >> 2, quarter = warp & 3, row = quarter * 32 + lane;
+        const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
+        int n = 0, piece = 0;
+        bool ok = true;
+        for (int k = blockIdx.x; ok && k < work; k += gridDim.x) {
+            const int r = k / a.slices, c = k - r * a.slices, lo = first_tile(r), hi = first_tile(r + 1);
+            if (lo >= hi) continue;
+            TileWalk walk = tile_at(a.seg, bounds, start, lo, kTileRows);
+            for (int i = lo; ok && i < hi;) {
+                const int e = walk.q / a.seg.B;
+                for (; ok && i < hi && walk.q / a.seg.B == e; ++i, ++n, next_tile(a.seg, walk, kTileRows)) {
+                    if ((n & 1) != group) continue;
+                    const int hs = n % a.hn;
+                    if (!(ok = WAIT(acc_full(group), n >> 1 & 1))) break;
+                    if (!(ok = WAIT(hid_empty(hs), (n / a.hn & 1) ^ 1))) break;
+                    tmem_fence_after();
+                    hidden_chunk<GRAD_X, HC, ACT, BF16, true>(acc0 + group * kAcc + lanes, base + a.off_h + hs * a.h_bytes, row);
+                    tmem_fence_before();
+                    bar_arrive(acc_empty(group));
+                    fence_async_shared();
+                    bar_arrive(hid_full(hs));
+                }
+                if (!ok || !(ok = WAIT(out_full, piece & 1))) break;
+                ++piece;
+                tmem_fence_after();
+                float* part = a.part + ((size_t)(r + e) * a.slices + c) * kAcc * a.C;
+                for (int m = 0; m < halves; ++m) {
+                    const int ch = m * 128 + row;
+                    for (int j = group * 48; j < group * 48 + 48; j += 16) {
+                        uint32_t v[16];
+                        tmem_load(v, tmem + m * kAcc + j + lanes);
+                        tmem_wait(v);
+#pragma unroll
+                        for (int q = 0; q < 16; ++q)
+                            if (ch < a.C) part[(size_t)(j + q) * a.C + ch] = __uint_as_float(v[q]);
+                    }
+                }
+                tmem_fence_before();
+                bar_arrive(out_empty);
+            }
+        }
+    }
+#undef WAIT
+    __syncwarp();
+    leave_after_timeout(&gave_up);
+    tmem_fence_before();
+    __syncthreads();
+    tmem_fence_after();
+    if (warp == 0) tmem_free(tmem, kTmemColumns);
+}
+
+struct WeightSumArgs {
+    RowSegments seg;
+    const float* part;
+    void* gate;
+    void* up;
+    void* down;
+    int C, H, slices, ranges, type;
+};
+
+// dW of 32 hidden units and 32 channels: the parts of the ranges that met the expert, in their order.
+__global__ void __launch_bounds__(256) ffn_sum_kernel(WeightSumArgs a) {
+    __shared__ int bounds[kMaxBounds];
+    __shared__ int start[kMaxSegments + 1];
+    __shared__ float tile[32][33];
+    load_bounds(a.seg, bounds);
+    segment_starts(a.seg, bounds, kTileRows, start);
+    const int columns = (a.C + 31) / 32, c0 = blockIdx.x % columns * 32, slice = blockIdx.x / columns, kind = blockIdx.y, e = blockIdx.z, B = a.seg.B;
+    const long long total = start[B * a.seg.E], from = start[e * B], to = start[(e + 1) * B];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    float s[4] = {0.f, 0.f, 0.f, 0.f};
+    if (from < to && c0 + lane < a.C) {
+        const int r0 = (int)(((from + 1) * a.ranges - 1) / total), r1 = (int)((to * a.ranges - 1) / total);
+        for (int r = r0; r <= r1; ++r) {
+            if (total * r / a.ranges == total * (r + 1) / a.ranges) continue;
+            const float* p = a.part + (((size_t)(r + e) * a.slices + slice) * 3 * kSlice + kind * kSlice + warp) * a.C + c0 + lane;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) s[k] += p[(size_t)8 * k * a.C];
+        }
+    }
+    uint16_t* out = static_cast<uint16_t*>(kind == 0 ? a.gate : kind == 1 ? a.up : a.down);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) tile[warp + 8 * k][lane] = s[k];
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        if (kind < 2) {                                   // [E, H, C]
+            const int h = slice * kSlice + warp + 8 * k, ch = c0 + lane;
+            if (h < a.H && ch < a.C) out[((size_t)e * a.H + h) * a.C + ch] = (uint16_t)as_halves(s[k], 0.f, a.type);
+        } else {                                          // [E, C, H]
+            const int h = slice * kSlice + lane, ch = c0 + warp + 8 * k;
+            if (h < a.H && ch < a.C) out[((size_t)e * a.C + ch) * a.H + h] = (uint16_t)as_halves(tile[lane][warp + 8 * k], 0.f, a.type);
+        }
+    }
+}
+
+// ---------------------------------------------------------------- host
+using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                                 const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeTiled encoder() {
+    static const EncodeTiled f = [] {
+        void* p = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &found) != cudaSuccess ||
+            found != cudaDriverEntryPointSuccess)
+            p = nullptr;
+        return reinterpret_cast<EncodeTiled>(p);
+    }();
+    return f;
+}
+
+// [z, y, x] of 16-bit values, copied as boxes of x_box columns (64 or 32, with the swizzle of that width) and y_box rows;
+// what lies outside reads as zeros.
+bool encode(CUtensorMap* map, const void* p, int type, uint64_t x, uint64_t y, uint64_t z, int x_box, int y_box) {
+    const cuuint64_t dims[3] = {x, y, z}, strides[2] = {x * 2, x * y * 2};
+    const cuuint32_t box[3] = {(cuuint32_t)x_box, (cuuint32_t)y_box, 1}, step[3] = {1, 1, 1};
+    const EncodeTiled f = encoder();
+    return f && f(map, type == EMC2_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, z ? 3 : 2, const_cast<void*>(p), dims,
+                  strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, x_box == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+                  CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+struct FfnCall {
+    RowSegments seg;
+    int C, H, type, act;
+    const void* x;
+    const void* dy;
+    const void* gate;
+    const void* up;
+    const void* down;
+};
+
+bool make_maps(const FfnCall& f, int hc, Maps* m) {
+    const int c16 = (f.C + 15) / 16 * 16;
+    const uint64_t rows = (uint64_t)f.seg.B * f.seg.N, E = (uint64_t)f.seg.E;
+    return encode(&m->x, f.x, f.type, f.C, rows, 0, 64, kTileRows) && encode(&m->dy, f.dy ? f.dy : f.x, f.type, f.C, rows, 0, 64, kTileRows) &&
+           encode(&m->gate, f.gate, f.type, f.C, f.H, E, 64, hc) && encode(&m->up, f.up, f.type, f.C, f.H, E, 64, hc) &&
+           encode(&m->down, f.down, f.type, f.H, f.C, E, hc, c16);
+}
+
+template <typename F, typename A>
+int launch_ffn(emc2_bridge* h, int kind, F kernel, const A& a, const Maps& m, int ctas, int threads, size_t shared, cudaStream_t st) {
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)shared);
+    if (e != cudaSuccess) return check_cuda(h, e);
+    LaunchScope ls(h, kind, st);
+    kernel<<<ctas, threads, shared, st>>>(a, m);
+    return check_cuda(h, cudaGetLastError());
+}
+
+template <int MODE, int HC, int NT>
+int launch_rows(emc2_bridge* h, const FfnCall& f, void* out, cudaStream_t st) {
+    RowArgs a;
+    a.seg = f.seg; a.out = out; a.C = f.C; a.H = f.H;
+    a.c16 = (f.C + 15) / 16 * 16;
+    a.blocks = (f.C + 63) / 64;
+    a.chunks = (f.H + HC - 1) / HC;
+    a.x_bytes = (MODE == FORWARD ? 1 : 2) * a.blocks * kBlockBytes;          // these are all multiples of 1 KB
+    a.g_bytes = a.blocks * 2 * HC * 128;
+    a.d_bytes = a.c16 * HC * 2;
+    a.h_bytes = (MODE == FORWARD ? 1 : 2) * kTileRows * HC * 2;
+    // As many stages as there is room for: first two of each, then more of the rows.
+    const bool tight = MODE == GRAD_X && a.c16 > 128;
+    a.xn = tight ? 1 : NT; a.gn = 2; a.dn = tight ? 1 : 2; a.hn = tight ? 1 : 2;
+    auto room = [&] { return (size_t)a.xn * a.x_bytes + (size_t)a.gn * a.g_bytes + (size_t)a.dn * a.d_bytes + (size_t)a.hn * a.h_bytes + 1024; };
+    while (a.xn < kMaxStages && room() + a.x_bytes <= kMaxShared) ++a.xn;
+    while (a.gn < kMaxStages && a.dn > 1 && room() + a.g_bytes + a.d_bytes <= kMaxShared) { ++a.gn; ++a.dn; }
+    a.off_g = a.xn * a.x_bytes;
+    a.off_d = a.off_g + a.gn * a.g_bytes;
+    a.off_h = a.off_d + a.dn * a.d_bytes;
+    Maps m;
+    if (!make_maps(f, HC, &m)) return EMC2_ERR_CUDA;
+    const size_t shared = std::max(room(), (size_t)(kMaxBounds + kMaxSegments + 1) * 4 + 1024);
+    const long long tiles = ((long long)f.seg.B * f.seg.N + kTileRows * NT - 1) / (kTileRows * NT) + (long long)f.seg.B * f.seg.E;
+    const int ctas = (int)std::min<long long>(tiles, h->num_sms), kind = MODE == FORWARD ? K_FFN : K_FFN_GRAD_X;
+    const bool bf16 = f.type == EMC2_BF16;
+    if (f.act == EMC2_ACT_SILU)
+        return bf16 ? launch_ffn(h, kind, ffn_rows_kernel<MODE, HC, NT, EMC2_ACT_SILU, true>, a, m, ctas, kRowThreads, shared, st)
+                    : launch_ffn(h, kind, ffn_rows_kernel<MODE, HC, NT, EMC2_ACT_SILU, false>, a, m, ctas, kRowThreads, shared, st);
+    return bf16 ? launch_ffn(h, kind, ffn_rows_kernel<MODE, HC, NT, EMC2_ACT_GELU, true>, a, m, ctas, kRowThreads, shared, st)
+                : launch_ffn(h, kind, ffn_rows_kernel<MODE, HC, NT, EMC2_ACT_GELU, false>, a, m, ctas, kRowThreads, shared, st);
+}
+
+// Ranges of the tiles: four units of work per SM.
+int weight_ranges(const emc2_bridge* h, int slices) { return std::max(1, 4 * h->num_sms / slices); }
+
+int launch_weights(emc2_bridge* h, const FfnCall& f, void* gate, void* up, void* down, cudaStream_t st) {
+    WeightArgs a;
+    a.seg = f.seg; a.C = f.C; a.H = f.H;
+    a.part = static_cast<float*>(h->rows_scratch.slab);
+    a.c16 = (f.C + 15) / 16 * 16;
+    a.blocks = (f.C + 63) / 64;
+    a.slices = (f.H + kSlice - 1) / kSlice;
+    a.ranges = weight_ranges(h, a.slices);
+    a.x_bytes = 2 * a.blocks * kBlockBytes;
+    a.w_bytes = a.blocks * 2 * kSlice * 128 + a.c16 * kSlice * 2;
+    a.h_bytes = 3 * kTileRows * kSlice * 2;
+    a.xn = 1; a.hn = a.c16 > 128 ? 1 : 2;
+    // The product of the transposed rows takes 128 channels at a time: with fewer than that it reads up to one block
+    // behind a tile's last (the results go to lanes that nobody reads), which the weights' room has to cover.
+    auto room = [&] { return (size_t)a.xn * a.x_bytes + std::max<size_t>(a.w_bytes + (size_t)a.hn * a.h_bytes, kBlockBytes) + 1024; };
+    while (a.xn < 3 && room() + a.x_bytes <= kMaxShared - 4608) ++a.xn;
+    if (a.xn == 1) a.hn = 1;
+    a.off_w = a.xn * a.x_bytes;
+    a.off_h = a.off_w + a.w_bytes;
+    Maps m;
+    if (!make_maps(f, kSlice, &m)) return EMC2_ERR_CUDA;
+    const int ctas = std::min(a.ranges * a.slices, h->num_sms);
+    const bool bf16 = f.type == EMC2_BF16;
+    int rc;
+    if (f.act == EMC2_ACT_SILU)
+        rc = bf16 ? launch_ffn(h, K_FFN_GRAD_W, ffn_weights_kernel<EMC2_ACT_SILU, true>, a, m, ctas, kWeightThreads, room(), st)
+                  : launch_ffn(h, K_FFN_GRAD_W, ffn_weights_kernel<EMC2_ACT_SILU, false>, a, m, ctas, kWeightThreads, room(), st);
+    else
+        rc = bf16 ? launch_ffn(h, K_FFN_GRAD_W, ffn_weights_kernel<EMC2_ACT_GELU, true>, a, m, ctas, kWeightThreads, room(), st)
+                  : launch_ffn(h, K_FFN_GRAD_W, ffn_weights_kernel<EMC2_ACT_GELU, false>, a, m, ctas, kWeightThreads, room(), st);
+    if (rc != EMC2_OK) return rc;
+    WeightSumArgs s;
+    s.seg = f.seg; s.part = a.part; s.gate = gate; s.up = up; s.down = down; s.C = f.C; s.H = f.H; s.slices = a.slices; s.ranges = a.ranges;
+    s.type = f.type;
+    LaunchScope ls(h, K_FFN_SUM, st);
+    ffn_sum_kernel<<<dim3(a.slices * ((f.C + 31) / 32), 3, f.seg.E), 256, 0, st>>>(s);
+    return check_cuda(h, cudaGetLastError());
+}
+
+int check_ffn(const emc2_bridge* h, int B, int N, int C, int H, int type, int act, const void* x, const int32_t* offsets, const void* gate,
+              const void* up, const void* down) {
+    if (!h || B < 0 || N < 0 || B > h->cfg.max_batch || N > h->cfg.max_points) return EMC2_ERR_INVALID_ARG;
+    if (C < 8 || C > kMaxFfnChannels || (C & 7) || H < 8 || H > kMaxFfnHidden || (H & 7)) return EMC2_ERR_INVALID_ARG;
+    if ((type != EMC2_BF16 && type != EMC2_F16) || (act != EMC2_ACT_SILU && act != EMC2_ACT_GELU)) return EMC2_ERR_INVALID_ARG;
+    if (!gate || !up || !down || !on_16_bytes(gate) || !on_16_bytes(up) || !on_16_bytes(down) || !on_16_bytes(x)) return EMC2_ERR_INVALID_ARG;
+    if (B > 0 && N > 0 && !x) return EMC2_ERR_INVALID_ARG;
+    if (reinterpret_cast<uintptr_t>(offsets) & 3) return EMC2_ERR_INVALID_ARG;
+    return EMC2_OK;
+}
+
+}  // namespace
+
+size_t ffn_scratch_bytes(const emc2_bridge* h, int max_channels, int max_hidden) {
+    if (max_hidden <= 0) return 0;
+    const int C = std::min(max_channels, kMaxFfnChannels);
+    size_t most = 0;
+    for (int slices = 1; slices <= (max_hidden + kSlice - 1) / kSlice; ++slices)
+        most = std::max(most, (size_t)(weight_ranges(h, slices) + EMC2_MAX_EXPERTS) * slices * 3 * kSlice * C * sizeof(float));
+    return most;
+}
+
+}  // namespace emc2
+
+using namespace emc2;
+
+extern "C" int emc2_expert_ffn(emc2_bridge_t* h, int32_t B, int32_t N, int32_t channels, int32_t hidden, int32_t type, int32_t act,
+                               const void* d_x, const int32_t* d_offsets, const void* d_w_gate, const void* d_w_up, const void* d_w_down,
+                               void* d_y, void* cuda_stream) {
+    const int rc = check_ffn(h, B, N, channels, hidden, type, act, d_x, d_offsets, d_w_gate, d_w_up, d_w_down);
+    if (rc != EMC2_OK) return rc;
+    if (!on_16_bytes(d_y)) return EMC2_ERR_INVALID_ARG;
+    if (B == 0 || N == 0) return EMC2_OK;
+    if (!d_y || d_y == d_x) return EMC2_ERR_INVALID_ARG;
+    RowsDevice device(h->cfg.device);
+    if (!device.ok) return EMC2_ERR_CUDA;
+    const FfnCall f = {row_segments(h, B, N, d_offsets), channels, hidden, type, act, d_x, nullptr, d_w_gate, d_w_up, d_w_down};
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    return channels <= 128 ? launch_rows<FORWARD, 64, 2>(h, f, d_y, st) : launch_rows<FORWARD, 32, 1>(h, f, d_y, st);
+}
+
+extern "C" int emc2_expert_ffn_grad(emc2_bridge_t* h, int32_t B, int32_t N, int32_t channels, int32_t hidden, int32_t type, int32_t act,
+                                    const void* d_x, const int32_t* d_offsets, const void* d_w_gate, const void* d_w_up,
+                                    const void* d_w_down, const void* d_grad_y, void* d_grad_x, void* d_grad_gate, void* d_grad_up,
+                                    void* d_grad_down, void* cuda_stream) {
+    int rc = check_ffn(h, B, N, channels, hidden, type, act, d_x, d_offsets, d_w_gate, d_w_up, d_w_down);
+    if (rc != EMC2_OK) return rc;
+    if (!d_grad_gate || !d_grad_up || !d_grad_down || !on_16_bytes(d_grad_y) || !on_16_bytes(d_grad_x) || !on_16_bytes(d_grad_gate) ||
+        !on_16_bytes(d_grad_up) || !on_16_bytes(d_grad_down))
+        return EMC2_ERR_INVALID_ARG;
+    const bool empty = B == 0 || N == 0;
+    if (!empty && (!d_grad_y || !d_grad_x || d_grad_x == d_x || d_grad_x == d_grad_y)) return EMC2_ERR_INVALID_ARG;
+    if (!h->rows_scratch.slab || channels > h->rows_scratch.max_channels || hidden > h->rows_scratch.max_hidden) return EMC2_ERR_TOO_LARGE;
+    RowsDevice device(h->cfg.device);
+    if (!device.ok) return EMC2_ERR_CUDA;
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    const FfnCall f = {row_segments(h, B, N, d_offsets), channels, hidden, type, act, d_x, d_grad_y, d_w_gate, d_w_up, d_w_down};
+    if (empty) {
+        const size_t bytes = (size_t)f.seg.E * hidden * channels * 2;
+        cudaError_t e = cudaMemsetAsync(d_grad_gate, 0, bytes, st);
+        if (e == cudaSuccess) e = cudaMemsetAsync(d_grad_up, 0, bytes, st);
+        if (e == cudaSuccess) e = cudaMemsetAsync(d_grad_down, 0, bytes, st);
+        return check_cuda(h, e);
+    }
+    rc = launch_rows<GRAD_X, 32, 1>(h, f, d_grad_x, st);
+    if (rc == EMC2_OK) rc = launch_weights(h, f, d_grad_gate, d_grad_up, d_grad_down, st);
+    return rc;
+}
