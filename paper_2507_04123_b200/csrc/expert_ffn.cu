@@ -9,8 +9,8 @@
 // products.  What lies between the two products of a chunk (h, or dg and du) is rounded to the rows' type, as the tensor
 // cores take it; all sums are held in fp32, results are rounded once.
 //
-// Three kinds of warps pass tiles along with mbarriers: one thread copies (tiled bulk copies), one issues products, eight
-// warps apply the activation from TMEM to shared memory, four per accumulator so that one is filled while the other is read.
+// Warps of several kinds pass tiles along with mbarriers: one thread copies (tiled bulk copies), one issues the products
+// before the activation and one those behind it (one thread for both was what all waited for), sixteen warps apply the activation from TMEM to shared memory, eight per accumulator so that one is filled while the other is read.
 #include <algorithm>
 
 #include "rows.cuh"
@@ -21,8 +21,8 @@ namespace {
 
 constexpr int kTileRows = 128;
 constexpr int kBlockBytes = kTileRows * 128;     // a tile's 64 columns
-constexpr int kCopyWarp = 8, kProductWarp = 9, kFixWarp = 10;
-constexpr int kRowThreads = 320, kWeightThreads = 352;
+constexpr int kCopyWarp = 16, kFirstWarp = 17, kSecondWarp = 18, kFixWarp = 19;
+constexpr int kRowThreads = 608, kWeightThreads = 640;
 constexpr int kTmemColumns = 512;
 constexpr int kMaxFfnChannels = 256, kMaxFfnHidden = 8192;
 constexpr int kMaxStages = 4;
@@ -70,27 +70,68 @@ __device__ __forceinline__ void next_tile(const RowSegments& s, TileWalk& w, int
     }
 }
 
-// ---------------------------------------------------------------- activations
-template <int ACT>
-__device__ __forceinline__ float activation(float g) {
-    if (ACT == EMC2_ACT_SILU) return __fdividef(g, 1.0f + __expf(-g));
-    return 0.5f * g * (1.0f + erff(g * 0.70710678118654752f));
+// ---------------------------------------------------------------- activations, two values at a time
+// The special-function unit is what the activation waits for (16 results a clock and SM), so exponentials, reciprocals and
+// hyperbolic tangents are what is saved.
+
+// 1 / (1 + exp(-g)).  For bf16 rows by one hyperbolic tangent, (1 + tanh(g / 2)) / 2, which is off by 2^-12 at most (tanh.approx
+// is by 2^-11 of itself): an eighth of the half step that rounding a value near 1 to bf16 costs afterwards.  For fp16 rows that
+// would be a whole half step: there by exponentials, off by a few units of fp32, and one reciprocal for two.  Their
+// argument ends at 2^60: below -41 the result is 2^-60 instead of less.
+template <bool BF16>
+__device__ __forceinline__ uint64_t sigmoid2(uint64_t g) {
+    if (BF16) {
+        const float2 x = unpair(mul2(g, pair(0.5f, 0.5f)));
+        return fma2(pair(fast_tanh(x.x), fast_tanh(x.y)), pair(0.5f, 0.5f), pair(0.5f, 0.5f));
+    }
+    const float2 x = unpair(mul2(g, pair(-1.44269504f, -1.44269504f)));
+    const float2 d = unpair(add2(pair(fast_exp2(fminf(x.x, 60.0f)), fast_exp2(fminf(x.y, 60.0f))), pair(1.0f, 1.0f)));
+    return reciprocals(d.x, d.y);
 }
-template <int ACT>
-__device__ __forceinline__ void activation_grad(float g, float& a, float& da) {
+
+// The normal distribution at g and its density times sqrt(2 pi): Abramowitz and Stegun 7.1.26 for the error function at
+// g / sqrt(2), off by 0.75e-7 at most.  Its exponential is the density's, so that both take one exponential and half a
+// reciprocal; the constants are the published ones, halved.
+__device__ __forceinline__ uint64_t normal2(uint64_t g, uint64_t& density) {
+    const float2 x = unpair(g), e = unpair(mul2(mul2(g, g), pair(-0.72134752f, -0.72134752f)));
+    density = pair(fast_exp2(e.x), fast_exp2(e.y));
+    constexpr float p = 0.3275911f * 0.70710678f;
+    const uint64_t t = reciprocals(fmaf(p, fminf(fabsf(x.x), 1e6f), 1.0f), fmaf(p, fminf(fabsf(x.y), 1e6f), 1.0f));
+    auto all = [](float v) { return pair(v, v); };
+    uint64_t q = fma2(t, all(0.5307027145f), all(-0.7265760135f));
+    q = fma2(t, q, all(0.7107068705f));
+    q = fma2(t, q, all(-0.142248368f));
+    q = fma2(t, q, all(0.127414796f));
+    const float2 tail = unpair(mul2(mul2(t, q), density));
+    return pair(x.x < 0.0f ? tail.x : 1.0f - tail.x, x.y < 0.0f ? tail.y : 1.0f - tail.y);
+}
+
+template <int ACT, bool BF16>
+__device__ __forceinline__ uint64_t activation2(uint64_t g) {
+    uint64_t density;
+    return mul2(g, ACT == EMC2_ACT_SILU ? sigmoid2<BF16>(g) : normal2(g, density));
+}
+template <int ACT, bool BF16>
+__device__ __forceinline__ void activation_grad2(uint64_t g, uint64_t& a, uint64_t& da) {
     if (ACT == EMC2_ACT_SILU) {
-        const float s = __fdividef(1.0f, 1.0f + __expf(-g));
-        a = g * s;
-        da = s + a * (1.0f - s);
+        const uint64_t s = sigmoid2<BF16>(g);
+        a = mul2(g, s);
+        da = fma2(a, fma2(s, pair(-1.0f, -1.0f), pair(1.0f, 1.0f)), s);        // s + a (1 - s)
     } else {
-        const float phi = 0.5f + 0.5f * erff(g * 0.70710678118654752f);
-        a = g * phi;
-        da = phi + g * 0.39894228040143268f * __expf(-0.5f * g * g);
+        uint64_t density;
+        const uint64_t phi = normal2(g, density);
+        a = mul2(g, phi);
+        da = fma2(mul2(g, pair(0.39894228f, 0.39894228f)), density, phi);
     }
 }
 
 template <bool BF16>
 __device__ __forceinline__ uint32_t pack(float a, float b) { return as_halves(a, b, BF16 ? EMC2_BF16 : EMC2_F16); }
+template <bool BF16>
+__device__ __forceinline__ uint32_t pack(uint64_t p) {
+    const float2 f = unpair(p);
+    return pack<BF16>(f.x, f.y);
+}
 
 __device__ __forceinline__ void store_shared(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
@@ -110,17 +151,18 @@ __device__ __forceinline__ void hidden8(const uint32_t (&g)[W], const uint32_t (
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const int j = j0 + 2 * i;
-        const float g0 = __uint_as_float(g[j]), g1 = __uint_as_float(g[j + 1]), u0 = __uint_as_float(u[j]), u1 = __uint_as_float(u[j + 1]);
+        uint32_t first = g[j];
+        if (WITH_H && i == 2) asm volatile("" : "+r"(first));     // half a piece after the other, see hidden_half
+        const uint64_t gg = pair(first, g[j + 1]), uu = pair(u[j], u[j + 1]);
         if (MODE == FORWARD) {
-            p[i] = pack<BF16>(activation<ACT>(g0) * u0, activation<ACT>(g1) * u1);
+            p[i] = pack<BF16>(mul2(activation2<ACT, BF16>(gg), uu));
         } else {
-            const float d0 = __uint_as_float(dh[j]), d1 = __uint_as_float(dh[j + 1]);
-            float a0, a1, da0, da1;
-            activation_grad<ACT>(g0, a0, da0);
-            activation_grad<ACT>(g1, a1, da1);
-            p[i] = pack<BF16>(d0 * u0 * da0, d1 * u1 * da1);
-            q[i] = pack<BF16>(d0 * a0, d1 * a1);
-            if (WITH_H) t[i] = pack<BF16>(a0 * u0, a1 * u1);
+            const uint64_t dd = pair(dh[j], dh[j + 1]);
+            uint64_t a, da;
+            activation_grad2<ACT, BF16>(gg, a, da);
+            p[i] = pack<BF16>(mul2(mul2(dd, uu), da));
+            q[i] = pack<BF16>(mul2(dd, a));
+            if (WITH_H) t[i] = pack<BF16>(mul2(a, uu));
         }
     }
     const uint32_t at = to + swizzled<HC>(r, c / 8);
@@ -131,22 +173,36 @@ __device__ __forceinline__ void hidden8(const uint32_t (&g)[W], const uint32_t (
     }
 }
 
-// The activation of one chunk of one tile: accumulators at `acc` (g, u and, for the gradients, dh, HC columns each) of
-// the warp's 32 rows into the blocks at `to`.  Eight columns at a time where more would not fit in the registers.
+// One arrival per warp, for what all its threads have done.
+__device__ __forceinline__ void warp_arrive(uint32_t bar) {
+    __syncwarp();
+    if ((threadIdx.x & 31) == 0) bar_arrive(bar);
+}
+
+// The activation of half of the columns of one chunk of one tile: accumulators at `acc` (g, u and, for the gradients, dh,
+// HC columns each) of the warp's 32 rows into the blocks at `to`.  The accumulators are given back once they are in
+// registers, before the arithmetic, so that the next products run beside it.
 template <int MODE, int HC, int ACT, bool BF16, bool WITH_H>
-__device__ __forceinline__ void hidden_chunk(uint32_t acc, uint32_t to, int r) {
-    constexpr int W = MODE == GRAD_X && ACT == EMC2_ACT_GELU ? 8 : 16;
+__device__ __forceinline__ void hidden_half(uint32_t acc, int half, uint32_t to, int r, uint32_t acc_empty, uint32_t hid_empty, uint32_t parity,
+                                            volatile int* gave_up, int* status) {
+    constexpr int W = HC / 2;
     uint32_t g[W], u[W], dh[W];
+    tmem_load(g, acc + half * W);
+    tmem_load(u, acc + HC + half * W);
+    if (MODE == GRAD_X) tmem_load(dh, acc + 2 * HC + half * W);
+    tmem_wait(g);
+    tmem_wait(u);
+    if (MODE == GRAD_X) tmem_wait(dh);
+    tmem_fence_before();
+    warp_arrive(acc_empty);
+    bar_wait_inline(hid_empty, parity, gave_up, status);                   // a call would save the values around it
 #pragma unroll
-    for (int c = 0; c < HC; c += W) {
-        tmem_load(g, acc + c);
-        tmem_load(u, acc + HC + c);
-        if (MODE == GRAD_X) tmem_load(dh, acc + 2 * HC + c);
-        tmem_wait(g);
-        tmem_wait(u);
-        if (MODE == GRAD_X) tmem_wait(dh);
+    for (int j = 0; j < W; j += 8) {
+        if (WITH_H || (MODE == FORWARD && ACT == EMC2_ACT_GELU)) {     // one piece after the other: the arithmetic of two would not fit in the registers
 #pragma unroll
-        for (int j = 0; j < W; j += 8) hidden8<MODE, HC, ACT, BF16, WITH_H>(g, u, dh, j, to, r, c + j);
+            for (int i = j; i < j + 8; ++i) asm volatile("" : "+r"(g[i]));
+        }
+        hidden8<MODE, HC, ACT, BF16, WITH_H>(g, u, dh, j, to, r, half * W + j);
     }
 }
 
@@ -171,8 +227,8 @@ __global__ void __launch_bounds__(kRowThreads, 1) ffn_rows_kernel(const RowArgs 
     __shared__ __align__(8) uint64_t bars[4 * kMaxStages * 2 + 16];
     __shared__ uint32_t tmem_at;
     __shared__ int gave_up;
-    const uint32_t base = (smem_u32(dynamic) + 1023u) & ~1023u;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t base = uniform((smem_u32(dynamic) + 1023u) & ~1023u);
+    const int warp = uniform((int)threadIdx.x >> 5), lane = threadIdx.x & 31;
     const uint32_t bar0 = smem_u32(bars);
     auto x_full = [&](int s) { return bar0 + 8 * s; };
     auto x_empty = [&](int s) { return bar0 + 8 * (4 + s); };
@@ -204,9 +260,9 @@ __global__ void __launch_bounds__(kRowThreads, 1) ffn_rows_kernel(const RowArgs 
             bar_init(d_full(s), 1); bar_init(d_empty(s), 1);
         }
         for (int s = 0; s < 2; ++s) {
-            bar_init(acc_full(s), 1); bar_init(acc_empty(s), 128);
-            bar_init(hid_full(s), 128); bar_init(hid_empty(s), 1);
-            bar_init(out_full(s), 1); bar_init(out_empty(s), NT == 2 ? 128 : 256);
+            bar_init(acc_full(s), 1); bar_init(acc_empty(s), 8);
+            bar_init(hid_full(s), 8); bar_init(hid_empty(s), 1);
+            bar_init(out_full(s), 1); bar_init(out_empty(s), NT == 2 ? 8 : 16);
         }
         fence_bar_init();
     }
@@ -215,123 +271,127 @@ __global__ void __launch_bounds__(kRowThreads, 1) ffn_rows_kernel(const RowArgs 
     tmem_fence_before();
     __syncthreads();
     tmem_fence_after();
-    const uint32_t tmem = tmem_at;
+    const uint32_t tmem = uniform(tmem_at);
     const uint32_t acc0 = tmem + NT * a.c16;                           // behind the output's accumulators
-    const int items = hi - lo, units = items * a.chunks * NT;
+    const int items = uniform(hi - lo), units = items * a.chunks * NT;
 #define WAIT(bar, parity) bar_wait(bar, parity, &gave_up, a.seg.status)
 
     if (warp == kCopyWarp) {
         if (lane == 0) {
-            int xc = 0, wc = 0;                                        // tiles and chunks copied so far
-            for (int it = 0; it < items; ++it, next_tile(a.seg, walk, kTileRows * NT)) {
+            Ring x(a.xn), g(a.gn), d(a.dn);
+            for (int it = 0; it < items && !*(volatile int*)&gave_up; ++it, next_tile(a.seg, walk, kTileRows * NT)) {
                 const int e = walk.q / a.seg.B;
-                bool ok = true;
-                for (int t = 0; ok && t < NT; ++t, ++xc) {
-                    const int s = xc % a.xn;
-                    if (!(ok = WAIT(x_empty(s), (xc / a.xn & 1) ^ 1))) break;
-                    bar_expect(x_full(s), a.x_bytes);
-                    const uint32_t to = base + s * a.x_bytes;
+                for (int t = 0; t < NT; ++t, x.next()) {
+                    WAIT(x_empty(x.at), x.parity ^ 1);
+                    bar_expect(x_full(x.at), a.x_bytes);
+                    const uint32_t to = base + x.at * a.x_bytes;
                     for (int b = 0; b < a.blocks; ++b) {
-                        copy_tile(to + b * kBlockBytes, &maps.x, 64 * b, walk.row + t * kTileRows, x_full(s));
-                        if (MODE == GRAD_X) copy_tile(to + (a.blocks + b) * kBlockBytes, &maps.dy, 64 * b, walk.row + t * kTileRows, x_full(s));
+                        copy_tile(to + b * kBlockBytes, &maps.x, 64 * b, walk.row + t * kTileRows, x_full(x.at));
+                        if (MODE == GRAD_X) copy_tile(to + (a.blocks + b) * kBlockBytes, &maps.dy, 64 * b, walk.row + t * kTileRows, x_full(x.at));
                     }
                 }
-                for (int j = 0; ok && j < a.chunks; ++j, ++wc) {
-                    const int s = wc % a.gn, d = wc % a.dn;
-                    if (!(ok = WAIT(g_empty(s), (wc / a.gn & 1) ^ 1))) break;
-                    bar_expect(g_full(s), a.g_bytes);
+                for (int j = 0; j < a.chunks && !*(volatile int*)&gave_up; ++j, g.next(), d.next()) {
+                    WAIT(g_empty(g.at), g.parity ^ 1);
+                    bar_expect(g_full(g.at), a.g_bytes);
                     for (int b = 0; b < a.blocks; ++b) {
-                        const uint32_t to = base + a.off_g + s * a.g_bytes + b * (2 * HC * 128);
-                        copy_tile(to, &maps.gate, 64 * b, j * HC, e, g_full(s));
-                        copy_tile(to + HC * 128, &maps.up, 64 * b, j * HC, e, g_full(s));
+                        const uint32_t to = base + a.off_g + g.at * a.g_bytes + b * (2 * HC * 128);
+                        copy_tile(to, &maps.gate, 64 * b, j * HC, e, g_full(g.at));
+                        copy_tile(to + HC * 128, &maps.up, 64 * b, j * HC, e, g_full(g.at));
                     }
-                    if (!(ok = WAIT(d_empty(d), (wc / a.dn & 1) ^ 1))) break;
-                    bar_expect(d_full(d), a.d_bytes);
-                    copy_tile(base + a.off_d + d * a.d_bytes, &maps.down, j * HC, 0, e, d_full(d));
+                    WAIT(d_empty(d.at), d.parity ^ 1);
+                    bar_expect(d_full(d.at), a.d_bytes);
+                    copy_tile(base + a.off_d + d.at * a.d_bytes, &maps.down, j * HC, 0, e, d_full(d.at));
                 }
-                if (!ok) break;
             }
         }
-    } else if (warp == kProductWarp) {
-        if (lane == 0) {
-            const uint32_t kind_gu = product_kind(2 * HC, BF16, false, false), kind_dh = product_kind(HC, BF16, false, true);
-            const uint32_t kind_out = product_kind(a.c16, BF16, false, MODE == GRAD_X);
-            int item = 0, j = 0, t = 0, pitem = 0, pj = 0, pt = 0;
-            // Unit n is chunk j of tile t of an item; the second product of a unit follows the first one of the next.
-            for (int n = 0; n <= units; ++n) {
-                if (n < units) {
-                    const int xc = item * NT + t, xs = xc % a.xn, wc = item * a.chunks + j, gs = wc % a.gn, ds = wc % a.dn;
-                    if (t == 0 && !WAIT(g_full(gs), wc / a.gn & 1)) break;
-                    if (MODE == GRAD_X && !WAIT(d_full(ds), wc / a.dn & 1)) break;
-                    if (j == 0 && !WAIT(x_full(xs), xc / a.xn & 1)) break;
-                    if (!WAIT(acc_empty(n & 1), (n >> 1 & 1) ^ 1)) break;
-                    tmem_fence_after();
-                    const uint32_t d = acc0 + (n & 1) * kAcc, x = base + xs * a.x_bytes, w = base + a.off_g + gs * a.g_bytes;
-                    for (int k = 0; k < a.c16 / 16; ++k)
-                        product(d, operand(x + (k >> 2) * kBlockBytes + (k & 3) * 32, 128, 0),
-                                operand(w + (k >> 2) * (2 * HC * 128) + (k & 3) * 32, 128, 0), kind_gu, k > 0);
-                    if (MODE == GRAD_X) {
-                        const uint32_t dy = x + a.blocks * kBlockBytes, wd = base + a.off_d + ds * a.d_bytes;
-                        for (int k = 0; k < a.c16 / 16; ++k)
-                            product(d + 2 * HC, operand(dy + (k >> 2) * kBlockBytes + (k & 3) * 32, 128, 0),
-                                    operand(wd + k * 16 * HC * 2, HC * 2, 0), kind_dh, k > 0);
-                    }
-                    products_done(acc_full(n & 1));
-                    if (MODE == FORWARD && t == NT - 1) products_done(g_empty(gs));
-                    if (MODE == GRAD_X) products_done(d_empty(ds));
-                    if (j == a.chunks - 1) products_done(x_empty(xs));
-                    if (++t == NT) { t = 0; if (++j == a.chunks) { j = 0; ++item; } }
+    } else if (warp == kFirstWarp) {
+        // Unit n is chunk j of tile t of an item.
+        const uint32_t lead = elected(), kind_gu = product_kind(2 * HC, BF16, false, false), kind_dh = product_kind(HC, BF16, false, true);
+        const int steps = a.c16 / 16;
+        const uint64_t x0 = operand(base, 128, 0), w0 = operand(base + a.off_g, 128, 0), wd0 = operand(base + a.off_d, HC * 2, 0);
+        Ring x(a.xn), g(a.gn), d(a.dn);
+        int j = 0, t = 0;
+        for (int n = 0; n < units; ++n) {
+            if (t == 0) WAIT(g_full(g.at), g.parity);
+            if (MODE == GRAD_X) WAIT(d_full(d.at), d.parity);
+            const int xs = x.at + t < a.xn ? x.at + t : x.at + t - a.xn;
+            if (j == 0) WAIT(x_full(xs), x.at + t < a.xn ? x.parity : x.parity ^ 1);
+            WAIT(acc_empty(n & 1), (n >> 1 & 1) ^ 1);
+            tmem_fence_after();
+            const uint32_t acc = acc0 + (n & 1) * kAcc;
+            const uint64_t xa = operand_at(x0, xs * a.x_bytes);
+            product_blocks(lead, acc, xa, kBlockBytes, operand_at(w0, g.at * a.g_bytes), 2 * HC * 128, steps, kind_gu);
+            if (MODE == GRAD_X)
+                product_blocks_mn(lead, acc + 2 * HC, operand_at(xa, a.blocks * kBlockBytes), kBlockBytes, operand_at(wd0, d.at * a.d_bytes), 32 * HC, steps, kind_dh);
+            products_done(lead, acc_full(n & 1));
+            // The gradients' second products take Wg and Wu again: the other warp gives them back.
+            if (MODE == FORWARD && t == NT - 1) products_done(lead, g_empty(g.at));
+            if (MODE == GRAD_X) products_done(lead, d_empty(d.at));
+            if (j == a.chunks - 1) products_done(lead, x_empty(xs));
+            if (++t == NT) {
+                t = 0;
+                g.next();
+                d.next();
+                if (++j == a.chunks) {
+                    j = 0;
+                    for (int k = 0; k < NT; ++k) x.next();
                 }
-                if (n > 0) {
-                    const int v = n - 1, hs = v % a.hn, wc = pitem * a.chunks + pj, gs = wc % a.gn, ds = wc % a.dn;
-                    if (!WAIT(hid_full(hs), v / a.hn & 1)) break;
-                    if (pj == 0 && !WAIT(out_empty(pt), (pitem & 1) ^ 1)) break;
-                    if (MODE == FORWARD && pt == 0 && !WAIT(d_full(ds), wc / a.dn & 1)) break;
-                    tmem_fence_after();
-                    const uint32_t d = tmem + pt * a.c16, hid = base + a.off_h + hs * a.h_bytes;
-                    if (MODE == FORWARD) {
-                        const uint32_t wd = base + a.off_d + ds * a.d_bytes;
-                        for (int k = 0; k < HC / 16; ++k)
-                            product(d, operand(hid + k * 32, HC * 2, 0), operand(wd + k * 32, HC * 2, 0), kind_out, pj > 0 || k > 0);
-                    } else {
-                        const uint32_t w = base + a.off_g + gs * a.g_bytes;
-                        for (int k = 0; k < 2 * HC / 16; ++k)
-                            product(d, operand(hid + k / (HC / 16) * kHidBlock + k % (HC / 16) * 32, HC * 2, 0),
-                                    operand(w + k * 16 * 128, 128, 2 * HC * 128), kind_out, pj > 0 || k > 0);
-                    }
-                    products_done(hid_empty(hs));
-                    if (MODE == FORWARD && pt == NT - 1) products_done(d_empty(ds));
-                    if (MODE == GRAD_X) products_done(g_empty(gs));
-                    if (pj == a.chunks - 1) products_done(out_full(pt));
-                    if (++pt == NT) { pt = 0; if (++pj == a.chunks) { pj = 0; ++pitem; } }
-                }
+            }
+        }
+    } else if (warp == kSecondWarp) {
+        const uint32_t lead = elected(), kind_out = product_kind(a.c16, BF16, false, MODE == GRAD_X);
+        const uint64_t w0 = MODE == FORWARD ? operand(base + a.off_d, HC * 2, 0) : operand(base + a.off_g, 128, 2 * HC * 128);
+        const uint64_t hid0 = operand(base + a.off_h, HC * 2, 0);
+        Ring w(MODE == FORWARD ? a.dn : a.gn), hid(a.hn);
+        int j = 0, t = 0;
+        uint32_t item_parity = 0;
+        for (int n = 0; n < units; ++n) {
+            // The first products of this unit have waited for the gradients' Wg and Wu, but not this warp.
+            if (t == 0) WAIT(MODE == FORWARD ? d_full(w.at) : g_full(w.at), w.parity);
+            if (j == 0) WAIT(out_empty(t), item_parity ^ 1);
+            WAIT(hid_full(hid.at), hid.parity);
+            tmem_fence_after();
+            const uint32_t out = tmem + t * a.c16;
+            const uint64_t h = operand_at(hid0, hid.at * a.h_bytes), ww = operand_at(w0, w.at * (MODE == FORWARD ? a.d_bytes : a.g_bytes));
+            if (MODE == FORWARD) {
+#pragma unroll
+                for (int k = 0; k < HC / 16; ++k) product(lead, out, operand_at(h, 32 * k), operand_at(ww, 32 * k), kind_out, j > 0 || k > 0);
+            } else {
+#pragma unroll
+                for (int k = 0; k < 2 * HC / 16; ++k)
+                    product(lead, out, operand_at(h, k / (HC / 16) * kHidBlock + k % (HC / 16) * 32), operand_at(ww, k * 16 * 128), kind_out, j > 0 || k > 0);
+            }
+            products_done(lead, hid_empty(hid.at));
+            if (t == NT - 1) products_done(lead, MODE == FORWARD ? d_empty(w.at) : g_empty(w.at));
+            if (j == a.chunks - 1) products_done(lead, out_full(t));
+            hid.next();
+            if (++t == NT) {
+                t = 0;
+                w.next();
+                if (++j == a.chunks) { j = 0; item_parity ^= 1; }
             }
         }
     } else {
-        const int group = warp >> 2, quarter = warp & 3, r = quarter * 32 + lane;
+        const int group = warp >> 3, half = warp >> 2 & 1, quarter = warp & 3, r = quarter * 32 + lane;
         const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
-        bool ok = true;
         int n = 0;
-        for (int it = 0; ok && it < items; ++it, next_tile(a.seg, walk, kTileRows * NT)) {
-            for (int k = 0; ok && k < a.chunks * NT; ++k, ++n) {
+        for (int it = 0; it < items; ++it, next_tile(a.seg, walk, kTileRows * NT)) {
+            for (int k = 0; k < a.chunks * NT; ++k, ++n) {
                 if ((n & 1) != group) continue;
                 const int hs = n % a.hn;
-                if (!(ok = WAIT(acc_full(group), n >> 1 & 1))) break;
-                if (!(ok = WAIT(hid_empty(hs), (n / a.hn & 1) ^ 1))) break;
+                WAIT(acc_full(group), n >> 1 & 1);
                 tmem_fence_after();
-                hidden_chunk<MODE, HC, ACT, BF16, false>(acc0 + group * kAcc + lanes, base + a.off_h + hs * a.h_bytes, r);
-                tmem_fence_before();
-                bar_arrive(acc_empty(group));
+                hidden_half<MODE, HC, ACT, BF16, false>(acc0 + group * kAcc + lanes, half, base + a.off_h + hs * a.h_bytes, r, acc_empty(group),
+                                                            hid_empty(hs), (n / a.hn & 1) ^ 1, &gave_up, a.seg.status);
                 fence_async_shared();
-                bar_arrive(hid_full(hs));
+                warp_arrive(hid_full(hs));
             }
-            if (!ok) break;
             const int t = NT == 2 ? group : 0;
-            if (!(ok = WAIT(out_full(t), it & 1))) break;
+            WAIT(out_full(t), it & 1);
             tmem_fence_after();
             const bool mine = t * kTileRows + r < walk.left;
             uint16_t* to = static_cast<uint16_t*>(a.out) + (size_t)(walk.row + t * kTileRows + r) * a.C;
-            for (int c = NT == 2 ? 0 : 16 * group; c < a.c16; c += NT == 2 ? 16 : 32) {
+            for (int c = 16 * (NT == 2 ? half : 2 * group + half); c < a.c16; c += NT == 2 ? 32 : 64) {
                 uint32_t v[16];
                 tmem_load(v, tmem + t * a.c16 + c + lanes);
                 tmem_wait(v);
@@ -343,7 +403,7 @@ __global__ void __launch_bounds__(kRowThreads, 1) ffn_rows_kernel(const RowArgs 
                             pack<BF16>(__uint_as_float(v[k + 4]), __uint_as_float(v[k + 5])), pack<BF16>(__uint_as_float(v[k + 6]), __uint_as_float(v[k + 7])));
             }
             tmem_fence_before();
-            bar_arrive(out_empty(t));
+            warp_arrive(out_empty(t));
         }
     }
     __syncwarp();
@@ -387,8 +447,8 @@ __global__ void __launch_bounds__(kWeightThreads, 1) ffn_weights_kernel(const We
     __shared__ int start[kMaxSegments + 1];
     __shared__ uint32_t tmem_at;
     __shared__ int gave_up;
-    const uint32_t base = (smem_u32(dynamic) + 1023u) & ~1023u;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t base = uniform((smem_u32(dynamic) + 1023u) & ~1023u);
+    const int warp = uniform((int)threadIdx.x >> 5), lane = threadIdx.x & 31;
     const uint32_t bar0 = smem_u32(bars);
     auto x_land = [&](int s) { return bar0 + 8 * s; };
     auto x_full = [&](int s) { return bar0 + 8 * (4 + s); };
@@ -401,16 +461,16 @@ __global__ void __launch_bounds__(kWeightThreads, 1) ffn_weights_kernel(const We
 
     load_bounds(a.seg, bounds);
     segment_starts(a.seg, bounds, kTileRows, start);
-    const int total = start[a.seg.B * a.seg.E], work = a.ranges * a.slices;
+    const int total = uniform(start[a.seg.B * a.seg.E]), work = a.ranges * a.slices;
     if (total == 0) return;
     if (threadIdx.x == 0) {
         gave_up = 0;
         for (int s = 0; s < kMaxStages; ++s) { bar_init(x_land(s), 1); bar_init(x_full(s), 1); bar_init(x_empty(s), 1); }
         for (int s = 0; s < 2; ++s) {
-            bar_init(acc_full(s), 1); bar_init(acc_empty(s), 128);
-            bar_init(hid_full(s), 128); bar_init(hid_empty(s), 1);
+            bar_init(acc_full(s), 1); bar_init(acc_empty(s), 8);
+            bar_init(hid_full(s), 8); bar_init(hid_empty(s), 1);
         }
-        bar_init(w_full, 1); bar_init(w_empty, 1); bar_init(out_full, 1); bar_init(out_empty, 256);
+        bar_init(w_full, 1); bar_init(w_empty, 1); bar_init(out_full, 1); bar_init(out_empty, 16);
         fence_bar_init();
     }
     if (warp == 0) tmem_alloc(smem_u32(&tmem_at), kTmemColumns);
@@ -418,7 +478,7 @@ __global__ void __launch_bounds__(kWeightThreads, 1) ffn_weights_kernel(const We
     tmem_fence_before();
     __syncthreads();
     tmem_fence_after();
-    const uint32_t tmem = tmem_at;
+    const uint32_t tmem = uniform(tmem_at);
     const int halves = (a.c16 + 127) / 128;                            // of the channels, 128 lanes each
     const uint32_t acc0 = tmem + 2 * kAcc;
     // Every role makes the same walk: for each unit of work its tiles, a piece for each expert.
@@ -427,16 +487,15 @@ __global__ void __launch_bounds__(kWeightThreads, 1) ffn_weights_kernel(const We
     if (warp == kCopyWarp) {
         if (lane == 0) {
             int n = 0, piece = 0;
-            bool ok = true;
-            for (int k = blockIdx.x; ok && k < work; k += gridDim.x) {
+            for (int k = blockIdx.x; k < work; k += gridDim.x) {
                 const int r = k / a.slices, c = k - r * a.slices, lo = first_tile(r), hi = first_tile(r + 1);
                 if (lo >= hi) continue;
                 TileWalk walk = tile_at(a.seg, bounds, start, lo, kTileRows);
                 int e = -1;
-                for (int i = lo; ok && i < hi; ++i, ++n, next_tile(a.seg, walk, kTileRows)) {
+                for (int i = lo; i < hi && !*(volatile int*)&gave_up; ++i, ++n, next_tile(a.seg, walk, kTileRows)) {
                     if (walk.q / a.seg.B != e) {
                         e = walk.q / a.seg.B;
-                        if (!(ok = WAIT(w_empty, (piece & 1) ^ 1))) break;
+                        WAIT(w_empty, (piece & 1) ^ 1);
                         bar_expect(w_full, a.w_bytes);
                         for (int b = 0; b < a.blocks; ++b) {
                             const uint32_t to = base + a.off_w + b * (2 * HC * 128);
@@ -447,7 +506,7 @@ __global__ void __launch_bounds__(kWeightThreads, 1) ffn_weights_kernel(const We
                         ++piece;
                     }
                     const int s = n % a.xn;
-                    if (!(ok = WAIT(x_empty(s), (n / a.xn & 1) ^ 1))) break;
+                    WAIT(x_empty(s), (n / a.xn & 1) ^ 1);
                     bar_expect(x_land(s), a.x_bytes);
                     const uint32_t to = base + s * a.x_bytes;
                     for (int b = 0; b < a.blocks; ++b) {
@@ -459,14 +518,13 @@ __global__ void __launch_bounds__(kWeightThreads, 1) ffn_weights_kernel(const We
         }
     } else if (warp == kFixWarp) {
         int n = 0;
-        bool ok = true;
-        for (int k = blockIdx.x; ok && k < work; k += gridDim.x) {
+        for (int k = blockIdx.x; k < work; k += gridDim.x) {
             const int r = k / a.slices, lo = first_tile(r), hi = first_tile(r + 1);
             if (lo >= hi) continue;
             TileWalk walk = tile_at(a.seg, bounds, start, lo, kTileRows);
             for (int i = lo; i < hi; ++i, ++n, next_tile(a.seg, walk, kTileRows)) {
                 const int s = n % a.xn;
-                if (!(ok = WAIT(x_land(s), n / a.xn & 1))) break;
+                WAIT(x_land(s), n / a.xn & 1);
                 if (walk.left < kTileRows) {
                     clear_rows(base + s * a.x_bytes, 2 * a.blocks, walk.left, lane);
                     fence_async_shared();
@@ -475,100 +533,87 @@ __global__ void __launch_bounds__(kWeightThreads, 1) ffn_weights_kernel(const We
                 if (lane == 0) bar_arrive(x_full(s));
             }
         }
-    } else if (warp == kProductWarp) {
-        if (lane == 0) {
-            const uint32_t kind_gu = product_kind(2 * HC, BF16, false, false), kind_dh = product_kind(HC, BF16, false, true);
-            const uint32_t kind_w2 = product_kind(2 * HC, BF16, true, true), kind_w1 = product_kind(HC, BF16, true, true);
-            int n = 0, piece = 0;
-            bool ok = true, pfirst = false, plast = false;
-            // The gradients' products of unit v, which is not before the unit behind it has begun.
-            auto second = [&](int v, int pc) {
-                const int hs = v % a.hn, s = v % a.xn;
-                if (!WAIT(hid_full(hs), v / a.hn & 1)) return false;
-                if (pfirst && !WAIT(out_empty, (pc & 1) ^ 1)) return false;
-                tmem_fence_after();
-                const uint32_t x = base + s * a.x_bytes, dy = x + a.blocks * kBlockBytes, hid = base + a.off_h + hs * a.h_bytes;
-                for (int m = 0; m < halves; ++m)
-                    for (int k = 0; k < kTileRows / 16; ++k) {
-                        const uint32_t at = 2 * m * kBlockBytes + k * 16 * 128;
-                        product(tmem + m * kAcc, operand(x + at, 128, kBlockBytes), operand(hid + k * 16 * HC * 2, HC * 2, kHidBlock), kind_w2,
-                                !pfirst || k > 0);
-                        product(tmem + m * kAcc + 2 * HC, operand(dy + at, 128, kBlockBytes), operand(hid + 2 * kHidBlock + k * 16 * HC * 2, HC * 2, kHidBlock),
-                                kind_w1, !pfirst || k > 0);
-                    }
-                products_done(hid_empty(hs));
-                products_done(x_empty(s));
-                if (plast) products_done(out_full);
-                return true;
-            };
-            for (int k = blockIdx.x; ok && k < work; k += gridDim.x) {
-                const int r = k / a.slices, lo = first_tile(r), hi = first_tile(r + 1);
-                if (lo >= hi) continue;
-                TileWalk walk = tile_at(a.seg, bounds, start, lo, kTileRows);
-                int e = -1;
-                for (int i = lo; i < hi; ++i, ++n) {
-                    const bool first = walk.q / a.seg.B != e;
-                    e = walk.q / a.seg.B;
-                    TileWalk after = walk;
-                    next_tile(a.seg, after, kTileRows);
-                    const bool last = i + 1 == hi || after.q / a.seg.B != e;
-                    walk = after;
-                    const int s = n % a.xn;
-                    if (first) {
-                        if (!(ok = WAIT(w_full, piece & 1))) break;
-                        ++piece;
-                    }
-                    if (!(ok = WAIT(x_full(s), n / a.xn & 1))) break;
-                    if (!(ok = WAIT(acc_empty(n & 1), (n >> 1 & 1) ^ 1))) break;
+    } else if (warp == kFirstWarp || warp == kSecondWarp) {
+        // Both warps make the walk; each has its own waits.
+        const uint32_t lead = elected(), kind_gu = product_kind(2 * HC, BF16, false, false), kind_dh = product_kind(HC, BF16, false, true);
+        const uint32_t kind_w2 = product_kind(2 * HC, BF16, true, true), kind_w1 = product_kind(HC, BF16, true, true);
+        const bool second = warp == kSecondWarp;
+        const uint64_t x0 = operand(base, 128, second ? kBlockBytes : 0), w0 = operand(base + a.off_w, 128, 0);
+        const uint64_t wd0 = operand(base + a.off_w + a.blocks * (2 * HC * 128), HC * 2, 0), hid0 = operand(base + a.off_h, HC * 2, kHidBlock);
+        Ring x(a.xn), hid(a.hn);
+        int n = 0, piece = 0;
+        for (int k = blockIdx.x; k < work; k += gridDim.x) {
+            const int r = k / a.slices, lo = first_tile(r), hi = first_tile(r + 1);
+            if (lo >= hi) continue;
+            TileWalk walk = tile_at(a.seg, bounds, start, lo, kTileRows);
+            int e = uniform(walk.q / a.seg.B);
+            bool first = true;
+            for (int i = lo; i < hi; ++i, ++n, x.next()) {
+                next_tile(a.seg, walk, kTileRows);
+                const int next_e = uniform(walk.q / a.seg.B);
+                const bool last = i + 1 == hi || next_e != e;
+                const uint64_t xa = operand_at(x0, x.at * a.x_bytes);
+                if (!second) {
+                    if (first) WAIT(w_full, piece & 1);
+                    WAIT(x_full(x.at), x.parity);
+                    WAIT(acc_empty(n & 1), (n >> 1 & 1) ^ 1);
                     tmem_fence_after();
-                    const uint32_t d = acc0 + (n & 1) * kAcc, x = base + s * a.x_bytes, dy = x + a.blocks * kBlockBytes;
-                    const uint32_t w = base + a.off_w, wd = w + a.blocks * (2 * HC * 128);
-                    for (int q = 0; q < a.c16 / 16; ++q)
-                        product(d, operand(x + (q >> 2) * kBlockBytes + (q & 3) * 32, 128, 0), operand(w + (q >> 2) * (2 * HC * 128) + (q & 3) * 32, 128, 0),
-                                kind_gu, q > 0);
-                    for (int q = 0; q < a.c16 / 16; ++q)
-                        product(d + 2 * HC, operand(dy + (q >> 2) * kBlockBytes + (q & 3) * 32, 128, 0), operand(wd + q * 16 * HC * 2, HC * 2, 0), kind_dh, q > 0);
-                    products_done(acc_full(n & 1));
-                    if (last) products_done(w_empty);
-                    // With one stage of tiles the next unit cannot begin before this one's second products.
-                    if (a.xn > 1 && n > 0 && !(ok = second(n - 1, piece - 1 - (first ? 1 : 0)))) break;
-                    pfirst = first;
-                    plast = last;
-                    if (a.xn == 1 && !(ok = second(n, piece - 1))) break;
+                    const uint32_t d = acc0 + (n & 1) * kAcc;
+                    product_blocks(lead, d, xa, kBlockBytes, w0, 2 * HC * 128, a.c16 / 16, kind_gu);
+                    product_blocks_mn(lead, d + 2 * HC, operand_at(xa, a.blocks * kBlockBytes), kBlockBytes, wd0, 32 * HC, a.c16 / 16, kind_dh);
+                    products_done(lead, acc_full(n & 1));
+                    if (last) products_done(lead, w_empty);
+                } else {
+                    if (first) WAIT(out_empty, (piece & 1) ^ 1);
+                    WAIT(x_full(x.at), x.parity);
+                    WAIT(hid_full(hid.at), hid.parity);
+                    tmem_fence_after();
+                    const uint64_t h = operand_at(hid0, hid.at * a.h_bytes);
+                    for (int m = 0; m < halves; ++m) {
+                        const uint64_t xm = operand_at(xa, 2 * m * kBlockBytes), ym = operand_at(xm, a.blocks * kBlockBytes);
+#pragma unroll
+                        for (int q = 0; q < kTileRows / 16; ++q)
+                            product(lead, tmem + m * kAcc, operand_at(xm, q * 16 * 128), operand_at(h, q * 32 * HC), kind_w2, !first || q > 0);
+#pragma unroll
+                        for (int q = 0; q < kTileRows / 16; ++q)
+                            product(lead, tmem + m * kAcc + 2 * HC, operand_at(ym, q * 16 * 128), operand_at(h, 2 * kHidBlock + q * 32 * HC), kind_w1, !first || q > 0);
+                    }
+                    products_done(lead, hid_empty(hid.at));
+                    products_done(lead, x_empty(x.at));
+                    if (last) products_done(lead, out_full);
+                    hid.next();
                 }
+                first = last;
+                if (last) { ++piece; e = next_e; }
             }
-            if (ok && a.xn > 1 && n > 0) second(n - 1, piece - 1);
         }
     } else {
-        const int group = warp >> 2, quarter = warp & 3, row = quarter * 32 + lane;
+        const int group = warp >> 3, half = warp >> 2 & 1, quarter = warp & 3, row = quarter * 32 + lane;
         const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
         int n = 0, piece = 0;
-        bool ok = true;
-        for (int k = blockIdx.x; ok && k < work; k += gridDim.x) {
+        for (int k = blockIdx.x; k < work; k += gridDim.x) {
             const int r = k / a.slices, c = k - r * a.slices, lo = first_tile(r), hi = first_tile(r + 1);
             if (lo >= hi) continue;
             TileWalk walk = tile_at(a.seg, bounds, start, lo, kTileRows);
-            for (int i = lo; ok && i < hi;) {
+            for (int i = lo; i < hi;) {
                 const int e = walk.q / a.seg.B;
-                for (; ok && i < hi && walk.q / a.seg.B == e; ++i, ++n, next_tile(a.seg, walk, kTileRows)) {
+                for (; i < hi && walk.q / a.seg.B == e; ++i, ++n, next_tile(a.seg, walk, kTileRows)) {
                     if ((n & 1) != group) continue;
                     const int hs = n % a.hn;
-                    if (!(ok = WAIT(acc_full(group), n >> 1 & 1))) break;
-                    if (!(ok = WAIT(hid_empty(hs), (n / a.hn & 1) ^ 1))) break;
+                    WAIT(acc_full(group), n >> 1 & 1);
                     tmem_fence_after();
-                    hidden_chunk<GRAD_X, HC, ACT, BF16, true>(acc0 + group * kAcc + lanes, base + a.off_h + hs * a.h_bytes, row);
-                    tmem_fence_before();
-                    bar_arrive(acc_empty(group));
-                    fence_async_shared();
-                    bar_arrive(hid_full(hs));
+                    hidden_half<GRAD_X, HC, ACT, BF16, true>(acc0 + group * kAcc + lanes, half, base + a.off_h + hs * a.h_bytes, row, acc_empty(group),
+                                                                 hid_empty(hs), (n / a.hn & 1) ^ 1, &gave_up, a.seg.status);
+                        fence_async_shared();
+                    warp_arrive(hid_full(hs));
                 }
-                if (!ok || !(ok = WAIT(out_full, piece & 1))) break;
+                WAIT(out_full, piece & 1);
                 ++piece;
                 tmem_fence_after();
                 float* part = a.part + ((size_t)(r + e) * a.slices + c) * kAcc * a.C;
                 for (int m = 0; m < halves; ++m) {
                     const int ch = m * 128 + row;
-                    for (int j = group * 48; j < group * 48 + 48; j += 16) {
+                    for (int j = 16 * (warp >> 2); j < kAcc; j += 64) {
                         uint32_t v[16];
                         tmem_load(v, tmem + m * kAcc + j + lanes);
                         tmem_wait(v);
@@ -578,7 +623,7 @@ __global__ void __launch_bounds__(kWeightThreads, 1) ffn_weights_kernel(const We
                     }
                 }
                 tmem_fence_before();
-                bar_arrive(out_empty);
+                warp_arrive(out_empty);
             }
         }
     }
@@ -705,8 +750,9 @@ int launch_rows(emc2_bridge* h, const FfnCall& f, void* out, cudaStream_t st) {
     const bool tight = MODE == GRAD_X && a.c16 > 128;
     a.xn = tight ? 1 : NT; a.gn = 2; a.dn = tight ? 1 : 2; a.hn = tight ? 1 : 2;
     auto room = [&] { return (size_t)a.xn * a.x_bytes + (size_t)a.gn * a.g_bytes + (size_t)a.dn * a.d_bytes + (size_t)a.hn * a.h_bytes + 1024; };
-    while (a.xn < kMaxStages && room() + a.x_bytes <= kMaxShared) ++a.xn;
-    while (a.gn < kMaxStages && a.dn > 1 && room() + a.g_bytes + a.d_bytes <= kMaxShared) { ++a.gn; ++a.dn; }
+    // The gradient's Wg and Wu stay for both products of a chunk: a third stage before a second tile of rows.
+    if (MODE == GRAD_X && !tight && room() + a.g_bytes + a.d_bytes <= kMaxShared) { ++a.gn; ++a.dn; }
+    while (a.xn < 2 * NT && room() + a.x_bytes <= kMaxShared) ++a.xn;
     a.off_g = a.xn * a.x_bytes;
     a.off_d = a.off_g + a.gn * a.g_bytes;
     a.off_h = a.off_d + a.dn * a.d_bytes;

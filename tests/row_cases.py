@@ -65,7 +65,7 @@ def ffn_reference(x, wg, wu, wd, act, dy=None):
 
     The bounds follow the roundings.  A sum of n products on the tensor cores is counted 4 u32 per term: it is added in fp32,
     whose adder may cut instead of round (2 u32 a term) and align terms to the largest (2 more).  The activations are off by
-    2^-18 of themselves (fast exponential and quotient).  Values between two products are rounded to the type, u of themselves
+    2^-18 of themselves (fast exponential and reciprocal), but SiLU on bf16 rows, whose 1 / (1 + exp(-g)) is off by 2^-12.  Values between two products are rounded to the type, u of themselves
     and half a step of its smallest numbers; so are the results."""
     dtype = x.dtype
     u, tiny, s = unit(dtype), torch.finfo(dtype).smallest_normal * torch.finfo(dtype).eps / 2, 4 * 2.0 ** -24
@@ -79,7 +79,10 @@ def ffn_reference(x, wg, wu, wd, act, dy=None):
     err_g, err_u = (C + 16) * s * (x.abs() @ wg.abs().t()), (C + 16) * s * (x.abs() @ wu.abs().t())
     a, da, slope, slope2 = activation(g, act)
     fast = 2.0 ** -18
-    err_a = slope * err_g + fast * (a.abs() + 2.0 ** -6 * g.abs())
+    quick = 1.01 * 2.0 ** -12 if act == "silu" and dtype == torch.bfloat16 else 0.0
+    err_a = slope * err_g + fast * (a.abs() + 2.0 ** -6 * g.abs()) + quick * g.abs()
+    if act == "gelu":
+        err_a = err_a + (0.75e-7 + 2.0 ** -22) * g.abs()      # of the formula used for the normal distribution, and its rounding
     h = a * up
     err_h = rounded(h, err_a * (up.abs() + err_u) + a.abs() * err_u + 2 * s * h.abs())
     y = h @ wd.t()
@@ -90,7 +93,7 @@ def ffn_reference(x, wg, wu, wd, act, dy=None):
     n = x.shape[0]
     dh = dy @ wd
     err_dh = (C + 16) * s * (dy.abs() @ wd.abs())
-    err_da = slope2 * err_g + 2 * fast * (1 + g.abs())
+    err_da = slope2 * err_g + 2 * fast * (1 + g.abs()) + quick * (1 + 2 * g.abs())       # s + g s (1 - s), s off by `quick`
     dg, du = dh * up * da, dh * a
     err_dg = rounded(dg, err_dh * ((up * da).abs()) + (dh.abs() + err_dh) * (err_u * (da.abs() + err_da) + up.abs() * err_da) + 3 * s * dg.abs())
     err_du = rounded(du, err_dh * a.abs() + (dh.abs() + err_dh) * err_a + 2 * s * du.abs())
