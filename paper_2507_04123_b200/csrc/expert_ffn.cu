@@ -6,7 +6,9 @@
 //
 // All products run on the tensor cores (tcgen05, fp32 accumulators in TMEM).  Nothing of width H reaches device memory:
 // tiles of 128 rows stay in shared memory while the hidden units pass by in chunks, whose weights are copied in beside the
-// products.  What lies between the two products of a chunk (h, or dg and du) is rounded to the rows' type, as the tensor
+// products.  What bounds the kernels is shared memory: a product of 128 x N x 16 reads (128 + N) * 32 bytes at about 110 bytes
+// a clock, which is longer than it computes below N = 200, and the copies and stores share that rate.  So the hidden
+// values go back to TMEM for the second product of y and dx, as its A, and chunks are as wide as TMEM allows.  What lies between the two products of a chunk (h, or dg and du) is rounded to the rows' type, as the tensor
 // cores take it; all sums are held in fp32, results are rounded once.
 //
 // Warps of several kinds pass tiles along with mbarriers: one thread copies (tiled bulk copies), one issues the products
@@ -21,7 +23,7 @@ namespace {
 
 constexpr int kTileRows = 128;
 constexpr int kBlockBytes = kTileRows * 128;     // a tile's 64 columns
-constexpr int kCopyWarp = 16, kFirstWarp = 17, kSecondWarp = 18, kFixWarp = 19;
+constexpr int kEpilogueWarps = 16, kCopyWarp = 16, kFirstWarp = 17, kSecondWarp = 18, kFixWarp = 19;
 constexpr int kRowThreads = 608, kWeightThreads = 640;
 constexpr int kTmemColumns = 512;
 constexpr int kMaxFfnChannels = 256, kMaxFfnHidden = 8192;
@@ -143,7 +145,13 @@ __device__ __forceinline__ uint32_t swizzled(int r, int piece) {
     return HC == 64 ? r * 128 + ((piece ^ (r & 7)) << 4) : r * 64 + ((piece ^ ((r >> 1) & 3)) << 4);
 }
 
+// The same for a block of `width` columns: 64, 32 or 16.
+__device__ __forceinline__ uint32_t swizzled(int width, int r, int piece) {
+    return width == 64 ? swizzled<64>(r, piece) : width == 32 ? swizzled<32>(r, piece) : r * 32 + ((piece ^ ((r >> 2) & 1)) << 4);
+}
+
 // Columns c .. c + 7 of a chunk, at j of the arrays: the values that go on to the second product, a 16-byte piece of row r.
+// `to`: where the row's values go, in TMEM for the rows' kernels, in shared memory (as B operands) for the weights'.
 template <int MODE, int HC, int ACT, bool BF16, bool WITH_H, int W>
 __device__ __forceinline__ void hidden8(const uint32_t (&g)[W], const uint32_t (&u)[W], const uint32_t (&dh)[W], int j0, uint32_t to, int r, int c) {
     constexpr uint32_t kBlock = kTileRows * HC * 2;
@@ -152,7 +160,7 @@ __device__ __forceinline__ void hidden8(const uint32_t (&g)[W], const uint32_t (
     for (int i = 0; i < 4; ++i) {
         const int j = j0 + 2 * i;
         uint32_t first = g[j];
-        if (WITH_H && i == 2) asm volatile("" : "+r"(first));     // half a piece after the other, see hidden_half
+        if (WITH_H) asm volatile("" : "+r"(first));                // and pair by pair here, see hidden_half
         const uint64_t gg = pair(first, g[j + 1]), uu = pair(u[j], u[j + 1]);
         if (MODE == FORWARD) {
             p[i] = pack<BF16>(mul2(activation2<ACT, BF16>(gg), uu));
@@ -165,11 +173,14 @@ __device__ __forceinline__ void hidden8(const uint32_t (&g)[W], const uint32_t (
             if (WITH_H) t[i] = pack<BF16>(mul2(a, uu));
         }
     }
-    const uint32_t at = to + swizzled<HC>(r, c / 8);
-    store_shared(at, p[0], p[1], p[2], p[3]);
-    if (MODE == GRAD_X) {
+    if (!WITH_H) {
+        tmem_store(to + c / 2, p[0], p[1], p[2], p[3]);
+        if (MODE == GRAD_X) tmem_store(to + (HC + c) / 2, q[0], q[1], q[2], q[3]);
+    } else {
+        const uint32_t at = to + swizzled<HC>(r, c / 8);
+        store_shared(at, p[0], p[1], p[2], p[3]);
         store_shared(at + kBlock, q[0], q[1], q[2], q[3]);
-        if (WITH_H) store_shared(at + 2 * kBlock, t[0], t[1], t[2], t[3]);
+        store_shared(at + 2 * kBlock, t[0], t[1], t[2], t[3]);
     }
 }
 
@@ -179,30 +190,44 @@ __device__ __forceinline__ void warp_arrive(uint32_t bar) {
     if ((threadIdx.x & 31) == 0) bar_arrive(bar);
 }
 
-// The activation of half of the columns of one chunk of one tile: accumulators at `acc` (g, u and, for the gradients, dh,
-// HC columns each) of the warp's 32 rows into the blocks at `to`.  The accumulators are given back once they are in
-// registers, before the arithmetic, so that the next products run beside it.
+// The activation of half of the columns of one chunk of one tile: accumulators of g and u, HC columns each, and of dh, of the
+// warp's 32 rows into the blocks at `to`.  The accumulators are given back as soon as they are in registers (which hold 32
+// columns of two or 8 to 16 of three), before the arithmetic, so that the next products run beside it.
 template <int MODE, int HC, int ACT, bool BF16, bool WITH_H>
-__device__ __forceinline__ void hidden_half(uint32_t acc, int half, uint32_t to, int r, uint32_t acc_empty, uint32_t hid_empty, uint32_t parity,
-                                            volatile int* gave_up, int* status) {
-    constexpr int W = HC / 2;
-    uint32_t g[W], u[W], dh[W];
-    tmem_load(g, acc + half * W);
-    tmem_load(u, acc + HC + half * W);
-    if (MODE == GRAD_X) tmem_load(dh, acc + 2 * HC + half * W);
-    tmem_wait(g);
-    tmem_wait(u);
-    if (MODE == GRAD_X) tmem_wait(dh);
-    tmem_fence_before();
-    warp_arrive(acc_empty);
-    bar_wait_inline(hid_empty, parity, gave_up, status);                   // a call would save the values around it
+__device__ __forceinline__ void hidden_half(uint32_t acc, uint32_t acc_dh, int half, uint32_t to, int r, uint32_t acc_empty, uint32_t hid_empty,
+                                            uint32_t parity, volatile int* gave_up, int* status) {
+    constexpr int W = MODE == FORWARD ? HC / 2 : HC == 64 || ACT == EMC2_ACT_GELU ? 8 : 16;
 #pragma unroll
-    for (int j = 0; j < W; j += 8) {
-        if (WITH_H || (MODE == FORWARD && ACT == EMC2_ACT_GELU)) {     // one piece after the other: the arithmetic of two would not fit in the registers
+    for (int c = 0; c < HC / 2; c += W) {
+        uint32_t g[W], u[W], dh[W];
+        const int at = half * (HC / 2) + c;
+        tmem_load(g, acc + at);
+        tmem_load(u, acc + HC + at);
+        if (MODE == GRAD_X) tmem_load(dh, acc_dh + at);
+        tmem_wait(g);
+        tmem_wait(u);
+        if (MODE == GRAD_X) tmem_wait(dh);
+        if (c + W == HC / 2) {
+            tmem_fence_before();
+            warp_arrive(acc_empty);
+        }
+        if (c == 0) {
+            bar_wait_inline(hid_empty, parity, gave_up, status);           // a call would save the values around it
+            __syncwarp();                                                  // stores to TMEM, and its loads, are for whole warps
+        }
+#pragma unroll
+        for (int j = 0; j < W; j += 8) {
+            // One piece after the other: the arithmetic of two would not fit in the registers.
 #pragma unroll
             for (int i = j; i < j + 8; ++i) asm volatile("" : "+r"(g[i]));
+            hidden8<MODE, HC, ACT, BF16, WITH_H>(g, u, dh, j, to, r, at + j);
         }
-        hidden8<MODE, HC, ACT, BF16, WITH_H>(g, u, dh, j, to, r, half * W + j);
+    }
+    if (WITH_H) {
+        fence_async_shared();
+    } else {
+        tmem_wait_stores();
+        tmem_fence_before();
     }
 }
 
@@ -210,19 +235,23 @@ __device__ __forceinline__ void hidden_half(uint32_t acc, int half, uint32_t to,
 struct RowArgs {
     RowSegments seg;
     void* out;
-    int C, H, c16, blocks, chunks;          // c16: C rounded up to 16; blocks of 64 columns; chunks of HC hidden units
-    int xn, gn, dn, hn;                     // stages of the rows' tiles, of Wg and Wu, of Wd, of the hidden values
-    uint32_t off_g, off_d, off_h;           // in the dynamic shared memory, behind the rows' tiles
-    uint32_t x_bytes, g_bytes, d_bytes, h_bytes;   // of a stage
+    int C, H, c16, chunks;                  // c16: C rounded up to 16; chunks of HC hidden units
+    int full, tail;                         // blocks of 64 columns, and the columns of a narrower one behind them: 0, 16 or 32
+    int xn, gn, dn;                         // stages of the rows' tiles, of Wg and Wu, of Wd
+    uint32_t off_g, off_d;                  // in the dynamic shared memory, behind the rows' tiles
+    uint32_t x_bytes, g_bytes, d_bytes;     // of a stage
+    uint32_t tile_bytes;                    // of one tensor's tile
 };
 struct Maps {
-    CUtensorMap x, dy, gate, up, down;
+    CUtensorMap x, dy, gate, up, down, out;
+    CUtensorMap x_tail, dy_tail, gate_tail, up_tail, out_tail;              // of the last block of columns, where it is narrower
 };
 
 template <int MODE, int HC, int NT, int ACT, bool BF16>
 __global__ void __launch_bounds__(kRowThreads, 1) ffn_rows_kernel(const RowArgs a, const __grid_constant__ Maps maps) {
-    constexpr int kAcc = (MODE == FORWARD ? 2 : 3) * HC;               // columns of an accumulator
-    constexpr int kHidBlock = kTileRows * HC * 2;
+    // TMEM: the output of NT tiles, two accumulators of g and u, for dx two of dh, and the hidden values of two units, or of
+    // one where 64 units of dg and du leave no room (up to 64 channels then, 96 for y).
+    constexpr int kHid = MODE == GRAD_X && HC == 64 ? 1 : 2, kHidColumns = MODE == FORWARD ? HC / 2 : HC;
     extern __shared__ uint8_t dynamic[];
     __shared__ __align__(8) uint64_t bars[4 * kMaxStages * 2 + 16];
     __shared__ uint32_t tmem_at;
@@ -242,6 +271,7 @@ __global__ void __launch_bounds__(kRowThreads, 1) ffn_rows_kernel(const RowArgs 
     auto hid_empty = [&](int s) { return bar0 + 8 * (30 + s); };
     auto out_full = [&](int t) { return bar0 + 8 * (32 + t); };
     auto out_empty = [&](int t) { return bar0 + 8 * (34 + t); };
+    auto staged = [&](int s) { return bar0 + 8 * (36 + s); };
 
     // The tables lie where the tiles come later.
     int* bounds = reinterpret_cast<int*>(dynamic + (base - smem_u32(dynamic)));
@@ -258,6 +288,7 @@ __global__ void __launch_bounds__(kRowThreads, 1) ffn_rows_kernel(const RowArgs 
             bar_init(x_full(s), 1); bar_init(x_empty(s), 1);
             bar_init(g_full(s), 1); bar_init(g_empty(s), 1);
             bar_init(d_full(s), 1); bar_init(d_empty(s), 1);
+            bar_init(staged(s), NT == 2 ? 8 : 16);
         }
         for (int s = 0; s < 2; ++s) {
             bar_init(acc_full(s), 1); bar_init(acc_empty(s), 8);
@@ -272,42 +303,92 @@ __global__ void __launch_bounds__(kRowThreads, 1) ffn_rows_kernel(const RowArgs 
     __syncthreads();
     tmem_fence_after();
     const uint32_t tmem = uniform(tmem_at);
-    const uint32_t acc0 = tmem + NT * a.c16;                           // behind the output's accumulators
+    const uint32_t acc0 = tmem + NT * a.c16, dh0 = acc0 + 4 * HC, hid0 = dh0 + (MODE == GRAD_X ? 2 * HC : 0);
     const int items = uniform(hi - lo), units = items * a.chunks * NT;
 #define WAIT(bar, parity) bar_wait(bar, parity, &gave_up, a.seg.status)
 
     if (warp == kCopyWarp) {
+        // One thread copies rows and weights, each as soon as a stage of theirs is free, and stores finished tiles from where
+        // their rows were: the wait for one must not hold up the others.
         if (lane == 0) {
-            Ring x(a.xn), g(a.gn), d(a.dn);
-            for (int it = 0; it < items && !*(volatile int*)&gave_up; ++it, next_tile(a.seg, walk, kTileRows * NT)) {
-                const int e = walk.q / a.seg.B;
-                for (int t = 0; t < NT; ++t, x.next()) {
-                    WAIT(x_empty(x.at), x.parity ^ 1);
-                    bar_expect(x_full(x.at), a.x_bytes);
-                    const uint32_t to = base + x.at * a.x_bytes;
-                    for (int b = 0; b < a.blocks; ++b) {
-                        copy_tile(to + b * kBlockBytes, &maps.x, 64 * b, walk.row + t * kTileRows, x_full(x.at));
-                        if (MODE == GRAD_X) copy_tile(to + (a.blocks + b) * kBlockBytes, &maps.dy, 64 * b, walk.row + t * kTileRows, x_full(x.at));
-                    }
+            Ring x(a.xn), g(a.gn), d(a.dn), done(a.xn);
+            TileWalk rows = walk, stored = walk;
+            int t = 0, left = items * NT, st = 0, pending = items * NT;   // tiles to copy, tiles to store
+            auto copy_rows = [&] {
+                bar_expect(x_full(x.at), a.x_bytes);
+                const uint32_t to = base + x.at * a.x_bytes;
+                const int row = rows.row + t * kTileRows;
+                for (int b = 0; b < a.full; ++b) {
+                    copy_tile(to + b * kBlockBytes, &maps.x, 64 * b, row, x_full(x.at));
+                    if (MODE == GRAD_X) copy_tile(to + a.tile_bytes + b * kBlockBytes, &maps.dy, 64 * b, row, x_full(x.at));
                 }
+                if (a.tail) {
+                    copy_tile(to + a.full * kBlockBytes, &maps.x_tail, 64 * a.full, row, x_full(x.at));
+                    if (MODE == GRAD_X) copy_tile(to + a.tile_bytes + a.full * kBlockBytes, &maps.dy_tail, 64 * a.full, row, x_full(x.at));
+                }
+                x.next();
+                --left;
+                if (++t == NT) { t = 0; next_tile(a.seg, rows, kTileRows * NT); }
+            };
+            auto store_rows = [&] {
+                const int row = stored.row + st * kTileRows;
+                if (stored.left - st * kTileRows >= kTileRows) {       // a ragged tile's rows have left directly
+                    for (int b = 0; b < a.full; ++b) store_tile(&maps.out, 64 * b, row, base + done.at * a.x_bytes + b * kBlockBytes);
+                    if (a.tail) store_tile(&maps.out_tail, 64 * a.full, row, base + done.at * a.x_bytes + a.full * kBlockBytes);
+                    stores_read();
+                }
+                bar_arrive(x_empty(done.at));
+                done.next();
+                --pending;
+                if (++st == NT) { st = 0; next_tile(a.seg, stored, kTileRows * NT); }
+            };
+            auto poll = [&] {
+                if (pending > 0 && bar_test(staged(done.at), done.parity)) store_rows();
+                if (left > 0 && bar_test(x_empty(x.at), x.parity ^ 1)) copy_rows();
+            };
+            auto wait = [&](uint32_t bar, uint32_t parity) {
+                for (int i = 0; !bar_try(bar, parity); ++i) {
+                    poll();
+                    if (i > kWaitTries) { gave_up = 1; atomicOr(a.seg.status, kStatusTimeout); }
+                    if (*(volatile int*)&gave_up) break;
+                }
+            };
+            copy_rows();
+            for (int it = 0; it < items; ++it, next_tile(a.seg, walk, kTileRows * NT)) {
+                const int e = walk.q / a.seg.B;
                 for (int j = 0; j < a.chunks && !*(volatile int*)&gave_up; ++j, g.next(), d.next()) {
-                    WAIT(g_empty(g.at), g.parity ^ 1);
+                    wait(g_empty(g.at), g.parity ^ 1);
                     bar_expect(g_full(g.at), a.g_bytes);
-                    for (int b = 0; b < a.blocks; ++b) {
-                        const uint32_t to = base + a.off_g + g.at * a.g_bytes + b * (2 * HC * 128);
-                        copy_tile(to, &maps.gate, 64 * b, j * HC, e, g_full(g.at));
-                        copy_tile(to + HC * 128, &maps.up, 64 * b, j * HC, e, g_full(g.at));
+                    const uint32_t to = base + a.off_g + g.at * a.g_bytes;
+                    // The gradients take Wg and Wu both ways: their last block is a whole one.
+                    const int whole = MODE == GRAD_X && a.tail ? a.full + 1 : a.full;
+                    for (int b = 0; b < whole; ++b) {
+                        copy_tile(to + b * (2 * HC * 128), &maps.gate, 64 * b, j * HC, e, g_full(g.at));
+                        copy_tile(to + b * (2 * HC * 128) + HC * 128, &maps.up, 64 * b, j * HC, e, g_full(g.at));
                     }
-                    WAIT(d_empty(d.at), d.parity ^ 1);
+                    if (MODE == FORWARD && a.tail) {
+                        copy_tile(to + a.full * (2 * HC * 128), &maps.gate_tail, 64 * a.full, j * HC, e, g_full(g.at));
+                        copy_tile(to + a.full * (2 * HC * 128) + HC * a.tail * 2, &maps.up_tail, 64 * a.full, j * HC, e, g_full(g.at));
+                    }
+                    wait(d_empty(d.at), d.parity ^ 1);
                     bar_expect(d_full(d.at), a.d_bytes);
                     copy_tile(base + a.off_d + d.at * a.d_bytes, &maps.down, j * HC, 0, e, d_full(d.at));
+                    poll();
                 }
             }
+            // What is left: the last tiles' results, and rows whose stage one of them held.
+            while (pending > 0 && !*(volatile int*)&gave_up) {
+                WAIT(staged(done.at), done.parity);
+                poll();
+            }
+            stores_written();
         }
     } else if (warp == kFirstWarp) {
         // Unit n is chunk j of tile t of an item.
         const uint32_t lead = elected(), kind_gu = product_kind(2 * HC, BF16, false, false), kind_dh = product_kind(HC, BF16, false, true);
-        const int steps = a.c16 / 16;
+        const int steps = 4 * a.full, tail_steps = a.tail / 16;
+        const uint64_t tail_x0 = operand(base + a.full * kBlockBytes, a.tail * 2, 0);
+        const uint64_t tail_w0 = operand(base + a.off_g + a.full * (2 * HC * 128), MODE == FORWARD ? a.tail * 2 : 128, 0);
         const uint64_t x0 = operand(base, 128, 0), w0 = operand(base + a.off_g, 128, 0), wd0 = operand(base + a.off_d, HC * 2, 0);
         Ring x(a.xn), g(a.gn), d(a.dn);
         int j = 0, t = 0;
@@ -318,16 +399,19 @@ __global__ void __launch_bounds__(kRowThreads, 1) ffn_rows_kernel(const RowArgs 
             if (j == 0) WAIT(x_full(xs), x.at + t < a.xn ? x.parity : x.parity ^ 1);
             WAIT(acc_empty(n & 1), (n >> 1 & 1) ^ 1);
             tmem_fence_after();
-            const uint32_t acc = acc0 + (n & 1) * kAcc;
-            const uint64_t xa = operand_at(x0, xs * a.x_bytes);
+            const uint32_t acc = acc0 + (n & 1) * 2 * HC;
+            const uint64_t xa = operand_at(x0, xs * a.x_bytes), xt = operand_at(tail_x0, xs * a.x_bytes);
             product_blocks(lead, acc, xa, kBlockBytes, operand_at(w0, g.at * a.g_bytes), 2 * HC * 128, steps, kind_gu);
-            if (MODE == GRAD_X)
-                product_blocks_mn(lead, acc + 2 * HC, operand_at(xa, a.blocks * kBlockBytes), kBlockBytes, operand_at(wd0, d.at * a.d_bytes), 32 * HC, steps, kind_dh);
+            product_blocks(lead, acc, xt, 0, operand_at(tail_w0, g.at * a.g_bytes), 0, tail_steps, kind_gu, steps > 0);
+            if (MODE == GRAD_X) {
+                const uint64_t wd = operand_at(wd0, d.at * a.d_bytes);
+                product_blocks_mn(lead, dh0 + (n & 1) * HC, operand_at(xa, a.tile_bytes), kBlockBytes, wd, 32 * HC, steps, kind_dh);
+                product_blocks_mn(lead, dh0 + (n & 1) * HC, operand_at(xt, a.tile_bytes), 0, operand_at(wd, steps * 32 * HC), 32 * HC, tail_steps, kind_dh, steps > 0);
+            }
             products_done(lead, acc_full(n & 1));
             // The gradients' second products take Wg and Wu again: the other warp gives them back.
             if (MODE == FORWARD && t == NT - 1) products_done(lead, g_empty(g.at));
             if (MODE == GRAD_X) products_done(lead, d_empty(d.at));
-            if (j == a.chunks - 1) products_done(lead, x_empty(xs));
             if (++t == NT) {
                 t = 0;
                 g.next();
@@ -341,69 +425,73 @@ __global__ void __launch_bounds__(kRowThreads, 1) ffn_rows_kernel(const RowArgs 
     } else if (warp == kSecondWarp) {
         const uint32_t lead = elected(), kind_out = product_kind(a.c16, BF16, false, MODE == GRAD_X);
         const uint64_t w0 = MODE == FORWARD ? operand(base + a.off_d, HC * 2, 0) : operand(base + a.off_g, 128, 2 * HC * 128);
-        const uint64_t hid0 = operand(base + a.off_h, HC * 2, 0);
-        Ring w(MODE == FORWARD ? a.dn : a.gn), hid(a.hn);
+        Ring w(MODE == FORWARD ? a.dn : a.gn);
         int j = 0, t = 0;
         uint32_t item_parity = 0;
         for (int n = 0; n < units; ++n) {
             // The first products of this unit have waited for the gradients' Wg and Wu, but not this warp.
             if (t == 0) WAIT(MODE == FORWARD ? d_full(w.at) : g_full(w.at), w.parity);
             if (j == 0) WAIT(out_empty(t), item_parity ^ 1);
-            WAIT(hid_full(hid.at), hid.parity);
+            WAIT(hid_full(n & 1), n >> 1 & 1);
             tmem_fence_after();
             const uint32_t out = tmem + t * a.c16;
-            const uint64_t h = operand_at(hid0, hid.at * a.h_bytes), ww = operand_at(w0, w.at * (MODE == FORWARD ? a.d_bytes : a.g_bytes));
-            if (MODE == FORWARD) {
+            const uint32_t h = hid0 + (kHid == 2 ? n & 1 : 0) * kHidColumns;
+            const uint64_t ww = operand_at(w0, w.at * (MODE == FORWARD ? a.d_bytes : a.g_bytes));
 #pragma unroll
-                for (int k = 0; k < HC / 16; ++k) product(lead, out, operand_at(h, 32 * k), operand_at(ww, 32 * k), kind_out, j > 0 || k > 0);
-            } else {
-#pragma unroll
-                for (int k = 0; k < 2 * HC / 16; ++k)
-                    product(lead, out, operand_at(h, k / (HC / 16) * kHidBlock + k % (HC / 16) * 32), operand_at(ww, k * 16 * 128), kind_out, j > 0 || k > 0);
-            }
-            products_done(lead, hid_empty(hid.at));
+            for (int k = 0; k < kHidColumns / 8; ++k)
+                product_tmem(lead, out, h + 8 * k, operand_at(ww, MODE == FORWARD ? 32 * k : k * 16 * 128), kind_out, j > 0 || k > 0);
+            products_done(lead, hid_empty(n & 1));
             if (t == NT - 1) products_done(lead, MODE == FORWARD ? d_empty(w.at) : g_empty(w.at));
             if (j == a.chunks - 1) products_done(lead, out_full(t));
-            hid.next();
             if (++t == NT) {
                 t = 0;
                 w.next();
                 if (++j == a.chunks) { j = 0; item_parity ^= 1; }
             }
         }
-    } else {
+    } else if (warp < kEpilogueWarps) {
         const int group = warp >> 3, half = warp >> 2 & 1, quarter = warp & 3, r = quarter * 32 + lane;
         const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
+        Ring x(a.xn);
         int n = 0;
         for (int it = 0; it < items; ++it, next_tile(a.seg, walk, kTileRows * NT)) {
             for (int k = 0; k < a.chunks * NT; ++k, ++n) {
                 if ((n & 1) != group) continue;
-                const int hs = n % a.hn;
-                WAIT(acc_full(group), n >> 1 & 1);
+                warp_wait(acc_full(group), n >> 1 & 1, &gave_up, a.seg.status);
                 tmem_fence_after();
-                hidden_half<MODE, HC, ACT, BF16, false>(acc0 + group * kAcc + lanes, half, base + a.off_h + hs * a.h_bytes, r, acc_empty(group),
-                                                            hid_empty(hs), (n / a.hn & 1) ^ 1, &gave_up, a.seg.status);
-                fence_async_shared();
-                warp_arrive(hid_full(hs));
+                // Where the hidden values were: those of unit n - 2, or n - 1, that its product has taken.  A group waits for
+                // every use of a barrier in turn (its parity says no more than whether the last use is over).
+                const int before = n - kHid, slot = before & 1;
+                hidden_half<MODE, HC, ACT, BF16, false>(acc0 + group * 2 * HC + lanes, dh0 + group * HC + lanes, half,
+                                                        hid0 + (kHid == 2 ? group : 0) * kHidColumns + lanes, r, acc_empty(group), hid_empty(slot),
+                                                        before >> 1 & 1, &gave_up, a.seg.status);
+                warp_arrive(hid_full(group));
             }
-            const int t = NT == 2 ? group : 0;
-            WAIT(out_full(t), it & 1);
+            // The result takes the place of the tile's rows, which no product reads any more, and leaves from there as
+            // whole lines (a thread's own row would be 16 bytes of each: 1,300 clocks a tile); rows of a ragged tile leave directly.
+            const int t = NT == 2 ? group : 0, xs = x.at + t < a.xn ? x.at + t : x.at + t - a.xn, left = walk.left - t * kTileRows;
+            warp_wait(out_full(t), it & 1, &gave_up, a.seg.status);
             tmem_fence_after();
-            const bool mine = t * kTileRows + r < walk.left;
+            const uint32_t stage = base + xs * a.x_bytes;
             uint16_t* to = static_cast<uint16_t*>(a.out) + (size_t)(walk.row + t * kTileRows + r) * a.C;
             for (int c = 16 * (NT == 2 ? half : 2 * group + half); c < a.c16; c += NT == 2 ? 32 : 64) {
                 uint32_t v[16];
+                __syncwarp();                                          // behind stores by some lanes
                 tmem_load(v, tmem + t * a.c16 + c + lanes);
                 tmem_wait(v);
 #pragma unroll
-                for (int k = 0; k < 16; k += 8)
-                    if (mine && c + k < a.C)
-                        *reinterpret_cast<uint4*>(to + c + k) = make_uint4(
-                            pack<BF16>(__uint_as_float(v[k]), __uint_as_float(v[k + 1])), pack<BF16>(__uint_as_float(v[k + 2]), __uint_as_float(v[k + 3])),
-                            pack<BF16>(__uint_as_float(v[k + 4]), __uint_as_float(v[k + 5])), pack<BF16>(__uint_as_float(v[k + 6]), __uint_as_float(v[k + 7])));
+                for (int k = 0; k < 16; k += 8) {
+                    const uint32_t p0 = pack<BF16>(pair(v[k], v[k + 1])), p1 = pack<BF16>(pair(v[k + 2], v[k + 3]));
+                    const uint32_t p2 = pack<BF16>(pair(v[k + 4], v[k + 5])), p3 = pack<BF16>(pair(v[k + 6], v[k + 7]));
+                    if (left >= kTileRows) store_shared(stage + (c >> 6) * kBlockBytes + swizzled(c >> 6 < a.full ? 64 : a.tail, r, (c & 63) / 8 + k / 8), p0, p1, p2, p3);
+                    else if (r < left && c + k < a.C) *reinterpret_cast<uint4*>(to + c + k) = make_uint4(p0, p1, p2, p3);
+                }
             }
             tmem_fence_before();
             warp_arrive(out_empty(t));
+            fence_async_shared();
+            warp_arrive(staged(xs));                                       // of the stage: it has no next use before this one is stored
+            for (int k = 0; k < NT; ++k) x.next();
         }
     }
     __syncwarp();
@@ -415,11 +503,9 @@ __global__ void __launch_bounds__(kRowThreads, 1) ffn_rows_kernel(const RowArgs 
 }
 
 // ---------------------------------------------------------------- weights: dWg, dWu, dWd
-constexpr int kSlice = 32;                  // hidden units whose weights a CTA holds
-
 struct WeightArgs {
     RowSegments seg;
-    float* part;                            // [ranges + E][slices][3 * kSlice][C]
+    float* part;                            // [ranges + E][slices][3 * HC][C]
     int C, H, c16, blocks, slices, ranges;
     int xn, hn;
     uint32_t off_w, off_h;
@@ -435,12 +521,12 @@ __device__ __forceinline__ void clear_rows(uint32_t tile, int blocks, int rows, 
 }
 
 // A unit of work is a slice of hidden units and a range of the tiles, with accumulators for the three gradients of the
-// slice, [C, kSlice] each (the channels in the lanes).  All slices of a range are taken at about the same time, so that its
+// slice, [C, HC] each (the channels in the lanes).  All slices of a range are taken at about the same time, so that its
 // tiles are read from device memory once.  A range that meets several experts has a part of the result for each: entry
 // r + e of `part`, which along the run of all tiles no other pair of range and expert has.
-template <int ACT, bool BF16>
+template <int HC, int ACT, bool BF16>
 __global__ void __launch_bounds__(kWeightThreads, 1) ffn_weights_kernel(const WeightArgs a, const __grid_constant__ Maps maps) {
-    constexpr int HC = kSlice, kAcc = 3 * HC, kHidBlock = kTileRows * HC * 2;
+    constexpr int kOut = 3 * HC, kTwoDh = HC == 32 ? 1 : 0, kHidBlock = kTileRows * HC * 2;
     extern __shared__ uint8_t dynamic[];
     __shared__ __align__(8) uint64_t bars[32];
     __shared__ int bounds[kMaxBounds];
@@ -480,7 +566,7 @@ __global__ void __launch_bounds__(kWeightThreads, 1) ffn_weights_kernel(const We
     tmem_fence_after();
     const uint32_t tmem = uniform(tmem_at);
     const int halves = (a.c16 + 127) / 128;                            // of the channels, 128 lanes each
-    const uint32_t acc0 = tmem + 2 * kAcc;
+    const uint32_t acc0 = tmem + halves * kOut, dh0 = acc0 + 4 * HC;
     // Every role makes the same walk: for each unit of work its tiles, a piece for each expert.
     auto first_tile = [&](int r) { return (int)((long long)total * r / a.ranges); };
 
@@ -558,27 +644,30 @@ __global__ void __launch_bounds__(kWeightThreads, 1) ffn_weights_kernel(const We
                     WAIT(x_full(x.at), x.parity);
                     WAIT(acc_empty(n & 1), (n >> 1 & 1) ^ 1);
                     tmem_fence_after();
-                    const uint32_t d = acc0 + (n & 1) * kAcc;
-                    product_blocks(lead, d, xa, kBlockBytes, w0, 2 * HC * 128, a.c16 / 16, kind_gu);
-                    product_blocks_mn(lead, d + 2 * HC, operand_at(xa, a.blocks * kBlockBytes), kBlockBytes, wd0, 32 * HC, a.c16 / 16, kind_dh);
+                    product_blocks(lead, acc0 + (n & 1) * 2 * HC, xa, kBlockBytes, w0, 2 * HC * 128, a.c16 / 16, kind_gu);
+                    if (!kTwoDh && n > 0) {
+                        WAIT(acc_empty((n - 1) & 1), (n - 1) >> 1 & 1);
+                        tmem_fence_after();
+                    }
+                    product_blocks_mn(lead, dh0 + kTwoDh * (n & 1) * HC, operand_at(xa, a.blocks * kBlockBytes), kBlockBytes, wd0, 32 * HC, a.c16 / 16, kind_dh);
                     products_done(lead, acc_full(n & 1));
                     if (last) products_done(lead, w_empty);
                 } else {
                     if (first) WAIT(out_empty, (piece & 1) ^ 1);
                     WAIT(x_full(x.at), x.parity);
-                    WAIT(hid_full(hid.at), hid.parity);
+                    WAIT(hid_full(n & 1), n >> 1 & 1);
                     tmem_fence_after();
                     const uint64_t h = operand_at(hid0, hid.at * a.h_bytes);
                     for (int m = 0; m < halves; ++m) {
                         const uint64_t xm = operand_at(xa, 2 * m * kBlockBytes), ym = operand_at(xm, a.blocks * kBlockBytes);
 #pragma unroll
                         for (int q = 0; q < kTileRows / 16; ++q)
-                            product(lead, tmem + m * kAcc, operand_at(xm, q * 16 * 128), operand_at(h, q * 32 * HC), kind_w2, !first || q > 0);
+                            product(lead, tmem + m * kOut, operand_at(xm, q * 16 * 128), operand_at(h, q * 32 * HC), kind_w2, !first || q > 0);
 #pragma unroll
                         for (int q = 0; q < kTileRows / 16; ++q)
-                            product(lead, tmem + m * kAcc + 2 * HC, operand_at(ym, q * 16 * 128), operand_at(h, 2 * kHidBlock + q * 32 * HC), kind_w1, !first || q > 0);
+                            product(lead, tmem + m * kOut + 2 * HC, operand_at(ym, q * 16 * 128), operand_at(h, 2 * kHidBlock + q * 32 * HC), kind_w1, !first || q > 0);
                     }
-                    products_done(lead, hid_empty(hid.at));
+                    products_done(lead, hid_empty(n & 1));
                     products_done(lead, x_empty(x.at));
                     if (last) products_done(lead, out_full);
                     hid.next();
@@ -587,7 +676,7 @@ __global__ void __launch_bounds__(kWeightThreads, 1) ffn_weights_kernel(const We
                 if (last) { ++piece; e = next_e; }
             }
         }
-    } else {
+    } else if (warp < kEpilogueWarps) {
         const int group = warp >> 3, half = warp >> 2 & 1, quarter = warp & 3, row = quarter * 32 + lane;
         const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
         int n = 0, piece = 0;
@@ -600,22 +689,24 @@ __global__ void __launch_bounds__(kWeightThreads, 1) ffn_weights_kernel(const We
                 for (; i < hi && walk.q / a.seg.B == e; ++i, ++n, next_tile(a.seg, walk, kTileRows)) {
                     if ((n & 1) != group) continue;
                     const int hs = n % a.hn;
-                    WAIT(acc_full(group), n >> 1 & 1);
+                    warp_wait(acc_full(group), n >> 1 & 1, &gave_up, a.seg.status);
                     tmem_fence_after();
-                    hidden_half<GRAD_X, HC, ACT, BF16, true>(acc0 + group * kAcc + lanes, half, base + a.off_h + hs * a.h_bytes, row, acc_empty(group),
-                                                                 hid_empty(hs), (n / a.hn & 1) ^ 1, &gave_up, a.seg.status);
-                        fence_async_shared();
-                    warp_arrive(hid_full(hs));
+                    const int before = n - a.hn, slot = before & 1;        // see ffn_rows_kernel
+                    hidden_half<GRAD_X, HC, ACT, BF16, true>(acc0 + group * 2 * HC + lanes, dh0 + kTwoDh * group * HC + lanes, half,
+                                                             base + a.off_h + hs * a.h_bytes, row, acc_empty(group), hid_empty(slot), before >> 1 & 1,
+                                                             &gave_up, a.seg.status);
+                    warp_arrive(hid_full(group));
                 }
-                WAIT(out_full, piece & 1);
+                warp_wait(out_full, piece & 1, &gave_up, a.seg.status);
                 ++piece;
                 tmem_fence_after();
-                float* part = a.part + ((size_t)(r + e) * a.slices + c) * kAcc * a.C;
+                float* part = a.part + ((size_t)(r + e) * a.slices + c) * kOut * a.C;
                 for (int m = 0; m < halves; ++m) {
                     const int ch = m * 128 + row;
-                    for (int j = 16 * (warp >> 2); j < kAcc; j += 64) {
+                    for (int j = 16 * (warp >> 2); j < kOut; j += 64) {
                         uint32_t v[16];
-                        tmem_load(v, tmem + m * kAcc + j + lanes);
+                        __syncwarp();
+                        tmem_load(v, tmem + m * kOut + j + lanes);
                         tmem_wait(v);
 #pragma unroll
                         for (int q = 0; q < 16; ++q)
@@ -642,42 +733,45 @@ struct WeightSumArgs {
     void* gate;
     void* up;
     void* down;
-    int C, H, slices, ranges, type;
+    int C, H, slice, slices, ranges, type;
 };
 
-// dW of 32 hidden units and 32 channels: the parts of the ranges that met the expert, in their order.
+// dW of eight hidden units and 32 channels: the parts of the ranges that met the expert, every eighth by one warp, then the
+// warps' sums in their order.
+constexpr int kSumUnits = 8;
 __global__ void __launch_bounds__(256) ffn_sum_kernel(WeightSumArgs a) {
     __shared__ int bounds[kMaxBounds];
     __shared__ int start[kMaxSegments + 1];
-    __shared__ float tile[32][33];
+    __shared__ float sums[8][kSumUnits][33];
     load_bounds(a.seg, bounds);
     segment_starts(a.seg, bounds, kTileRows, start);
-    const int columns = (a.C + 31) / 32, c0 = blockIdx.x % columns * 32, slice = blockIdx.x / columns, kind = blockIdx.y, e = blockIdx.z, B = a.seg.B;
+    const int columns = (a.C + 31) / 32, kind = blockIdx.y, e = blockIdx.z, B = a.seg.B, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const long long total = start[B * a.seg.E], from = start[e * B], to = start[(e + 1) * B];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    float s[4] = {0.f, 0.f, 0.f, 0.f};
-    if (from < to && c0 + lane < a.C) {
-        const int r0 = (int)(((from + 1) * a.ranges - 1) / total), r1 = (int)((to * a.ranges - 1) / total);
-        for (int r = r0; r <= r1; ++r) {
-            if (total * r / a.ranges == total * (r + 1) / a.ranges) continue;
-            const float* p = a.part + (((size_t)(r + e) * a.slices + slice) * 3 * kSlice + kind * kSlice + warp) * a.C + c0 + lane;
-#pragma unroll
-            for (int k = 0; k < 4; ++k) s[k] += p[(size_t)8 * k * a.C];
-        }
-    }
+    const int r0 = from < to ? (int)(((from + 1) * a.ranges - 1) / total) : 0, r1 = from < to ? (int)((to * a.ranges - 1) / total) : -1;
     uint16_t* out = static_cast<uint16_t*>(kind == 0 ? a.gate : kind == 1 ? a.up : a.down);
+    for (int tile = blockIdx.x; tile < columns * ((a.H + kSumUnits - 1) / kSumUnits); tile += gridDim.x) {
+        const int c0 = tile % columns * 32, h0 = tile / columns * kSumUnits;
+        float s[kSumUnits];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) tile[warp + 8 * k][lane] = s[k];
-    __syncthreads();
+        for (int k = 0; k < kSumUnits; ++k) s[k] = 0.f;
+        if (c0 + lane < a.C)
+            for (int r = r0 + warp; r <= r1; r += 8) {
+                if (total * r / a.ranges == total * (r + 1) / a.ranges) continue;     // more ranges than tiles: it had none
+                const float* p = a.part + (((size_t)(r + e) * a.slices + h0 / a.slice) * 3 * a.slice + kind * a.slice + h0 % a.slice) * a.C + c0 + lane;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        if (kind < 2) {                                   // [E, H, C]
-            const int h = slice * kSlice + warp + 8 * k, ch = c0 + lane;
-            if (h < a.H && ch < a.C) out[((size_t)e * a.H + h) * a.C + ch] = (uint16_t)as_halves(s[k], 0.f, a.type);
-        } else {                                          // [E, C, H]
-            const int h = slice * kSlice + lane, ch = c0 + warp + 8 * k;
-            if (h < a.H && ch < a.C) out[((size_t)e * a.C + ch) * a.H + h] = (uint16_t)as_halves(tile[lane][warp + 8 * k], 0.f, a.type);
-        }
+                for (int k = 0; k < kSumUnits; ++k) s[k] += p[(size_t)k * a.C];
+            }
+#pragma unroll
+        for (int k = 0; k < kSumUnits; ++k) sums[warp][k][lane] = s[k];
+        __syncthreads();
+        // Consecutive threads write consecutive addresses: channels of [E, H, C], hidden units of [E, C, H].
+        const int h = kind < 2 ? warp : threadIdx.x & 7, c = kind < 2 ? lane : threadIdx.x >> 3;
+        float v = sums[0][h][c];
+#pragma unroll
+        for (int w = 1; w < 8; ++w) v += sums[w][h][c];
+        if (h0 + h < a.H && c0 + c < a.C)
+            out[kind < 2 ? ((size_t)e * a.H + h0 + h) * a.C + c0 + c : ((size_t)e * a.C + c0 + c) * a.H + h0 + h] = (uint16_t)as_halves(v, 0.f, a.type);
+        __syncthreads();
     }
 }
 
@@ -697,14 +791,14 @@ EncodeTiled encoder() {
     return f;
 }
 
-// [z, y, x] of 16-bit values, copied as boxes of x_box columns (64 or 32, with the swizzle of that width) and y_box rows;
+// [z, y, x] of 16-bit values, copied as boxes of x_box columns (64, 32 or 16, with the swizzle of that width) and y_box rows;
 // what lies outside reads as zeros.
 bool encode(CUtensorMap* map, const void* p, int type, uint64_t x, uint64_t y, uint64_t z, int x_box, int y_box) {
     const cuuint64_t dims[3] = {x, y, z}, strides[2] = {x * 2, x * y * 2};
     const cuuint32_t box[3] = {(cuuint32_t)x_box, (cuuint32_t)y_box, 1}, step[3] = {1, 1, 1};
     const EncodeTiled f = encoder();
     return f && f(map, type == EMC2_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, z ? 3 : 2, const_cast<void*>(p), dims,
-                  strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, x_box == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+                  strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, x_box == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : x_box == 32 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_32B,
                   CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
@@ -716,12 +810,18 @@ struct FfnCall {
     const void* gate;
     const void* up;
     const void* down;
+    void* out;
 };
 
-bool make_maps(const FfnCall& f, int hc, Maps* m) {
+bool make_maps(const FfnCall& f, int hc, int tail, Maps* m) {
     const int c16 = (f.C + 15) / 16 * 16;
     const uint64_t rows = (uint64_t)f.seg.B * f.seg.N, E = (uint64_t)f.seg.E;
+    if (tail && !(encode(&m->x_tail, f.x, f.type, f.C, rows, 0, tail, kTileRows) && encode(&m->dy_tail, f.dy ? f.dy : f.x, f.type, f.C, rows, 0, tail, kTileRows) &&
+                  encode(&m->out_tail, f.out, f.type, f.C, rows, 0, tail, kTileRows) && encode(&m->gate_tail, f.gate, f.type, f.C, f.H, E, tail, hc) &&
+                  encode(&m->up_tail, f.up, f.type, f.C, f.H, E, tail, hc)))
+        return false;
     return encode(&m->x, f.x, f.type, f.C, rows, 0, 64, kTileRows) && encode(&m->dy, f.dy ? f.dy : f.x, f.type, f.C, rows, 0, 64, kTileRows) &&
+           encode(&m->out, f.out, f.type, f.C, rows, 0, 64, kTileRows) &&
            encode(&m->gate, f.gate, f.type, f.C, f.H, E, 64, hc) && encode(&m->up, f.up, f.type, f.C, f.H, E, 64, hc) &&
            encode(&m->down, f.down, f.type, f.H, f.C, E, hc, c16);
 }
@@ -735,32 +835,39 @@ int launch_ffn(emc2_bridge* h, int kind, F kernel, const A& a, const Maps& m, in
     return check_cuda(h, cudaGetLastError());
 }
 
+// Tiles of 128 * NT rows there can be.
+long long row_tiles(const RowSegments& s, int NT) {
+    return ((long long)s.B * s.N + kTileRows * NT - 1) / (kTileRows * NT) + (long long)s.B * s.E;
+}
+
 template <int MODE, int HC, int NT>
-int launch_rows(emc2_bridge* h, const FfnCall& f, void* out, cudaStream_t st) {
+int launch_rows(emc2_bridge* h, const FfnCall& f, cudaStream_t st) {
     RowArgs a;
-    a.seg = f.seg; a.out = out; a.C = f.C; a.H = f.H;
+    a.seg = f.seg; a.out = f.out; a.C = f.C; a.H = f.H;
     a.c16 = (f.C + 15) / 16 * 16;
-    a.blocks = (f.C + 63) / 64;
     a.chunks = (f.H + HC - 1) / HC;
-    a.x_bytes = (MODE == FORWARD ? 1 : 2) * a.blocks * kBlockBytes;          // these are all multiples of 1 KB
-    a.g_bytes = a.blocks * 2 * HC * 128;
+    a.full = a.c16 / 64;
+    a.tail = a.c16 % 64;
+    if (a.tail == 48) { a.tail = 0; ++a.full; }                              // no swizzle of that width
+    a.tile_bytes = a.full * kBlockBytes + kTileRows * a.tail * 2;            // these are all multiples of 1 KB
+    a.x_bytes = (MODE == FORWARD ? 1 : 2) * a.tile_bytes;
+    a.g_bytes = 2 * HC * (MODE == FORWARD ? a.full * 128 + a.tail * 2 : (a.full + (a.tail > 0)) * 128);
     a.d_bytes = a.c16 * HC * 2;
-    a.h_bytes = (MODE == FORWARD ? 1 : 2) * kTileRows * HC * 2;
     // As many stages as there is room for: first two of each, then more of the rows.
-    const bool tight = MODE == GRAD_X && a.c16 > 128;
-    a.xn = tight ? 1 : NT; a.gn = 2; a.dn = tight ? 1 : 2; a.hn = tight ? 1 : 2;
-    auto room = [&] { return (size_t)a.xn * a.x_bytes + (size_t)a.gn * a.g_bytes + (size_t)a.dn * a.d_bytes + (size_t)a.hn * a.h_bytes + 1024; };
-    // The gradient's Wg and Wu stay for both products of a chunk: a third stage before a second tile of rows.
-    if (MODE == GRAD_X && !tight && room() + a.g_bytes + a.d_bytes <= kMaxShared) { ++a.gn; ++a.dn; }
-    while (a.xn < 2 * NT && room() + a.x_bytes <= kMaxShared) ++a.xn;
+    a.xn = NT; a.gn = 2; a.dn = 2;
+    auto room = [&] { return (size_t)a.xn * a.x_bytes + (size_t)a.gn * a.g_bytes + (size_t)a.dn * a.d_bytes + 1024; };
+    // What is left goes to a third stage of the weights, the next item's rows, a fourth.
+    auto more_weights = [&](int n) { while (a.gn < n && room() + a.g_bytes + a.d_bytes <= kMaxShared) { ++a.gn; ++a.dn; } };
+    auto more_rows = [&](int n) { while (a.xn < n && room() + a.x_bytes <= kMaxShared) ++a.xn; };
+    more_weights(3);
+    more_rows(2 * NT);
+    more_weights(kMaxStages);
     a.off_g = a.xn * a.x_bytes;
     a.off_d = a.off_g + a.gn * a.g_bytes;
-    a.off_h = a.off_d + a.dn * a.d_bytes;
     Maps m;
-    if (!make_maps(f, HC, &m)) return EMC2_ERR_CUDA;
+    if (!make_maps(f, HC, a.tail, &m)) return EMC2_ERR_CUDA;
     const size_t shared = std::max(room(), (size_t)(kMaxBounds + kMaxSegments + 1) * 4 + 1024);
-    const long long tiles = ((long long)f.seg.B * f.seg.N + kTileRows * NT - 1) / (kTileRows * NT) + (long long)f.seg.B * f.seg.E;
-    const int ctas = (int)std::min<long long>(tiles, h->num_sms), kind = MODE == FORWARD ? K_FFN : K_FFN_GRAD_X;
+    const int ctas = (int)std::min<long long>(row_tiles(f.seg, NT), h->num_sms), kind = MODE == FORWARD ? K_FFN : K_FFN_GRAD_X;
     const bool bf16 = f.type == EMC2_BF16;
     if (f.act == EMC2_ACT_SILU)
         return bf16 ? launch_ffn(h, kind, ffn_rows_kernel<MODE, HC, NT, EMC2_ACT_SILU, true>, a, m, ctas, kRowThreads, shared, st)
@@ -769,45 +876,70 @@ int launch_rows(emc2_bridge* h, const FfnCall& f, void* out, cudaStream_t st) {
                 : launch_ffn(h, kind, ffn_rows_kernel<MODE, HC, NT, EMC2_ACT_GELU, false>, a, m, ctas, kRowThreads, shared, st);
 }
 
-// Ranges of the tiles: four units of work per SM.
-int weight_ranges(const emc2_bridge* h, int slices) { return std::max(1, 4 * h->num_sms / slices); }
+// Ranges of the tiles: four units of work per SM, but eight tiles in each while that leaves one unit per SM.
+int weight_ranges(const emc2_bridge* h, int slices, long long tiles) {
+    const long long most = std::max(1, 4 * h->num_sms / slices), few = std::max<long long>(tiles / 8, (h->num_sms + slices - 1) / slices);
+    return (int)std::max<long long>(1, std::min({most, few, tiles}));
+}
+
+// Stages that fit: of the hidden values two, of the tiles up to three.  The product of the transposed rows takes 128
+// channels at a time: with fewer than that it reads up to one block behind a tile's last (the results go to lanes that
+// nobody reads), which the weights' room has to cover.
+template <int HC>
+size_t plan_weights(WeightArgs& a, const FfnCall& f) {
+    a.seg = f.seg; a.C = f.C; a.H = f.H;
+    a.c16 = (f.C + 15) / 16 * 16;
+    a.blocks = (f.C + 63) / 64;
+    a.slices = (f.H + HC - 1) / HC;
+    a.x_bytes = 2 * a.blocks * kBlockBytes;
+    a.w_bytes = a.blocks * 2 * HC * 128 + a.c16 * HC * 2;
+    a.h_bytes = 3 * kTileRows * HC * 2;
+    a.xn = 1; a.hn = 1;
+    constexpr size_t most = kMaxShared - 4096;                             // the tables of the segments are static here
+    auto room = [&] { return (size_t)a.xn * a.x_bytes + std::max<size_t>(a.w_bytes + (size_t)a.hn * a.h_bytes, kBlockBytes) + 1024; };
+    if (room() + a.x_bytes <= most) ++a.xn;
+    if (room() + a.h_bytes <= most) ++a.hn;
+    if (a.xn == 2 && room() + a.x_bytes <= most) ++a.xn;
+    a.off_w = a.xn * a.x_bytes;
+    a.off_h = a.off_w + a.w_bytes;
+    return room();
+}
+
+template <int HC>
+int launch_slices(emc2_bridge* h, const FfnCall& f, WeightArgs& a, cudaStream_t st) {
+    const size_t shared = plan_weights<HC>(a, f);
+    a.part = static_cast<float*>(h->rows_scratch.slab);
+    a.ranges = weight_ranges(h, a.slices, row_tiles(f.seg, 1));
+    Maps m;
+    if (!make_maps(f, HC, 0, &m)) return EMC2_ERR_CUDA;
+    const int ctas = std::min(a.ranges * a.slices, h->num_sms);
+    const bool bf16 = f.type == EMC2_BF16;
+    if (f.act == EMC2_ACT_SILU)
+        return bf16 ? launch_ffn(h, K_FFN_GRAD_W, ffn_weights_kernel<HC, EMC2_ACT_SILU, true>, a, m, ctas, kWeightThreads, shared, st)
+                    : launch_ffn(h, K_FFN_GRAD_W, ffn_weights_kernel<HC, EMC2_ACT_SILU, false>, a, m, ctas, kWeightThreads, shared, st);
+    return bf16 ? launch_ffn(h, K_FFN_GRAD_W, ffn_weights_kernel<HC, EMC2_ACT_GELU, true>, a, m, ctas, kWeightThreads, shared, st)
+                : launch_ffn(h, K_FFN_GRAD_W, ffn_weights_kernel<HC, EMC2_ACT_GELU, false>, a, m, ctas, kWeightThreads, shared, st);
+}
+
+// Slices of 64 hidden units where two stages of tiles fit beside them (up to 96 channels): half the products, each of which
+// waits for its 128 rows of A below N = 128.
+bool wide_slices(const FfnCall& f) {
+    WeightArgs a;
+    plan_weights<64>(a, f);
+    return a.c16 <= 128 && a.xn >= 2;
+}
 
 int launch_weights(emc2_bridge* h, const FfnCall& f, void* gate, void* up, void* down, cudaStream_t st) {
     WeightArgs a;
-    a.seg = f.seg; a.C = f.C; a.H = f.H;
-    a.part = static_cast<float*>(h->rows_scratch.slab);
-    a.c16 = (f.C + 15) / 16 * 16;
-    a.blocks = (f.C + 63) / 64;
-    a.slices = (f.H + kSlice - 1) / kSlice;
-    a.ranges = weight_ranges(h, a.slices);
-    a.x_bytes = 2 * a.blocks * kBlockBytes;
-    a.w_bytes = a.blocks * 2 * kSlice * 128 + a.c16 * kSlice * 2;
-    a.h_bytes = 3 * kTileRows * kSlice * 2;
-    a.xn = 1; a.hn = a.c16 > 128 ? 1 : 2;
-    // The product of the transposed rows takes 128 channels at a time: with fewer than that it reads up to one block
-    // behind a tile's last (the results go to lanes that nobody reads), which the weights' room has to cover.
-    auto room = [&] { return (size_t)a.xn * a.x_bytes + std::max<size_t>(a.w_bytes + (size_t)a.hn * a.h_bytes, kBlockBytes) + 1024; };
-    while (a.xn < 3 && room() + a.x_bytes <= kMaxShared - 4608) ++a.xn;
-    if (a.xn == 1) a.hn = 1;
-    a.off_w = a.xn * a.x_bytes;
-    a.off_h = a.off_w + a.w_bytes;
-    Maps m;
-    if (!make_maps(f, kSlice, &m)) return EMC2_ERR_CUDA;
-    const int ctas = std::min(a.ranges * a.slices, h->num_sms);
-    const bool bf16 = f.type == EMC2_BF16;
-    int rc;
-    if (f.act == EMC2_ACT_SILU)
-        rc = bf16 ? launch_ffn(h, K_FFN_GRAD_W, ffn_weights_kernel<EMC2_ACT_SILU, true>, a, m, ctas, kWeightThreads, room(), st)
-                  : launch_ffn(h, K_FFN_GRAD_W, ffn_weights_kernel<EMC2_ACT_SILU, false>, a, m, ctas, kWeightThreads, room(), st);
-    else
-        rc = bf16 ? launch_ffn(h, K_FFN_GRAD_W, ffn_weights_kernel<EMC2_ACT_GELU, true>, a, m, ctas, kWeightThreads, room(), st)
-                  : launch_ffn(h, K_FFN_GRAD_W, ffn_weights_kernel<EMC2_ACT_GELU, false>, a, m, ctas, kWeightThreads, room(), st);
+    const bool wide = wide_slices(f);
+    const int rc = wide ? launch_slices<64>(h, f, a, st) : launch_slices<32>(h, f, a, st);
     if (rc != EMC2_OK) return rc;
     WeightSumArgs s;
-    s.seg = f.seg; s.part = a.part; s.gate = gate; s.up = up; s.down = down; s.C = f.C; s.H = f.H; s.slices = a.slices; s.ranges = a.ranges;
+    s.seg = f.seg; s.part = a.part; s.gate = gate; s.up = up; s.down = down; s.C = f.C; s.H = f.H; s.slice = wide ? 64 : 32; s.slices = a.slices; s.ranges = a.ranges;
     s.type = f.type;
     LaunchScope ls(h, K_FFN_SUM, st);
-    ffn_sum_kernel<<<dim3(a.slices * ((f.C + 31) / 32), 3, f.seg.E), 256, 0, st>>>(s);
+    const int sums = (f.H + kSumUnits - 1) / kSumUnits * ((f.C + 31) / 32), most = std::max(1, 6 * h->num_sms / (3 * f.seg.E));
+    ffn_sum_kernel<<<dim3(std::min(sums, most), 3, f.seg.E), 256, 0, st>>>(s);
     return check_cuda(h, cudaGetLastError());
 }
 
@@ -828,8 +960,9 @@ size_t ffn_scratch_bytes(const emc2_bridge* h, int max_channels, int max_hidden)
     if (max_hidden <= 0) return 0;
     const int C = std::min(max_channels, kMaxFfnChannels);
     size_t most = 0;
-    for (int slices = 1; slices <= (max_hidden + kSlice - 1) / kSlice; ++slices)
-        most = std::max(most, (size_t)(weight_ranges(h, slices) + EMC2_MAX_EXPERTS) * slices * 3 * kSlice * C * sizeof(float));
+    for (int slice : {32, 64})
+        for (int slices = 1; slices <= (max_hidden + slice - 1) / slice; ++slices)
+            most = std::max(most, (size_t)(weight_ranges(h, slices, 1LL << 40) + EMC2_MAX_EXPERTS) * slices * 3 * slice * C * sizeof(float));
     return most;
 }
 
@@ -847,9 +980,11 @@ extern "C" int emc2_expert_ffn(emc2_bridge_t* h, int32_t B, int32_t N, int32_t c
     if (!d_y || d_y == d_x) return EMC2_ERR_INVALID_ARG;
     RowsDevice device(h->cfg.device);
     if (!device.ok) return EMC2_ERR_CUDA;
-    const FfnCall f = {row_segments(h, B, N, d_offsets), channels, hidden, type, act, d_x, nullptr, d_w_gate, d_w_up, d_w_down};
+    const FfnCall f = {row_segments(h, B, N, d_offsets), channels, hidden, type, act, d_x, nullptr, d_w_gate, d_w_up, d_w_down, d_y};
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-    return channels <= 128 ? launch_rows<FORWARD, 64, 2>(h, f, d_y, st) : launch_rows<FORWARD, 32, 1>(h, f, d_y, st);
+    // Chunks of hidden units, and tiles that share their weights, as TMEM has room for (see ffn_rows_kernel).
+    if (channels <= 96) return launch_rows<FORWARD, 64, 2>(h, f, st);
+    return channels <= 128 ? launch_rows<FORWARD, 32, 2>(h, f, st) : launch_rows<FORWARD, 32, 1>(h, f, st);
 }
 
 extern "C" int emc2_expert_ffn_grad(emc2_bridge_t* h, int32_t B, int32_t N, int32_t channels, int32_t hidden, int32_t type, int32_t act,
@@ -867,7 +1002,7 @@ extern "C" int emc2_expert_ffn_grad(emc2_bridge_t* h, int32_t B, int32_t N, int3
     RowsDevice device(h->cfg.device);
     if (!device.ok) return EMC2_ERR_CUDA;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-    const FfnCall f = {row_segments(h, B, N, d_offsets), channels, hidden, type, act, d_x, d_grad_y, d_w_gate, d_w_up, d_w_down};
+    const FfnCall f = {row_segments(h, B, N, d_offsets), channels, hidden, type, act, d_x, d_grad_y, d_w_gate, d_w_up, d_w_down, d_grad_x};
     if (empty) {
         const size_t bytes = (size_t)f.seg.E * hidden * channels * 2;
         cudaError_t e = cudaMemsetAsync(d_grad_gate, 0, bytes, st);
@@ -875,7 +1010,7 @@ extern "C" int emc2_expert_ffn_grad(emc2_bridge_t* h, int32_t B, int32_t N, int3
         if (e == cudaSuccess) e = cudaMemsetAsync(d_grad_down, 0, bytes, st);
         return check_cuda(h, e);
     }
-    rc = launch_rows<GRAD_X, 32, 1>(h, f, d_grad_x, st);
+    rc = channels <= 64 ? launch_rows<GRAD_X, 64, 1>(h, f, st) : launch_rows<GRAD_X, 32, 1>(h, f, st);
     if (rc == EMC2_OK) rc = launch_weights(h, f, d_grad_gate, d_grad_up, d_grad_down, st);
     return rc;
 }

@@ -21,6 +21,7 @@ __device__ __forceinline__ void bar_arrive(uint32_t bar) {
 __device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes) {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
+// Whether the phase of that parity is over; try_wait suspends the thread for a while first, test_wait does not.
 __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
     uint32_t done;
     asm volatile(
@@ -30,11 +31,20 @@ __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
         : "=r"(done) : "r"(bar), "r"(parity) : "memory");
     return done != 0;
 }
+__device__ __forceinline__ bool bar_test(uint32_t bar, uint32_t parity) {
+    uint32_t done;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+    return done != 0;
+}
 
 // A wait that ends: after kWaitTries tries it sets *gave_up, and from then on every wait of the CTA that is not over at once
 // is given up.  The CTA then runs through the rest of its steps without waiting (what it computes is void, as the status
-// says) and winds up, see leave_after_timeout.  A try suspends the thread for up to some microseconds by itself.  Only the
-// first try is in line: the warps that copy and issue products run through little else, and what they fetch counts.
+// says) and winds up, see leave_after_timeout.  A hint for a long suspension made everything 10 % slower, polling without any
+// 3 % (forward, 1.2 M rows of 80 channels).  Only the first try is in line: the warps that copy and issue products run through little else, and what they fetch counts.
 constexpr int kWaitTries = 1 << 22;
 constexpr int kStatusTimeout = 2;            // device status: EMC2_ERR_TIMEOUT
 __device__ __forceinline__ void bar_wait_inline(uint32_t bar, uint32_t parity, volatile int* gave_up, int* status) {
@@ -50,6 +60,12 @@ __device__ __noinline__ static void bar_wait_on(uint32_t bar, uint32_t parity, v
 }
 __device__ __forceinline__ void bar_wait(uint32_t bar, uint32_t parity, volatile int* gave_up, int* status) {
     if (!bar_try(bar, parity)) bar_wait_on(bar, parity, gave_up, status);
+}
+// The same by whole warps before instructions that a warp has to reach together (all loads and stores of TMEM): lanes can
+// leave the loop of a wait in different turns.
+__device__ __forceinline__ void warp_wait(uint32_t bar, uint32_t parity, volatile int* gave_up, int* status) {
+    bar_wait(bar, parity, gave_up, status);
+    __syncwarp();
 }
 // Copies and products still in flight get this long to land before the CTA gives its memory back.
 __device__ __forceinline__ void leave_after_timeout(volatile int* gave_up) {
@@ -69,6 +85,16 @@ __device__ __forceinline__ void copy_tile(uint32_t dst, const CUtensorMap* map, 
     asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
                  ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
 }
+
+// And back: the tile at src, whose reads the thread waits for with stores_read.
+__device__ __forceinline__ void store_tile(const CUtensorMap* map, int x, int y, uint32_t src) {
+    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"(map), "r"(x), "r"(y), "r"(src) : "memory");
+}
+__device__ __forceinline__ void stores_read() {
+    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+    asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+}
+__device__ __forceinline__ void stores_written() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
 
 // ---- TMEM
 __device__ __forceinline__ void tmem_alloc(uint32_t dst, uint32_t columns) {
@@ -129,6 +155,12 @@ __device__ __forceinline__ void tmem_wait(uint32_t (&a)[32]) {
                    "+r"(a[28]), "+r"(a[29]), "+r"(a[30]), "+r"(a[31])::"memory");
 }
 
+// Four columns of the warp's 32 lanes; complete after tmem_wait_stores.
+__device__ __forceinline__ void tmem_store(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+__device__ __forceinline__ void tmem_wait_stores() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
 // ---- pairs of floats in one instruction
 __device__ __forceinline__ uint64_t pair(float a, float b) {
     uint64_t r;
@@ -177,13 +209,13 @@ __device__ __forceinline__ uint64_t reciprocals(float a, float b) {
 // A whole warp comes here, with the same arguments in every lane, and its elected lane issues: the descriptors then stay in
 // uniform registers.  Issued by a thread on a branch of its own each product took 71 clocks whatever its N; so it takes
 // what the tensor core does: 52 at N = 32, 58 at 64, 72 at 128, 127 at 256 (B200; below N = 128 it waits for A, 4 KB).
-// Shared-memory operands are tiles of rows of `row_bytes` (128 or 64, with the swizzle of that width): groups of eight
+// Shared-memory operands are tiles of rows of `row_bytes` (128, 64 or 32, with the swizzle of that width): groups of eight
 // rows follow one another every 8 * row_bytes.
 //   K-major  (a row holds consecutive k of one m or n): a step of 16 k is 32 bytes further in the row
 //   MN-major (a row holds consecutive m or n of one k): a step of 16 k is 16 rows further; blocks of row_bytes / 2
 //            columns are `block` bytes apart
 __device__ __forceinline__ uint64_t operand(uint32_t addr, int row_bytes, uint32_t block) {
-    const uint64_t swizzle = row_bytes == 128 ? 2 : 4;
+    const uint64_t swizzle = row_bytes == 128 ? 2 : row_bytes == 64 ? 4 : 6;
     return (uint64_t)((addr & 0x3FFFFu) >> 4) | (uint64_t)((block & 0x3FFFFu) >> 4) << 16 | (uint64_t)((8 * row_bytes) >> 4) << 32 |
            1ull << 46 | swizzle << 61;
 }
@@ -203,6 +235,13 @@ __device__ __forceinline__ void product(uint32_t lead, uint32_t d, uint64_t a, u
         "@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
         ::"r"(d), "l"(a), "l"(b), "r"(kind), "r"((uint32_t)add), "r"(lead) : "memory");
 }
+// The same with A in TMEM: row m in lane m, two values of k per column, a step of 16 k in eight columns.
+__device__ __forceinline__ void product_tmem(uint32_t lead, uint32_t d, uint32_t a, uint64_t b, uint32_t kind, bool add) {
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t"
+        "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+        ::"r"(d), "r"(a), "l"(b), "r"(kind), "r"((uint32_t)add), "r"(lead) : "memory");
+}
 // The value of lane 0, which the compiler then knows to be the same in all lanes.
 __device__ __forceinline__ uint32_t uniform(uint32_t v) { return __shfl_sync(0xFFFFFFFFu, v, 0); }
 __device__ __forceinline__ int uniform(int v) { return __shfl_sync(0xFFFFFFFFu, v, 0); }
@@ -210,8 +249,8 @@ __device__ __forceinline__ int uniform(int v) { return __shfl_sync(0xFFFFFFFFu, 
 __device__ __forceinline__ uint64_t operand_at(uint64_t op, uint32_t bytes) { return op + (bytes >> 4); }
 // `steps` steps of 16 k with both operands K-major in blocks of 64 columns.  What is computed
 // between two products counts: four steps are written out.
-__device__ __forceinline__ void product_blocks(uint32_t lead, uint32_t d, uint64_t a, uint32_t a_block, uint64_t b, uint32_t b_block, int steps, uint32_t kind) {
-    bool add = false;
+__device__ __forceinline__ void product_blocks(uint32_t lead, uint32_t d, uint64_t a, uint32_t a_block, uint64_t b, uint32_t b_block, int steps, uint32_t kind,
+                                               bool add = false) {
     for (; steps >= 4; steps -= 4) {
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
@@ -227,8 +266,8 @@ __device__ __forceinline__ void product_blocks(uint32_t lead, uint32_t d, uint64
     }
 }
 // The same with B MN-major in one block, a step of it `b_step` bytes further.
-__device__ __forceinline__ void product_blocks_mn(uint32_t lead, uint32_t d, uint64_t a, uint32_t a_block, uint64_t b, uint32_t b_step, int steps, uint32_t kind) {
-    bool add = false;
+__device__ __forceinline__ void product_blocks_mn(uint32_t lead, uint32_t d, uint64_t a, uint32_t a_block, uint64_t b, uint32_t b_step, int steps, uint32_t kind,
+                                                  bool add = false) {
     for (; steps >= 4; steps -= 4) {
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
