@@ -23,8 +23,8 @@ namespace {
 
 constexpr int kTileRows = 128;
 constexpr int kBlockBytes = kTileRows * 128;     // a tile's 64 columns
-constexpr int kEpilogueWarps = 16, kCopyWarp = 16, kFirstWarp = 17, kSecondWarp = 18, kFixWarp = 19;
-constexpr int kRowThreads = 608, kWeightThreads = 640;
+constexpr int kEpilogueWarps = 16, kCopyWarp = 16, kFirstWarp = 17, kSecondWarp = 18, kOtherFirstWarp = 19, kFixWarp = 19;
+constexpr int kFfnThreads = 640;
 constexpr int kTmemColumns = 512;
 constexpr int kMaxFfnChannels = 256, kMaxFfnHidden = 8192;
 constexpr int kMaxStages = 4;
@@ -248,7 +248,7 @@ struct Maps {
 };
 
 template <int MODE, int HC, int NT, int ACT, bool BF16>
-__global__ void __launch_bounds__(kRowThreads, 1) ffn_rows_kernel(const RowArgs a, const __grid_constant__ Maps maps) {
+__global__ void __launch_bounds__(kFfnThreads, 1) ffn_rows_kernel(const RowArgs a, const __grid_constant__ Maps maps) {
     // TMEM: the output of NT tiles, two accumulators of g and u, for dx two of dh, and the hidden values of two units, or of
     // one where 64 units of dg and du leave no room (up to 64 channels then, 96 for y).
     constexpr int kHid = MODE == GRAD_X && HC == 64 ? 1 : 2, kHidColumns = MODE == FORWARD ? HC / 2 : HC;
@@ -286,7 +286,7 @@ __global__ void __launch_bounds__(kRowThreads, 1) ffn_rows_kernel(const RowArgs 
         gave_up = 0;
         for (int s = 0; s < kMaxStages; ++s) {
             bar_init(x_full(s), 1); bar_init(x_empty(s), 1);
-            bar_init(g_full(s), 1); bar_init(g_empty(s), 1);
+            bar_init(g_full(s), 1); bar_init(g_empty(s), MODE == FORWARD ? NT : 1);
             bar_init(d_full(s), 1); bar_init(d_empty(s), 1);
             bar_init(staged(s), NT == 2 ? 8 : 16);
         }
@@ -308,119 +308,123 @@ __global__ void __launch_bounds__(kRowThreads, 1) ffn_rows_kernel(const RowArgs 
 #define WAIT(bar, parity) bar_wait(bar, parity, &gave_up, a.seg.status)
 
     if (warp == kCopyWarp) {
-        // One thread copies rows and weights, each as soon as a stage of theirs is free, and stores finished tiles from where
+        // One warp copies rows and weights, each as soon as a stage of theirs is free, and stores finished tiles from where
         // their rows were: the wait for one must not hold up the others.
-        if (lane == 0) {
-            Ring x(a.xn), g(a.gn), d(a.dn), done(a.xn);
-            TileWalk rows = walk, stored = walk;
-            int t = 0, left = items * NT, st = 0, pending = items * NT;   // tiles to copy, tiles to store
-            auto copy_rows = [&] {
-                bar_expect(x_full(x.at), a.x_bytes);
-                const uint32_t to = base + x.at * a.x_bytes;
-                const int row = rows.row + t * kTileRows;
-                for (int b = 0; b < a.full; ++b) {
-                    copy_tile(to + b * kBlockBytes, &maps.x, 64 * b, row, x_full(x.at));
-                    if (MODE == GRAD_X) copy_tile(to + a.tile_bytes + b * kBlockBytes, &maps.dy, 64 * b, row, x_full(x.at));
-                }
-                if (a.tail) {
-                    copy_tile(to + a.full * kBlockBytes, &maps.x_tail, 64 * a.full, row, x_full(x.at));
-                    if (MODE == GRAD_X) copy_tile(to + a.tile_bytes + a.full * kBlockBytes, &maps.dy_tail, 64 * a.full, row, x_full(x.at));
-                }
-                x.next();
-                --left;
-                if (++t == NT) { t = 0; next_tile(a.seg, rows, kTileRows * NT); }
-            };
-            auto store_rows = [&] {
-                const int row = stored.row + st * kTileRows;
-                if (stored.left - st * kTileRows >= kTileRows) {       // a ragged tile's rows have left directly
-                    for (int b = 0; b < a.full; ++b) store_tile(&maps.out, 64 * b, row, base + done.at * a.x_bytes + b * kBlockBytes);
-                    if (a.tail) store_tile(&maps.out_tail, 64 * a.full, row, base + done.at * a.x_bytes + a.full * kBlockBytes);
-                    stores_read();
-                }
-                bar_arrive(x_empty(done.at));
-                done.next();
-                --pending;
-                if (++st == NT) { st = 0; next_tile(a.seg, stored, kTileRows * NT); }
-            };
-            auto poll = [&] {
-                if (pending > 0 && bar_test(staged(done.at), done.parity)) store_rows();
-                if (left > 0 && bar_test(x_empty(x.at), x.parity ^ 1)) copy_rows();
-            };
-            auto wait = [&](uint32_t bar, uint32_t parity) {
-                for (int i = 0; !bar_try(bar, parity); ++i) {
-                    poll();
-                    if (i > kWaitTries) { gave_up = 1; atomicOr(a.seg.status, kStatusTimeout); }
-                    if (*(volatile int*)&gave_up) break;
-                }
-            };
-            copy_rows();
-            for (int it = 0; it < items; ++it, next_tile(a.seg, walk, kTileRows * NT)) {
-                const int e = walk.q / a.seg.B;
-                for (int j = 0; j < a.chunks && !*(volatile int*)&gave_up; ++j, g.next(), d.next()) {
-                    wait(g_empty(g.at), g.parity ^ 1);
-                    bar_expect(g_full(g.at), a.g_bytes);
-                    const uint32_t to = base + a.off_g + g.at * a.g_bytes;
-                    // The gradients take Wg and Wu both ways: their last block is a whole one.
-                    const int whole = MODE == GRAD_X && a.tail ? a.full + 1 : a.full;
-                    for (int b = 0; b < whole; ++b) {
-                        copy_tile(to + b * (2 * HC * 128), &maps.gate, 64 * b, j * HC, e, g_full(g.at));
-                        copy_tile(to + b * (2 * HC * 128) + HC * 128, &maps.up, 64 * b, j * HC, e, g_full(g.at));
-                    }
-                    if (MODE == FORWARD && a.tail) {
-                        copy_tile(to + a.full * (2 * HC * 128), &maps.gate_tail, 64 * a.full, j * HC, e, g_full(g.at));
-                        copy_tile(to + a.full * (2 * HC * 128) + HC * a.tail * 2, &maps.up_tail, 64 * a.full, j * HC, e, g_full(g.at));
-                    }
-                    wait(d_empty(d.at), d.parity ^ 1);
-                    bar_expect(d_full(d.at), a.d_bytes);
-                    copy_tile(base + a.off_d + d.at * a.d_bytes, &maps.down, j * HC, 0, e, d_full(d.at));
-                    poll();
-                }
+        const uint32_t lead = elected();
+        Ring x(a.xn), g(a.gn), d(a.dn), done(a.xn);
+        TileWalk rows = walk, stored = walk;
+        int t = 0, left = items * NT, st = 0, pending = items * NT;        // tiles to copy, tiles to store
+        auto copy_rows = [&] {
+            const uint32_t to = base + x.at * a.x_bytes, bar = x_full(x.at);
+            const int row = uniform(rows.row) + t * kTileRows;
+            bar_expect(lead, bar, a.x_bytes);
+            for (int b = 0; b < a.full; ++b) {
+                copy_tile(lead, to + b * kBlockBytes, &maps.x, 64 * b, row, bar);
+                if (MODE == GRAD_X) copy_tile(lead, to + a.tile_bytes + b * kBlockBytes, &maps.dy, 64 * b, row, bar);
             }
-            // What is left: the last tiles' results, and rows whose stage one of them held.
-            while (pending > 0 && !*(volatile int*)&gave_up) {
-                WAIT(staged(done.at), done.parity);
+            if (a.tail) {
+                copy_tile(lead, to + a.full * kBlockBytes, &maps.x_tail, 64 * a.full, row, bar);
+                if (MODE == GRAD_X) copy_tile(lead, to + a.tile_bytes + a.full * kBlockBytes, &maps.dy_tail, 64 * a.full, row, bar);
+            }
+            x.next();
+            --left;
+            if (++t == NT) { t = 0; next_tile(a.seg, rows, kTileRows * NT); }
+        };
+        auto store_rows = [&] {
+            const int row = uniform(stored.row) + st * kTileRows;
+            if (uniform(stored.left) - st * kTileRows >= kTileRows) {      // a ragged tile's rows have left directly
+                const uint32_t from = base + done.at * a.x_bytes;
+                for (int b = 0; b < a.full; ++b) store_tile(lead, &maps.out, 64 * b, row, from + b * kBlockBytes);
+                if (a.tail) store_tile(lead, &maps.out_tail, 64 * a.full, row, from + a.full * kBlockBytes);
+                stores_read();
+                __syncwarp();
+            }
+            if (lead) bar_arrive(x_empty(done.at));
+            done.next();
+            --pending;
+            if (++st == NT) { st = 0; next_tile(a.seg, stored, kTileRows * NT); }
+        };
+        auto over = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xFFFFFFFFu, bar_test(bar, parity)) != 0; };
+        auto given_up = [&] { return __any_sync(0xFFFFFFFFu, *(volatile int*)&gave_up) != 0; };
+        auto poll = [&] {
+            if (pending > 0 && over(staged(done.at), done.parity)) store_rows();
+            if (left > 0 && over(x_empty(x.at), x.parity ^ 1)) copy_rows();
+        };
+        auto wait = [&](uint32_t bar, uint32_t parity) {
+            for (int i = 0; !__all_sync(0xFFFFFFFFu, bar_try(bar, parity)); ++i) {
+                poll();
+                if (i > kWaitTries) { gave_up = 1; atomicOr(a.seg.status, kStatusTimeout); }
+                if (given_up()) break;
+            }
+        };
+        copy_rows();
+        for (int it = 0; it < items && !given_up(); ++it, next_tile(a.seg, walk, kTileRows * NT)) {
+            const int e = uniform(walk.q / a.seg.B);
+            for (int j = 0; j < a.chunks; ++j, g.next(), d.next()) {
+                wait(g_empty(g.at), g.parity ^ 1);
+                const uint32_t to = base + a.off_g + g.at * a.g_bytes, bar = g_full(g.at);
+                bar_expect(lead, bar, a.g_bytes);
+                // The gradients take Wg and Wu both ways: their last block is a whole one.
+                const int whole = MODE == GRAD_X && a.tail ? a.full + 1 : a.full;
+                for (int b = 0; b < whole; ++b) {
+                    copy_tile(lead, to + b * (2 * HC * 128), &maps.gate, 64 * b, j * HC, e, bar);
+                    copy_tile(lead, to + b * (2 * HC * 128) + HC * 128, &maps.up, 64 * b, j * HC, e, bar);
+                }
+                if (MODE == FORWARD && a.tail) {
+                    copy_tile(lead, to + a.full * (2 * HC * 128), &maps.gate_tail, 64 * a.full, j * HC, e, bar);
+                    copy_tile(lead, to + a.full * (2 * HC * 128) + HC * a.tail * 2, &maps.up_tail, 64 * a.full, j * HC, e, bar);
+                }
+                wait(d_empty(d.at), d.parity ^ 1);
+                bar_expect(lead, d_full(d.at), a.d_bytes);
+                copy_tile(lead, base + a.off_d + d.at * a.d_bytes, &maps.down, j * HC, 0, e, d_full(d.at));
                 poll();
             }
-            stores_written();
         }
-    } else if (warp == kFirstWarp) {
-        // Unit n is chunk j of tile t of an item.
+        // What is left: the last tiles' results, and rows whose stage one of them held.
+        while (pending > 0 && !given_up()) {
+            WAIT(staged(done.at), done.parity);
+            __syncwarp();
+            poll();
+        }
+        stores_written();
+    } else if (warp == kFirstWarp || warp == kOtherFirstWarp) {
+        // Unit n is chunk j of tile t of an item; two warps take them in turn.  Issuing returns little before the last product
+        // begins, and every wait takes 100 clocks even if it is over: one waits while the other's products run.
+        // A barrier's parity says no more than whether its last use is over.  So a warp waits for every use of a stage in
+        // turn, and no stage comes round before both are done with it: each tile of an item, or each second chunk where an
+        // item is one tile, has stages of its own (their numbers are even).
+        const int mine = warp == kFirstWarp ? 0 : 1;
         const uint32_t lead = elected(), kind_gu = product_kind(2 * HC, BF16, false, false), kind_dh = product_kind(HC, BF16, false, true);
         const int steps = 4 * a.full, tail_steps = a.tail / 16;
         const uint64_t tail_x0 = operand(base + a.full * kBlockBytes, a.tail * 2, 0);
         const uint64_t tail_w0 = operand(base + a.off_g + a.full * (2 * HC * 128), MODE == FORWARD ? a.tail * 2 : 128, 0);
         const uint64_t x0 = operand(base, 128, 0), w0 = operand(base + a.off_g, 128, 0), wd0 = operand(base + a.off_d, HC * 2, 0);
         Ring x(a.xn), g(a.gn), d(a.dn);
-        int j = 0, t = 0;
-        for (int n = 0; n < units; ++n) {
-            if (t == 0) WAIT(g_full(g.at), g.parity);
-            if (MODE == GRAD_X) WAIT(d_full(d.at), d.parity);
-            const int xs = x.at + t < a.xn ? x.at + t : x.at + t - a.xn;
-            if (j == 0) WAIT(x_full(xs), x.at + t < a.xn ? x.parity : x.parity ^ 1);
-            WAIT(acc_empty(n & 1), (n >> 1 & 1) ^ 1);
-            tmem_fence_after();
-            const uint32_t acc = acc0 + (n & 1) * 2 * HC;
-            const uint64_t xa = operand_at(x0, xs * a.x_bytes), xt = operand_at(tail_x0, xs * a.x_bytes);
-            product_blocks(lead, acc, xa, kBlockBytes, operand_at(w0, g.at * a.g_bytes), 2 * HC * 128, steps, kind_gu);
-            product_blocks(lead, acc, xt, 0, operand_at(tail_w0, g.at * a.g_bytes), 0, tail_steps, kind_gu, steps > 0);
-            if (MODE == GRAD_X) {
-                const uint64_t wd = operand_at(wd0, d.at * a.d_bytes);
-                product_blocks_mn(lead, dh0 + (n & 1) * HC, operand_at(xa, a.tile_bytes), kBlockBytes, wd, 32 * HC, steps, kind_dh);
-                product_blocks_mn(lead, dh0 + (n & 1) * HC, operand_at(xt, a.tile_bytes), 0, operand_at(wd, steps * 32 * HC), 32 * HC, tail_steps, kind_dh, steps > 0);
-            }
-            products_done(lead, acc_full(n & 1));
-            // The gradients' second products take Wg and Wu again: the other warp gives them back.
-            if (MODE == FORWARD && t == NT - 1) products_done(lead, g_empty(g.at));
-            if (MODE == GRAD_X) products_done(lead, d_empty(d.at));
-            if (++t == NT) {
-                t = 0;
-                g.next();
-                d.next();
-                if (++j == a.chunks) {
-                    j = 0;
-                    for (int k = 0; k < NT; ++k) x.next();
+        if (NT == 2 && mine == 1) x.next();
+        const uint32_t acc = acc0 + mine * 2 * HC;
+        uint32_t use = 1;                                              // parity of the wait for this warp's accumulators
+        for (int it = 0, n = 0; it < items; ++it) {
+            WAIT(x_full(x.at), x.parity);
+            const uint64_t xa = operand_at(x0, x.at * a.x_bytes), xt = operand_at(tail_x0, x.at * a.x_bytes);
+            for (int j = 0; j < a.chunks; ++j, ++n, g.next(), d.next()) {
+                if (NT == 1 && (n & 1) != mine) continue;
+                WAIT(g_full(g.at), g.parity);
+                if (MODE == GRAD_X) WAIT(d_full(d.at), d.parity);
+                WAIT(acc_empty(mine), use);
+                use ^= 1;
+                tmem_fence_after();
+                product_blocks(lead, acc, xa, kBlockBytes, operand_at(w0, g.at * a.g_bytes), 2 * HC * 128, steps, kind_gu);
+                product_blocks(lead, acc, xt, 0, operand_at(tail_w0, g.at * a.g_bytes), 0, tail_steps, kind_gu, steps > 0);
+                if (MODE == GRAD_X) {
+                    const uint64_t wd = operand_at(wd0, d.at * a.d_bytes);
+                    product_blocks_mn(lead, dh0 + mine * HC, operand_at(xa, a.tile_bytes), kBlockBytes, wd, 32 * HC, steps, kind_dh);
+                    product_blocks_mn(lead, dh0 + mine * HC, operand_at(xt, a.tile_bytes), 0, operand_at(wd, steps * 32 * HC), 32 * HC, tail_steps, kind_dh, steps > 0);
                 }
+                products_done(lead, acc_full(mine));
+                // The gradients' second products take Wg and Wu again: their warp gives them back.
+                products_done(lead, MODE == FORWARD ? g_empty(g.at) : d_empty(d.at));
             }
+            for (int k = 0; k < NT; ++k) x.next();
         }
     } else if (warp == kSecondWarp) {
         const uint32_t lead = elected(), kind_out = product_kind(a.c16, BF16, false, MODE == GRAD_X);
@@ -525,7 +529,7 @@ __device__ __forceinline__ void clear_rows(uint32_t tile, int blocks, int rows, 
 // tiles are read from device memory once.  A range that meets several experts has a part of the result for each: entry
 // r + e of `part`, which along the run of all tiles no other pair of range and expert has.
 template <int HC, int ACT, bool BF16>
-__global__ void __launch_bounds__(kWeightThreads, 1) ffn_weights_kernel(const WeightArgs a, const __grid_constant__ Maps maps) {
+__global__ void __launch_bounds__(kFfnThreads, 1) ffn_weights_kernel(const WeightArgs a, const __grid_constant__ Maps maps) {
     constexpr int kOut = 3 * HC, kTwoDh = HC == 32 ? 1 : 0, kHidBlock = kTileRows * HC * 2;
     extern __shared__ uint8_t dynamic[];
     __shared__ __align__(8) uint64_t bars[32];
@@ -571,34 +575,34 @@ __global__ void __launch_bounds__(kWeightThreads, 1) ffn_weights_kernel(const We
     auto first_tile = [&](int r) { return (int)((long long)total * r / a.ranges); };
 
     if (warp == kCopyWarp) {
-        if (lane == 0) {
-            int n = 0, piece = 0;
-            for (int k = blockIdx.x; k < work; k += gridDim.x) {
-                const int r = k / a.slices, c = k - r * a.slices, lo = first_tile(r), hi = first_tile(r + 1);
-                if (lo >= hi) continue;
-                TileWalk walk = tile_at(a.seg, bounds, start, lo, kTileRows);
-                int e = -1;
-                for (int i = lo; i < hi && !*(volatile int*)&gave_up; ++i, ++n, next_tile(a.seg, walk, kTileRows)) {
-                    if (walk.q / a.seg.B != e) {
-                        e = walk.q / a.seg.B;
-                        WAIT(w_empty, (piece & 1) ^ 1);
-                        bar_expect(w_full, a.w_bytes);
-                        for (int b = 0; b < a.blocks; ++b) {
-                            const uint32_t to = base + a.off_w + b * (2 * HC * 128);
-                            copy_tile(to, &maps.gate, 64 * b, c * HC, e, w_full);
-                            copy_tile(to + HC * 128, &maps.up, 64 * b, c * HC, e, w_full);
-                        }
-                        copy_tile(base + a.off_w + a.blocks * (2 * HC * 128), &maps.down, c * HC, 0, e, w_full);
-                        ++piece;
-                    }
-                    const int s = n % a.xn;
-                    WAIT(x_empty(s), (n / a.xn & 1) ^ 1);
-                    bar_expect(x_land(s), a.x_bytes);
-                    const uint32_t to = base + s * a.x_bytes;
+        const uint32_t lead = elected();
+        Ring x(a.xn);
+        int piece = 0;
+        for (int k = blockIdx.x; k < work && !__any_sync(0xFFFFFFFFu, *(volatile int*)&gave_up); k += gridDim.x) {
+            const int r = k / a.slices, c = k - r * a.slices, lo = first_tile(r), hi = first_tile(r + 1);
+            if (lo >= hi) continue;
+            TileWalk walk = tile_at(a.seg, bounds, start, lo, kTileRows);
+            int e = -1;
+            for (int i = lo; i < hi; ++i, x.next(), next_tile(a.seg, walk, kTileRows)) {
+                const int now = uniform(walk.q / a.seg.B), row = uniform(walk.row);
+                if (now != e) {
+                    e = now;
+                    WAIT(w_empty, (piece & 1) ^ 1);
+                    bar_expect(lead, w_full, a.w_bytes);
                     for (int b = 0; b < a.blocks; ++b) {
-                        copy_tile(to + b * kBlockBytes, &maps.x, 64 * b, walk.row, x_land(s));
-                        copy_tile(to + (a.blocks + b) * kBlockBytes, &maps.dy, 64 * b, walk.row, x_land(s));
+                        const uint32_t to = base + a.off_w + b * (2 * HC * 128);
+                        copy_tile(lead, to, &maps.gate, 64 * b, c * HC, e, w_full);
+                        copy_tile(lead, to + HC * 128, &maps.up, 64 * b, c * HC, e, w_full);
                     }
+                    copy_tile(lead, base + a.off_w + a.blocks * (2 * HC * 128), &maps.down, c * HC, 0, e, w_full);
+                    ++piece;
+                }
+                WAIT(x_empty(x.at), x.parity ^ 1);
+                const uint32_t to = base + x.at * a.x_bytes, bar = x_land(x.at);
+                bar_expect(lead, bar, a.x_bytes);
+                for (int b = 0; b < a.blocks; ++b) {
+                    copy_tile(lead, to + b * kBlockBytes, &maps.x, 64 * b, row, bar);
+                    copy_tile(lead, to + (a.blocks + b) * kBlockBytes, &maps.dy, 64 * b, row, bar);
                 }
             }
         }
@@ -856,12 +860,12 @@ int launch_rows(emc2_bridge* h, const FfnCall& f, cudaStream_t st) {
     // As many stages as there is room for: first two of each, then more of the rows.
     a.xn = NT; a.gn = 2; a.dn = 2;
     auto room = [&] { return (size_t)a.xn * a.x_bytes + (size_t)a.gn * a.g_bytes + (size_t)a.dn * a.d_bytes + 1024; };
-    // What is left goes to a third stage of the weights, the next item's rows, a fourth.
-    auto more_weights = [&](int n) { while (a.gn < n && room() + a.g_bytes + a.d_bytes <= kMaxShared) { ++a.gn; ++a.dn; } };
-    auto more_rows = [&](int n) { while (a.xn < n && room() + a.x_bytes <= kMaxShared) ++a.xn; };
-    more_weights(3);
-    more_rows(2 * NT);
-    more_weights(kMaxStages);
+    // What is left goes to the next item's rows and to twice the stages of the weights (see the first products' warps for the
+    // even numbers).
+    auto more_rows = [&](int n) { while (a.xn < n && room() + NT * a.x_bytes <= kMaxShared) a.xn += NT; };
+    if (NT == 2) more_rows(4);
+    if (room() + 2 * (a.g_bytes + a.d_bytes) <= kMaxShared) { a.gn += 2; a.dn += 2; }
+    if (NT == 1) more_rows(2);
     a.off_g = a.xn * a.x_bytes;
     a.off_d = a.off_g + a.gn * a.g_bytes;
     Maps m;
@@ -870,10 +874,10 @@ int launch_rows(emc2_bridge* h, const FfnCall& f, cudaStream_t st) {
     const int ctas = (int)std::min<long long>(row_tiles(f.seg, NT), h->num_sms), kind = MODE == FORWARD ? K_FFN : K_FFN_GRAD_X;
     const bool bf16 = f.type == EMC2_BF16;
     if (f.act == EMC2_ACT_SILU)
-        return bf16 ? launch_ffn(h, kind, ffn_rows_kernel<MODE, HC, NT, EMC2_ACT_SILU, true>, a, m, ctas, kRowThreads, shared, st)
-                    : launch_ffn(h, kind, ffn_rows_kernel<MODE, HC, NT, EMC2_ACT_SILU, false>, a, m, ctas, kRowThreads, shared, st);
-    return bf16 ? launch_ffn(h, kind, ffn_rows_kernel<MODE, HC, NT, EMC2_ACT_GELU, true>, a, m, ctas, kRowThreads, shared, st)
-                : launch_ffn(h, kind, ffn_rows_kernel<MODE, HC, NT, EMC2_ACT_GELU, false>, a, m, ctas, kRowThreads, shared, st);
+        return bf16 ? launch_ffn(h, kind, ffn_rows_kernel<MODE, HC, NT, EMC2_ACT_SILU, true>, a, m, ctas, kFfnThreads, shared, st)
+                    : launch_ffn(h, kind, ffn_rows_kernel<MODE, HC, NT, EMC2_ACT_SILU, false>, a, m, ctas, kFfnThreads, shared, st);
+    return bf16 ? launch_ffn(h, kind, ffn_rows_kernel<MODE, HC, NT, EMC2_ACT_GELU, true>, a, m, ctas, kFfnThreads, shared, st)
+                : launch_ffn(h, kind, ffn_rows_kernel<MODE, HC, NT, EMC2_ACT_GELU, false>, a, m, ctas, kFfnThreads, shared, st);
 }
 
 // Ranges of the tiles: four units of work per SM, but eight tiles in each while that leaves one unit per SM.
@@ -915,10 +919,10 @@ int launch_slices(emc2_bridge* h, const FfnCall& f, WeightArgs& a, cudaStream_t 
     const int ctas = std::min(a.ranges * a.slices, h->num_sms);
     const bool bf16 = f.type == EMC2_BF16;
     if (f.act == EMC2_ACT_SILU)
-        return bf16 ? launch_ffn(h, K_FFN_GRAD_W, ffn_weights_kernel<HC, EMC2_ACT_SILU, true>, a, m, ctas, kWeightThreads, shared, st)
-                    : launch_ffn(h, K_FFN_GRAD_W, ffn_weights_kernel<HC, EMC2_ACT_SILU, false>, a, m, ctas, kWeightThreads, shared, st);
-    return bf16 ? launch_ffn(h, K_FFN_GRAD_W, ffn_weights_kernel<HC, EMC2_ACT_GELU, true>, a, m, ctas, kWeightThreads, shared, st)
-                : launch_ffn(h, K_FFN_GRAD_W, ffn_weights_kernel<HC, EMC2_ACT_GELU, false>, a, m, ctas, kWeightThreads, shared, st);
+        return bf16 ? launch_ffn(h, K_FFN_GRAD_W, ffn_weights_kernel<HC, EMC2_ACT_SILU, true>, a, m, ctas, kFfnThreads, shared, st)
+                    : launch_ffn(h, K_FFN_GRAD_W, ffn_weights_kernel<HC, EMC2_ACT_SILU, false>, a, m, ctas, kFfnThreads, shared, st);
+    return bf16 ? launch_ffn(h, K_FFN_GRAD_W, ffn_weights_kernel<HC, EMC2_ACT_GELU, true>, a, m, ctas, kFfnThreads, shared, st)
+                : launch_ffn(h, K_FFN_GRAD_W, ffn_weights_kernel<HC, EMC2_ACT_GELU, false>, a, m, ctas, kFfnThreads, shared, st);
 }
 
 // Slices of 64 hidden units where two stages of tiles fit beside them (up to 96 channels): half the products, each of which

@@ -11,6 +11,14 @@ namespace emc2 {
 
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 
+__device__ __forceinline__ uint32_t elected() {
+    uint32_t p;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+    return p;
+}
+// The value of lane 0, which the compiler then knows to be the same in all lanes.
+__device__ __forceinline__ uint32_t uniform(uint32_t v) { return __shfl_sync(0xFFFFFFFFu, v, 0); }
+__device__ __forceinline__ int uniform(int v) { return __shfl_sync(0xFFFFFFFFu, v, 0); }
 // ---- mbarriers, by shared-memory address
 __device__ __forceinline__ void bar_init(uint32_t bar, uint32_t arrivals) {
     asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(arrivals) : "memory");
@@ -18,8 +26,9 @@ __device__ __forceinline__ void bar_init(uint32_t bar, uint32_t arrivals) {
 __device__ __forceinline__ void bar_arrive(uint32_t bar) {
     asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
 }
-__device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes) {
-    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+__device__ __forceinline__ void bar_expect(uint32_t lead, uint32_t bar, uint32_t bytes) {
+    asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %2, 0;\n\t"
+                 "@q mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n\t}" ::"r"(bar), "r"(bytes), "r"(lead) : "memory");
 }
 // Whether the phase of that parity is over; try_wait suspends the thread for a while first, test_wait does not.
 __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
@@ -76,19 +85,23 @@ __device__ __forceinline__ void leave_after_timeout(volatile int* gave_up) {
 __device__ __forceinline__ void fence_async_shared() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 __device__ __forceinline__ void fence_bar_init() { asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory"); }
 
-// ---- tiled bulk copies into shared memory; x counts elements of the innermost dimension (a multiple of 16 bytes)
-__device__ __forceinline__ void copy_tile(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
-    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
-                 ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
+// ---- tiled bulk copies; x counts elements of the innermost dimension (a multiple of 16 bytes)
+// As with the products below, a whole warp comes here with the same arguments and one lane (`lead`) issues.
+__device__ __forceinline__ void copy_tile(uint32_t lead, uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
+    asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %5, 0;\n\t"
+                 "@q cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];\n\t}"
+                 ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar), "r"(lead) : "memory");
 }
-__device__ __forceinline__ void copy_tile(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
-    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
-                 ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
+__device__ __forceinline__ void copy_tile(uint32_t lead, uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
+    asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %6, 0;\n\t"
+                 "@q cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];\n\t}"
+                 ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar), "r"(lead) : "memory");
 }
-
-// And back: the tile at src, whose reads the thread waits for with stores_read.
-__device__ __forceinline__ void store_tile(const CUtensorMap* map, int x, int y, uint32_t src) {
-    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"(map), "r"(x), "r"(y), "r"(src) : "memory");
+// And back: the tile at src, whose reads the lane that issued waits for with stores_read.
+__device__ __forceinline__ void store_tile(uint32_t lead, const CUtensorMap* map, int x, int y, uint32_t src) {
+    asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %4, 0;\n\t"
+                 "@q cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];\n\t}"
+                 ::"l"(map), "r"(x), "r"(y), "r"(src), "r"(lead) : "memory");
 }
 __device__ __forceinline__ void stores_read() {
     asm volatile("cp.async.bulk.commit_group;" ::: "memory");
@@ -224,11 +237,6 @@ __device__ __forceinline__ uint32_t product_kind(int n, bool bf16, bool a_mn, bo
     return 1u << 4 | (bf16 ? 1u : 0u) << 7 | (bf16 ? 1u : 0u) << 10 | (a_mn ? 1u : 0u) << 15 | (b_mn ? 1u : 0u) << 16 |
            (uint32_t)(n >> 3) << 17 | (uint32_t)(128 >> 4) << 24;
 }
-__device__ __forceinline__ uint32_t elected() {
-    uint32_t p;
-    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
-    return p;
-}
 __device__ __forceinline__ void product(uint32_t lead, uint32_t d, uint64_t a, uint64_t b, uint32_t kind, bool add) {
     asm volatile(
         "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t"
@@ -242,9 +250,6 @@ __device__ __forceinline__ void product_tmem(uint32_t lead, uint32_t d, uint32_t
         "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
         ::"r"(d), "r"(a), "l"(b), "r"(kind), "r"((uint32_t)add), "r"(lead) : "memory");
 }
-// The value of lane 0, which the compiler then knows to be the same in all lanes.
-__device__ __forceinline__ uint32_t uniform(uint32_t v) { return __shfl_sync(0xFFFFFFFFu, v, 0); }
-__device__ __forceinline__ int uniform(int v) { return __shfl_sync(0xFFFFFFFFu, v, 0); }
 // Further on by a multiple of 16 bytes.
 __device__ __forceinline__ uint64_t operand_at(uint64_t op, uint32_t bytes) { return op + (bytes >> 4); }
 // `steps` steps of 16 k with both operands K-major in blocks of 64 columns.  What is computed
