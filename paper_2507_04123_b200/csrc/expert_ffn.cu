@@ -31,6 +31,8 @@ constexpr int kMaxStages = 4;
 constexpr size_t kMaxShared = 232448 - 1024;     // what a CTA can have, less the kernels' static part
 
 enum { FORWARD = 0, GRAD_X = 1 };
+// Where the hidden values go: to TMEM, to shared memory, or there with h beside dg and du.
+enum { TO_TMEM = 0, TO_SHARED = 1, TO_SHARED_WITH_H = 2 };
 
 // ---------------------------------------------------------------- a walk over the tiles, expert by expert
 // Tiles hold up to 128 * NT rows of one (expert, frame) segment.
@@ -151,8 +153,7 @@ __device__ __forceinline__ uint32_t swizzled(int width, int r, int piece) {
 }
 
 // Columns c .. c + 7 of a chunk, at j of the arrays: the values that go on to the second product, a 16-byte piece of row r.
-// `to`: where the row's values go, in TMEM for the rows' kernels, in shared memory (as B operands) for the weights'.
-template <int MODE, int HC, int ACT, bool BF16, bool WITH_H, int W>
+template <int MODE, int HC, int ACT, bool BF16, int TO, int W>
 __device__ __forceinline__ void hidden8(const uint32_t (&g)[W], const uint32_t (&u)[W], const uint32_t (&dh)[W], int j0, uint32_t to, int r, int c) {
     constexpr uint32_t kBlock = kTileRows * HC * 2;
     uint32_t p[4], q[4], t[4];
@@ -160,7 +161,7 @@ __device__ __forceinline__ void hidden8(const uint32_t (&g)[W], const uint32_t (
     for (int i = 0; i < 4; ++i) {
         const int j = j0 + 2 * i;
         uint32_t first = g[j];
-        if (WITH_H) asm volatile("" : "+r"(first));                // and pair by pair here, see hidden_half
+        if (TO != TO_TMEM) asm volatile("" : "+r"(first));           // and pair by pair here, see hidden_half
         const uint64_t gg = pair(first, g[j + 1]), uu = pair(u[j], u[j + 1]);
         if (MODE == FORWARD) {
             p[i] = pack<BF16>(mul2(activation2<ACT, BF16>(gg), uu));
@@ -170,17 +171,17 @@ __device__ __forceinline__ void hidden8(const uint32_t (&g)[W], const uint32_t (
             activation_grad2<ACT, BF16>(gg, a, da);
             p[i] = pack<BF16>(mul2(mul2(dd, uu), da));
             q[i] = pack<BF16>(mul2(dd, a));
-            if (WITH_H) t[i] = pack<BF16>(mul2(a, uu));
+            if (TO == TO_SHARED_WITH_H) t[i] = pack<BF16>(mul2(a, uu));
         }
     }
-    if (!WITH_H) {
+    if (TO == TO_TMEM) {
         tmem_store(to + c / 2, p[0], p[1], p[2], p[3]);
         if (MODE == GRAD_X) tmem_store(to + (HC + c) / 2, q[0], q[1], q[2], q[3]);
     } else {
         const uint32_t at = to + swizzled<HC>(r, c / 8);
         store_shared(at, p[0], p[1], p[2], p[3]);
-        store_shared(at + kBlock, q[0], q[1], q[2], q[3]);
-        store_shared(at + 2 * kBlock, t[0], t[1], t[2], t[3]);
+        if (MODE == GRAD_X) store_shared(at + kBlock, q[0], q[1], q[2], q[3]);
+        if (TO == TO_SHARED_WITH_H) store_shared(at + 2 * kBlock, t[0], t[1], t[2], t[3]);
     }
 }
 
@@ -193,7 +194,7 @@ __device__ __forceinline__ void warp_arrive(uint32_t bar) {
 // The activation of half of the columns of one chunk of one tile: accumulators of g and u, HC columns each, and of dh, of the
 // warp's 32 rows into the blocks at `to`.  The accumulators are given back as soon as they are in registers (which hold 32
 // columns of two or 8 to 16 of three), before the arithmetic, so that the next products run beside it.
-template <int MODE, int HC, int ACT, bool BF16, bool WITH_H>
+template <int MODE, int HC, int ACT, bool BF16, int TO>
 __device__ __forceinline__ void hidden_half(uint32_t acc, uint32_t acc_dh, int half, uint32_t to, int r, uint32_t acc_empty, uint32_t hid_empty,
                                             uint32_t parity, volatile int* gave_up, int* status) {
     constexpr int W = MODE == FORWARD ? HC / 2 : HC == 64 || ACT == EMC2_ACT_GELU ? 8 : 16;
@@ -220,10 +221,10 @@ __device__ __forceinline__ void hidden_half(uint32_t acc, uint32_t acc_dh, int h
             // One piece after the other: the arithmetic of two would not fit in the registers.
 #pragma unroll
             for (int i = j; i < j + 8; ++i) asm volatile("" : "+r"(g[i]));
-            hidden8<MODE, HC, ACT, BF16, WITH_H>(g, u, dh, j, to, r, at + j);
+            hidden8<MODE, HC, ACT, BF16, TO>(g, u, dh, j, to, r, at + j);
         }
     }
-    if (WITH_H) {
+    if (TO != TO_TMEM) {
         fence_async_shared();
     } else {
         tmem_wait_stores();
@@ -238,8 +239,8 @@ struct RowArgs {
     int C, H, c16, chunks;                  // c16: C rounded up to 16; chunks of HC hidden units
     int full, tail;                         // blocks of 64 columns, and the columns of a narrower one behind them: 0, 16 or 32
     int xn, gn, dn;                         // stages of the rows' tiles, of Wg and Wu, of Wd
-    uint32_t off_g, off_d;                  // in the dynamic shared memory, behind the rows' tiles
-    uint32_t x_bytes, g_bytes, d_bytes;     // of a stage
+    uint32_t off_g, off_d, off_h;           // in the dynamic shared memory, behind the rows' tiles
+    uint32_t x_bytes, g_bytes, d_bytes, h_bytes;   // of a stage; h: of a unit's hidden values, two of them, if they go there
     uint32_t tile_bytes;                    // of one tensor's tile
 };
 struct Maps {
@@ -247,11 +248,11 @@ struct Maps {
     CUtensorMap x_tail, dy_tail, gate_tail, up_tail, out_tail;              // of the last block of columns, where it is narrower
 };
 
-template <int MODE, int HC, int NT, int ACT, bool BF16>
+template <int MODE, int HC, int NT, int TO, int ACT, bool BF16>
 __global__ void __launch_bounds__(kFfnThreads, 1) ffn_rows_kernel(const RowArgs a, const __grid_constant__ Maps maps) {
-    // TMEM: the output of NT tiles, two accumulators of g and u, for dx two of dh, and the hidden values of two units, or of
-    // one where 64 units of dg and du leave no room (up to 64 channels then, 96 for y).
-    constexpr int kHid = MODE == GRAD_X && HC == 64 ? 1 : 2, kHidColumns = MODE == FORWARD ? HC / 2 : HC;
+    // TMEM: the output of NT tiles, two accumulators of g and u, for dx two of dh, and the hidden values of two units unless
+    // those go to shared memory.
+    constexpr int kHidColumns = MODE == FORWARD ? HC / 2 : HC, kHidBlock = kTileRows * HC * 2;
     extern __shared__ uint8_t dynamic[];
     __shared__ __align__(8) uint64_t bars[4 * kMaxStages * 2 + 16];
     __shared__ uint32_t tmem_at;
@@ -429,6 +430,7 @@ __global__ void __launch_bounds__(kFfnThreads, 1) ffn_rows_kernel(const RowArgs 
     } else if (warp == kSecondWarp) {
         const uint32_t lead = elected(), kind_out = product_kind(a.c16, BF16, false, MODE == GRAD_X);
         const uint64_t w0 = MODE == FORWARD ? operand(base + a.off_d, HC * 2, 0) : operand(base + a.off_g, 128, 2 * HC * 128);
+        const uint64_t hs0 = operand(base + a.off_h, HC * 2, 0);
         Ring w(MODE == FORWARD ? a.dn : a.gn);
         int j = 0, t = 0;
         uint32_t item_parity = 0;
@@ -439,11 +441,13 @@ __global__ void __launch_bounds__(kFfnThreads, 1) ffn_rows_kernel(const RowArgs 
             WAIT(hid_full(n & 1), n >> 1 & 1);
             tmem_fence_after();
             const uint32_t out = tmem + t * a.c16;
-            const uint32_t h = hid0 + (kHid == 2 ? n & 1 : 0) * kHidColumns;
             const uint64_t ww = operand_at(w0, w.at * (MODE == FORWARD ? a.d_bytes : a.g_bytes));
 #pragma unroll
-            for (int k = 0; k < kHidColumns / 8; ++k)
-                product_tmem(lead, out, h + 8 * k, operand_at(ww, MODE == FORWARD ? 32 * k : k * 16 * 128), kind_out, j > 0 || k > 0);
+            for (int k = 0; k < kHidColumns / 8; ++k) {
+                const uint64_t b = operand_at(ww, MODE == FORWARD ? 32 * k : k * 16 * 128);
+                if (TO == TO_TMEM) product_tmem(lead, out, hid0 + (n & 1) * kHidColumns + 8 * k, b, kind_out, j > 0 || k > 0);
+                else product(lead, out, operand_at(hs0, (n & 1) * a.h_bytes + k / (HC / 16) * kHidBlock + k % (HC / 16) * 32), b, kind_out, j > 0 || k > 0);
+            }
             products_done(lead, hid_empty(n & 1));
             if (t == NT - 1) products_done(lead, MODE == FORWARD ? d_empty(w.at) : g_empty(w.at));
             if (j == a.chunks - 1) products_done(lead, out_full(t));
@@ -463,12 +467,9 @@ __global__ void __launch_bounds__(kFfnThreads, 1) ffn_rows_kernel(const RowArgs 
                 if ((n & 1) != group) continue;
                 warp_wait(acc_full(group), n >> 1 & 1, &gave_up, a.seg.status);
                 tmem_fence_after();
-                // Where the hidden values were: those of unit n - 2, or n - 1, that its product has taken.  A group waits for
-                // every use of a barrier in turn (its parity says no more than whether the last use is over).
-                const int before = n - kHid, slot = before & 1;
-                hidden_half<MODE, HC, ACT, BF16, false>(acc0 + group * 2 * HC + lanes, dh0 + group * HC + lanes, half,
-                                                        hid0 + (kHid == 2 ? group : 0) * kHidColumns + lanes, r, acc_empty(group), hid_empty(slot),
-                                                        before >> 1 & 1, &gave_up, a.seg.status);
+                hidden_half<MODE, HC, ACT, BF16, TO>(acc0 + group * 2 * HC + lanes, dh0 + group * HC + lanes, half,
+                                                     TO == TO_TMEM ? hid0 + group * kHidColumns + lanes : base + a.off_h + group * a.h_bytes, r, acc_empty(group), hid_empty(group),
+                                                     (n >> 1 & 1) ^ 1, &gave_up, a.seg.status);
                 warp_arrive(hid_full(group));
             }
             // The result takes the place of the tile's rows, which no product reads any more, and leaves from there as
@@ -532,7 +533,7 @@ template <int HC, int ACT, bool BF16>
 __global__ void __launch_bounds__(kFfnThreads, 1) ffn_weights_kernel(const WeightArgs a, const __grid_constant__ Maps maps) {
     constexpr int kOut = 3 * HC, kTwoDh = HC == 32 ? 1 : 0, kHidBlock = kTileRows * HC * 2;
     extern __shared__ uint8_t dynamic[];
-    __shared__ __align__(8) uint64_t bars[32];
+    __shared__ __align__(8) uint64_t bars[36];
     __shared__ int bounds[kMaxBounds];
     __shared__ int start[kMaxSegments + 1];
     __shared__ uint32_t tmem_at;
@@ -540,14 +541,15 @@ __global__ void __launch_bounds__(kFfnThreads, 1) ffn_weights_kernel(const Weigh
     const uint32_t base = uniform((smem_u32(dynamic) + 1023u) & ~1023u);
     const int warp = uniform((int)threadIdx.x >> 5), lane = threadIdx.x & 31;
     const uint32_t bar0 = smem_u32(bars);
-    auto x_land = [&](int s) { return bar0 + 8 * s; };
-    auto x_full = [&](int s) { return bar0 + 8 * (4 + s); };
-    auto x_empty = [&](int s) { return bar0 + 8 * (8 + s); };
-    auto acc_full = [&](int s) { return bar0 + 8 * (12 + s); };
-    auto acc_empty = [&](int s) { return bar0 + 8 * (14 + s); };
-    auto hid_full = [&](int s) { return bar0 + 8 * (16 + s); };
-    auto hid_empty = [&](int s) { return bar0 + 8 * (18 + s); };
-    const uint32_t w_full = bar0 + 8 * 20, w_empty = bar0 + 8 * 21, out_full = bar0 + 8 * 22, out_empty = bar0 + 8 * 23;
+    // A tile's stage comes and goes in parts: its rows' channels by 128, then those of dy.
+    auto x_land = [&](int p) { return bar0 + 8 * p; };
+    auto x_full = [&](int p) { return bar0 + 8 * (8 + p); };
+    auto x_empty = [&](int p) { return bar0 + 8 * (16 + p); };
+    auto acc_full = [&](int s) { return bar0 + 8 * (24 + s); };
+    auto acc_empty = [&](int s) { return bar0 + 8 * (26 + s); };
+    auto hid_full = [&](int s) { return bar0 + 8 * (28 + s); };
+    auto hid_empty = [&](int s) { return bar0 + 8 * (30 + s); };
+    const uint32_t w_full = bar0 + 8 * 32, w_empty = bar0 + 8 * 33, out_full = bar0 + 8 * 34, out_empty = bar0 + 8 * 35;
 
     load_bounds(a.seg, bounds);
     segment_starts(a.seg, bounds, kTileRows, start);
@@ -555,7 +557,7 @@ __global__ void __launch_bounds__(kFfnThreads, 1) ffn_weights_kernel(const Weigh
     if (total == 0) return;
     if (threadIdx.x == 0) {
         gave_up = 0;
-        for (int s = 0; s < kMaxStages; ++s) { bar_init(x_land(s), 1); bar_init(x_full(s), 1); bar_init(x_empty(s), 1); }
+        for (int p = 0; p < 8; ++p) { bar_init(x_land(p), 1); bar_init(x_full(p), 1); bar_init(x_empty(p), 1); }
         for (int s = 0; s < 2; ++s) {
             bar_init(acc_full(s), 1); bar_init(acc_empty(s), 8);
             bar_init(hid_full(s), 8); bar_init(hid_empty(s), 1);
@@ -569,7 +571,8 @@ __global__ void __launch_bounds__(kFfnThreads, 1) ffn_weights_kernel(const Weigh
     __syncthreads();
     tmem_fence_after();
     const uint32_t tmem = uniform(tmem_at);
-    const int halves = (a.c16 + 127) / 128;                            // of the channels, 128 lanes each
+    const int halves = (a.c16 + 127) / 128, parts = 2 * halves;        // of the channels, 128 lanes each
+    auto blocks_of = [&](int m) { return a.blocks - 2 * m < 2 ? a.blocks - 2 * m : 2; };
     const uint32_t acc0 = tmem + halves * kOut, dh0 = acc0 + 4 * HC;
     // Every role makes the same walk: for each unit of work its tiles, a piece for each expert.
     auto first_tile = [&](int r) { return (int)((long long)total * r / a.ranges); };
@@ -597,30 +600,36 @@ __global__ void __launch_bounds__(kFfnThreads, 1) ffn_weights_kernel(const Weigh
                     copy_tile(lead, base + a.off_w + a.blocks * (2 * HC * 128), &maps.down, c * HC, 0, e, w_full);
                     ++piece;
                 }
-                WAIT(x_empty(x.at), x.parity ^ 1);
-                const uint32_t to = base + x.at * a.x_bytes, bar = x_land(x.at);
-                bar_expect(lead, bar, a.x_bytes);
-                for (int b = 0; b < a.blocks; ++b) {
-                    copy_tile(lead, to + b * kBlockBytes, &maps.x, 64 * b, row, bar);
-                    copy_tile(lead, to + (a.blocks + b) * kBlockBytes, &maps.dy, 64 * b, row, bar);
+                const uint32_t to = base + x.at * a.x_bytes;
+                for (int p = 0; p < parts; ++p) {
+                    const int m = p < halves ? p : p - halves, index = x.at * parts + p;
+                    WAIT(x_empty(index), x.parity ^ 1);
+                    bar_expect(lead, x_land(index), blocks_of(m) * kBlockBytes);
+                    for (int b = 2 * m; b < 2 * m + blocks_of(m); ++b) {
+                        if (p < halves) copy_tile(lead, to + b * kBlockBytes, &maps.x, 64 * b, row, x_land(index));
+                        else copy_tile(lead, to + (a.blocks + b) * kBlockBytes, &maps.dy, 64 * b, row, x_land(index));
+                    }
                 }
             }
         }
     } else if (warp == kFixWarp) {
-        int n = 0;
+        Ring x(a.xn);
         for (int k = blockIdx.x; k < work; k += gridDim.x) {
             const int r = k / a.slices, lo = first_tile(r), hi = first_tile(r + 1);
             if (lo >= hi) continue;
             TileWalk walk = tile_at(a.seg, bounds, start, lo, kTileRows);
-            for (int i = lo; i < hi; ++i, ++n, next_tile(a.seg, walk, kTileRows)) {
-                const int s = n % a.xn;
-                WAIT(x_land(s), n / a.xn & 1);
-                if (walk.left < kTileRows) {
-                    clear_rows(base + s * a.x_bytes, 2 * a.blocks, walk.left, lane);
-                    fence_async_shared();
+            for (int i = lo; i < hi; ++i, x.next(), next_tile(a.seg, walk, kTileRows)) {
+                for (int p = 0; p < parts; ++p) {
+                    const int m = p < halves ? p : p - halves, index = x.at * parts + p;
+                    WAIT(x_land(index), x.parity);
+                    if (walk.left < kTileRows) {
+                        __syncwarp();
+                        clear_rows(base + x.at * a.x_bytes + ((p < halves ? 0 : a.blocks) + 2 * m) * kBlockBytes, blocks_of(m), walk.left, lane);
+                        fence_async_shared();
+                    }
+                    __syncwarp();
+                    if (lane == 0) bar_arrive(x_full(index));
                 }
-                __syncwarp();
-                if (lane == 0) bar_arrive(x_full(s));
             }
         }
     } else if (warp == kFirstWarp || warp == kSecondWarp) {
@@ -645,34 +654,43 @@ __global__ void __launch_bounds__(kFfnThreads, 1) ffn_weights_kernel(const Weigh
                 const uint64_t xa = operand_at(x0, x.at * a.x_bytes);
                 if (!second) {
                     if (first) WAIT(w_full, piece & 1);
-                    WAIT(x_full(x.at), x.parity);
                     WAIT(acc_empty(n & 1), (n >> 1 & 1) ^ 1);
-                    tmem_fence_after();
-                    product_blocks(lead, acc0 + (n & 1) * 2 * HC, xa, kBlockBytes, w0, 2 * HC * 128, a.c16 / 16, kind_gu);
-                    if (!kTwoDh && n > 0) {
-                        WAIT(acc_empty((n - 1) & 1), (n - 1) >> 1 & 1);
+                    for (int m = 0; m < halves; ++m) {
+                        WAIT(x_full(x.at * parts + m), x.parity);
                         tmem_fence_after();
+                        product_blocks(lead, acc0 + (n & 1) * 2 * HC, operand_at(xa, 2 * m * kBlockBytes), kBlockBytes, operand_at(w0, 2 * m * (2 * HC * 128)),
+                                       2 * HC * 128, min(8, a.c16 / 16 - 8 * m), kind_gu, m > 0);
                     }
-                    product_blocks_mn(lead, dh0 + kTwoDh * (n & 1) * HC, operand_at(xa, a.blocks * kBlockBytes), kBlockBytes, wd0, 32 * HC, a.c16 / 16, kind_dh);
+                    if (!kTwoDh && n > 0) WAIT(acc_empty((n - 1) & 1), (n - 1) >> 1 & 1);
+                    for (int m = 0; m < halves; ++m) {
+                        WAIT(x_full(x.at * parts + halves + m), x.parity);
+                        tmem_fence_after();
+                        product_blocks_mn(lead, dh0 + kTwoDh * (n & 1) * HC, operand_at(xa, (a.blocks + 2 * m) * kBlockBytes), kBlockBytes,
+                                          operand_at(wd0, 8 * m * 32 * HC), 32 * HC, min(8, a.c16 / 16 - 8 * m), kind_dh, m > 0);
+                    }
                     products_done(lead, acc_full(n & 1));
                     if (last) products_done(lead, w_empty);
                 } else {
                     if (first) WAIT(out_empty, (piece & 1) ^ 1);
-                    WAIT(x_full(x.at), x.parity);
-                    WAIT(hid_full(n & 1), n >> 1 & 1);
+                    WAIT(hid_full(n & 1), n >> 1 & 1);                     // so the tile is there, and the first products are through with it
                     tmem_fence_after();
                     const uint64_t h = operand_at(hid0, hid.at * a.h_bytes);
-                    for (int m = 0; m < halves; ++m) {
-                        const uint64_t xm = operand_at(xa, 2 * m * kBlockBytes), ym = operand_at(xm, a.blocks * kBlockBytes);
+                    for (int p = 0; p < parts; ++p) {
+                        const int m = p < halves ? p : p - halves;
+                        if (p < halves) {
+                            const uint64_t xm = operand_at(xa, 2 * m * kBlockBytes);
 #pragma unroll
-                        for (int q = 0; q < kTileRows / 16; ++q)
-                            product(lead, tmem + m * kOut, operand_at(xm, q * 16 * 128), operand_at(h, q * 32 * HC), kind_w2, !first || q > 0);
+                            for (int q = 0; q < kTileRows / 16; ++q)
+                                product(lead, tmem + m * kOut, operand_at(xm, q * 16 * 128), operand_at(h, q * 32 * HC), kind_w2, !first || q > 0);
+                        } else {
+                            const uint64_t ym = operand_at(xa, (a.blocks + 2 * m) * kBlockBytes);
 #pragma unroll
-                        for (int q = 0; q < kTileRows / 16; ++q)
-                            product(lead, tmem + m * kOut + 2 * HC, operand_at(ym, q * 16 * 128), operand_at(h, 2 * kHidBlock + q * 32 * HC), kind_w1, !first || q > 0);
+                            for (int q = 0; q < kTileRows / 16; ++q)
+                                product(lead, tmem + m * kOut + 2 * HC, operand_at(ym, q * 16 * 128), operand_at(h, 2 * kHidBlock + q * 32 * HC), kind_w1, !first || q > 0);
+                        }
+                        products_done(lead, x_empty(x.at * parts + p));
                     }
                     products_done(lead, hid_empty(n & 1));
-                    products_done(lead, x_empty(x.at));
                     if (last) products_done(lead, out_full);
                     hid.next();
                 }
@@ -695,8 +713,8 @@ __global__ void __launch_bounds__(kFfnThreads, 1) ffn_weights_kernel(const Weigh
                     const int hs = n % a.hn;
                     warp_wait(acc_full(group), n >> 1 & 1, &gave_up, a.seg.status);
                     tmem_fence_after();
-                    const int before = n - a.hn, slot = before & 1;        // see ffn_rows_kernel
-                    hidden_half<GRAD_X, HC, ACT, BF16, true>(acc0 + group * 2 * HC + lanes, dh0 + kTwoDh * group * HC + lanes, half,
+                    const int before = n - a.hn, slot = before & 1;        // a group waits for every use of a barrier in turn
+                    hidden_half<GRAD_X, HC, ACT, BF16, TO_SHARED_WITH_H>(acc0 + group * 2 * HC + lanes, dh0 + kTwoDh * group * HC + lanes, half,
                                                              base + a.off_h + hs * a.h_bytes, row, acc_empty(group), hid_empty(slot), before >> 1 & 1,
                                                              &gave_up, a.seg.status);
                     warp_arrive(hid_full(group));
@@ -844,7 +862,7 @@ long long row_tiles(const RowSegments& s, int NT) {
     return ((long long)s.B * s.N + kTileRows * NT - 1) / (kTileRows * NT) + (long long)s.B * s.E;
 }
 
-template <int MODE, int HC, int NT>
+template <int MODE, int HC, int NT, int TO>
 int launch_rows(emc2_bridge* h, const FfnCall& f, cudaStream_t st) {
     RowArgs a;
     a.seg = f.seg; a.out = f.out; a.C = f.C; a.H = f.H;
@@ -857,9 +875,10 @@ int launch_rows(emc2_bridge* h, const FfnCall& f, cudaStream_t st) {
     a.x_bytes = (MODE == FORWARD ? 1 : 2) * a.tile_bytes;
     a.g_bytes = 2 * HC * (MODE == FORWARD ? a.full * 128 + a.tail * 2 : (a.full + (a.tail > 0)) * 128);
     a.d_bytes = a.c16 * HC * 2;
+    a.h_bytes = TO == TO_TMEM ? 0 : (MODE == FORWARD ? 1 : 2) * kTileRows * HC * 2;
     // As many stages as there is room for: first two of each, then more of the rows.
     a.xn = NT; a.gn = 2; a.dn = 2;
-    auto room = [&] { return (size_t)a.xn * a.x_bytes + (size_t)a.gn * a.g_bytes + (size_t)a.dn * a.d_bytes + 1024; };
+    auto room = [&] { return (size_t)a.xn * a.x_bytes + (size_t)a.gn * a.g_bytes + (size_t)a.dn * a.d_bytes + 2 * a.h_bytes + 1024; };
     // What is left goes to the next item's rows and to twice the stages of the weights (see the first products' warps for the
     // even numbers).
     auto more_rows = [&](int n) { while (a.xn < n && room() + NT * a.x_bytes <= kMaxShared) a.xn += NT; };
@@ -868,16 +887,19 @@ int launch_rows(emc2_bridge* h, const FfnCall& f, cudaStream_t st) {
     if (NT == 1) more_rows(2);
     a.off_g = a.xn * a.x_bytes;
     a.off_d = a.off_g + a.gn * a.g_bytes;
+    a.off_h = a.off_d + a.dn * a.d_bytes;
     Maps m;
     if (!make_maps(f, HC, a.tail, &m)) return EMC2_ERR_CUDA;
     const size_t shared = std::max(room(), (size_t)(kMaxBounds + kMaxSegments + 1) * 4 + 1024);
     const int ctas = (int)std::min<long long>(row_tiles(f.seg, NT), h->num_sms), kind = MODE == FORWARD ? K_FFN : K_FFN_GRAD_X;
     const bool bf16 = f.type == EMC2_BF16;
     if (f.act == EMC2_ACT_SILU)
-        return bf16 ? launch_ffn(h, kind, ffn_rows_kernel<MODE, HC, NT, EMC2_ACT_SILU, true>, a, m, ctas, kFfnThreads, shared, st)
-                    : launch_ffn(h, kind, ffn_rows_kernel<MODE, HC, NT, EMC2_ACT_SILU, false>, a, m, ctas, kFfnThreads, shared, st);
-    return bf16 ? launch_ffn(h, kind, ffn_rows_kernel<MODE, HC, NT, EMC2_ACT_GELU, true>, a, m, ctas, kFfnThreads, shared, st)
-                : launch_ffn(h, kind, ffn_rows_kernel<MODE, HC, NT, EMC2_ACT_GELU, false>, a, m, ctas, kFfnThreads, shared, st);
+        return bf16 ? launch_ffn(h, kind, ffn_rows_kernel<MODE, HC, NT, TO, EMC2_ACT_SILU, true>, a, m, ctas, kFfnThreads, shared, st)
+                    : launch_ffn(h, kind, ffn_rows_kernel<MODE, HC, NT, TO, EMC2_ACT_SILU, false>, a, m, ctas, kFfnThreads, shared, st);
+    if constexpr (TO == TO_TMEM)
+        return bf16 ? launch_ffn(h, kind, ffn_rows_kernel<MODE, HC, NT, TO, EMC2_ACT_GELU, true>, a, m, ctas, kFfnThreads, shared, st)
+                    : launch_ffn(h, kind, ffn_rows_kernel<MODE, HC, NT, TO, EMC2_ACT_GELU, false>, a, m, ctas, kFfnThreads, shared, st);
+    return EMC2_ERR_INTERNAL;
 }
 
 // Ranges of the tiles: four units of work per SM, but eight tiles in each while that leaves one unit per SM.
@@ -987,8 +1009,8 @@ extern "C" int emc2_expert_ffn(emc2_bridge_t* h, int32_t B, int32_t N, int32_t c
     const FfnCall f = {row_segments(h, B, N, d_offsets), channels, hidden, type, act, d_x, nullptr, d_w_gate, d_w_up, d_w_down, d_y};
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     // Chunks of hidden units, and tiles that share their weights, as TMEM has room for (see ffn_rows_kernel).
-    if (channels <= 96) return launch_rows<FORWARD, 64, 2>(h, f, st);
-    return channels <= 128 ? launch_rows<FORWARD, 32, 2>(h, f, st) : launch_rows<FORWARD, 32, 1>(h, f, st);
+    if (channels <= 96) return launch_rows<FORWARD, 64, 2, TO_TMEM>(h, f, st);
+    return channels <= 128 ? launch_rows<FORWARD, 32, 2, TO_TMEM>(h, f, st) : launch_rows<FORWARD, 32, 1, TO_TMEM>(h, f, st);
 }
 
 extern "C" int emc2_expert_ffn_grad(emc2_bridge_t* h, int32_t B, int32_t N, int32_t channels, int32_t hidden, int32_t type, int32_t act,
@@ -1014,7 +1036,8 @@ extern "C" int emc2_expert_ffn_grad(emc2_bridge_t* h, int32_t B, int32_t N, int3
         if (e == cudaSuccess) e = cudaMemsetAsync(d_grad_down, 0, bytes, st);
         return check_cuda(h, e);
     }
-    rc = channels <= 64 ? launch_rows<GRAD_X, 64, 1>(h, f, st) : launch_rows<GRAD_X, 32, 1>(h, f, st);
+    // Hidden values in shared memory leave TMEM to chunks of 64 units; GELU's arithmetic has no registers for those.
+    rc = channels <= 64 && act == EMC2_ACT_SILU ? launch_rows<GRAD_X, 64, 1, TO_SHARED>(h, f, st) : launch_rows<GRAD_X, 32, 1, TO_TMEM>(h, f, st);
     if (rc == EMC2_OK) rc = launch_weights(h, f, d_grad_gate, d_grad_up, d_grad_down, st);
     return rc;
 }
