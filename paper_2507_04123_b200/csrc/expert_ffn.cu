@@ -508,9 +508,11 @@ __global__ void __launch_bounds__(kFfnThreads, 1) ffn_rows_kernel(const RowArgs 
 }
 
 // ---------------------------------------------------------------- weights: dWg, dWu, dWd
+constexpr int kShareInts = 64;              // 2 * EMC2_MAX_EXPERTS and up to a multiple of 256 bytes
 struct WeightArgs {
     RowSegments seg;
     float* part;                            // [ranges + E][slices][3 * HC][C]
+    int* share;                             // see WeightSumArgs
     int C, H, c16, blocks, slices, ranges;
     int xn, hn;
     uint32_t off_w, off_h;
@@ -553,7 +555,13 @@ __global__ void __launch_bounds__(kFfnThreads, 1) ffn_weights_kernel(const Weigh
 
     load_bounds(a.seg, bounds);
     segment_starts(a.seg, bounds, kTileRows, start);
-    const int total = uniform(start[a.seg.B * a.seg.E]), work = a.ranges * a.slices;
+    const int total = uniform(start[a.seg.B * a.seg.E]), ranges = min(a.ranges, total), work = ranges * a.slices;
+    // Range r has tiles total * r / ranges .. total * (r + 1) / ranges - 1, one at least.
+    if (blockIdx.x == 0 && threadIdx.x < a.seg.E) {
+        const long long from = start[threadIdx.x * a.seg.B], to = start[(threadIdx.x + 1) * a.seg.B];
+        a.share[2 * threadIdx.x] = from < to ? (int)(((from + 1) * ranges - 1) / total) : 0;
+        a.share[2 * threadIdx.x + 1] = from < to ? (int)((to * ranges - 1) / total) + 1 : 0;
+    }
     if (total == 0) return;
     if (threadIdx.x == 0) {
         gave_up = 0;
@@ -575,7 +583,8 @@ __global__ void __launch_bounds__(kFfnThreads, 1) ffn_weights_kernel(const Weigh
     auto blocks_of = [&](int m) { return a.blocks - 2 * m < 2 ? a.blocks - 2 * m : 2; };
     const uint32_t acc0 = tmem + halves * kOut, dh0 = acc0 + 4 * HC;
     // Every role makes the same walk: for each unit of work its tiles, a piece for each expert.
-    auto first_tile = [&](int r) { return (int)((long long)total * r / a.ranges); };
+    auto expert_of = [&](int tile) { return tile < total ? segment_of(start, a.seg.B * a.seg.E, tile) / a.seg.B : a.seg.E; };
+    auto first_tile = [&](int r) { return (int)((long long)total * r / ranges); };
 
     if (warp == kCopyWarp) {
         const uint32_t lead = elected();
@@ -583,7 +592,6 @@ __global__ void __launch_bounds__(kFfnThreads, 1) ffn_weights_kernel(const Weigh
         int piece = 0;
         for (int k = blockIdx.x; k < work && !__any_sync(0xFFFFFFFFu, *(volatile int*)&gave_up); k += gridDim.x) {
             const int r = k / a.slices, c = k - r * a.slices, lo = first_tile(r), hi = first_tile(r + 1);
-            if (lo >= hi) continue;
             TileWalk walk = tile_at(a.seg, bounds, start, lo, kTileRows);
             int e = -1;
             for (int i = lo; i < hi; ++i, x.next(), next_tile(a.seg, walk, kTileRows)) {
@@ -616,7 +624,6 @@ __global__ void __launch_bounds__(kFfnThreads, 1) ffn_weights_kernel(const Weigh
         Ring x(a.xn);
         for (int k = blockIdx.x; k < work; k += gridDim.x) {
             const int r = k / a.slices, lo = first_tile(r), hi = first_tile(r + 1);
-            if (lo >= hi) continue;
             TileWalk walk = tile_at(a.seg, bounds, start, lo, kTileRows);
             for (int i = lo; i < hi; ++i, x.next(), next_tile(a.seg, walk, kTileRows)) {
                 for (int p = 0; p < parts; ++p) {
@@ -643,14 +650,11 @@ __global__ void __launch_bounds__(kFfnThreads, 1) ffn_weights_kernel(const Weigh
         int n = 0, piece = 0;
         for (int k = blockIdx.x; k < work; k += gridDim.x) {
             const int r = k / a.slices, lo = first_tile(r), hi = first_tile(r + 1);
-            if (lo >= hi) continue;
-            TileWalk walk = tile_at(a.seg, bounds, start, lo, kTileRows);
-            int e = uniform(walk.q / a.seg.B);
-            bool first = true;
+            int end = lo;                                                  // of the piece
             for (int i = lo; i < hi; ++i, ++n, x.next()) {
-                next_tile(a.seg, walk, kTileRows);
-                const int next_e = uniform(walk.q / a.seg.B);
-                const bool last = i + 1 == hi || next_e != e;
+                const bool first = i == end;
+                if (first) end = uniform(min(hi, start[(expert_of(i) + 1) * a.seg.B]));
+                const bool last = i + 1 == end;
                 const uint64_t xa = operand_at(x0, x.at * a.x_bytes);
                 if (!second) {
                     if (first) WAIT(w_full, piece & 1);
@@ -694,28 +698,23 @@ __global__ void __launch_bounds__(kFfnThreads, 1) ffn_weights_kernel(const Weigh
                     if (last) products_done(lead, out_full);
                     hid.next();
                 }
-                first = last;
-                if (last) { ++piece; e = next_e; }
+                if (last) ++piece;
             }
         }
     } else if (warp < kEpilogueWarps) {
         const int group = warp >> 3, half = warp >> 2 & 1, quarter = warp & 3, row = quarter * 32 + lane;
-        const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
+        const uint32_t lanes = (uint32_t)(quarter * 32) << 16, hid = base + a.off_h;
         int n = 0, piece = 0;
         for (int k = blockIdx.x; k < work; k += gridDim.x) {
             const int r = k / a.slices, c = k - r * a.slices, lo = first_tile(r), hi = first_tile(r + 1);
-            if (lo >= hi) continue;
-            TileWalk walk = tile_at(a.seg, bounds, start, lo, kTileRows);
-            for (int i = lo; i < hi;) {
-                const int e = walk.q / a.seg.B;
-                for (; i < hi && walk.q / a.seg.B == e; ++i, ++n, next_tile(a.seg, walk, kTileRows)) {
+            for (int i = lo, e = expert_of(lo); i < hi; e = expert_of(i)) {
+                for (const int end = min(hi, start[(e + 1) * a.seg.B]); i < end; ++i, ++n) {
                     if ((n & 1) != group) continue;
-                    const int hs = n % a.hn;
                     warp_wait(acc_full(group), n >> 1 & 1, &gave_up, a.seg.status);
                     tmem_fence_after();
                     const int before = n - a.hn, slot = before & 1;        // a group waits for every use of a barrier in turn
                     hidden_half<GRAD_X, HC, ACT, BF16, TO_SHARED_WITH_H>(acc0 + group * 2 * HC + lanes, dh0 + kTwoDh * group * HC + lanes, half,
-                                                             base + a.off_h + hs * a.h_bytes, row, acc_empty(group), hid_empty(slot), before >> 1 & 1,
+                                                             hid + (a.hn == 2 ? group * a.h_bytes : 0), row, acc_empty(group), hid_empty(slot), before >> 1 & 1,
                                                              &gave_up, a.seg.status);
                     warp_arrive(hid_full(group));
                 }
@@ -750,50 +749,44 @@ __global__ void __launch_bounds__(kFfnThreads, 1) ffn_weights_kernel(const Weigh
 }
 
 struct WeightSumArgs {
-    RowSegments seg;
     const float* part;
+    const int* share;               // [E][2]: first range with tiles of the expert and the one behind the last; as ffn_weights_kernel left it
     void* gate;
     void* up;
     void* down;
-    int C, H, slice, slices, ranges, type;
+    int C, H, E, slice, slices, ranges, type;
 };
 
-// dW of eight hidden units and 32 channels: the parts of the ranges that met the expert, every eighth by one warp, then the
-// warps' sums in their order.
-constexpr int kSumUnits = 8;
+// dW of 32 / RS hidden units and 32 channels: the parts of the ranges that met the expert.  Four units per warp; every RS-th
+// part by one warp where there are many, then the warps' sums in their order.
+template <int RS>
 __global__ void __launch_bounds__(256) ffn_sum_kernel(WeightSumArgs a) {
-    __shared__ int bounds[kMaxBounds];
-    __shared__ int start[kMaxSegments + 1];
-    __shared__ float sums[8][kSumUnits][33];
-    load_bounds(a.seg, bounds);
-    segment_starts(a.seg, bounds, kTileRows, start);
-    const int columns = (a.C + 31) / 32, kind = blockIdx.y, e = blockIdx.z, B = a.seg.B, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const long long total = start[B * a.seg.E], from = start[e * B], to = start[(e + 1) * B];
-    const int r0 = from < to ? (int)(((from + 1) * a.ranges - 1) / total) : 0, r1 = from < to ? (int)((to * a.ranges - 1) / total) : -1;
+    constexpr int kUnits = 32 / RS;
+    __shared__ float sums[RS][kUnits][33];
+    const int columns = (a.C + 31) / 32, kind = blockIdx.y, e = blockIdx.z, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int c0 = blockIdx.x % columns * 32, h0 = blockIdx.x / columns * kUnits, mine = warp % RS, u0 = warp / RS * 4;
+    const int r0 = __ldg(a.share + 2 * e), r1 = __ldg(a.share + 2 * e + 1);
+    float s[4] = {0.f, 0.f, 0.f, 0.f};
+    if (c0 + lane < a.C) {
+        const size_t step = (size_t)a.slices * 3 * a.slice * a.C;             // from a range to the next
+        const float* p = a.part + ((size_t)e * a.slices + h0 / a.slice) * 3 * a.slice * a.C + ((size_t)kind * a.slice + h0 % a.slice + u0) * a.C + c0 + lane;
+#pragma unroll 4
+        for (int r = r0 + mine; r < r1; r += RS)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) s[k] += __ldg(p + r * step + (size_t)k * a.C);
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) sums[mine][u0 + k][lane] = s[k];
+    __syncthreads();
     uint16_t* out = static_cast<uint16_t*>(kind == 0 ? a.gate : kind == 1 ? a.up : a.down);
-    for (int tile = blockIdx.x; tile < columns * ((a.H + kSumUnits - 1) / kSumUnits); tile += gridDim.x) {
-        const int c0 = tile % columns * 32, h0 = tile / columns * kSumUnits;
-        float s[kSumUnits];
-#pragma unroll
-        for (int k = 0; k < kSumUnits; ++k) s[k] = 0.f;
-        if (c0 + lane < a.C)
-            for (int r = r0 + warp; r <= r1; r += 8) {
-                if (total * r / a.ranges == total * (r + 1) / a.ranges) continue;     // more ranges than tiles: it had none
-                const float* p = a.part + (((size_t)(r + e) * a.slices + h0 / a.slice) * 3 * a.slice + kind * a.slice + h0 % a.slice) * a.C + c0 + lane;
-#pragma unroll
-                for (int k = 0; k < kSumUnits; ++k) s[k] += p[(size_t)k * a.C];
-            }
-#pragma unroll
-        for (int k = 0; k < kSumUnits; ++k) sums[warp][k][lane] = s[k];
-        __syncthreads();
+    for (int i = threadIdx.x; i < kUnits * 32; i += 256) {
         // Consecutive threads write consecutive addresses: channels of [E, H, C], hidden units of [E, C, H].
-        const int h = kind < 2 ? warp : threadIdx.x & 7, c = kind < 2 ? lane : threadIdx.x >> 3;
+        const int h = kind < 2 ? i >> 5 : i % kUnits, c = kind < 2 ? i & 31 : i / kUnits;
         float v = sums[0][h][c];
 #pragma unroll
-        for (int w = 1; w < 8; ++w) v += sums[w][h][c];
+        for (int w = 1; w < RS; ++w) v += sums[w][h][c];
         if (h0 + h < a.H && c0 + c < a.C)
             out[kind < 2 ? ((size_t)e * a.H + h0 + h) * a.C + c0 + c : ((size_t)e * a.C + c0 + c) * a.H + h0 + h] = (uint16_t)as_halves(v, 0.f, a.type);
-        __syncthreads();
     }
 }
 
@@ -934,7 +927,8 @@ size_t plan_weights(WeightArgs& a, const FfnCall& f) {
 template <int HC>
 int launch_slices(emc2_bridge* h, const FfnCall& f, WeightArgs& a, cudaStream_t st) {
     const size_t shared = plan_weights<HC>(a, f);
-    a.part = static_cast<float*>(h->rows_scratch.slab);
+    a.share = static_cast<int*>(h->rows_scratch.slab);
+    a.part = reinterpret_cast<float*>(a.share + kShareInts);
     a.ranges = weight_ranges(h, a.slices, row_tiles(f.seg, 1));
     Maps m;
     if (!make_maps(f, HC, 0, &m)) return EMC2_ERR_CUDA;
@@ -961,11 +955,13 @@ int launch_weights(emc2_bridge* h, const FfnCall& f, void* gate, void* up, void*
     const int rc = wide ? launch_slices<64>(h, f, a, st) : launch_slices<32>(h, f, a, st);
     if (rc != EMC2_OK) return rc;
     WeightSumArgs s;
-    s.seg = f.seg; s.part = a.part; s.gate = gate; s.up = up; s.down = down; s.C = f.C; s.H = f.H; s.slice = wide ? 64 : 32; s.slices = a.slices; s.ranges = a.ranges;
-    s.type = f.type;
+    s.part = a.part; s.share = a.share; s.gate = gate; s.up = up; s.down = down; s.C = f.C; s.H = f.H; s.E = f.seg.E;
+    s.slice = wide ? 64 : 32; s.slices = a.slices; s.ranges = a.ranges; s.type = f.type;
     LaunchScope ls(h, K_FFN_SUM, st);
-    const int sums = (f.H + kSumUnits - 1) / kSumUnits * ((f.C + 31) / 32), most = std::max(1, 6 * h->num_sms / (3 * f.seg.E));
-    ffn_sum_kernel<<<dim3(std::min(sums, most), 3, f.seg.E), 256, 0, st>>>(s);
+    // A few parts for each expert, or many.
+    const int columns = (f.C + 31) / 32;
+    if (a.ranges > 16 * f.seg.E) ffn_sum_kernel<8><<<dim3((f.H + 3) / 4 * columns, 3, f.seg.E), 256, 0, st>>>(s);
+    else ffn_sum_kernel<1><<<dim3((f.H + 31) / 32 * columns, 3, f.seg.E), 256, 0, st>>>(s);
     return check_cuda(h, cudaGetLastError());
 }
 
@@ -989,7 +985,7 @@ size_t ffn_scratch_bytes(const emc2_bridge* h, int max_channels, int max_hidden)
     for (int slice : {32, 64})
         for (int slices = 1; slices <= (max_hidden + slice - 1) / slice; ++slices)
             most = std::max(most, (size_t)(weight_ranges(h, slices, 1LL << 40) + EMC2_MAX_EXPERTS) * slices * 3 * slice * C * sizeof(float));
-    return most;
+    return most + kShareInts * sizeof(int);
 }
 
 }  // namespace emc2

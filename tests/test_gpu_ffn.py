@@ -11,10 +11,10 @@ SHAPES = [(1, 1, 8, 8, 1), (1, 128, 64, 64, 1), (1, 129, 64, 256, 4), (3, 300, 8
           (1, 400, 256, 1024, 5), (32, 40, 24, 72, 16), (1, 3000, 72, 200, 2), (2, 700, 200, 136, 3), (1, 513, 192, 64, 1), (1, 37, 16, 2048, 1)]
 
 
-def inputs(B, N, C, H, E, dtype, seed=0):
+def inputs(B, N, C, H, E, dtype, seed=0, rows=lambda offsets, N: offsets):
     g = torch.Generator(device=DEV)
     g.manual_seed(seed + B * N + C)
-    offsets = ascending_offsets(B, N, E, seed=N + seed)
+    offsets = rows(ascending_offsets(B, N, E, seed=N + seed), N).to(torch.int32).contiguous()
     e = expert_of_rows(offsets, N, E)
     x, dy = (torch.randn((B, N, C), generator=g, device=DEV).to(dtype) for _ in range(2))
     x[e == E], dy[e == E] = float("nan"), float("inf")                     # rows of no expert reach nothing
@@ -46,11 +46,20 @@ def test_ffn(B, N, C, H, E, dtype, act):
     br.close()
 
 
+def spread(offsets, N):
+    return offsets
+
+
+def few(offsets, N):
+    """Almost every row belongs to no expert."""
+    return torch.clamp(offsets - (N - 5), min=0) + 3 * (N > 200)
+
+
 @pytest.mark.parametrize("act", ["silu", "gelu"])
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16], ids=str)
-@pytest.mark.parametrize("B,N,C,H,E", SHAPES)
-def test_ffn_gradients(B, N, C, H, E, dtype, act):
-    x, dy, offsets, e, (wg, wu, wd) = inputs(B, N, C, H, E, dtype)
+@pytest.mark.parametrize("B,N,C,H,E,rows", [(*shape, spread) for shape in SHAPES] + [(3, 5000, 64, 96, 3, few), (2, 9000, 200, 72, 2, few)])
+def test_ffn_gradients(B, N, C, H, E, rows, dtype, act):
+    x, dy, offsets, e, (wg, wu, wd) = inputs(B, N, C, H, E, dtype, rows=rows)
     br = handle(B, N, E)
     br.reserve_rows(C, H)
     out = {"grad_x": torch.full_like(x, 7.0), **{k: torch.full_like(w, float("nan")) for k, w in (("grad_gate", wg), ("grad_up", wu), ("grad_down", wd))}}
