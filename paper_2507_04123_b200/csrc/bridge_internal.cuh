@@ -270,11 +270,6 @@ int launch_voxelize(emc2_bridge* h, int B, int N, const float* d_points, int32_t
                     const int32_t capacity[2], int32_t* d_num_voxels, float* d_bev, cudaStream_t st,
                     bool marked = false, bool chained = false);
 int dedup_arm_alloc(emc2_bridge* h);
-// Sorts n (key, value) pairs by the low `bits` bits of the key, stably; returns which buffer holds the result.  counts:
-// [256][sort_tiles(n)], row_tot: [256].  `kind`: the kernel kind that the launches count as.
-int sort_tiles(size_t n);
-int radix_sort(emc2_bridge* h, int kind, int n, int bits, uint32_t* const keys[2], uint32_t* const vals[2], bool with_vals, int* counts,
-               int* row_tot, cudaStream_t st);
 // Scratch that the operators on rows of up to max_channels channels need on this handle.
 size_t norm_scratch_bytes(const emc2_bridge* h, int max_channels);
 size_t lookup_scratch_bytes(const emc2_bridge* h, int max_channels);

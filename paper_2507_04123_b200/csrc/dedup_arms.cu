@@ -352,26 +352,25 @@ int key_bits(uint64_t cells_in_call) {               // bits that tell every cel
     return bits;
 }
 
-}  // namespace
-
-int sort_tiles(size_t n) { return (int)((n + kSortTile - 1) / kSortTile); }
-
-int radix_sort(emc2_bridge* h, int kind, int n, int bits, uint32_t* const keys[2], uint32_t* const vals[2], bool with_vals, int* counts,
-               int* row_tot, cudaStream_t st) {
-    const int tiles = sort_tiles((size_t)n);
+// Sorts n (key, value) pairs by the low `bits` bits of the key; returns which buffer holds the result.
+int radix_sort(emc2_bridge* h, int n, int bits, uint32_t* keys[2], uint32_t* vals[2], bool with_vals, cudaStream_t st) {
+    const int tiles = (n + kSortTile - 1) / kSortTile;
     int cur = 0;
     for (int shift = 0; shift < bits; shift += 8) {
         {
-            LaunchScope ls(h, kind, st);
-            rs_hist_kernel<<<tiles, kThreads, 0, st>>>(keys[cur], n, shift, tiles, counts);
-            rs_rowscan_kernel<<<256, kThreads, 0, st>>>(counts, tiles, row_tot);
+            LaunchScope ls(h, K_ARM_SORT, st);
+            rs_hist_kernel<<<tiles, kThreads, 0, st>>>(keys[cur], n, shift, tiles, h->arm.counts);
+            rs_rowscan_kernel<<<256, kThreads, 0, st>>>(h->arm.counts, tiles, h->arm.row_tot);
             rs_scatter_kernel<<<tiles, kThreads, 0, st>>>(keys[cur], with_vals ? vals[cur] : nullptr, keys[cur ^ 1],
-                                                          with_vals ? vals[cur ^ 1] : nullptr, n, shift, tiles, counts, row_tot);
+                                                          with_vals ? vals[cur ^ 1] : nullptr, n, shift, tiles,
+                                                          h->arm.counts, h->arm.row_tot);
         }
         cur ^= 1;
     }
     return cur;
 }
+
+}  // namespace
 
 int dedup_arm_alloc(emc2_bridge* h) {
     if (h->arm.slab) return EMC2_OK;
@@ -431,7 +430,7 @@ int launch_dedup_arm(emc2_bridge* h, int s, int design, int B, int N, const floa
             arm_keys_kernel<5><<<blocks, kThreads, 0, st>>>(d_points, n, N, g, h->arm.keys[0], design == 2 ? h->arm.vals[0] : nullptr);
     }
     if (design == 2) {
-        const int cur = radix_sort(h, K_ARM_SORT, n, bits, h->arm.keys, h->arm.vals, true, h->arm.counts, h->arm.row_tot, st);
+        const int cur = radix_sort(h, n, bits, h->arm.keys, h->arm.vals, true, st);
         const int head_tiles = (n + kHeadTile - 1) / kHeadTile;
         LaunchScope ls(h, K_ARM_RANK, st);
         head_count_kernel<<<head_tiles, kThreads, 0, st>>>(h->arm.keys[cur], n, h->arm.tile_tot);
@@ -446,7 +445,7 @@ int launch_dedup_arm(emc2_bridge* h, int s, int design, int B, int N, const floa
             hash_insert_kernel<<<blocks, kThreads, 0, st>>>(h->arm.keys[0], n, h->arm.tab_keys, h->arm.slots - 1,
                                                             h->arm.vals[0], h->d_status);
         }
-        const int cur = radix_sort(h, K_ARM_SORT, n, bits, h->arm.vals, h->arm.keys, false, h->arm.counts, h->arm.row_tot, st);
+        const int cur = radix_sort(h, n, bits, h->arm.vals, h->arm.keys, false, st);
         LaunchScope ls(h, K_ARM_RANK, st);
         hash_assign_kernel<<<blocks, kThreads, 0, st>>>(h->arm.vals[cur], n, h->arm.tab_keys, h->arm.tab_rows,
                                                         h->arm.slots - 1, h->arm.d_total, o);

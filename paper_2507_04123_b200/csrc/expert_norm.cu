@@ -3,7 +3,8 @@
 //   m = mean(x), r = 1 / sqrt(mean((x - m)^2) + eps), h = (x - m) r, y = h w_e + b_e
 //   g = dy w_e:  dx = r (g - mean(g) - h mean(g h)),  dw_e = sum dy h,  db_e = sum dy   over the expert's rows
 //
-// Bound by memory: a row is read once, held in the registers of a group of lanes (see row_split), and written once.
+// Bound by memory: a row is read once, held in the registers of a group of lanes (see row_split), and written once.  The
+// weights are read from shared memory, so that registers are left for enough warps to keep the loads in flight.
 // Sums, means and gradients of the parameters are held in fp32; y and dx are rounded once.
 #include <algorithm>
 
@@ -13,6 +14,7 @@ namespace emc2 {
 namespace {
 
 constexpr int kNormThreads = 256;
+constexpr int kNormShared = 24 * 1024;       // of weights; more are read through the L1 cache
 
 struct NormArgs {
     RowSegments seg;
@@ -24,21 +26,34 @@ struct NormArgs {
     float* mean;                 // or null
     float* rstd;                 // or null
     float eps, inv_c;
-    int nvec, log, type_x, type_y;
+    int nvec, log, type_x, type_y, shared;
 };
 
-// Rows in the caller's order, one per group of lanes and step.  The weights of the expert whose rows a group is at stay
-// in its registers.
+// Weights (and biases) of all experts in shared memory, or where they are.  The caller synchronises the CTA.
+__device__ __forceinline__ void stage_weights(const float* w, const float* bias, int vectors, bool shared, float4* at, const float4*& ws, const float4*& bs) {
+    ws = reinterpret_cast<const float4*>(w);
+    bs = reinterpret_cast<const float4*>(bias);
+    if (!shared) return;
+    for (int i = threadIdx.x; i < vectors; i += blockDim.x) {
+        at[i] = ws[i];
+        if (bias) at[vectors + i] = bs[i];
+    }
+    ws = at;
+    if (bias) bs = at + vectors;
+}
+
+// Rows in the caller's order, one per group of lanes and step.
 template <int K>
-__global__ void __launch_bounds__(kNormThreads) norm_kernel(NormArgs a) {
+__global__ void __launch_bounds__(kNormThreads, K <= 2 ? 6 : K <= 4 ? 4 : K <= 6 ? 3 : 2) norm_kernel(NormArgs a) {
     __shared__ int bounds[kMaxBounds];
+    extern __shared__ float4 weights[];
+    const float4 *ws, *bs;
+    stage_weights(a.weight, a.bias, a.seg.E * a.nvec, a.shared, weights, ws, bs);
     load_bounds(a.seg, bounds);
     const int lane = threadIdx.x & ((1 << a.log) - 1);
     const uint32_t rows = (uint32_t)a.seg.B * a.seg.N, groups = (gridDim.x * kNormThreads) >> a.log;
     const uint32_t sub = (threadIdx.x & 31) >> a.log, first = (blockIdx.x * kNormThreads + threadIdx.x) >> a.log;
     const int E = a.seg.E;
-    float4 w[K], bias[K];
-    int have = -1;
     // All groups of a warp make the same number of steps: the sums are taken by the whole warp.
     for (uint32_t r0 = first - sub; r0 < rows; r0 += groups) {
         const uint32_t row = r0 + sub;
@@ -55,16 +70,6 @@ __global__ void __launch_bounds__(kNormThreads) norm_kernel(NormArgs a) {
         const bool in = e < E;
         float4 x[K];
         load_row<K>(x, a.x, (size_t)row * a.nvec, lane, a.log, in ? a.nvec : 0, a.type_x);
-        if (in && e != have) {
-            have = e;
-#pragma unroll
-            for (int i = 0; i < K; ++i) {
-                const int v = lane + (i << a.log);
-                const float4 zero = make_float4(0.f, 0.f, 0.f, 0.f);
-                w[i] = v < a.nvec ? __ldg(reinterpret_cast<const float4*>(a.weight) + e * a.nvec + v) : zero;
-                bias[i] = a.bias && v < a.nvec ? __ldg(reinterpret_cast<const float4*>(a.bias) + e * a.nvec + v) : zero;
-            }
-        }
         float s = 0.f;
 #pragma unroll
         for (int i = 0; i < K; ++i) s += (x[i].x + x[i].y) + (x[i].z + x[i].w);
@@ -83,8 +88,12 @@ __global__ void __launch_bounds__(kNormThreads) norm_kernel(NormArgs a) {
         for (int i = 0; i < K; ++i) {
             const int v = lane + (i << a.log);
             if (v >= a.nvec) continue;
-            const float4 o = make_float4(x[i].x * r * w[i].x + bias[i].x, x[i].y * r * w[i].y + bias[i].y,
-                                         x[i].z * r * w[i].z + bias[i].z, x[i].w * r * w[i].w + bias[i].w);
+            const float4 w = ws[e * a.nvec + v];
+            float4 o = make_float4(x[i].x * r * w.x, x[i].y * r * w.y, x[i].z * r * w.z, x[i].w * r * w.w);
+            if (a.bias) {
+                const float4 c = bs[e * a.nvec + v];
+                o.x += c.x; o.y += c.y; o.z += c.z; o.w += c.w;
+            }
             store_row4(a.y, (size_t)row * a.nvec + v, o, a.type_y);
         }
         if (lane == 0) {
@@ -103,6 +112,7 @@ struct NormGradArgs {
     const float* rstd;
     void* dx;
     float* part;                 // [gridDim.x + E][2][C]: sums of dw and db of a CTA's rows of an expert
+    int* share;                  // [E][2]: first CTA with rows of the expert and the one behind the last
     float inv_c;
     int nvec, log, type_x, type_y;
 };
@@ -111,25 +121,33 @@ struct NormGradArgs {
 // gradients of each in registers.  Entry i + e of `part` holds those of CTA i and expert e: along the run of all rows
 // either i or e goes up, so no two share an entry.
 template <int K>
-__global__ void __launch_bounds__(kNormThreads, 1) norm_grad_kernel(NormGradArgs a) {
+__global__ void __launch_bounds__(kNormThreads, K <= 2 ? 3 : K <= 4 ? 2 : 1) norm_grad_kernel(NormGradArgs a) {
     __shared__ int bounds[kMaxBounds];
     __shared__ int start[kMaxSegments + 1];
     extern __shared__ float4 sums[];             // [warps][2][nvec]
+    __shared__ float4 ws[kMaxRowChannels / 4];
     load_bounds(a.seg, bounds);
     segment_starts(a.seg, bounds, 1, start);
-    const int B = a.seg.B, E = a.seg.E, total = start[B * E];
-    const int lo = (int)((long long)total * blockIdx.x / gridDim.x), hi = (int)((long long)total * (blockIdx.x + 1) / gridDim.x);
+    // CTA i has rows total * i / ctas .. total * (i + 1) / ctas - 1 of the run of all rows, one at least.
+    const int B = a.seg.B, E = a.seg.E, total = start[B * E], ctas = min((int)gridDim.x, total);
+    if (blockIdx.x == 0 && threadIdx.x < E) {
+        const long long from = start[threadIdx.x * B], to = start[(threadIdx.x + 1) * B];
+        a.share[2 * threadIdx.x] = from < to ? (int)(((from + 1) * ctas - 1) / total) : 0;
+        a.share[2 * threadIdx.x + 1] = from < to ? (int)((to * ctas - 1) / total) + 1 : 0;
+    }
+    if ((int)blockIdx.x >= ctas) return;
+    const int lo = (int)((long long)total * blockIdx.x / ctas), hi = (int)((long long)total * (blockIdx.x + 1) / ctas);
     const int lanes = 1 << a.log, lane = threadIdx.x & (lanes - 1), warp = threadIdx.x >> 5;
     const int per_warp = 32 >> a.log, sub = (threadIdx.x & 31) >> a.log, step = kNormThreads >> a.log;
-    if (lo >= hi) return;
     for (int e = segment_of(start, B * E, lo) / B; e < E && start[e * B] < hi; ++e) {
         const int from = max(lo, start[e * B]), to = min(hi, start[(e + 1) * B]);
         if (from >= to) continue;
-        float4 w[K], dw[K], db[K];
+        float4 dw[K], db[K];
+        __syncthreads();                                          // the weights of the expert before are done with
+        for (int v = threadIdx.x; v < a.nvec; v += kNormThreads) ws[v] = __ldg(reinterpret_cast<const float4*>(a.weight) + e * a.nvec + v);
+        __syncthreads();
 #pragma unroll
         for (int i = 0; i < K; ++i) {
-            const int v = lane + (i << a.log);
-            w[i] = v < a.nvec ? __ldg(reinterpret_cast<const float4*>(a.weight) + e * a.nvec + v) : make_float4(0.f, 0.f, 0.f, 0.f);
             dw[i] = db[i] = make_float4(0.f, 0.f, 0.f, 0.f);
         }
         int q = e * B;
@@ -153,7 +171,8 @@ __global__ void __launch_bounds__(kNormThreads, 1) norm_grad_kernel(NormGradArgs
                 x[i].x = (x[i].x - m) * r; x[i].y = (x[i].y - m) * r; x[i].z = (x[i].z - m) * r; x[i].w = (x[i].w - m) * r;
                 dw[i].x += g[i].x * x[i].x; dw[i].y += g[i].y * x[i].y; dw[i].z += g[i].z * x[i].z; dw[i].w += g[i].w * x[i].w;
                 db[i].x += g[i].x; db[i].y += g[i].y; db[i].z += g[i].z; db[i].w += g[i].w;
-                g[i].x *= w[i].x; g[i].y *= w[i].y; g[i].z *= w[i].z; g[i].w *= w[i].w;
+                const float4 w = ws[lane + (i << a.log)];
+                g[i].x *= w.x; g[i].y *= w.y; g[i].z *= w.z; g[i].w *= w.w;
                 s += (g[i].x + g[i].y) + (g[i].z + g[i].w);
                 t += (g[i].x * x[i].x + g[i].y * x[i].y) + (g[i].z * x[i].z + g[i].w * x[i].w);
             }
@@ -201,39 +220,36 @@ __global__ void __launch_bounds__(kNormThreads, 1) norm_grad_kernel(NormGradArgs
 }
 
 struct NormSumArgs {
-    RowSegments seg;
     const float* part;
+    const int* share;
     float* dweight;
     float* dbias;                // or null
-    int ctas, C;                 // of norm_grad_kernel
+    int C;
 };
 
-// dw_e and db_e: the entries of the CTAs that had rows of expert e, in their order; 32 columns per CTA.
-__global__ void __launch_bounds__(kNormThreads) norm_sum_kernel(NormSumArgs a) {
-    constexpr int kWarps = kNormThreads / 32;
-    __shared__ int bounds[kMaxBounds];
-    __shared__ int start[kMaxSegments + 1];
-    __shared__ float sum[kWarps][32];
-    load_bounds(a.seg, bounds);
-    segment_starts(a.seg, bounds, 1, start);
-    const int e = blockIdx.y, B = a.seg.B, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const long long total = start[B * a.seg.E], from = start[e * B], to = start[(e + 1) * B];
-    const int c = blockIdx.x * 32 + lane;                                  // column of [dw | db]
+// dw_e and db_e: the entries of the CTAs that had rows of expert e, every 32nd by one warp, then the warps' sums in their
+// order; 32 columns per CTA.
+constexpr int kNormSumThreads = 1024;
+__global__ void __launch_bounds__(kNormSumThreads) norm_sum_kernel(NormSumArgs a) {
+    constexpr int kWarps = kNormSumThreads / 32;
+    __shared__ float sum[kWarps][33];
+    const int e = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;     // column of [dw | db]
+    const int i0 = __ldg(a.share + 2 * e), i1 = __ldg(a.share + 2 * e + 1);
     float s = 0.f;
-    if (from < to && c < 2 * a.C) {
-        // CTA i has rows total * i / ctas .. total * (i + 1) / ctas - 1: those of the first and of the last row.
-        const int i0 = (int)(((from + 1) * a.ctas - 1) / total), i1 = (int)((to * a.ctas - 1) / total);
-        for (int i = i0 + warp; i <= i1; i += kWarps) {
-            if (total * i / a.ctas == total * (i + 1) / a.ctas) continue;  // more CTAs than rows: it had none
-            s += a.part[(size_t)(i + e) * 2 * a.C + c];
-        }
+    if (c < 2 * a.C) {
+#pragma unroll 4
+        for (int i = i0 + warp; i < i1; i += kWarps) s += __ldg(a.part + (size_t)(i + e) * 2 * a.C + c);
     }
     sum[warp][lane] = s;
     __syncthreads();
-    if (warp == 0 && c < 2 * a.C) {
-        for (int k = 1; k < kWarps; ++k) s += sum[k][lane];
-        if (c < a.C) a.dweight[e * a.C + c] = s;
-        else if (a.dbias) a.dbias[e * a.C + c - a.C] = s;
+    // Warp w adds up column w: its lanes hold the warps' sums.
+    float v = sum[lane][warp];
+#pragma unroll
+    for (int d = 16; d; d >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, d);
+    const int mine = blockIdx.x * 32 + warp;
+    if (lane == 0 && mine < 2 * a.C) {
+        if (mine < a.C) a.dweight[e * a.C + mine] = v;
+        else if (a.dbias) a.dbias[e * a.C + mine - a.C] = v;
     }
 }
 
@@ -253,18 +269,20 @@ void by_vectors(int per, const A&... args) {
 
 template <int K>
 struct Norm {
-    static void go(const NormArgs& a, int ctas, cudaStream_t st) { norm_kernel<K><<<ctas, kNormThreads, 0, st>>>(a); }
+    static void go(const NormArgs& a, int ctas, size_t shared, cudaStream_t st) { norm_kernel<K><<<ctas, kNormThreads, shared, st>>>(a); }
 };
 template <int K>
 struct NormGrad {
     static void go(const NormGradArgs& a, int ctas, size_t shared, cudaStream_t st) {
-        if (shared > 32 * 1024)
+        if (shared > 24 * 1024)
             cudaFuncSetAttribute(norm_grad_kernel<K>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)shared);
         norm_grad_kernel<K><<<ctas, kNormThreads, shared, st>>>(a);
     }
 };
 
-int norm_grad_ctas(const emc2_bridge* h) { return 2 * h->num_sms; }
+// As many as are resident, see the kernel's launch bounds.
+int norm_grad_ctas(const emc2_bridge* h, int per) { return (per <= 2 ? 3 : per <= 4 ? 2 : 1) * h->num_sms; }
+constexpr int kShareInts = 64;               // 2 * EMC2_MAX_EXPERTS and up to a multiple of 256 bytes
 
 int check_norm(const emc2_bridge* h, int B, int N, int channels, int type_x, int type_y, const void* x, const int32_t* offsets,
                const float* weight) {
@@ -279,7 +297,7 @@ int check_norm(const emc2_bridge* h, int B, int N, int channels, int type_x, int
 }  // namespace
 
 size_t norm_scratch_bytes(const emc2_bridge* h, int max_channels) {
-    return (size_t)(norm_grad_ctas(h) + EMC2_MAX_EXPERTS) * 2 * max_channels * sizeof(float);
+    return kShareInts * sizeof(int) + (size_t)(norm_grad_ctas(h, 1) + EMC2_MAX_EXPERTS) * 2 * max_channels * sizeof(float);
 }
 
 }  // namespace emc2
@@ -302,12 +320,14 @@ extern "C" int emc2_expert_norm(emc2_bridge_t* h, int32_t B, int32_t N, int32_t 
     a.frame = make_fast_div((uint32_t)N);
     a.x = d_x; a.weight = d_weight; a.bias = d_bias; a.y = d_y; a.mean = d_mean; a.rstd = d_rstd;
     a.eps = eps; a.inv_c = 1.0f / (float)channels; a.nvec = channels / 4; a.type_x = type_x; a.type_y = type_y;
-    const RowSplit split = row_split(a.nvec);
+    const RowSplit split = row_split(a.nvec, 8);
     a.log = split.log;
+    const size_t weights = (size_t)(d_bias ? 2 : 1) * a.seg.E * channels * sizeof(float);
+    a.shared = weights <= kNormShared;
     const long long rows = (long long)B * N, per_cta = kNormThreads >> split.log;
     const int ctas = (int)std::min<long long>((rows + per_cta - 1) / per_cta, 8LL * h->num_sms);
     LaunchScope ls(h, K_NORM, st);
-    by_vectors<Norm>(split.per, a, ctas, st);
+    by_vectors<Norm>(split.per, a, ctas, a.shared ? weights : 0, st);
     return check_cuda(h, cudaGetLastError());
 }
 
@@ -324,31 +344,32 @@ extern "C" int emc2_expert_norm_grad(emc2_bridge_t* h, int32_t B, int32_t N, int
     RowsDevice device(h->cfg.device);
     if (!device.ok) return EMC2_ERR_CUDA;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-    NormSumArgs t;
-    t.seg = row_segments(h, B, N, d_offsets);
+    const RowSegments seg = row_segments(h, B, N, d_offsets);
     if (empty) {
-        const size_t bytes = (size_t)t.seg.E * channels * sizeof(float);
+        const size_t bytes = (size_t)seg.E * channels * sizeof(float);
         cudaError_t e = cudaMemsetAsync(d_grad_weight, 0, bytes, st);
         if (e == cudaSuccess && d_grad_bias) e = cudaMemsetAsync(d_grad_bias, 0, bytes, st);
         return check_cuda(h, e);
     }
     NormGradArgs a;
-    a.seg = t.seg;
+    a.seg = seg;
     a.x = d_x; a.dy = d_grad_y; a.weight = d_weight; a.mean = d_mean; a.rstd = d_rstd; a.dx = d_grad_x;
-    a.part = static_cast<float*>(h->rows_scratch.slab);
+    a.share = static_cast<int*>(h->rows_scratch.slab);
+    a.part = reinterpret_cast<float*>(a.share + kShareInts);
     a.inv_c = 1.0f / (float)channels; a.nvec = channels / 4; a.type_x = type_x; a.type_y = type_y;
-    const RowSplit split = row_split(a.nvec);
+    const RowSplit split = row_split(a.nvec, 3);
     a.log = split.log;
     const long long rows = (long long)B * N, per_cta = kNormThreads >> split.log;
-    t.ctas = (int)std::min<long long>((rows + per_cta - 1) / per_cta, norm_grad_ctas(h));
-    t.part = a.part; t.dweight = d_grad_weight; t.dbias = d_grad_bias; t.C = channels;
+    const int ctas = (int)std::min<long long>((rows + per_cta - 1) / per_cta, norm_grad_ctas(h, split.per));
+    NormSumArgs t;
+    t.part = a.part; t.share = a.share; t.dweight = d_grad_weight; t.dbias = d_grad_bias; t.C = channels;
     {
         LaunchScope ls(h, K_NORM_GRAD, st);
-        by_vectors<NormGrad>(split.per, a, t.ctas, (size_t)(kNormThreads / 32) * 2 * a.nvec * sizeof(float4), st);
+        by_vectors<NormGrad>(split.per, a, ctas, (size_t)(kNormThreads / 32) * 2 * a.nvec * sizeof(float4), st);
     }
     {
         LaunchScope ls(h, K_NORM_SUM, st);
-        norm_sum_kernel<<<dim3((2 * channels + 31) / 32, t.seg.E), kNormThreads, 0, st>>>(t);
+        norm_sum_kernel<<<dim3((2 * channels + 31) / 32, seg.E), kNormSumThreads, 0, st>>>(t);
     }
     return check_cuda(h, cudaGetLastError());
 }

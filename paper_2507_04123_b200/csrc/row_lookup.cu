@@ -28,45 +28,209 @@ struct LookupArgs {
     const void* table;
     void* out;
     float scale;
-    int n, rows, nvec, type;
-    FastDiv row;                // division by nvec
-    uint32_t vectors;           // n * nvec
+    int rows, type;
+    FastDiv row;                // division by the units of a row
+    uint32_t units;             // n rows of them
     int* status;
 };
 
-// A vector of four elements per thread and step, kLookupUnroll of them requested before the first is stored.
+// A unit of 16 bytes per thread and step (of 8 where a row of 16-bit elements is no multiple of 16), kLookupUnroll of them
+// requested before the first is stored.  The result passes the L2 cache by, which the table's rows need.
+template <typename Unit>
 __global__ void __launch_bounds__(kLookupThreads) lookup_kernel(LookupArgs a) {
     const uint32_t t0 = blockIdx.x * (kLookupThreads * kLookupUnroll) + threadIdx.x;
-    float4 f[kLookupUnroll];
+    Unit f[kLookupUnroll];
     bool bad = false;
 #pragma unroll
     for (int u = 0; u < kLookupUnroll; ++u) {
         const uint32_t t = t0 + u * kLookupThreads;
-        f[u] = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (t >= a.vectors) continue;
+        f[u] = Unit{};
+        if (t >= a.units) continue;
         uint32_t i, v;
         a.row.divmod(t, i, v);
         const int id = __ldg(a.ids + i);
         bad |= id >= a.rows;
-        if (id >= 0 && id < a.rows) f[u] = load_row4(a.table, (size_t)id * a.nvec + v, a.type);
+        if (id >= 0 && id < a.rows) f[u] = __ldg(static_cast<const Unit*>(a.table) + (size_t)id * a.row.d + v);
     }
 #pragma unroll
     for (int u = 0; u < kLookupUnroll; ++u) {
         const uint32_t t = t0 + u * kLookupThreads;
-        if (t < a.vectors) store_row4(a.out, t, scaled(f[u], a.scale), a.type);
+        if (t >= a.units) continue;
+        uint32_t* w = reinterpret_cast<uint32_t*>(&f[u]);
+#pragma unroll
+        for (int k = 0; k < (int)sizeof(Unit) / 4; ++k) {
+            if (a.type == EMC2_F32) {
+                w[k] = __float_as_uint(__uint_as_float(w[k]) * a.scale);
+            } else {
+                const float4 p = as_floats(make_uint2(w[k], 0u), a.type);
+                w[k] = as_halves(p.x * a.scale, p.y * a.scale, a.type);
+            }
+        }
+        __stcs(static_cast<Unit*>(a.out) + t, f[u]);
     }
     if (bad) atomicOr(a.status, kStatusBadRows);
 }
 
-// Keys of the sort: the id, or `rows` (sorted behind all of them) where there is none.
-__global__ void __launch_bounds__(kLookupThreads)
-lookup_keys_kernel(const int32_t* ids, int n, int rows, uint32_t* keys, uint32_t* vals, int* status) {
-    const int i = blockIdx.x * kLookupThreads + threadIdx.x;
-    if (i >= n) return;
-    const int id = ids[i];
-    if (id >= rows) atomicOr(status, kStatusBadRows);
-    keys[i] = id >= 0 && id < rows ? (uint32_t)id : (uint32_t)rows;
-    vals[i] = (uint32_t)i;
+// ---------------------------------------------------------------- the ids in ascending order, each with its place
+// A stable radix sort, least significant digit first, of up to ten bits per pass (two passes for a million table rows, one
+// for a thousand).  The key of an id is the id, or `rows` (behind all of them) where there is none.
+constexpr int kSortThreads = 256, kSortWarps = kSortThreads / 32;
+constexpr int kSortRounds = 8;                         // of 32 items per warp
+constexpr int kSortItems = kSortThreads * kSortRounds; // of a tile
+constexpr int kMaxDigits = 1024;
+
+struct SortArgs {
+    const int32_t* ids;         // of the first pass, else null
+    const uint32_t* keys_in;
+    const uint32_t* vals_in;
+    uint32_t* keys_out;
+    uint32_t* vals_out;
+    int* counts;                // [digits][tiles]
+    int* totals;                // [digits]
+    int* status;
+    int n, rows, tiles, shift, digits;
+};
+
+__device__ __forceinline__ uint32_t sort_key(const SortArgs& a, int i) {
+    if (!a.ids) return a.keys_in[i];
+    const int id = a.ids[i];
+    return id >= 0 && id < a.rows ? (uint32_t)id : (uint32_t)a.rows;
+}
+
+// counts[d][tile]: items of the tile with digit d.
+__global__ void __launch_bounds__(kSortThreads) sort_count_kernel(SortArgs a) {
+    __shared__ int hist[kMaxDigits];
+    for (int d = threadIdx.x; d < a.digits; d += kSortThreads) hist[d] = 0;
+    __syncthreads();
+    bool bad = false;
+#pragma unroll
+    for (int k = 0; k < kSortRounds; ++k) {
+        const int i = blockIdx.x * kSortItems + k * kSortThreads + threadIdx.x;
+        if (i >= a.n) continue;
+        const uint32_t key = sort_key(a, i);
+        bad |= a.ids && a.ids[i] >= a.rows;
+        atomicAdd(&hist[key >> a.shift & (a.digits - 1)], 1);
+    }
+    __syncthreads();
+    for (int d = threadIdx.x; d < a.digits; d += kSortThreads) a.counts[(size_t)d * a.tiles + blockIdx.x] = hist[d];
+    if (bad) atomicOr(a.status, kStatusBadRows);
+}
+
+// Exclusive prefix sums over every row of counts, a warp per digit, and the digits' totals.
+__global__ void __launch_bounds__(kSortThreads) sort_scan_kernel(SortArgs a) {
+    const int d = blockIdx.x * kSortWarps + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+    if (d >= a.digits) return;
+    int* row = a.counts + (size_t)d * a.tiles;
+    int run = 0;
+    for (int t0 = 0; t0 < a.tiles; t0 += 32) {
+        const int t = t0 + lane, v = t < a.tiles ? row[t] : 0;
+        int inc = v;
+#pragma unroll
+        for (int k = 1; k < 32; k <<= 1) {
+            const int y = __shfl_up_sync(0xFFFFFFFFu, inc, k);
+            if (lane >= k) inc += y;
+        }
+        if (t < a.tiles) row[t] = run + inc - v;
+        run += __shfl_sync(0xFFFFFFFFu, inc, 31);
+    }
+    if (lane == 0) a.totals[d] = run;
+}
+
+// Exclusive prefix sum of v[0 .. n) in shared memory, n <= kMaxDigits, by the whole CTA.
+__device__ __forceinline__ void scan_digits(int* v, int n, int* warp_sums) {
+    constexpr int kPer = kMaxDigits / kSortThreads;
+    const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
+    int x[kPer], sum = 0;
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) {
+        x[k] = t * kPer + k < n ? v[t * kPer + k] : 0;
+        sum += x[k];
+    }
+    int inc = sum;
+#pragma unroll
+    for (int k = 1; k < 32; k <<= 1) {
+        const int y = __shfl_up_sync(0xFFFFFFFFu, inc, k);
+        if (lane >= k) inc += y;
+    }
+    if (lane == 31) warp_sums[warp] = inc;
+    __syncthreads();
+    int run = inc - sum;
+    for (int w = 0; w < warp; ++w) run += warp_sums[w];
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) {
+        if (t * kPer + k < n) v[t * kPer + k] = run;
+        run += x[k];
+    }
+    __syncthreads();
+}
+
+// Moves a tile's items to their places.  A warp takes 256 consecutive items in rounds of 32, so that "earlier in the list" is
+// "earlier round, or lower lane": the rank among the warp's items of a digit is a running count plus a match over the lanes.
+// The tile is put in order in shared memory first and leaves in runs.
+__global__ void __launch_bounds__(kSortThreads) sort_move_kernel(SortArgs a) {
+    __shared__ uint16_t wcnt[kSortWarps][kMaxDigits];  // items of a digit by warp, then those of the warps before
+    __shared__ int first[kMaxDigits];                  // place of a digit's first item in the tile ...
+    __shared__ int to[kMaxDigits];                     // ... and of it in the whole list, less that
+    __shared__ int warp_sums[kSortWarps];
+    __shared__ uint32_t keys[kSortItems], vals[kSortItems];
+    const int t = threadIdx.x, lane = t & 31, warp = t >> 5, tile0 = blockIdx.x * kSortItems;
+    const uint32_t mask = a.digits - 1;
+    for (int d = t; d < a.digits; d += kSortThreads) {
+#pragma unroll
+        for (int w = 0; w < kSortWarps; ++w) wcnt[w][d] = 0;
+        to[d] = a.totals[d];
+    }
+    __syncthreads();
+    scan_digits(to, a.digits, warp_sums);              // items of smaller digits in the whole list
+    uint32_t key[kSortRounds];
+    uint16_t rank[kSortRounds];
+#pragma unroll
+    for (int k = 0; k < kSortRounds; ++k) {
+        const int i = tile0 + warp * (32 * kSortRounds) + k * 32 + lane;
+        key[k] = i < a.n ? sort_key(a, i) : 0xFFFFFFFFu;
+    }
+#pragma unroll
+    for (int k = 0; k < kSortRounds; ++k) {
+        const bool in = tile0 + warp * (32 * kSortRounds) + k * 32 + lane < a.n;
+        const uint32_t d = key[k] >> a.shift & mask;
+        const unsigned peers = __match_any_sync(0xFFFFFFFFu, in ? d : 0xFFFFFFFFu);
+        const int before = in ? wcnt[warp][d] : 0;
+        rank[k] = (uint16_t)(before + __popc(peers & ((1u << lane) - 1u)));
+        __syncwarp();
+        if (in && (peers & ((1u << lane) - 1u)) == 0) wcnt[warp][d] = (uint16_t)(before + __popc(peers));
+        __syncwarp();
+    }
+    __syncthreads();
+    for (int d = t; d < a.digits; d += kSortThreads) {
+        int run = 0;
+#pragma unroll
+        for (int w = 0; w < kSortWarps; ++w) {
+            const int c = wcnt[w][d];
+            wcnt[w][d] = (uint16_t)run;
+            run += c;
+        }
+        first[d] = run;
+    }
+    __syncthreads();
+    scan_digits(first, a.digits, warp_sums);
+    for (int d = t; d < a.digits; d += kSortThreads) to[d] += a.counts[(size_t)d * a.tiles + blockIdx.x] - first[d];
+#pragma unroll
+    for (int k = 0; k < kSortRounds; ++k) {
+        const int i = tile0 + warp * (32 * kSortRounds) + k * 32 + lane;
+        if (i >= a.n) continue;
+        const uint32_t d = key[k] >> a.shift & mask;
+        const int at = first[d] + wcnt[warp][d] + rank[k];
+        keys[at] = key[k];
+        vals[at] = a.ids ? (uint32_t)i : a.vals_in[i];
+    }
+    __syncthreads();
+    const int here = min(kSortItems, a.n - tile0);
+    for (int i = t; i < here; i += kSortThreads) {
+        const uint32_t k = keys[i];
+        const int place = to[k >> a.shift & mask] + i;
+        a.keys_out[place] = k;
+        a.vals_out[place] = vals[i];
+    }
 }
 
 // First place in [lo, hi) of the ascending keys whose key is at least k; hi if there is none.
@@ -117,44 +281,72 @@ struct SumArgs {
     float4* partial;            // [CTAs][2][nvec]: sums of head and tail
 };
 
-// A group of lanes adds up `items` places of the sorted list; the CTA then joins its groups in order.
+// A group of lanes adds up `items` places of the sorted list; the CTA then joins its groups in order.  The rows of two
+// places are requested before the first is added.
 template <int K>
-__global__ void __launch_bounds__(kLookupThreads) lookup_sum_kernel(SumArgs a) {
-    extern __shared__ float4 part[];            // [groups][2][nvec]
+__global__ void __launch_bounds__(kLookupThreads, K <= 3 ? 4 : K == 4 ? 3 : 2) lookup_sum_kernel(SumArgs a) {
+    extern __shared__ float4 part[];            // [groups][2][nvec], behind it the CTA's keys (one more at each end) and places
     __shared__ RunEnds ends[kLookupThreads];
     const int lanes = 1 << a.log, lane = threadIdx.x & (lanes - 1), group = threadIdx.x >> a.log, groups = kLookupThreads >> a.log;
     const uint32_t none = (uint32_t)a.rows;
-    const long long p0 = ((long long)blockIdx.x * groups + group) * a.items;
-    const int from = (int)min(p0, (long long)a.n), to = (int)min(p0 + a.items, (long long)a.n);
+    uint32_t* keys = reinterpret_cast<uint32_t*>(part + groups * 2 * a.nvec) + 1;
+    uint32_t* vals = keys + groups * kRunItems + 1;
     RunEnds mine = {-1, 0, -1, 0};
     float4 acc[K];
 #pragma unroll
     for (int i = 0; i < K; ++i) acc[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (from < to) {
-        uint32_t key = a.keys[from];
-        bool begun = from == 0 || a.keys[from - 1] != key;            // the run begins here
-        for (int p = from; p < to && key != none; ++p) {
-            const uint32_t next = p + 1 < a.n ? a.keys[p + 1] : none;
-            const size_t row = a.vals[p];
-            float4 x[K];
-            load_row<K>(x, a.dout, row * a.nvec, lane, a.log, a.nvec, a.type);
+    auto add = [&](const float4 (&x)[K]) {
 #pragma unroll
-            for (int i = 0; i < K; ++i) { acc[i].x += x[i].x; acc[i].y += x[i].y; acc[i].z += x[i].z; acc[i].w += x[i].w; }
-            const bool over = next != key;
-            if (!over && p + 1 < to) continue;
+        for (int i = 0; i < K; ++i) { acc[i].x += x[i].x; acc[i].y += x[i].y; acc[i].z += x[i].z; acc[i].w += x[i].w; }
+    };
+    bool begun = false;                                               // the open run begins in this group's places
+    // Pieces of kRunItems places per group; only very long lists have more than one.
+    const long long cta0 = (long long)blockIdx.x * groups * a.items;
+    for (int piece = 0; piece < a.items; piece += kRunItems) {
+        __syncthreads();
+        for (int i = (int)threadIdx.x - 1; i <= groups * kRunItems; i += kLookupThreads) {
+            // Place i of the staged ones belongs to group i / kRunItems; -1 and the one behind the last are neighbours.
+            const int g = i < 0 ? 0 : min(i / kRunItems, groups - 1), k = i - g * kRunItems;
+            const long long p = cta0 + (long long)g * a.items + piece + k;
+            keys[i] = p >= 0 && p < a.n ? a.keys[p] : p < 0 ? 0xFFFFFFFFu : none;
+            if (i >= 0 && i < groups * kRunItems) vals[i] = p < a.n ? a.vals[p] : 0u;
+        }
+        __syncthreads();
+        const long long p0 = cta0 + (long long)group * a.items + piece;
+        const int here = (int)max(0LL, min((long long)min(kRunItems, a.items - piece), (long long)a.n - p0)), at = group * kRunItems;
+        if (here > 0) {
+            // With several pieces a group's neighbours are not its neighbours in the staged list.
+            const uint32_t before = a.items == kRunItems ? keys[at - 1] : p0 > 0 ? a.keys[p0 - 1] : 0xFFFFFFFFu;
+            const uint32_t behind = a.items == kRunItems ? keys[at + here] : p0 + here < a.n ? a.keys[p0 + here] : none;
+            if (before != keys[at]) begun = true;
+            else if (piece == 0) begun = false;
+            for (int k = 0; k < here; k += 2) {
+                if (keys[at + k] == none) break;
+                const bool two = k + 1 < here && keys[at + k + 1] != none;
+                float4 x[2][K];
+                load_row<K>(x[0], a.dout, (size_t)vals[at + k] * a.nvec, lane, a.log, a.nvec, a.type);
+                if (two) load_row<K>(x[1], a.dout, (size_t)vals[at + k + 1] * a.nvec, lane, a.log, a.nvec, a.type);
 #pragma unroll
-            for (int i = 0; i < K; ++i) {
-                const int v = lane + (i << a.log);
-                if (v < a.nvec) {
-                    if (begun && over) store_row4(a.dtable, (size_t)key * a.nvec + v, scaled(acc[i], a.scale), a.type);
-                    else part[(group * 2 + (begun ? 1 : 0)) * a.nvec + v] = acc[i];
+                for (int q = 0; q < 2; ++q) {
+                    if (q == 1 && !two) break;
+                    const uint32_t key = keys[at + k + q], next = k + q + 1 < here ? keys[at + k + q + 1] : behind;
+                    add(x[q]);
+                    const bool over = next != key, last = piece + k + q + 1 >= a.items || p0 + k + q + 1 >= a.n;
+                    if (!over && !last) continue;
+#pragma unroll
+                    for (int i = 0; i < K; ++i) {
+                        const int v = lane + (i << a.log);
+                        if (v < a.nvec) {
+                            if (begun && over) store_row4(a.dtable, (size_t)key * a.nvec + v, scaled(acc[i], a.scale), a.type);
+                            else part[(group * 2 + (begun ? 1 : 0)) * a.nvec + v] = acc[i];
+                        }
+                        acc[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+                    }
+                    if (!begun) { mine.head = (int)key; mine.through = !over; }
+                    else if (!over) mine.tail = (int)key;
+                    begun = true;
                 }
-                acc[i] = make_float4(0.f, 0.f, 0.f, 0.f);
             }
-            if (!begun) { mine.head = (int)key; mine.through = !over; }
-            else if (!over) mine.tail = (int)key;
-            key = next;
-            begun = true;
         }
     }
     if (lane == 0) ends[group] = mine;
@@ -247,7 +439,7 @@ int check_lookup(const emc2_bridge* h, int n, int rows, int channels, int type, 
 int sum_items(long long n, int groups, int* ctas) {
     long long items = kRunItems;
     const long long most = (long long)groups * kMaxSumCtas;
-    if (n > items * most) items = (n + most - 1) / most;
+    if (n > items * most) items = ((n + most - 1) / most + kRunItems - 1) / kRunItems * kRunItems;
     *ctas = (int)((n + items * groups - 1) / (items * groups));
     return (int)items;
 }
@@ -262,8 +454,8 @@ LookupScratch lookup_scratch(long long n, int ctas, int nvec) {
     size_t off = 0;
     auto take = [&](size_t bytes) { const size_t o = off; off += (bytes + 255) & ~(size_t)255; return o; };
     for (int k = 0; k < 2; ++k) { s.keys[k] = take((size_t)n * 4); s.vals[k] = take((size_t)n * 4); }
-    s.counts = take((size_t)256 * sort_tiles((size_t)n) * 4);
-    s.row_tot = take(256 * 4);
+    s.counts = take((size_t)kMaxDigits * ((n + kSortItems - 1) / kSortItems) * 4);
+    s.row_tot = take(kMaxDigits * 4);
     s.ends = take((size_t)ctas * sizeof(RunEnds));
     s.partial = take((size_t)ctas * 2 * nvec * sizeof(float4));
     s.bytes = off;
@@ -278,7 +470,7 @@ size_t lookup_scratch_bytes(const emc2_bridge* h, int max_channels) {
     // Narrower rows have more groups per CTA, so fewer CTAs: which width needs most depends on n.
     for (int c = 4; c <= max_channels; c += 4) {
         int ctas;
-        sum_items(n, kLookupThreads >> row_split(c / 4).log, &ctas);
+        sum_items(n, kLookupThreads >> row_split(c / 4, 8).log, &ctas);
         most = std::max(most, lookup_scratch(n, ctas, c / 4).bytes);
     }
     return most;
@@ -297,15 +489,17 @@ extern "C" int emc2_row_lookup(emc2_bridge_t* h, int32_t n, int32_t rows, int32_
     if (!d_out || (rows > 0 && !d_table) || d_out == d_table) return EMC2_ERR_INVALID_ARG;
     RowsDevice device(h->cfg.device);
     if (!device.ok) return EMC2_ERR_CUDA;
+    const int row_bytes = channels * type_bytes(type), unit = row_bytes % 16 == 0 ? 16 : 8;
     LookupArgs a;
-    a.ids = d_ids; a.table = d_table; a.out = d_out; a.scale = scale; a.n = n; a.rows = rows; a.nvec = channels / 4; a.type = type;
-    a.row = make_fast_div((uint32_t)a.nvec);
-    a.vectors = (uint32_t)n * (uint32_t)a.nvec;
+    a.ids = d_ids; a.table = d_table; a.out = d_out; a.scale = scale; a.rows = rows; a.type = type;
+    a.row = make_fast_div((uint32_t)(row_bytes / unit));
+    a.units = (uint32_t)n * (uint32_t)(row_bytes / unit);
     a.status = h->d_status;
-    const uint32_t per_cta = kLookupThreads * kLookupUnroll;
+    const uint32_t per_cta = kLookupThreads * kLookupUnroll, ctas = (a.units + per_cta - 1) / per_cta;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     LaunchScope ls(h, K_ROW_LOOKUP, st);
-    lookup_kernel<<<(a.vectors + per_cta - 1) / per_cta, kLookupThreads, 0, st>>>(a);
+    if (unit == 16) lookup_kernel<uint4><<<ctas, kLookupThreads, 0, st>>>(a);
+    else lookup_kernel<uint2><<<ctas, kLookupThreads, 0, st>>>(a);
     return check_cuda(h, cudaGetLastError());
 }
 
@@ -326,7 +520,7 @@ extern "C" int emc2_row_lookup_grad(emc2_bridge_t* h, int32_t n, int32_t rows, i
     }
     SumArgs a;
     a.nvec = channels / 4;
-    const RowSplit split = row_split(a.nvec);
+    const RowSplit split = row_split(a.nvec, 8);
     const int groups = kLookupThreads >> split.log;
     int ctas;
     a.items = sum_items(n, groups, &ctas);
@@ -334,14 +528,21 @@ extern "C" int emc2_row_lookup_grad(emc2_bridge_t* h, int32_t n, int32_t rows, i
     char* base = static_cast<char*>(h->rows_scratch.slab);
     uint32_t* keys[2] = {reinterpret_cast<uint32_t*>(base + s.keys[0]), reinterpret_cast<uint32_t*>(base + s.keys[1])};
     uint32_t* vals[2] = {reinterpret_cast<uint32_t*>(base + s.vals[0]), reinterpret_cast<uint32_t*>(base + s.vals[1])};
-    {
-        LaunchScope ls(h, K_LOOKUP_SORT, st);
-        lookup_keys_kernel<<<(n + kLookupThreads - 1) / kLookupThreads, kLookupThreads, 0, st>>>(d_ids, n, rows, keys[0], vals[0], h->d_status);
-    }
-    int bits = 0;
+    int bits = 1;
     while (bits < 32 && ((uint64_t)1 << bits) < (uint64_t)rows + 1) ++bits;         // the keys are 0 .. rows
-    const int at = radix_sort(h, K_LOOKUP_SORT, n, bits, keys, vals, true, reinterpret_cast<int*>(base + s.counts),
-                              reinterpret_cast<int*>(base + s.row_tot), st);
+    const int passes = (bits + 9) / 10, digit = (bits + passes - 1) / passes;
+    int at = 1;
+    for (int p = 0; p < passes; ++p, at ^= 1) {
+        SortArgs o;
+        o.ids = p == 0 ? d_ids : nullptr;
+        o.keys_in = keys[at]; o.vals_in = vals[at]; o.keys_out = keys[at ^ 1]; o.vals_out = vals[at ^ 1];
+        o.counts = reinterpret_cast<int*>(base + s.counts); o.totals = reinterpret_cast<int*>(base + s.row_tot); o.status = h->d_status;
+        o.n = n; o.rows = rows; o.tiles = (n + kSortItems - 1) / kSortItems; o.shift = p * digit; o.digits = 1 << digit;
+        LaunchScope ls(h, K_LOOKUP_SORT, st);
+        sort_count_kernel<<<o.tiles, kSortThreads, 0, st>>>(o);
+        sort_scan_kernel<<<(o.digits + kSortWarps - 1) / kSortWarps, kSortThreads, 0, st>>>(o);
+        sort_move_kernel<<<o.tiles, kSortThreads, 0, st>>>(o);
+    }
     a.keys = keys[at]; a.vals = vals[at]; a.dout = d_grad_out; a.dtable = d_grad_table; a.scale = scale; a.n = n; a.rows = rows;
     a.log = split.log; a.type = type;
     a.ends = reinterpret_cast<RunEnds*>(base + s.ends);
@@ -352,7 +553,7 @@ extern "C" int emc2_row_lookup_grad(emc2_bridge_t* h, int32_t n, int32_t rows, i
             a.keys, n, rows, a.nvec, make_fast_div((uint32_t)a.nvec), d_grad_table, type);
     }
     {
-        const size_t shared = (size_t)groups * 2 * a.nvec * sizeof(float4);
+        const size_t shared = (size_t)groups * 2 * a.nvec * sizeof(float4) + ((size_t)groups * kRunItems * 2 + 4) * sizeof(uint32_t);
         LaunchScope ls(h, K_LOOKUP_SUM, st);
         switch (split.per) {
             case 1: launch_sum<1>(a, ctas, shared, st); break;

@@ -42,17 +42,16 @@ inline RowSegments row_segments(const emc2_bridge* h, int B, int N, const int32_
 }
 
 // A row of nvec vectors of four elements is spread over 1 << log lanes that hold up to `per` vectors each (vector
-// lane + i * lanes).  The split that leaves fewest places empty, and of those the one with four or fewer vectors per lane
-// and fewest lanes: the more a lane loads at once, the more is in flight.
+// lane + i * lanes): the split that leaves fewest places empty with at most `most` vectors per lane (or what 32 lanes need),
+// and of those the one with fewest lanes, since the more a lane loads at once, the more is in flight.
 struct RowSplit {
     int log, per;
 };
-inline RowSplit row_split(int nvec) {
+inline RowSplit row_split(int nvec, int most) {
     RowSplit best = {5, (nvec + 31) / 32};
     for (int log = 4; log >= 0; --log) {
-        const int lanes = 1 << log, per = (nvec + lanes - 1) / lanes, places = best.per << best.log;
-        if (per > 8) break;
-        if (per * lanes < places || (per * lanes == places && per <= 4)) best = {log, per};
+        const int lanes = 1 << log, per = (nvec + lanes - 1) / lanes;
+        if (per <= most && per * lanes <= best.per << best.log) best = {log, per};
     }
     return best;
 }
