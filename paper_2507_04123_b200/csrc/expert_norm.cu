@@ -161,9 +161,12 @@ __global__ void __launch_bounds__(kNormThreads, K <= 2 ? 3 : K <= 4 ? 2 : 1) nor
                 row = (size_t)b * a.seg.N + bounds[b * (E + 1) + e] + (p - start[q]);
             }
             const float m = in ? __ldg(a.mean + row) : 0.f, r = in ? __ldg(a.rstd + row) : 0.f;
+            uint4 raw_x[K], raw_g[K];
+            request_row<K>(raw_x, a.x, row * a.nvec, lane, a.log, in ? a.nvec : 0, a.type_x);
+            request_row<K>(raw_g, a.dy, row * a.nvec, lane, a.log, in ? a.nvec : 0, a.type_y);
             float4 x[K], g[K];
-            load_row<K>(x, a.x, row * a.nvec, lane, a.log, in ? a.nvec : 0, a.type_x);
-            load_row<K>(g, a.dy, row * a.nvec, lane, a.log, in ? a.nvec : 0, a.type_y);
+#pragma unroll
+            for (int i = 0; i < K; ++i) { x[i] = row_floats(raw_x[i], a.type_x); g[i] = row_floats(raw_g[i], a.type_y); }
             float s = 0.f, t = 0.f;
 #pragma unroll
             for (int i = 0; i < K; ++i) {

@@ -8,6 +8,7 @@
 // run of equal ids holds its rows in ascending order), the sorted list is cut into equal parts whatever the lengths of the
 // runs, and runs that a cut divides are joined afterwards.  Sums are held in fp32 and rounded once.
 #include <algorithm>
+#include <type_traits>
 
 #include "rows.cuh"
 
@@ -17,7 +18,6 @@ namespace {
 constexpr int kLookupThreads = 256;
 constexpr int kLookupUnroll = 4;
 constexpr int kRunItems = 16;                 // sorted places per group of lanes, at least
-constexpr int kMaxSumCtas = 16384;
 
 __device__ __forceinline__ float4 scaled(float4 f, float s) {
     return make_float4(f.x * s, f.y * s, f.z * s, f.w * s);
@@ -85,10 +85,10 @@ struct SortArgs {
     const uint32_t* vals_in;
     uint32_t* keys_out;
     uint32_t* vals_out;
-    int* counts;                // [digits][tiles]
+    int* counts;                // [digits][stride], one per tile; the stride a multiple of 4
     int* totals;                // [digits]
     int* status;
-    int n, rows, tiles, shift, digits;
+    int n, rows, tiles, stride, shift, digits;
 };
 
 __device__ __forceinline__ uint32_t sort_key(const SortArgs& a, int i) {
@@ -112,25 +112,34 @@ __global__ void __launch_bounds__(kSortThreads) sort_count_kernel(SortArgs a) {
         atomicAdd(&hist[key >> a.shift & (a.digits - 1)], 1);
     }
     __syncthreads();
-    for (int d = threadIdx.x; d < a.digits; d += kSortThreads) a.counts[(size_t)d * a.tiles + blockIdx.x] = hist[d];
+    for (int d = threadIdx.x; d < a.digits; d += kSortThreads) a.counts[(size_t)d * a.stride + blockIdx.x] = hist[d];
     if (bad) atomicOr(a.status, kStatusBadRows);
 }
 
-// Exclusive prefix sums over every row of counts, a warp per digit, and the digits' totals.
+// Exclusive prefix sums over every row of counts, a warp per digit and 128 tiles at a time, and the digits' totals.
 __global__ void __launch_bounds__(kSortThreads) sort_scan_kernel(SortArgs a) {
     const int d = blockIdx.x * kSortWarps + (threadIdx.x >> 5), lane = threadIdx.x & 31;
     if (d >= a.digits) return;
-    int* row = a.counts + (size_t)d * a.tiles;
+    int4* row = reinterpret_cast<int4*>(a.counts + (size_t)d * a.stride);
     int run = 0;
-    for (int t0 = 0; t0 < a.tiles; t0 += 32) {
-        const int t = t0 + lane, v = t < a.tiles ? row[t] : 0;
-        int inc = v;
+    for (int t0 = 0; t0 < a.stride / 4; t0 += 32) {
+        const int t = t0 + lane;
+        int4 v = t < a.stride / 4 ? row[t] : make_int4(0, 0, 0, 0);
+        if (4 * t + 3 >= a.tiles) {                                        // behind the last tile
+            if (4 * t >= a.tiles) v.x = 0;
+            if (4 * t + 1 >= a.tiles) v.y = 0;
+            if (4 * t + 2 >= a.tiles) v.z = 0;
+            v.w = 0;
+        }
+        const int sum = v.x + v.y + v.z + v.w;
+        int inc = sum;
 #pragma unroll
         for (int k = 1; k < 32; k <<= 1) {
             const int y = __shfl_up_sync(0xFFFFFFFFu, inc, k);
             if (lane >= k) inc += y;
         }
-        if (t < a.tiles) row[t] = run + inc - v;
+        const int x = run + inc - sum;
+        if (t < a.stride / 4) row[t] = make_int4(x, x + v.x, x + v.x + v.y, x + v.x + v.y + v.z);
         run += __shfl_sync(0xFFFFFFFFu, inc, 31);
     }
     if (lane == 0) a.totals[d] = run;
@@ -167,7 +176,7 @@ __device__ __forceinline__ void scan_digits(int* v, int n, int* warp_sums) {
 // Moves a tile's items to their places.  A warp takes 256 consecutive items in rounds of 32, so that "earlier in the list" is
 // "earlier round, or lower lane": the rank among the warp's items of a digit is a running count plus a match over the lanes.
 // The tile is put in order in shared memory first and leaves in runs.
-__global__ void __launch_bounds__(kSortThreads) sort_move_kernel(SortArgs a) {
+__global__ void __launch_bounds__(kSortThreads, 4) sort_move_kernel(SortArgs a) {
     __shared__ uint16_t wcnt[kSortWarps][kMaxDigits];  // items of a digit by warp, then those of the warps before
     __shared__ int first[kMaxDigits];                  // place of a digit's first item in the tile ...
     __shared__ int to[kMaxDigits];                     // ... and of it in the whole list, less that
@@ -175,6 +184,17 @@ __global__ void __launch_bounds__(kSortThreads) sort_move_kernel(SortArgs a) {
     __shared__ uint32_t keys[kSortItems], vals[kSortItems];
     const int t = threadIdx.x, lane = t & 31, warp = t >> 5, tile0 = blockIdx.x * kSortItems;
     const uint32_t mask = a.digits - 1;
+    // Requested before anything waits: the items, and the places of their digits (a column of `counts`).
+    uint32_t key[kSortRounds], val[kSortRounds];
+    uint16_t rank[kSortRounds];
+#pragma unroll
+    for (int k = 0; k < kSortRounds; ++k) {
+        const int i = tile0 + warp * (32 * kSortRounds) + k * 32 + lane;
+        key[k] = i < a.n ? sort_key(a, i) : 0xFFFFFFFFu;
+        val[k] = a.ids || i >= a.n ? (uint32_t)i : a.vals_in[i];
+    }
+    int* place = reinterpret_cast<int*>(keys);          // until the keys come there
+    for (int d = t; d < a.digits; d += kSortThreads) place[d] = a.counts[(size_t)d * a.stride + blockIdx.x];
     for (int d = t; d < a.digits; d += kSortThreads) {
 #pragma unroll
         for (int w = 0; w < kSortWarps; ++w) wcnt[w][d] = 0;
@@ -182,13 +202,6 @@ __global__ void __launch_bounds__(kSortThreads) sort_move_kernel(SortArgs a) {
     }
     __syncthreads();
     scan_digits(to, a.digits, warp_sums);              // items of smaller digits in the whole list
-    uint32_t key[kSortRounds];
-    uint16_t rank[kSortRounds];
-#pragma unroll
-    for (int k = 0; k < kSortRounds; ++k) {
-        const int i = tile0 + warp * (32 * kSortRounds) + k * 32 + lane;
-        key[k] = i < a.n ? sort_key(a, i) : 0xFFFFFFFFu;
-    }
 #pragma unroll
     for (int k = 0; k < kSortRounds; ++k) {
         const bool in = tile0 + warp * (32 * kSortRounds) + k * 32 + lane < a.n;
@@ -213,7 +226,8 @@ __global__ void __launch_bounds__(kSortThreads) sort_move_kernel(SortArgs a) {
     }
     __syncthreads();
     scan_digits(first, a.digits, warp_sums);
-    for (int d = t; d < a.digits; d += kSortThreads) to[d] += a.counts[(size_t)d * a.tiles + blockIdx.x] - first[d];
+    for (int d = t; d < a.digits; d += kSortThreads) to[d] += place[d] - first[d];
+    __syncthreads();
 #pragma unroll
     for (int k = 0; k < kSortRounds; ++k) {
         const int i = tile0 + warp * (32 * kSortRounds) + k * 32 + lane;
@@ -221,7 +235,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_move_kernel(SortArgs a) {
         const uint32_t d = key[k] >> a.shift & mask;
         const int at = first[d] + wcnt[warp][d] + rank[k];
         keys[at] = key[k];
-        vals[at] = a.ids ? (uint32_t)i : a.vals_in[i];
+        vals[at] = val[k];
     }
     __syncthreads();
     const int here = min(kSortItems, a.n - tile0);
@@ -241,25 +255,45 @@ __device__ __forceinline__ int lower_place(const uint32_t* keys, int lo, int hi,
     }
     return lo;
 }
+// The same by a warp, which probes 32 places at a time: four rounds for a million keys instead of twenty.
+__device__ __forceinline__ int lower_place_warp(const uint32_t* keys, int lo, int hi, uint32_t k) {
+    const int lane = threadIdx.x & 31;
+    while (hi - lo > 32) {
+        const long long span = hi - lo;
+        const int at = lo + (int)(span * (lane + 1) / 33);
+        const int less = __popc(__ballot_sync(0xFFFFFFFFu, keys[at] < k));     // the first `less` probes are
+        const int from = lo;
+        if (less > 0) lo = from + (int)(span * less / 33) + 1;
+        if (less < 32) hi = from + (int)(span * (less + 1) / 33);
+    }
+    const int at = lo + lane;
+    return lo + __popc(__ballot_sync(0xFFFFFFFFu, at < hi && keys[at] < k));
+}
 
 // Zeros in the table rows that no id names: 256 rows per CTA, looked up in the part of the sorted ids that theirs lie in.
 // Clearing the whole table first would write the rows with ids twice.
-__global__ void __launch_bounds__(kLookupThreads) lookup_zero_kernel(const uint32_t* keys, int n, int rows, int nvec, FastDiv row, void* out, int type) {
+__device__ __forceinline__ void zero_rows(const uint32_t* keys, int n, int rows, int nvec, uint32_t block, void* out, int type) {
     __shared__ int ends[2];
     __shared__ bool named[kLookupThreads];
-    const uint32_t r0 = blockIdx.x * kLookupThreads;
-    const int here = (int)min((uint32_t)kLookupThreads, (uint32_t)rows - r0);
-    if ((threadIdx.x & 31) == 0 && threadIdx.x < 64) ends[threadIdx.x >> 5] = lower_place(keys, 0, n, threadIdx.x ? r0 + here : r0);
-    __syncthreads();
-    const uint32_t r = r0 + threadIdx.x;
-    const int at = lower_place(keys, ends[0], ends[1], r);
-    named[threadIdx.x] = at < ends[1] && keys[at] == r;
-    __syncthreads();
-    for (int t = threadIdx.x; t < here * nvec; t += kLookupThreads) {
-        uint32_t k, v;
-        row.divmod((uint32_t)t, k, v);
-        if (!named[k]) store_row4(out, (size_t)r0 * nvec + t, make_float4(0.f, 0.f, 0.f, 0.f), type);
+    const uint32_t r0 = block * kLookupThreads;
+    const int here = (int)min((uint32_t)kLookupThreads, (uint32_t)rows - r0), warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    named[threadIdx.x] = false;
+    if (warp < 2) {
+        const int at = lower_place_warp(keys, 0, n, warp ? r0 + here : r0);
+        if (lane == 0) ends[warp] = at;
     }
+    __syncthreads();
+    const int lo = ends[0], hi = ends[1];
+    if (hi - lo <= 16 * kLookupThreads) {
+        for (int i = lo + threadIdx.x; i < hi; i += kLookupThreads) named[keys[i] - r0] = true;
+    } else {                                                              // long runs of few ids
+        const int at = lower_place(keys, lo, hi, r0 + threadIdx.x);
+        named[threadIdx.x] = at < hi && keys[at] == r0 + threadIdx.x;
+    }
+    __syncthreads();
+    for (int k = warp; k < here; k += kLookupThreads / 32)
+        if (!named[k])
+            for (int v = lane; v < nvec; v += 32) store_row4(out, (size_t)(r0 + k) * nvec + v, make_float4(0.f, 0.f, 0.f, 0.f), type);
 }
 
 // What a part of the sorted list leaves of the runs that its ends divide.
@@ -277,14 +311,21 @@ struct SumArgs {
     void* dtable;
     float scale;
     int n, rows, nvec, log, type, items;
-    RunEnds* ends;              // [CTAs]
+    int parts;                  // CTAs that sum; those behind them clear the rows without ids beside them
+    RunEnds* ends;              // [parts]
     float4* partial;            // [CTAs][2][nvec]: sums of head and tail
 };
 
-// A group of lanes adds up `items` places of the sorted list; the CTA then joins its groups in order.  The rows of two
-// places are requested before the first is added.
-template <int K>
-__global__ void __launch_bounds__(kLookupThreads, K <= 3 ? 4 : K == 4 ? 3 : 2) lookup_sum_kernel(SumArgs a) {
+// A group of lanes adds up `items` places of the sorted list; the CTA then joins its groups in order.  The rows of
+// several places are requested before the first is added.
+template <int K, bool kHalf>
+__global__ void __launch_bounds__(kLookupThreads, K == 1 ? 4 : K <= 3 ? 3 : 2) lookup_sum_kernel(SumArgs a) {
+    using Raw = std::conditional_t<kHalf, uint2, float4>;
+
+    if ((int)blockIdx.x >= a.parts) {
+        zero_rows(a.keys, a.n, a.rows, a.nvec, blockIdx.x - a.parts, a.dtable, a.type);
+        return;
+    }
     extern __shared__ float4 part[];            // [groups][2][nvec], behind it the CTA's keys (one more at each end) and places
     __shared__ RunEnds ends[kLookupThreads];
     const int lanes = 1 << a.log, lane = threadIdx.x & (lanes - 1), group = threadIdx.x >> a.log, groups = kLookupThreads >> a.log;
@@ -292,12 +333,17 @@ __global__ void __launch_bounds__(kLookupThreads, K <= 3 ? 4 : K == 4 ? 3 : 2) l
     uint32_t* keys = reinterpret_cast<uint32_t*>(part + groups * 2 * a.nvec) + 1;
     uint32_t* vals = keys + groups * kRunItems + 1;
     RunEnds mine = {-1, 0, -1, 0};
+    constexpr int U = (kHalf ? 2 : 1) * (K <= 2 ? 4 : K == 3 ? 2 : 1);
     float4 acc[K];
 #pragma unroll
     for (int i = 0; i < K; ++i) acc[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-    auto add = [&](const float4 (&x)[K]) {
+    auto add = [&](const Raw (&x)[K]) {
 #pragma unroll
-        for (int i = 0; i < K; ++i) { acc[i].x += x[i].x; acc[i].y += x[i].y; acc[i].z += x[i].z; acc[i].w += x[i].w; }
+        for (int i = 0; i < K; ++i) {
+            float4 f;
+            if constexpr (kHalf) f = as_floats(x[i], a.type); else f = x[i];
+            acc[i].x += f.x; acc[i].y += f.y; acc[i].z += f.z; acc[i].w += f.w;
+        }
     };
     bool begun = false;                                               // the open run begins in this group's places
     // Pieces of kRunItems places per group; only very long lists have more than one.
@@ -320,15 +366,24 @@ __global__ void __launch_bounds__(kLookupThreads, K <= 3 ? 4 : K == 4 ? 3 : 2) l
             const uint32_t behind = a.items == kRunItems ? keys[at + here] : p0 + here < a.n ? a.keys[p0 + here] : none;
             if (before != keys[at]) begun = true;
             else if (piece == 0) begun = false;
-            for (int k = 0; k < here; k += 2) {
+            for (int k = 0; k < here; k += U) {
                 if (keys[at + k] == none) break;
-                const bool two = k + 1 < here && keys[at + k + 1] != none;
-                float4 x[2][K];
-                load_row<K>(x[0], a.dout, (size_t)vals[at + k] * a.nvec, lane, a.log, a.nvec, a.type);
-                if (two) load_row<K>(x[1], a.dout, (size_t)vals[at + k + 1] * a.nvec, lane, a.log, a.nvec, a.type);
+                Raw x[U][K];
+                int rows = 1;
 #pragma unroll
-                for (int q = 0; q < 2; ++q) {
-                    if (q == 1 && !two) break;
+                for (int q = 0; q < U; ++q) {
+                    const bool in = k + q < here && keys[at + k + q] != none;
+                    rows = in ? q + 1 : rows;
+                    const Raw* from = static_cast<const Raw*>(a.dout) + (size_t)(in ? vals[at + k + q] : 0u) * a.nvec;
+#pragma unroll
+                    for (int i = 0; i < K; ++i) {
+                        const int v = lane + (i << a.log);
+                        x[q][i] = in && v < a.nvec ? __ldg(from + v) : Raw{};
+                    }
+                }
+#pragma unroll
+                for (int q = 0; q < U; ++q) {
+                    if (q >= rows) break;
                     const uint32_t key = keys[at + k + q], next = k + q + 1 < here ? keys[at + k + q + 1] : behind;
                     add(x[q]);
                     const bool over = next != key, last = piece + k + q + 1 >= a.items || p0 + k + q + 1 >= a.n;
@@ -419,10 +474,15 @@ __global__ void __launch_bounds__(kLookupThreads) lookup_join_kernel(SumArgs a, 
     }
 }
 
+template <int K, bool kHalf>
+void launch_sum_of(const SumArgs& a, int ctas, size_t shared, cudaStream_t st) {
+    if (shared > 40 * 1024) cudaFuncSetAttribute(lookup_sum_kernel<K, kHalf>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)shared);
+    lookup_sum_kernel<K, kHalf><<<ctas, kLookupThreads, shared, st>>>(a);
+}
 template <int K>
 void launch_sum(const SumArgs& a, int ctas, size_t shared, cudaStream_t st) {
-    if (shared > 40 * 1024) cudaFuncSetAttribute(lookup_sum_kernel<K>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)shared);
-    lookup_sum_kernel<K><<<ctas, kLookupThreads, shared, st>>>(a);
+    if (a.type == EMC2_F32) launch_sum_of<K, false>(a, ctas, shared, st);
+    else launch_sum_of<K, true>(a, ctas, shared, st);
 }
 
 int check_lookup(const emc2_bridge* h, int n, int rows, int channels, int type, const void* ids) {
@@ -435,11 +495,11 @@ int check_lookup(const emc2_bridge* h, int n, int rows, int channels, int type, 
     return EMC2_OK;
 }
 
-// Places per group and CTAs of lookup_sum_kernel.
-int sum_items(long long n, int groups, int* ctas) {
-    long long items = kRunItems;
-    const long long most = (long long)groups * kMaxSumCtas;
-    if (n > items * most) items = ((n + most - 1) / most + kRunItems - 1) / kRunItems * kRunItems;
+// Places per group and CTAs of lookup_sum_kernel: as many places as make about four CTAs per SM, so that their ends do not
+// weigh.
+int sum_items(const emc2_bridge* h, long long n, int groups, int* ctas) {
+    const long long most = (long long)groups * 4 * h->num_sms;
+    const long long items = std::max<long long>(1, (n + most * kRunItems - 1) / (most * kRunItems)) * kRunItems;
     *ctas = (int)((n + items * groups - 1) / (items * groups));
     return (int)items;
 }
@@ -454,7 +514,7 @@ LookupScratch lookup_scratch(long long n, int ctas, int nvec) {
     size_t off = 0;
     auto take = [&](size_t bytes) { const size_t o = off; off += (bytes + 255) & ~(size_t)255; return o; };
     for (int k = 0; k < 2; ++k) { s.keys[k] = take((size_t)n * 4); s.vals[k] = take((size_t)n * 4); }
-    s.counts = take((size_t)kMaxDigits * ((n + kSortItems - 1) / kSortItems) * 4);
+    s.counts = take((size_t)kMaxDigits * ((n + kSortItems - 1) / kSortItems + 3) * 4);
     s.row_tot = take(kMaxDigits * 4);
     s.ends = take((size_t)ctas * sizeof(RunEnds));
     s.partial = take((size_t)ctas * 2 * nvec * sizeof(float4));
@@ -470,7 +530,7 @@ size_t lookup_scratch_bytes(const emc2_bridge* h, int max_channels) {
     // Narrower rows have more groups per CTA, so fewer CTAs: which width needs most depends on n.
     for (int c = 4; c <= max_channels; c += 4) {
         int ctas;
-        sum_items(n, kLookupThreads >> row_split(c / 4, 8).log, &ctas);
+        sum_items(h, n, kLookupThreads >> row_split(c / 4, 3).log, &ctas);
         most = std::max(most, lookup_scratch(n, ctas, c / 4).bytes);
     }
     return most;
@@ -520,10 +580,10 @@ extern "C" int emc2_row_lookup_grad(emc2_bridge_t* h, int32_t n, int32_t rows, i
     }
     SumArgs a;
     a.nvec = channels / 4;
-    const RowSplit split = row_split(a.nvec, 8);
+    const RowSplit split = row_split(a.nvec, 3);
     const int groups = kLookupThreads >> split.log;
     int ctas;
-    a.items = sum_items(n, groups, &ctas);
+    a.items = sum_items(h, n, groups, &ctas);
     const LookupScratch s = lookup_scratch(n, ctas, a.nvec);
     char* base = static_cast<char*>(h->rows_scratch.slab);
     uint32_t* keys[2] = {reinterpret_cast<uint32_t*>(base + s.keys[0]), reinterpret_cast<uint32_t*>(base + s.keys[1])};
@@ -537,7 +597,7 @@ extern "C" int emc2_row_lookup_grad(emc2_bridge_t* h, int32_t n, int32_t rows, i
         o.ids = p == 0 ? d_ids : nullptr;
         o.keys_in = keys[at]; o.vals_in = vals[at]; o.keys_out = keys[at ^ 1]; o.vals_out = vals[at ^ 1];
         o.counts = reinterpret_cast<int*>(base + s.counts); o.totals = reinterpret_cast<int*>(base + s.row_tot); o.status = h->d_status;
-        o.n = n; o.rows = rows; o.tiles = (n + kSortItems - 1) / kSortItems; o.shift = p * digit; o.digits = 1 << digit;
+        o.n = n; o.rows = rows; o.tiles = (n + kSortItems - 1) / kSortItems; o.stride = (o.tiles + 3) / 4 * 4; o.shift = p * digit; o.digits = 1 << digit;
         LaunchScope ls(h, K_LOOKUP_SORT, st);
         sort_count_kernel<<<o.tiles, kSortThreads, 0, st>>>(o);
         sort_scan_kernel<<<(o.digits + kSortWarps - 1) / kSortWarps, kSortThreads, 0, st>>>(o);
@@ -547,23 +607,20 @@ extern "C" int emc2_row_lookup_grad(emc2_bridge_t* h, int32_t n, int32_t rows, i
     a.log = split.log; a.type = type;
     a.ends = reinterpret_cast<RunEnds*>(base + s.ends);
     a.partial = reinterpret_cast<float4*>(base + s.partial);
-    if (rows > 0) {
-        LaunchScope ls(h, K_LOOKUP_SUM, st);
-        lookup_zero_kernel<<<(rows + kLookupThreads - 1) / kLookupThreads, kLookupThreads, 0, st>>>(
-            a.keys, n, rows, a.nvec, make_fast_div((uint32_t)a.nvec), d_grad_table, type);
-    }
+    a.parts = ctas;
+    const int grid = ctas + (rows + kLookupThreads - 1) / kLookupThreads;
     {
         const size_t shared = (size_t)groups * 2 * a.nvec * sizeof(float4) + ((size_t)groups * kRunItems * 2 + 4) * sizeof(uint32_t);
         LaunchScope ls(h, K_LOOKUP_SUM, st);
         switch (split.per) {
-            case 1: launch_sum<1>(a, ctas, shared, st); break;
-            case 2: launch_sum<2>(a, ctas, shared, st); break;
-            case 3: launch_sum<3>(a, ctas, shared, st); break;
-            case 4: launch_sum<4>(a, ctas, shared, st); break;
-            case 5: launch_sum<5>(a, ctas, shared, st); break;
-            case 6: launch_sum<6>(a, ctas, shared, st); break;
-            case 7: launch_sum<7>(a, ctas, shared, st); break;
-            default: launch_sum<8>(a, ctas, shared, st); break;
+            case 1: launch_sum<1>(a, grid, shared, st); break;
+            case 2: launch_sum<2>(a, grid, shared, st); break;
+            case 3: launch_sum<3>(a, grid, shared, st); break;
+            case 4: launch_sum<4>(a, grid, shared, st); break;
+            case 5: launch_sum<5>(a, grid, shared, st); break;
+            case 6: launch_sum<6>(a, grid, shared, st); break;
+            case 7: launch_sum<7>(a, grid, shared, st); break;
+            default: launch_sum<8>(a, grid, shared, st); break;
         }
     }
     {

@@ -83,16 +83,41 @@ __device__ __forceinline__ uint32_t as_halves(float a, float b, int type) {
 }
 
 // Vector v (four elements) of a buffer of `type`.
-__device__ __forceinline__ float4 load_row4(const void* p, size_t v, int type) {
-    if (type == EMC2_F32) return __ldg(static_cast<const float4*>(p) + v);
-    return as_floats(__ldg(static_cast<const uint2*>(p) + v), type);
-}
 __device__ __forceinline__ void store_row4(void* p, size_t v, const float4& f, int type) {
     if (type == EMC2_F32) static_cast<float4*>(p)[v] = f;
     else static_cast<uint2*>(p)[v] = make_uint2(as_halves(f.x, f.y, type), as_halves(f.z, f.w, type));
 }
 
-// The same for the vectors lane + i * lanes of a row, the loads of all of them first.
+// The vectors lane + i * lanes of a row as they lie in memory (a 16-bit type's in the first half), zeros past nvec, and the
+// values of one.  Apart, so that a thread can request several rows before it converts the first: behind a conversion, which
+// branches on the type, the compiler puts no earlier load.
+template <int K>
+__device__ __forceinline__ void request_row(uint4 (&r)[K], const void* p, size_t v0, int lane, int log, int nvec, int type) {
+#pragma unroll
+    for (int i = 0; i < K; ++i) r[i] = make_uint4(0u, 0u, 0u, 0u);
+    if (type == EMC2_F32) {
+#pragma unroll
+        for (int i = 0; i < K; ++i) {
+            const int v = lane + (i << log);
+            if (v < nvec) r[i] = __ldg(static_cast<const uint4*>(p) + v0 + v);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < K; ++i) {
+            const int v = lane + (i << log);
+            if (v >= nvec) continue;
+            const uint2 h = __ldg(static_cast<const uint2*>(p) + v0 + v);
+            r[i].x = h.x;
+            r[i].y = h.y;
+        }
+    }
+}
+__device__ __forceinline__ float4 row_floats(const uint4& r, int type) {
+    if (type == EMC2_F32) return make_float4(__uint_as_float(r.x), __uint_as_float(r.y), __uint_as_float(r.z), __uint_as_float(r.w));
+    return as_floats(make_uint2(r.x, r.y), type);
+}
+
+// The row's values at once, for a kernel that has one row to wait for.
 template <int K>
 __device__ __forceinline__ void load_row(float4 (&f)[K], const void* p, size_t v0, int lane, int log, int nvec, int type) {
     if (type == EMC2_F32) {
