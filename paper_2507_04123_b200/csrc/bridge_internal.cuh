@@ -82,6 +82,7 @@ enum KernelKind {
     K_FFN_GRAD_X,
     K_FFN_GRAD_W,
     K_FFN_SUM,
+    K_FFN_JOIN,
     K_KINDS
 };
 

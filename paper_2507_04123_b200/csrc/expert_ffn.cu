@@ -74,6 +74,17 @@ __device__ __forceinline__ void next_tile(const RowSegments& s, TileWalk& w, int
     }
 }
 
+// An item is a tile, or one of `splits` shares of its hidden units.
+struct ItemWalk {
+    TileWalk tile;
+    int split;
+};
+__device__ __forceinline__ void next_item(const RowSegments& s, ItemWalk& w, int tile_rows, int splits) {
+    if (++w.split < splits) return;
+    w.split = 0;
+    next_tile(s, w.tile, tile_rows);
+}
+
 // ---------------------------------------------------------------- activations, two values at a time
 // The special-function unit is what the activation waits for (16 results a clock and SM), so exponentials, reciprocals and
 // hyperbolic tangents are what is saved.
@@ -239,6 +250,8 @@ struct RowArgs {
     int C, H, c16, chunks;                  // c16: C rounded up to 16; chunks of HC hidden units
     int full, tail;                         // blocks of 64 columns, and the columns of a narrower one behind them: 0, 16 or 32
     int xn, gn, dn;                         // stages of the rows' tiles, of Wg and Wu, of Wd
+    int splits;                             // shares of the hidden units, each an item of its own; 1 unless NT is
+    float* part;                            // [items][128][C]: what the shares leave, or null
     uint32_t off_g, off_d, off_h;           // in the dynamic shared memory, behind the rows' tiles
     uint32_t x_bytes, g_bytes, d_bytes, h_bytes;   // of a stage; h: of a unit's hidden values, two of them, if they go there
     uint32_t tile_bytes;                    // of one tensor's tile
@@ -279,10 +292,12 @@ __global__ void __launch_bounds__(kFfnThreads, 1) ffn_rows_kernel(const RowArgs 
     int* start = bounds + kMaxBounds;
     load_bounds(a.seg, bounds);
     segment_starts(a.seg, bounds, kTileRows * NT, start);
-    const int total = start[a.seg.B * a.seg.E];
-    const int lo = (int)((long long)total * blockIdx.x / gridDim.x), hi = (int)((long long)total * (blockIdx.x + 1) / gridDim.x);
+    const int total = start[a.seg.B * a.seg.E] * a.splits;
+    const int lo = uniform((int)((long long)total * blockIdx.x / gridDim.x)), hi = (int)((long long)total * (blockIdx.x + 1) / gridDim.x);
     if (lo >= hi) return;
-    TileWalk walk = tile_at(a.seg, bounds, start, lo, kTileRows * NT);
+    ItemWalk walk = {tile_at(a.seg, bounds, start, lo / a.splits, kTileRows * NT), lo % a.splits};
+    auto advance = [&](ItemWalk& w) { next_item(a.seg, w, kTileRows * NT, a.splits); };
+    auto first_chunk = [&](int split) { return split * a.chunks / a.splits; };
     if (threadIdx.x == 0) {
         gave_up = 0;
         for (int s = 0; s < kMaxStages; ++s) {
@@ -305,7 +320,7 @@ __global__ void __launch_bounds__(kFfnThreads, 1) ffn_rows_kernel(const RowArgs 
     tmem_fence_after();
     const uint32_t tmem = uniform(tmem_at);
     const uint32_t acc0 = tmem + NT * a.c16, dh0 = acc0 + 4 * HC, hid0 = dh0 + (MODE == GRAD_X ? 2 * HC : 0);
-    const int items = uniform(hi - lo), units = items * a.chunks * NT;
+    const int items = uniform(hi - lo);
 #define WAIT(bar, parity) bar_wait(bar, parity, &gave_up, a.seg.status)
 
     if (warp == kCopyWarp) {
@@ -313,11 +328,11 @@ __global__ void __launch_bounds__(kFfnThreads, 1) ffn_rows_kernel(const RowArgs 
         // their rows were: the wait for one must not hold up the others.
         const uint32_t lead = elected();
         Ring x(a.xn), g(a.gn), d(a.dn), done(a.xn);
-        TileWalk rows = walk, stored = walk;
+        ItemWalk rows = walk, stored = walk;
         int t = 0, left = items * NT, st = 0, pending = items * NT;        // tiles to copy, tiles to store
         auto copy_rows = [&] {
             const uint32_t to = base + x.at * a.x_bytes, bar = x_full(x.at);
-            const int row = uniform(rows.row) + t * kTileRows;
+            const int row = uniform(rows.tile.row) + t * kTileRows;
             bar_expect(lead, bar, a.x_bytes);
             for (int b = 0; b < a.full; ++b) {
                 copy_tile(lead, to + b * kBlockBytes, &maps.x, 64 * b, row, bar);
@@ -329,11 +344,11 @@ __global__ void __launch_bounds__(kFfnThreads, 1) ffn_rows_kernel(const RowArgs 
             }
             x.next();
             --left;
-            if (++t == NT) { t = 0; next_tile(a.seg, rows, kTileRows * NT); }
+            if (++t == NT) { t = 0; advance(rows); }
         };
         auto store_rows = [&] {
-            const int row = uniform(stored.row) + st * kTileRows;
-            if (uniform(stored.left) - st * kTileRows >= kTileRows) {      // a ragged tile's rows have left directly
+            const int row = uniform(stored.tile.row) + st * kTileRows;
+            if (!a.part && uniform(stored.tile.left) - st * kTileRows >= kTileRows) {      // others have left directly
                 const uint32_t from = base + done.at * a.x_bytes;
                 for (int b = 0; b < a.full; ++b) store_tile(lead, &maps.out, 64 * b, row, from + b * kBlockBytes);
                 if (a.tail) store_tile(lead, &maps.out_tail, 64 * a.full, row, from + a.full * kBlockBytes);
@@ -343,7 +358,7 @@ __global__ void __launch_bounds__(kFfnThreads, 1) ffn_rows_kernel(const RowArgs 
             if (lead) bar_arrive(x_empty(done.at));
             done.next();
             --pending;
-            if (++st == NT) { st = 0; next_tile(a.seg, stored, kTileRows * NT); }
+            if (++st == NT) { st = 0; advance(stored); }
         };
         auto over = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xFFFFFFFFu, bar_test(bar, parity)) != 0; };
         auto given_up = [&] { return __any_sync(0xFFFFFFFFu, *(volatile int*)&gave_up) != 0; };
@@ -359,9 +374,9 @@ __global__ void __launch_bounds__(kFfnThreads, 1) ffn_rows_kernel(const RowArgs 
             }
         };
         copy_rows();
-        for (int it = 0; it < items && !given_up(); ++it, next_tile(a.seg, walk, kTileRows * NT)) {
-            const int e = uniform(walk.q / a.seg.B);
-            for (int j = 0; j < a.chunks; ++j, g.next(), d.next()) {
+        for (int it = 0; it < items && !given_up(); ++it, advance(walk)) {
+            const int e = uniform(walk.tile.q / a.seg.B), split = uniform(walk.split), end = first_chunk(split + 1);
+            for (int j = first_chunk(split); j < end; ++j, g.next(), d.next()) {
                 wait(g_empty(g.at), g.parity ^ 1);
                 const uint32_t to = base + a.off_g + g.at * a.g_bytes, bar = g_full(g.at);
                 bar_expect(lead, bar, a.g_bytes);
@@ -404,10 +419,10 @@ __global__ void __launch_bounds__(kFfnThreads, 1) ffn_rows_kernel(const RowArgs 
         if (NT == 2 && mine == 1) x.next();
         const uint32_t acc = acc0 + mine * 2 * HC;
         uint32_t use = 1;                                              // parity of the wait for this warp's accumulators
-        for (int it = 0, n = 0; it < items; ++it) {
+        for (int it = 0, n = 0, split = lo % a.splits; it < items; ++it, split = split + 1 < a.splits ? split + 1 : 0) {
             WAIT(x_full(x.at), x.parity);
             const uint64_t xa = operand_at(x0, x.at * a.x_bytes), xt = operand_at(tail_x0, x.at * a.x_bytes);
-            for (int j = 0; j < a.chunks; ++j, ++n, g.next(), d.next()) {
+            for (int j = first_chunk(split); j < first_chunk(split + 1); ++j, ++n, g.next(), d.next()) {
                 if (NT == 1 && (n & 1) != mine) continue;
                 WAIT(g_full(g.at), g.parity);
                 if (MODE == GRAD_X) WAIT(d_full(d.at), d.parity);
@@ -432,38 +447,35 @@ __global__ void __launch_bounds__(kFfnThreads, 1) ffn_rows_kernel(const RowArgs 
         const uint64_t w0 = MODE == FORWARD ? operand(base + a.off_d, HC * 2, 0) : operand(base + a.off_g, 128, 2 * HC * 128);
         const uint64_t hs0 = operand(base + a.off_h, HC * 2, 0);
         Ring w(MODE == FORWARD ? a.dn : a.gn);
-        int j = 0, t = 0;
-        uint32_t item_parity = 0;
-        for (int n = 0; n < units; ++n) {
-            // The first products of this unit have waited for the gradients' Wg and Wu, but not this warp.
-            if (t == 0) WAIT(MODE == FORWARD ? d_full(w.at) : g_full(w.at), w.parity);
-            if (j == 0) WAIT(out_empty(t), item_parity ^ 1);
-            WAIT(hid_full(n & 1), n >> 1 & 1);
-            tmem_fence_after();
-            const uint32_t out = tmem + t * a.c16;
-            const uint64_t ww = operand_at(w0, w.at * (MODE == FORWARD ? a.d_bytes : a.g_bytes));
+        for (int it = 0, n = 0, split = lo % a.splits; it < items; ++it, split = split + 1 < a.splits ? split + 1 : 0) {
+            const int from = first_chunk(split), end = first_chunk(split + 1);
+            for (int j = from; j < end; ++j, w.next())
+                for (int t = 0; t < NT; ++t, ++n) {
+                    // The first products of this unit have waited for the gradients' Wg and Wu, but not this warp.
+                    if (t == 0) WAIT(MODE == FORWARD ? d_full(w.at) : g_full(w.at), w.parity);
+                    if (j == from) WAIT(out_empty(t), (it & 1) ^ 1);
+                    WAIT(hid_full(n & 1), n >> 1 & 1);
+                    tmem_fence_after();
+                    const uint32_t out = tmem + t * a.c16;
+                    const uint64_t ww = operand_at(w0, w.at * (MODE == FORWARD ? a.d_bytes : a.g_bytes));
 #pragma unroll
-            for (int k = 0; k < kHidColumns / 8; ++k) {
-                const uint64_t b = operand_at(ww, MODE == FORWARD ? 32 * k : k * 16 * 128);
-                if (TO == TO_TMEM) product_tmem(lead, out, hid0 + (n & 1) * kHidColumns + 8 * k, b, kind_out, j > 0 || k > 0);
-                else product(lead, out, operand_at(hs0, (n & 1) * a.h_bytes + k / (HC / 16) * kHidBlock + k % (HC / 16) * 32), b, kind_out, j > 0 || k > 0);
-            }
-            products_done(lead, hid_empty(n & 1));
-            if (t == NT - 1) products_done(lead, MODE == FORWARD ? d_empty(w.at) : g_empty(w.at));
-            if (j == a.chunks - 1) products_done(lead, out_full(t));
-            if (++t == NT) {
-                t = 0;
-                w.next();
-                if (++j == a.chunks) { j = 0; item_parity ^= 1; }
-            }
+                    for (int k = 0; k < kHidColumns / 8; ++k) {
+                        const uint64_t b = operand_at(ww, MODE == FORWARD ? 32 * k : k * 16 * 128);
+                        if (TO == TO_TMEM) product_tmem(lead, out, hid0 + (n & 1) * kHidColumns + 8 * k, b, kind_out, j > from || k > 0);
+                        else product(lead, out, operand_at(hs0, (n & 1) * a.h_bytes + k / (HC / 16) * kHidBlock + k % (HC / 16) * 32), b, kind_out, j > from || k > 0);
+                    }
+                    products_done(lead, hid_empty(n & 1));
+                    if (t == NT - 1) products_done(lead, MODE == FORWARD ? d_empty(w.at) : g_empty(w.at));
+                    if (j == end - 1) products_done(lead, out_full(t));
+                }
         }
     } else if (warp < kEpilogueWarps) {
         const int group = warp >> 3, half = warp >> 2 & 1, quarter = warp & 3, r = quarter * 32 + lane;
         const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
         Ring x(a.xn);
         int n = 0;
-        for (int it = 0; it < items; ++it, next_tile(a.seg, walk, kTileRows * NT)) {
-            for (int k = 0; k < a.chunks * NT; ++k, ++n) {
+        for (int it = 0; it < items; ++it, advance(walk)) {
+            for (int k = (first_chunk(walk.split + 1) - first_chunk(walk.split)) * NT; k > 0; --k, ++n) {
                 if ((n & 1) != group) continue;
                 warp_wait(acc_full(group), n >> 1 & 1, &gave_up, a.seg.status);
                 tmem_fence_after();
@@ -474,16 +486,24 @@ __global__ void __launch_bounds__(kFfnThreads, 1) ffn_rows_kernel(const RowArgs 
             }
             // The result takes the place of the tile's rows, which no product reads any more, and leaves from there as
             // whole lines (a thread's own row would be 16 bytes of each: 1,300 clocks a tile); rows of a ragged tile leave directly.
-            const int t = NT == 2 ? group : 0, xs = x.at + t < a.xn ? x.at + t : x.at + t - a.xn, left = walk.left - t * kTileRows;
+            const int t = NT == 2 ? group : 0, xs = x.at + t < a.xn ? x.at + t : x.at + t - a.xn, left = walk.tile.left - t * kTileRows;
             warp_wait(out_full(t), it & 1, &gave_up, a.seg.status);
             tmem_fence_after();
             const uint32_t stage = base + xs * a.x_bytes;
-            uint16_t* to = static_cast<uint16_t*>(a.out) + (size_t)(walk.row + t * kTileRows + r) * a.C;
+            uint16_t* to = static_cast<uint16_t*>(a.out) + (size_t)(walk.tile.row + t * kTileRows + r) * a.C;
             for (int c = 16 * (NT == 2 ? half : 2 * group + half); c < a.c16; c += NT == 2 ? 32 : 64) {
                 uint32_t v[16];
                 __syncwarp();                                          // behind stores by some lanes
                 tmem_load(v, tmem + t * a.c16 + c + lanes);
                 tmem_wait(v);
+                if (NT == 1 && a.part) {                               // a share of the sum: ffn_join_kernel adds them up and rounds
+                    float4* part = reinterpret_cast<float4*>(a.part + ((size_t)(lo + it) * kTileRows + r) * a.C + c);
+#pragma unroll
+                    for (int k = 0; k < 16; k += 4)
+                        if (c + k < a.C)
+                            part[k / 4] = make_float4(__uint_as_float(v[k]), __uint_as_float(v[k + 1]), __uint_as_float(v[k + 2]), __uint_as_float(v[k + 3]));
+                    continue;
+                }
 #pragma unroll
                 for (int k = 0; k < 16; k += 8) {
                     const uint32_t p0 = pack<BF16>(pair(v[k], v[k + 1])), p1 = pack<BF16>(pair(v[k + 2], v[k + 3]));
@@ -505,6 +525,34 @@ __global__ void __launch_bounds__(kFfnThreads, 1) ffn_rows_kernel(const RowArgs 
     __syncthreads();
     tmem_fence_after();
     if (warp == 0) tmem_free(tmem, kTmemColumns);
+}
+
+struct JoinArgs {
+    RowSegments seg;
+    const float* part;
+    void* out;
+    int C, splits, type;
+};
+
+// The rows of one tile: the shares in their order, rounded once.
+__global__ void __launch_bounds__(256) ffn_join_kernel(JoinArgs a) {
+    __shared__ int bounds[kMaxBounds];
+    __shared__ int start[kMaxSegments + 1];
+    load_bounds(a.seg, bounds);
+    segment_starts(a.seg, bounds, kTileRows, start);
+    if ((int)blockIdx.x >= start[a.seg.B * a.seg.E]) return;
+    const TileWalk w = tile_at(a.seg, bounds, start, blockIdx.x, kTileRows);
+    const int vectors = min(w.left, kTileRows) * (a.C / 4);
+    const float4* part = reinterpret_cast<const float4*>(a.part) + (size_t)blockIdx.x * a.splits * kTileRows * (a.C / 4);
+    for (int v = blockIdx.y * 256 + threadIdx.x; v < vectors; v += gridDim.y * 256) {
+        float4 s = part[v];
+#pragma unroll 4
+        for (int k = 1; k < a.splits; ++k) {
+            const float4 x = part[(size_t)k * kTileRows * (a.C / 4) + v];
+            s.x += x.x; s.y += x.y; s.z += x.z; s.w += x.w;
+        }
+        store_row4(a.out, (size_t)w.row * (a.C / 4) + v, s, a.type);
+    }
 }
 
 // ---------------------------------------------------------------- weights: dWg, dWu, dWd
@@ -884,15 +932,26 @@ int launch_rows(emc2_bridge* h, const FfnCall& f, cudaStream_t st) {
     Maps m;
     if (!make_maps(f, HC, a.tail, &m)) return EMC2_ERR_CUDA;
     const size_t shared = std::max(room(), (size_t)(kMaxBounds + kMaxSegments + 1) * 4 + 1024);
-    const int ctas = (int)std::min<long long>(row_tiles(f.seg, NT), h->num_sms), kind = MODE == FORWARD ? K_FFN : K_FFN_GRAD_X;
+    // Few rows: shares of their hidden units keep the other SMs busy, if there is scratch for what they leave.
+    const long long tiles = row_tiles(f.seg, NT);
+    const RowsScratch& r = h->rows_scratch;
+    a.splits = 1;
+    if (NT == 1 && 2 * tiles <= h->num_sms && r.slab && f.C <= r.max_channels && r.max_hidden > 0) a.splits = (int)std::min<long long>(a.chunks, h->num_sms / tiles);
+    a.part = a.splits > 1 ? static_cast<float*>(r.slab) : nullptr;
+    const int ctas = (int)std::min<long long>(tiles * a.splits, h->num_sms), kind = MODE == FORWARD ? K_FFN : K_FFN_GRAD_X;
     const bool bf16 = f.type == EMC2_BF16;
+    int rc = EMC2_ERR_INTERNAL;
     if (f.act == EMC2_ACT_SILU)
-        return bf16 ? launch_ffn(h, kind, ffn_rows_kernel<MODE, HC, NT, TO, EMC2_ACT_SILU, true>, a, m, ctas, kFfnThreads, shared, st)
-                    : launch_ffn(h, kind, ffn_rows_kernel<MODE, HC, NT, TO, EMC2_ACT_SILU, false>, a, m, ctas, kFfnThreads, shared, st);
-    if constexpr (TO == TO_TMEM)
-        return bf16 ? launch_ffn(h, kind, ffn_rows_kernel<MODE, HC, NT, TO, EMC2_ACT_GELU, true>, a, m, ctas, kFfnThreads, shared, st)
-                    : launch_ffn(h, kind, ffn_rows_kernel<MODE, HC, NT, TO, EMC2_ACT_GELU, false>, a, m, ctas, kFfnThreads, shared, st);
-    return EMC2_ERR_INTERNAL;
+        rc = bf16 ? launch_ffn(h, kind, ffn_rows_kernel<MODE, HC, NT, TO, EMC2_ACT_SILU, true>, a, m, ctas, kFfnThreads, shared, st)
+                  : launch_ffn(h, kind, ffn_rows_kernel<MODE, HC, NT, TO, EMC2_ACT_SILU, false>, a, m, ctas, kFfnThreads, shared, st);
+    else if constexpr (TO == TO_TMEM)
+        rc = bf16 ? launch_ffn(h, kind, ffn_rows_kernel<MODE, HC, NT, TO, EMC2_ACT_GELU, true>, a, m, ctas, kFfnThreads, shared, st)
+                  : launch_ffn(h, kind, ffn_rows_kernel<MODE, HC, NT, TO, EMC2_ACT_GELU, false>, a, m, ctas, kFfnThreads, shared, st);
+    if (rc != EMC2_OK || a.splits == 1) return rc;
+    const JoinArgs join = {f.seg, a.part, f.out, f.C, a.splits, f.type};
+    LaunchScope ls(h, K_FFN_JOIN, st);
+    ffn_join_kernel<<<dim3((unsigned)tiles, (kTileRows * f.C / 4 + 1023) / 1024), 256, 0, st>>>(join);
+    return check_cuda(h, cudaGetLastError());
 }
 
 // Ranges of the tiles: four units of work per SM, but eight tiles in each while that leaves one unit per SM.
@@ -985,7 +1044,8 @@ size_t ffn_scratch_bytes(const emc2_bridge* h, int max_channels, int max_hidden)
     for (int slice : {32, 64})
         for (int slices = 1; slices <= (max_hidden + slice - 1) / slice; ++slices)
             most = std::max(most, (size_t)(weight_ranges(h, slices, 1LL << 40) + EMC2_MAX_EXPERTS) * slices * 3 * slice * C * sizeof(float));
-    return most + kShareInts * sizeof(int);
+    most += kShareInts * sizeof(int);
+    return std::max(most, (size_t)h->num_sms * kTileRows * C * sizeof(float));               // the shares of few rows
 }
 
 }  // namespace emc2
@@ -1005,8 +1065,10 @@ extern "C" int emc2_expert_ffn(emc2_bridge_t* h, int32_t B, int32_t N, int32_t c
     const FfnCall f = {row_segments(h, B, N, d_offsets), channels, hidden, type, act, d_x, nullptr, d_w_gate, d_w_up, d_w_down, d_y};
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     // Chunks of hidden units, and tiles that share their weights, as TMEM has room for (see ffn_rows_kernel).
-    if (channels <= 96) return launch_rows<FORWARD, 64, 2, TO_TMEM>(h, f, st);
-    return channels <= 128 ? launch_rows<FORWARD, 32, 2, TO_TMEM>(h, f, st) : launch_rows<FORWARD, 32, 1, TO_TMEM>(h, f, st);
+    // Two tiles share a chunk's weights where every SM has as many.
+    const bool pairs = row_tiles(f.seg, 1) > h->num_sms;
+    if (channels <= 96) return pairs ? launch_rows<FORWARD, 64, 2, TO_TMEM>(h, f, st) : launch_rows<FORWARD, 64, 1, TO_TMEM>(h, f, st);
+    return channels <= 128 && pairs ? launch_rows<FORWARD, 32, 2, TO_TMEM>(h, f, st) : launch_rows<FORWARD, 32, 1, TO_TMEM>(h, f, st);
 }
 
 extern "C" int emc2_expert_ffn_grad(emc2_bridge_t* h, int32_t B, int32_t N, int32_t channels, int32_t hidden, int32_t type, int32_t act,

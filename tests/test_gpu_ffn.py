@@ -29,12 +29,15 @@ def close(got, ref, where):
     assert not bad.any(), (where, int(bad.sum()), float((got.double() - want).abs().max()), float(bound.max()))
 
 
+@pytest.mark.parametrize("reserved", [False, True])           # with scratch, few rows are shared out by hidden units
 @pytest.mark.parametrize("act", ["silu", "gelu"])
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16], ids=str)
-@pytest.mark.parametrize("B,N,C,H,E", SHAPES)
-def test_ffn(B, N, C, H, E, dtype, act):
+@pytest.mark.parametrize("B,N,C,H,E", SHAPES + [(1, 20000, 120, 72, 2), (1, 21000, 96, 200, 3)])
+def test_ffn(B, N, C, H, E, dtype, act, reserved):
     x, _, offsets, e, (wg, wu, wd) = inputs(B, N, C, H, E, dtype)
     br = handle(B, N, E)
+    if reserved:
+        br.reserve_rows(C, H)
     y = torch.full_like(x, 7.0)
     br.expert_ffn(x, offsets, wg, wu, wd, act, out=y)
     br.status()
