@@ -386,7 +386,7 @@ int emc2_expert_ffn_grad(emc2_bridge_t* bridge, int32_t B, int32_t N, int32_t ch
                          const void* d_w_down, const void* d_grad_y, void* d_grad_x, void* d_grad_gate, void* d_grad_up,
                          void* d_grad_down, void* cuda_stream);
 
-/* Turns the handle's own streams in emc2_bridge_run off (0) or on (non-zero, the default).  Off, every
+/* Turns the handle's own streams in emc2_bridge_run and emc2_expert_ffn_grad off (0) or on (non-zero, the default).  Off, every
  * kernel of the call is enqueued on `cuda_stream` itself, one after another: for callers that
  * want no second stream, and for timing kernels one at a time. */
 int emc2_bridge_set_overlap(emc2_bridge_t* bridge, int enable);

@@ -619,7 +619,8 @@ class Bridge:
         return out
 
     def set_overlap(self, enable: bool) -> None:
-        """emc2_bridge_set_overlap: stage 1 of :meth:`run` beside stages 2 - 4 (default) or after them."""
+        """emc2_bridge_set_overlap: stage 1 of :meth:`run` beside stages 2 - 4 (default) or after them; the weights'
+        gradients of :meth:`expert_ffn_grad` beside or after the rows'."""
         self._raise(self.lib.emc2_bridge_set_overlap(self._h, int(enable)), "emc2_bridge_set_overlap")
 
     def set_tuning(self, knob, value: int) -> None:

@@ -252,6 +252,8 @@ struct RowArgs {
     int xn, gn, dn;                         // stages of the rows' tiles, of Wg and Wu, of Wd
     int splits;                             // shares of the hidden units, each an item of its own; 1 unless NT is
     float* part;                            // [items][128][C]: what the shares leave, or null
+    int2* tiles;                            // then [max_tiles] for ffn_join_kernel: a tile's first row and how many it has
+    int max_tiles;
     uint32_t off_g, off_d, off_h;           // in the dynamic shared memory, behind the rows' tiles
     uint32_t x_bytes, g_bytes, d_bytes, h_bytes;   // of a stage; h: of a unit's hidden values, two of them, if they go there
     uint32_t tile_bytes;                    // of one tensor's tile
@@ -294,6 +296,15 @@ __global__ void __launch_bounds__(kFfnThreads, 1) ffn_rows_kernel(const RowArgs 
     segment_starts(a.seg, bounds, kTileRows * NT, start);
     const int total = start[a.seg.B * a.seg.E] * a.splits;
     const int lo = uniform((int)((long long)total * blockIdx.x / gridDim.x)), hi = (int)((long long)total * (blockIdx.x + 1) / gridDim.x);
+    if (a.part && blockIdx.x == 0)
+        for (int t = threadIdx.x; t < a.max_tiles; t += kFfnThreads) {
+            int2 rows = make_int2(0, 0);
+            if (t * a.splits < total) {
+                const TileWalk w = tile_at(a.seg, bounds, start, t, kTileRows);
+                rows = make_int2(w.row, min(w.left, kTileRows));
+            }
+            a.tiles[t] = rows;
+        }
     if (lo >= hi) return;
     ItemWalk walk = {tile_at(a.seg, bounds, start, lo / a.splits, kTileRows * NT), lo % a.splits};
     auto advance = [&](ItemWalk& w) { next_item(a.seg, w, kTileRows * NT, a.splits); };
@@ -528,31 +539,29 @@ __global__ void __launch_bounds__(kFfnThreads, 1) ffn_rows_kernel(const RowArgs 
 }
 
 struct JoinArgs {
-    RowSegments seg;
     const float* part;
+    const int2* tiles;
     void* out;
     int C, splits, type;
 };
 
-// The rows of one tile: the shares in their order, rounded once.
+// Rows of one tile, a vector of four channels per thread: the shares in their order, rounded once.
 __global__ void __launch_bounds__(256) ffn_join_kernel(JoinArgs a) {
-    __shared__ int bounds[kMaxBounds];
-    __shared__ int start[kMaxSegments + 1];
-    load_bounds(a.seg, bounds);
-    segment_starts(a.seg, bounds, kTileRows, start);
-    if ((int)blockIdx.x >= start[a.seg.B * a.seg.E]) return;
-    const TileWalk w = tile_at(a.seg, bounds, start, blockIdx.x, kTileRows);
-    const int vectors = min(w.left, kTileRows) * (a.C / 4);
-    const float4* part = reinterpret_cast<const float4*>(a.part) + (size_t)blockIdx.x * a.splits * kTileRows * (a.C / 4);
-    for (int v = blockIdx.y * 256 + threadIdx.x; v < vectors; v += gridDim.y * 256) {
-        float4 s = part[v];
-#pragma unroll 4
-        for (int k = 1; k < a.splits; ++k) {
-            const float4 x = part[(size_t)k * kTileRows * (a.C / 4) + v];
+    await_predecessor();
+    const int2 rows = a.tiles[blockIdx.x];
+    const int v = blockIdx.y * 256 + threadIdx.x;
+    const size_t step = (size_t)kTileRows * (a.C / 4);
+    if (v < rows.y * (a.C / 4)) {
+        const float4* part = reinterpret_cast<const float4*>(a.part) + (size_t)blockIdx.x * a.splits * step + v;
+        float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
+        for (int k = 0; k < a.splits; ++k) {
+            const float4 x = part[k * step];
             s.x += x.x; s.y += x.y; s.z += x.z; s.w += x.w;
         }
-        store_row4(a.out, (size_t)w.row * (a.C / 4) + v, s, a.type);
+        store_row4(a.out, (size_t)rows.x * (a.C / 4) + v, s, a.type);
     }
+    release_successor();
 }
 
 // ---------------------------------------------------------------- weights: dWg, dWu, dWd
@@ -809,11 +818,12 @@ struct WeightSumArgs {
 // part by one warp where there are many, then the warps' sums in their order.
 template <int RS>
 __global__ void __launch_bounds__(256) ffn_sum_kernel(WeightSumArgs a) {
+    await_predecessor();
     constexpr int kUnits = 32 / RS;
     __shared__ float sums[RS][kUnits][33];
     const int columns = (a.C + 31) / 32, kind = blockIdx.y, e = blockIdx.z, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int c0 = blockIdx.x % columns * 32, h0 = blockIdx.x / columns * kUnits, mine = warp % RS, u0 = warp / RS * 4;
-    const int r0 = __ldg(a.share + 2 * e), r1 = __ldg(a.share + 2 * e + 1);
+    const int r0 = a.share[2 * e], r1 = a.share[2 * e + 1];
     float s[4] = {0.f, 0.f, 0.f, 0.f};
     if (c0 + lane < a.C) {
         const size_t step = (size_t)a.slices * 3 * a.slice * a.C;             // from a range to the next
@@ -821,7 +831,7 @@ __global__ void __launch_bounds__(256) ffn_sum_kernel(WeightSumArgs a) {
 #pragma unroll 4
         for (int r = r0 + mine; r < r1; r += RS)
 #pragma unroll
-            for (int k = 0; k < 4; ++k) s[k] += __ldg(p + r * step + (size_t)k * a.C);
+            for (int k = 0; k < 4; ++k) s[k] += p[r * step + (size_t)k * a.C];
     }
 #pragma unroll
     for (int k = 0; k < 4; ++k) sums[mine][u0 + k][lane] = s[k];
@@ -836,6 +846,7 @@ __global__ void __launch_bounds__(256) ffn_sum_kernel(WeightSumArgs a) {
         if (h0 + h < a.H && c0 + c < a.C)
             out[kind < 2 ? ((size_t)e * a.H + h0 + h) * a.C + c0 + c : ((size_t)e * a.C + c0 + c) * a.H + h0 + h] = (uint16_t)as_halves(v, 0.f, a.type);
     }
+    release_successor();
 }
 
 // ---------------------------------------------------------------- host
@@ -932,12 +943,15 @@ int launch_rows(emc2_bridge* h, const FfnCall& f, cudaStream_t st) {
     Maps m;
     if (!make_maps(f, HC, a.tail, &m)) return EMC2_ERR_CUDA;
     const size_t shared = std::max(room(), (size_t)(kMaxBounds + kMaxSegments + 1) * 4 + 1024);
-    // Few rows: shares of their hidden units keep the other SMs busy, if there is scratch for what they leave.
+    // Few rows: shares of their hidden units, of four chunks at least, keep the other SMs busy, if there is scratch for what
+    // they leave.  (64 rows of 64 channels, 1,024 units: 21 us in one piece, 13 and the join in four.)
     const long long tiles = row_tiles(f.seg, NT);
     const RowsScratch& r = h->rows_scratch;
     a.splits = 1;
-    if (NT == 1 && 2 * tiles <= h->num_sms && r.slab && f.C <= r.max_channels && r.max_hidden > 0) a.splits = (int)std::min<long long>(a.chunks, h->num_sms / tiles);
+    if (NT == 1 && 2 * tiles <= h->num_sms && r.slab && f.C <= r.max_channels && r.max_hidden > 0) a.splits = std::max(1, (int)std::min<long long>(a.chunks / 4, h->num_sms / tiles));
     a.part = a.splits > 1 ? static_cast<float*>(r.slab) : nullptr;
+    a.max_tiles = (int)std::min<long long>(tiles, h->num_sms);
+    a.tiles = reinterpret_cast<int2*>(a.part + (size_t)h->num_sms * kTileRows * f.C);
     const int ctas = (int)std::min<long long>(tiles * a.splits, h->num_sms), kind = MODE == FORWARD ? K_FFN : K_FFN_GRAD_X;
     const bool bf16 = f.type == EMC2_BF16;
     int rc = EMC2_ERR_INTERNAL;
@@ -948,9 +962,9 @@ int launch_rows(emc2_bridge* h, const FfnCall& f, cudaStream_t st) {
         rc = bf16 ? launch_ffn(h, kind, ffn_rows_kernel<MODE, HC, NT, TO, EMC2_ACT_GELU, true>, a, m, ctas, kFfnThreads, shared, st)
                   : launch_ffn(h, kind, ffn_rows_kernel<MODE, HC, NT, TO, EMC2_ACT_GELU, false>, a, m, ctas, kFfnThreads, shared, st);
     if (rc != EMC2_OK || a.splits == 1) return rc;
-    const JoinArgs join = {f.seg, a.part, f.out, f.C, a.splits, f.type};
+    const JoinArgs join = {a.part, a.tiles, f.out, f.C, a.splits, f.type};
     LaunchScope ls(h, K_FFN_JOIN, st);
-    ffn_join_kernel<<<dim3((unsigned)tiles, (kTileRows * f.C / 4 + 1023) / 1024), 256, 0, st>>>(join);
+    launch_chained(ffn_join_kernel, dim3((unsigned)tiles, (kTileRows * f.C / 4 + 255) / 256), 256, 0, st, join);
     return check_cuda(h, cudaGetLastError());
 }
 
@@ -1019,8 +1033,8 @@ int launch_weights(emc2_bridge* h, const FfnCall& f, void* gate, void* up, void*
     LaunchScope ls(h, K_FFN_SUM, st);
     // A few parts for each expert, or many.
     const int columns = (f.C + 31) / 32;
-    if (a.ranges > 16 * f.seg.E) ffn_sum_kernel<8><<<dim3((f.H + 3) / 4 * columns, 3, f.seg.E), 256, 0, st>>>(s);
-    else ffn_sum_kernel<1><<<dim3((f.H + 31) / 32 * columns, 3, f.seg.E), 256, 0, st>>>(s);
+    if (a.ranges > 16 * f.seg.E) launch_chained(ffn_sum_kernel<8>, dim3((f.H + 3) / 4 * columns, 3, f.seg.E), 256, 0, st, s);
+    else launch_chained(ffn_sum_kernel<1>, dim3((f.H + 31) / 32 * columns, 3, f.seg.E), 256, 0, st, s);
     return check_cuda(h, cudaGetLastError());
 }
 
@@ -1045,7 +1059,7 @@ size_t ffn_scratch_bytes(const emc2_bridge* h, int max_channels, int max_hidden)
         for (int slices = 1; slices <= (max_hidden + slice - 1) / slice; ++slices)
             most = std::max(most, (size_t)(weight_ranges(h, slices, 1LL << 40) + EMC2_MAX_EXPERTS) * slices * 3 * slice * C * sizeof(float));
     most += kShareInts * sizeof(int);
-    return std::max(most, (size_t)h->num_sms * kTileRows * C * sizeof(float));               // the shares of few rows
+    return std::max(most, (size_t)h->num_sms * (kTileRows * C * sizeof(float) + sizeof(int2)));      // the shares of few rows
 }
 
 }  // namespace emc2
@@ -1094,8 +1108,24 @@ extern "C" int emc2_expert_ffn_grad(emc2_bridge_t* h, int32_t B, int32_t N, int3
         if (e == cudaSuccess) e = cudaMemsetAsync(d_grad_down, 0, bytes, st);
         return check_cuda(h, e);
     }
+    // The weights' gradients need nothing of dx: they run on a stream of the handle, whose CTAs take the SMs over as those of
+    // dx end, instead of waiting for the last.  Not where dx is in shares, which lie in the same scratch, nor for few channels,
+    // whose CTAs of the two would be on an SM together, in each other's way.  us on one stream and on two: 15,000 rows of 128
+    // channels, 512 units 70.7 and 65.5; 60,000 of 256, 1,024 units 588 and 563; 120,000 of 64, 1,024 units, GELU 373 and 403.
+    const bool aside = h->overlap && 2 * row_tiles(f.seg, 1) > h->num_sms && channels > 96;
+    const cudaStream_t weights_st = aside ? h->side : st;
+    if (aside) {
+        cudaError_t e = cudaEventRecord(h->ev_fork, st);
+        if (e == cudaSuccess) e = cudaStreamWaitEvent(h->side, h->ev_fork, 0);
+        if (e != cudaSuccess) return check_cuda(h, e);
+    }
     // Hidden values in shared memory leave TMEM to chunks of 64 units; GELU's arithmetic has no registers for those.
     rc = channels <= 64 && act == EMC2_ACT_SILU ? launch_rows<GRAD_X, 64, 1, TO_SHARED>(h, f, st) : launch_rows<GRAD_X, 32, 1, TO_TMEM>(h, f, st);
-    if (rc == EMC2_OK) rc = launch_weights(h, f, d_grad_gate, d_grad_up, d_grad_down, st);
+    if (rc == EMC2_OK) rc = launch_weights(h, f, d_grad_gate, d_grad_up, d_grad_down, weights_st);
+    if (aside) {                                                           // also after an error: `st` never runs ahead
+        cudaError_t e = cudaEventRecord(h->ev_join, h->side);
+        if (e == cudaSuccess) e = cudaStreamWaitEvent(st, h->ev_join, 0);
+        if (rc == EMC2_OK) rc = check_cuda(h, e);
+    }
     return rc;
 }

@@ -234,14 +234,15 @@ struct NormSumArgs {
 // order; 32 columns per CTA.
 constexpr int kNormSumThreads = 1024;
 __global__ void __launch_bounds__(kNormSumThreads) norm_sum_kernel(NormSumArgs a) {
+    await_predecessor();
     constexpr int kWarps = kNormSumThreads / 32;
     __shared__ float sum[kWarps][33];
     const int e = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;     // column of [dw | db]
-    const int i0 = __ldg(a.share + 2 * e), i1 = __ldg(a.share + 2 * e + 1);
+    const int i0 = a.share[2 * e], i1 = a.share[2 * e + 1];
     float s = 0.f;
     if (c < 2 * a.C) {
 #pragma unroll 4
-        for (int i = i0 + warp; i < i1; i += kWarps) s += __ldg(a.part + (size_t)(i + e) * 2 * a.C + c);
+        for (int i = i0 + warp; i < i1; i += kWarps) s += a.part[(size_t)(i + e) * 2 * a.C + c];
     }
     sum[warp][lane] = s;
     __syncthreads();
@@ -254,6 +255,7 @@ __global__ void __launch_bounds__(kNormSumThreads) norm_sum_kernel(NormSumArgs a
         if (mine < a.C) a.dweight[e * a.C + mine] = v;
         else if (a.dbias) a.dbias[e * a.C + mine - a.C] = v;
     }
+    release_successor();
 }
 
 template <template <int> class F, typename... A>
@@ -372,7 +374,7 @@ extern "C" int emc2_expert_norm_grad(emc2_bridge_t* h, int32_t B, int32_t N, int
     }
     {
         LaunchScope ls(h, K_NORM_SUM, st);
-        norm_sum_kernel<<<dim3((2 * channels + 31) / 32, seg.E), kNormSumThreads, 0, st>>>(t);
+        launch_chained(norm_sum_kernel, dim3((2 * channels + 31) / 32, seg.E), kNormSumThreads, 0, st, t);
     }
     return check_cuda(h, cudaGetLastError());
 }

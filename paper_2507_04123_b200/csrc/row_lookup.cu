@@ -99,6 +99,7 @@ __device__ __forceinline__ uint32_t sort_key(const SortArgs& a, int i) {
 
 // counts[d][tile]: items of the tile with digit d.
 __global__ void __launch_bounds__(kSortThreads) sort_count_kernel(SortArgs a) {
+    await_predecessor();
     __shared__ int hist[kMaxDigits];
     for (int d = threadIdx.x; d < a.digits; d += kSortThreads) hist[d] = 0;
     __syncthreads();
@@ -114,10 +115,12 @@ __global__ void __launch_bounds__(kSortThreads) sort_count_kernel(SortArgs a) {
     __syncthreads();
     for (int d = threadIdx.x; d < a.digits; d += kSortThreads) a.counts[(size_t)d * a.stride + blockIdx.x] = hist[d];
     if (bad) atomicOr(a.status, kStatusBadRows);
+    release_successor();
 }
 
 // Exclusive prefix sums over every row of counts, a warp per digit and 128 tiles at a time, and the digits' totals.
 __global__ void __launch_bounds__(kSortThreads) sort_scan_kernel(SortArgs a) {
+    await_predecessor();
     const int d = blockIdx.x * kSortWarps + (threadIdx.x >> 5), lane = threadIdx.x & 31;
     if (d >= a.digits) return;
     int4* row = reinterpret_cast<int4*>(a.counts + (size_t)d * a.stride);
@@ -143,6 +146,7 @@ __global__ void __launch_bounds__(kSortThreads) sort_scan_kernel(SortArgs a) {
         run += __shfl_sync(0xFFFFFFFFu, inc, 31);
     }
     if (lane == 0) a.totals[d] = run;
+    release_successor();
 }
 
 // Exclusive prefix sum of v[0 .. n) in shared memory, n <= kMaxDigits, by the whole CTA.
@@ -177,6 +181,7 @@ __device__ __forceinline__ void scan_digits(int* v, int n, int* warp_sums) {
 // "earlier round, or lower lane": the rank among the warp's items of a digit is a running count plus a match over the lanes.
 // The tile is put in order in shared memory first and leaves in runs.
 __global__ void __launch_bounds__(kSortThreads, 4) sort_move_kernel(SortArgs a) {
+    await_predecessor();
     __shared__ uint16_t wcnt[kSortWarps][kMaxDigits];  // items of a digit by warp, then those of the warps before
     __shared__ int first[kMaxDigits];                  // place of a digit's first item in the tile ...
     __shared__ int to[kMaxDigits];                     // ... and of it in the whole list, less that
@@ -245,6 +250,7 @@ __global__ void __launch_bounds__(kSortThreads, 4) sort_move_kernel(SortArgs a) 
         a.keys_out[place] = k;
         a.vals_out[place] = vals[i];
     }
+    release_successor();
 }
 
 // First place in [lo, hi) of the ascending keys whose key is at least k; hi if there is none.
@@ -320,6 +326,7 @@ struct SumArgs {
 // several places are requested before the first is added.
 template <int K, bool kHalf>
 __global__ void __launch_bounds__(kLookupThreads, K == 1 ? 4 : K <= 3 ? 3 : 2) lookup_sum_kernel(SumArgs a) {
+    await_predecessor();
     using Raw = std::conditional_t<kHalf, uint2, float4>;
 
     if ((int)blockIdx.x >= a.parts) {
@@ -435,10 +442,12 @@ __global__ void __launch_bounds__(kLookupThreads, K == 1 ? 4 : K <= 3 ? 3 : 2) l
         else if (all.through) partial[0] = run;
         if (v == 0) a.ends[blockIdx.x] = all;
     }
+    release_successor();
 }
 
 // The runs that the CTAs' parts divide: CTA i joins the one that begins in part i, its warps every eighth part of it.
 __global__ void __launch_bounds__(kLookupThreads) lookup_join_kernel(SumArgs a, int parts) {
+    await_predecessor();
     constexpr int kWarps = kLookupThreads / 32;
     extern __shared__ float4 part[];            // [warps][nvec]
     const int i = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -472,12 +481,13 @@ __global__ void __launch_bounds__(kLookupThreads) lookup_join_kernel(SumArgs a, 
         }
         store_row4(a.dtable, (size_t)id * a.nvec + v, scaled(s, a.scale), a.type);
     }
+    release_successor();
 }
 
 template <int K, bool kHalf>
 void launch_sum_of(const SumArgs& a, int ctas, size_t shared, cudaStream_t st) {
     if (shared > 40 * 1024) cudaFuncSetAttribute(lookup_sum_kernel<K, kHalf>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)shared);
-    lookup_sum_kernel<K, kHalf><<<ctas, kLookupThreads, shared, st>>>(a);
+    launch_chained(lookup_sum_kernel<K, kHalf>, dim3(ctas), kLookupThreads, shared, st, a);
 }
 template <int K>
 void launch_sum(const SumArgs& a, int ctas, size_t shared, cudaStream_t st) {
@@ -599,9 +609,9 @@ extern "C" int emc2_row_lookup_grad(emc2_bridge_t* h, int32_t n, int32_t rows, i
         o.counts = reinterpret_cast<int*>(base + s.counts); o.totals = reinterpret_cast<int*>(base + s.row_tot); o.status = h->d_status;
         o.n = n; o.rows = rows; o.tiles = (n + kSortItems - 1) / kSortItems; o.stride = (o.tiles + 3) / 4 * 4; o.shift = p * digit; o.digits = 1 << digit;
         LaunchScope ls(h, K_LOOKUP_SORT, st);
-        sort_count_kernel<<<o.tiles, kSortThreads, 0, st>>>(o);
-        sort_scan_kernel<<<(o.digits + kSortWarps - 1) / kSortWarps, kSortThreads, 0, st>>>(o);
-        sort_move_kernel<<<o.tiles, kSortThreads, 0, st>>>(o);
+        launch_kernel(p > 0, sort_count_kernel, dim3(o.tiles), kSortThreads, 0, st, o);
+        launch_chained(sort_scan_kernel, dim3((o.digits + kSortWarps - 1) / kSortWarps), kSortThreads, 0, st, o);
+        launch_chained(sort_move_kernel, dim3(o.tiles), kSortThreads, 0, st, o);
     }
     a.keys = keys[at]; a.vals = vals[at]; a.dout = d_grad_out; a.dtable = d_grad_table; a.scale = scale; a.n = n; a.rows = rows;
     a.log = split.log; a.type = type;
@@ -625,7 +635,7 @@ extern "C" int emc2_row_lookup_grad(emc2_bridge_t* h, int32_t n, int32_t rows, i
     }
     {
         LaunchScope ls(h, K_LOOKUP_JOIN, st);
-        lookup_join_kernel<<<ctas, kLookupThreads, (size_t)(kLookupThreads / 32) * a.nvec * sizeof(float4), st>>>(a, ctas);
+        launch_chained(lookup_join_kernel, dim3(ctas), kLookupThreads, (size_t)(kLookupThreads / 32) * a.nvec * sizeof(float4), st, a, ctas);
     }
     return check_cuda(h, cudaGetLastError());
 }

@@ -166,6 +166,49 @@ def test_ffn_captured_replayed_and_on_another_stream():
     fresh.close()
 
 
+def test_ffn_gradients_on_two_streams_of_the_handle():
+    """Enough rows and channels that the weights' gradients run beside the rows': the same bits as one after the other, with
+    the inputs overwritten right behind the call, and captured."""
+    B, N, C, H, E = 2, 6000, 136, 64, 3
+    g = torch.Generator(device=DEV)
+    g.manual_seed(8)
+    br = handle(B, N, E)
+    br.reserve_rows(C, H)
+    offsets = ascending_offsets(B, N, E, seed=9)
+    rows = rand(g, 2, B, N, C, dtype=torch.bfloat16)
+    ws = [rand(g, *s, dtype=torch.bfloat16, scale=0.1) for s in ((E, H, C), (E, H, C), (E, C, H))]
+    x, dy = rows.clone()
+    br.set_overlap(False)
+    out = {k: torch.zeros_like(v) for k, v in br.expert_ffn_grad(x, offsets, *ws, dy).items()}
+    br.expert_ffn_grad(x, offsets, *ws, dy, out=out)
+    want = {k: v.clone() for k, v in out.items()}
+    br.set_overlap(True)
+    for _ in range(20):
+        x.copy_(rows[0])
+        dy.copy_(rows[1])
+        for v in out.values():
+            v.zero_()
+        br.expert_ffn_grad(x, offsets, *ws, dy, out=out)
+        x.zero_()
+        dy.zero_()
+        assert all(torch.equal(out[k], want[k]) for k in want)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        x.copy_(rows[0])
+        dy.copy_(rows[1])
+        br.expert_ffn_grad(x, offsets, *ws, dy, out=out)
+        x.zero_()
+        dy.zero_()
+    for _ in range(3):
+        for v in out.values():
+            v.zero_()
+        graph.replay()
+        assert all(torch.equal(out[k], want[k]) for k in want)
+    br.status()
+    del graph
+    br.close()
+
+
 def test_one_expert_without_offsets_and_empty_batches():
     br = handle(2, 64, 4)
     br.reserve_rows(32, 64)
