@@ -6,13 +6,16 @@
 //
 // All products run on the tensor cores (tcgen05, fp32 accumulators in TMEM).  Nothing of width H reaches device memory:
 // tiles of 128 rows stay in shared memory while the hidden units pass by in chunks, whose weights are copied in beside the
-// products.  What bounds the kernels is shared memory: a product of 128 x N x 16 reads (128 + N) * 32 bytes at about 110 bytes
-// a clock, which is longer than it computes below N = 200, and the copies and stores share that rate.  So the hidden
-// values go back to TMEM for the second product of y and dx, as its A, and chunks are as wide as TMEM allows.  What lies between the two products of a chunk (h, or dg and du) is rounded to the rows' type, as the tensor
-// cores take it; all sums are held in fp32, results are rounded once.
+// products.  What bounds the kernels are the products' own times at these widths and the activation beside them.  A product of
+// 128 x N x 16 takes N / 2 clocks by its arithmetic; issued back to back it was measured at 45 clocks for N = 32, 49 for 64, 65
+// for 128, 129 for 256, and at no less than 63 with A in TMEM.  So chunks are as wide as TMEM allows.  The hidden values go
+// back to TMEM for the second product of y and dx, as its A, which leaves the shared memory to the copies; where TMEM is
+// needed for wider chunks they go to shared memory.  What lies between the two products of a chunk (h, or dg and du) is
+// rounded to the rows' type, as the tensor cores take it; all sums are held in fp32, results are rounded once.
 //
-// Warps of several kinds pass tiles along with mbarriers: one thread copies (tiled bulk copies), one issues the products
-// before the activation and one those behind it (one thread for both was what all waited for), sixteen warps apply the activation from TMEM to shared memory, eight per accumulator so that one is filled while the other is read.
+// Warps of several kinds pass tiles along with mbarriers: one copies (tiled bulk copies), two issue the products before the
+// activation and one those behind it (one for all was what all waited for), sixteen apply the activation from TMEM to TMEM or
+// shared memory, eight per accumulator so that one is filled while the other is read.
 #include <algorithm>
 
 #include "rows.cuh"
@@ -419,7 +422,8 @@ __global__ void __launch_bounds__(kFfnThreads, 1) ffn_rows_kernel(const RowArgs 
         // begins, and every wait takes 100 clocks even if it is over: one waits while the other's products run.
         // A barrier's parity says no more than whether its last use is over.  So a warp waits for every use of a stage in
         // turn, and no stage comes round before both are done with it: each tile of an item, or each second chunk where an
-        // item is one tile, has stages of its own (their numbers are even).
+        // item is one tile, has stages of its own (their numbers are even), and an item is not over before both have issued a
+        // chunk of it; if it has a single one, the first warp takes all.
         const int mine = warp == kFirstWarp ? 0 : 1;
         const uint32_t lead = elected(), kind_gu = product_kind(2 * HC, BF16, false, false), kind_dh = product_kind(HC, BF16, false, true);
         const int steps = 4 * a.full, tail_steps = a.tail / 16;
@@ -428,26 +432,27 @@ __global__ void __launch_bounds__(kFfnThreads, 1) ffn_rows_kernel(const RowArgs 
         const uint64_t x0 = operand(base, 128, 0), w0 = operand(base + a.off_g, 128, 0), wd0 = operand(base + a.off_d, HC * 2, 0);
         Ring x(a.xn), g(a.gn), d(a.dn);
         if (NT == 2 && mine == 1) x.next();
-        const uint32_t acc = acc0 + mine * 2 * HC;
-        uint32_t use = 1;                                              // parity of the wait for this warp's accumulators
-        for (int it = 0, n = 0, split = lo % a.splits; it < items; ++it, split = split + 1 < a.splits ? split + 1 : 0) {
+        const bool alone = NT == 1 && a.chunks == 1;
+        const int mine_items = alone && mine == 1 ? 0 : items;
+        for (int it = 0, n = 0, split = lo % a.splits; it < mine_items; ++it, split = split + 1 < a.splits ? split + 1 : 0) {
             WAIT(x_full(x.at), x.parity);
             const uint64_t xa = operand_at(x0, x.at * a.x_bytes), xt = operand_at(tail_x0, x.at * a.x_bytes);
             for (int j = first_chunk(split); j < first_chunk(split + 1); ++j, ++n, g.next(), d.next()) {
-                if (NT == 1 && (n & 1) != mine) continue;
+                if (NT == 1 && (n & 1) != mine && !alone) continue;
+                const int slot = NT == 2 ? mine : n & 1;               // of the accumulators
+                const uint32_t acc = acc0 + slot * 2 * HC, dh = dh0 + slot * HC;
                 WAIT(g_full(g.at), g.parity);
                 if (MODE == GRAD_X) WAIT(d_full(d.at), d.parity);
-                WAIT(acc_empty(mine), use);
-                use ^= 1;
+                WAIT(acc_empty(slot), ((NT == 2 ? n : n >> 1) & 1) ^ 1);
                 tmem_fence_after();
                 product_blocks(lead, acc, xa, kBlockBytes, operand_at(w0, g.at * a.g_bytes), 2 * HC * 128, steps, kind_gu);
                 product_blocks(lead, acc, xt, 0, operand_at(tail_w0, g.at * a.g_bytes), 0, tail_steps, kind_gu, steps > 0);
                 if (MODE == GRAD_X) {
                     const uint64_t wd = operand_at(wd0, d.at * a.d_bytes);
-                    product_blocks_mn(lead, dh0 + mine * HC, operand_at(xa, a.tile_bytes), kBlockBytes, wd, 32 * HC, steps, kind_dh);
-                    product_blocks_mn(lead, dh0 + mine * HC, operand_at(xt, a.tile_bytes), 0, operand_at(wd, steps * 32 * HC), 32 * HC, tail_steps, kind_dh, steps > 0);
+                    product_blocks_mn(lead, dh, operand_at(xa, a.tile_bytes), kBlockBytes, wd, 32 * HC, steps, kind_dh);
+                    product_blocks_mn(lead, dh, operand_at(xt, a.tile_bytes), 0, operand_at(wd, steps * 32 * HC), 32 * HC, tail_steps, kind_dh, steps > 0);
                 }
-                products_done(lead, acc_full(mine));
+                products_done(lead, acc_full(slot));
                 // The gradients' second products take Wg and Wu again: their warp gives them back.
                 products_done(lead, MODE == FORWARD ? g_empty(g.at) : d_empty(d.at));
             }
@@ -811,7 +816,7 @@ struct WeightSumArgs {
     void* gate;
     void* up;
     void* down;
-    int C, H, E, slice, slices, ranges, type;
+    int C, H, slice, slices, type;
 };
 
 // dW of 32 / RS hidden units and 32 channels: the parts of the ranges that met the expert.  Four units per warp; every RS-th
@@ -944,14 +949,16 @@ int launch_rows(emc2_bridge* h, const FfnCall& f, cudaStream_t st) {
     if (!make_maps(f, HC, a.tail, &m)) return EMC2_ERR_CUDA;
     const size_t shared = std::max(room(), (size_t)(kMaxBounds + kMaxSegments + 1) * 4 + 1024);
     // Few rows: shares of their hidden units, of four chunks at least, keep the other SMs busy, if there is scratch for what
-    // they leave.  (64 rows of 64 channels, 1,024 units: 21 us in one piece, 13 and the join in four.)
+    // they leave and more than 16 chunks.  us in one piece, and in shares with their join: 64 rows of 64 channels, 4,096 units
+    // 41.8 and 20.1; 512 units 18.6 and 23.2.
     const long long tiles = row_tiles(f.seg, NT);
     const RowsScratch& r = h->rows_scratch;
     a.splits = 1;
-    if (NT == 1 && 2 * tiles <= h->num_sms && r.slab && f.C <= r.max_channels && r.max_hidden > 0) a.splits = std::max(1, (int)std::min<long long>(a.chunks / 4, h->num_sms / tiles));
+    if (NT == 1 && 2 * tiles <= h->num_sms && r.slab && f.C <= r.max_channels && r.max_hidden > 0 && a.chunks > 16)
+        a.splits = (int)std::min<long long>(a.chunks / 4, h->num_sms / tiles);
     a.part = a.splits > 1 ? static_cast<float*>(r.slab) : nullptr;
     a.max_tiles = (int)std::min<long long>(tiles, h->num_sms);
-    a.tiles = reinterpret_cast<int2*>(a.part + (size_t)h->num_sms * kTileRows * f.C);
+    a.tiles = a.part ? reinterpret_cast<int2*>(a.part + (size_t)h->num_sms * kTileRows * f.C) : nullptr;
     const int ctas = (int)std::min<long long>(tiles * a.splits, h->num_sms), kind = MODE == FORWARD ? K_FFN : K_FFN_GRAD_X;
     const bool bf16 = f.type == EMC2_BF16;
     int rc = EMC2_ERR_INTERNAL;
@@ -1014,8 +1021,9 @@ int launch_slices(emc2_bridge* h, const FfnCall& f, WeightArgs& a, cudaStream_t 
                 : launch_ffn(h, K_FFN_GRAD_W, ffn_weights_kernel<HC, EMC2_ACT_GELU, false>, a, m, ctas, kFfnThreads, shared, st);
 }
 
-// Slices of 64 hidden units where two stages of tiles fit beside them (up to 96 channels): half the products, each of which
-// waits for its 128 rows of A below N = 128.
+// Slices of 64 hidden units where two stages of tiles fit beside them (up to 96 channels): half the products, which below
+// N = 128 take little less for half the columns.  us with 64 and with 32, 60,000 rows: 64 channels, 1,024 units 88.9 and
+// 123.4; 96 channels, 512 units 74.2 and 84.9.
 bool wide_slices(const FfnCall& f) {
     WeightArgs a;
     plan_weights<64>(a, f);
@@ -1028,12 +1036,14 @@ int launch_weights(emc2_bridge* h, const FfnCall& f, void* gate, void* up, void*
     const int rc = wide ? launch_slices<64>(h, f, a, st) : launch_slices<32>(h, f, a, st);
     if (rc != EMC2_OK) return rc;
     WeightSumArgs s;
-    s.part = a.part; s.share = a.share; s.gate = gate; s.up = up; s.down = down; s.C = f.C; s.H = f.H; s.E = f.seg.E;
-    s.slice = wide ? 64 : 32; s.slices = a.slices; s.ranges = a.ranges; s.type = f.type;
+    s.part = a.part; s.share = a.share; s.gate = gate; s.up = up; s.down = down; s.C = f.C; s.H = f.H;
+    s.slice = wide ? 64 : 32; s.slices = a.slices; s.type = f.type;
     LaunchScope ls(h, K_FFN_SUM, st);
-    // A few parts for each expert, or many.
+    // Where the CTAs with 32 units each would be two per SM or fewer, eight times as many share out the parts.  us with 32 units
+    // and with 4: 60,000 rows of 64 channels and 256 units, four experts (192 CTAs) 14.5 and 9.2; of 128 and 512 (768 CTAs)
+    // 13.7 and 17.8.
     const int columns = (f.C + 31) / 32;
-    if (a.ranges > 16 * f.seg.E) launch_chained(ffn_sum_kernel<8>, dim3((f.H + 3) / 4 * columns, 3, f.seg.E), 256, 0, st, s);
+    if ((f.H + 31) / 32 * columns * 3 * f.seg.E <= 2 * h->num_sms) launch_chained(ffn_sum_kernel<8>, dim3((f.H + 3) / 4 * columns, 3, f.seg.E), 256, 0, st, s);
     else launch_chained(ffn_sum_kernel<1>, dim3((f.H + 31) / 32 * columns, 3, f.seg.E), 256, 0, st, s);
     return check_cuda(h, cudaGetLastError());
 }
@@ -1078,8 +1088,10 @@ extern "C" int emc2_expert_ffn(emc2_bridge_t* h, int32_t B, int32_t N, int32_t c
     if (!device.ok) return EMC2_ERR_CUDA;
     const FfnCall f = {row_segments(h, B, N, d_offsets), channels, hidden, type, act, d_x, nullptr, d_w_gate, d_w_up, d_w_down, d_y};
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-    // Chunks of hidden units, and tiles that share their weights, as TMEM has room for (see ffn_rows_kernel).
-    // Two tiles share a chunk's weights where every SM has as many.
+    // Chunks of hidden units, and tiles that share their weights, as TMEM has room for (see ffn_rows_kernel).  Two tiles share
+    // a chunk's weights where there is more than one per SM.  us
+    // of one and of two: 15,000 rows of 64 channels, 1,024 units 21.7 and 26.8; 20,000 30.9 and 27.2; 60,000 52.1
+    // and 44.0; 60,000 of 128 channels, 512 units 50.9 and 38.5.
     const bool pairs = row_tiles(f.seg, 1) > h->num_sms;
     if (channels <= 96) return pairs ? launch_rows<FORWARD, 64, 2, TO_TMEM>(h, f, st) : launch_rows<FORWARD, 64, 1, TO_TMEM>(h, f, st);
     return channels <= 128 && pairs ? launch_rows<FORWARD, 32, 2, TO_TMEM>(h, f, st) : launch_rows<FORWARD, 32, 1, TO_TMEM>(h, f, st);
@@ -1119,7 +1131,8 @@ extern "C" int emc2_expert_ffn_grad(emc2_bridge_t* h, int32_t B, int32_t N, int3
         if (e == cudaSuccess) e = cudaStreamWaitEvent(h->side, h->ev_fork, 0);
         if (e != cudaSuccess) return check_cuda(h, e);
     }
-    // Hidden values in shared memory leave TMEM to chunks of 64 units; GELU's arithmetic has no registers for those.
+    // Hidden values in shared memory leave TMEM to chunks of 64 units; GELU's arithmetic has no registers for those.  us of dx
+    // with them and with chunks of 32: 60,000 rows of 64 channels, 1,024 units, SiLU 62.7 and 85.2; 256 units 32.1 and 35.1.
     rc = channels <= 64 && act == EMC2_ACT_SILU ? launch_rows<GRAD_X, 64, 1, TO_SHARED>(h, f, st) : launch_rows<GRAD_X, 32, 1, TO_TMEM>(h, f, st);
     if (rc == EMC2_OK) rc = launch_weights(h, f, d_grad_gate, d_grad_up, d_grad_down, weights_st);
     if (aside) {                                                           // also after an error: `st` never runs ahead

@@ -220,8 +220,8 @@ __device__ __forceinline__ uint64_t reciprocals(float a, float b) {
 
 // ---- products: D[128, N] (+)= A[128, 16] B[16, N], fp32 accumulators
 // A whole warp comes here, with the same arguments in every lane, and its elected lane issues: the descriptors then stay in
-// uniform registers.  Issued by a thread on a branch of its own each product took 71 clocks whatever its N; so it takes
-// what the tensor core does: 52 at N = 32, 58 at 64, 72 at 128, 127 at 256 (B200; below N = 128 it waits for A, 4 KB).
+// uniform registers.  Issued by a thread on a branch of its own each product took 71 clocks or more; so it takes what the
+// tensor core does: 45 up to N = 32, 49 at 64, 65 at 128, 97 at 192, 129 at 256, and with A in TMEM 63 up to N = 128 (B200).
 // Shared-memory operands are tiles of rows of `row_bytes` (128, 64 or 32, with the swizzle of that width): groups of eight
 // rows follow one another every 8 * row_bytes.
 //   K-major  (a row holds consecutive k of one m or n): a step of 16 k is 32 bytes further in the row
