@@ -211,7 +211,7 @@ __device__ __forceinline__ void warp_arrive(uint32_t bar) {
 template <int MODE, int HC, int ACT, bool BF16, int TO>
 __device__ __forceinline__ void hidden_half(uint32_t acc, uint32_t acc_dh, int half, uint32_t to, int r, uint32_t acc_empty, uint32_t hid_empty,
                                             uint32_t parity, volatile int* gave_up, int* status) {
-    constexpr int W = MODE == FORWARD ? HC / 2 : HC == 64 || ACT == EMC2_ACT_GELU ? 8 : 16;
+    constexpr int W = MODE == FORWARD ? HC / 2 : HC == 64 || (ACT == EMC2_ACT_GELU && TO != TO_TMEM) ? 8 : 16;
 #pragma unroll
     for (int c = 0; c < HC / 2; c += W) {
         uint32_t g[W], u[W], dh[W];
@@ -266,7 +266,7 @@ struct Maps {
     CUtensorMap x_tail, dy_tail, gate_tail, up_tail, out_tail;              // of the last block of columns, where it is narrower
 };
 
-template <int MODE, int HC, int NT, int TO, int ACT, bool BF16>
+template <int MODE, int HC, int NT, int TO, int ACT, bool BF16, bool SHARES>
 __global__ void __launch_bounds__(kFfnThreads, 1) ffn_rows_kernel(const RowArgs a, const __grid_constant__ Maps maps) {
     // TMEM: the output of NT tiles, two accumulators of g and u, for dx two of dh, and the hidden values of two units unless
     // those go to shared memory.
@@ -297,21 +297,21 @@ __global__ void __launch_bounds__(kFfnThreads, 1) ffn_rows_kernel(const RowArgs 
     int* start = bounds + kMaxBounds;
     load_bounds(a.seg, bounds);
     segment_starts(a.seg, bounds, kTileRows * NT, start);
-    const int total = start[a.seg.B * a.seg.E] * a.splits;
+    const int splits = SHARES ? a.splits : 1, total = start[a.seg.B * a.seg.E] * splits;
     const int lo = uniform((int)((long long)total * blockIdx.x / gridDim.x)), hi = (int)((long long)total * (blockIdx.x + 1) / gridDim.x);
-    if (a.part && blockIdx.x == 0)
+    if (SHARES && blockIdx.x == 0)
         for (int t = threadIdx.x; t < a.max_tiles; t += kFfnThreads) {
             int2 rows = make_int2(0, 0);
-            if (t * a.splits < total) {
+            if (t * splits < total) {
                 const TileWalk w = tile_at(a.seg, bounds, start, t, kTileRows);
                 rows = make_int2(w.row, min(w.left, kTileRows));
             }
             a.tiles[t] = rows;
         }
     if (lo >= hi) return;
-    ItemWalk walk = {tile_at(a.seg, bounds, start, lo / a.splits, kTileRows * NT), lo % a.splits};
-    auto advance = [&](ItemWalk& w) { next_item(a.seg, w, kTileRows * NT, a.splits); };
-    auto first_chunk = [&](int split) { return split * a.chunks / a.splits; };
+    ItemWalk walk = {tile_at(a.seg, bounds, start, lo / splits, kTileRows * NT), lo % splits};
+    auto advance = [&](ItemWalk& w) { next_item(a.seg, w, kTileRows * NT, splits); };
+    auto first_chunk = [&](int split) { return SHARES ? split * a.chunks / splits : split > 0 ? a.chunks : 0; };
     if (threadIdx.x == 0) {
         gave_up = 0;
         for (int s = 0; s < kMaxStages; ++s) {
@@ -362,7 +362,7 @@ __global__ void __launch_bounds__(kFfnThreads, 1) ffn_rows_kernel(const RowArgs 
         };
         auto store_rows = [&] {
             const int row = uniform(stored.tile.row) + st * kTileRows;
-            if (!a.part && uniform(stored.tile.left) - st * kTileRows >= kTileRows) {      // others have left directly
+            if (!SHARES && uniform(stored.tile.left) - st * kTileRows >= kTileRows) {      // others have left directly
                 const uint32_t from = base + done.at * a.x_bytes;
                 for (int b = 0; b < a.full; ++b) store_tile(lead, &maps.out, 64 * b, row, from + b * kBlockBytes);
                 if (a.tail) store_tile(lead, &maps.out_tail, 64 * a.full, row, from + a.full * kBlockBytes);
@@ -434,7 +434,7 @@ __global__ void __launch_bounds__(kFfnThreads, 1) ffn_rows_kernel(const RowArgs 
         if (NT == 2 && mine == 1) x.next();
         const bool alone = NT == 1 && a.chunks == 1;
         const int mine_items = alone && mine == 1 ? 0 : items;
-        for (int it = 0, n = 0, split = lo % a.splits; it < mine_items; ++it, split = split + 1 < a.splits ? split + 1 : 0) {
+        for (int it = 0, n = 0, split = lo % splits; it < mine_items; ++it, split = split + 1 < splits ? split + 1 : 0) {
             WAIT(x_full(x.at), x.parity);
             const uint64_t xa = operand_at(x0, x.at * a.x_bytes), xt = operand_at(tail_x0, x.at * a.x_bytes);
             for (int j = first_chunk(split); j < first_chunk(split + 1); ++j, ++n, g.next(), d.next()) {
@@ -463,7 +463,7 @@ __global__ void __launch_bounds__(kFfnThreads, 1) ffn_rows_kernel(const RowArgs 
         const uint64_t w0 = MODE == FORWARD ? operand(base + a.off_d, HC * 2, 0) : operand(base + a.off_g, 128, 2 * HC * 128);
         const uint64_t hs0 = operand(base + a.off_h, HC * 2, 0);
         Ring w(MODE == FORWARD ? a.dn : a.gn);
-        for (int it = 0, n = 0, split = lo % a.splits; it < items; ++it, split = split + 1 < a.splits ? split + 1 : 0) {
+        for (int it = 0, n = 0, split = lo % splits; it < items; ++it, split = split + 1 < splits ? split + 1 : 0) {
             const int from = first_chunk(split), end = first_chunk(split + 1);
             for (int j = from; j < end; ++j, w.next())
                 for (int t = 0; t < NT; ++t, ++n) {
@@ -512,20 +512,20 @@ __global__ void __launch_bounds__(kFfnThreads, 1) ffn_rows_kernel(const RowArgs 
                 __syncwarp();                                          // behind stores by some lanes
                 tmem_load(v, tmem + t * a.c16 + c + lanes);
                 tmem_wait(v);
-                if (NT == 1 && a.part) {                               // a share of the sum: ffn_join_kernel adds them up and rounds
+                if constexpr (SHARES) {                                // part of the sum: ffn_join_kernel adds them up and rounds
                     float4* part = reinterpret_cast<float4*>(a.part + ((size_t)(lo + it) * kTileRows + r) * a.C + c);
 #pragma unroll
                     for (int k = 0; k < 16; k += 4)
                         if (c + k < a.C)
                             part[k / 4] = make_float4(__uint_as_float(v[k]), __uint_as_float(v[k + 1]), __uint_as_float(v[k + 2]), __uint_as_float(v[k + 3]));
-                    continue;
-                }
+                } else {
 #pragma unroll
-                for (int k = 0; k < 16; k += 8) {
-                    const uint32_t p0 = pack<BF16>(pair(v[k], v[k + 1])), p1 = pack<BF16>(pair(v[k + 2], v[k + 3]));
-                    const uint32_t p2 = pack<BF16>(pair(v[k + 4], v[k + 5])), p3 = pack<BF16>(pair(v[k + 6], v[k + 7]));
-                    if (left >= kTileRows) store_shared(stage + (c >> 6) * kBlockBytes + swizzled(c >> 6 < a.full ? 64 : a.tail, r, (c & 63) / 8 + k / 8), p0, p1, p2, p3);
-                    else if (r < left && c + k < a.C) *reinterpret_cast<uint4*>(to + c + k) = make_uint4(p0, p1, p2, p3);
+                    for (int k = 0; k < 16; k += 8) {
+                        const uint32_t p0 = pack<BF16>(pair(v[k], v[k + 1])), p1 = pack<BF16>(pair(v[k + 2], v[k + 3]));
+                        const uint32_t p2 = pack<BF16>(pair(v[k + 4], v[k + 5])), p3 = pack<BF16>(pair(v[k + 6], v[k + 7]));
+                        if (left >= kTileRows) store_shared(stage + (c >> 6) * kBlockBytes + swizzled(c >> 6 < a.full ? 64 : a.tail, r, (c & 63) / 8 + k / 8), p0, p1, p2, p3);
+                        else if (r < left && c + k < a.C) *reinterpret_cast<uint4*>(to + c + k) = make_uint4(p0, p1, p2, p3);
+                    }
                 }
             }
             tmem_fence_before();
@@ -919,6 +919,19 @@ long long row_tiles(const RowSegments& s, int NT) {
     return ((long long)s.B * s.N + kTileRows * NT - 1) / (kTileRows * NT) + (long long)s.B * s.E;
 }
 
+template <int MODE, int HC, int NT, int TO, bool SHARES>
+int launch_rows_kernel(emc2_bridge* h, const FfnCall& f, const RowArgs& a, const Maps& m, int ctas, size_t shared, cudaStream_t st) {
+    const int kind = MODE == FORWARD ? K_FFN : K_FFN_GRAD_X;
+    const bool bf16 = f.type == EMC2_BF16;
+    if (f.act == EMC2_ACT_SILU)
+        return bf16 ? launch_ffn(h, kind, ffn_rows_kernel<MODE, HC, NT, TO, EMC2_ACT_SILU, true, SHARES>, a, m, ctas, kFfnThreads, shared, st)
+                    : launch_ffn(h, kind, ffn_rows_kernel<MODE, HC, NT, TO, EMC2_ACT_SILU, false, SHARES>, a, m, ctas, kFfnThreads, shared, st);
+    if constexpr (TO == TO_TMEM)
+        return bf16 ? launch_ffn(h, kind, ffn_rows_kernel<MODE, HC, NT, TO, EMC2_ACT_GELU, true, SHARES>, a, m, ctas, kFfnThreads, shared, st)
+                    : launch_ffn(h, kind, ffn_rows_kernel<MODE, HC, NT, TO, EMC2_ACT_GELU, false, SHARES>, a, m, ctas, kFfnThreads, shared, st);
+    return EMC2_ERR_INTERNAL;
+}
+
 template <int MODE, int HC, int NT, int TO>
 int launch_rows(emc2_bridge* h, const FfnCall& f, cudaStream_t st) {
     RowArgs a;
@@ -959,16 +972,10 @@ int launch_rows(emc2_bridge* h, const FfnCall& f, cudaStream_t st) {
     a.part = a.splits > 1 ? static_cast<float*>(r.slab) : nullptr;
     a.max_tiles = (int)std::min<long long>(tiles, h->num_sms);
     a.tiles = a.part ? reinterpret_cast<int2*>(a.part + (size_t)h->num_sms * kTileRows * f.C) : nullptr;
-    const int ctas = (int)std::min<long long>(tiles * a.splits, h->num_sms), kind = MODE == FORWARD ? K_FFN : K_FFN_GRAD_X;
-    const bool bf16 = f.type == EMC2_BF16;
-    int rc = EMC2_ERR_INTERNAL;
-    if (f.act == EMC2_ACT_SILU)
-        rc = bf16 ? launch_ffn(h, kind, ffn_rows_kernel<MODE, HC, NT, TO, EMC2_ACT_SILU, true>, a, m, ctas, kFfnThreads, shared, st)
-                  : launch_ffn(h, kind, ffn_rows_kernel<MODE, HC, NT, TO, EMC2_ACT_SILU, false>, a, m, ctas, kFfnThreads, shared, st);
-    else if constexpr (TO == TO_TMEM)
-        rc = bf16 ? launch_ffn(h, kind, ffn_rows_kernel<MODE, HC, NT, TO, EMC2_ACT_GELU, true>, a, m, ctas, kFfnThreads, shared, st)
-                  : launch_ffn(h, kind, ffn_rows_kernel<MODE, HC, NT, TO, EMC2_ACT_GELU, false>, a, m, ctas, kFfnThreads, shared, st);
-    if (rc != EMC2_OK || a.splits == 1) return rc;
+    const int ctas = (int)std::min<long long>(tiles * a.splits, h->num_sms);
+    if (a.splits == 1) return launch_rows_kernel<MODE, HC, NT, TO, false>(h, f, a, m, ctas, shared, st);
+    const int rc = launch_rows_kernel<MODE, HC, 1, TO, true>(h, f, a, m, ctas, shared, st);
+    if (rc != EMC2_OK) return rc;
     const JoinArgs join = {a.part, a.tiles, f.out, f.C, a.splits, f.type};
     LaunchScope ls(h, K_FFN_JOIN, st);
     launch_chained(ffn_join_kernel, dim3((unsigned)tiles, (kTileRows * f.C / 4 + 255) / 256), 256, 0, st, join);
