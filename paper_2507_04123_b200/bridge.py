@@ -478,7 +478,8 @@ class Bridge:
 
     # ------------------------------------------------------------------ operators on dispatched rows
     def reserve_rows(self, channels: int, hidden: int = 0) -> None:
-        """emc2_rows_reserve: scratch of the gradient calls below for rows of up to ``channels`` channels."""
+        """emc2_rows_reserve: scratch of the gradient calls below for rows of up to ``channels`` channels (and
+        ``hidden`` hidden units); with ``hidden``, :meth:`expert_ffn` shares out few rows' units with it too."""
         self._raise(self.lib.emc2_rows_reserve(self._h, int(channels), int(hidden)), "emc2_rows_reserve")
 
     def _row_type(self, t: torch.Tensor, name: str) -> int:
