@@ -335,7 +335,8 @@ int emc2_rows_reserve(emc2_bridge_t* bridge, int32_t max_channels, int32_t max_h
  * d_cam mark points without a voxel or camera.  For voxel rows brought back to their points, or learned rows by
  * expert, camera or ring.
  *   d_ids    int32 [n], n <= max_batch * max_points     d_table  type [rows, channels]     d_out  type [n, channels]
- * channels is a multiple of 4 up to 1024.  The product is rounded once.  An id >= rows makes EMC2_ERR_INVALID_ARG
+ * channels is a multiple of 4 up to 1024; n * channels / 4 and rows * channels / 4 are at most 2^32 - 65536.  The product is
+ * rounded once.  An id >= rows makes EMC2_ERR_INVALID_ARG
  * sticky and gives zeros. */
 int emc2_row_lookup(emc2_bridge_t* bridge, int32_t n, int32_t rows, int32_t channels, int32_t type, const int32_t* d_ids,
                     const void* d_table, float scale, void* d_out, void* cuda_stream);

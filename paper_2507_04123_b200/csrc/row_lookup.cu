@@ -625,7 +625,7 @@ extern "C" int emc2_row_lookup_grad(emc2_bridge_t* h, int32_t n, int32_t rows, i
     a.ends = reinterpret_cast<RunEnds*>(base + s.ends);
     a.partial = reinterpret_cast<float4*>(base + s.partial);
     a.parts = ctas;
-    const int grid = ctas + (rows + kLookupThreads - 1) / kLookupThreads;
+    const int grid = ctas + (int)(((long long)rows + kLookupThreads - 1) / kLookupThreads);
     {
         const size_t shared = (size_t)groups * 2 * a.nvec * sizeof(float4) + ((size_t)groups * kRunItems * 2 + 4) * sizeof(uint32_t);
         LaunchScope ls(h, K_LOOKUP_SUM, st);

@@ -98,6 +98,28 @@ def test_lookup_gradient(n, V, C, dtype, pattern):
     br.close()
 
 
+def test_lookup_and_gradient_of_the_largest_table():
+    """2^31 - 1 rows: row numbers, their count of CTAs and the rows' addresses at the end of 32 bits."""
+    n, V, C = 3000, 2 ** 31 - 1, 4
+    g = generator(31)
+    br = handle(1, n)
+    br.reserve_rows(C)
+    ids = torch.randint(0, V, (n,), generator=g, device=DEV, dtype=torch.int32)
+    ids[:3], ids[3:6] = V - 1, torch.tensor([0, -1, V - 2], dtype=torch.int32, device=DEV)
+    dout = torch.randint(1, 4, (n, C), generator=g, device=DEV).to(torch.bfloat16)          # sums that bf16 holds
+    table = torch.full((V, C), float("nan"), dtype=torch.bfloat16, device=DEV)
+    br.row_lookup_grad(ids, dout, V, out=table)
+    named, at = torch.unique(ids[ids >= 0].long(), return_inverse=True)
+    want = torch.zeros((len(named), C), device=DEV).index_add_(0, at, dout[ids >= 0].float())
+    assert torch.equal(table[named].float(), want)
+    rows = br.row_lookup(ids, table)
+    assert torch.equal(rows[ids >= 0].float(), want[at]) and (rows[ids < 0] == 0).all()
+    table[named] = 0
+    assert all(bool((part == 0).all()) for part in table.split(2 ** 26))
+    br.status()
+    br.close()
+
+
 def test_lookup_gradient_against_differences():
     g = generator(5)
     n, V, C = 300, 40, 8
