@@ -120,14 +120,18 @@ struct NormGradArgs {
 
 // The rows are taken expert by expert, an equal run of them per CTA: a CTA meets few experts, and sums the parameters'
 // gradients of each in registers.  Entry i + e of `part` holds those of CTA i and expert e: along the run of all rows
-// either i or e goes up, so no two share an entry.  The two rows and the sums fill the registers, so that few warps have loads
-// in flight, which is what it waits for: 960,000 rows of 64 fp32 channels 135 us, 4.6 TB/s of the rows.
+// either i or e goes up, so no two share an entry.  Rows and sums fill the registers, so
+// that few warps have loads in flight, which is what it waits for: 960,000 rows of 64 fp32 channels 117 us, 5.3 TB/s of the rows.
 template <int K>
 __global__ void __launch_bounds__(kNormThreads, K <= 2 ? 3 : K <= 4 ? 2 : 1) norm_grad_kernel(NormGradArgs a) {
     __shared__ int bounds[kMaxBounds];
     __shared__ int start[kMaxSegments + 1];
     extern __shared__ float4 sums[];             // [warps][2][nvec]
     __shared__ float4 ws[kMaxRowChannels / 4];
+    // A warp's next rows are requested before it works on these, where the registers of two CTAs per SM, or else of one, allow it
+    // (us for 100,000 rows of 256 fp32 channels 57.8, without 68.4; of 1,024 225 and 253; of 512, where it would cost the
+    // second CTA, 142 and 114).
+    constexpr bool kAhead = K != 4;
     load_bounds(a.seg, bounds);
     segment_starts(a.seg, bounds, 1, start);
     // CTA i has rows total * i / ctas .. total * (i + 1) / ctas - 1 of the run of all rows, one at least.
@@ -138,11 +142,14 @@ __global__ void __launch_bounds__(kNormThreads, K <= 2 ? 3 : K <= 4 ? 2 : 1) nor
         a.share[2 * threadIdx.x + 1] = from < to ? (int)((to * ctas - 1) / total) + 1 : 0;
     }
     if ((int)blockIdx.x >= ctas) return;
-    const int lo = (int)((long long)total * blockIdx.x / ctas), hi = (int)((long long)total * (blockIdx.x + 1) / ctas);
+    // Ends of the CTA's run, in shared memory for want of registers.
+    __shared__ int run[2];
+    if (threadIdx.x < 2) run[threadIdx.x] = (int)((long long)total * (blockIdx.x + threadIdx.x) / ctas);
+    __syncthreads();
     const int lanes = 1 << a.log, lane = threadIdx.x & (lanes - 1), warp = threadIdx.x >> 5;
     const int per_warp = 32 >> a.log, sub = (threadIdx.x & 31) >> a.log, step = kNormThreads >> a.log;
-    for (int e = segment_of(start, B * E, lo) / B; e < E && start[e * B] < hi; ++e) {
-        const int from = max(lo, start[e * B]), to = min(hi, start[(e + 1) * B]);
+    for (int e = segment_of(start, B * E, run[0]) / B; e < E && start[e * B] < run[1]; ++e) {
+        const int from = max(run[0], start[e * B]), to = min(run[1], start[(e + 1) * B]);
         if (from >= to) continue;
         float4 dw[K], db[K];
         __syncthreads();                                          // the weights of the expert before are done with
@@ -153,19 +160,34 @@ __global__ void __launch_bounds__(kNormThreads, K <= 2 ? 3 : K <= 4 ? 2 : 1) nor
             dw[i] = db[i] = make_float4(0.f, 0.f, 0.f, 0.f);
         }
         int q = e * B;
-        for (int p0 = from + warp * per_warp; p0 < to; p0 += step) {
-            const int p = p0 + sub;
-            const bool in = p < to;
-            size_t row = 0;
-            if (in) {
+        uint4 next_x[K], next_g[K];
+        float next_m = 0.f, next_r = 0.f;
+        uint32_t next_row = 0;                                    // 2^24 rows at most
+        auto request = [&](int p) {
+            int n = 0;                                            // vectors of the row, none behind the last
+            if (p < to) {
+                n = a.nvec;
                 while (p >= start[q + 1]) ++q;                    // p < start[(e + 1) * B]
                 const int b = q - e * B;
-                row = (size_t)b * a.seg.N + bounds[b * (E + 1) + e] + (p - start[q]);
+                next_row = (uint32_t)(b * a.seg.N + bounds[b * (E + 1) + e] + (p - start[q]));
+                next_m = __ldg(a.mean + next_row);
+                next_r = __ldg(a.rstd + next_row);
             }
-            const float m = in ? __ldg(a.mean + row) : 0.f, r = in ? __ldg(a.rstd + row) : 0.f;
+            request_row<K>(next_x, a.x, (size_t)next_row * a.nvec, lane, a.log, n, a.type_x);
+            request_row<K>(next_g, a.dy, (size_t)next_row * a.nvec, lane, a.log, n, a.type_y);
+        };
+        int p = from + warp * per_warp + sub;                     // the group's; a warp goes on while any of its groups has one
+        if (kAhead) request(p);
+        while (p - sub < to) {
+            if (!kAhead) request(p);
+            const bool in = p < to;
+            const uint32_t row = next_row;
+            const float m = next_m, r = next_r;
             uint4 raw_x[K], raw_g[K];
-            request_row<K>(raw_x, a.x, row * a.nvec, lane, a.log, in ? a.nvec : 0, a.type_x);
-            request_row<K>(raw_g, a.dy, row * a.nvec, lane, a.log, in ? a.nvec : 0, a.type_y);
+#pragma unroll
+            for (int i = 0; i < K; ++i) { raw_x[i] = next_x[i]; raw_g[i] = next_g[i]; }
+            p += step;
+            if (kAhead) request(p);
             float4 x[K], g[K];
 #pragma unroll
             for (int i = 0; i < K; ++i) { x[i] = row_floats(raw_x[i], a.type_x); g[i] = row_floats(raw_g[i], a.type_y); }
@@ -190,7 +212,7 @@ __global__ void __launch_bounds__(kNormThreads, K <= 2 ? 3 : K <= 4 ? 2 : 1) nor
                 if (v >= a.nvec) continue;
                 const float4 o = make_float4(r * (g[i].x - s - x[i].x * t), r * (g[i].y - s - x[i].y * t),
                                              r * (g[i].z - s - x[i].z * t), r * (g[i].w - s - x[i].w * t));
-                store_row4(a.dx, row * a.nvec + v, o, a.type_x);
+                store_row4(a.dx, (size_t)row * a.nvec + v, o, a.type_x);
             }
         }
         // The groups of a warp hold the same columns in the same lanes, then the warps' sums in their order.
