@@ -1067,7 +1067,7 @@ int check_ffn(const emc2_bridge* h, int B, int N, int C, int H, int type, int ac
     if ((type != EMC2_BF16 && type != EMC2_F16) || (act != EMC2_ACT_SILU && act != EMC2_ACT_GELU)) return EMC2_ERR_INVALID_ARG;
     if (!gate || !up || !down || !on_16_bytes(gate) || !on_16_bytes(up) || !on_16_bytes(down) || !on_16_bytes(x)) return EMC2_ERR_INVALID_ARG;
     if (B > 0 && N > 0 && !x) return EMC2_ERR_INVALID_ARG;
-    if (reinterpret_cast<uintptr_t>(offsets) & 3) return EMC2_ERR_INVALID_ARG;
+    if (!on_4_bytes(offsets)) return EMC2_ERR_INVALID_ARG;
     return EMC2_OK;
 }
 

@@ -319,7 +319,7 @@ int check_norm(const emc2_bridge* h, int B, int N, int channels, int type_x, int
     if (channels < 4 || channels > kMaxRowChannels || (channels & 3) || !is_type(type_x) || !is_type(type_y)) return EMC2_ERR_INVALID_ARG;
     if (!weight || !on_16_bytes(weight) || !on_16_bytes(x)) return EMC2_ERR_INVALID_ARG;
     if (B > 0 && N > 0 && !x) return EMC2_ERR_INVALID_ARG;
-    if (reinterpret_cast<uintptr_t>(offsets) & 3) return EMC2_ERR_INVALID_ARG;
+    if (!on_4_bytes(offsets)) return EMC2_ERR_INVALID_ARG;
     return EMC2_OK;
 }
 
@@ -338,7 +338,7 @@ extern "C" int emc2_expert_norm(emc2_bridge_t* h, int32_t B, int32_t N, int32_t 
                                 void* d_y, float* d_mean, float* d_rstd, void* cuda_stream) {
     const int rc = check_norm(h, B, N, channels, type_x, type_y, d_x, d_offsets, d_weight);
     if (rc != EMC2_OK) return rc;
-    if (!on_16_bytes(d_bias) || !on_16_bytes(d_y) || !(eps >= 0.0f)) return EMC2_ERR_INVALID_ARG;
+    if (!on_16_bytes(d_bias) || !on_16_bytes(d_y) || !on_4_bytes(d_mean) || !on_4_bytes(d_rstd) || !(eps >= 0.0f)) return EMC2_ERR_INVALID_ARG;
     if (B == 0 || N == 0) return EMC2_OK;
     if (!d_y || d_y == d_x) return EMC2_ERR_INVALID_ARG;
     RowsDevice device(h->cfg.device);
@@ -366,7 +366,9 @@ extern "C" int emc2_expert_norm_grad(emc2_bridge_t* h, int32_t B, int32_t N, int
                                      float* d_grad_bias, void* cuda_stream) {
     const int rc = check_norm(h, B, N, channels, type_x, type_y, d_x, d_offsets, d_weight);
     if (rc != EMC2_OK) return rc;
-    if (!d_grad_weight || !on_16_bytes(d_grad_y) || !on_16_bytes(d_grad_x)) return EMC2_ERR_INVALID_ARG;
+    if (!d_grad_weight || !on_16_bytes(d_grad_y) || !on_16_bytes(d_grad_x) || !on_4_bytes(d_mean) || !on_4_bytes(d_rstd) ||
+        !on_4_bytes(d_grad_weight) || !on_4_bytes(d_grad_bias))
+        return EMC2_ERR_INVALID_ARG;
     const bool empty = B == 0 || N == 0;
     if (!empty && (!d_mean || !d_rstd || !d_grad_y || !d_grad_x || d_grad_x == d_x || d_grad_x == d_grad_y)) return EMC2_ERR_INVALID_ARG;
     if (!h->rows_scratch.slab || channels > h->rows_scratch.max_channels) return EMC2_ERR_TOO_LARGE;

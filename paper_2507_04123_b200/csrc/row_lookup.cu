@@ -508,7 +508,7 @@ int check_lookup(const emc2_bridge* h, int n, int rows, int channels, int type, 
     // Vectors of the rows are counted in 32 bits.
     if ((uint64_t)std::max(n, rows) * (uint64_t)(channels / 4) > 0xFFFF0000ull) return EMC2_ERR_INVALID_ARG;
     if (n > 0 && !ids) return EMC2_ERR_INVALID_ARG;
-    if (reinterpret_cast<uintptr_t>(ids) & 3) return EMC2_ERR_INVALID_ARG;
+    if (!on_4_bytes(ids)) return EMC2_ERR_INVALID_ARG;
     return EMC2_OK;
 }
 

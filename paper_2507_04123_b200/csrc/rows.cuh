@@ -16,6 +16,7 @@ constexpr int kMaxBounds = EMC2_MAX_BATCH * (EMC2_MAX_EXPERTS + 1);
 inline int type_bytes(int type) { return type == EMC2_F32 ? 4 : 2; }
 inline bool is_type(int type) { return type >= EMC2_F32 && type <= EMC2_F16; }
 inline bool on_16_bytes(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+inline bool on_4_bytes(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3) == 0; }
 
 // Makes the handle's device current for a call.
 struct RowsDevice {

@@ -301,14 +301,15 @@ def test_calls_that_are_refused():
     good = (1, 4, 8, 0, 1, p, None, p, None, 1e-5, q, None, None)
     assert lib.emc2_expert_norm(h, *good, None) == 0
     for i, v in ((0, 3), (0, -1), (1, 65), (1, -1), (2, 10), (2, 1028), (3, 3), (4, -1), (5, None), (5, p + 4), (6, p + 2), (7, None), (7, p + 4), (8, p + 4), (9, -1.0),
-                 (9, float("nan")), (10, None), (10, p), (10, q + 8)):
+                 (9, float("nan")), (10, None), (10, p), (10, q + 8), (11, q + 2), (12, q + 1)):
         bad = list(good)
         bad[i] = v
         assert lib.emc2_expert_norm(h, *bad, None) == INVALID, (i, v)
     # B, N, channels, types, x, offsets, weight, mean, rstd, grad_y, grad_x, grad_weight, grad_bias
     good = (1, 4, 8, 0, 1, p, None, p, p, p, p, q, q, None)
     assert lib.emc2_expert_norm_grad(h, *good, None) == 0
-    for i, v in ((0, 3), (2, 2), (3, 7), (5, None), (7, None), (8, None), (9, None), (10, None), (10, p + 8), (11, None), (11, p), (12, None)):
+    for i, v in ((0, 3), (2, 2), (3, 7), (5, None), (7, None), (8, None), (9, None), (10, None), (10, p + 8), (11, None), (11, p), (12, None), (8, p + 2), (9, p + 1), (12, q + 2),
+                 (13, q + 2)):
         bad = list(good)
         bad[i] = v
         assert lib.emc2_expert_norm_grad(h, *bad, None) == INVALID, (i, v)
