@@ -429,7 +429,8 @@ __global__ void __launch_bounds__(kFfnThreads, 1) ffn_rows_kernel(const RowArgs 
         // chunk of it; if it has a single one, the first warp takes all.
         const int mine = warp == kFirstWarp ? 0 : 1;
         const uint32_t lead = elected(), kind_gu = product_kind(2 * HC, BF16, false, false), kind_dh = product_kind(HC, BF16, false, true);
-        const int steps = 4 * a.full, tail_steps = a.tail / 16;
+        // Wd's stage ends with the channels, where the other tiles' last block is a whole one (see `tail`).
+        const int steps = 4 * a.full, tail_steps = a.tail / 16, dh_steps = a.c16 / 16 - tail_steps;
         const uint64_t tail_x0 = operand(base + a.full * kBlockBytes, a.tail * 2, 0);
         const uint64_t tail_w0 = operand(base + a.off_g + a.full * (2 * HC * 128), MODE == FORWARD ? a.tail * 2 : 128, 0);
         const uint64_t x0 = operand(base, 128, 0), w0 = operand(base + a.off_g, 128, 0), wd0 = operand(base + a.off_d, HC * 2, 0);
@@ -452,8 +453,8 @@ __global__ void __launch_bounds__(kFfnThreads, 1) ffn_rows_kernel(const RowArgs 
                 product_blocks(lead, acc, xt, 0, operand_at(tail_w0, g.at * a.g_bytes), 0, tail_steps, kind_gu, steps > 0);
                 if (MODE == GRAD_X) {
                     const uint64_t wd = operand_at(wd0, d.at * a.d_bytes);
-                    product_blocks_mn(lead, dh, operand_at(xa, a.tile_bytes), kBlockBytes, wd, 32 * HC, steps, kind_dh);
-                    product_blocks_mn(lead, dh, operand_at(xt, a.tile_bytes), 0, operand_at(wd, steps * 32 * HC), 32 * HC, tail_steps, kind_dh, steps > 0);
+                    product_blocks_mn(lead, dh, operand_at(xa, a.tile_bytes), kBlockBytes, wd, 32 * HC, dh_steps, kind_dh);
+                    product_blocks_mn(lead, dh, operand_at(xt, a.tile_bytes), 0, operand_at(wd, dh_steps * 32 * HC), 32 * HC, tail_steps, kind_dh, dh_steps > 0);
                 }
                 products_done(lead, acc_full(slot));
                 // The gradients' second products take Wg and Wu again: their warp gives them back.

@@ -8,7 +8,8 @@ pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
 
 SHAPES = [(1, 1, 8, 8, 1), (1, 128, 64, 64, 1), (1, 129, 64, 256, 4), (3, 300, 80, 320, 4), (2, 500, 128, 96, 3), (2, 260, 136, 40, 2),
-          (1, 400, 256, 1024, 5), (32, 40, 24, 72, 16), (1, 3000, 72, 200, 2), (2, 700, 200, 136, 3), (1, 513, 192, 64, 1), (1, 37, 16, 2048, 1)]
+          (1, 400, 256, 1024, 5), (32, 40, 24, 72, 16), (1, 3000, 72, 200, 2), (2, 700, 200, 136, 3), (1, 513, 192, 64, 1), (1, 37, 16, 2048, 1),
+          (1, 300, 48, 128, 2), (2, 150, 40, 384, 3), (1, 200, 104, 64, 1), (1, 300, 176, 72, 2), (1, 140, 240, 96, 1), (1, 60, 112, 2048, 1)]
 
 
 def inputs(B, N, C, H, E, dtype, seed=0, rows=lambda offsets, N: offsets):
