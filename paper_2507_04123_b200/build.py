@@ -11,7 +11,7 @@ CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libemc2_bridge.so")
 SOURCES = ["bridge.cu", "voxelize.cu", "project_gather.cu", "route_dispatch.cu", "voxel_image.cu", "occlusion.cu", "rulebook.cu", "dedup_arms.cu", "row_lookup.cu",
            "expert_norm.cu", "expert_ffn.cu"]
-HEADERS = [os.path.join(CSRC, "bridge_internal.cuh"), os.path.join(CSRC, "rules.cuh"), os.path.join(CSRC, "rows.cuh"), os.path.join(CSRC, "umma.cuh"),
+HEADERS = [os.path.join(CSRC, "bridge_internal.cuh"), os.path.join(CSRC, "rules.cuh"), os.path.join(CSRC, "rows.cuh"), os.path.join(CSRC, "row_sizes.cuh"), os.path.join(CSRC, "umma.cuh"),
             os.path.join(ROOT, "include", "emc2_bridge.h")]
 
 

@@ -15,9 +15,7 @@
 namespace emc2 {
 namespace {
 
-constexpr int kLookupThreads = 256;
 constexpr int kLookupUnroll = 4;
-constexpr int kRunItems = 16;                 // sorted places per group of lanes, at least
 
 __device__ __forceinline__ float4 scaled(float4 f, float s) {
     return make_float4(f.x * s, f.y * s, f.z * s, f.w * s);
@@ -80,8 +78,7 @@ __global__ void __launch_bounds__(kLookupThreads) lookup_kernel(LookupArgs a) {
 // the counts, 12 for their sums, 32 for the moves, of 15 MB).
 constexpr int kSortThreads = 256, kSortWarps = kSortThreads / 32;
 constexpr int kSortRounds = 8;                         // of 32 items per warp
-constexpr int kSortItems = kSortThreads * kSortRounds; // of a tile
-constexpr int kMaxDigits = 1024;
+static_assert(kSortItems == kSortThreads * kSortRounds, "a tile is a CTA's");
 
 struct SortArgs {
     const int32_t* ids;         // of the first pass, else null
@@ -306,14 +303,6 @@ __device__ __forceinline__ void zero_rows(const uint32_t* keys, int n, int rows,
             for (int v = lane; v < nvec; v += 32) store_row4(out, (size_t)(r0 + k) * nvec + v, make_float4(0.f, 0.f, 0.f, 0.f), type);
 }
 
-// What a part of the sorted list leaves of the runs that its ends divide.
-struct RunEnds {
-    int head;                   // id of a run that begins before the part, or -1
-    int through;                // that run also goes on behind the part
-    int tail;                   // id of a run that begins in the part and goes on behind it, or -1
-    int pad;
-};
-
 struct SumArgs {
     const uint32_t* keys;
     const uint32_t* vals;
@@ -512,45 +501,10 @@ int check_lookup(const emc2_bridge* h, int n, int rows, int channels, int type, 
     return EMC2_OK;
 }
 
-// Places per group and CTAs of lookup_sum_kernel: as many places as make about four CTAs per SM, so that their ends do not
-// weigh.
-int sum_items(const emc2_bridge* h, long long n, int groups, int* ctas) {
-    const long long most = (long long)groups * 4 * h->num_sms;
-    const long long items = std::max<long long>(1, (n + most * kRunItems - 1) / (most * kRunItems)) * kRunItems;
-    *ctas = (int)((n + items * groups - 1) / (items * groups));
-    return (int)items;
-}
-
-struct LookupScratch {
-    size_t keys[2], vals[2], counts, row_tot, ends, partial, bytes;
-};
-
-// Scratch of the gradient for n ids and rows of nvec vectors, as offsets.
-LookupScratch lookup_scratch(long long n, int ctas, int nvec) {
-    LookupScratch s;
-    size_t off = 0;
-    auto take = [&](size_t bytes) { const size_t o = off; off += (bytes + 255) & ~(size_t)255; return o; };
-    for (int k = 0; k < 2; ++k) { s.keys[k] = take((size_t)n * 4); s.vals[k] = take((size_t)n * 4); }
-    s.counts = take((size_t)kMaxDigits * ((n + kSortItems - 1) / kSortItems + 3) * 4);
-    s.row_tot = take(kMaxDigits * 4);
-    s.ends = take((size_t)ctas * sizeof(RunEnds));
-    s.partial = take((size_t)ctas * 2 * nvec * sizeof(float4));
-    s.bytes = off;
-    return s;
-}
-
 }  // namespace
 
 size_t lookup_scratch_bytes(const emc2_bridge* h, int max_channels) {
-    const long long n = (long long)h->cfg.max_batch * h->cfg.max_points;
-    size_t most = 0;
-    // Narrower rows have more groups per CTA, so fewer CTAs: which width needs most depends on n.
-    for (int c = 4; c <= max_channels; c += 4) {
-        int ctas;
-        sum_items(h, n, kLookupThreads >> row_split(c / 4, 3).log, &ctas);
-        most = std::max(most, lookup_scratch(n, ctas, c / 4).bytes);
-    }
-    return most;
+    return lookup_scratch_most(h->num_sms, (long long)h->cfg.max_batch * h->cfg.max_points, max_channels);
 }
 
 }  // namespace emc2
@@ -598,10 +552,11 @@ extern "C" int emc2_row_lookup_grad(emc2_bridge_t* h, int32_t n, int32_t rows, i
     SumArgs a;
     a.nvec = channels / 4;
     const RowSplit split = row_split(a.nvec, 3);
-    const int groups = kLookupThreads >> split.log;
-    int ctas;
-    a.items = sum_items(h, n, groups, &ctas);
+    const LookupParts parts = lookup_parts(h->num_sms, n, a.nvec);
+    const int groups = parts.groups, ctas = parts.ctas;
+    a.items = parts.items;
     const LookupScratch s = lookup_scratch(n, ctas, a.nvec);
+    if (s.bytes > h->rows_scratch.bytes) return EMC2_ERR_TOO_LARGE;
     char* base = static_cast<char*>(h->rows_scratch.slab);
     uint32_t* keys[2] = {reinterpret_cast<uint32_t*>(base + s.keys[0]), reinterpret_cast<uint32_t*>(base + s.keys[1])};
     uint32_t* vals[2] = {reinterpret_cast<uint32_t*>(base + s.vals[0]), reinterpret_cast<uint32_t*>(base + s.vals[1])};

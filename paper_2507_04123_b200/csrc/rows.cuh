@@ -5,6 +5,7 @@
 #include <cuda_fp16.h>
 
 #include "bridge_internal.cuh"
+#include "row_sizes.cuh"
 
 namespace emc2 {
 
@@ -40,21 +41,6 @@ struct RowSegments {
 
 inline RowSegments row_segments(const emc2_bridge* h, int B, int N, const int32_t* offsets) {
     return {offsets, B, N, offsets ? h->cfg.num_experts : 1, h->d_status};
-}
-
-// A row of nvec vectors of four elements is spread over 1 << log lanes that hold up to `per` vectors each (vector
-// lane + i * lanes): the split that leaves fewest places empty with at most `most` vectors per lane (or what 32 lanes need),
-// and of those the one with fewest lanes, since the more a lane loads at once, the more is in flight.
-struct RowSplit {
-    int log, per;
-};
-inline RowSplit row_split(int nvec, int most) {
-    RowSplit best = {5, (nvec + 31) / 32};
-    for (int log = 4; log >= 0; --log) {
-        const int lanes = 1 << log, per = (nvec + lanes - 1) / lanes;
-        if (per <= most && per * lanes <= best.per << best.log) best = {log, per};
-    }
-    return best;
 }
 
 #ifdef __CUDACC__
