@@ -89,22 +89,21 @@ __device__ __forceinline__ void next_item(const RowSegments& s, ItemWalk& w, int
 }
 
 // ---------------------------------------------------------------- activations, two values at a time
-// The special-function unit is what the activation waits for (16 results a clock and SM), so exponentials, reciprocals and
-// hyperbolic tangents are what is saved.
+// The special-function unit is what the activation waits for (16 results a clock and SM), so exponentials and reciprocals are
+// what is saved.
 
-// 1 / (1 + exp(-g)).  For bf16 rows by one hyperbolic tangent, (1 + tanh(g / 2)) / 2, which is off by 2^-12 at most (tanh.approx
-// is by 2^-11 of itself): an eighth of the half step that rounding a value near 1 to bf16 costs afterwards.  For fp16 rows that
-// would be a whole half step: there by exponentials, off by a few units of fp32, and one reciprocal for two.  Their
-// argument ends at 2^60: below -41 the result is 2^-60 instead of less.
-template <bool BF16>
-__device__ __forceinline__ uint64_t sigmoid2(uint64_t g) {
-    if (BF16) {
-        const float2 x = unpair(mul2(g, pair(0.5f, 0.5f)));
-        return fma2(pair(fast_tanh(x.x), fast_tanh(x.y)), pair(0.5f, 0.5f), pair(0.5f, 0.5f));
-    }
-    const float2 x = unpair(mul2(g, pair(-1.44269504f, -1.44269504f)));
-    const float2 d = unpair(add2(pair(fast_exp2(fminf(x.x, 60.0f)), fast_exp2(fminf(x.y, 60.0f))), pair(1.0f, 1.0f)));
-    return reciprocals(d.x, d.y);
+// g / (1 + exp(-g)) and the sigmoid 1 / (1 + exp(-g)), by exponentials and one reciprocal for two (a reciprocal each: 260 us
+// instead of 220 for 1.2 million rows of 80 channels, 320 units).  Both are right to a few units of fp32 relative to themselves,
+// which the roundings behind them need: for negative g they are small, and a form that is right to 2^-12 of 1, like
+// (1 + tanh.approx(g / 2)) / 2 (183 us), has none of their bits left at g = -9.  Gates below -41.5 are taken as -41.5, where the result
+// is above -2^-54: the denominators' product then stays below 2^120.  A NaN stays one.
+__device__ __forceinline__ uint64_t silu2(uint64_t g, uint64_t& sigmoid) {
+    const float2 x = unpair(g);
+    const uint64_t c = pair(max_nan(x.x, -41.5f), max_nan(x.y, -41.5f));
+    const float2 e = unpair(mul2(c, pair(-1.44269504f, -1.44269504f)));
+    const float2 d = unpair(add2(pair(fast_exp2(e.x), fast_exp2(e.y)), pair(1.0f, 1.0f)));
+    sigmoid = reciprocals(d.x, d.y);
+    return mul2(c, sigmoid);
 }
 
 // The normal distribution at g and its density times sqrt(2 pi): Abramowitz and Stegun 7.1.26 for the error function at
@@ -124,16 +123,16 @@ __device__ __forceinline__ uint64_t normal2(uint64_t g, uint64_t& density) {
     return pair(x.x < 0.0f ? tail.x : 1.0f - tail.x, x.y < 0.0f ? tail.y : 1.0f - tail.y);
 }
 
-template <int ACT, bool BF16>
+template <int ACT>
 __device__ __forceinline__ uint64_t activation2(uint64_t g) {
-    uint64_t density;
-    return mul2(g, ACT == EMC2_ACT_SILU ? sigmoid2<BF16>(g) : normal2(g, density));
+    uint64_t beside;
+    return ACT == EMC2_ACT_SILU ? silu2(g, beside) : mul2(g, normal2(g, beside));
 }
-template <int ACT, bool BF16>
+template <int ACT>
 __device__ __forceinline__ void activation_grad2(uint64_t g, uint64_t& a, uint64_t& da) {
     if (ACT == EMC2_ACT_SILU) {
-        const uint64_t s = sigmoid2<BF16>(g);
-        a = mul2(g, s);
+        uint64_t s;
+        a = silu2(g, s);
         da = fma2(a, fma2(s, pair(-1.0f, -1.0f), pair(1.0f, 1.0f)), s);        // s + a (1 - s)
     } else {
         uint64_t density;
@@ -178,11 +177,11 @@ __device__ __forceinline__ void hidden8(const uint32_t (&g)[W], const uint32_t (
         if (TO != TO_TMEM) asm volatile("" : "+r"(first));           // and pair by pair here, see hidden_half
         const uint64_t gg = pair(first, g[j + 1]), uu = pair(u[j], u[j + 1]);
         if (MODE == FORWARD) {
-            p[i] = pack<BF16>(mul2(activation2<ACT, BF16>(gg), uu));
+            p[i] = pack<BF16>(mul2(activation2<ACT>(gg), uu));
         } else {
             const uint64_t dd = pair(dh[j], dh[j + 1]);
             uint64_t a, da;
-            activation_grad2<ACT, BF16>(gg, a, da);
+            activation_grad2<ACT>(gg, a, da);
             p[i] = pack<BF16>(mul2(mul2(dd, uu), da));
             q[i] = pack<BF16>(mul2(dd, a));
             if (TO == TO_SHARED_WITH_H) t[i] = pack<BF16>(mul2(a, uu));
@@ -266,9 +265,10 @@ struct Maps {
     CUtensorMap x_tail, dy_tail, gate_tail, up_tail, out_tail;              // of the last block of columns, where it is narrower
 };
 
-// 1.2 million rows of 80 bf16 channels, 320 units, SiLU: 182 us, 1.0 PFLOP/s in products of N = 128 and 80, whose own times at
-// those widths are half of it; half of the special-function unit's rate goes to the activation.  dx of 480,000 fp16 rows of 64
-// channels, 256 units, GELU: 162 us; of 95,000 bf16 rows of 256, 1,024 units, SiLU: 327 us, 0.76 PFLOP/s.
+// 1.2 million rows of 80 bf16 channels, 320 units, SiLU: 220 us, 0.84 PFLOP/s in products of N = 128 and 80.  What bounds it is the
+// special-function unit: three results for two activations are 126 us of its rate, and each more or fewer was measured at 40 us.
+// dx of 480,000 fp16 rows of 64 channels, 256 units, GELU: 162 us; of 95,000 bf16 rows of 256, 1,024 units, SiLU: 327 us, 0.76
+// PFLOP/s.
 template <int MODE, int HC, int NT, int TO, int ACT, bool BF16, bool SHARES>
 __global__ void __launch_bounds__(kFfnThreads, 1) ffn_rows_kernel(const RowArgs a, const __grid_constant__ Maps maps) {
     // TMEM: the output of NT tiles, two accumulators of g and u, for dx two of dh, and the hidden values of two units unless

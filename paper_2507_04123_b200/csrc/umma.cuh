@@ -206,9 +206,10 @@ __device__ __forceinline__ float fast_exp2(float x) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
     return r;
 }
-__device__ __forceinline__ float fast_tanh(float x) {
+// The larger of both; NaN if one is.
+__device__ __forceinline__ float max_nan(float a, float b) {
     float r;
-    asm("tanh.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
     return r;
 }
 // Both reciprocals from one: a and b from 1 to 2^60.
