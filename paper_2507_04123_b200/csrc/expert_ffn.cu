@@ -965,7 +965,7 @@ int launch_rows(emc2_bridge* h, const FfnCall& f, cudaStream_t st) {
     a.off_d = a.off_g + a.gn * a.g_bytes;
     a.off_h = a.off_d + a.dn * a.d_bytes;
     Maps m;
-    if (!make_maps(f, HC, a.tail, &m)) return EMC2_ERR_CUDA;
+    if (!make_maps(f, HC, a.tail, &m)) return check_cuda(h, cudaErrorInvalidValue);
     const size_t shared = std::max(room(), (size_t)(kMaxBounds + kMaxSegments + 1) * 4 + 1024);
     // Few rows: shares of their hidden units, of four chunks at least, keep the other SMs busy, if there is scratch for what
     // they leave and more than 16 chunks.  us in one piece, and in shares with their join: 64 rows of 64 channels, 4,096 units
@@ -1024,7 +1024,7 @@ int launch_slices(emc2_bridge* h, const FfnCall& f, WeightArgs& a, cudaStream_t 
     a.part = reinterpret_cast<float*>(a.share + kShareInts);
     a.ranges = weight_ranges(h, a.slices, row_tiles(f.seg, 1));
     Maps m;
-    if (!make_maps(f, HC, 0, &m)) return EMC2_ERR_CUDA;
+    if (!make_maps(f, HC, 0, &m)) return check_cuda(h, cudaErrorInvalidValue);
     const int ctas = std::min(a.ranges * a.slices, h->num_sms);
     const bool bf16 = f.type == EMC2_BF16;
     if (f.act == EMC2_ACT_SILU)

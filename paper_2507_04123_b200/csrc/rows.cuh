@@ -19,12 +19,13 @@ inline bool is_type(int type) { return type >= EMC2_F32 && type <= EMC2_F16; }
 inline bool on_16_bytes(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 inline bool on_4_bytes(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3) == 0; }
 
-// Makes the handle's device current for a call.
+// Makes the handle's device current for a call.  It is set where it is current already too: a host thread that has made no CUDA
+// call yet has the device's number but not its context, which the encoding of a tensor map needs.
 struct RowsDevice {
     int prev = -1;
     bool ok = true;
     explicit RowsDevice(int dev) {
-        ok = cudaGetDevice(&prev) == cudaSuccess && (prev == dev || cudaSetDevice(dev) == cudaSuccess);
+        ok = cudaGetDevice(&prev) == cudaSuccess && cudaSetDevice(dev) == cudaSuccess;
         if (prev == dev) prev = -1;
     }
     ~RowsDevice() {
