@@ -32,6 +32,7 @@ constexpr int kTmemColumns = 512;
 constexpr int kMaxFfnChannels = 256, kMaxFfnHidden = 8192;
 constexpr int kMaxStages = 4;
 constexpr size_t kMaxShared = 232448 - 1024;     // what a CTA can have, less the kernels' static part
+constexpr size_t kMaxWeightShared = kMaxShared - 4096;                     // ffn_weights_kernel's tables of the segments are static
 
 enum { FORWARD = 0, GRAD_X = 1 };
 // Where the hidden values go: to TMEM, to shared memory, or there with h beside dg and du.
@@ -912,8 +913,8 @@ bool make_maps(const FfnCall& f, int hc, int tail, Maps* m) {
 }
 
 template <typename F, typename A>
-int launch_ffn(emc2_bridge* h, int kind, F kernel, const A& a, const Maps& m, int ctas, int threads, size_t shared, cudaStream_t st) {
-    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)shared);
+int launch_ffn(emc2_bridge* h, int kind, F kernel, const A& a, const Maps& m, int ctas, int threads, size_t shared, size_t most, cudaStream_t st) {
+    const cudaError_t e = allow_shared(kernel, most);
     if (e != cudaSuccess) return check_cuda(h, e);
     LaunchScope ls(h, kind, st);
     kernel<<<ctas, threads, shared, st>>>(a, m);
@@ -930,11 +931,11 @@ int launch_rows_kernel(emc2_bridge* h, const FfnCall& f, const RowArgs& a, const
     const int kind = MODE == FORWARD ? K_FFN : K_FFN_GRAD_X;
     const bool bf16 = f.type == EMC2_BF16;
     if (f.act == EMC2_ACT_SILU)
-        return bf16 ? launch_ffn(h, kind, ffn_rows_kernel<MODE, HC, NT, TO, EMC2_ACT_SILU, true, SHARES>, a, m, ctas, kFfnThreads, shared, st)
-                    : launch_ffn(h, kind, ffn_rows_kernel<MODE, HC, NT, TO, EMC2_ACT_SILU, false, SHARES>, a, m, ctas, kFfnThreads, shared, st);
+        return bf16 ? launch_ffn(h, kind, ffn_rows_kernel<MODE, HC, NT, TO, EMC2_ACT_SILU, true, SHARES>, a, m, ctas, kFfnThreads, shared, kMaxShared, st)
+                    : launch_ffn(h, kind, ffn_rows_kernel<MODE, HC, NT, TO, EMC2_ACT_SILU, false, SHARES>, a, m, ctas, kFfnThreads, shared, kMaxShared, st);
     if constexpr (TO == TO_TMEM)
-        return bf16 ? launch_ffn(h, kind, ffn_rows_kernel<MODE, HC, NT, TO, EMC2_ACT_GELU, true, SHARES>, a, m, ctas, kFfnThreads, shared, st)
-                    : launch_ffn(h, kind, ffn_rows_kernel<MODE, HC, NT, TO, EMC2_ACT_GELU, false, SHARES>, a, m, ctas, kFfnThreads, shared, st);
+        return bf16 ? launch_ffn(h, kind, ffn_rows_kernel<MODE, HC, NT, TO, EMC2_ACT_GELU, true, SHARES>, a, m, ctas, kFfnThreads, shared, kMaxShared, st)
+                    : launch_ffn(h, kind, ffn_rows_kernel<MODE, HC, NT, TO, EMC2_ACT_GELU, false, SHARES>, a, m, ctas, kFfnThreads, shared, kMaxShared, st);
     return EMC2_ERR_INTERNAL;
 }
 
@@ -1007,7 +1008,7 @@ size_t plan_weights(WeightArgs& a, const FfnCall& f) {
     a.w_bytes = a.blocks * 2 * HC * 128 + a.c16 * HC * 2;
     a.h_bytes = 3 * kTileRows * HC * 2;
     a.xn = 1; a.hn = 1;
-    constexpr size_t most = kMaxShared - 4096;                             // the tables of the segments are static here
+    constexpr size_t most = kMaxWeightShared;
     auto room = [&] { return (size_t)a.xn * a.x_bytes + std::max<size_t>(a.w_bytes + (size_t)a.hn * a.h_bytes, kBlockBytes) + 1024; };
     if (room() + a.x_bytes <= most) ++a.xn;
     if (room() + a.h_bytes <= most) ++a.hn;
@@ -1028,10 +1029,10 @@ int launch_slices(emc2_bridge* h, const FfnCall& f, WeightArgs& a, cudaStream_t 
     const int ctas = std::min(a.ranges * a.slices, h->num_sms);
     const bool bf16 = f.type == EMC2_BF16;
     if (f.act == EMC2_ACT_SILU)
-        return bf16 ? launch_ffn(h, K_FFN_GRAD_W, ffn_weights_kernel<HC, EMC2_ACT_SILU, true>, a, m, ctas, kFfnThreads, shared, st)
-                    : launch_ffn(h, K_FFN_GRAD_W, ffn_weights_kernel<HC, EMC2_ACT_SILU, false>, a, m, ctas, kFfnThreads, shared, st);
-    return bf16 ? launch_ffn(h, K_FFN_GRAD_W, ffn_weights_kernel<HC, EMC2_ACT_GELU, true>, a, m, ctas, kFfnThreads, shared, st)
-                : launch_ffn(h, K_FFN_GRAD_W, ffn_weights_kernel<HC, EMC2_ACT_GELU, false>, a, m, ctas, kFfnThreads, shared, st);
+        return bf16 ? launch_ffn(h, K_FFN_GRAD_W, ffn_weights_kernel<HC, EMC2_ACT_SILU, true>, a, m, ctas, kFfnThreads, shared, kMaxWeightShared, st)
+                    : launch_ffn(h, K_FFN_GRAD_W, ffn_weights_kernel<HC, EMC2_ACT_SILU, false>, a, m, ctas, kFfnThreads, shared, kMaxWeightShared, st);
+    return bf16 ? launch_ffn(h, K_FFN_GRAD_W, ffn_weights_kernel<HC, EMC2_ACT_GELU, true>, a, m, ctas, kFfnThreads, shared, kMaxWeightShared, st)
+                : launch_ffn(h, K_FFN_GRAD_W, ffn_weights_kernel<HC, EMC2_ACT_GELU, false>, a, m, ctas, kFfnThreads, shared, kMaxWeightShared, st);
 }
 
 // Slices of 64 hidden units where two stages of tiles fit beside them (up to 96 channels): half the products, which below

@@ -283,29 +283,35 @@ __global__ void __launch_bounds__(kNormSumThreads) norm_sum_kernel(NormSumArgs a
 }
 
 template <template <int> class F, typename... A>
-void by_vectors(int per, const A&... args) {
+cudaError_t by_vectors(int per, const A&... args) {
     switch (per) {
-        case 1: F<1>::go(args...); break;
-        case 2: F<2>::go(args...); break;
-        case 3: F<3>::go(args...); break;
-        case 4: F<4>::go(args...); break;
-        case 5: F<5>::go(args...); break;
-        case 6: F<6>::go(args...); break;
-        case 7: F<7>::go(args...); break;
-        default: F<8>::go(args...); break;
+        case 1: return F<1>::go(args...);
+        case 2: return F<2>::go(args...);
+        case 3: return F<3>::go(args...);
+        case 4: return F<4>::go(args...);
+        case 5: return F<5>::go(args...);
+        case 6: return F<6>::go(args...);
+        case 7: return F<7>::go(args...);
+        default: return F<8>::go(args...);
     }
 }
 
 template <int K>
 struct Norm {
-    static void go(const NormArgs& a, int ctas, size_t shared, cudaStream_t st) { norm_kernel<K><<<ctas, kNormThreads, shared, st>>>(a); }
+    static cudaError_t go(const NormArgs& a, int ctas, size_t shared, cudaStream_t st) {
+        norm_kernel<K><<<ctas, kNormThreads, shared, st>>>(a);
+        return cudaSuccess;
+    }
 };
 template <int K>
 struct NormGrad {
-    static void go(const NormGradArgs& a, int ctas, size_t shared, cudaStream_t st) {
-        if (shared > 24 * 1024)
-            cudaFuncSetAttribute(norm_grad_kernel<K>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)shared);
+    static cudaError_t go(const NormGradArgs& a, int ctas, size_t shared, cudaStream_t st) {
+        if (shared > 24 * 1024) {                // the sums of eight warps, two of up to 32 * K vectors each
+            const cudaError_t e = allow_shared(norm_grad_kernel<K>, (size_t)(kNormThreads / 32) * 2 * 32 * K * sizeof(float4));
+            if (e != cudaSuccess) return e;
+        }
         norm_grad_kernel<K><<<ctas, kNormThreads, shared, st>>>(a);
+        return cudaSuccess;
     }
 };
 
@@ -356,8 +362,8 @@ extern "C" int emc2_expert_norm(emc2_bridge_t* h, int32_t B, int32_t N, int32_t 
     const long long rows = (long long)B * N, per_cta = kNormThreads >> split.log;
     const int ctas = (int)std::min<long long>((rows + per_cta - 1) / per_cta, 8LL * h->num_sms);
     LaunchScope ls(h, K_NORM, st);
-    by_vectors<Norm>(split.per, a, ctas, a.shared ? weights : 0, st);
-    return check_cuda(h, cudaGetLastError());
+    const cudaError_t e = by_vectors<Norm>(split.per, a, ctas, a.shared ? weights : 0, st);
+    return check_cuda(h, e != cudaSuccess ? e : cudaGetLastError());
 }
 
 extern "C" int emc2_expert_norm_grad(emc2_bridge_t* h, int32_t B, int32_t N, int32_t channels, int32_t type_x, int32_t type_y,
@@ -396,7 +402,8 @@ extern "C" int emc2_expert_norm_grad(emc2_bridge_t* h, int32_t B, int32_t N, int
     t.part = a.part; t.share = a.share; t.dweight = d_grad_weight; t.dbias = d_grad_bias; t.C = channels;
     {
         LaunchScope ls(h, K_NORM_GRAD, st);
-        by_vectors<NormGrad>(split.per, a, ctas, (size_t)(kNormThreads / 32) * 2 * a.nvec * sizeof(float4), st);
+        const cudaError_t e = by_vectors<NormGrad>(split.per, a, ctas, (size_t)(kNormThreads / 32) * 2 * a.nvec * sizeof(float4), st);
+        if (e != cudaSuccess) return check_cuda(h, e);
     }
     {
         LaunchScope ls(h, K_NORM_SUM, st);

@@ -481,14 +481,19 @@ __global__ void __launch_bounds__(kLookupThreads) lookup_join_kernel(SumArgs a, 
 }
 
 template <int K, bool kHalf>
-void launch_sum_of(const SumArgs& a, int ctas, size_t shared, cudaStream_t st) {
-    if (shared > 40 * 1024) cudaFuncSetAttribute(lookup_sum_kernel<K, kHalf>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)shared);
+cudaError_t launch_sum_of(const SumArgs& a, int ctas, size_t shared, cudaStream_t st) {
+    // Sums of a CTA's groups, two of up to K vectors per thread, and the keys and places of up to a group per thread.
+    constexpr size_t most = (size_t)kLookupThreads * (2 * K * sizeof(float4) + kRunItems * 2 * sizeof(uint32_t)) + 4 * sizeof(uint32_t);
+    if (shared > 40 * 1024) {
+        const cudaError_t e = allow_shared(lookup_sum_kernel<K, kHalf>, most);
+        if (e != cudaSuccess) return e;
+    }
     launch_chained(lookup_sum_kernel<K, kHalf>, dim3(ctas), kLookupThreads, shared, st, a);
+    return cudaSuccess;
 }
 template <int K>
-void launch_sum(const SumArgs& a, int ctas, size_t shared, cudaStream_t st) {
-    if (a.type == EMC2_F32) launch_sum_of<K, false>(a, ctas, shared, st);
-    else launch_sum_of<K, true>(a, ctas, shared, st);
+cudaError_t launch_sum(const SumArgs& a, int ctas, size_t shared, cudaStream_t st) {
+    return a.type == EMC2_F32 ? launch_sum_of<K, false>(a, ctas, shared, st) : launch_sum_of<K, true>(a, ctas, shared, st);
 }
 
 int check_lookup(const emc2_bridge* h, int n, int rows, int channels, int type, const void* ids) {
@@ -584,16 +589,18 @@ extern "C" int emc2_row_lookup_grad(emc2_bridge_t* h, int32_t n, int32_t rows, i
     {
         const size_t shared = (size_t)groups * 2 * a.nvec * sizeof(float4) + ((size_t)groups * kRunItems * 2 + 4) * sizeof(uint32_t);
         LaunchScope ls(h, K_LOOKUP_SUM, st);
+        cudaError_t e;
         switch (split.per) {
-            case 1: launch_sum<1>(a, grid, shared, st); break;
-            case 2: launch_sum<2>(a, grid, shared, st); break;
-            case 3: launch_sum<3>(a, grid, shared, st); break;
-            case 4: launch_sum<4>(a, grid, shared, st); break;
-            case 5: launch_sum<5>(a, grid, shared, st); break;
-            case 6: launch_sum<6>(a, grid, shared, st); break;
-            case 7: launch_sum<7>(a, grid, shared, st); break;
-            default: launch_sum<8>(a, grid, shared, st); break;
+            case 1: e = launch_sum<1>(a, grid, shared, st); break;
+            case 2: e = launch_sum<2>(a, grid, shared, st); break;
+            case 3: e = launch_sum<3>(a, grid, shared, st); break;
+            case 4: e = launch_sum<4>(a, grid, shared, st); break;
+            case 5: e = launch_sum<5>(a, grid, shared, st); break;
+            case 6: e = launch_sum<6>(a, grid, shared, st); break;
+            case 7: e = launch_sum<7>(a, grid, shared, st); break;
+            default: e = launch_sum<8>(a, grid, shared, st); break;
         }
+        if (e != cudaSuccess) return check_cuda(h, e);
     }
     {
         LaunchScope ls(h, K_LOOKUP_JOIN, st);

@@ -33,6 +33,14 @@ struct RowsDevice {
     }
 };
 
+// Lets a kernel be launched with up to `most` bytes of dynamic shared memory, the largest that any call of it has.  The setting is
+// the process's: a call's own size could be lowered by another handle's call on another thread before the launch, which
+// would then be refused.
+template <typename F>
+cudaError_t allow_shared(F kernel, size_t most) {
+    return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)most);
+}
+
 // The experts' segments of a call.  offsets null: one expert owns all rows.
 struct RowSegments {
     const int32_t* offsets;
