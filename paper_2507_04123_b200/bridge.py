@@ -184,6 +184,13 @@ def _check(t: torch.Tensor, dtype, shape, name: str, device) -> None:
                          f"got {t.dtype} {tuple(t.shape)} on {t.device}")
 
 
+def _sizes(*values: int) -> None:
+    """Refuses sizes that the library's int32 arguments cannot hold; ctypes would cut them down to 32 bits."""
+    for v in values:
+        if not -2 ** 31 <= v < 2 ** 31:
+            raise ValueError(f"a size of {v} does not fit 32 bits")
+
+
 def route_dispatch_static(config: Emc2Config, points: torch.Tensor, vis_mask: torch.Tensor,
                           gathered: torch.Tensor, out: Dict[str, torch.Tensor]) -> Dict[str, torch.Tensor]:
     """emc2_route_dispatch_static: stages 3 and 4 without a handle and without any allocation.
@@ -480,6 +487,7 @@ class Bridge:
     def reserve_rows(self, channels: int, hidden: int = 0) -> None:
         """emc2_rows_reserve: scratch of the gradient calls below for rows of up to ``channels`` channels (and
         ``hidden`` hidden units); with ``hidden``, :meth:`expert_ffn` shares out few rows' units with it too."""
+        _sizes(int(channels), int(hidden))
         self._raise(self.lib.emc2_rows_reserve(self._h, int(channels), int(hidden)), "emc2_rows_reserve")
 
     def _row_type(self, t: torch.Tensor, name: str) -> int:
@@ -497,6 +505,7 @@ class Bridge:
                    out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """emc2_row_lookup: ``scale * table[ids]`` with zero rows where an id is negative; ids of any shape."""
         rows, C = table.shape
+        _sizes(ids.numel(), rows, C)
         kind = self._row_type(table, "table")
         _check(ids, torch.int32, ids.shape, "ids", self.device)
         _check(table, table.dtype, (rows, C), "table", self.device)
@@ -513,6 +522,7 @@ class Bridge:
                         out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """emc2_row_lookup_grad: gradient [rows, channels] of the table of :meth:`row_lookup` (needs :meth:`reserve_rows`)."""
         C = grad_out.shape[-1]
+        _sizes(ids.numel(), int(rows), C)
         kind = self._row_type(grad_out, "grad_out")
         _check(ids, torch.int32, ids.shape, "ids", self.device)
         _check(grad_out, grad_out.dtype, (*ids.shape, C), "grad_out", self.device)
@@ -530,6 +540,7 @@ class Bridge:
         """emc2_expert_norm: ``y``, and the ``mean`` and ``rstd`` of every row for the gradient (None in ``out``: not stored).
         Rows of no expert are left as they are in ``out``; without ``out`` they are unspecified."""
         B, N, C = x.shape
+        _sizes(B, N, C)
         E = self._experts(offsets, B)
         _check(x, x.dtype, (B, N, C), "x", self.device)
         _check(weight, torch.float32, (E, C), "weight", self.device)
@@ -555,6 +566,7 @@ class Bridge:
                          out: Optional[Dict[str, Optional[torch.Tensor]]] = None) -> Dict[str, Optional[torch.Tensor]]:
         """emc2_expert_norm_grad: ``grad_x``, ``grad_weight``, ``grad_bias`` (needs :meth:`reserve_rows`)."""
         B, N, C = x.shape
+        _sizes(B, N, C)
         E = self._experts(offsets, B)
         _check(x, x.dtype, (B, N, C), "x", self.device)
         _check(weight, torch.float32, (E, C), "weight", self.device)
@@ -578,6 +590,7 @@ class Bridge:
         B, N, C = x.shape
         E = self._experts(offsets, B)
         H = w_gate.shape[1]
+        _sizes(B, N, C, H)
         if act not in ACTIVATIONS:
             raise ValueError(f"act: expected one of {sorted(ACTIVATIONS)}, got {act!r}")
         if x.dtype not in (torch.bfloat16, torch.float16):
