@@ -96,7 +96,8 @@ __device__ __forceinline__ void next_item(const RowSegments& s, ItemWalk& w, int
 // g / (1 + exp(-g)) and the sigmoid 1 / (1 + exp(-g)), by exponentials and one reciprocal for two (a reciprocal each: 260 us
 // instead of 220 for 1.2 million rows of 80 channels, 320 units).  Both are right to a few units of fp32 relative to themselves,
 // which the roundings behind them need: for negative g they are small, and a form that is right to 2^-12 of 1, like
-// (1 + tanh.approx(g / 2)) / 2 (183 us), has none of their bits left at g = -9.  Gates below -41.5 are taken as -41.5, where the result
+// (1 + tanh.approx(g / 2)) / 2 (183 us), has none of their bits left at g = -9.  The exponentials of one pair in four, or of every
+// other, by a polynomial on the fp32 units: 233 and 236 us.  Gates below -41.5 are taken as -41.5, where the result
 // is above -2^-54: the denominators' product then stays below 2^120.  A NaN stays one.
 __device__ __forceinline__ uint64_t silu2(uint64_t g, uint64_t& sigmoid) {
     const float2 x = unpair(g);
@@ -266,10 +267,10 @@ struct Maps {
     CUtensorMap x_tail, dy_tail, gate_tail, up_tail, out_tail;              // of the last block of columns, where it is narrower
 };
 
-// 1.2 million rows of 80 bf16 channels, 320 units, SiLU: 220 us, 0.84 PFLOP/s in products of N = 128 and 80.  What bounds it is the
-// special-function unit: three results for two activations are 126 us of its rate, and each more or fewer was measured at 40 us.
-// dx of 480,000 fp16 rows of 64 channels, 256 units, GELU: 162 us; of 95,000 bf16 rows of 256, 1,024 units, SiLU: 327 us, 0.76
-// PFLOP/s.
+// 1.2 million rows of 80 bf16 channels, 320 units, SiLU: 220 us, 0.84 PFLOP/s in products of N = 128 and 80 (fp16 223; GELU
+// 293).  What it waits for is the activation: three results of the special-function unit for two values, 59 % of that unit's rate beside
+// 52 % of the issue slots; a fourth result costs 40 us.  dx of 480,000 fp16 rows of 64 channels, 256 units, GELU: 162 us; of 95,000 bf16 rows
+// of 256, 1,024 units, SiLU: 346 us, 0.72 PFLOP/s, where products of N = 64 and 32 take as long as twice as wide ones would.
 template <int MODE, int HC, int NT, int TO, int ACT, bool BF16, bool SHARES>
 __global__ void __launch_bounds__(kFfnThreads, 1) ffn_rows_kernel(const RowArgs a, const __grid_constant__ Maps maps) {
     // TMEM: the output of NT tiles, two accumulators of g and u, for dx two of dh, and the hidden values of two units unless
@@ -598,7 +599,7 @@ __device__ __forceinline__ void clear_rows(uint32_t tile, int blocks, int rows, 
 // slice, [C, HC] each (the channels in the lanes).  All slices of a range are taken at about the same time, so that its
 // tiles are read from device memory once.  A range that meets several experts has a part of the result for each: entry
 // r + e of `part`, which along the run of all tiles no other pair of range and expert has.
-// 480,000 fp16 rows of 64 channels, 256 units, GELU: 200 us; 95,000 bf16 rows of 256, 1,024 units, SiLU: 563 us, 0.53 PFLOP/s:
+// 480,000 fp16 rows of 64 channels, 256 units, GELU: 200 us; 95,000 bf16 rows of 256, 1,024 units, SiLU: 545 us, 0.55 PFLOP/s:
 // of a tile's products those of the transposed rows have N = 64 and 32 columns at C > 128, which take 49 and 45 clocks for 32 and 16.
 template <int HC, int ACT, bool BF16>
 __global__ void __launch_bounds__(kFfnThreads, 1) ffn_weights_kernel(const WeightArgs a, const __grid_constant__ Maps maps) {
@@ -970,7 +971,7 @@ int launch_rows(emc2_bridge* h, const FfnCall& f, cudaStream_t st) {
     const size_t shared = std::max(room(), (size_t)(kMaxBounds + kMaxSegments + 1) * 4 + 1024);
     // Few rows: shares of their hidden units, of four chunks at least, keep the other SMs busy, if there is scratch for what
     // they leave and more than 16 chunks.  us in one piece, and in shares with their join: 64 rows of 64 channels, 4,096 units
-    // 41.8 and 20.1; 512 units 18.6 and 23.2.
+    // 47.2 and 21.5; 1,280 units 26.6 and 21.2; 512 units 20.5 and 21.4.
     const long long tiles = row_tiles(f.seg, NT);
     const RowsScratch& r = h->rows_scratch;
     a.splits = 1;
@@ -1036,8 +1037,8 @@ int launch_slices(emc2_bridge* h, const FfnCall& f, WeightArgs& a, cudaStream_t 
 }
 
 // Slices of 64 hidden units where two stages of tiles fit beside them (up to 96 channels): half the products, which below
-// N = 128 take little less for half the columns.  us with 64 and with 32, 60,000 rows: 64 channels, 1,024 units 88.9 and
-// 123.4; 96 channels, 512 units 74.2 and 84.9.
+// N = 128 take little less for half the columns.  us with 64 and with 32, 60,000 rows: 64 channels, 1,024 units 96.8 and
+// 125.4; 96 channels, 512 units 80.3 and 87.6.
 bool wide_slices(const FfnCall& f) {
     WeightArgs a;
     plan_weights<64>(a, f);
@@ -1103,9 +1104,11 @@ extern "C" int emc2_expert_ffn(emc2_bridge_t* h, int32_t B, int32_t N, int32_t c
     const FfnCall f = {row_segments(h, B, N, d_offsets), channels, hidden, type, act, d_x, nullptr, d_w_gate, d_w_up, d_w_down, d_y};
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     // Chunks of hidden units, and tiles that share their weights, as TMEM has room for (see ffn_rows_kernel).  Two tiles share
-    // a chunk's weights where there is more than one per SM.  us
-    // of one and of two: 15,000 rows of 64 channels, 1,024 units 21.7 and 26.8; 20,000 30.9 and 27.2; 60,000 52.1
-    // and 44.0; 60,000 of 128 channels, 512 units 50.9 and 38.5.
+    // a chunk's weights where there can be more than one per SM, counted by the rows and one more per segment: where the segments
+    // end is known on the device only.  Calls of many short segments therefore run tiles that are mostly empty.  us
+    // of one and of two: 15,000 rows of 64 channels, 1,024 units 23.3 and 31.5; 20,000 30.7 and 30.7; 60,000 52.0 and 51.2 (but
+    // 40,000, whose pairs are just more than the SMs, 41.7 and 50.0); 60,000 of 80 channels, 320 units 31.5 and 29.4; of 128 channels,
+    // 512 units 47.1 and 41.0.
     const bool pairs = row_tiles(f.seg, 1) > h->num_sms;
     if (channels <= 96) return pairs ? launch_rows<FORWARD, 64, 2, TO_TMEM>(h, f, st) : launch_rows<FORWARD, 64, 1, TO_TMEM>(h, f, st);
     return channels <= 128 && pairs ? launch_rows<FORWARD, 32, 2, TO_TMEM>(h, f, st) : launch_rows<FORWARD, 32, 1, TO_TMEM>(h, f, st);
@@ -1137,7 +1140,8 @@ extern "C" int emc2_expert_ffn_grad(emc2_bridge_t* h, int32_t B, int32_t N, int3
     // The weights' gradients need nothing of dx: they run on a stream of the handle, whose CTAs take the SMs over as those of
     // dx end, instead of waiting for the last.  Not where dx is in shares, which lie in the same scratch, nor for few channels,
     // whose CTAs of the two would be on an SM together, in each other's way.  us on one stream and on two: 15,000 rows of 128
-    // channels, 512 units 70.7 and 65.5; 60,000 of 256, 1,024 units 588 and 563; 120,000 of 64, 1,024 units, GELU 373 and 403.
+    // channels, 512 units 70.7 and 63.5; 60,000 of 256, 1,024 units 607 and 582; of 64, 1,024 units 179 and 182; 120,000 of 64, 1,024
+    // units, GELU 345 and 363.
     const bool aside = h->overlap && 2 * row_tiles(f.seg, 1) > h->num_sms && channels > 96;
     const cudaStream_t weights_st = aside ? h->side : st;
     if (aside) {
@@ -1146,7 +1150,7 @@ extern "C" int emc2_expert_ffn_grad(emc2_bridge_t* h, int32_t B, int32_t N, int3
         if (e != cudaSuccess) return check_cuda(h, e);
     }
     // Hidden values in shared memory leave TMEM to chunks of 64 units; GELU's arithmetic has no registers for those.  us of dx
-    // with them and with chunks of 32: 60,000 rows of 64 channels, 1,024 units, SiLU 62.7 and 85.2; 256 units 32.1 and 35.1.
+    // with them and with chunks of 32: 60,000 rows of 64 channels, 1,024 units, SiLU 75.8 and 81.9; 256 units 34.9 and 35.7.
     rc = channels <= 64 && act == EMC2_ACT_SILU ? launch_rows<GRAD_X, 64, 1, TO_SHARED>(h, f, st) : launch_rows<GRAD_X, 32, 1, TO_TMEM>(h, f, st);
     if (rc == EMC2_OK) rc = launch_weights(h, f, d_grad_gate, d_grad_up, d_grad_down, weights_st);
     if (aside) {                                                           // also after an error: `st` never runs ahead

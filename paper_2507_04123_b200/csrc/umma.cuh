@@ -53,7 +53,8 @@ __device__ __forceinline__ bool bar_test(uint32_t bar, uint32_t parity) {
 // A wait that ends: after kWaitTries tries it sets *gave_up, and from then on every wait of the CTA that is not over at once
 // is given up.  The CTA then runs through the rest of its steps without waiting (what it computes is void, as the status
 // says) and winds up, see leave_after_timeout.  A hint for a long suspension made everything 10 % slower, polling without any
-// 3 % (forward, 1.2 M rows of 80 channels).  Only the first try is in line: the warps that copy and issue products run through little else, and what they fetch counts.
+// 3 % (forward, 1.2 M rows of 80 channels, at 183 us).  Only the first try is in line: the warps that copy and issue products run
+// through little else, and what they fetch counts.
 constexpr int kWaitTries = 1 << 22;
 constexpr int kStatusTimeout = 2;            // device status: EMC2_ERR_TIMEOUT
 __device__ __forceinline__ void bar_wait_inline(uint32_t bar, uint32_t parity, volatile int* gave_up, int* status) {
