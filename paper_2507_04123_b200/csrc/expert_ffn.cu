@@ -1139,7 +1139,7 @@ extern "C" int emc2_expert_ffn_grad(emc2_bridge_t* h, int32_t B, int32_t N, int3
     }
     // The weights' gradients need nothing of dx: they run on a stream of the handle, whose CTAs take the SMs over as those of
     // dx end, instead of waiting for the last.  Not where dx is in shares, which lie in the same scratch, nor for few channels,
-    // whose CTAs of the two would be on an SM together, in each other's way.  us on one stream and on two: 15,000 rows of 128
+    // where it was measured to be slower.  us on one stream and on two: 15,000 rows of 128
     // channels, 512 units 70.7 and 63.5; 60,000 of 256, 1,024 units 607 and 582; of 64, 1,024 units 179 and 182; 120,000 of 64, 1,024
     // units, GELU 345 and 363.
     const bool aside = h->overlap && 2 * row_tiles(f.seg, 1) > h->num_sms && channels > 96;
