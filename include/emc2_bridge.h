@@ -389,6 +389,46 @@ int emc2_expert_ffn_grad(emc2_bridge_t* bridge, int32_t B, int32_t N, int32_t ch
                          const void* d_w_down, const void* d_grad_y, void* d_grad_x, void* d_grad_gate, void* d_grad_up,
                          void* d_grad_down, void* cuda_stream);
 
+/* Dropout of rows: d_y = d_x / (1 - p) where the element is kept, 0 (whatever d_x holds) where it is dropped.  No mask is
+ * stored: it follows from the seed, and the same call on the gradient of d_y gives the gradient of d_x.
+ *   d_x, d_y  type [n, channels], n <= max_batch * max_points; channels a multiple of 4 up to 1024
+ *   d_seed    int64 [2] on the DEVICE, on 8 bytes: a seed and the number of the call, so that a captured call takes new ones
+ * Channels 8 g .. 8 g + 7 of row i share one number of the counter-based generator Philox4x32-10 (Salmon et al., 2011) with the key
+ * seed, seed >> 32 and the counter i, g, number, number >> 32.  Channel 8 g + j takes 16 bits, the low half of word j / 2 for even
+ * j, the high half for odd j, and is kept where these are >= t = floor(65536 p + 1/2): p counts as t / 65536, in the factor too.
+ * 0 <= p <= 1 (with t = 65536 everything is dropped).  The product is taken in fp32 and rounded once. */
+int emc2_row_dropout(emc2_bridge_t* bridge, int32_t n, int32_t channels, int32_t type, const void* d_x, float p, const int64_t* d_seed,
+                     void* d_y, void* cuda_stream);
+
+/* What follows an expert's block, in one pass: norm of its result d_f, dropout, gate, residual scale, sum with its rows
+ * d_x, and the norm before the next block.  Per row, with the weights of its expert:
+ *   post  = (f - mean) * rstd * post_weight + post_bias        as emc2_expert_norm; without post_weight, f
+ *   d_out = x + scale * gate * dropout(post)                   dropout as emc2_row_dropout, row b * N + j
+ *   d_y   = (out - mean') * rstd' * pre_weight + pre_bias      of d_out before its rounding
+ *   d_x, d_out   type_x [B, N, channels]     d_f  type_f     d_y  type_y; channels a multiple of 4 up to 1024
+ *   d_gate       float [B, N], or NULL: 1
+ *   d_post_weight, d_post_bias, d_scale, d_pre_weight, d_pre_bias   float [E, channels]; each may be NULL (a weight: that norm is left out,
+ *                and its bias has to be NULL; the scale: 1; a bias: 0).  d_y is NULL where d_pre_weight is, and only there
+ *   d_stats      float [B, N, 4]: mean, rstd, mean', rstd' (0, 1 of a norm left out), for the gradient; may be NULL
+ * p and d_seed as in emc2_row_dropout; d_seed may be NULL where p is 0.  fp32 throughout, results rounded once.  eps >= 0. */
+int emc2_expert_residual(emc2_bridge_t* bridge, int32_t B, int32_t N, int32_t channels, int32_t type_x, int32_t type_f, int32_t type_y,
+                         const void* d_x, const void* d_f, const int32_t* d_offsets, const float* d_gate, const float* d_post_weight,
+                         const float* d_post_bias, const float* d_scale, const float* d_pre_weight, const float* d_pre_bias, float eps,
+                         float p, const int64_t* d_seed, void* d_out, void* d_y, float* d_stats, void* cuda_stream);
+
+/* Its gradients (scratch) for d_grad_out, type_x (NULL: zeros, where there is d_pre_weight) and d_grad_y, type_y (NULL without
+ * d_pre_weight), from the d_out (not read without d_pre_weight) and d_stats (not read without both weights) that the forward call
+ * left, and the forward call's d_f, d_gate, weights, p and seed:
+ *   d_grad_x  type_x [B, N, channels]     d_grad_f  type_f     d_grad_gate  float [B, N], or NULL
+ *   d_grad_post_weight, d_grad_post_bias, d_grad_scale, d_grad_pre_weight, d_grad_pre_bias  float [E, channels]; each may be NULL, and has
+ *             to be where what it belongs to is left out (the scale's gradient is given without a scale too) */
+int emc2_expert_residual_grad(emc2_bridge_t* bridge, int32_t B, int32_t N, int32_t channels, int32_t type_x, int32_t type_f, int32_t type_y,
+                              const void* d_out, const void* d_f, const int32_t* d_offsets, const float* d_stats, const void* d_grad_out,
+                              const void* d_grad_y, const float* d_gate, const float* d_post_weight, const float* d_post_bias,
+                              const float* d_scale, const float* d_pre_weight, float p, const int64_t* d_seed, void* d_grad_x,
+                              void* d_grad_f, float* d_grad_gate, float* d_grad_post_weight, float* d_grad_post_bias,
+                              float* d_grad_scale, float* d_grad_pre_weight, float* d_grad_pre_bias, void* cuda_stream);
+
 /* Turns the handle's own streams in emc2_bridge_run and emc2_expert_ffn_grad off (0) or on (non-zero, the default).  Off, every
  * kernel of the call is enqueued on `cuda_stream` itself, one after another: for callers that
  * want no second stream, and for timing kernels one at a time. */

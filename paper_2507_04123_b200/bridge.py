@@ -39,6 +39,7 @@ ABI_SYMBOLS = (
     "emc2_bridge_set_tuning", "emc2_bridge_profile_timeline", "emc2_voxel_image_pooled",
     "emc2_rows_reserve", "emc2_row_lookup", "emc2_row_lookup_grad", "emc2_expert_norm", "emc2_expert_norm_grad",
     "emc2_expert_ffn", "emc2_expert_ffn_grad",
+    "emc2_row_dropout", "emc2_expert_residual", "emc2_expert_residual_grad",
 )
 
 # emc2_type_t
@@ -121,6 +122,9 @@ def load_library() -> ctypes.CDLL:
     lib.emc2_expert_norm_grad.argtypes = [vp] + [i32] * 5 + [vp] * 10
     lib.emc2_expert_ffn.argtypes = [vp] + [i32] * 6 + [vp] * 7
     lib.emc2_expert_ffn_grad.argtypes = [vp] + [i32] * 6 + [vp] * 11
+    lib.emc2_row_dropout.argtypes = [vp, i32, i32, i32, vp, f32, vp, vp, vp]
+    lib.emc2_expert_residual.argtypes = [vp] + [i32] * 6 + [vp] * 9 + [f32, f32] + [vp] * 5
+    lib.emc2_expert_residual_grad.argtypes = [vp] + [i32] * 6 + [vp] * 11 + [f32] + [vp] * 10
     lib.emc2_bridge_destroy.argtypes = [vp]
     lib.emc2_status_string.argtypes = [ctypes.c_int]
     lib.emc2_status_string.restype = ctypes.c_char_p
@@ -630,6 +634,109 @@ class Bridge:
                                            out["grad_x"].data_ptr(), out["grad_gate"].data_ptr(), out["grad_up"].data_ptr(),
                                            out["grad_down"].data_ptr(), self._stream())
         self._raise(rc, "emc2_expert_ffn_grad")
+        return out
+
+    def row_dropout(self, x: torch.Tensor, p: float, seed: torch.Tensor, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """emc2_row_dropout: rows [.., channels] with a share ``p`` of the elements dropped, the others divided by 1 - p.  ``seed``:
+        int64 [2] on the device, a seed and the number of the call.  On the gradient of the result, the gradient."""
+        C = x.shape[-1]
+        n = x.numel() // C if C else 0
+        _sizes(n, C)
+        kind = self._row_type(x, "x")
+        _check(x, x.dtype, x.shape, "x", self.device)
+        _check(seed, torch.int64, (2,), "seed", self.device)
+        if out is None:
+            out = torch.empty_like(x)
+        _check(out, x.dtype, x.shape, "out", self.device)
+        rc = self.lib.emc2_row_dropout(self._h, n, C, kind, x.data_ptr(), float(p), seed.data_ptr(), out.data_ptr(), self._stream())
+        self._raise(rc, "emc2_row_dropout")
+        return out
+
+    def _check_residual(self, x, f, offsets, gate, params, p, seed):
+        B, N, C = x.shape
+        _sizes(B, N, C)
+        E = self._experts(offsets, B)
+        _check(x, x.dtype, (B, N, C), "rows", self.device)
+        _check(f, f.dtype, (B, N, C), "f", self.device)
+        for name, t in params.items():
+            if t is not None:
+                _check(t, torch.float32, (E, C), name, self.device)
+        if gate is not None:
+            _check(gate, torch.float32, (B, N), "gate", self.device)
+        if seed is not None:
+            _check(seed, torch.int64, (2,), "seed", self.device)
+        elif p:
+            raise ValueError("seed: dropout needs one")
+        return B, N, C, E
+
+    def expert_residual(self, x: torch.Tensor, f: torch.Tensor, offsets: Optional[torch.Tensor], gate: Optional[torch.Tensor] = None,
+                        post_weight: Optional[torch.Tensor] = None, post_bias: Optional[torch.Tensor] = None,
+                        scale: Optional[torch.Tensor] = None, pre_weight: Optional[torch.Tensor] = None,
+                        pre_bias: Optional[torch.Tensor] = None, eps: float = 1e-5, p: float = 0.0, seed: Optional[torch.Tensor] = None,
+                        y_dtype: Optional[torch.dtype] = None,
+                        out: Optional[Dict[str, Optional[torch.Tensor]]] = None) -> Dict[str, Optional[torch.Tensor]]:
+        """emc2_expert_residual: ``out = x + scale * gate * dropout(norm(f))`` and ``y = norm(out)``, with the ``stats`` for the
+        gradient (None in ``out``: not stored).  Without ``post_weight`` f is not normed, without ``pre_weight`` there is no y.  Rows
+        of no expert are left as they are in ``out``; without ``out`` they are unspecified."""
+        params = {"post_weight": post_weight, "post_bias": post_bias, "scale": scale, "pre_weight": pre_weight, "pre_bias": pre_bias}
+        B, N, C, _ = self._check_residual(x, f, offsets, gate, params, p, seed)
+        if out is None:
+            out = {"out": torch.empty_like(x), "stats": torch.empty((B, N, 4), dtype=torch.float32, device=self.device),
+                   "y": None if pre_weight is None else torch.empty((B, N, C), dtype=y_dtype or f.dtype, device=self.device)}
+        y = out.get("y")
+        if (y is None) != (pre_weight is None):
+            raise ValueError("y: given with pre_weight, and only with it")
+        _check(out["out"], x.dtype, (B, N, C), "out", self.device)
+        if y is not None:
+            _check(y, y_dtype or y.dtype, (B, N, C), "y", self.device)
+        if out.get("stats") is not None:
+            _check(out["stats"], torch.float32, (B, N, 4), "stats", self.device)
+        rc = self.lib.emc2_expert_residual(
+            self._h, B, N, C, self._row_type(x, "x"), self._row_type(f, "f"), self._row_type(f if y is None else y, "y"), x.data_ptr(),
+            f.data_ptr(), _ptr(offsets), _ptr(gate), *[_ptr(t) for t in params.values()], float(eps), float(p), _ptr(seed),
+            out["out"].data_ptr(), _ptr(y), _ptr(out.get("stats")), self._stream())
+        self._raise(rc, "emc2_expert_residual")
+        return out
+
+    def expert_residual_grad(self, rows: torch.Tensor, f: torch.Tensor, offsets: Optional[torch.Tensor], stats: Optional[torch.Tensor],
+                             grad_out: Optional[torch.Tensor], grad_y: Optional[torch.Tensor], gate: Optional[torch.Tensor] = None,
+                             post_weight: Optional[torch.Tensor] = None, post_bias: Optional[torch.Tensor] = None,
+                             scale: Optional[torch.Tensor] = None, pre_weight: Optional[torch.Tensor] = None, p: float = 0.0,
+                             seed: Optional[torch.Tensor] = None,
+                             out: Optional[Dict[str, Optional[torch.Tensor]]] = None) -> Dict[str, Optional[torch.Tensor]]:
+        """emc2_expert_residual_grad: ``grad_x``, ``grad_f``, ``grad_gate`` and the gradients of the parameters given, from ``rows``
+        (the ``out`` of :meth:`expert_residual`) and its ``stats``; None in ``out``: not computed (needs :meth:`reserve_rows`)."""
+        params = {"post_weight": post_weight, "post_bias": post_bias, "scale": scale, "pre_weight": pre_weight}
+        B, N, C, E = self._check_residual(rows, f, offsets, gate, params, p, seed)
+        if (grad_y is None) != (pre_weight is None):
+            raise ValueError("grad_y: given with pre_weight, and only with it")
+        if grad_out is None and pre_weight is None:
+            raise ValueError("grad_out: needed without pre_weight")
+        if grad_out is not None:
+            _check(grad_out, rows.dtype, (B, N, C), "grad_out", self.device)
+        if grad_y is not None:
+            _check(grad_y, grad_y.dtype, (B, N, C), "grad_y", self.device)
+        if stats is not None:
+            _check(stats, torch.float32, (B, N, 4), "stats", self.device)
+        elif pre_weight is not None or post_weight is not None:
+            raise ValueError("stats: needed for a norm's gradient")
+        of = {"post_weight": post_weight, "post_bias": post_bias, "scale": scale, "pre_weight": pre_weight, "pre_bias": pre_weight}
+        if out is None:
+            out = {"grad_x": torch.empty_like(rows), "grad_f": torch.empty_like(f), "grad_gate": None if gate is None else torch.empty_like(gate)}
+            out.update({"grad_" + k: None if t is None else torch.empty_like(t) for k, t in of.items()})
+        _check(out["grad_x"], rows.dtype, (B, N, C), "grad_x", self.device)
+        _check(out["grad_f"], f.dtype, (B, N, C), "grad_f", self.device)
+        if out.get("grad_gate") is not None:
+            _check(out["grad_gate"], torch.float32, (B, N), "grad_gate", self.device)
+        for k in of:
+            if out.get("grad_" + k) is not None:
+                _check(out["grad_" + k], torch.float32, (E, C), "grad_" + k, self.device)
+        rc = self.lib.emc2_expert_residual_grad(
+            self._h, B, N, C, self._row_type(rows, "rows"), self._row_type(f, "f"), self._row_type(f if grad_y is None else grad_y, "grad_y"),
+            rows.data_ptr(), f.data_ptr(), _ptr(offsets), _ptr(stats), _ptr(grad_out), _ptr(grad_y), _ptr(gate),
+            *[_ptr(t) for t in params.values()], float(p), _ptr(seed), out["grad_x"].data_ptr(), out["grad_f"].data_ptr(),
+            _ptr(out.get("grad_gate")), *[_ptr(out.get("grad_" + k)) for k in of], self._stream())
+        self._raise(rc, "emc2_expert_residual_grad")
         return out
 
     def set_overlap(self, enable: bool) -> None:

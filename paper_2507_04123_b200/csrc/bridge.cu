@@ -13,7 +13,8 @@ static const char* const kKernelNames[K_KINDS] = {
     "project_gather", "project_route", "gather_scatter", "route_hist", "route_scan", "dispatch_scatter", "scene_route", "pool_features",
     "vif_scan", "vif_fill", "vif_mean", "vif_sample", "occl_fill", "occl_splat", "occl_test",
     "channels_last", "rb_mark", "rb_count", "rb_scan", "rb_fill", "rb_clear",
-    "row_lookup", "lookup_sort", "lookup_sum", "lookup_join", "norm", "norm_grad", "norm_sum", "ffn", "ffn_grad_x", "ffn_grad_w", "ffn_sum", "ffn_join"};
+    "row_lookup", "lookup_sort", "lookup_sum", "lookup_join", "norm", "norm_grad", "norm_sum", "ffn", "ffn_grad_x", "ffn_grad_w", "ffn_sum", "ffn_join",
+    "row_dropout", "residual", "residual_grad", "residual_sum"};
 
 int check_cuda(emc2_bridge* h, cudaError_t e) {
     if (e == cudaSuccess) return EMC2_OK;
@@ -652,7 +653,7 @@ int emc2_rows_reserve(emc2_bridge_t* h, int32_t max_channels, int32_t max_hidden
     RowsScratch& r = h->rows_scratch;
     if (r.slab && max_channels <= r.max_channels && max_hidden <= r.max_hidden) return EMC2_OK;
     const int channels = std::max(max_channels, r.max_channels), hidden = std::max(max_hidden, r.max_hidden);
-    const size_t bytes = std::max({norm_scratch_bytes(h, channels), lookup_scratch_bytes(h, channels), ffn_scratch_bytes(h, channels, hidden)});
+    const size_t bytes = std::max({norm_scratch_bytes(h, channels), residual_scratch_bytes(h, channels), lookup_scratch_bytes(h, channels), ffn_scratch_bytes(h, channels, hidden)});
     DeviceGuard guard(h->cfg.device);
     if (!guard.ok) return EMC2_ERR_CUDA;
     if (!r.slab || bytes > r.bytes) {

@@ -83,6 +83,10 @@ enum KernelKind {
     K_FFN_GRAD_W,
     K_FFN_SUM,
     K_FFN_JOIN,
+    K_ROW_DROPOUT,
+    K_RESIDUAL,
+    K_RESIDUAL_GRAD,
+    K_RESIDUAL_SUM,
     K_KINDS
 };
 
@@ -273,6 +277,7 @@ int launch_voxelize(emc2_bridge* h, int B, int N, const float* d_points, int32_t
 int dedup_arm_alloc(emc2_bridge* h);
 // Scratch that the operators on rows of up to max_channels channels need on this handle.
 size_t norm_scratch_bytes(const emc2_bridge* h, int max_channels);
+size_t residual_scratch_bytes(const emc2_bridge* h, int max_channels);
 size_t lookup_scratch_bytes(const emc2_bridge* h, int max_channels);
 size_t ffn_scratch_bytes(const emc2_bridge* h, int max_channels, int max_hidden);
 int launch_dedup_arm(emc2_bridge* h, int s, int design, int B, int N, const float* d_points, int capacity,

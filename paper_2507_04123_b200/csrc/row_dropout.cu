@@ -1,0 +1,74 @@
+// Dropout of rows: y = x / (1 - p) where the generator keeps the element, else 0.  The gradient is the same call on dy.
+//
+// Bound by memory, next by the generator: eight elements share one of its numbers, see dropout.cuh, and a thread requests its elements
+// before it computes theirs.
+#include <algorithm>
+
+#include "dropout.cuh"
+
+namespace emc2 {
+namespace {
+
+constexpr int kDropThreads = 256;
+constexpr int kDropGroups = 4;               // of eight elements per thread
+
+struct DropArgs {
+    const void* x;
+    void* y;
+    FastDiv width;                           // division by the groups of a row
+    Dropout drop;
+    uint32_t groups;                         // of all rows
+    int nvec, type;
+};
+
+template <bool WIDE>
+__global__ void __launch_bounds__(kDropThreads) dropout_kernel(DropArgs a) {
+    const uint32_t first = blockIdx.x * (kDropThreads * kDropGroups) + threadIdx.x;
+    Raw8 raw[kDropGroups];
+    uint32_t row[kDropGroups], at[kDropGroups];
+#pragma unroll
+    for (int i = 0; i < kDropGroups; ++i) {
+        const uint32_t g = first + i * kDropThreads;
+        const bool in = g < a.groups;
+        a.width.divmod(g, row[i], at[i]);
+        raw[i] = request8<WIDE>(a.x, (size_t)row[i] * a.nvec + 2 * at[i], in, in && 2 * at[i] + 1 < (uint32_t)a.nvec, a.type);
+    }
+    const DropoutSeed seed = dropout_seed(a.drop);
+#pragma unroll
+    for (int i = 0; i < kDropGroups; ++i) {
+        if (first + i * kDropThreads >= a.groups) break;
+        const uint4 bits = dropout_bits(seed, row[i], at[i]);
+        float f[8];
+        floats8(f, raw[i], a.type);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) f[j] = dropout_keeps(bits, j, a.drop.threshold) ? f[j] * a.drop.factor : 0.0f;
+        store8<WIDE>(a.y, (size_t)row[i] * a.nvec + 2 * at[i], 2 * at[i] + 1 < (uint32_t)a.nvec, f, a.type);
+    }
+}
+
+}  // namespace
+}  // namespace emc2
+
+using namespace emc2;
+
+extern "C" int emc2_row_dropout(emc2_bridge_t* h, int32_t n, int32_t channels, int32_t type, const void* d_x, float p,
+                                const int64_t* d_seed, void* d_y, void* cuda_stream) {
+    if (!h || n < 0 || (int64_t)n > (int64_t)h->cfg.max_batch * h->cfg.max_points) return EMC2_ERR_INVALID_ARG;
+    if (channels < 4 || channels > kMaxRowChannels || (channels & 3) || !is_type(type) || !is_share(p)) return EMC2_ERR_INVALID_ARG;
+    if (!d_seed || !on_8_bytes(d_seed) || !on_16_bytes(d_x) || !on_16_bytes(d_y)) return EMC2_ERR_INVALID_ARG;
+    if (n == 0) return EMC2_OK;
+    if (!d_x || !d_y || d_x == d_y) return EMC2_ERR_INVALID_ARG;
+    RowsDevice device(h->cfg.device);
+    if (!device.ok) return EMC2_ERR_CUDA;
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    DropArgs a;
+    a.x = d_x; a.y = d_y; a.drop = make_dropout(p, d_seed); a.nvec = channels / 4; a.type = type;
+    const uint32_t width = (uint32_t)(channels + 7) / 8;
+    a.width = make_fast_div(width);
+    a.groups = (uint32_t)n * width;                              // 2^24 rows of 128 at most
+    const unsigned ctas = (a.groups + kDropThreads * kDropGroups - 1) / (kDropThreads * kDropGroups);
+    LaunchScope ls(h, K_ROW_DROPOUT, st);
+    if (is_wide(channels, type, d_x) && is_wide(channels, type, d_y)) dropout_kernel<true><<<ctas, kDropThreads, 0, st>>>(a);
+    else dropout_kernel<false><<<ctas, kDropThreads, 0, st>>>(a);
+    return check_cuda(h, cudaGetLastError());
+}
