@@ -16,7 +16,8 @@ namespace emc2 {
 
 struct Dropout {
     const unsigned long long* seed;      // {seed, number of the call} on the device
-    uint32_t threshold;                  // 0: nothing is dropped; 65536: everything
+    uint32_t any;                        // 0: nothing is dropped
+    uint32_t above;                      // else 16 bits are compared as the upper half of a word that has to be above this
     float factor;
 };
 
@@ -24,8 +25,10 @@ inline bool is_share(float p) { return p >= 0.0f && p <= 1.0f; }
 inline Dropout make_dropout(float p, const int64_t* d_seed) {
     Dropout d;
     d.seed = reinterpret_cast<const unsigned long long*>(d_seed);
-    d.threshold = (uint32_t)std::floor((double)p * 65536.0 + 0.5);
-    d.factor = d.threshold < 65536u ? (float)(65536.0 / (65536 - (int)d.threshold)) : 0.0f;
+    const int threshold = (int)std::floor((double)p * 65536.0 + 0.5);
+    d.any = threshold > 0;
+    d.above = (uint32_t)threshold * 65536u - 1u;         // of 65536: no word is above it
+    d.factor = threshold < 65536 ? (float)(65536.0 / (65536 - threshold)) : 0.0f;
     return d;
 }
 
@@ -39,25 +42,30 @@ __device__ __forceinline__ DropoutSeed dropout_seed(const Dropout& d) {
     return {(uint32_t)key, (uint32_t)(key >> 32), (uint32_t)call, (uint32_t)(call >> 32)};
 }
 
-__device__ __forceinline__ uint4 dropout_bits(const DropoutSeed& s, uint32_t row, uint32_t group) {
-    uint32_t c0 = row, c1 = group, c2 = s.call0, c3 = s.call1, k0 = s.key0, k1 = s.key1;
+// Bits of K groups at once, round by round: the rounds' keys are worked out once for all, and the products of one group fill the
+// waits of another's.
+template <int K>
+__device__ __forceinline__ void dropout_bits(uint4 (&bits)[K], const DropoutSeed& s, const uint32_t (&row)[K], const uint32_t (&group)[K]) {
+    uint32_t k0 = s.key0, k1 = s.key1;
+#pragma unroll
+    for (int i = 0; i < K; ++i) bits[i] = make_uint4(row[i], group[i], s.call0, s.call1);
 #pragma unroll
     for (int r = 0; r < 10; ++r) {
-        const unsigned long long a = (unsigned long long)c0 * 0xD2511F53u, b = (unsigned long long)c2 * 0xCD9E8D57u;
-        c0 = (uint32_t)(b >> 32) ^ c1 ^ k0;
-        c1 = (uint32_t)b;
-        c2 = (uint32_t)(a >> 32) ^ c3 ^ k1;
-        c3 = (uint32_t)a;
+#pragma unroll
+        for (int i = 0; i < K; ++i) {
+            uint4& c = bits[i];
+            const unsigned long long a = (unsigned long long)c.x * 0xD2511F53u, b = (unsigned long long)c.z * 0xCD9E8D57u;
+            c = make_uint4((uint32_t)(b >> 32) ^ c.y ^ k0, (uint32_t)b, (uint32_t)(a >> 32) ^ c.w ^ k1, (uint32_t)a);
+        }
         k0 += 0x9E3779B9u;
         k1 += 0xBB67AE85u;
     }
-    return make_uint4(c0, c1, c2, c3);
 }
 
 // Whether element j (known at compile time) of the eight is kept.
-__device__ __forceinline__ bool dropout_keeps(const uint4& bits, int j, uint32_t threshold) {
+__device__ __forceinline__ bool dropout_keeps(const uint4& bits, int j, uint32_t above) {
     const uint32_t w = j < 2 ? bits.x : j < 4 ? bits.y : j < 6 ? bits.z : bits.w;
-    return ((j & 1) ? w >> 16 : w & 0xFFFFu) >= threshold;
+    return ((j & 1) ? w : w << 16) > above;              // the lower half of an odd element's word decides nothing: above ends in 0xFFFF
 }
 
 // ---- Eight elements of a row, at a multiple of eight channels.  `hi`: the row has the second four.  WIDE: rows of a multiple of eight

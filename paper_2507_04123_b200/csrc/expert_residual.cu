@@ -28,18 +28,28 @@ struct ResParams {
     const float* p[kParams];                 // [E][C]; null: ones for weights and the scale, zeros for biases
 };
 
-// Eight entries of a parameter at vector v of an expert's; `hi`: the second four are there.
-__device__ __forceinline__ void param8(float (&f)[8], const float4* p, int v, bool hi, float missing) {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) f[j] = missing;
-    if (!p) return;
-    const float4 a = p[v];
-    f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w;
-    if (hi) {
-        const float4 b = p[v + 1];
-        f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
-    }
+// What the kernels take of them: s w and s b of the block's side, and w' and b'; one vector, at v of all experts' rows.
+enum Folded { SIDE_W = 0, SIDE_B, NEXT_W, NEXT_B, kFolded };
+__device__ __forceinline__ float4 folded_param(const ResParams& par, int i, int v) {
+    auto of = [&](const float* p, float missing) {
+        return p ? __ldg(reinterpret_cast<const float4*>(p) + v) : make_float4(missing, missing, missing, missing);
+    };
+    if (i >= NEXT_W) return of(i == NEXT_W ? par.p[PRE_W] : par.p[PRE_B], 0.f);
+    const float4 s = of(par.p[SCALE], 1.f), w = i == SIDE_W ? of(par.p[POST_W], 1.f) : of(par.p[POST_B], 0.f);
+    return make_float4(s.x * w.x, s.y * w.y, s.z * w.z, s.w * w.w);
 }
+
+// The usual calls have kernels of their own, without the branches on what a call can lack, which were half of the instructions: both norms, a
+// gradient from behind, bf16 blocks, rows in fp32 or bf16 of a multiple of eight channels.
+enum Usual { ANY = 0, F32_ROWS, BF16_ROWS };
+inline int usual_of(int type_x, int type_f, int type_y) {
+    if (type_f != EMC2_BF16 || type_y != EMC2_BF16) return ANY;
+    return type_x == EMC2_F32 ? F32_ROWS : type_x == EMC2_BF16 ? BF16_ROWS : ANY;
+}
+template <int U>
+__device__ __forceinline__ int rows_type(int type) { return U == F32_ROWS ? EMC2_F32 : U == BF16_ROWS ? EMC2_BF16 : type; }
+template <int U>
+__device__ __forceinline__ int block_type(int type) { return U == ANY ? type : EMC2_BF16; }
 
 struct ResArgs {
     RowSegments seg;
@@ -54,59 +64,122 @@ struct ResArgs {
     Dropout drop;
     float eps, inv_c;
     int nvec, log, type_x, type_f, type_y, shared;
+    uint32_t params_bytes;                   // of the parameters in shared memory
 };
 
-template <int K, bool WIDE>
+// ---- A thread's next rows on their way to shared memory, in places that it alone reads.
+template <int BYTES>
+__device__ __forceinline__ void copy_ahead(uint32_t dst, const void* src) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(dst), "l"(src), "n"(BYTES) : "memory");
+}
+// Eight elements take a slot of 16 bytes a thread, in fp32 two.
+constexpr uint32_t kSlotBytes = kResThreads * 16;
+template <bool WIDE, uint32_t SLOT = kSlotBytes>
+__device__ __forceinline__ void ahead8(uint32_t dst, const void* p, uint32_t vec, bool hi, int type) {
+    if (type == EMC2_F32) {
+        copy_ahead<16>(dst, static_cast<const float4*>(p) + vec);
+        if (WIDE || hi) copy_ahead<16>(dst + SLOT, static_cast<const float4*>(p) + vec + 1);
+    } else if (WIDE) {
+        copy_ahead<16>(dst, static_cast<const uint2*>(p) + vec);
+    } else {
+        copy_ahead<8>(dst, static_cast<const uint2*>(p) + vec);
+        if (hi) copy_ahead<8>(dst + 8, static_cast<const uint2*>(p) + vec + 1);
+    }
+}
+template <uint32_t SLOT = kSlotBytes>
+__device__ __forceinline__ Raw8 slot8(const char* at, int type) {
+    Raw8 r;
+    r.a = *reinterpret_cast<const uint4*>(at);
+    r.b = type == EMC2_F32 ? *reinterpret_cast<const uint4*>(at + SLOT) : make_uint4(0u, 0u, 0u, 0u);
+    return r;
+}
+__device__ __forceinline__ void clear_second(Raw8& r, int type) {
+    if (type == EMC2_F32) r.b = make_uint4(0u, 0u, 0u, 0u);
+    else r.a.z = r.a.w = 0u;
+}
+
+// Rows in the caller's order, one per group of lanes and step, with few lanes and up to five groups of eight channels per lane: the
+// more a lane requests at once, the more is in flight, and the fewer steps its four sums over the lanes take.
+template <int K, bool WIDE, int U, bool DROP>
 __global__ void __launch_bounds__(kResThreads, K <= 1 ? 4 : K <= 2 ? 3 : 2) residual_kernel(ResArgs a) {
     __shared__ int bounds[kMaxBounds];
-    extern __shared__ float4 staged[];
-    const float4* par[kParams];
-    {
-        float4* at = staged;
-        const int vectors = a.seg.E * a.nvec;
-#pragma unroll
-        for (int i = 0; i < kParams; ++i) {
-            par[i] = reinterpret_cast<const float4*>(a.par.p[i]);
-            if (!a.shared || !par[i]) continue;
-            for (int v = threadIdx.x; v < vectors; v += kResThreads) at[v] = __ldg(par[i] + v);
-            par[i] = at;
-            at += vectors;
-        }
-    }
+    extern __shared__ float4 staged[];       // [kFolded][E][nvec] if they fit, then slots of the rows on their way
+    const int E = a.seg.E, plane = E * a.nvec;
+    const bool post = U || a.par.p[POST_W] != nullptr, pre = U || a.par.p[PRE_W] != nullptr, drop = U ? DROP : a.drop.any != 0;
+    const bool shared = U || a.shared;
+    const int type_x = rows_type<U>(a.type_x), type_f = block_type<U>(a.type_f), type_y = block_type<U>(a.type_y);
+    if (shared)
+        for (int i = 0; i < kFolded; ++i)
+            for (int v = threadIdx.x; v < plane; v += kResThreads) staged[i * plane + v] = folded_param(a.par, i, v);
     load_bounds(a.seg, bounds);
-    const int lane = threadIdx.x & ((1 << a.log) - 1), E = a.seg.E;
+    auto param8 = [&](float (&f)[8], int i, int v, bool hi) {
+        const float4 p = shared ? staged[i * plane + v] : folded_param(a.par, i, v);
+        float4 q = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (hi) q = shared ? staged[i * plane + v + 1] : folded_param(a.par, i, v + 1);
+        f[0] = p.x; f[1] = p.y; f[2] = p.z; f[3] = p.w;
+        f[4] = q.x; f[5] = q.y; f[6] = q.z; f[7] = q.w;
+    };
+    const int lane = threadIdx.x & ((1 << a.log) - 1);
     const uint32_t rows = (uint32_t)a.seg.B * a.seg.N, groups = (gridDim.x * kResThreads) >> a.log;
     const uint32_t sub = (threadIdx.x & 31) >> a.log, first = (blockIdx.x * kResThreads + threadIdx.x) >> a.log;
     DropoutSeed seed = {};
-    if (a.drop.threshold) seed = dropout_seed(a.drop);
-    // All groups of a warp make the same number of steps: the sums are taken by the whole warp.
-    for (uint32_t r0 = first - sub; r0 < rows; r0 += groups) {
-        const uint32_t row = r0 + sub;
-        int e = E;
-        if (row < rows) {
-            uint32_t b, j;
-            a.frame.divmod(row, b, j);
-            const int* of = bounds + b * (E + 1);
-            if ((int)j >= of[0]) {
-                e = 0;
-                while (e < E && (int)j >= of[e + 1]) ++e;
-            }
-        }
-        const bool in = e < E;
-        Raw8 rx[K], rf[K];
+    if (drop) seed = dropout_seed(a.drop);
+    const uint32_t f_slots = type_f == EMC2_F32 ? 2u : 1u, x_slots = type_x == EMC2_F32 ? 2u : 1u;
+    char* const slots_f = reinterpret_cast<char*>(staged) + a.params_bytes + threadIdx.x * 16;
+    char* const slots_x = slots_f + K * f_slots * kSlotBytes;
+    auto expert_of = [&](uint32_t row) {                          // E: none
+        if (row >= rows) return E;
+        uint32_t b, j;
+        a.frame.divmod(row, b, j);
+        const int* of = bounds + b * (E + 1);
+        if ((int)j < of[0]) return E;
+        int e = 0;
+        while (e < E && (int)j >= of[e + 1]) ++e;
+        return e;
+    };
+    auto request = [&](char* slots, uint32_t per, const void* p, uint32_t row, int type, bool in) {
 #pragma unroll
         for (int i = 0; i < K; ++i) {
             const int v = 2 * (lane + (i << a.log));
-            const size_t at = (size_t)row * a.nvec + v;
-            rf[i] = request8<WIDE>(a.f, at, in && v < a.nvec, in && v + 1 < a.nvec, a.type_f);
-            rx[i] = request8<WIDE>(a.x, at, in && v < a.nvec, in && v + 1 < a.nvec, a.type_x);
+            if (in && (U || v < a.nvec)) ahead8<WIDE>((uint32_t)__cvta_generic_to_shared(slots + i * per * kSlotBytes), p, row * (uint32_t)a.nvec + v, v + 1 < a.nvec, type);
         }
-        const float gate = in && a.gate ? __ldg(a.gate + row) : 1.0f;
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    auto taken = [&](float (&f)[8], const char* slots, uint32_t per, int i, int type, bool hi) {
+        Raw8 raw = slot8(slots + i * per * kSlotBytes, type);
+        if (!WIDE && !hi) clear_second(raw, type);
+        floats8(f, raw, type);
+    };
+    int e_next = expert_of(first);
+    request(slots_f, f_slots, a.f, first, type_f, e_next < E);
+    request(slots_x, x_slots, a.x, first, type_x, e_next < E);
+    // All groups of a warp make the same number of steps: the sums are taken by the whole warp.
+    for (uint32_t r0 = first - sub; r0 < rows; r0 += groups) {
+        const uint32_t row = r0 + sub, after = row + groups;
+        const int e = e_next;
+        const bool in = e < E;
+        float gate = in && a.gate ? __ldg(a.gate + row) : 1.0f;
+        e_next = expert_of(after);
+        uint4 bits[K];                       // worked out while the rows are on their way
+        if (drop) {
+            uint32_t of[K], group[K];
+#pragma unroll
+            for (int i = 0; i < K; ++i) { of[i] = row; group[i] = (uint32_t)(lane + (i << a.log)); }
+            dropout_bits(bits, seed, of, group);
+            gate *= a.drop.factor;
+        }
+        asm volatile("cp.async.wait_group 1;" ::: "memory");
         float o[K][8];
 #pragma unroll
-        for (int i = 0; i < K; ++i) floats8(o[i], rf[i], a.type_f);
+        for (int i = 0; i < K; ++i) {
+            const int v = 2 * (lane + (i << a.log));
+#pragma unroll
+            for (int j = 0; j < 8; ++j) o[i][j] = 0.f;
+            if (in && (U || v < a.nvec)) taken(o[i], slots_f, f_slots, i, type_f, v + 1 < a.nvec);
+        }
+        request(slots_f, f_slots, a.f, after, type_f, e_next < E);
         float m = 0.f, r = 1.f;
-        if (a.par.p[POST_W]) {
+        if (post) {
             float s = 0.f, q = 0.f;
 #pragma unroll
             for (int i = 0; i < K; ++i)
@@ -118,7 +191,7 @@ __global__ void __launch_bounds__(kResThreads, K <= 1 ? 4 : K <= 2 ? 3 : 2) resi
                 const int v = 2 * (lane + (i << a.log));
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    if (v + j / 4 >= a.nvec) continue;
+                    if (!U && v + (WIDE ? 0 : j / 4) >= a.nvec) continue;
                     o[i][j] -= m;
                     q += o[i][j] * o[i][j];
                 }
@@ -126,32 +199,27 @@ __global__ void __launch_bounds__(kResThreads, K <= 1 ? 4 : K <= 2 ? 3 : 2) resi
             r = rsqrtf(group_sum(q, a.log) * a.inv_c + a.eps);
         }
         float s2 = 0.f;
+        asm volatile("cp.async.wait_group 1;" ::: "memory");
 #pragma unroll
         for (int i = 0; i < K; ++i) {
             const int v = 2 * (lane + (i << a.log));
-            if (!in || v >= a.nvec) continue;
+            if (!in || (!U && v >= a.nvec)) continue;
             const bool hi = WIDE || v + 1 < a.nvec;
             float w[8], c[8], x[8];
-            param8(w, par[POST_W], e * a.nvec + v, hi, 1.f);
-            param8(c, par[POST_B], e * a.nvec + v, hi, 0.f);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) o[i][j] = o[i][j] * r * w[j] + c[j];
-            if (a.drop.threshold) {
-                const uint4 bits = dropout_bits(seed, row, (uint32_t)(v >> 1));
-#pragma unroll
-                for (int j = 0; j < 8; ++j) o[i][j] = dropout_keeps(bits, j, a.drop.threshold) ? o[i][j] * a.drop.factor : 0.f;
-            }
-            param8(w, par[SCALE], e * a.nvec + v, hi, 1.f);
-            floats8(x, rx[i], a.type_x);
+            param8(w, SIDE_W, e * a.nvec + v, hi);
+            param8(c, SIDE_B, e * a.nvec + v, hi);
+            taken(x, slots_x, x_slots, i, type_x, hi);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                o[i][j] = x[j] + w[j] * gate * o[i][j];
+                const float t = x[j] + gate * (o[i][j] * r * w[j] + c[j]);
+                o[i][j] = !drop || dropout_keeps(bits[i], j, a.drop.above) ? t : x[j];
                 if (WIDE || j < 4 || hi) s2 += o[i][j];
             }
-            store8<WIDE>(a.out, (size_t)row * a.nvec + v, hi, o[i], a.type_x);
+            store8<WIDE>(a.out, (size_t)row * a.nvec + v, hi, o[i], type_x);
         }
+        request(slots_x, x_slots, a.x, after, type_x, e_next < E);
         float m2 = 0.f, r2 = 1.f;
-        if (a.par.p[PRE_W]) {
+        if (pre) {
             m2 = group_sum(s2, a.log) * a.inv_c;
             float q = 0.f;
 #pragma unroll
@@ -159,7 +227,7 @@ __global__ void __launch_bounds__(kResThreads, K <= 1 ? 4 : K <= 2 ? 3 : 2) resi
                 const int v = 2 * (lane + (i << a.log));
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    if (v + j / 4 >= a.nvec) continue;
+                    if (!U && v + (WIDE ? 0 : j / 4) >= a.nvec) continue;
                     o[i][j] -= m2;
                     q += o[i][j] * o[i][j];
                 }
@@ -168,14 +236,14 @@ __global__ void __launch_bounds__(kResThreads, K <= 1 ? 4 : K <= 2 ? 3 : 2) resi
 #pragma unroll
             for (int i = 0; i < K; ++i) {
                 const int v = 2 * (lane + (i << a.log));
-                if (!in || v >= a.nvec) continue;
+                if (!in || (!U && v >= a.nvec)) continue;
                 const bool hi = WIDE || v + 1 < a.nvec;
                 float w[8], c[8];
-                param8(w, par[PRE_W], e * a.nvec + v, hi, 1.f);
-                param8(c, par[PRE_B], e * a.nvec + v, hi, 0.f);
+                param8(w, NEXT_W, e * a.nvec + v, hi);
+                param8(c, NEXT_B, e * a.nvec + v, hi);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) o[i][j] = o[i][j] * r2 * w[j] + c[j];
-                store8<WIDE>(a.y, (size_t)row * a.nvec + v, hi, o[i], a.type_y);
+                store8<WIDE>(a.y, (size_t)row * a.nvec + v, hi, o[i], type_y);
             }
         }
         if (lane == 0 && in && a.stats) a.stats[row] = make_float4(m, r, m2, r2);
@@ -198,21 +266,36 @@ struct ResGradArgs {
     float* part;                             // [gridDim.x + E][4][C]: S2, S1, dw', db' of a CTA's rows of an expert
     int* share;                              // [E][2]: first CTA with rows of the expert and the one behind the last
     float inv_c;
-    int nvec, log, type_x, type_f, type_y;
+    int nvec, lanes, type_x, type_f, type_y; // lanes of a row, any number up to 32
 };
 
-// The rows are taken expert by expert, an equal run of them per CTA, which sums its rows of an expert before it goes to the next;
-// entry i + e of `part` holds those of CTA i and expert e (along the run of all rows either i or e goes up, so no two share one).
-// The sums stay in registers for rows of up to 256 channels (K = 1); wider rows, whose values alone fill the registers, have them
-// in shared memory, an entry per warp and column that one lane adds to.
-template <int K, bool WIDE>
-__global__ void __launch_bounds__(kResThreads, K == 1 ? 2 : 1) residual_grad_kernel(ResGradArgs a) {
-    constexpr bool kInShared = K > 1;
-    constexpr int kWarps = kResThreads / 32;
-    __shared__ int bounds[kMaxBounds];
-    __shared__ int start[kMaxSegments + 1];
-    __shared__ int run[2];
-    extern __shared__ float4 sums[];         // [warps][4][nvec]
+// Sums of N values over the lanes of a row's group, `l` a lane's place in it and `base` the warp's lane of its first; every
+// lane gets them.  Any number of lanes: rows of 80 channels take ten, three of them a warp.  `even`: a power of two.
+template <int N>
+__device__ __forceinline__ void group_sums(float (&v)[N], int lanes, bool even, int l, int base) {
+    if (even) {
+        for (int d = 1; d < lanes; d <<= 1) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(0xFFFFFFFFu, v[i], d);
+        }
+        return;
+    }
+    for (int n = lanes; n > 1;) {
+        const int half = (n + 1) >> 1;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const float x = __shfl_down_sync(0xFFFFFFFFu, v[i], half);
+            if (l + half < n) v[i] += x;
+        }
+        n = half;
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = __shfl_sync(0xFFFFFFFFu, v[i], base);
+}
+
+// The run of rows that a CTA has, as a part of all rows expert by expert.  The first CTA notes which CTAs have rows of an expert.
+// Called by a whole CTA; false: it has none.
+__device__ __forceinline__ bool take_run(const ResGradArgs& a, int* bounds, int* start, int* run) {
     load_bounds(a.seg, bounds);
     segment_starts(a.seg, bounds, 1, start);
     const int B = a.seg.B, E = a.seg.E, total = start[B * E], ctas = min((int)gridDim.x, total);
@@ -221,185 +304,415 @@ __global__ void __launch_bounds__(kResThreads, K == 1 ? 2 : 1) residual_grad_ker
         a.share[2 * threadIdx.x] = from < to ? (int)(((from + 1) * ctas - 1) / total) : 0;
         a.share[2 * threadIdx.x + 1] = from < to ? (int)((to * ctas - 1) / total) + 1 : 0;
     }
-    if ((int)blockIdx.x >= ctas) return;
+    if ((int)blockIdx.x >= ctas) return false;
     if (threadIdx.x < 2) run[threadIdx.x] = (int)((long long)total * (blockIdx.x + threadIdx.x) / ctas);
     __syncthreads();
-    const int lanes = 1 << a.log, lane = threadIdx.x & (lanes - 1), warp = threadIdx.x >> 5;
-    const int per_warp = 32 >> a.log, sub = (threadIdx.x & 31) >> a.log, step = kResThreads >> a.log;
-    const bool pre = a.par.p[PRE_W] != nullptr, post = a.par.p[POST_W] != nullptr;
+    return true;
+}
+// Rows at places of the run of an expert's rows, for ascending places.
+struct RowAt {
+    const int *bounds, *start;
+    int N, E, e, b, until, shift;
+    __device__ __forceinline__ RowAt(const ResGradArgs& a, const int* bounds_, const int* start_, int e_)
+        : bounds(bounds_), start(start_ + e_ * a.seg.B), N(a.seg.N), E(a.seg.E), e(e_), b(-1), until(start[0]), shift(0) {}
+    __device__ __forceinline__ uint32_t operator()(int p) {
+        while (p >= until) {                                      // p is before the end of the expert's rows
+            ++b;
+            shift = b * N + bounds[b * (E + 1) + e] - start[b];
+            until = start[b + 1];
+        }
+        return (uint32_t)(p + shift);
+    }
+};
+// Sums of the warps, [warps][4][nvec], in their order to the entry of the CTA and expert.
+template <int THREADS>
+__device__ __forceinline__ void give_sums(const ResGradArgs& a, const float4* sums, int e) {
+    __syncthreads();
+    float4* part = reinterpret_cast<float4*>(a.part) + (size_t)(blockIdx.x + e) * 4 * a.nvec;
+    for (int v = threadIdx.x; v < 4 * a.nvec; v += THREADS) {
+        float4 o = sums[v];
+        for (int w = 1; w < THREADS / 32; ++w) {
+            const float4 y = sums[w * 4 * a.nvec + v];
+            o.x += y.x; o.y += y.y; o.z += y.z; o.w += y.w;
+        }
+        part[v] = o;
+    }
+    __syncthreads();
+}
+
+// Rows of up to 256 channels, eight per lane.  The rows are taken expert by expert, an equal run of them per CTA, which sums its rows of an
+// expert before it goes to the next; entry i + e of `part` holds those of CTA i and expert e (along the run of all rows either i or e
+// goes up, so no two share one).  The sums stay in registers; a group of lanes has two rows in work, whose waits for one another's lanes
+// and for shared memory fill each other, and the next two on their way to shared memory, for which no registers are left.
+constexpr int kNarrowThreads = 128;
+constexpr int kNarrowCtas = 3;               // per SM
+constexpr uint32_t kNarrowSlot = kNarrowThreads * 16;
+template <bool WIDE, int U, bool DROP>
+__global__ void __launch_bounds__(kNarrowThreads, kNarrowCtas) residual_grad_kernel(ResGradArgs a) {
+    constexpr int kWarps = kNarrowThreads / 32;
+    __shared__ int bounds[kMaxBounds];
+    __shared__ int start[kMaxSegments + 1];
+    __shared__ int run[2];
+    __shared__ float4 folded[kFolded - 1][64];                    // the expert's s w, s b and w'
+    extern __shared__ float4 sums[];         // [warps][4][nvec]; before that two stages of two rows
+    if (!take_run(a, bounds, start, run)) return;
+    const int B = a.seg.B, E = a.seg.E;
+    const int type_x = rows_type<U>(a.type_x), type_f = block_type<U>(a.type_f), type_y = block_type<U>(a.type_y);
+    const int lanes = a.lanes, warp = threadIdx.x >> 5, per_warp = 32 / lanes;
+    const int sub = (threadIdx.x & 31) / lanes, base = sub * lanes, l = (threadIdx.x & 31) - base, step = kWarps * per_warp;
+    const bool pre = U || a.par.p[PRE_W] != nullptr, post = U || a.par.p[POST_W] != nullptr, behind = U || a.dout, noted = U || a.stats;
+    const bool drop = U ? DROP : a.drop.any != 0, even = (lanes & (lanes - 1)) == 0, active = sub < per_warp, hi = WIDE || 2 * l + 1 < a.nvec;
     DropoutSeed seed = {};
-    if (a.drop.threshold) seed = dropout_seed(a.drop);
+    if (drop) seed = dropout_seed(a.drop);
+    // Where a row's places have what; all of a thread's are 16 bytes at its number.
+    const uint32_t at_y = (pre ? (type_x == EMC2_F32 ? 2u : 1u) : 0u) * kNarrowSlot;
+    const uint32_t at_d = at_y + (pre ? (type_y == EMC2_F32 ? 2u : 1u) : 0u) * kNarrowSlot;
+    const uint32_t at_f = at_d + (behind ? (type_x == EMC2_F32 ? 2u : 1u) : 0u) * kNarrowSlot;
+    const uint32_t at_s = at_f + (type_f == EMC2_F32 ? 2u : 1u) * kNarrowSlot;
+    const uint32_t at_g = at_s + (noted ? kNarrowSlot : 0u), row_bytes = at_g + (a.gate ? kNarrowSlot : 0u);
+    char* const ring = reinterpret_cast<char*>(sums) + threadIdx.x * 16;
+    const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring);
+    for (int e = segment_of(start, B * E, run[0]) / B; e < E && start[e * B] < run[1]; ++e) {
+        const int from = max(run[0], start[e * B]), to = min(run[1], start[(e + 1) * B]);
+        if (from >= to) continue;
+        for (int v = threadIdx.x; v < a.nvec; v += kNarrowThreads)
+            for (int i = SIDE_W; i <= NEXT_W; ++i) folded[i][v] = folded_param(a.par, i, e * a.nvec + v);
+        __syncthreads();
+        auto param8 = [&](float (&f)[8], int i) {
+            const float4 x = folded[i][2 * l];
+            float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (hi) y = folded[i][2 * l + 1];
+            f[0] = x.x; f[1] = x.y; f[2] = x.z; f[3] = x.w;
+            f[4] = y.x; f[5] = y.y; f[6] = y.z; f[7] = y.w;
+        };
+        float acc[4][8];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) acc[i][j] = 0.f;
+        RowAt row_at(a, bounds, start, e);
+        uint32_t next[2];
+        auto request = [&](int p, uint32_t dst) {
+#pragma unroll
+            for (int k = 0; k < 2; ++k, p += step, dst += row_bytes) {
+                next[k] = 0;
+                if (p >= to || !active) continue;
+                const uint32_t row = next[k] = row_at(p);
+                const uint32_t at = row * (uint32_t)a.nvec + 2 * l;             // 2^24 rows of 64 vectors at most
+                if (pre) {
+                    ahead8<WIDE, kNarrowSlot>(dst, a.o, at, hi, type_x);
+                    ahead8<WIDE, kNarrowSlot>(dst + at_y, a.dy, at, hi, type_y);
+                }
+                if (behind) ahead8<WIDE, kNarrowSlot>(dst + at_d, a.dout, at, hi, type_x);
+                ahead8<WIDE, kNarrowSlot>(dst + at_f, a.f, at, hi, type_f);
+                if (noted) copy_ahead<16>(dst + at_s, a.stats + row);
+                if (a.gate) copy_ahead<4>(dst + at_g, a.gate + row);
+            }
+            asm volatile("cp.async.commit_group;" ::: "memory");
+        };
+        const int first = from + warp * per_warp + sub;
+        uint32_t stage = 0;
+        request(first, ring_at);
+        // A warp goes on while any of its groups has a row.
+        for (int p = first; p - sub < to; p += 2 * step) {
+            const bool in[2] = {active && p < to, active && p + step < to};
+            const uint32_t row[2] = {next[0], next[1]};
+            const char* at = ring + stage * 2 * row_bytes;
+            stage ^= 1;
+            request(p + 2 * step, ring_at + stage * 2 * row_bytes);
+            uint4 bits[2];
+            if (drop) {                                           // while the rows are on their way
+                const uint32_t group[2] = {(uint32_t)l, (uint32_t)l};
+                dropout_bits(bits, seed, row, group);
+            }
+            asm volatile("cp.async.wait_group 1;" ::: "memory");
+            // Lanes without a row go on with zeros, which add nothing.
+            float d[2][8], h[2][8], gate[2];
+            float4 st[2];
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                auto taken = [&](float (&f)[8], uint32_t slot, int type) {
+                    Raw8 raw;
+                    raw.a = raw.b = make_uint4(0u, 0u, 0u, 0u);
+                    if (in[k]) raw = slot8<kNarrowSlot>(at + k * row_bytes + slot, type);
+                    if (!WIDE && !hi) clear_second(raw, type);
+                    floats8(f, raw, type);
+                };
+                st[k] = make_float4(0.f, 1.f, 0.f, 1.f);
+                if (noted && in[k]) st[k] = *reinterpret_cast<const float4*>(at + k * row_bytes + at_s);
+                gate[k] = 1.0f;
+                if (a.gate && in[k]) gate[k] = *reinterpret_cast<const float*>(at + k * row_bytes + at_g);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) d[k][j] = 0.f;
+                if (behind) taken(d[k], at_d, type_x);
+                taken(h[k], at_f, type_f);
+            }
+            if (pre) {
+                float o[2][8], g[2][8], w[8], means[4] = {0.f, 0.f, 0.f, 0.f};
+                param8(w, NEXT_W);
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    auto taken = [&](float (&f)[8], uint32_t slot, int type) {
+                        Raw8 raw;
+                        raw.a = raw.b = make_uint4(0u, 0u, 0u, 0u);
+                        if (in[k]) raw = slot8<kNarrowSlot>(at + k * row_bytes + slot, type);
+                        if (!WIDE && !hi) clear_second(raw, type);
+                        floats8(f, raw, type);
+                    };
+                    taken(o[k], 0, type_x);
+                    taken(g[k], at_y, type_y);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        o[k][j] = (o[k][j] - st[k].z) * st[k].w;
+                        if (!WIDE && j >= 4 && !hi) o[k][j] = 0.f;
+                        acc[2][j] += g[k][j] * o[k][j];
+                        acc[3][j] += g[k][j];
+                        g[k][j] *= w[j];
+                        means[k] += g[k][j];
+                        means[2 + k] += g[k][j] * o[k][j];
+                    }
+                }
+                group_sums(means, lanes, even, l, base);
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const float m = means[k] * a.inv_c, t = means[2 + k] * a.inv_c;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) d[k][j] += st[k].w * ((g[k][j] - m) - o[k][j] * t);
+                }
+            }
+            float w[8], means[6] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+            param8(w, SIDE_W);
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                if (in[k]) store8<WIDE>(a.dx, (size_t)row[k] * a.nvec + 2 * l, hi, d[k], type_x);
+                // What is dropped passes nothing on, whatever it holds; behind a norm no element of a row with NaN or infinities has a
+                // value.
+                if (drop) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        d[k][j] = dropout_keeps(bits[k], j, a.drop.above) ? d[k][j] : 0.f;
+                        if (!post) h[k][j] = dropout_keeps(bits[k], j, a.drop.above) ? h[k][j] : 0.f;
+                    }
+                }
+                if (post) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) h[k][j] = (h[k][j] - st[k].x) * st[k].y;
+                }
+                if (!WIDE && !hi) {
+#pragma unroll
+                    for (int j = 4; j < 8; ++j) d[k][j] = h[k][j] = 0.f;
+                }
+            }
+            if (a.dgate) {
+                float c[8];
+                param8(c, SIDE_B);
+#pragma unroll
+                for (int k = 0; k < 2; ++k)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) means[4 + k] += d[k][j] * (h[k][j] * w[j] + c[j]);
+            }
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const float through = drop ? a.drop.factor * gate[k] : gate[k];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    d[k][j] *= through;
+                    acc[1][j] += d[k][j];
+                    acc[0][j] += d[k][j] * h[k][j];
+                    d[k][j] *= w[j];
+                    means[k] += d[k][j];
+                    means[2 + k] += d[k][j] * h[k][j];
+                }
+            }
+            if (post || a.dgate) group_sums(means, lanes, even, l, base);
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                if (!in[k]) continue;
+                if (a.dgate && l == 0) a.dgate[row[k]] = drop ? means[4 + k] * a.drop.factor : means[4 + k];
+                if (post) {
+                    const float m = means[k] * a.inv_c, t = means[2 + k] * a.inv_c;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) d[k][j] = st[k].y * ((d[k][j] - m) - h[k][j] * t);
+                }
+                store8<WIDE>(a.df, (size_t)row[k] * a.nvec + 2 * l, hi, d[k], type_f);
+            }
+        }
+        asm volatile("cp.async.wait_group 0;" ::: "memory");
+        __syncthreads();                                          // every thread is done with its stages
+        // The groups of a warp hold the same columns at the same places.
+        float4* mine = sums + warp * 4 * a.nvec + 2 * l;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                float total = acc[i][j];
+                for (int w = 1; w < per_warp; ++w) total += __shfl_sync(0xFFFFFFFFu, acc[i][j], (l + w * lanes) & 31);
+                acc[i][j] = total;
+            }
+            if (sub == 0) {
+                mine[i * a.nvec] = make_float4(acc[i][0], acc[i][1], acc[i][2], acc[i][3]);
+                if (hi) mine[i * a.nvec + 1] = make_float4(acc[i][4], acc[i][5], acc[i][6], acc[i][7]);
+            }
+        }
+        give_sums<kNarrowThreads>(a, sums, e);
+    }
+}
+
+// Wider rows, K groups of eight channels per lane of a warp, whose values fill the registers: the sums are in shared memory, an entry per
+// warp and column that one lane adds to, and nothing is requested ahead.
+template <int K, bool WIDE>
+__global__ void __launch_bounds__(kResThreads, 1) residual_grad_wide_kernel(ResGradArgs a) {
+    constexpr int kWarps = kResThreads / 32;
+    __shared__ int bounds[kMaxBounds];
+    __shared__ int start[kMaxSegments + 1];
+    __shared__ int run[2];
+    __shared__ float4 folded[kFolded - 1][64 * K];
+    extern __shared__ float4 sums[];         // [warps][4][nvec]
+    if (!take_run(a, bounds, start, run)) return;
+    const int B = a.seg.B, E = a.seg.E, type_x = a.type_x, type_f = a.type_f, type_y = a.type_y;
+    const int warp = threadIdx.x >> 5, l = threadIdx.x & 31;
+    const bool pre = a.par.p[PRE_W] != nullptr, post = a.par.p[POST_W] != nullptr, drop = a.drop.any != 0;
+    DropoutSeed seed = {};
+    if (drop) seed = dropout_seed(a.drop);
     float4* mine = sums + warp * 4 * a.nvec;
     for (int e = segment_of(start, B * E, run[0]) / B; e < E && start[e * B] < run[1]; ++e) {
         const int from = max(run[0], start[e * B]), to = min(run[1], start[(e + 1) * B]);
         if (from >= to) continue;
-        const float4* par[kParams];
-#pragma unroll
-        for (int i = 0; i < kParams; ++i) par[i] = a.par.p[i] ? reinterpret_cast<const float4*>(a.par.p[i]) + e * a.nvec : nullptr;
-        float acc[kInShared ? 1 : 4][8];
-        if (kInShared) {
-            for (int v = threadIdx.x; v < kWarps * 4 * a.nvec; v += kResThreads) sums[v] = make_float4(0.f, 0.f, 0.f, 0.f);
-            __syncthreads();
-        } else {
-#pragma unroll
-            for (int i = 0; i < (kInShared ? 1 : 4); ++i)
-#pragma unroll
-                for (int j = 0; j < 8; ++j) acc[i][j] = 0.f;
-        }
-        auto add = [&](int plane, int i, int v, bool hi, const float (&t)[8]) {
-            if (!kInShared) {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) acc[kInShared ? 0 : plane][j] += t[j];
-                return;
-            }
+        for (int v = threadIdx.x; v < a.nvec; v += kResThreads)
+            for (int i = SIDE_W; i <= NEXT_W; ++i) folded[i][v] = folded_param(a.par, i, e * a.nvec + v);
+        for (int v = threadIdx.x; v < kWarps * 4 * a.nvec; v += kResThreads) sums[v] = make_float4(0.f, 0.f, 0.f, 0.f);
+        __syncthreads();
+        auto param8 = [&](float (&f)[8], int i, int v, bool hi) {
+            const float4 x = folded[i][v];
+            float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (hi) y = folded[i][v + 1];
+            f[0] = x.x; f[1] = x.y; f[2] = x.z; f[3] = x.w;
+            f[4] = y.x; f[5] = y.y; f[6] = y.z; f[7] = y.w;
+        };
+        // t w to a sum, per channel.
+        auto add = [&](int plane, int v, bool hi, const float (&t)[8], const float (&w)[8]) {
             float4* at = mine + plane * a.nvec + v;
             float4 s = at[0];
-            at[0] = make_float4(s.x + t[0], s.y + t[1], s.z + t[2], s.w + t[3]);
+            at[0] = make_float4(s.x + t[0] * w[0], s.y + t[1] * w[1], s.z + t[2] * w[2], s.w + t[3] * w[3]);
             if (!hi) return;
             s = at[1];
-            at[1] = make_float4(s.x + t[4], s.y + t[5], s.z + t[6], s.w + t[7]);
+            at[1] = make_float4(s.x + t[4] * w[4], s.y + t[5] * w[5], s.z + t[6] * w[6], s.w + t[7] * w[7]);
         };
-        int q = e * B;
-        // A warp goes on while any of its groups has a row.
-        for (int p = from + warp * per_warp + sub; p - sub < to; p += step) {
-            const bool in = p < to;
-            uint32_t row = 0;
-            if (in) {
-                while (p >= start[q + 1]) ++q;                    // p < start[(e + 1) * B]
-                const int b = q - e * B;
-                row = (uint32_t)(b * a.seg.N + bounds[b * (E + 1) + e] + (p - start[q]));
-            }
+        const float ones[8] = {1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f};
+        RowAt row_at(a, bounds, start, e);
+        for (int p = from + warp; p < to; p += kWarps) {
+            const uint32_t row = row_at(p);
             Raw8 ro[K], rf[K], rd[K], ry[K];
 #pragma unroll
             for (int i = 0; i < K; ++i) {
-                const int v = 2 * (lane + (i << a.log));
-                const bool lo = in && v < a.nvec, hi = in && v + 1 < a.nvec;
+                const int v = 2 * (l + i * 32);
+                const bool lo = v < a.nvec, hi = v + 1 < a.nvec;
                 const size_t at = (size_t)row * a.nvec + v;
                 if (pre) {
-                    ro[i] = request8<WIDE>(a.o, at, lo, hi, a.type_x);
-                    ry[i] = request8<WIDE>(a.dy, at, lo, hi, a.type_y);
+                    ro[i] = request8<WIDE>(a.o, at, lo, hi, type_x);
+                    ry[i] = request8<WIDE>(a.dy, at, lo, hi, type_y);
                 }
-                rd[i] = request8<WIDE>(a.dout, at, lo && a.dout, hi && a.dout, a.type_x);
-                rf[i] = request8<WIDE>(a.f, at, lo, hi, a.type_f);
+                rd[i] = request8<WIDE>(a.dout, at, lo && a.dout, hi && a.dout, type_x);
+                rf[i] = request8<WIDE>(a.f, at, lo, hi, type_f);
             }
-            float4 st = make_float4(0.f, 1.f, 0.f, 1.f);
-            if (in && a.stats) st = __ldg(a.stats + row);
-            const float gate = in && a.gate ? __ldg(a.gate + row) : 1.0f;
+            const float4 st = a.stats ? __ldg(a.stats + row) : make_float4(0.f, 1.f, 0.f, 1.f);
+            const float gate = a.gate ? __ldg(a.gate + row) : 1.0f;
             float d[K][8];
 #pragma unroll
-            for (int i = 0; i < K; ++i) floats8(d[i], rd[i], a.type_x);
+            for (int i = 0; i < K; ++i) floats8(d[i], rd[i], type_x);
             if (pre) {
-                float o[K][8], g[K][8], s = 0.f, t = 0.f;
+                float o[K][8], g[K][8], means[2] = {0.f, 0.f};
 #pragma unroll
                 for (int i = 0; i < K; ++i) {
-                    const int v = 2 * (lane + (i << a.log));
-                    floats8(o[i], ro[i], a.type_x);
-                    floats8(g[i], ry[i], a.type_y);
-                    if (!in || v >= a.nvec) continue;
+                    const int v = 2 * (l + i * 32);
+                    floats8(o[i], ro[i], type_x);
+                    floats8(g[i], ry[i], type_y);
+                    if (v >= a.nvec) continue;
                     const bool hi = WIDE || v + 1 < a.nvec;
                     float w[8];
-                    add(3, i, v, hi, g[i]);
+                    param8(w, NEXT_W, v, hi);
 #pragma unroll
                     for (int j = 0; j < 8; ++j) {
                         o[i][j] = (o[i][j] - st.z) * st.w;
                         if (!WIDE && j >= 4 && !hi) o[i][j] = 0.f;
-                        w[j] = g[i][j] * o[i][j];
                     }
-                    add(2, i, v, hi, w);
-                    param8(w, par[PRE_W], v, hi, 0.f);
+                    add(3, v, hi, g[i], ones);
+                    add(2, v, hi, g[i], o[i]);
 #pragma unroll
                     for (int j = 0; j < 8; ++j) {
                         g[i][j] *= w[j];
-                        s += g[i][j];
-                        t += g[i][j] * o[i][j];
+                        means[0] += g[i][j];
+                        means[1] += g[i][j] * o[i][j];
                     }
                 }
-                s = group_sum(s, a.log) * a.inv_c;
-                t = group_sum(t, a.log) * a.inv_c;
+                group_sums(means, 32, true, l, 0);
+                const float m = means[0] * a.inv_c, t = means[1] * a.inv_c;
 #pragma unroll
                 for (int i = 0; i < K; ++i)
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) d[i][j] += st.w * (g[i][j] - s - o[i][j] * t);
+                    for (int j = 0; j < 8; ++j) d[i][j] += st.w * ((g[i][j] - m) - o[i][j] * t);
             }
-            float h[K][8], s = 0.f, t = 0.f, u = 0.f;
+            float h[K][8], means[3] = {0.f, 0.f, 0.f};
+            const float through = drop ? a.drop.factor * gate : gate;
 #pragma unroll
             for (int i = 0; i < K; ++i) {
-                const int v = 2 * (lane + (i << a.log));
-                floats8(h[i], rf[i], a.type_f);
-                if (!in || v >= a.nvec) continue;
+                const int v = 2 * (l + i * 32);
+                floats8(h[i], rf[i], type_f);
+                if (v >= a.nvec) continue;
                 const bool hi = WIDE || v + 1 < a.nvec;
-                store8<WIDE>(a.dx, (size_t)row * a.nvec + v, hi, d[i], a.type_x);
-                uint4 bits = make_uint4(0u, 0u, 0u, 0u);
-                if (a.drop.threshold) bits = dropout_bits(seed, row, (uint32_t)(v >> 1));
+                store8<WIDE>(a.dx, (size_t)row * a.nvec + v, hi, d[i], type_x);
                 float w[8], c[8];
-                param8(w, par[POST_W], v, hi, 1.f);
-                param8(c, par[POST_B], v, hi, 0.f);
-                float sc[8], k[8];
-                param8(sc, par[SCALE], v, hi, 1.f);
-                // What is dropped passes nothing on, whatever it holds.
+                param8(w, SIDE_W, v, hi);
+                param8(c, SIDE_B, v, hi);
+                // As above.
+                if (drop) {
+                    uint4 bits[1];
+                    const uint32_t of[1] = {row}, group[1] = {(uint32_t)(l + i * 32)};
+                    dropout_bits(bits, seed, of, group);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const bool kept = (!a.drop.threshold || dropout_keeps(bits, j, a.drop.threshold)) && (WIDE || j < 4 || hi);
-                    h[i][j] = (h[i][j] - st.x) * st.y;
-                    const float through = kept ? (a.drop.threshold ? d[i][j] * a.drop.factor : d[i][j]) : 0.f;
-                    u += kept ? sc[j] * through * (h[i][j] * w[j] + c[j]) : 0.f;
-                    d[i][j] = through * gate;
-                    k[j] = kept ? d[i][j] * h[i][j] : 0.f;
+                    for (int j = 0; j < 8; ++j) {
+                        d[i][j] = dropout_keeps(bits[0], j, a.drop.above) ? d[i][j] : 0.f;
+                        if (!post) h[i][j] = dropout_keeps(bits[0], j, a.drop.above) ? h[i][j] : 0.f;
+                    }
                 }
-                add(1, i, v, hi, d[i]);
-                add(0, i, v, hi, k);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    d[i][j] *= sc[j] * w[j];
-                    if (!WIDE && j >= 4 && !hi) h[i][j] = 0.f;
-                    s += d[i][j];
-                    t += d[i][j] * h[i][j];
-                }
-            }
-            if (post) {
-                s = group_sum(s, a.log) * a.inv_c;
-                t = group_sum(t, a.log) * a.inv_c;
-            }
-            if (a.dgate) {
-                u = group_sum(u, a.log);
-                if (in && lane == 0) a.dgate[row] = u;
-            }
-#pragma unroll
-            for (int i = 0; i < K; ++i) {
-                const int v = 2 * (lane + (i << a.log));
-                if (!in || v >= a.nvec) continue;
                 if (post) {
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) d[i][j] = st.y * (d[i][j] - s - h[i][j] * t);
+                    for (int j = 0; j < 8; ++j) h[i][j] = (h[i][j] - st.x) * st.y;
                 }
-                store8<WIDE>(a.df, (size_t)row * a.nvec + v, WIDE || v + 1 < a.nvec, d[i], a.type_f);
-            }
-        }
-        // The groups of a warp hold the same columns in the same lanes, then the warps' sums in their order.
-        if (!kInShared) {
-            const int v = 2 * lane;
+                if (!WIDE && !hi) {
 #pragma unroll
-            for (int i = 0; i < (kInShared ? 1 : 4); ++i) {
+                    for (int j = 4; j < 8; ++j) d[i][j] = h[i][j] = 0.f;
+                }
+                if (a.dgate) {
 #pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    for (int w = lanes; w < 32; w <<= 1) acc[i][j] += __shfl_xor_sync(0xFFFFFFFFu, acc[i][j], w);
-                if (sub == 0 && v < a.nvec) {
-                    mine[i * a.nvec + v] = make_float4(acc[i][0], acc[i][1], acc[i][2], acc[i][3]);
-                    if (v + 1 < a.nvec) mine[i * a.nvec + v + 1] = make_float4(acc[i][4], acc[i][5], acc[i][6], acc[i][7]);
+                    for (int j = 0; j < 8; ++j) means[2] += d[i][j] * (h[i][j] * w[j] + c[j]);
+                }
+#pragma unroll
+                for (int j = 0; j < 8; ++j) d[i][j] *= through;
+                add(1, v, hi, d[i], ones);
+                add(0, v, hi, d[i], h[i]);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    d[i][j] *= w[j];
+                    means[0] += d[i][j];
+                    means[1] += d[i][j] * h[i][j];
                 }
             }
-        }
-        __syncthreads();
-        float4* part = reinterpret_cast<float4*>(a.part) + (size_t)(blockIdx.x + e) * 4 * a.nvec;
-        for (int v = threadIdx.x; v < 4 * a.nvec; v += kResThreads) {
-            float4 o = sums[v];
-            for (int w = 1; w < kWarps; ++w) {
-                const float4 y = sums[w * 4 * a.nvec + v];
-                o.x += y.x; o.y += y.y; o.z += y.z; o.w += y.w;
+            if (post || a.dgate) group_sums(means, 32, true, l, 0);
+            if (a.dgate && l == 0) a.dgate[row] = drop ? means[2] * a.drop.factor : means[2];
+            const float m = means[0] * a.inv_c, t = means[1] * a.inv_c;
+#pragma unroll
+            for (int i = 0; i < K; ++i) {
+                const int v = 2 * (l + i * 32);
+                if (v >= a.nvec) continue;
+                if (post) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) d[i][j] = st.y * ((d[i][j] - m) - h[i][j] * t);
+                }
+                store8<WIDE>(a.df, (size_t)row * a.nvec + v, WIDE || v + 1 < a.nvec, d[i], type_f);
             }
-            part[v] = o;
         }
-        __syncthreads();
+        give_sums<kResThreads>(a, sums, e);
     }
 }
 
@@ -448,29 +761,53 @@ __global__ void __launch_bounds__(kResSumThreads) residual_sum_kernel(const __gr
 
 template <int K>
 struct Residual {
-    static cudaError_t go(const ResArgs& a, bool wide, int ctas, size_t shared, cudaStream_t st) {
-        if (wide) residual_kernel<K, true><<<ctas, kResThreads, shared, st>>>(a);
-        else residual_kernel<K, false><<<ctas, kResThreads, shared, st>>>(a);
-        return cudaSuccess;
-    }
-};
-template <int K>
-struct ResidualGrad {
-    static cudaError_t go(const ResGradArgs& a, bool wide, int ctas, size_t shared, cudaStream_t st) {
-        auto kernel = wide ? residual_grad_kernel<K, true> : residual_grad_kernel<K, false>;
-        if (shared > 24 * 1024) {            // the sums of eight warps, four of up to 64 * K vectors each
-            const cudaError_t e = allow_shared(kernel, (size_t)(kResThreads / 32) * 4 * 64 * K * sizeof(float4));
+    template <typename F>
+    static cudaError_t go(F kernel, const ResArgs& a, int ctas, size_t shared, cudaStream_t st) {
+        if (shared > 24 * 1024) {
+            const cudaError_t e = allow_shared(kernel, kResShared + K * 4 * kSlotBytes);
             if (e != cudaSuccess) return e;
         }
         kernel<<<ctas, kResThreads, shared, st>>>(a);
         return cudaSuccess;
     }
+    static cudaError_t go(const ResArgs& a, bool wide, int usual, int ctas, cudaStream_t st) {
+        auto slots = [](int type) { return type == EMC2_F32 ? 2 : 1; };
+        const size_t shared = a.params_bytes + (size_t)K * (slots(a.type_x) + slots(a.type_f)) * kSlotBytes;
+        if (usual == F32_ROWS)
+            return a.drop.any ? go(residual_kernel<K, true, F32_ROWS, true>, a, ctas, shared, st) : go(residual_kernel<K, true, F32_ROWS, false>, a, ctas, shared, st);
+        if (usual == BF16_ROWS)
+            return a.drop.any ? go(residual_kernel<K, true, BF16_ROWS, true>, a, ctas, shared, st) : go(residual_kernel<K, true, BF16_ROWS, false>, a, ctas, shared, st);
+        return wide ? go(residual_kernel<K, true, ANY, true>, a, ctas, shared, st) : go(residual_kernel<K, false, ANY, true>, a, ctas, shared, st);
+    }
 };
+template <typename F>
+cudaError_t launch_grad(F kernel, const ResGradArgs& a, int ctas, int threads, size_t shared, size_t most, cudaStream_t st) {
+    if (shared > 24 * 1024) {
+        const cudaError_t e = allow_shared(kernel, most);
+        if (e != cudaSuccess) return e;
+    }
+    kernel<<<ctas, threads, shared, st>>>(a);
+    return cudaSuccess;
+}
+cudaError_t launch_narrow(const ResGradArgs& a, bool wide, int usual, int ctas, cudaStream_t st) {
+    auto slots = [](int type) { return type == EMC2_F32 ? 2 : 1; };
+    const bool pre = a.par.p[PRE_W] != nullptr;
+    const int n = (pre ? slots(a.type_x) + slots(a.type_y) : 0) + (a.dout ? slots(a.type_x) : 0) + slots(a.type_f) + (a.stats ? 1 : 0) + (a.gate ? 1 : 0);
+    const size_t shared = std::max((size_t)(kNarrowThreads / 32) * 4 * a.nvec * sizeof(float4), (size_t)4 * n * kNarrowSlot);
+    constexpr size_t most = 4 * 10 * kNarrowSlot;                 // two stages of two rows of all slots; the sums need less
+    auto kernel = wide ? residual_grad_kernel<true, ANY, true> : residual_grad_kernel<false, ANY, true>;
+    if (usual == F32_ROWS) kernel = a.drop.any ? residual_grad_kernel<true, F32_ROWS, true> : residual_grad_kernel<true, F32_ROWS, false>;
+    if (usual == BF16_ROWS) kernel = a.drop.any ? residual_grad_kernel<true, BF16_ROWS, true> : residual_grad_kernel<true, BF16_ROWS, false>;
+    return launch_grad(kernel, a, ctas, kNarrowThreads, shared, most, st);
+}
+template <int K>
+cudaError_t launch_wide(const ResGradArgs& a, bool wide, int ctas, cudaStream_t st) {
+    constexpr int warps = kResThreads / 32;
+    return launch_grad(wide ? residual_grad_wide_kernel<K, true> : residual_grad_wide_kernel<K, false>, a, ctas, kResThreads,
+                       (size_t)warps * 4 * a.nvec * sizeof(float4), (size_t)warps * 4 * 64 * K * sizeof(float4), st);
+}
 
-// Lanes of a row: groups of eight channels, one per lane up to 32 lanes, and vectors of them per lane.
-RowSplit residual_split(int channels) { return row_split((channels + 7) / 8, 1); }
-
-int residual_grad_ctas(const emc2_bridge* h, int per) { return (per == 1 ? 2 : 1) * h->num_sms; }
+int residual_grad_ctas(const emc2_bridge* h, int per) { return (per == 1 ? kNarrowCtas : 1) * h->num_sms; }
 constexpr int kShareInts = 64;               // 2 * EMC2_MAX_EXPERTS and up to a multiple of 256 bytes
 
 int check_residual(const emc2_bridge* h, int B, int N, int channels, int type_x, int type_f, int type_y, const void* f, const int32_t* offsets,
@@ -517,24 +854,26 @@ extern "C" int emc2_expert_residual(emc2_bridge_t* h, int32_t B, int32_t N, int3
     a.x = d_x; a.f = d_f; a.gate = d_gate; a.par = par; a.out = d_out; a.y = d_y; a.stats = reinterpret_cast<float4*>(d_stats);
     a.drop = make_dropout(p, d_seed);
     a.eps = eps; a.inv_c = 1.0f / (float)channels; a.nvec = channels / 4; a.type_x = type_x; a.type_f = type_f; a.type_y = type_y;
-    const RowSplit split = residual_split(channels);
+    const RowSplit split = row_split((channels + 7) / 8, 5);
     a.log = split.log;
-    int given = 0;
-    for (const float* q : par.p) given += q != nullptr;
-    const size_t staged = (size_t)given * a.seg.E * channels * sizeof(float);
+    const size_t staged = (size_t)kFolded * a.seg.E * channels * sizeof(float);
     a.shared = staged <= kResShared;
     const bool wide = is_wide(channels, type_x, d_x) && is_wide(channels, type_x, d_out) && is_wide(channels, type_f, d_f) &&
                       (!d_y || is_wide(channels, type_y, d_y));
     const long long rows = (long long)B * N, per_cta = kResThreads >> split.log;
     const int ctas = (int)std::min<long long>((rows + per_cta - 1) / per_cta, 8LL * h->num_sms);
     LaunchScope ls(h, K_RESIDUAL, st);
-    const size_t shared = a.shared ? staged : 0;
+    a.params_bytes = a.shared ? (uint32_t)staged : 0u;
+    // Every lane of a row full, and the parameters in shared memory.
+    const bool full = wide && a.shared && d_post_weight && d_pre_weight && (channels / 8) == split.per << split.log;
+    const int usual = full ? usual_of(type_x, type_f, type_y) : ANY;
     cudaError_t e;
     switch (split.per) {
-        case 1: e = Residual<1>::go(a, wide, ctas, shared, st); break;
-        case 2: e = Residual<2>::go(a, wide, ctas, shared, st); break;
-        case 3: e = Residual<3>::go(a, wide, ctas, shared, st); break;
-        default: e = Residual<4>::go(a, wide, ctas, shared, st);
+        case 1: e = Residual<1>::go(a, wide, usual, ctas, st); break;
+        case 2: e = Residual<2>::go(a, wide, usual, ctas, st); break;
+        case 3: e = Residual<3>::go(a, wide, usual, ctas, st); break;
+        case 4: e = Residual<4>::go(a, wide, usual, ctas, st); break;
+        default: e = Residual<5>::go(a, wide, usual, ctas, st);
     }
     return check_cuda(h, e != cudaSuccess ? e : cudaGetLastError());
 }
@@ -592,22 +931,22 @@ extern "C" int emc2_expert_residual_grad(emc2_bridge_t* h, int32_t B, int32_t N,
     a.part = reinterpret_cast<float*>(a.share + kShareInts);
     a.inv_c = 1.0f / (float)channels; a.nvec = channels / 4; a.type_x = type_x; a.type_f = type_f; a.type_y = type_y;
     t.part = a.part; t.share = a.share;
-    const RowSplit split = residual_split(channels);
-    a.log = split.log;
+    const int groups = (channels + 7) / 8, per = (groups + 31) / 32;
+    a.lanes = std::min(groups, 32);
     const bool wide = is_wide(channels, type_x, d_grad_x) && is_wide(channels, type_f, d_f) && is_wide(channels, type_f, d_grad_f) &&
                       (!d_grad_out || is_wide(channels, type_x, d_grad_out)) &&
                       (!d_pre_weight || (is_wide(channels, type_x, d_out) && is_wide(channels, type_y, d_grad_y)));
-    const long long rows = (long long)B * N, per_cta = kResThreads >> split.log;
-    const int ctas = (int)std::min<long long>((rows + per_cta - 1) / per_cta, residual_grad_ctas(h, split.per));
-    const size_t shared = (size_t)(kResThreads / 32) * 4 * a.nvec * sizeof(float4);
+    const long long rows = (long long)B * N, per_cta = per == 1 ? 2 * (kNarrowThreads / 32) * (32 / a.lanes) : kResThreads / 32;
+    const int ctas = (int)std::min<long long>((rows + per_cta - 1) / per_cta, residual_grad_ctas(h, per));
+    const int usual = wide && d_post_weight && d_pre_weight && d_grad_out ? usual_of(type_x, type_f, type_y) : ANY;
     {
         LaunchScope ls(h, K_RESIDUAL_GRAD, st);
         cudaError_t e;
-        switch (split.per) {
-            case 1: e = ResidualGrad<1>::go(a, wide, ctas, shared, st); break;
-            case 2: e = ResidualGrad<2>::go(a, wide, ctas, shared, st); break;
-            case 3: e = ResidualGrad<3>::go(a, wide, ctas, shared, st); break;
-            default: e = ResidualGrad<4>::go(a, wide, ctas, shared, st);
+        switch (per) {
+            case 1: e = launch_narrow(a, wide, usual, ctas, st); break;
+            case 2: e = launch_wide<2>(a, wide, ctas, st); break;
+            case 3: e = launch_wide<3>(a, wide, ctas, st); break;
+            default: e = launch_wide<4>(a, wide, ctas, st);
         }
         if (e != cudaSuccess) return check_cuda(h, e);
     }

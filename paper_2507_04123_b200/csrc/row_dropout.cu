@@ -18,10 +18,11 @@ struct DropArgs {
     FastDiv width;                           // division by the groups of a row
     Dropout drop;
     uint32_t groups;                         // of all rows
-    int nvec, type;
+    int nvec;
 };
 
-template <bool WIDE>
+// The type is a constant: a branch on it per pair of elements was a quarter of the instructions.
+template <bool WIDE, int TYPE>
 __global__ void __launch_bounds__(kDropThreads) dropout_kernel(DropArgs a) {
     const uint32_t first = blockIdx.x * (kDropThreads * kDropGroups) + threadIdx.x;
     Raw8 raw[kDropGroups];
@@ -31,19 +32,29 @@ __global__ void __launch_bounds__(kDropThreads) dropout_kernel(DropArgs a) {
         const uint32_t g = first + i * kDropThreads;
         const bool in = g < a.groups;
         a.width.divmod(g, row[i], at[i]);
-        raw[i] = request8<WIDE>(a.x, (size_t)row[i] * a.nvec + 2 * at[i], in, in && 2 * at[i] + 1 < (uint32_t)a.nvec, a.type);
+        raw[i] = request8<WIDE>(a.x, (size_t)row[i] * a.nvec + 2 * at[i], in, in && 2 * at[i] + 1 < (uint32_t)a.nvec, TYPE);
     }
-    const DropoutSeed seed = dropout_seed(a.drop);
+    uint4 bits[kDropGroups];
+    dropout_bits(bits, dropout_seed(a.drop), row, at);
+    if (!a.drop.any) {
+#pragma unroll
+        for (int i = 0; i < kDropGroups; ++i) bits[i] = make_uint4(~0u, ~0u, ~0u, ~0u);
+    }
+    const uint32_t above = a.drop.any ? a.drop.above : 0u;
 #pragma unroll
     for (int i = 0; i < kDropGroups; ++i) {
-        if (first + i * kDropThreads >= a.groups) break;
-        const uint4 bits = dropout_bits(seed, row[i], at[i]);
         float f[8];
-        floats8(f, raw[i], a.type);
+        floats8(f, raw[i], TYPE);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) f[j] = dropout_keeps(bits, j, a.drop.threshold) ? f[j] * a.drop.factor : 0.0f;
-        store8<WIDE>(a.y, (size_t)row[i] * a.nvec + 2 * at[i], 2 * at[i] + 1 < (uint32_t)a.nvec, f, a.type);
+        for (int j = 0; j < 8; ++j) f[j] = dropout_keeps(bits[i], j, above) ? f[j] * a.drop.factor : 0.0f;
+        if (first + i * kDropThreads < a.groups) store8<WIDE>(a.y, (size_t)row[i] * a.nvec + 2 * at[i], 2 * at[i] + 1 < (uint32_t)a.nvec, f, TYPE);
     }
+}
+
+template <int TYPE>
+void launch_dropout(const DropArgs& a, bool wide, unsigned ctas, cudaStream_t st) {
+    if (wide) dropout_kernel<true, TYPE><<<ctas, kDropThreads, 0, st>>>(a);
+    else dropout_kernel<false, TYPE><<<ctas, kDropThreads, 0, st>>>(a);
 }
 
 }  // namespace
@@ -62,13 +73,15 @@ extern "C" int emc2_row_dropout(emc2_bridge_t* h, int32_t n, int32_t channels, i
     if (!device.ok) return EMC2_ERR_CUDA;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     DropArgs a;
-    a.x = d_x; a.y = d_y; a.drop = make_dropout(p, d_seed); a.nvec = channels / 4; a.type = type;
+    a.x = d_x; a.y = d_y; a.drop = make_dropout(p, d_seed); a.nvec = channels / 4;
     const uint32_t width = (uint32_t)(channels + 7) / 8;
     a.width = make_fast_div(width);
     a.groups = (uint32_t)n * width;                              // 2^24 rows of 128 at most
     const unsigned ctas = (a.groups + kDropThreads * kDropGroups - 1) / (kDropThreads * kDropGroups);
     LaunchScope ls(h, K_ROW_DROPOUT, st);
-    if (is_wide(channels, type, d_x) && is_wide(channels, type, d_y)) dropout_kernel<true><<<ctas, kDropThreads, 0, st>>>(a);
-    else dropout_kernel<false><<<ctas, kDropThreads, 0, st>>>(a);
+    const bool wide = is_wide(channels, type, d_x) && is_wide(channels, type, d_y);
+    if (type == EMC2_F32) launch_dropout<EMC2_F32>(a, wide, ctas, st);
+    else if (type == EMC2_BF16) launch_dropout<EMC2_BF16>(a, wide, ctas, st);
+    else launch_dropout<EMC2_F16>(a, wide, ctas, st);
     return check_cuda(h, cudaGetLastError());
 }
