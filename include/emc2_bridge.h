@@ -429,6 +429,43 @@ int emc2_expert_residual_grad(emc2_bridge_t* bridge, int32_t B, int32_t N, int32
                               void* d_grad_f, float* d_grad_gate, float* d_grad_post_weight, float* d_grad_post_bias,
                               float* d_grad_scale, float* d_grad_pre_weight, float* d_grad_pre_bias, void* cuda_stream);
 
+/* Microscaled 4-bit floating point (OCP Microscaling, E2M1 elements): the form of weights that emc2_expert_layer_mx4 reads.  Elements
+ * are 0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives (codes 0 .. 7, and 8 more with the sign); blocks of 32 along a row share a power of two.
+ *   d_x       type [rows, channels], channels a multiple of 4 up to 8192, rows * ceil(channels / 32) <= 2^29
+ *   d_codes   uint8 [rows, 16 * ceil(channels / 32)]: element i in the low half of byte i / 2 for even i, the high half for odd i; those
+ *             behind the row are 0
+ *   d_scales  uint8 [rows, ceil(channels / 32)]: the power's exponent + 127; 255: NaN
+ *   d_values  type [rows, channels], what the codes stand for; d_values, or both of d_codes and d_scales, may be NULL
+ * The power is 2^(floor(log2 m) - 2) for the block's largest size m, 2^-127 at least; elements are rounded to the nearest, halves to even, to
+ * sizes of 6 at most.  A block with an infinity or NaN has codes 0 and the power NaN. */
+int emc2_mx4_quantise(emc2_bridge_t* bridge, int32_t rows, int32_t channels, int32_t type, const void* d_x, uint8_t* d_codes,
+                      uint8_t* d_scales, void* d_values, void* cuda_stream);
+
+/* A whole mixture-of-experts layer for a few rows (scratch, reserved for that many channels and hidden units): per row x the
+ * logits x w_router^T + b_router, its `choices` experts of the largest logits, in that order, weights p = the softmax over those, and
+ * d_y = the sum of p_j times the gated feed-forward block of emc2_expert_ffn with the weights of expert j.
+ *   d_x, d_y       type [n, channels], type EMC2_BF16 or EMC2_F16, n <= 128; channels a multiple of 8 up to 1024
+ *   d_count        int32 on the device, or NULL (n): only so many rows, of the first, are in use; the others are not read, and
+ *                  their results left untouched.  A count outside 0 .. n makes EMC2_ERR_INVALID_ARG sticky and counts as the nearest
+ *   d_w_router     float [experts, channels], d_b_router float [experts] or NULL; 1 <= experts <= 256 (the layer's own: rows need no
+ *                  dispatch), 1 <= choices <= 8, choices <= experts
+ *   d_w_gate, d_w_up  type [experts, hidden, channels]     d_w_down  type [experts, channels, hidden]; hidden a multiple of 8 up to 8192
+ *   d_ids          int32 [n, choices]     d_weights  float [n, choices]: the chosen experts and p
+ * Logits are summed in 64 bits; of equal ones the lower expert is first, and NaN are behind all others.  Products are summed in fp32;
+ * act(g) * u is rounded to the type before the last product (in EMC2_F16 it has to stay below 65504), the result once. */
+int emc2_expert_layer(emc2_bridge_t* bridge, int32_t n, int32_t channels, int32_t hidden, int32_t experts, int32_t choices, int32_t type,
+                      int32_t act, const void* d_x, const int32_t* d_count, const float* d_w_router, const float* d_b_router,
+                      const void* d_w_gate, const void* d_w_up, const void* d_w_down, void* d_y, int32_t* d_ids, float* d_weights,
+                      void* cuda_stream);
+
+/* The same with weights in the form of emc2_mx4_quantise (the rows are [experts * hidden] of `channels` for the gate and the up
+ * projection, [experts * channels] of `hidden` for the down projection): products with what the codes stand for, summed in fp32. */
+int emc2_expert_layer_mx4(emc2_bridge_t* bridge, int32_t n, int32_t channels, int32_t hidden, int32_t experts, int32_t choices, int32_t type,
+                          int32_t act, const void* d_x, const int32_t* d_count, const float* d_w_router, const float* d_b_router,
+                          const uint8_t* d_gate_codes, const uint8_t* d_gate_scales, const uint8_t* d_up_codes, const uint8_t* d_up_scales,
+                          const uint8_t* d_down_codes, const uint8_t* d_down_scales, void* d_y, int32_t* d_ids, float* d_weights,
+                          void* cuda_stream);
+
 /* Turns the handle's own streams in emc2_bridge_run and emc2_expert_ffn_grad off (0) or on (non-zero, the default).  Off, every
  * kernel of the call is enqueued on `cuda_stream` itself, one after another: for callers that
  * want no second stream, and for timing kernels one at a time. */

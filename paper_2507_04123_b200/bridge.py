@@ -40,6 +40,7 @@ ABI_SYMBOLS = (
     "emc2_rows_reserve", "emc2_row_lookup", "emc2_row_lookup_grad", "emc2_expert_norm", "emc2_expert_norm_grad",
     "emc2_expert_ffn", "emc2_expert_ffn_grad",
     "emc2_row_dropout", "emc2_expert_residual", "emc2_expert_residual_grad",
+    "emc2_mx4_quantise", "emc2_expert_layer", "emc2_expert_layer_mx4",
 )
 
 # emc2_type_t
@@ -125,6 +126,9 @@ def load_library() -> ctypes.CDLL:
     lib.emc2_row_dropout.argtypes = [vp, i32, i32, i32, vp, f32, vp, vp, vp]
     lib.emc2_expert_residual.argtypes = [vp] + [i32] * 6 + [vp] * 9 + [f32, f32] + [vp] * 5
     lib.emc2_expert_residual_grad.argtypes = [vp] + [i32] * 6 + [vp] * 11 + [f32] + [vp] * 10
+    lib.emc2_mx4_quantise.argtypes = [vp, i32, i32, i32] + [vp] * 5
+    lib.emc2_expert_layer.argtypes = [vp] + [i32] * 7 + [vp] * 11
+    lib.emc2_expert_layer_mx4.argtypes = [vp] + [i32] * 7 + [vp] * 14
     lib.emc2_bridge_destroy.argtypes = [vp]
     lib.emc2_status_string.argtypes = [ctypes.c_int]
     lib.emc2_status_string.restype = ctypes.c_char_p
@@ -737,6 +741,72 @@ class Bridge:
             *[_ptr(t) for t in params.values()], float(p), _ptr(seed), out["grad_x"].data_ptr(), out["grad_f"].data_ptr(),
             _ptr(out.get("grad_gate")), *[_ptr(out.get("grad_" + k)) for k in of], self._stream())
         self._raise(rc, "emc2_expert_residual_grad")
+        return out
+
+    def mx4_quantise(self, x: torch.Tensor, out: Optional[Dict[str, Optional[torch.Tensor]]] = None) -> Dict[str, Optional[torch.Tensor]]:
+        """emc2_mx4_quantise: rows [.., channels] as ``codes`` and ``scales`` of microscaled 4-bit floating point, and the ``values``
+        that these stand for if ``out`` has room for them."""
+        C = x.shape[-1]
+        rows = x.numel() // C if C else 0
+        _sizes(rows, C)
+        kind = self._row_type(x, "x")
+        _check(x, x.dtype, x.shape, "x", self.device)
+        blocks = -(-C // 32)
+        lead = tuple(x.shape[:-1])
+        if out is None:
+            out = {"codes": torch.empty((*lead, 16 * blocks), dtype=torch.uint8, device=self.device),
+                   "scales": torch.empty((*lead, blocks), dtype=torch.uint8, device=self.device)}
+        for k, dtype, width in (("codes", torch.uint8, 16 * blocks), ("scales", torch.uint8, blocks), ("values", x.dtype, C)):
+            if out.get(k) is not None:
+                _check(out[k], dtype, (*lead, width), k, self.device)
+        rc = self.lib.emc2_mx4_quantise(self._h, rows, C, kind, x.data_ptr(), _ptr(out.get("codes")), _ptr(out.get("scales")),
+                                        _ptr(out.get("values")), self._stream())
+        self._raise(rc, "emc2_mx4_quantise")
+        return out
+
+    def expert_layer(self, x: torch.Tensor, w_router: torch.Tensor, w_gate, w_up, w_down, choices: int, act: str = "silu",
+                     b_router: Optional[torch.Tensor] = None, count: Optional[torch.Tensor] = None,
+                     out: Optional[Dict[str, torch.Tensor]] = None) -> Dict[str, torch.Tensor]:
+        """emc2_expert_layer, or emc2_expert_layer_mx4 where the weights are dicts of :meth:`mx4_quantise`: router, choice, gated
+        feed-forward of the chosen experts and weighted sum for up to 128 rows; ``y``, ``ids`` and ``weights`` (needs
+        :meth:`reserve_rows`).  ``count``: int32 [1] on the device, the rows in use; the others are left as they are in ``out``."""
+        n, C = x.shape
+        E = w_router.shape[0]
+        mx = isinstance(w_gate, dict)
+        H = (w_gate["codes"] if mx else w_gate).shape[1]
+        _sizes(n, C, E, H, int(choices))
+        if act not in ACTIVATIONS:
+            raise ValueError(f"act: expected one of {sorted(ACTIVATIONS)}, got {act!r}")
+        if x.dtype not in (torch.bfloat16, torch.float16):
+            raise ValueError(f"x: expected bfloat16 or float16, got {x.dtype}")
+        _check(x, x.dtype, (n, C), "x", self.device)
+        _check(w_router, torch.float32, (E, C), "w_router", self.device)
+        ptrs = []
+        for name, w, M, K in (("w_gate", w_gate, H, C), ("w_up", w_up, H, C), ("w_down", w_down, C, H)):
+            if isinstance(w, dict) != mx:
+                raise ValueError(f"{name}: all weights have the same form")
+            if mx:
+                _check(w["codes"], torch.uint8, (E, M, 16 * (-(-K // 32))), name + " codes", self.device)
+                _check(w["scales"], torch.uint8, (E, M, -(-K // 32)), name + " scales", self.device)
+                ptrs += [w["codes"].data_ptr(), w["scales"].data_ptr()]
+            else:
+                _check(w, x.dtype, (E, M, K), name, self.device)
+                ptrs.append(w.data_ptr())
+        if b_router is not None:
+            _check(b_router, torch.float32, (E,), "b_router", self.device)
+        if count is not None:
+            _check(count, torch.int32, (1,), "count", self.device)
+        if out is None:
+            out = {"y": torch.empty_like(x), "ids": torch.empty((n, int(choices)), dtype=torch.int32, device=self.device),
+                   "weights": torch.empty((n, int(choices)), dtype=torch.float32, device=self.device)}
+        _check(out["y"], x.dtype, (n, C), "y", self.device)
+        _check(out["ids"], torch.int32, (n, int(choices)), "ids", self.device)
+        _check(out["weights"], torch.float32, (n, int(choices)), "weights", self.device)
+        name = "emc2_expert_layer_mx4" if mx else "emc2_expert_layer"
+        rc = getattr(self.lib, name)(self._h, n, C, H, E, int(choices), ROW_TYPES[x.dtype], ACTIVATIONS[act], x.data_ptr(), _ptr(count),
+                                     w_router.data_ptr(), _ptr(b_router), *ptrs, out["y"].data_ptr(), out["ids"].data_ptr(),
+                                     out["weights"].data_ptr(), self._stream())
+        self._raise(rc, name)
         return out
 
     def set_overlap(self, enable: bool) -> None:

@@ -10,8 +10,9 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libemc2_bridge.so")
 SOURCES = ["bridge.cu", "voxelize.cu", "project_gather.cu", "route_dispatch.cu", "voxel_image.cu", "occlusion.cu", "rulebook.cu", "dedup_arms.cu", "row_lookup.cu",
-           "expert_norm.cu", "expert_ffn.cu", "row_dropout.cu", "expert_residual.cu"]
-HEADERS = [os.path.join(CSRC, "bridge_internal.cuh"), os.path.join(CSRC, "rules.cuh"), os.path.join(CSRC, "rows.cuh"), os.path.join(CSRC, "row_sizes.cuh"), os.path.join(CSRC, "umma.cuh"), os.path.join(CSRC, "dropout.cuh"),
+           "expert_norm.cu", "expert_ffn.cu", "row_dropout.cu", "expert_residual.cu",
+           "mx4.cu", "expert_layer.cu"]
+HEADERS = [os.path.join(CSRC, "bridge_internal.cuh"), os.path.join(CSRC, "rules.cuh"), os.path.join(CSRC, "rows.cuh"), os.path.join(CSRC, "row_sizes.cuh"), os.path.join(CSRC, "umma.cuh"), os.path.join(CSRC, "dropout.cuh"), os.path.join(CSRC, "mx4.cuh"),
             os.path.join(ROOT, "include", "emc2_bridge.h")]
 
 

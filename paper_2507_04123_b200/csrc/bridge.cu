@@ -14,7 +14,7 @@ static const char* const kKernelNames[K_KINDS] = {
     "vif_scan", "vif_fill", "vif_mean", "vif_sample", "occl_fill", "occl_splat", "occl_test",
     "channels_last", "rb_mark", "rb_count", "rb_scan", "rb_fill", "rb_clear",
     "row_lookup", "lookup_sort", "lookup_sum", "lookup_join", "norm", "norm_grad", "norm_sum", "ffn", "ffn_grad_x", "ffn_grad_w", "ffn_sum", "ffn_join",
-    "row_dropout", "residual", "residual_grad", "residual_sum"};
+    "row_dropout", "residual", "residual_grad", "residual_sum", "mx4", "layer_route", "layer_hidden", "layer_down"};
 
 int check_cuda(emc2_bridge* h, cudaError_t e) {
     if (e == cudaSuccess) return EMC2_OK;
@@ -653,9 +653,19 @@ int emc2_rows_reserve(emc2_bridge_t* h, int32_t max_channels, int32_t max_hidden
     RowsScratch& r = h->rows_scratch;
     if (r.slab && max_channels <= r.max_channels && max_hidden <= r.max_hidden) return EMC2_OK;
     const int channels = std::max(max_channels, r.max_channels), hidden = std::max(max_hidden, r.max_hidden);
-    const size_t bytes = std::max({norm_scratch_bytes(h, channels), residual_scratch_bytes(h, channels), lookup_scratch_bytes(h, channels), ffn_scratch_bytes(h, channels, hidden)});
+    const size_t bytes = std::max({norm_scratch_bytes(h, channels), residual_scratch_bytes(h, channels), lookup_scratch_bytes(h, channels), ffn_scratch_bytes(h, channels, hidden),
+                                   layer_scratch_bytes(channels, hidden)});
     DeviceGuard guard(h->cfg.device);
     if (!guard.ok) return EMC2_ERR_CUDA;
+    if (hidden > 0 && !r.notes) {
+        void* p = nullptr;
+        cudaError_t e = cudaMalloc(&p, layer_notes_bytes());
+        if (e != cudaSuccess) { cudaGetLastError(); return check_cuda(h, e); }
+        e = cudaMemset(p, 0, layer_notes_bytes());
+        if (e == cudaSuccess) e = cudaStreamSynchronize(nullptr);           // before any stream's first call
+        if (e != cudaSuccess) { cudaFree(p); return check_cuda(h, e); }
+        r.notes = p;
+    }
     if (!r.slab || bytes > r.bytes) {
         // Room for the old area's place in the list first: a failure must not lose it.
         try { r.outgrown.reserve(r.outgrown.size() + 1); } catch (...) { return EMC2_ERR_INTERNAL; }
@@ -704,6 +714,7 @@ int emc2_bridge_destroy(emc2_bridge_t* h) {
     if (h->slab && cudaFree(h->slab) != cudaSuccess) rc = EMC2_ERR_CUDA;
     if (h->arm.slab && cudaFree(h->arm.slab) != cudaSuccess) rc = EMC2_ERR_CUDA;
     if (h->rows_scratch.slab && cudaFree(h->rows_scratch.slab) != cudaSuccess) rc = EMC2_ERR_CUDA;
+    if (h->rows_scratch.notes && cudaFree(h->rows_scratch.notes) != cudaSuccess) rc = EMC2_ERR_CUDA;
     for (void* p : h->rows_scratch.outgrown)
         if (cudaFree(p) != cudaSuccess) rc = EMC2_ERR_CUDA;
     delete h;
@@ -725,7 +736,7 @@ const char* emc2_status_string(int status) {
 }
 
 int emc2_bridge_last_cuda_error(const emc2_bridge_t* h) { return h ? h->last_cuda_error : 0; }
-size_t emc2_bridge_scratch_bytes(const emc2_bridge_t* h) { return h ? h->slab_bytes + h->arm.bytes + h->rows_scratch.bytes + h->rows_scratch.outgrown_bytes : 0; }
+size_t emc2_bridge_scratch_bytes(const emc2_bridge_t* h) { return h ? h->slab_bytes + h->arm.bytes + h->rows_scratch.bytes + h->rows_scratch.outgrown_bytes + (h->rows_scratch.notes ? layer_notes_bytes() : 0) : 0; }
 
 int emc2_bridge_kernel_kinds(void) { return K_KINDS; }
 const char* emc2_bridge_kernel_name(int kind) { return kind >= 0 && kind < K_KINDS ? kKernelNames[kind] : ""; }

@@ -87,6 +87,10 @@ enum KernelKind {
     K_RESIDUAL,
     K_RESIDUAL_GRAD,
     K_RESIDUAL_SUM,
+    K_MX4,
+    K_LAYER_ROUTE,
+    K_LAYER_HIDDEN,
+    K_LAYER_DOWN,
     K_KINDS
 };
 
@@ -208,6 +212,7 @@ struct RowsScratch {
     int max_channels = 0, max_hidden = 0;
     std::vector<void*> outgrown;                // smaller ones that captured graphs may still use
     size_t outgrown_bytes = 0;
+    void* notes = nullptr;                      // of emc2_expert_layer: counters that are zero between calls
 };
 
 struct ProfRec {
@@ -279,6 +284,8 @@ int dedup_arm_alloc(emc2_bridge* h);
 size_t norm_scratch_bytes(const emc2_bridge* h, int max_channels);
 size_t residual_scratch_bytes(const emc2_bridge* h, int max_channels);
 size_t lookup_scratch_bytes(const emc2_bridge* h, int max_channels);
+size_t layer_notes_bytes();
+size_t layer_scratch_bytes(int max_channels, int max_hidden);
 size_t ffn_scratch_bytes(const emc2_bridge* h, int max_channels, int max_hidden);
 int launch_dedup_arm(emc2_bridge* h, int s, int design, int B, int N, const float* d_points, int capacity,
                      int32_t* d_num_voxels, cudaStream_t st);
