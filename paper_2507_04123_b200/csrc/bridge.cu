@@ -14,7 +14,7 @@ static const char* const kKernelNames[K_KINDS] = {
     "vif_scan", "vif_fill", "vif_mean", "vif_sample", "occl_fill", "occl_splat", "occl_test",
     "channels_last", "rb_mark", "rb_count", "rb_scan", "rb_fill", "rb_clear",
     "row_lookup", "lookup_sort", "lookup_sum", "lookup_join", "norm", "norm_grad", "norm_sum", "ffn", "ffn_grad_x", "ffn_grad_w", "ffn_sum", "ffn_join",
-    "row_dropout", "residual", "residual_grad", "residual_sum", "mx4", "layer_route", "layer_hidden", "layer_down"};
+    "row_dropout", "residual", "residual_grad", "residual_sum", "mx4", "layer_route", "layer_hidden", "layer_down", "layer_sum"};
 
 int check_cuda(emc2_bridge* h, cudaError_t e) {
     if (e == cudaSuccess) return EMC2_OK;

@@ -91,6 +91,7 @@ enum KernelKind {
     K_LAYER_ROUTE,
     K_LAYER_HIDDEN,
     K_LAYER_DOWN,
+    K_LAYER_SUM,
     K_KINDS
 };
 

@@ -3,15 +3,16 @@
 //   l = x w_router^T + b;  the k largest;  p = softmax over these
 //   y = sum_j p_j (act(x w_gate[e_j]^T) * (x w_up[e_j]^T)) w_down[e_j]^T
 //
-// Bound by the weights of the experts that are asked for, which are read once: three kernels, each set up while the one before still
-// runs.  The first has a CTA per row; the last of them to finish sorts the pairs (row, choice) by expert.  The second has a CTA per expert
-// and tile of hidden units, the third per expert, tile of channels and share of the hidden units; the last CTA of a tile of channels adds up
-// what all left for it, in the order of a row's choices.  In both, every warp streams its own rows of weights from memory into the registers
-// of m16n8k16 products, whose 16 rows are the weights' and whose 8 columns are the rows at hand: a row of x more costs no
-// more reading, and there are too few of them for larger products to help.
+// Bound by the weights of the experts that are asked for, which are read once.  The first kernel has a CTA per row; the last of them to finish
+// sorts the pairs (row, choice) by expert.  The second has a CTA per expert and tile of hidden units, the third per expert, tile of channels
+// and share of the hidden units; what they leave is added up in the order of a row's choices, by the last CTA of a tile of channels or, for more
+// rows, by a fourth kernel.  Each kernel is set up while the one before still runs.  In both products every warp streams its own rows of weights
+// from memory into the registers of m16n8k16 products, whose 16 rows are the weights' and whose 8 columns are the rows at hand: a row
+// of x more costs no more reading, and there are too few of them for larger products to help.
 //
-// The logits are summed in 64 bits, so that the choice does not depend on an order of summation; products in fp32; act(g) * u is rounded to
-// the type, y once.
+// The logits are summed in 64 bits, so that the choice does not depend on an order of summation; products in fp32.  act(g) * u goes into the
+// last product as the sum of two numbers of the type where an expert has up to 16 rows, whose products have columns to spare, else rounded to
+// one.  y is rounded once.
 #include <algorithm>
 
 #include "mx4.cuh"
@@ -19,17 +20,21 @@
 namespace emc2 {
 namespace {
 
-constexpr int kLayerThreads = 256;
+constexpr int kRouteThreads = 256;           // one per expert
+constexpr int kRouteWarps = kRouteThreads / 32;
+constexpr int kLayerThreads = 256;           // of the products; two CTAs per SM
 constexpr int kLayerWarps = kLayerThreads / 32;
 constexpr int kMaxLayerRows = 128;
 constexpr int kMaxLayerExperts = 256;
 constexpr int kMaxChoices = 8;
 constexpr int kMaxSlots = kMaxLayerRows * kMaxChoices;     // pairs (row, choice)
 constexpr int kMaxLayerHidden = 8192;
-constexpr int kPanel = 512;                  // elements of the rows at hand in shared memory at a time
+constexpr int kPanel = 256;                  // elements of the rows at hand in shared memory at a time
 constexpr int kRowsAtOnce = 32;
 constexpr int kMaxShares = 8;                // of the hidden units in the third kernel
 constexpr int kMaxTiles = 64;                // of channels, per counter
+constexpr int kTwoParts = 16;                // rows of an expert whose hidden values are held in two parts, at most
+constexpr int kLastAdds = 64;                // partial results of an output that the third kernel adds up itself, at most
 
 // What the kernels leave one another, on the device.
 struct LayerNotes {
@@ -53,18 +58,23 @@ struct LayerArgs {
     float* weights;
     void* y;
     LayerNotes* notes;
-    void* hidden;                            // [sorted pair][H]
+    const void* ordered;                     // 4-bit weights: x in the order that eight codes come in
+    void* hidden;                            // [sorted pair][2][H]
     float* part;                             // [share][sorted pair][C]
     int* status;
     int n, C, H, E, k, act;
     int split;                               // warps that share a tile, each with every split-th block
     int tiles;                               // CTAs per expert
     int shares;                              // third kernel: of the hidden units
+    int last_adds;                           // ... and whether its last CTAs add up
 };
 
 __device__ __forceinline__ float type_float(const void* p, size_t i, bool bf16) {
     return bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(p)[i]) : __half2float(static_cast<const __half*>(p)[i]);
 }
+
+// Place of element i among eight, in the order that codes come in.
+__host__ __device__ __forceinline__ int ordered_place(int i) { return (i & 3) * 2 + (i >> 2); }
 
 // Numbers that ascend as the logits do; NaN below all.  0 is left for what has been taken.
 __device__ __forceinline__ unsigned long long logit_key(double v) {
@@ -75,8 +85,8 @@ __device__ __forceinline__ unsigned long long logit_key(double v) {
 
 // One CTA per row.
 template <bool BF16>
-__global__ void __launch_bounds__(kLayerThreads) layer_route_kernel(LayerArgs a) {
-    __shared__ __align__(16) float x[kMaxRowChannels];
+__global__ void __launch_bounds__(kRouteThreads) layer_route_kernel(LayerArgs a) {
+    __shared__ __align__(16) double x[kMaxRowChannels];
     __shared__ unsigned long long key[kMaxLayerExperts];
     __shared__ double logit[kMaxLayerExperts];
     __shared__ int last;
@@ -90,26 +100,46 @@ __global__ void __launch_bounds__(kLayerThreads) layer_route_kernel(LayerArgs a)
         }
     }
     if (row < used) {
-        for (int i = tid; i < a.C; i += kLayerThreads) x[i] = type_float(a.x, (size_t)row * a.C + i, BF16);
-        __syncthreads();
-        for (int e = warp; e < a.E; e += kLayerWarps) {
-            const float4* w = reinterpret_cast<const float4*>(a.w_router + (size_t)e * a.C);
-            double s = 0.0, t = 0.0;
-#pragma unroll 4
-            for (int v = lane; v < a.C / 4; v += 32) {
-                const float4 f = __ldg(w + v), g = *reinterpret_cast<const float4*>(x + 4 * v);
-                s += (double)f.x * (double)g.x;
-                t += (double)f.y * (double)g.y;
-                s += (double)f.z * (double)g.z;
-                t += (double)f.w * (double)g.w;
+        for (int i = tid; i < a.C; i += kRouteThreads) {
+            const float v = type_float(a.x, (size_t)row * a.C + i, BF16);
+            x[i] = (double)v;
+            // Eight codes come as the pairs (0, 4), (1, 5), (2, 6), (3, 7).
+            if (a.ordered) {
+                uint16_t* to = static_cast<uint16_t*>(const_cast<void*>(a.ordered)) + (size_t)row * a.C + (i & ~7) + ordered_place(i & 7);
+                *to = static_cast<const uint16_t*>(a.x)[(size_t)row * a.C + i];
             }
-            s += t;
+        }
+        __syncthreads();
+        // Four experts at a time, so that their weights are under way together.
+        for (int e0 = warp * 4; e0 < a.E; e0 += kRouteWarps * 4) {
+            double sum[4] = {0.0, 0.0, 0.0, 0.0};
+#pragma unroll 2
+            for (int v = lane; v < a.C / 4; v += 32) {
+                float4 f[4];
 #pragma unroll
-            for (int d = 16; d; d >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, d);
-            if (lane == 0) {
-                if (a.b_router) s += (double)__ldg(a.b_router + e);
-                logit[e] = s;
-                key[e] = logit_key(s);
+                for (int q = 0; q < 4; ++q)
+                    f[q] = e0 + q < a.E ? __ldg(reinterpret_cast<const float4*>(a.w_router + (size_t)(e0 + q) * a.C) + v) : make_float4(0.f, 0.f, 0.f, 0.f);
+                const double2 g = *reinterpret_cast<const double2*>(x + 4 * v), h = *reinterpret_cast<const double2*>(x + 4 * v + 2);
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    sum[q] += (double)f[q].x * g.x;
+                    sum[q] += (double)f[q].y * g.y;
+                    sum[q] += (double)f[q].z * h.x;
+                    sum[q] += (double)f[q].w * h.y;
+                }
+            }
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+#pragma unroll
+                for (int d = 16; d; d >>= 1) sum[q] += __shfl_xor_sync(0xFFFFFFFFu, sum[q], d);
+            }
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int e = e0 + q;
+                if (lane != q || e >= a.E) continue;
+                const double l = a.b_router ? sum[q] + (double)__ldg(a.b_router + e) : sum[q];
+                logit[e] = l;
+                key[e] = logit_key(l);
             }
         }
         __syncthreads();
@@ -154,12 +184,12 @@ __global__ void __launch_bounds__(kLayerThreads) layer_route_kernel(LayerArgs a)
     __threadfence();
     __shared__ int of[kMaxSlots];
     __shared__ uint16_t piece[kMaxSlots / 32][kMaxLayerExperts];
-    __shared__ int base[kMaxLayerExperts], warp_sum[2][kLayerWarps];
+    __shared__ int base[kMaxLayerExperts], warp_sum[2][kRouteWarps];
     const int pairs = used * a.k, pieces = (pairs + 31) / 32;
-    for (int i = tid; i < pairs; i += kLayerThreads) of[i] = __ldcg(a.ids + i);
-    for (int i = tid; i < pieces * kMaxLayerExperts / 2; i += kLayerThreads) reinterpret_cast<uint32_t*>(piece)[i] = 0u;
+    for (int i = tid; i < pairs; i += kRouteThreads) of[i] = __ldcg(a.ids + i);
+    for (int i = tid; i < pieces * kMaxLayerExperts / 2; i += kRouteThreads) reinterpret_cast<uint32_t*>(piece)[i] = 0u;
     __syncthreads();
-    for (int p = warp; p < pieces; p += kLayerWarps) {
+    for (int p = warp; p < pieces; p += kRouteWarps) {
         const int i = p * 32 + lane, e = i < pairs ? of[i] : -1;
         const unsigned same = __match_any_sync(0xFFFFFFFFu, e);
         if (e >= 0 && (same & ((1u << lane) - 1)) == 0) piece[p][e] = (uint16_t)__popc(same);
@@ -186,14 +216,14 @@ __global__ void __launch_bounds__(kLayerThreads) layer_route_kernel(LayerArgs a)
         a.notes->expert[rank - 1] = tid;
         a.notes->start[rank] = sum;
     }
-    if (tid == kLayerThreads - 1) {
+    if (tid == kRouteThreads - 1) {
         a.notes->active = rank;
         a.notes->used = used;
         a.notes->start[0] = 0;
         a.notes->arrived = 0;
     }
     __syncthreads();
-    for (int p = warp; p < pieces; p += kLayerWarps) {
+    for (int p = warp; p < pieces; p += kRouteWarps) {
         const int i = p * 32 + lane, e = i < pairs ? of[i] : -1;
         const unsigned same = __match_any_sync(0xFFFFFFFFu, e);
         if (e < 0) continue;
@@ -207,35 +237,34 @@ __global__ void __launch_bounds__(kLayerThreads) layer_route_kernel(LayerArgs a)
 template <bool BF16>
 __device__ __forceinline__ void product(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     if (BF16)
-        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+            : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
     else
-        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+            : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-// Eight codes as four pairs of the type, by the bytes of the eight magnitudes.
+// Eight codes as the pairs (0, 4), (1, 5), (2, 6), (3, 7), times the type's smallest power that is not its last: the three bits of a size
+// are put at the end of the exponent and the start of the mantissa, where they read as the element times 2^-126 (bf16) or 2^-14 (fp16),
+// its number below 1 too, and `factor` makes up for it.
 template <bool BF16>
-__device__ __forceinline__ void decode8(uint32_t (&r)[4], uint32_t codes) {
-    constexpr uint32_t top_low = BF16 ? 0x3F3F3F00u : 0x3E3C3800u, top_high = BF16 ? 0x40404040u : 0x46444240u;
-    constexpr uint32_t end_low = 0xC0800000u, end_high = 0xC0804000u;
-    const uint32_t m = codes & 0x77777777u;
+__device__ __forceinline__ void decode8(uint32_t (&r)[4], uint32_t codes, uint32_t factor) {
+    constexpr uint32_t size = BF16 ? 0x01C001C0u : 0x0E000E00u, sign = 0x80008000u;
+    constexpr int up = BF16 ? 6 : 9;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const uint32_t at = m >> (16 * i), s = codes >> (16 * i);
-        const uint32_t top = __byte_perm(top_low, top_high, at);
-        const uint32_t end = BF16 ? __byte_perm(end_low, end_high, at) : 0u;
-        r[2 * i] = __byte_perm(end, top, 0x5140) | (s << 12 & 0x00008000u) | (s << 24 & 0x80000000u);
-        r[2 * i + 1] = __byte_perm(end, top, 0x7362) | (s << 4 & 0x00008000u) | (s << 16 & 0x80000000u);
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t m = up >= 4 * i ? codes << (up - 4 * i) : codes >> (4 * i - up);
+        const uint32_t v = (m & size) | ((codes << (12 - 4 * i)) & sign);
+        if (BF16) asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r[i]) : "r"(v), "r"(factor));
+        else asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r[i]) : "r"(v), "r"(factor));
     }
 }
-
-// A block of 32 elements of a product: lane (g, t) has elements 8t .. 8t + 7 of rows g and g + 8 of the weights and of row g of the rows at
-// hand; which element stands at which place of an instruction does not matter, if both sides agree.
-__device__ __forceinline__ uint4 load_weights(const void* p) {
-    uint4 v;
-    asm volatile("ld.global.nc.L1::no_allocate.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
-    return v;
+// The pair of factors for a block whose power is 2^-below of its row's.
+template <bool BF16>
+__device__ __forceinline__ uint32_t block_factor(int below) {
+    if (BF16) return (uint32_t)max(253 - below, 0) * 0x00800080u;
+    const uint32_t h = below < 29 ? (uint32_t)(29 - below) << 10 : below <= 38 ? 1u << (38 - below) : 0u;
+    return h * 0x00010001u;
 }
 
 enum Stage { HIDDEN = 0, DOWN };
@@ -244,10 +273,19 @@ enum Stage { HIDDEN = 0, DOWN };
 // different banks.
 constexpr int kPanelStride = kPanel * 2 + 64;
 constexpr int kPanelBytes = kRowsAtOnce * kPanelStride;
+constexpr uint32_t kRingRow = kLayerThreads * 16;
+constexpr size_t kProductShared = 2 * kPanelBytes + 4 * 4 * kRingRow;
 
-// What a warp's rows of weights are: two tiles of 16, of the gate's and the up projection's rows or of the down projection's.
+// What a warp's rows of weights are: two tiles of 16, of the gate's and the up projection's rows or of the down projection's.  Lane (g, t)
+// has rows g and g + 8 of both.  Which element stands at which place of an instruction does not matter, if weights and rows agree.
+//   16 bits: a block of 32 elements to a step, of which the lane has 8t .. 8t + 7.
+//    4 bits: four blocks to a step, of which the lane has the t-th.  A block's elements are taken relative to the largest power that the row
+//            has had so far, which the sums are relative to; when it rises, they are scaled down.
+// The weights of the next three steps are on their way to shared memory, in places that the lane alone reads: registers have no room for as
+// much as the memory needs to be asked for at once (50 KB per SM and more).
 template <int STAGE, bool MX, bool BF16, int NT>
-__device__ __forceinline__ void layer_rows(const LayerArgs& a, char* smem, int e, int pair0, int rows) {
+__device__ __forceinline__ void layer_rows(const LayerArgs& a, char* smem, int e, int pair0, int rows, bool two) {
+    constexpr int kPiece = MX ? 128 : 32;                         // elements of a step
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
     const int per_cta = kLayerWarps / a.split, part = warp % a.split, slot = warp / a.split;
     const int K = STAGE == HIDDEN ? a.C : a.H, M = STAGE == HIDDEN ? a.H : a.C;
@@ -271,128 +309,136 @@ __device__ __forceinline__ void layer_rows(const LayerArgs& a, char* smem, int e
         for (int n = 0; n < NT; ++n)
 #pragma unroll
             for (int c = 0; c < 4; ++c) acc[m][n][c] = 0.f;
-    // Copies a panel; what lies behind the rows or behind K is zero.
-    const uint32_t panels = (uint32_t)__cvta_generic_to_shared(smem), mine_at = g * kPanelStride + t * 16;
+    // Copies a panel; what lies behind the rows or behind K is zero.  4 bits: the sixteen vectors of four blocks are put so that those
+    // that the four lanes read together lie side by side.
+    const uint32_t panels = (uint32_t)__cvta_generic_to_shared(smem);
     auto copy_panel = [&](int at, uint32_t to) {
         constexpr int chunks = kPanel / 8;
         for (int i = tid; i < 8 * NT * chunks; i += kLayerThreads) {
-            const int r = i / chunks, c = i % chunks, k = at + c * 8;
-            const bool in = r < rows && k < k1;
+            const int r = i / chunks, c = i % chunks, k = at + c * 8, pair = pair0 + (two ? r >> 1 : r);
+            const bool in = r < (two ? 2 * rows : rows) && k < k1;
             const void* from = a.x;
             if (in) {
-                if (STAGE == HIDDEN) from = static_cast<const char*>(a.x) + ((size_t)a.notes->row[pair0 + r] * a.C + k) * 2;
-                else from = static_cast<const char*>(a.hidden) + ((size_t)(pair0 + r) * a.H + k) * 2;
+                if (STAGE == HIDDEN) from = static_cast<const char*>(MX ? a.ordered : a.x) + ((size_t)a.notes->row[pair] * a.C + k) * 2;
+                else from = static_cast<const char*>(a.hidden) + ((size_t)(2 * pair + (two ? r & 1 : 0)) * a.H + k) * 2;
             }
-            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to + (uint32_t)(r * kPanelStride + c * 16)),
-                         "l"(from), "r"(in ? 16 : 0) : "memory");
+            const int place = MX ? (c & ~15) | (c >> 2 & 3) | (c & 3) << 2 : c;
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to + (uint32_t)(r * kPanelStride + place * 16)), "l"(from), "r"(in ? 16 : 0)
+                         : "memory");
         }
-        asm volatile("cp.async.commit_group;" ::: "memory");
     };
-    auto rows_at = [&](uint32_t panel, int block, int n) {
+    auto rows_at = [&](uint32_t panel, int vectors, int n) {       // of 64 bytes before, in the panel
         uint4 v;
         asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
-                     : "r"(panel + (uint32_t)(n * 8 * kPanelStride + block * 64)));
+                     : "r"(panel + (uint32_t)(n * 8 * kPanelStride + vectors * 64)));
         return v;
     };
-    copy_panel(k0, panels);
-    int buffer = 0;
-    for (int p = k0; p < k1; p += kPanel, buffer ^= 1) {
-        asm volatile("cp.async.wait_group 0;" ::: "memory");
-        __syncthreads();                                          // the panel is there, and the other one is done with
-        if (p + kPanel < k1) copy_panel(p + kPanel, panels + (buffer ^ 1) * kPanelBytes);
-        const uint32_t panel = panels + buffer * kPanelBytes + mine_at;
-        const int end = min(kPanel, k1 - p);
+    const uint32_t ring = panels + 2 * kPanelBytes + tid * 16;
+    const int stride = kPiece * a.split, steps = (k1 - k0 + stride - 1) / stride, per_panel = kPanel / stride;
+    auto request = [&](int step, uint32_t stage, uint32_t& powers) {          // powers: of the lane's block, a byte for each of the four rows
+        const int k = k0 + step * stride + part * kPiece + (MX ? 32 : 8) * t;
+        powers = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const bool in = has(i) && k < k1;
+            const uint32_t at = in ? row_of(i) + (uint32_t)k / (MX ? 32 : 8) : 0u;
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(ring + (stage * 4 + i) * kRingRow), "l"(weights_of(i) + at), "r"(in ? 16 : 0) : "memory");
+            if (MX && in) powers |= (uint32_t)__ldg(scales_of(i) + at) << (8 * i);
+        }
+    };
+    uint32_t largest = 0;                                         // powers that the sums are relative to, of the lane's four rows
+    auto multiply = [&](uint32_t stage, uint32_t powers, uint32_t panel, int first) {     // first: element of the panel
+        uint4 v[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v[i].x), "=r"(v[i].y), "=r"(v[i].z), "=r"(v[i].w) : "r"(ring + (stage * 4 + i) * kRingRow));
         if (!MX) {
-            // Blocks of weights under way at once, as the registers have room.
-            constexpr int kAtOnce = NT == 4 ? 3 : 4;
-            for (int b = part * 32; b < end; b += a.split * 32 * kAtOnce) {
-                uint4 v[kAtOnce][4];
 #pragma unroll
-                for (int u = 0; u < kAtOnce; ++u) {
-                    const int k = b + u * a.split * 32 + t * 8;
+            for (int n = 0; n < NT; ++n) {
+                const uint4 x = rows_at(panel, first >> 5, n);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        v[u][i] = make_uint4(0u, 0u, 0u, 0u);
-                        if (has(i) && k < end) v[u][i] = load_weights(weights_of(i) + (row_of(i) + (uint32_t)(p + k) / 8));
-                    }
-                }
+                for (int m = 0; m < 2; ++m) product<BF16>(acc[m][n], v[2 * m].x, v[2 * m + 1].x, v[2 * m].y, v[2 * m + 1].y, x.x, x.y);
 #pragma unroll
-                for (int u = 0; u < kAtOnce; ++u) {
-                    const int k = b + u * a.split * 32;
-                    if (k >= end) break;
+                for (int m = 0; m < 2; ++m) product<BF16>(acc[m][n], v[2 * m].z, v[2 * m + 1].z, v[2 * m].w, v[2 * m + 1].w, x.z, x.w);
+            }
+            return;
+        }
+        uint32_t top = __vmaxu4(powers, __shfl_xor_sync(0xFFFFFFFFu, powers, 1));
+        top = __vmaxu4(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
+        top = __vmaxu4(top, largest);
+        if (__any_sync(0xFFFFFFFFu, top != largest)) {
 #pragma unroll
-                    for (int n = 0; n < NT; ++n) {
-                        const uint4 x = rows_at(panel, k >> 5, n);
+            for (int i = 0; i < 4; ++i) {
+                const int fall = (int)(top >> (8 * i) & 255u) - (int)(largest >> (8 * i) & 255u);
+                const float f = __uint_as_float((uint32_t)max(127 - fall, 0) << 23);
 #pragma unroll
-                        for (int m = 0; m < 2; ++m) {
-                            const uint4 &lo = v[u][2 * m], &hi = v[u][2 * m + 1];
-                            product<BF16>(acc[m][n], lo.x, hi.x, lo.y, hi.y, x.x, x.y);
-                            product<BF16>(acc[m][n], lo.z, hi.z, lo.w, hi.w, x.z, x.w);
-                        }
-                    }
+                for (int n = 0; n < NT; ++n) {
+                    acc[i >> 1][n][(i & 1) * 2] *= f;
+                    acc[i >> 1][n][(i & 1) * 2 + 1] *= f;
                 }
             }
-        } else {
-            // Four blocks to a step: lane t reads the codes of block t and passes them round the four lanes, so that each has its eight
-            // elements of every block.
-            for (int b = part * 128; b < end; b += a.split * 128) {
-                const int block = (p + b) / kMxBlock;
-                uint4 v[4];
-                uint32_t powers = 0;                              // of block t, a byte for each of the four rows
+            largest = top;
+        }
+        uint32_t factor[4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    v[i] = make_uint4(0u, 0u, 0u, 0u);
-                    if (has(i) && block + t < blocks) v[i] = load_weights(weights_of(i) + (row_of(i) + (uint32_t)(block + t)));
-                    if (has(i) && block + t < blocks) powers |= (uint32_t)__ldg(scales_of(i) + (row_of(i) + (uint32_t)(block + t))) << (8 * i);
-                }
-                uint32_t mine[4][4];                              // [row][block]
+        for (int i = 0; i < 4; ++i) factor[i] = block_factor<BF16>((int)(top >> (8 * i) & 255u) - (int)(powers >> (8 * i) & 255u));
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const uint32_t c[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
-                    uint32_t got[4];                              // by the distance of the lane that it came from
+        for (int j = 0; j < 4; ++j) {
+            uint32_t r[4][4];
 #pragma unroll
-                    for (int d = 0; d < 4; ++d) {
-                        const int to = t ^ d;
-                        const uint32_t out = to == 0 ? c[0] : to == 1 ? c[1] : to == 2 ? c[2] : c[3];
-                        got[d] = d ? __shfl_xor_sync(0xFFFFFFFFu, out, d) : out;
-                    }
+            for (int i = 0; i < 4; ++i) decode8<BF16>(r[i], j == 0 ? v[i].x : j == 1 ? v[i].y : j == 2 ? v[i].z : v[i].w, factor[i]);
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        const int d = q ^ t;
-                        mine[i][q] = d == 0 ? got[0] : d == 1 ? got[1] : d == 2 ? got[2] : got[3];
-                    }
-                }
+            for (int n = 0; n < NT; ++n) {
+                const uint4 x = rows_at(panel, (first >> 5) + j, n);
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    if (b + q * 32 >= end) break;
-                    uint32_t r[4][4];
-                    float s[4];
-                    const uint32_t power = __shfl_sync(0xFFFFFFFFu, powers, (lane & 28) | q);
+                for (int m = 0; m < 2; ++m) product<BF16>(acc[m][n], r[2 * m][0], r[2 * m + 1][0], r[2 * m][1], r[2 * m + 1][1], x.x, x.y);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        decode8<BF16>(r[i], mine[i][q]);
-                        s[i] = mx_power(power >> (8 * i) & 255u);
-                    }
+                for (int m = 0; m < 2; ++m) product<BF16>(acc[m][n], r[2 * m][2], r[2 * m + 1][2], r[2 * m][3], r[2 * m + 1][3], x.z, x.w);
+            }
+        }
+    };
+    uint32_t powers[4];
+    copy_panel(k0, panels);
 #pragma unroll
-                    for (int n = 0; n < NT; ++n) {
-                        const uint4 x = rows_at(panel, (b >> 5) + q, n);
+    for (int s = 0; s < 3; ++s) {
+        if (s < steps) request(s, s, powers[s]);
+        asm volatile("cp.async.commit_group;" ::: "memory");     // of step s, with the first panel in step 0's
+    }
+    // Step s, with the copies of step s + 3 in a group of their own.  A panel was asked for with those of three steps behind the start of the
+    // one before.
+    auto turn = [&](int s, uint32_t stage, uint32_t p, uint32_t& later) {
+        const int panel = s / per_panel, in_panel = s - panel * per_panel;
+        if (in_panel == 0) {
+            if (per_panel >= 3 || s == 0) asm volatile("cp.async.wait_group 2;" ::: "memory");
+            else if (per_panel == 2) asm volatile("cp.async.wait_group 1;" ::: "memory");
+            else asm volatile("cp.async.wait_group 0;" ::: "memory");
+            __syncthreads();                                      // the panel is there, and the other one is done with
+            if (k0 + (panel + 1) * kPanel < k1) copy_panel(k0 + (panel + 1) * kPanel, panels + ((panel & 1) ^ 1) * kPanelBytes);
+        }
+        if (s + 3 < steps) request(s + 3, (stage + 3) & 3, later);
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        asm volatile("cp.async.wait_group 3;" ::: "memory");
+        multiply(stage, p, panels + (panel & 1) * kPanelBytes + g * kPanelStride + t * 16, in_panel * stride + part * kPiece);
+    };
+    for (int s = 0; s < steps; s += 4) {
+        turn(s, 0, powers[0], powers[3]);
+        if (s + 1 < steps) turn(s + 1, 1, powers[1], powers[0]);
+        if (s + 2 < steps) turn(s + 2, 2, powers[2], powers[1]);
+        if (s + 3 < steps) turn(s + 3, 3, powers[3], powers[2]);
+    }
+    if (MX) {
 #pragma unroll
-                        for (int m = 0; m < 2; ++m) {
-                            float c[4] = {0.f, 0.f, 0.f, 0.f};
-                            product<BF16>(c, r[2 * m][0], r[2 * m + 1][0], r[2 * m][1], r[2 * m + 1][1], x.x, x.y);
-                            product<BF16>(c, r[2 * m][2], r[2 * m + 1][2], r[2 * m][3], r[2 * m + 1][3], x.z, x.w);
-                            acc[m][n][0] += s[2 * m] * c[0];
-                            acc[m][n][1] += s[2 * m] * c[1];
-                            acc[m][n][2] += s[2 * m + 1] * c[2];
-                            acc[m][n][3] += s[2 * m + 1] * c[3];
-                        }
-                    }
-                }
+        for (int i = 0; i < 4; ++i) {
+            const float f = mx_power(largest >> (8 * i) & 255u);
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                acc[i >> 1][n][(i & 1) * 2] *= f;
+                acc[i >> 1][n][(i & 1) * 2 + 1] *= f;
             }
         }
     }
     asm volatile("cp.async.wait_group 0;" ::: "memory");         // an empty share has its panel of zeros under way
-    // The warps' sums in shared memory, [warp][2][column][16]; those that share a tile are added in their order.
+    // The warps' sums in shared memory, [warp][2][column][17]; those that share a tile are added in their order.
     __syncthreads();
     float* sums = reinterpret_cast<float*>(smem);
 #pragma unroll
@@ -404,23 +450,34 @@ __device__ __forceinline__ void layer_rows(const LayerArgs& a, char* smem, int e
                 sums[((warp * 2 + m) * (8 * NT) + n * 8 + 2 * t + (c & 1)) * 17 + g + (c >> 1) * 8] = acc[m][n][c];
     __syncthreads();
     const int width = STAGE == HIDDEN ? 16 : 32;
-    for (int i = tid; i < per_cta * 8 * NT * width; i += kLayerThreads) {
-        const int u = i % width, c = i / width % (8 * NT), s = i / (width * 8 * NT), at = (unit * per_cta + s) * width + u;
-        if (c >= rows || at >= M) continue;
-        auto sum = [&](int m, int r) {
+    for (int i = tid; i < per_cta * rows * width; i += kLayerThreads) {
+        const int u = i % width, c = i / width % rows, s = i / (width * rows), at = (unit * per_cta + s) * width + u;
+        if (at >= M) continue;
+        auto sum = [&](int m, int column, int r) {
             float v = 0.f;
-            for (int q = 0; q < a.split; ++q) v += sums[(((s * a.split + q) * 2 + m) * (8 * NT) + c) * 17 + r];
+            for (int q = 0; q < a.split; ++q) v += sums[(((s * a.split + q) * 2 + m) * (8 * NT) + column) * 17 + r];
             return v;
         };
         if (STAGE == HIDDEN) {
-            const float gate = sum(0, u), up = sum(1, u);
+            const float gate = sum(0, c, u), up = sum(1, c, u);
             const float f = a.act == EMC2_ACT_SILU ? gate / (1.0f + expf(-gate)) : 0.5f * gate * erfcf(-0.70710678f * gate);
             const float h = f * up;
-            const size_t to = (size_t)(pair0 + c) * a.H + at;
-            if (BF16) static_cast<__nv_bfloat16*>(a.hidden)[to] = __float2bfloat16_rn(h);
-            else static_cast<__half*>(a.hidden)[to] = __float2half_rn(h);
+            const size_t to = (size_t)(2 * (pair0 + c)) * a.H + (MX ? (at & ~7) + ordered_place(at & 7) : at);
+            // What the first part leaves is exact; an infinite one leaves nothing.
+            if (BF16) {
+                __nv_bfloat16* p = static_cast<__nv_bfloat16*>(a.hidden) + to;
+                p[0] = __float2bfloat16_rn(h);
+                const float rest = h - __bfloat162float(p[0]);
+                p[a.H] = __float2bfloat16_rn(isinf(h) ? 0.f : rest);
+            } else {
+                __half* p = static_cast<__half*>(a.hidden) + to;
+                p[0] = __float2half_rn(h);
+                const float rest = h - __half2float(p[0]);
+                p[a.H] = __float2half_rn(isinf(__half2float(p[0])) ? 0.f : rest);
+            }
         } else {
-            a.part[((size_t)blockIdx.y * (a.n * a.k) + pair0 + c) * a.C + at] = sum(u >> 4, u & 15);
+            const float z = two ? sum(u >> 4, 2 * c, u & 15) + sum(u >> 4, 2 * c + 1, u & 15) : sum(u >> 4, c, u & 15);
+            a.part[((size_t)blockIdx.y * (a.n * a.k) + pair0 + c) * a.C + at] = z;
         }
     }
     __syncthreads();
@@ -431,11 +488,31 @@ template <int STAGE, bool MX, bool BF16>
 __device__ __forceinline__ void layer_unit(const LayerArgs& a, char* smem) {
     const int i = blockIdx.x / a.tiles;
     for (int p = a.notes->start[i]; p < a.notes->start[i + 1]; p += kRowsAtOnce) {
-        const int e = a.notes->expert[i], rows = min(kRowsAtOnce, a.notes->start[i + 1] - p);
-        if (rows <= 8) layer_rows<STAGE, MX, BF16, 1>(a, smem, e, p, rows);
-        else if (rows <= 16) layer_rows<STAGE, MX, BF16, 2>(a, smem, e, p, rows);
-        else layer_rows<STAGE, MX, BF16, 4>(a, smem, e, p, rows);
+        const bool two = STAGE == DOWN && a.notes->start[i + 1] - a.notes->start[i] <= kTwoParts;
+        const int e = a.notes->expert[i], rows = min(kRowsAtOnce, a.notes->start[i + 1] - p), columns = two ? 2 * rows : rows;
+        if (columns <= 8) layer_rows<STAGE, MX, BF16, 1>(a, smem, e, p, rows, two);
+        else if (columns <= 16) layer_rows<STAGE, MX, BF16, 2>(a, smem, e, p, rows, two);
+        else layer_rows<STAGE, MX, BF16, 4>(a, smem, e, p, rows, two);
     }
+}
+
+// y of four channels of a row: its choices in their order, of each the shares in theirs.
+template <bool BF16>
+__device__ __forceinline__ void layer_sum(const LayerArgs& a, int row, int c) {
+    const size_t apart = (size_t)a.n * a.k * a.C;
+    float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int j = 0; j < a.k; ++j) {
+        const float* at = a.part + (size_t)a.notes->place[row * a.k + j] * a.C + c;
+        const float p = a.weights[row * a.k + j];
+        float4 z = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+        for (int s = 0; s < a.shares; ++s) {
+            const float4 q = __ldcg(reinterpret_cast<const float4*>(at + s * apart));
+            z.x += q.x; z.y += q.y; z.z += q.z; z.w += q.w;
+        }
+        y.x += p * z.x; y.y += p * z.y; y.z += p * z.z; y.w += p * z.w;
+    }
+    store_row4(a.y, ((size_t)row * a.C + c) / 4, y, BF16 ? EMC2_BF16 : EMC2_F16);
 }
 
 template <bool MX, bool BF16>
@@ -453,6 +530,10 @@ __global__ void __launch_bounds__(kLayerThreads, 2) layer_down_kernel(LayerArgs 
     __shared__ int last;
     if ((int)blockIdx.x >= a.notes->active * a.tiles) return;
     layer_unit<DOWN, MX, BF16>(a, panels);
+    if (!a.last_adds) {
+        release_successor();
+        return;
+    }
     const int unit = blockIdx.x % a.tiles, tid = threadIdx.x;
     __syncthreads();
     if (tid == 0) {
@@ -462,20 +543,17 @@ __global__ void __launch_bounds__(kLayerThreads, 2) layer_down_kernel(LayerArgs 
     __syncthreads();
     if (!last) return;
     __threadfence();
-    const int width = min(a.C - unit * (kLayerWarps / a.split) * 32, (kLayerWarps / a.split) * 32), used = a.notes->used, pairs = a.n * a.k;
-    for (int o = tid; o < used * width; o += kLayerThreads) {
-        const int row = o / width, c = unit * (kLayerWarps / a.split) * 32 + o % width;
-        float y = 0.f;
-        for (int j = 0; j < a.k; ++j) {
-            const int at = a.notes->place[row * a.k + j];
-            float z = 0.f;
-            for (int s = 0; s < a.shares; ++s) z += __ldcg(a.part + ((size_t)s * pairs + at) * a.C + c);
-            y += a.weights[row * a.k + j] * z;
-        }
-        if (BF16) static_cast<__nv_bfloat16*>(a.y)[(size_t)row * a.C + c] = __float2bfloat16_rn(y);
-        else static_cast<__half*>(a.y)[(size_t)row * a.C + c] = __float2half_rn(y);
-    }
+    const int wide = kLayerWarps / a.split * 32, width = min(a.C - unit * wide, wide) / 4;
+    for (int o = tid; o < a.notes->used * width; o += kLayerThreads) layer_sum<BF16>(a, o / width, unit * wide + o % width * 4);
     if (tid == 0) a.notes->arrived_tile[unit] = 0;
+}
+
+template <bool BF16>
+__global__ void __launch_bounds__(kLayerThreads) layer_sum_kernel(LayerArgs a) {
+    await_predecessor();
+    const int o = blockIdx.x * kLayerThreads + threadIdx.x, width = a.C / 4;
+    if (o < a.notes->used * width) layer_sum<BF16>(a, o / width, o % width * 4);
+    release_successor();
 }
 
 // ---- scratch: notes, hidden values, partial sums
@@ -484,25 +562,25 @@ constexpr int kPartRows = 2 * kMaxSlots;     // shares times pairs, at most
 
 template <bool MX, bool BF16>
 cudaError_t launch_layer(emc2_bridge* h, LayerArgs a, cudaStream_t st) {
-    constexpr size_t most = 2 * kPanelBytes;
+    constexpr size_t most = kProductShared;
     cudaError_t e = allow_shared(layer_hidden_kernel<MX, BF16>, most);
     if (e == cudaSuccess) e = allow_shared(layer_down_kernel<MX, BF16>, most);
     if (e != cudaSuccess) return e;
     const int experts = std::min(a.E, a.n * a.k);
     const int step = MX ? 128 : 32;
-    // Warps that share a tile: as many as fill the SMs, and as have blocks.
+    // Warps that share a tile: as many as fill the SMs, and as have steps.
     auto plan = [&](int K, int M, int width) {
-        const int blocks = (K + step - 1) / step, most_split = std::min(kPanel / step, kLayerWarps);
+        const int steps = (K + step - 1) / step, most_split = std::min(kPanel / step, kLayerWarps);
         a.split = 1;
         for (;; a.split *= 2) {
             const int per = kLayerWarps / a.split * width;
             a.tiles = (M + per - 1) / per;
-            if (a.tiles * experts >= 2 * h->num_sms || 2 * a.split > most_split || a.split >= blocks) break;
+            if (a.tiles * experts >= 2 * h->num_sms || 2 * a.split > most_split || a.split >= steps) break;
         }
     };
     {
         LaunchScope ls(h, K_LAYER_ROUTE, st);
-        layer_route_kernel<BF16><<<a.n, kLayerThreads, 0, st>>>(a);
+        layer_route_kernel<BF16><<<a.n, kRouteThreads, 0, st>>>(a);
     }
     {
         LaunchScope ls(h, K_LAYER_HIDDEN, st);
@@ -516,7 +594,12 @@ cudaError_t launch_layer(emc2_bridge* h, LayerArgs a, cudaStream_t st) {
         while (a.shares < kMaxShares && a.tiles * experts * a.shares < 4 * h->num_sms && a.H >= 2 * a.shares * 256 &&
                2 * a.shares * a.n * a.k <= kPartRows)
             a.shares *= 2;
+        a.last_adds = a.n * a.k * a.shares <= kLastAdds;
         launch_chained(layer_down_kernel<MX, BF16>, dim3((unsigned)(a.tiles * experts), (unsigned)a.shares), kLayerThreads, most, st, a);
+    }
+    if (!a.last_adds) {
+        LaunchScope ls(h, K_LAYER_SUM, st);
+        launch_chained(layer_sum_kernel<BF16>, dim3((unsigned)(a.n * a.C / 4 + kLayerThreads - 1) / kLayerThreads), kLayerThreads, 0, st, a);
     }
     return cudaGetLastError();
 }
@@ -539,8 +622,12 @@ int run_layer(emc2_bridge* h, LayerArgs a, int type, bool mx, cudaStream_t st) {
     if (!device.ok) return EMC2_ERR_CUDA;
     a.status = h->d_status;
     a.notes = static_cast<LayerNotes*>(r.notes);
-    a.hidden = r.slab;
-    a.part = reinterpret_cast<float*>(static_cast<char*>(r.slab) + up256((size_t)kMaxSlots * a.H * 2));
+    char* at = static_cast<char*>(r.slab);
+    a.hidden = at;
+    at += up256((size_t)kMaxSlots * 2 * a.H * 2);
+    a.part = reinterpret_cast<float*>(at);
+    at += up256((size_t)kPartRows * a.C * sizeof(float));
+    a.ordered = mx ? at : nullptr;
     a.split = a.tiles = a.shares = 1;
     const cudaError_t e = type == EMC2_BF16 ? (mx ? launch_layer<true, true>(h, a, st) : launch_layer<false, true>(h, a, st))
                                             : (mx ? launch_layer<true, false>(h, a, st) : launch_layer<false, false>(h, a, st));
@@ -552,7 +639,7 @@ int run_layer(emc2_bridge* h, LayerArgs a, int type, bool mx, cudaStream_t st) {
 size_t layer_notes_bytes() { return up256(sizeof(LayerNotes)); }
 size_t layer_scratch_bytes(int max_channels, int max_hidden) {
     if (max_hidden <= 0) return 0;
-    return up256((size_t)kMaxSlots * max_hidden * 2) + (size_t)kPartRows * max_channels * sizeof(float);
+    return up256((size_t)kMaxSlots * 2 * max_hidden * 2) + up256((size_t)kPartRows * max_channels * sizeof(float)) + (size_t)kMaxLayerRows * max_channels * 2;
 }
 
 }  // namespace emc2
