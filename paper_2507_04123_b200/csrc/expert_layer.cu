@@ -63,7 +63,7 @@ struct LayerArgs {
     float* part;                             // [share][sorted pair][C]
     int* status;
     int n, C, H, E, k, act;
-    int split;                               // warps that share a tile, each with every split-th block
+    int split_log;                           // warps that share a tile, each with every such step: 1 << split_log
     int tiles;                               // CTAs per expert
     int shares;                              // third kernel: of the hidden units
     int last_adds;                           // ... and whether its last CTAs add up
@@ -287,21 +287,21 @@ template <int STAGE, bool MX, bool BF16, int NT>
 __device__ __forceinline__ void layer_rows(const LayerArgs& a, char* smem, int e, int pair0, int rows, bool two) {
     constexpr int kPiece = MX ? 128 : 32;                         // elements of a step
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
-    const int per_cta = kLayerWarps / a.split, part = warp % a.split, slot = warp / a.split;
+    const int split = 1 << a.split_log, per_cta = kLayerWarps >> a.split_log, part = warp & (split - 1), slot = warp >> a.split_log;
     const int K = STAGE == HIDDEN ? a.C : a.H, M = STAGE == HIDDEN ? a.H : a.C;
     const int unit = blockIdx.x % a.tiles, tile = unit * per_cta + slot;        // of 16 hidden units, or of 32 channels
     // The third kernel's share of the hidden units, whole steps of the products; the last ones ragged.
     const int each = STAGE == HIDDEN ? K : ((K + a.shares - 1) / a.shares + 127) / 128 * 128;
     const int k0 = STAGE == HIDDEN ? 0 : min(K, (int)blockIdx.y * each), k1 = min(K, k0 + each);
-    // The rows of weights that this lane reads: the first, in units of 16 bytes (all of a call's have fewer than 2^29), and how many of
-    // those after every eighth there are.
+    // The lane's next vector of its first row of weights (of the up projection's too) and of the powers; the others are a constant number of
+    // rows behind.  Rows behind the last are read as the last, and come to nothing.
     const int blocks = (K + kMxBlock - 1) / kMxBlock, units = MX ? blocks : K / 8, r0 = tile * (STAGE == HIDDEN ? 16 : 32) + g;
-    const uint32_t w0 = (uint32_t)(e * M + r0) * (uint32_t)units;
-    const int there = max(0, (M - r0 + 7) / 8);
-    auto has = [&](int i) { return (STAGE == HIDDEN ? i & 1 : i) < there; };
-    auto row_of = [&](int i) { return w0 + (uint32_t)((STAGE == HIDDEN ? i & 1 : i) * 8 * units); };
-    auto weights_of = [&](int i) { return static_cast<const uint4*>(a.w[STAGE == HIDDEN ? i >> 1 : 2]); };
-    auto scales_of = [&](int i) { return a.scales[STAGE == HIDDEN ? i >> 1 : 2]; };
+    const size_t start = (size_t)(e * M) * units + k0 / (MX ? 32 : 8) + part * 4 + t;         // of the expert's row 0, in units of 16 bytes
+    uint32_t row_at[STAGE == HIDDEN ? 2 : 4];
+#pragma unroll
+    for (int i = 0; i < (STAGE == HIDDEN ? 2 : 4); ++i) row_at[i] = (uint32_t)min(r0 + 8 * i, M - 1) * (uint32_t)units;
+    const uint4* w[2] = {static_cast<const uint4*>(a.w[STAGE == HIDDEN ? 0 : 2]) + start, static_cast<const uint4*>(a.w[1]) + (STAGE == HIDDEN ? start : 0)};
+    const uint8_t* sc[2] = {MX ? a.scales[STAGE == HIDDEN ? 0 : 2] + start : nullptr, MX && STAGE == HIDDEN ? a.scales[1] + start : nullptr};
     float acc[2][NT][4];
 #pragma unroll
     for (int m = 0; m < 2; ++m)
@@ -312,19 +312,27 @@ __device__ __forceinline__ void layer_rows(const LayerArgs& a, char* smem, int e
     // Copies a panel; what lies behind the rows or behind K is zero.  4 bits: the sixteen vectors of four blocks are put so that those
     // that the four lanes read together lie side by side.
     const uint32_t panels = (uint32_t)__cvta_generic_to_shared(smem);
-    auto copy_panel = [&](int at, uint32_t to) {
-        constexpr int chunks = kPanel / 8;
-        for (int i = tid; i < 8 * NT * chunks; i += kLayerThreads) {
-            const int r = i / chunks, c = i % chunks, k = at + c * 8, pair = pair0 + (two ? r >> 1 : r);
-            const bool in = r < (two ? 2 * rows : rows) && k < k1;
-            const void* from = a.x;
-            if (in) {
-                if (STAGE == HIDDEN) from = static_cast<const char*>(MX ? a.ordered : a.x) + ((size_t)a.notes->row[pair] * a.C + k) * 2;
-                else from = static_cast<const char*>(a.hidden) + ((size_t)(2 * pair + (two ? r & 1 : 0)) * a.H + k) * 2;
-            }
-            const int place = MX ? (c & ~15) | (c >> 2 & 3) | (c & 3) << 2 : c;
-            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to + (uint32_t)(r * kPanelStride + place * 16)), "l"(from), "r"(in ? 16 : 0)
-                         : "memory");
+    constexpr int kChunks = kPanel / 8;                           // vectors of a panel's row; a thread copies one of NT rows
+    static_assert(kLayerThreads == 8 * kChunks, "rows of a panel");
+    const char* from[NT];
+    {
+        const int r = tid / kChunks, c = tid % kChunks;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const int column = r + 8 * n, pair = pair0 + (two ? column >> 1 : column);
+            from[n] = nullptr;
+            if (column >= (two ? 2 * rows : rows)) continue;
+            if (STAGE == HIDDEN) from[n] = static_cast<const char*>(MX ? a.ordered : a.x) + ((size_t)a.notes->row[pair] * a.C + c * 8) * 2;
+            else from[n] = static_cast<const char*>(a.hidden) + ((size_t)(2 * pair + (two ? column & 1 : 0)) * a.H + c * 8) * 2;
+        }
+    }
+    auto copy_panel = [&](int k, uint32_t to) {
+        const int r = tid / kChunks, c = tid % kChunks, place = MX ? (c & ~15) | (c >> 2 & 3) | (c & 3) << 2 : c;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const bool in = from[n] && k + c * 8 < k1;
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to + (uint32_t)((r + 8 * n) * kPanelStride + place * 16)),
+                         "l"(in ? from[n] + 2 * k : static_cast<const char*>(a.x)), "r"(in ? 16 : 0) : "memory");
         }
     };
     auto rows_at = [&](uint32_t panel, int vectors, int n) {       // of 64 bytes before, in the panel
@@ -334,16 +342,23 @@ __device__ __forceinline__ void layer_rows(const LayerArgs& a, char* smem, int e
         return v;
     };
     const uint32_t ring = panels + 2 * kPanelBytes + tid * 16;
-    const int stride = kPiece * a.split, steps = (k1 - k0 + stride - 1) / stride, per_panel = kPanel / stride;
-    auto request = [&](int step, uint32_t stage, uint32_t& powers) {          // powers: of the lane's block, a byte for each of the four rows
-        const int k = k0 + step * stride + part * kPiece + (MX ? 32 : 8) * t;
+    const int stride = kPiece << a.split_log, steps = (k1 - k0 + stride - 1) / stride, panel_log = (MX ? 1 : 3) - a.split_log;       // steps of a panel
+    int left = k1 - (k0 + part * kPiece + (MX ? 32 : 8) * t);     // elements from the lane's next vector on
+    auto request = [&](uint32_t stage, uint32_t& powers) {        // powers: of the lane's block, a byte for each of the four rows
+        const bool in = left > 0;
         powers = 0;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const bool in = has(i) && k < k1;
-            const uint32_t at = in ? row_of(i) + (uint32_t)k / (MX ? 32 : 8) : 0u;
-            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(ring + (stage * 4 + i) * kRingRow), "l"(weights_of(i) + at), "r"(in ? 16 : 0) : "memory");
-            if (MX && in) powers |= (uint32_t)__ldg(scales_of(i) + at) << (8 * i);
+            const int q = STAGE == HIDDEN ? i >> 1 : 0, r = STAGE == HIDDEN ? i & 1 : i;
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(ring + (stage * 4 + i) * kRingRow),
+                         "l"(in ? w[q] + row_at[r] : static_cast<const uint4*>(a.x)), "r"(in ? 16 : 0) : "memory");
+            if (MX && in) powers |= (uint32_t)__ldg(sc[q] + row_at[r]) << (8 * i);
+        }
+        left -= stride;
+#pragma unroll
+        for (int q = 0; q < (STAGE == HIDDEN ? 2 : 1); ++q) {
+            w[q] += stride / (MX ? 32 : 8);
+            if (MX) sc[q] += stride / 32;
         }
     };
     uint32_t largest = 0;                                         // powers that the sums are relative to, of the lane's four rows
@@ -353,14 +368,17 @@ __device__ __forceinline__ void layer_rows(const LayerArgs& a, char* smem, int e
         for (int i = 0; i < 4; ++i)
             asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v[i].x), "=r"(v[i].y), "=r"(v[i].z), "=r"(v[i].w) : "r"(ring + (stage * 4 + i) * kRingRow));
         if (!MX) {
+            uint4 x[NT];
 #pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                const uint4 x = rows_at(panel, first >> 5, n);
+            for (int n = 0; n < NT; ++n) x[n] = rows_at(panel, first >> 5, n);
 #pragma unroll
-                for (int m = 0; m < 2; ++m) product<BF16>(acc[m][n], v[2 * m].x, v[2 * m + 1].x, v[2 * m].y, v[2 * m + 1].y, x.x, x.y);
+            for (int n = 0; n < NT; ++n)
 #pragma unroll
-                for (int m = 0; m < 2; ++m) product<BF16>(acc[m][n], v[2 * m].z, v[2 * m + 1].z, v[2 * m].w, v[2 * m + 1].w, x.z, x.w);
-            }
+                for (int m = 0; m < 2; ++m) product<BF16>(acc[m][n], v[2 * m].x, v[2 * m + 1].x, v[2 * m].y, v[2 * m + 1].y, x[n].x, x[n].y);
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int m = 0; m < 2; ++m) product<BF16>(acc[m][n], v[2 * m].z, v[2 * m + 1].z, v[2 * m].w, v[2 * m + 1].w, x[n].z, x[n].w);
             return;
         }
         uint32_t top = __vmaxu4(powers, __shfl_xor_sync(0xFFFFFFFFu, powers, 1));
@@ -401,21 +419,21 @@ __device__ __forceinline__ void layer_rows(const LayerArgs& a, char* smem, int e
     copy_panel(k0, panels);
 #pragma unroll
     for (int s = 0; s < 3; ++s) {
-        if (s < steps) request(s, s, powers[s]);
+        if (s < steps) request(s, powers[s]);
         asm volatile("cp.async.commit_group;" ::: "memory");     // of step s, with the first panel in step 0's
     }
     // Step s, with the copies of step s + 3 in a group of their own.  A panel was asked for with those of three steps behind the start of the
     // one before.
     auto turn = [&](int s, uint32_t stage, uint32_t p, uint32_t& later) {
-        const int panel = s / per_panel, in_panel = s - panel * per_panel;
+        const int panel = s >> panel_log, in_panel = s & ((1 << panel_log) - 1);
         if (in_panel == 0) {
-            if (per_panel >= 3 || s == 0) asm volatile("cp.async.wait_group 2;" ::: "memory");
-            else if (per_panel == 2) asm volatile("cp.async.wait_group 1;" ::: "memory");
+            if (panel_log >= 2 || s == 0) asm volatile("cp.async.wait_group 2;" ::: "memory");
+            else if (panel_log == 1) asm volatile("cp.async.wait_group 1;" ::: "memory");
             else asm volatile("cp.async.wait_group 0;" ::: "memory");
             __syncthreads();                                      // the panel is there, and the other one is done with
             if (k0 + (panel + 1) * kPanel < k1) copy_panel(k0 + (panel + 1) * kPanel, panels + ((panel & 1) ^ 1) * kPanelBytes);
         }
-        if (s + 3 < steps) request(s + 3, (stage + 3) & 3, later);
+        if (s + 3 < steps) request((stage + 3) & 3, later);
         asm volatile("cp.async.commit_group;" ::: "memory");
         asm volatile("cp.async.wait_group 3;" ::: "memory");
         multiply(stage, p, panels + (panel & 1) * kPanelBytes + g * kPanelStride + t * 16, in_panel * stride + part * kPiece);
@@ -450,12 +468,13 @@ __device__ __forceinline__ void layer_rows(const LayerArgs& a, char* smem, int e
                 sums[((warp * 2 + m) * (8 * NT) + n * 8 + 2 * t + (c & 1)) * 17 + g + (c >> 1) * 8] = acc[m][n][c];
     __syncthreads();
     const int width = STAGE == HIDDEN ? 16 : 32;
-    for (int i = tid; i < per_cta * rows * width; i += kLayerThreads) {
-        const int u = i % width, c = i / width % rows, s = i / (width * rows), at = (unit * per_cta + s) * width + u;
+    for (int s = 0; s < per_cta; ++s)
+    for (int c = tid / width; c < rows; c += kLayerThreads / width) {
+        const int u = tid % width, at = (unit * per_cta + s) * width + u;
         if (at >= M) continue;
         auto sum = [&](int m, int column, int r) {
             float v = 0.f;
-            for (int q = 0; q < a.split; ++q) v += sums[(((s * a.split + q) * 2 + m) * (8 * NT) + column) * 17 + r];
+            for (int q = 0; q < split; ++q) v += sums[(((s * split + q) * 2 + m) * (8 * NT) + column) * 17 + r];
             return v;
         };
         if (STAGE == HIDDEN) {
@@ -543,7 +562,7 @@ __global__ void __launch_bounds__(kLayerThreads, 2) layer_down_kernel(LayerArgs 
     __syncthreads();
     if (!last) return;
     __threadfence();
-    const int wide = kLayerWarps / a.split * 32, width = min(a.C - unit * wide, wide) / 4;
+    const int wide = (kLayerWarps >> a.split_log) * 32, width = min(a.C - unit * wide, wide) / 4;
     for (int o = tid; o < a.notes->used * width; o += kLayerThreads) layer_sum<BF16>(a, o / width, unit * wide + o % width * 4);
     if (tid == 0) a.notes->arrived_tile[unit] = 0;
 }
@@ -570,12 +589,11 @@ cudaError_t launch_layer(emc2_bridge* h, LayerArgs a, cudaStream_t st) {
     const int step = MX ? 128 : 32;
     // Warps that share a tile: as many as fill the SMs, and as have steps.
     auto plan = [&](int K, int M, int width) {
-        const int steps = (K + step - 1) / step, most_split = std::min(kPanel / step, kLayerWarps);
-        a.split = 1;
-        for (;; a.split *= 2) {
-            const int per = kLayerWarps / a.split * width;
+        const int steps = (K + step - 1) / step, most_log = MX ? 1 : 3;
+        for (a.split_log = 0;; ++a.split_log) {
+            const int per = (kLayerWarps >> a.split_log) * width;
             a.tiles = (M + per - 1) / per;
-            if (a.tiles * experts >= 2 * h->num_sms || 2 * a.split > most_split || a.split >= steps) break;
+            if (a.tiles * experts >= 2 * h->num_sms || a.split_log == most_log || (1 << a.split_log) >= steps) break;
         }
     };
     {
@@ -628,7 +646,7 @@ int run_layer(emc2_bridge* h, LayerArgs a, int type, bool mx, cudaStream_t st) {
     a.part = reinterpret_cast<float*>(at);
     at += up256((size_t)kPartRows * a.C * sizeof(float));
     a.ordered = mx ? at : nullptr;
-    a.split = a.tiles = a.shares = 1;
+    a.tiles = a.shares = 1;
     const cudaError_t e = type == EMC2_BF16 ? (mx ? launch_layer<true, true>(h, a, st) : launch_layer<false, true>(h, a, st))
                                             : (mx ? launch_layer<true, false>(h, a, st) : launch_layer<false, false>(h, a, st));
     return check_cuda(h, e);
