@@ -7,7 +7,7 @@
 // sorts the pairs (row, choice) by expert.  The second has a CTA per expert and tile of hidden units, the third per expert, tile of channels
 // and share of the hidden units; what they leave is added up in the order of a row's choices, by the last CTA of a tile of channels or, for more
 // rows, by a fourth kernel.  Each kernel is set up while the one before still runs.  In both products every warp streams its own rows of weights
-// from memory into the registers of m16n8k16 products, whose 16 rows are the weights' and whose 8 columns are the rows at hand: a row
+// from memory into the registers of m16n8k16 products, whose 16 rows are the rows at hand and whose 8 columns are the weights': a row
 // of x more costs no more reading, and there are too few of them for larger products to help.
 //
 // The logits are summed in 64 bits, so that the choice does not depend on an order of summation; products in fp32.  act(g) * u goes into the
@@ -269,21 +269,21 @@ __device__ __forceinline__ uint32_t block_factor(int below) {
 
 enum Stage { HIDDEN = 0, DOWN };
 
-// Panels of the rows at hand, in two buffers: [row][kPanel] and 64 bytes more, so that the eight rows that lanes read together lie on
-// different banks.
-constexpr int kPanelStride = kPanel * 2 + 64;
-constexpr int kPanelBytes = kRowsAtOnce * kPanelStride;
+// Panels of the rows at hand, in two buffers, as the 16-byte registers of a product's lanes: [16 rows][8 blocks of 32 elements][2 halves]
+// [32 lanes].  A lane's vector has two words of row g and, between them, those of row g + 8.
+constexpr int kPanelBytes = kRowsAtOnce / 16 * kPanel / 32 * 2 * 512;
 constexpr uint32_t kRingRow = kLayerThreads * 16;
 constexpr size_t kProductShared = 2 * kPanelBytes + 4 * 4 * kRingRow;
+static_assert(kLayerWarps * 2 * kRowsAtOnce * 17 * 4 <= kProductShared, "sums");
 
-// What a warp's rows of weights are: two tiles of 16, of the gate's and the up projection's rows or of the down projection's.  Lane (g, t)
-// has rows g and g + 8 of both.  Which element stands at which place of an instruction does not matter, if weights and rows agree.
+// What a warp's rows of weights are: four tiles of eight, of the gate's and the up projection's rows or of the down projection's.  Lane (g, t)
+// has row g of each.  Which element stands at which place of a product does not matter, if weights and rows agree.
 //   16 bits: a block of 32 elements to a step, of which the lane has 8t .. 8t + 7.
 //    4 bits: four blocks to a step, of which the lane has the t-th.  A block's elements are taken relative to the largest power that the row
 //            has had so far, which the sums are relative to; when it rises, they are scaled down.
 // The weights of the next three steps are on their way to shared memory, in places that the lane alone reads: registers have no room for as
 // much as the memory needs to be asked for at once (50 KB per SM and more).
-template <int STAGE, bool MX, bool BF16, int NT>
+template <int STAGE, bool MX, bool BF16, int MT>
 __device__ __forceinline__ void layer_rows(const LayerArgs& a, char* smem, int e, int pair0, int rows, bool two) {
     constexpr int kPiece = MX ? 128 : 32;                         // elements of a step
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
@@ -302,43 +302,52 @@ __device__ __forceinline__ void layer_rows(const LayerArgs& a, char* smem, int e
     for (int i = 0; i < (STAGE == HIDDEN ? 2 : 4); ++i) row_at[i] = (uint32_t)min(r0 + 8 * i, M - 1) * (uint32_t)units;
     const uint4* w[2] = {static_cast<const uint4*>(a.w[STAGE == HIDDEN ? 0 : 2]) + start, static_cast<const uint4*>(a.w[1]) + (STAGE == HIDDEN ? start : 0)};
     const uint8_t* sc[2] = {MX ? a.scales[STAGE == HIDDEN ? 0 : 2] + start : nullptr, MX && STAGE == HIDDEN ? a.scales[1] + start : nullptr};
-    float acc[2][NT][4];
+    float acc[MT][4][4];                                          // [16 rows][tile]
 #pragma unroll
-    for (int m = 0; m < 2; ++m)
+    for (int m = 0; m < MT; ++m)
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
+        for (int i = 0; i < 4; ++i)
 #pragma unroll
-            for (int c = 0; c < 4; ++c) acc[m][n][c] = 0.f;
-    // Copies a panel; what lies behind the rows or behind K is zero.  4 bits: the sixteen vectors of four blocks are put so that those
-    // that the four lanes read together lie side by side.
+            for (int c = 0; c < 4; ++c) acc[m][i][c] = 0.f;
+    // A thread brings the vectors of rows g and g + 8 for its lane number and, in every 16 rows, the warp's block of a panel, through registers:
+    // their words change places.  Two parts of a hidden value stand in rows g and g + 8, whose sums the lane adds.
     const uint32_t panels = (uint32_t)__cvta_generic_to_shared(smem);
-    constexpr int kChunks = kPanel / 8;                           // vectors of a panel's row; a thread copies one of NT rows
-    static_assert(kLayerThreads == 8 * kChunks, "rows of a panel");
-    const char* from[NT];
-    {
-        const int r = tid / kChunks, c = tid % kChunks;
+    static_assert(kLayerWarps == kPanel / 32, "a block of a panel per warp");
+    const int chunk = MX ? (warp & ~3) * 4 + t * 4 + (warp & 3) : warp * 4 + t;       // vector of a panel's row
+    const char* from[MT][2];
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            const int column = r + 8 * n, pair = pair0 + (two ? column >> 1 : column);
-            from[n] = nullptr;
-            if (column >= (two ? 2 * rows : rows)) continue;
-            if (STAGE == HIDDEN) from[n] = static_cast<const char*>(MX ? a.ordered : a.x) + ((size_t)a.notes->row[pair] * a.C + c * 8) * 2;
-            else from[n] = static_cast<const char*>(a.hidden) + ((size_t)(2 * pair + (two ? column & 1 : 0)) * a.H + c * 8) * 2;
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+            const int r = two ? m * 8 + g : m * 16 + q * 8 + g;
+            from[m][q] = nullptr;
+            if (r >= rows) continue;
+            if (STAGE == HIDDEN) from[m][q] = static_cast<const char*>(MX ? a.ordered : a.x) + ((size_t)a.notes->row[pair0 + r] * a.C + chunk * 8) * 2;
+            else from[m][q] = static_cast<const char*>(a.hidden) + ((size_t)(2 * (pair0 + r) + (two ? q : 0)) * a.H + chunk * 8) * 2;
         }
-    }
-    auto copy_panel = [&](int k, uint32_t to) {
-        const int r = tid / kChunks, c = tid % kChunks, place = MX ? (c & ~15) | (c >> 2 & 3) | (c & 3) << 2 : c;
+    uint4 brought[MT][2];
+    auto bring = [&](int k) {
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            const bool in = from[n] && k + c * 8 < k1;
-            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to + (uint32_t)((r + 8 * n) * kPanelStride + place * 16)),
-                         "l"(in ? from[n] + 2 * k : static_cast<const char*>(a.x)), "r"(in ? 16 : 0) : "memory");
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                brought[m][q] = make_uint4(0u, 0u, 0u, 0u);
+                if (from[m][q] && k + chunk * 8 < k1) brought[m][q] = *reinterpret_cast<const uint4*>(from[m][q] + 2 * k);
+            }
+    };
+    auto put = [&](uint32_t to) {
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+            const uint4 &u = brought[m][0], &v = brought[m][1];
+            const uint32_t at = to + (uint32_t)((m * (kPanel / 32) + warp) * 1024 + lane * 16);
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(u.x), "r"(v.x), "r"(u.y), "r"(v.y) : "memory");
+            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at + 512), "r"(u.z), "r"(v.z), "r"(u.w), "r"(v.w) : "memory");
         }
     };
-    auto rows_at = [&](uint32_t panel, int vectors, int n) {       // of 64 bytes before, in the panel
+    auto rows_at = [&](uint32_t panel, int block, int m, int half) {
         uint4 v;
         asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
-                     : "r"(panel + (uint32_t)(n * 8 * kPanelStride + vectors * 64)));
+                     : "r"(panel + (uint32_t)((m * (kPanel / 32) + block) * 1024 + half * 512)));
         return v;
     };
     const uint32_t ring = panels + 2 * kPanelBytes + tid * 16;
@@ -361,24 +370,31 @@ __device__ __forceinline__ void layer_rows(const LayerArgs& a, char* smem, int e
             if (MX) sc[q] += stride / 32;
         }
     };
-    uint32_t largest = 0;                                         // powers that the sums are relative to, of the lane's four rows
-    auto multiply = [&](uint32_t stage, uint32_t powers, uint32_t panel, int first) {     // first: element of the panel
+    uint32_t largest = 0;                                         // powers that the sums are relative to, of the lane's four rows of weights
+    // The sums' columns are rows 2t and 2t + 1 of a tile of weights: their factors are with the lanes that have these.
+    auto scale = [&](int i, float f) {
+        const float f0 = __shfl_sync(0xFFFFFFFFu, f, 8 * t), f1 = __shfl_sync(0xFFFFFFFFu, f, 8 * t + 4);
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+            acc[m][i][0] *= f0; acc[m][i][1] *= f1;
+            acc[m][i][2] *= f0; acc[m][i][3] *= f1;
+        }
+    };
+    auto multiply = [&](uint32_t stage, uint32_t powers, uint32_t panel, int first) {     // first: block of the panel
         uint4 v[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i)
             asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v[i].x), "=r"(v[i].y), "=r"(v[i].z), "=r"(v[i].w) : "r"(ring + (stage * 4 + i) * kRingRow));
         if (!MX) {
-            uint4 x[NT];
 #pragma unroll
-            for (int n = 0; n < NT; ++n) x[n] = rows_at(panel, first >> 5, n);
+            for (int half = 0; half < 2; ++half) {
 #pragma unroll
-            for (int n = 0; n < NT; ++n)
+                for (int m = 0; m < MT; ++m) {
+                    const uint4 x = rows_at(panel, first, m, half);
 #pragma unroll
-                for (int m = 0; m < 2; ++m) product<BF16>(acc[m][n], v[2 * m].x, v[2 * m + 1].x, v[2 * m].y, v[2 * m + 1].y, x[n].x, x[n].y);
-#pragma unroll
-            for (int n = 0; n < NT; ++n)
-#pragma unroll
-                for (int m = 0; m < 2; ++m) product<BF16>(acc[m][n], v[2 * m].z, v[2 * m + 1].z, v[2 * m].w, v[2 * m + 1].w, x[n].z, x[n].w);
+                    for (int i = 0; i < 4; ++i) product<BF16>(acc[m][i], x.x, x.y, x.z, x.w, half ? v[i].z : v[i].x, half ? v[i].w : v[i].y);
+                }
+            }
             return;
         }
         uint32_t top = __vmaxu4(powers, __shfl_xor_sync(0xFFFFFFFFu, powers, 1));
@@ -388,12 +404,7 @@ __device__ __forceinline__ void layer_rows(const LayerArgs& a, char* smem, int e
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int fall = (int)(top >> (8 * i) & 255u) - (int)(largest >> (8 * i) & 255u);
-                const float f = __uint_as_float((uint32_t)max(127 - fall, 0) << 23);
-#pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    acc[i >> 1][n][(i & 1) * 2] *= f;
-                    acc[i >> 1][n][(i & 1) * 2 + 1] *= f;
-                }
+                scale(i, __uint_as_float((uint32_t)max(127 - fall, 0) << 23));
             }
             largest = top;
         }
@@ -406,37 +417,36 @@ __device__ __forceinline__ void layer_rows(const LayerArgs& a, char* smem, int e
 #pragma unroll
             for (int i = 0; i < 4; ++i) decode8<BF16>(r[i], j == 0 ? v[i].x : j == 1 ? v[i].y : j == 2 ? v[i].z : v[i].w, factor[i]);
 #pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                const uint4 x = rows_at(panel, (first >> 5) + j, n);
+            for (int half = 0; half < 2; ++half) {
 #pragma unroll
-                for (int m = 0; m < 2; ++m) product<BF16>(acc[m][n], r[2 * m][0], r[2 * m + 1][0], r[2 * m][1], r[2 * m + 1][1], x.x, x.y);
+                for (int m = 0; m < MT; ++m) {
+                    const uint4 x = rows_at(panel, first + j, m, half);
 #pragma unroll
-                for (int m = 0; m < 2; ++m) product<BF16>(acc[m][n], r[2 * m][2], r[2 * m + 1][2], r[2 * m][3], r[2 * m + 1][3], x.z, x.w);
+                    for (int i = 0; i < 4; ++i) product<BF16>(acc[m][i], x.x, x.y, x.z, x.w, r[i][2 * half], r[i][2 * half + 1]);
+                }
             }
         }
     };
     uint32_t powers[4];
-    copy_panel(k0, panels);
+    bring(k0);
 #pragma unroll
     for (int s = 0; s < 3; ++s) {
         if (s < steps) request(s, powers[s]);
-        asm volatile("cp.async.commit_group;" ::: "memory");     // of step s, with the first panel in step 0's
+        asm volatile("cp.async.commit_group;" ::: "memory");
     }
-    // Step s, with the copies of step s + 3 in a group of their own.  A panel was asked for with those of three steps behind the start of the
-    // one before.
+    put(panels);
+    // Step s, with the copies of step s + 3 in a group of their own.
     auto turn = [&](int s, uint32_t stage, uint32_t p, uint32_t& later) {
-        const int panel = s >> panel_log, in_panel = s & ((1 << panel_log) - 1);
+        const int panel = s >> panel_log, in_panel = s & ((1 << panel_log) - 1), next = k0 + (panel + 1) * kPanel;
         if (in_panel == 0) {
-            if (panel_log >= 2 || s == 0) asm volatile("cp.async.wait_group 2;" ::: "memory");
-            else if (panel_log == 1) asm volatile("cp.async.wait_group 1;" ::: "memory");
-            else asm volatile("cp.async.wait_group 0;" ::: "memory");
             __syncthreads();                                      // the panel is there, and the other one is done with
-            if (k0 + (panel + 1) * kPanel < k1) copy_panel(k0 + (panel + 1) * kPanel, panels + ((panel & 1) ^ 1) * kPanelBytes);
+            if (next < k1) bring(next);
         }
         if (s + 3 < steps) request((stage + 3) & 3, later);
         asm volatile("cp.async.commit_group;" ::: "memory");
         asm volatile("cp.async.wait_group 3;" ::: "memory");
-        multiply(stage, p, panels + (panel & 1) * kPanelBytes + g * kPanelStride + t * 16, in_panel * stride + part * kPiece);
+        multiply(stage, p, panels + (panel & 1) * kPanelBytes + lane * 16, (in_panel * stride + part * kPiece) >> 5);
+        if (in_panel == (1 << panel_log) - 1 && next < k1) put(panels + ((panel & 1) ^ 1) * kPanelBytes);
     };
     for (int s = 0; s < steps; s += 4) {
         turn(s, 0, powers[0], powers[3]);
@@ -446,59 +456,59 @@ __device__ __forceinline__ void layer_rows(const LayerArgs& a, char* smem, int e
     }
     if (MX) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float f = mx_power(largest >> (8 * i) & 255u);
-#pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                acc[i >> 1][n][(i & 1) * 2] *= f;
-                acc[i >> 1][n][(i & 1) * 2 + 1] *= f;
-            }
-        }
+        for (int i = 0; i < 4; ++i) scale(i, mx_power(largest >> (8 * i) & 255u));
     }
-    asm volatile("cp.async.wait_group 0;" ::: "memory");         // an empty share has its panel of zeros under way
-    // The warps' sums in shared memory, [warp][2][column][17]; those that share a tile are added in their order.
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
+    // The warps' sums in shared memory, [warp][32 rows of weights][17] for every 16 rows; those that share a tile are added in their order.
     __syncthreads();
     float* sums = reinterpret_cast<float*>(smem);
+    const int held = two ? 8 : 16;                                // rows of every 16 that there are sums of
 #pragma unroll
-    for (int m = 0; m < 2; ++m)
+    for (int m = 0; m < MT; ++m)
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
+        for (int i = 0; i < 4; ++i)
 #pragma unroll
-            for (int c = 0; c < 4; ++c)
-                sums[((warp * 2 + m) * (8 * NT) + n * 8 + 2 * t + (c & 1)) * 17 + g + (c >> 1) * 8] = acc[m][n][c];
+            for (int c = 0; c < 2; ++c) {
+                float* to = sums + ((warp * MT + m) * 32 + i * 8 + 2 * t + c) * 17 + g;
+                if (two) {
+                    to[0] = acc[m][i][c] + acc[m][i][2 + c];
+                } else {
+                    to[0] = acc[m][i][c];
+                    to[8] = acc[m][i][2 + c];
+                }
+            }
     __syncthreads();
     const int width = STAGE == HIDDEN ? 16 : 32;
     for (int s = 0; s < per_cta; ++s)
-    for (int c = tid / width; c < rows; c += kLayerThreads / width) {
-        const int u = tid % width, at = (unit * per_cta + s) * width + u;
-        if (at >= M) continue;
-        auto sum = [&](int m, int column, int r) {
-            float v = 0.f;
-            for (int q = 0; q < split; ++q) v += sums[(((s * split + q) * 2 + m) * (8 * NT) + column) * 17 + r];
-            return v;
-        };
-        if (STAGE == HIDDEN) {
-            const float gate = sum(0, c, u), up = sum(1, c, u);
-            const float f = a.act == EMC2_ACT_SILU ? gate / (1.0f + expf(-gate)) : 0.5f * gate * erfcf(-0.70710678f * gate);
-            const float h = f * up;
-            const size_t to = (size_t)(2 * (pair0 + c)) * a.H + (MX ? (at & ~7) + ordered_place(at & 7) : at);
-            // What the first part leaves is exact; an infinite one leaves nothing.
-            if (BF16) {
-                __nv_bfloat16* p = static_cast<__nv_bfloat16*>(a.hidden) + to;
-                p[0] = __float2bfloat16_rn(h);
-                const float rest = h - __bfloat162float(p[0]);
-                p[a.H] = __float2bfloat16_rn(isinf(h) ? 0.f : rest);
+        for (int c = tid / width; c < rows; c += kLayerThreads / width) {
+            const int u = tid % width, at = (unit * per_cta + s) * width + u;
+            if (at >= M) continue;
+            auto sum = [&](int column) {
+                float v = 0.f;
+                for (int q = 0; q < split; ++q) v += sums[(((s * split + q) * MT + c / held) * 32 + column) * 17 + c % held];
+                return v;
+            };
+            if (STAGE == HIDDEN) {
+                const float gate = sum(u), up = sum(16 + u);
+                const float f = a.act == EMC2_ACT_SILU ? gate / (1.0f + expf(-gate)) : 0.5f * gate * erfcf(-0.70710678f * gate);
+                const float h = f * up;
+                const size_t to = (size_t)(2 * (pair0 + c)) * a.H + (MX ? (at & ~7) + ordered_place(at & 7) : at);
+                // What the first part leaves is exact; an infinite one leaves nothing.
+                if (BF16) {
+                    __nv_bfloat16* p = static_cast<__nv_bfloat16*>(a.hidden) + to;
+                    const __nv_bfloat16 first = __float2bfloat16_rn(h);
+                    p[0] = first;
+                    p[a.H] = __float2bfloat16_rn(isinf(__bfloat162float(first)) ? 0.f : h - __bfloat162float(first));
+                } else {
+                    __half* p = static_cast<__half*>(a.hidden) + to;
+                    const __half first = __float2half_rn(h);
+                    p[0] = first;
+                    p[a.H] = __float2half_rn(isinf(__half2float(first)) ? 0.f : h - __half2float(first));
+                }
             } else {
-                __half* p = static_cast<__half*>(a.hidden) + to;
-                p[0] = __float2half_rn(h);
-                const float rest = h - __half2float(p[0]);
-                p[a.H] = __float2half_rn(isinf(__half2float(p[0])) ? 0.f : rest);
+                a.part[((size_t)blockIdx.y * (a.n * a.k) + pair0 + c) * a.C + at] = sum(u);
             }
-        } else {
-            const float z = two ? sum(u >> 4, 2 * c, u & 15) + sum(u >> 4, 2 * c + 1, u & 15) : sum(u >> 4, c, u & 15);
-            a.part[((size_t)blockIdx.y * (a.n * a.k) + pair0 + c) * a.C + at] = z;
         }
-    }
     __syncthreads();
 }
 
@@ -508,10 +518,9 @@ __device__ __forceinline__ void layer_unit(const LayerArgs& a, char* smem) {
     const int i = blockIdx.x / a.tiles;
     for (int p = a.notes->start[i]; p < a.notes->start[i + 1]; p += kRowsAtOnce) {
         const bool two = STAGE == DOWN && a.notes->start[i + 1] - a.notes->start[i] <= kTwoParts;
-        const int e = a.notes->expert[i], rows = min(kRowsAtOnce, a.notes->start[i + 1] - p), columns = two ? 2 * rows : rows;
-        if (columns <= 8) layer_rows<STAGE, MX, BF16, 1>(a, smem, e, p, rows, two);
-        else if (columns <= 16) layer_rows<STAGE, MX, BF16, 2>(a, smem, e, p, rows, two);
-        else layer_rows<STAGE, MX, BF16, 4>(a, smem, e, p, rows, two);
+        const int e = a.notes->expert[i], rows = min(kRowsAtOnce, a.notes->start[i + 1] - p);
+        if ((two ? 2 * rows : rows) <= 16) layer_rows<STAGE, MX, BF16, 1>(a, smem, e, p, rows, two);
+        else layer_rows<STAGE, MX, BF16, 2>(a, smem, e, p, rows, two);
     }
 }
 
