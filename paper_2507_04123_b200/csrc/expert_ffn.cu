@@ -863,21 +863,6 @@ __global__ void __launch_bounds__(256) ffn_sum_kernel(WeightSumArgs a) {
 }
 
 // ---------------------------------------------------------------- host
-using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
-                                 const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-EncodeTiled encoder() {
-    static const EncodeTiled f = [] {
-        void* p = nullptr;
-        cudaDriverEntryPointQueryResult found;
-        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &found) != cudaSuccess ||
-            found != cudaDriverEntryPointSuccess)
-            p = nullptr;
-        return reinterpret_cast<EncodeTiled>(p);
-    }();
-    return f;
-}
-
 // [z, y, x] of 16-bit values, copied as boxes of x_box columns (64, 32 or 16, with the swizzle of that width) and y_box rows;
 // what lies outside reads as zeros.
 bool encode(CUtensorMap* map, const void* p, int type, uint64_t x, uint64_t y, uint64_t z, int x_box, int y_box) {

@@ -16,6 +16,7 @@
 #include <algorithm>
 
 #include "mx4.cuh"
+#include "umma.cuh"
 
 namespace emc2 {
 namespace {
@@ -113,7 +114,7 @@ __global__ void __launch_bounds__(kRouteThreads) layer_route_kernel(LayerArgs a)
         // Four experts at a time, so that their weights are under way together.
         for (int e0 = warp * 4; e0 < a.E; e0 += kRouteWarps * 4) {
             double sum[4] = {0.0, 0.0, 0.0, 0.0};
-#pragma unroll 2
+#pragma unroll 4
             for (int v = lane; v < a.C / 4; v += 32) {
                 float4 f[4];
 #pragma unroll
@@ -269,39 +270,60 @@ __device__ __forceinline__ uint32_t block_factor(int below) {
 
 enum Stage { HIDDEN = 0, DOWN };
 
+// Weights as [experts * rows][elements or bytes of codes], in boxes of 64 bytes of 16 rows (gate, up) or 32 (down); what lies behind a row
+// reads as zeros.
+struct LayerMaps {
+    CUtensorMap w[3];
+};
+
+// A CTA's place: share of the hidden units (the third kernel's), tile of its rows of weights, active expert, the last slowest.
+template <int STAGE>
+__device__ __forceinline__ int share_of(const LayerArgs& a) { return STAGE == DOWN ? blockIdx.x % a.shares : 0; }
+template <int STAGE>
+__device__ __forceinline__ int unit_of(const LayerArgs& a) { return (STAGE == DOWN ? blockIdx.x / a.shares : blockIdx.x) % a.tiles; }
+template <int STAGE>
+__device__ __forceinline__ int active_of(const LayerArgs& a) { return (STAGE == DOWN ? blockIdx.x / a.shares : blockIdx.x) / a.tiles; }
+
 // Panels of the rows at hand, in two buffers, as the 16-byte registers of a product's lanes: [16 rows][8 blocks of 32 elements][2 halves]
 // [32 lanes].  A lane's vector has two words of row g and, between them, those of row g + 8.
 constexpr int kPanelBytes = kRowsAtOnce / 16 * kPanel / 32 * 2 * 512;
-constexpr uint32_t kRingRow = kLayerThreads * 16;
-constexpr size_t kProductShared = 2 * kPanelBytes + 4 * 4 * kRingRow;
-static_assert(kLayerWarps * 2 * kRowsAtOnce * 17 * 4 <= kProductShared, "sums");
+// The warps' sums take the panels' place when the products are done: [warp][16 rows][32 rows of weights][16], the last index mixed with the
+// one before, so that writers and readers meet few of the same banks.
+static_assert(kLayerWarps * kRowsAtOnce * 32 * 4 <= 2 * kPanelBytes, "sums");
+// Behind them the ring: [stage][warp][32 rows][64 bytes].
+constexpr uint32_t kWarpStage = 32 * 64, kStage = kLayerWarps * kWarpStage;
+constexpr int kStages = 4;
+constexpr size_t kProductShared = 2 * kPanelBytes + kStages * kStage;
+
+// A warp's barriers, one per stage, and the parities that it waits for next.
+struct Ring {
+    uint32_t bars, phases;
+    volatile int* gave_up;
+};
 
 // What a warp's rows of weights are: four tiles of eight, of the gate's and the up projection's rows or of the down projection's.  Lane (g, t)
 // has row g of each.  Which element stands at which place of a product does not matter, if weights and rows agree.
 //   16 bits: a block of 32 elements to a step, of which the lane has 8t .. 8t + 7.
 //    4 bits: four blocks to a step, of which the lane has the t-th.  A block's elements are taken relative to the largest power that the row
 //            has had so far, which the sums are relative to; when it rises, they are scaled down.
-// The weights of the next three steps are on their way to shared memory, in places that the lane alone reads: registers have no room for as
-// much as the memory needs to be asked for at once (50 KB per SM and more).
+// The weights of the next three steps are on their way to shared memory, in boxes that the warp alone reads: registers have no room for as
+// much as the memory needs to be asked for at once (50 KB per SM and more), and copies of 16 bytes a lane came to 5.3 TB/s where boxes TODO.
 template <int STAGE, bool MX, bool BF16, int MT>
-__device__ __forceinline__ void layer_rows(const LayerArgs& a, char* smem, int e, int pair0, int rows, bool two) {
+__device__ __forceinline__ void layer_rows(const LayerArgs& a, const LayerMaps& maps, char* smem, Ring& wait, int e, int pair0, int rows, bool two) {
     constexpr int kPiece = MX ? 128 : 32;                         // elements of a step
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
     const int split = 1 << a.split_log, per_cta = kLayerWarps >> a.split_log, part = warp & (split - 1), slot = warp >> a.split_log;
     const int K = STAGE == HIDDEN ? a.C : a.H, M = STAGE == HIDDEN ? a.H : a.C;
-    const int unit = blockIdx.x % a.tiles, tile = unit * per_cta + slot;        // of 16 hidden units, or of 32 channels
+    const int unit = unit_of<STAGE>(a), tile = unit * per_cta + slot;        // of 16 hidden units, or of 32 channels
     // The third kernel's share of the hidden units, whole steps of the products; the last ones ragged.
-    const int each = STAGE == HIDDEN ? K : ((K + a.shares - 1) / a.shares + 127) / 128 * 128;
-    const int k0 = STAGE == HIDDEN ? 0 : min(K, (int)blockIdx.y * each), k1 = min(K, k0 + each);
-    // The lane's next vector of its first row of weights (of the up projection's too) and of the powers; the others are a constant number of
-    // rows behind.  Rows behind the last are read as the last, and come to nothing.
-    const int blocks = (K + kMxBlock - 1) / kMxBlock, units = MX ? blocks : K / 8, r0 = tile * (STAGE == HIDDEN ? 16 : 32) + g;
-    const size_t start = (size_t)(e * M) * units + k0 / (MX ? 32 : 8) + part * 4 + t;         // of the expert's row 0, in units of 16 bytes
-    uint32_t row_at[STAGE == HIDDEN ? 2 : 4];
+    const int each = STAGE == HIDDEN ? K : ((K + a.shares - 1) / a.shares + 255) / 256 * 256;
+    const int k0 = STAGE == HIDDEN ? 0 : min(K, share_of<STAGE>(a) * each), k1 = min(K, k0 + each);
+    // 4 bits: where the lane finds its block's powers, of its rows of weights.  Rows behind the last are read as the last, and come to nothing.
+    constexpr int kRows = STAGE == HIDDEN ? 2 : 4;
+    const int blocks = (K + kMxBlock - 1) / kMxBlock, r0 = tile * (STAGE == HIDDEN ? 16 : 32);
+    uint32_t at[kRows];
 #pragma unroll
-    for (int i = 0; i < (STAGE == HIDDEN ? 2 : 4); ++i) row_at[i] = (uint32_t)min(r0 + 8 * i, M - 1) * (uint32_t)units;
-    const uint4* w[2] = {static_cast<const uint4*>(a.w[STAGE == HIDDEN ? 0 : 2]) + start, static_cast<const uint4*>(a.w[1]) + (STAGE == HIDDEN ? start : 0)};
-    const uint8_t* sc[2] = {MX ? a.scales[STAGE == HIDDEN ? 0 : 2] + start : nullptr, MX && STAGE == HIDDEN ? a.scales[1] + start : nullptr};
+    for (int i = 0; i < kRows; ++i) at[i] = (uint32_t)(e * M + min(r0 + g + 8 * i, M - 1)) * (uint32_t)blocks + (uint32_t)(k0 / kMxBlock + part * 4 + t);
     float acc[MT][4][4];                                          // [16 rows][tile]
 #pragma unroll
     for (int m = 0; m < MT; ++m)
@@ -350,25 +372,27 @@ __device__ __forceinline__ void layer_rows(const LayerArgs& a, char* smem, int e
                      : "r"(panel + (uint32_t)((m * (kPanel / 32) + block) * 1024 + half * 512)));
         return v;
     };
-    const uint32_t ring = panels + 2 * kPanelBytes + tid * 16;
+    const uint32_t ring = panels + 2 * kPanelBytes + warp * kWarpStage, mine = ring + g * 64 + t * 16;
     const int stride = kPiece << a.split_log, steps = (k1 - k0 + stride - 1) / stride, panel_log = (MX ? 1 : 3) - a.split_log;       // steps of a panel
-    int left = k1 - (k0 + part * kPiece + (MX ? 32 : 8) * t);     // elements from the lane's next vector on
-    auto request = [&](uint32_t stage, uint32_t& powers) {        // powers: of the lane's block, a byte for each of the four rows
-        const bool in = left > 0;
+    const uint32_t lead = elected();
+    auto request = [&](int s, uint32_t& powers) {                 // powers: of the lane's block, a byte for each of the four rows
+        const int k = k0 + s * stride + part * kPiece;
+        const uint32_t stage = s & (kStages - 1), to = ring + stage * kStage, bar = wait.bars + stage * 8;
+        bar_expect(lead, bar, kWarpStage);
+        if (STAGE == HIDDEN) {
+            copy_tile(lead, to, &maps.w[0], MX ? k / 2 : k, e * M + r0, bar);
+            copy_tile(lead, to + kWarpStage / 2, &maps.w[1], MX ? k / 2 : k, e * M + r0, bar);
+        } else {
+            copy_tile(lead, to, &maps.w[2], MX ? k / 2 : k, e * M + r0, bar);
+        }
+        if (!MX) return;
         powers = 0;
+        if (k + 32 * t < k1) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int q = STAGE == HIDDEN ? i >> 1 : 0, r = STAGE == HIDDEN ? i & 1 : i;
-            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(ring + (stage * 4 + i) * kRingRow),
-                         "l"(in ? w[q] + row_at[r] : static_cast<const uint4*>(a.x)), "r"(in ? 16 : 0) : "memory");
-            if (MX && in) powers |= (uint32_t)__ldg(sc[q] + row_at[r]) << (8 * i);
+            for (int i = 0; i < 4; ++i) powers |= (uint32_t)__ldg(a.scales[STAGE == HIDDEN ? i >> 1 : 2] + at[i % kRows]) << (8 * i);
         }
-        left -= stride;
 #pragma unroll
-        for (int q = 0; q < (STAGE == HIDDEN ? 2 : 1); ++q) {
-            w[q] += stride / (MX ? 32 : 8);
-            if (MX) sc[q] += stride / 32;
-        }
+        for (int i = 0; i < kRows; ++i) at[i] += stride / kMxBlock;
     };
     uint32_t largest = 0;                                         // powers that the sums are relative to, of the lane's four rows of weights
     // The sums' columns are rows 2t and 2t + 1 of a tile of weights: their factors are with the lanes that have these.
@@ -380,11 +404,11 @@ __device__ __forceinline__ void layer_rows(const LayerArgs& a, char* smem, int e
             acc[m][i][2] *= f0; acc[m][i][3] *= f1;
         }
     };
-    auto multiply = [&](uint32_t stage, uint32_t powers, uint32_t panel, int first) {     // first: block of the panel
+    auto multiply = [&](uint32_t stage, uint32_t power_of_block, uint32_t panel, int first) {     // first: block of the panel
         uint4 v[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v[i].x), "=r"(v[i].y), "=r"(v[i].z), "=r"(v[i].w) : "r"(ring + (stage * 4 + i) * kRingRow));
+            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v[i].x), "=r"(v[i].y), "=r"(v[i].z), "=r"(v[i].w) : "r"(mine + stage + i * 512));
         if (!MX) {
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
@@ -397,10 +421,11 @@ __device__ __forceinline__ void layer_rows(const LayerArgs& a, char* smem, int e
             }
             return;
         }
-        uint32_t top = __vmaxu4(powers, __shfl_xor_sync(0xFFFFFFFFu, powers, 1));
+        uint32_t top = __vmaxu4(power_of_block, __shfl_xor_sync(0xFFFFFFFFu, power_of_block, 1));
         top = __vmaxu4(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
-        top = __vmaxu4(top, largest);
-        if (__any_sync(0xFFFFFFFFu, top != largest)) {
+        if (__any_sync(0xFFFFFFFFu, __vmaxu4(top, largest) != largest)) {
+            // With two powers to spare, so that the next rise is seldom.
+            top = __vmaxu4(__vmaxu4(__vminu4(__vaddus4(top, 0x02020202u), 0xFEFEFEFEu), top), largest);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int fall = (int)(top >> (8 * i) & 255u) - (int)(largest >> (8 * i) & 255u);
@@ -409,8 +434,9 @@ __device__ __forceinline__ void layer_rows(const LayerArgs& a, char* smem, int e
             largest = top;
         }
         uint32_t factor[4];
+        const uint32_t below = largest - power_of_block;          // byte by byte: none is larger
 #pragma unroll
-        for (int i = 0; i < 4; ++i) factor[i] = block_factor<BF16>((int)(top >> (8 * i) & 255u) - (int)(powers >> (8 * i) & 255u));
+        for (int i = 0; i < 4; ++i) factor[i] = block_factor<BF16>((int)(below >> (8 * i) & 255u));
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             uint32_t r[4][4];
@@ -427,54 +453,53 @@ __device__ __forceinline__ void layer_rows(const LayerArgs& a, char* smem, int e
             }
         }
     };
-    uint32_t powers[4];
-    bring(k0);
+    uint32_t powers[3];
+    __syncwarp();                                                 // of the pass before, the warp has read all
 #pragma unroll
-    for (int s = 0; s < 3; ++s) {
+    for (int s = 0; s < 3; ++s)
         if (s < steps) request(s, powers[s]);
-        asm volatile("cp.async.commit_group;" ::: "memory");
-    }
+    bring(k0);
     put(panels);
-    // Step s, with the copies of step s + 3 in a group of their own.
-    auto turn = [&](int s, uint32_t stage, uint32_t p, uint32_t& later) {
+    // Not unrolled: the products of several steps do not fit the instruction cache (4 bits, the second kernel: 102 and 95 us).
+#pragma unroll 1
+    for (int s = 0; s < steps; ++s) {
         const int panel = s >> panel_log, in_panel = s & ((1 << panel_log) - 1), next = k0 + (panel + 1) * kPanel;
         if (in_panel == 0) {
             __syncthreads();                                      // the panel is there, and the other one is done with
             if (next < k1) bring(next);
         }
-        if (s + 3 < steps) request((stage + 3) & 3, later);
-        asm volatile("cp.async.commit_group;" ::: "memory");
-        asm volatile("cp.async.wait_group 3;" ::: "memory");
-        multiply(stage, p, panels + (panel & 1) * kPanelBytes + lane * 16, (in_panel * stride + part * kPiece) >> 5);
+        uint32_t later = 0;
+        if (s + 3 < steps) request(s + 3, later);
+        const uint32_t stage = s & (kStages - 1);
+        warp_wait(wait.bars + stage * 8, wait.phases >> stage & 1u, wait.gave_up, a.status);
+        wait.phases ^= 1u << stage;
+        multiply(stage * kStage, powers[0], panels + (panel & 1) * kPanelBytes + lane * 16, (in_panel * stride + part * kPiece) >> 5);
+        __syncwarp();                                             // the stage is done with
+        powers[0] = powers[1];
+        powers[1] = powers[2];
+        powers[2] = later;
         if (in_panel == (1 << panel_log) - 1 && next < k1) put(panels + ((panel & 1) ^ 1) * kPanelBytes);
-    };
-    for (int s = 0; s < steps; s += 4) {
-        turn(s, 0, powers[0], powers[3]);
-        if (s + 1 < steps) turn(s + 1, 1, powers[1], powers[0]);
-        if (s + 2 < steps) turn(s + 2, 2, powers[2], powers[1]);
-        if (s + 3 < steps) turn(s + 3, 3, powers[3], powers[2]);
     }
     if (MX) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) scale(i, mx_power(largest >> (8 * i) & 255u));
     }
-    asm volatile("cp.async.wait_group 0;" ::: "memory");
-    // The warps' sums in shared memory, [warp][32 rows of weights][17] for every 16 rows; those that share a tile are added in their order.
-    __syncthreads();
+    __syncthreads();                                              // the panels are done with; the warps that share a tile are added in their order
     float* sums = reinterpret_cast<float*>(smem);
     const int held = two ? 8 : 16;                                // rows of every 16 that there are sums of
+    auto sum_at = [&](int w, int m, int column, int r) { return ((w * MT + m) * 32 + column) * 16 + (r ^ (column >> 1)); };
 #pragma unroll
     for (int m = 0; m < MT; ++m)
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
-                float* to = sums + ((warp * MT + m) * 32 + i * 8 + 2 * t + c) * 17 + g;
+                const int column = i * 8 + 2 * t + c;
                 if (two) {
-                    to[0] = acc[m][i][c] + acc[m][i][2 + c];
+                    sums[sum_at(warp, m, column, g)] = acc[m][i][c] + acc[m][i][2 + c];
                 } else {
-                    to[0] = acc[m][i][c];
-                    to[8] = acc[m][i][2 + c];
+                    sums[sum_at(warp, m, column, g)] = acc[m][i][c];
+                    sums[sum_at(warp, m, column, g + 8)] = acc[m][i][2 + c];
                 }
             }
     __syncthreads();
@@ -485,7 +510,7 @@ __device__ __forceinline__ void layer_rows(const LayerArgs& a, char* smem, int e
             if (at >= M) continue;
             auto sum = [&](int column) {
                 float v = 0.f;
-                for (int q = 0; q < split; ++q) v += sums[(((s * split + q) * MT + c / held) * 32 + column) * 17 + c % held];
+                for (int q = 0; q < split; ++q) v += sums[sum_at(s * split + q, c / held, column, c % held)];
                 return v;
             };
             if (STAGE == HIDDEN) {
@@ -506,7 +531,7 @@ __device__ __forceinline__ void layer_rows(const LayerArgs& a, char* smem, int e
                     p[a.H] = __float2half_rn(isinf(__half2float(first)) ? 0.f : h - __half2float(first));
                 }
             } else {
-                a.part[((size_t)blockIdx.y * (a.n * a.k) + pair0 + c) * a.C + at] = sum(u);
+                a.part[((size_t)share_of<STAGE>(a) * (a.n * a.k) + pair0 + c) * a.C + at] = sum(u);
             }
         }
     __syncthreads();
@@ -514,14 +539,24 @@ __device__ __forceinline__ void layer_rows(const LayerArgs& a, char* smem, int e
 
 // The rows of the CTA's expert, 32 at a time, against its weights.
 template <int STAGE, bool MX, bool BF16>
-__device__ __forceinline__ void layer_unit(const LayerArgs& a, char* smem) {
-    const int i = blockIdx.x / a.tiles;
+__device__ __forceinline__ void layer_unit(const LayerArgs& a, const LayerMaps& maps, char* smem) {
+    __shared__ __align__(8) unsigned long long bars[kLayerWarps][kStages];
+    __shared__ int gave_up;
+    if (threadIdx.x == 0) gave_up = 0;
+    Ring ring = {smem_u32(bars[threadIdx.x >> 5]), 0u, &gave_up};
+    if ((threadIdx.x & 31) == 0)
+        for (int s = 0; s < kStages; ++s) bar_init(ring.bars + s * 8, 1);
+    fence_bar_init();
+    fence_async_shared();
+    __syncthreads();
+    const int i = active_of<STAGE>(a);
     for (int p = a.notes->start[i]; p < a.notes->start[i + 1]; p += kRowsAtOnce) {
         const bool two = STAGE == DOWN && a.notes->start[i + 1] - a.notes->start[i] <= kTwoParts;
         const int e = a.notes->expert[i], rows = min(kRowsAtOnce, a.notes->start[i + 1] - p);
-        if ((two ? 2 * rows : rows) <= 16) layer_rows<STAGE, MX, BF16, 1>(a, smem, e, p, rows, two);
-        else layer_rows<STAGE, MX, BF16, 2>(a, smem, e, p, rows, two);
+        if ((two ? 2 * rows : rows) <= 16) layer_rows<STAGE, MX, BF16, 1>(a, maps, smem, ring, e, p, rows, two);
+        else layer_rows<STAGE, MX, BF16, 2>(a, maps, smem, ring, e, p, rows, two);
     }
+    leave_after_timeout(&gave_up);
 }
 
 // y of four channels of a row: its choices in their order, of each the shares in theirs.
@@ -544,25 +579,25 @@ __device__ __forceinline__ void layer_sum(const LayerArgs& a, int row, int c) {
 }
 
 template <bool MX, bool BF16>
-__global__ void __launch_bounds__(kLayerThreads, 2) layer_hidden_kernel(LayerArgs a) {
+__global__ void __launch_bounds__(kLayerThreads, 2) layer_hidden_kernel(LayerArgs a, const __grid_constant__ LayerMaps maps) {
     await_predecessor();
-    extern __shared__ __align__(16) char panels[];
-    if ((int)blockIdx.x < a.notes->active * a.tiles) layer_unit<HIDDEN, MX, BF16>(a, panels);
+    extern __shared__ __align__(128) char panels[];
+    if ((int)blockIdx.x < a.notes->active * a.tiles) layer_unit<HIDDEN, MX, BF16>(a, maps, panels);
     release_successor();
 }
 
 template <bool MX, bool BF16>
-__global__ void __launch_bounds__(kLayerThreads, 2) layer_down_kernel(LayerArgs a) {
+__global__ void __launch_bounds__(kLayerThreads, 2) layer_down_kernel(LayerArgs a, const __grid_constant__ LayerMaps maps) {
     await_predecessor();
-    extern __shared__ __align__(16) char panels[];
+    extern __shared__ __align__(128) char panels[];
     __shared__ int last;
-    if ((int)blockIdx.x >= a.notes->active * a.tiles) return;
-    layer_unit<DOWN, MX, BF16>(a, panels);
+    if ((int)blockIdx.x >= a.notes->active * a.tiles * a.shares) return;
+    layer_unit<DOWN, MX, BF16>(a, maps, panels);
     if (!a.last_adds) {
         release_successor();
         return;
     }
-    const int unit = blockIdx.x % a.tiles, tid = threadIdx.x;
+    const int unit = unit_of<DOWN>(a), tid = threadIdx.x;
     __syncthreads();
     if (tid == 0) {
         __threadfence();
@@ -594,6 +629,18 @@ cudaError_t launch_layer(emc2_bridge* h, LayerArgs a, cudaStream_t st) {
     cudaError_t e = allow_shared(layer_hidden_kernel<MX, BF16>, most);
     if (e == cudaSuccess) e = allow_shared(layer_down_kernel<MX, BF16>, most);
     if (e != cudaSuccess) return e;
+    LayerMaps maps;
+    for (int i = 0; i < 3; ++i) {
+        const int K = i < 2 ? a.C : a.H, M = i < 2 ? a.H : a.C;
+        const cuuint64_t row = MX ? (cuuint64_t)mx4_blocks(K) * 16 : (cuuint64_t)K * 2;
+        const cuuint64_t dims[2] = {MX ? row : (cuuint64_t)K, (cuuint64_t)a.E * M}, strides[1] = {row};
+        const cuuint32_t box[2] = {MX ? 64u : 32u, i < 2 ? 16u : 32u}, step[2] = {1, 1};
+        const EncodeTiled f = encoder();
+        if (!f || f(&maps.w[i], MX ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2,
+                    const_cast<void*>(a.w[i]), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE,
+                    CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+            return cudaErrorInvalidValue;
+    }
     const int experts = std::min(a.E, a.n * a.k);
     const int step = MX ? 128 : 32;
     // Warps that share a tile: as many as fill the SMs, and as have steps.
@@ -612,7 +659,7 @@ cudaError_t launch_layer(emc2_bridge* h, LayerArgs a, cudaStream_t st) {
     {
         LaunchScope ls(h, K_LAYER_HIDDEN, st);
         plan(a.C, a.H, 16);
-        launch_chained(layer_hidden_kernel<MX, BF16>, dim3((unsigned)(a.tiles * experts)), kLayerThreads, most, st, a);
+        launch_chained(layer_hidden_kernel<MX, BF16>, dim3((unsigned)(a.tiles * experts)), kLayerThreads, most, st, a, maps);
     }
     {
         LaunchScope ls(h, K_LAYER_DOWN, st);
@@ -622,7 +669,7 @@ cudaError_t launch_layer(emc2_bridge* h, LayerArgs a, cudaStream_t st) {
                2 * a.shares * a.n * a.k <= kPartRows)
             a.shares *= 2;
         a.last_adds = a.n * a.k * a.shares <= kLastAdds;
-        launch_chained(layer_down_kernel<MX, BF16>, dim3((unsigned)(a.tiles * experts), (unsigned)a.shares), kLayerThreads, most, st, a);
+        launch_chained(layer_down_kernel<MX, BF16>, dim3((unsigned)(a.tiles * experts * a.shares)), kLayerThreads, most, st, a, maps);
     }
     if (!a.last_adds) {
         LaunchScope ls(h, K_LAYER_SUM, st);
