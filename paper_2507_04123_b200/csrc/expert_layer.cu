@@ -270,8 +270,8 @@ __device__ __forceinline__ uint32_t block_factor(int below) {
 
 enum Stage { HIDDEN = 0, DOWN };
 
-// Weights as [experts * rows][elements or bytes of codes], in boxes of 64 bytes of 16 rows (gate, up) or 32 (down); what lies behind a row
-// reads as zeros.
+// Weights as [experts * rows][elements or bytes of codes], in boxes of 128 bytes of 16 rows (gate, up) or 32 (down), whose vectors are
+// mixed with the row's number (the copies' swizzle); what lies behind a row reads as zeros.
 struct LayerMaps {
     CUtensorMap w[3];
 };
@@ -290,10 +290,9 @@ constexpr int kPanelBytes = kRowsAtOnce / 16 * kPanel / 32 * 2 * 512;
 // The warps' sums take the panels' place when the products are done: [warp][16 rows][32 rows of weights][16], the last index mixed with the
 // one before, so that writers and readers meet few of the same banks.
 static_assert(kLayerWarps * kRowsAtOnce * 32 * 4 <= 2 * kPanelBytes, "sums");
-// Behind them the ring: [stage][warp][32 rows][64 bytes].
-constexpr uint32_t kWarpStage = 32 * 64, kStage = kLayerWarps * kWarpStage;
-constexpr int kStages = 4;
-constexpr size_t kProductShared = 2 * kPanelBytes + kStages * kStage;
+// Behind them the ring: [stage][warp][32 rows][128 bytes], on 1,024 bytes.
+constexpr uint32_t kWarpStage = 32 * 128, kStage = kLayerWarps * kWarpStage;
+constexpr size_t kProductShared = 1024 + 2 * kPanelBytes + 2 * kStage;
 
 // A warp's barriers, one per stage, and the parities that it waits for next.
 struct Ring {
@@ -302,15 +301,16 @@ struct Ring {
 };
 
 // What a warp's rows of weights are: four tiles of eight, of the gate's and the up projection's rows or of the down projection's.  Lane (g, t)
-// has row g of each.  Which element stands at which place of a product does not matter, if weights and rows agree.
-//   16 bits: a block of 32 elements to a step, of which the lane has 8t .. 8t + 7.
-//    4 bits: four blocks to a step, of which the lane has the t-th.  A block's elements are taken relative to the largest power that the row
-//            has had so far, which the sums are relative to; when it rises, they are scaled down.
-// The weights of the next three steps are on their way to shared memory, in boxes that the warp alone reads: registers have no room for as
-// much as the memory needs to be asked for at once (50 KB per SM and more), and copies of 16 bytes a lane came to 5.3 TB/s where boxes TODO.
+// has row g / 2 + 4 (g % 2) of each, so that the eight vectors that lanes read together lie on different banks.  Which element stands at which
+// place of a product does not matter, if weights and rows agree.
+//   16 bits: two blocks of 32 elements to a step, of each of which the lane has 8t .. 8t + 7.
+//    4 bits: eight blocks to a step, of which the lane has the t-th of either half.  A block's elements are taken relative to the largest power
+//            that the row has had so far, which the sums are relative to; when it rises, they are scaled down.
+// The weights of the next step are on their way to shared memory, in boxes that the warp alone reads: registers have no room for as much as the
+// memory needs to be asked for at once (50 KB per SM and more).
 template <int STAGE, bool MX, bool BF16, int MT>
 __device__ __forceinline__ void layer_rows(const LayerArgs& a, const LayerMaps& maps, char* smem, Ring& wait, int e, int pair0, int rows, bool two) {
-    constexpr int kPiece = MX ? 128 : 32;                         // elements of a step
+    constexpr int kPiece = MX ? 256 : 64;                         // elements of a step
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
     const int split = 1 << a.split_log, per_cta = kLayerWarps >> a.split_log, part = warp & (split - 1), slot = warp >> a.split_log;
     const int K = STAGE == HIDDEN ? a.C : a.H, M = STAGE == HIDDEN ? a.H : a.C;
@@ -321,9 +321,10 @@ __device__ __forceinline__ void layer_rows(const LayerArgs& a, const LayerMaps& 
     // 4 bits: where the lane finds its block's powers, of its rows of weights.  Rows behind the last are read as the last, and come to nothing.
     constexpr int kRows = STAGE == HIDDEN ? 2 : 4;
     const int blocks = (K + kMxBlock - 1) / kMxBlock, r0 = tile * (STAGE == HIDDEN ? 16 : 32);
+    const int row = g >> 1 | (g & 1) << 2;
     uint32_t at[kRows];
 #pragma unroll
-    for (int i = 0; i < kRows; ++i) at[i] = (uint32_t)(e * M + min(r0 + g + 8 * i, M - 1)) * (uint32_t)blocks + (uint32_t)(k0 / kMxBlock + part * 4 + t);
+    for (int i = 0; i < kRows; ++i) at[i] = (uint32_t)(e * M + min(r0 + row + 8 * i, M - 1)) * (uint32_t)blocks + (uint32_t)(k0 / kMxBlock + part * 8 + t);
     float acc[MT][4][4];                                          // [16 rows][tile]
 #pragma unroll
     for (int m = 0; m < MT; ++m)
@@ -372,12 +373,13 @@ __device__ __forceinline__ void layer_rows(const LayerArgs& a, const LayerMaps& 
                      : "r"(panel + (uint32_t)((m * (kPanel / 32) + block) * 1024 + half * 512)));
         return v;
     };
-    const uint32_t ring = panels + 2 * kPanelBytes + warp * kWarpStage, mine = ring + g * 64 + t * 16;
-    const int stride = kPiece << a.split_log, steps = (k1 - k0 + stride - 1) / stride, panel_log = (MX ? 1 : 3) - a.split_log;       // steps of a panel
+    const uint32_t ring = panels + 2 * kPanelBytes + warp * kWarpStage;
+    const uint32_t mine[2] = {ring + row * 128 + ((t ^ row) << 4), ring + row * 128 + (((t + 4) ^ row) << 4)};
+    const int stride = kPiece << a.split_log, steps = (k1 - k0 + stride - 1) / stride, panel_log = (MX ? 0 : 2) - a.split_log;       // steps of a panel
     const uint32_t lead = elected();
-    auto request = [&](int s, uint32_t& powers) {                 // powers: of the lane's block, a byte for each of the four rows
+    auto request = [&](int s, uint32_t (&powers)[2]) {            // powers: of the lane's blocks, a byte for each of the four rows
         const int k = k0 + s * stride + part * kPiece;
-        const uint32_t stage = s & (kStages - 1), to = ring + stage * kStage, bar = wait.bars + stage * 8;
+        const uint32_t to = ring + (s & 1) * kStage, bar = wait.bars + (s & 1) * 8;
         bar_expect(lead, bar, kWarpStage);
         if (STAGE == HIDDEN) {
             copy_tile(lead, to, &maps.w[0], MX ? k / 2 : k, e * M + r0, bar);
@@ -386,16 +388,18 @@ __device__ __forceinline__ void layer_rows(const LayerArgs& a, const LayerMaps& 
             copy_tile(lead, to, &maps.w[2], MX ? k / 2 : k, e * M + r0, bar);
         }
         if (!MX) return;
-        powers = 0;
-        if (k + 32 * t < k1) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) powers |= (uint32_t)__ldg(a.scales[STAGE == HIDDEN ? i >> 1 : 2] + at[i % kRows]) << (8 * i);
+        for (int u = 0; u < 2; ++u) {
+            powers[u] = 0;
+            if (k + (4 * u + t) * kMxBlock >= k1) continue;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) powers[u] |= (uint32_t)__ldg(a.scales[STAGE == HIDDEN ? i >> 1 : 2] + (at[i % kRows] + 4 * u)) << (8 * i);
         }
 #pragma unroll
         for (int i = 0; i < kRows; ++i) at[i] += stride / kMxBlock;
     };
     uint32_t largest = 0;                                         // powers that the sums are relative to, of the lane's four rows of weights
-    // The sums' columns are rows 2t and 2t + 1 of a tile of weights: their factors are with the lanes that have these.
+    // The sums' columns 2t and 2t + 1 of a tile are those of the lanes with these g, which have their factors.
     auto scale = [&](int i, float f) {
         const float f0 = __shfl_sync(0xFFFFFFFFu, f, 8 * t), f1 = __shfl_sync(0xFFFFFFFFu, f, 8 * t + 4);
 #pragma unroll
@@ -404,11 +408,11 @@ __device__ __forceinline__ void layer_rows(const LayerArgs& a, const LayerMaps& 
             acc[m][i][2] *= f0; acc[m][i][3] *= f1;
         }
     };
-    auto multiply = [&](uint32_t stage, uint32_t power_of_block, uint32_t panel, int first) {     // first: block of the panel
+    auto multiply = [&](uint32_t stage, int u, uint32_t power_of_block, uint32_t panel, int first) {      // u: half of the step; first: block of the panel
         uint4 v[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v[i].x), "=r"(v[i].y), "=r"(v[i].z), "=r"(v[i].w) : "r"(mine + stage + i * 512));
+            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v[i].x), "=r"(v[i].y), "=r"(v[i].z), "=r"(v[i].w) : "r"(mine[u] + stage + i * 1024));
         if (!MX) {
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
@@ -453,14 +457,14 @@ __device__ __forceinline__ void layer_rows(const LayerArgs& a, const LayerMaps& 
             }
         }
     };
-    uint32_t powers[3];
+    uint32_t powers[2][2];
     __syncwarp();                                                 // of the pass before, the warp has read all
 #pragma unroll
-    for (int s = 0; s < 3; ++s)
+    for (int s = 0; s < 2; ++s)
         if (s < steps) request(s, powers[s]);
     bring(k0);
     put(panels);
-    // Not unrolled: the products of several steps do not fit the instruction cache (4 bits, the second kernel: 102 and 95 us).
+    // Not unrolled: the products of several steps do not fit the instruction cache.
 #pragma unroll 1
     for (int s = 0; s < steps; ++s) {
         const int panel = s >> panel_log, in_panel = s & ((1 << panel_log) - 1), next = k0 + (panel + 1) * kPanel;
@@ -468,16 +472,16 @@ __device__ __forceinline__ void layer_rows(const LayerArgs& a, const LayerMaps& 
             __syncthreads();                                      // the panel is there, and the other one is done with
             if (next < k1) bring(next);
         }
-        uint32_t later = 0;
-        if (s + 3 < steps) request(s + 3, later);
-        const uint32_t stage = s & (kStages - 1);
+        const uint32_t stage = s & 1;
         warp_wait(wait.bars + stage * 8, wait.phases >> stage & 1u, wait.gave_up, a.status);
         wait.phases ^= 1u << stage;
-        multiply(stage * kStage, powers[0], panels + (panel & 1) * kPanelBytes + lane * 16, (in_panel * stride + part * kPiece) >> 5);
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+            multiply(stage * kStage, u, powers[0][u], panels + (panel & 1) * kPanelBytes + lane * 16, ((in_panel * stride + part * kPiece) >> 5) + (MX ? 4 : 1) * u);
         __syncwarp();                                             // the stage is done with
-        powers[0] = powers[1];
-        powers[1] = powers[2];
-        powers[2] = later;
+        powers[0][0] = powers[1][0];
+        powers[0][1] = powers[1][1];
+        if (s + 2 < steps) request(s + 2, powers[1]);
         if (in_panel == (1 << panel_log) - 1 && next < k1) put(panels + ((panel & 1) ^ 1) * kPanelBytes);
     }
     if (MX) {
@@ -494,7 +498,7 @@ __device__ __forceinline__ void layer_rows(const LayerArgs& a, const LayerMaps& 
         for (int i = 0; i < 4; ++i)
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
-                const int column = i * 8 + 2 * t + c;
+                const int column = i * 8 + t + 4 * c;                // the row of lanes with g = 2t + c
                 if (two) {
                     sums[sum_at(warp, m, column, g)] = acc[m][i][c] + acc[m][i][2 + c];
                 } else {
@@ -540,12 +544,13 @@ __device__ __forceinline__ void layer_rows(const LayerArgs& a, const LayerMaps& 
 // The rows of the CTA's expert, 32 at a time, against its weights.
 template <int STAGE, bool MX, bool BF16>
 __device__ __forceinline__ void layer_unit(const LayerArgs& a, const LayerMaps& maps, char* smem) {
-    __shared__ __align__(8) unsigned long long bars[kLayerWarps][kStages];
+    __shared__ __align__(8) unsigned long long bars[kLayerWarps][2];
     __shared__ int gave_up;
     if (threadIdx.x == 0) gave_up = 0;
+    smem += (1024 - (smem_u32(smem) & 1023)) & 1023;
     Ring ring = {smem_u32(bars[threadIdx.x >> 5]), 0u, &gave_up};
     if ((threadIdx.x & 31) == 0)
-        for (int s = 0; s < kStages; ++s) bar_init(ring.bars + s * 8, 1);
+        for (int s = 0; s < 2; ++s) bar_init(ring.bars + s * 8, 1);
     fence_bar_init();
     fence_async_shared();
     __syncthreads();
@@ -634,18 +639,18 @@ cudaError_t launch_layer(emc2_bridge* h, LayerArgs a, cudaStream_t st) {
         const int K = i < 2 ? a.C : a.H, M = i < 2 ? a.H : a.C;
         const cuuint64_t row = MX ? (cuuint64_t)mx4_blocks(K) * 16 : (cuuint64_t)K * 2;
         const cuuint64_t dims[2] = {MX ? row : (cuuint64_t)K, (cuuint64_t)a.E * M}, strides[1] = {row};
-        const cuuint32_t box[2] = {MX ? 64u : 32u, i < 2 ? 16u : 32u}, step[2] = {1, 1};
+        const cuuint32_t box[2] = {MX ? 128u : 64u, i < 2 ? 16u : 32u}, step[2] = {1, 1};
         const EncodeTiled f = encoder();
         if (!f || f(&maps.w[i], MX ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2,
-                    const_cast<void*>(a.w[i]), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE,
+                    const_cast<void*>(a.w[i]), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                     CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
             return cudaErrorInvalidValue;
     }
     const int experts = std::min(a.E, a.n * a.k);
-    const int step = MX ? 128 : 32;
+    const int step = MX ? 256 : 64;
     // Warps that share a tile: as many as fill the SMs, and as have steps.
     auto plan = [&](int K, int M, int width) {
-        const int steps = (K + step - 1) / step, most_log = MX ? 1 : 3;
+        const int steps = (K + step - 1) / step, most_log = MX ? 0 : 2;
         for (a.split_log = 0;; ++a.split_log) {
             const int per = (kLayerWarps >> a.split_log) * width;
             a.tiles = (M + per - 1) / per;
