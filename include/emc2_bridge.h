@@ -451,15 +451,17 @@ int emc2_mx4_quantise(emc2_bridge_t* bridge, int32_t rows, int32_t channels, int
  *                  dispatch), 1 <= choices <= 8, choices <= experts
  *   d_w_gate, d_w_up  type [experts, hidden, channels]     d_w_down  type [experts, channels, hidden]; hidden a multiple of 8 up to 8192
  *   d_ids          int32 [n, choices]     d_weights  float [n, choices]: the chosen experts and p
- * Logits are summed in 64 bits; of equal ones the lower expert is first, and NaN are behind all others.  Products are summed in fp32;
- * act(g) * u is rounded to the type before the last product (in EMC2_F16 it has to stay below 65504), the result once. */
+ * Logits are within 2^-38 of the sum of their terms' sizes; of equal ones the lower expert is first, and NaN are behind all others.
+ * Products are summed in fp32; act(g) * u goes into the last product as the sum of two numbers of the type where an expert has up to 16
+ * rows of the call, else rounded to the type (in EMC2_F16 it has to stay below 65504); the result is rounded once. */
 int emc2_expert_layer(emc2_bridge_t* bridge, int32_t n, int32_t channels, int32_t hidden, int32_t experts, int32_t choices, int32_t type,
                       int32_t act, const void* d_x, const int32_t* d_count, const float* d_w_router, const float* d_b_router,
                       const void* d_w_gate, const void* d_w_up, const void* d_w_down, void* d_y, int32_t* d_ids, float* d_weights,
                       void* cuda_stream);
 
 /* The same with weights in the form of emc2_mx4_quantise (the rows are [experts * hidden] of `channels` for the gate and the up
- * projection, [experts * channels] of `hidden` for the down projection): products with what the codes stand for, summed in fp32. */
+ * projection, [experts * channels] of `hidden` for the down projection): products with what the codes stand for, summed in fp32; in
+ * EMC2_F16 elements are rounded to multiples of 2^-24 of their row's largest power. */
 int emc2_expert_layer_mx4(emc2_bridge_t* bridge, int32_t n, int32_t channels, int32_t hidden, int32_t experts, int32_t choices, int32_t type,
                           int32_t act, const void* d_x, const int32_t* d_count, const float* d_w_router, const float* d_b_router,
                           const uint8_t* d_gate_codes, const uint8_t* d_gate_scales, const uint8_t* d_up_codes, const uint8_t* d_up_scales,

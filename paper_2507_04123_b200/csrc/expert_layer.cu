@@ -10,7 +10,9 @@
 // from memory into the registers of m16n8k16 products, whose 16 rows are the rows at hand and whose 8 columns are the weights': a row
 // of x more costs no more reading, and there are too few of them for larger products to help.
 //
-// The logits are summed in 64 bits, so that the choice does not depend on an order of summation; products in fp32.  act(g) * u goes into the
+// A logit is the sum of a sum in fp32 and of all that its roundings left (Ogita, Rump and Oishi, "Accurate sum and dot product", 2005), as if
+// of twice the bits, so that the choice does not depend on an order of summation; 64-bit arithmetic took six times as long.  Products are
+// summed in fp32.  act(g) * u goes into the
 // last product as the sum of two numbers of the type where an expert has up to 16 rows, whose products have columns to spare, else rounded to
 // one.  y is rounded once.
 #include <algorithm>
@@ -70,10 +72,6 @@ struct LayerArgs {
     int last_adds;                           // ... and whether its last CTAs add up
 };
 
-__device__ __forceinline__ float type_float(const void* p, size_t i, bool bf16) {
-    return bf16 ? __bfloat162float(static_cast<const __nv_bfloat16*>(p)[i]) : __half2float(static_cast<const __half*>(p)[i]);
-}
-
 // Place of element i among eight, in the order that codes come in.
 __host__ __device__ __forceinline__ int ordered_place(int i) { return (i & 3) * 2 + (i >> 2); }
 
@@ -84,14 +82,22 @@ __device__ __forceinline__ unsigned long long logit_key(double v) {
     return b < 0 ? ~(unsigned long long)b : (unsigned long long)b | 0x8000000000000000ull;
 }
 
+// high + rest += a b, the products' and the sums' roundings kept.
+__device__ __forceinline__ void add_product(float& high, float& rest, float a, float b) {
+    const float p = __fmul_rn(a, b), left = __fmaf_rn(a, b, -p), s = __fadd_rn(high, p), t = __fsub_rn(s, high);
+    rest = __fadd_rn(rest, __fadd_rn(__fadd_rn(__fsub_rn(high, __fsub_rn(s, t)), __fsub_rn(p, t)), left));
+    high = s;
+}
+
 // One CTA per row.
 template <bool BF16>
 __global__ void __launch_bounds__(kRouteThreads) layer_route_kernel(LayerArgs a) {
-    __shared__ __align__(16) double x[kMaxRowChannels];
+    __shared__ __align__(16) float x[kMaxRowChannels];
     __shared__ unsigned long long key[kMaxLayerExperts];
     __shared__ double logit[kMaxLayerExperts];
     __shared__ int last;
     const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    release_successor();                                          // at once: what follows waits for the end of this kernel, set up
     int used = a.n;
     if (a.count) {
         used = *a.count;
@@ -101,33 +107,40 @@ __global__ void __launch_bounds__(kRouteThreads) layer_route_kernel(LayerArgs a)
         }
     }
     if (row < used) {
-        for (int i = tid; i < a.C; i += kRouteThreads) {
-            const float v = type_float(a.x, (size_t)row * a.C + i, BF16);
-            x[i] = (double)v;
+        if (tid < a.C / 8) {
+            const uint4 v = __ldg(static_cast<const uint4*>(a.x) + (size_t)row * (a.C / 8) + tid);
+            const float4 f = as_floats(make_uint2(v.x, v.y), BF16 ? EMC2_BF16 : EMC2_F16), g = as_floats(make_uint2(v.z, v.w), BF16 ? EMC2_BF16 : EMC2_F16);
+            reinterpret_cast<float4*>(x)[2 * tid] = f;
+            reinterpret_cast<float4*>(x)[2 * tid + 1] = g;
             // Eight codes come as the pairs (0, 4), (1, 5), (2, 6), (3, 7).
-            if (a.ordered) {
-                uint16_t* to = static_cast<uint16_t*>(const_cast<void*>(a.ordered)) + (size_t)row * a.C + (i & ~7) + ordered_place(i & 7);
-                *to = static_cast<const uint16_t*>(a.x)[(size_t)row * a.C + i];
-            }
+            if (a.ordered)
+                static_cast<uint4*>(const_cast<void*>(a.ordered))[(size_t)row * (a.C / 8) + tid] =
+                    make_uint4(__byte_perm(v.x, v.z, 0x5410), __byte_perm(v.x, v.z, 0x7632), __byte_perm(v.y, v.w, 0x5410), __byte_perm(v.y, v.w, 0x7632));
         }
         __syncthreads();
         // Four experts at a time, so that their weights are under way together.
         for (int e0 = warp * 4; e0 < a.E; e0 += kRouteWarps * 4) {
-            double sum[4] = {0.0, 0.0, 0.0, 0.0};
+            float high[4] = {0.f, 0.f, 0.f, 0.f}, rest[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
             for (int v = lane; v < a.C / 4; v += 32) {
                 float4 f[4];
 #pragma unroll
                 for (int q = 0; q < 4; ++q)
                     f[q] = e0 + q < a.E ? __ldg(reinterpret_cast<const float4*>(a.w_router + (size_t)(e0 + q) * a.C) + v) : make_float4(0.f, 0.f, 0.f, 0.f);
-                const double2 g = *reinterpret_cast<const double2*>(x + 4 * v), h = *reinterpret_cast<const double2*>(x + 4 * v + 2);
+                const float4 g = reinterpret_cast<const float4*>(x)[v];
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
-                    sum[q] += (double)f[q].x * g.x;
-                    sum[q] += (double)f[q].y * g.y;
-                    sum[q] += (double)f[q].z * h.x;
-                    sum[q] += (double)f[q].w * h.y;
+                    add_product(high[q], rest[q], f[q].x, g.x);
+                    add_product(high[q], rest[q], f[q].y, g.y);
+                    add_product(high[q], rest[q], f[q].z, g.z);
+                    add_product(high[q], rest[q], f[q].w, g.w);
                 }
+            }
+            double sum[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                sum[q] = (double)high[q] + (double)rest[q];
+                if (!isfinite(high[q])) sum[q] = (double)high[q];            // what is left of an infinite sum is no number
             }
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
@@ -149,15 +162,15 @@ __global__ void __launch_bounds__(kRouteThreads) layer_route_kernel(LayerArgs a)
             int id = 0;
             for (int j = 0; j < a.k; ++j) {
                 unsigned long long best = 0;
-                int at = 0;
+                unsigned at = 0;
                 for (int e = lane; e < a.E; e += 32)
                     if (key[e] > best) { best = key[e]; at = e; }
-#pragma unroll
-                for (int d = 16; d; d >>= 1) {
-                    const unsigned long long other = __shfl_xor_sync(0xFFFFFFFFu, best, d);
-                    const int o = __shfl_xor_sync(0xFFFFFFFFu, at, d);
-                    if (other > best || (other == best && o < at)) { best = other; at = o; }
-                }
+                // The largest upper half, of those the largest lower half, of those the lowest expert.
+                const unsigned upper = __reduce_max_sync(0xFFFFFFFFu, (unsigned)(best >> 32));
+                bool mine = (unsigned)(best >> 32) == upper;
+                const unsigned lower = __reduce_max_sync(0xFFFFFFFFu, mine ? (unsigned)best : 0u);
+                mine = mine && (unsigned)best == lower && best != 0;
+                at = __reduce_min_sync(0xFFFFFFFFu, mine ? at : ~0u);
                 if (j == 0) top = logit[at];
                 if (lane == j) { chosen = logit[at]; id = at; }
                 if (lane == 0) key[at] = 0;
@@ -175,18 +188,48 @@ __global__ void __launch_bounds__(kRouteThreads) layer_route_kernel(LayerArgs a)
     }
     // The last CTA sorts the pairs: stable, by the counts of every expert in pieces of 32 pairs.
     __syncthreads();
-    if (tid == 0) {
+    if (gridDim.x > 1) {
+        if (tid == 0) {
+            __threadfence();
+            last = atomicAdd(&a.notes->arrived, 1) == (int)gridDim.x - 1;
+        }
+        __syncthreads();
+        if (!last) return;
         __threadfence();
-        last = atomicAdd(&a.notes->arrived, 1) == (int)gridDim.x - 1;
     }
-    __syncthreads();
-    release_successor();
-    if (!last) return;
-    __threadfence();
+    const int pairs = used * a.k;
+    if (pairs <= 32) {                                            // by one warp, whose lanes are the pairs
+        if (warp > 0) return;
+        const int e = lane < pairs ? __ldcg(a.ids + lane) : kMaxLayerExperts;
+        const unsigned same = __match_any_sync(0xFFFFFFFFu, e);
+        const int rank = __popc(same & ((1u << lane) - 1));
+        int before = 0, active = 0;                               // pairs, and experts, of lower numbers
+        for (int i = 0; i < pairs; ++i) {
+            const int other = __shfl_sync(0xFFFFFFFFu, e, i), first = __shfl_sync(0xFFFFFFFFu, rank, i) == 0;
+            before += other < e;
+            active += other < e && first;
+        }
+        if (lane < pairs) {
+            a.notes->row[before + rank] = lane / a.k;
+            a.notes->place[lane] = before + rank;
+            if (rank == 0) {
+                a.notes->expert[active] = e;
+                a.notes->start[active + 1] = before + __popc(same);
+            }
+        }
+        const int all = __popc(__ballot_sync(0xFFFFFFFFu, lane < pairs && rank == 0));
+        if (lane == 0) {
+            a.notes->active = all;
+            a.notes->used = used;
+            a.notes->start[0] = 0;
+            a.notes->arrived = 0;
+        }
+        return;
+    }
     __shared__ int of[kMaxSlots];
     __shared__ uint16_t piece[kMaxSlots / 32][kMaxLayerExperts];
     __shared__ int base[kMaxLayerExperts], warp_sum[2][kRouteWarps];
-    const int pairs = used * a.k, pieces = (pairs + 31) / 32;
+    const int pieces = (pairs + 31) / 32;
     for (int i = tid; i < pairs; i += kRouteThreads) of[i] = __ldcg(a.ids + i);
     for (int i = tid; i < pieces * kMaxLayerExperts / 2; i += kRouteThreads) reinterpret_cast<uint32_t*>(piece)[i] = 0u;
     __syncthreads();
@@ -586,22 +629,20 @@ __device__ __forceinline__ void layer_sum(const LayerArgs& a, int row, int c) {
 template <bool MX, bool BF16>
 __global__ void __launch_bounds__(kLayerThreads, 2) layer_hidden_kernel(LayerArgs a, const __grid_constant__ LayerMaps maps) {
     await_predecessor();
+    release_successor();
     extern __shared__ __align__(128) char panels[];
     if ((int)blockIdx.x < a.notes->active * a.tiles) layer_unit<HIDDEN, MX, BF16>(a, maps, panels);
-    release_successor();
 }
 
 template <bool MX, bool BF16>
 __global__ void __launch_bounds__(kLayerThreads, 2) layer_down_kernel(LayerArgs a, const __grid_constant__ LayerMaps maps) {
     await_predecessor();
+    release_successor();
     extern __shared__ __align__(128) char panels[];
     __shared__ int last;
     if ((int)blockIdx.x >= a.notes->active * a.tiles * a.shares) return;
     layer_unit<DOWN, MX, BF16>(a, maps, panels);
-    if (!a.last_adds) {
-        release_successor();
-        return;
-    }
+    if (!a.last_adds) return;
     const int unit = unit_of<DOWN>(a), tid = threadIdx.x;
     __syncthreads();
     if (tid == 0) {
