@@ -14,6 +14,8 @@ from typing import Dict, List, Optional, Sequence, Tuple
 
 import torch
 
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
 _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG, "libemc2_bridge.so")
 
@@ -187,7 +189,7 @@ def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
 
 
 def _check(t: torch.Tensor, dtype, shape, name: str, device) -> None:
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous() or t.device != device:
+    if t.dtype != dtype or t.shape != shape or not t.is_contiguous() or t.device != device:
         raise ValueError(f"{name}: expected contiguous {dtype} {tuple(shape)} on {device}, "
                          f"got {t.dtype} {tuple(t.shape)} on {t.device}")
 
@@ -251,7 +253,8 @@ class Bridge:
             raise Emc2Error(rc, where, self.lib.emc2_status_string(rc).decode())
 
     def _stream(self) -> int:
-        return torch.cuda.current_stream(self.device).cuda_stream
+        # The stream's handle without an object around it: 2 us less per call, where torch has the function.
+        return _raw_stream(self.device.index) if _raw_stream else torch.cuda.current_stream(self.device).cuda_stream
 
     def close(self) -> None:
         if getattr(self, "_h", None) is not None and self._h.value:

@@ -16,6 +16,7 @@
 // last product as the sum of two numbers of the type where an expert has up to 16 rows, whose products have columns to spare, else rounded to
 // one.  y is rounded once.
 #include <algorithm>
+#include <atomic>
 
 #include "mx4.cuh"
 #include "umma.cuh"
@@ -672,9 +673,14 @@ constexpr int kPartRows = 2 * kMaxSlots;     // shares times pairs, at most
 template <bool MX, bool BF16>
 cudaError_t launch_layer(emc2_bridge* h, LayerArgs a, cudaStream_t st) {
     constexpr size_t most = kProductShared;
-    cudaError_t e = allow_shared(layer_hidden_kernel<MX, BF16>, most);
-    if (e == cudaSuccess) e = allow_shared(layer_down_kernel<MX, BF16>, most);
-    if (e != cudaSuccess) return e;
+    static std::atomic<uint64_t> allowed{0};                      // devices; one bound for every call, so once for each
+    const uint64_t bit = h->cfg.device < 64 ? (uint64_t)1 << h->cfg.device : 0;
+    if (!(allowed.load(std::memory_order_relaxed) & bit)) {
+        cudaError_t e = allow_shared(layer_hidden_kernel<MX, BF16>, most);
+        if (e == cudaSuccess) e = allow_shared(layer_down_kernel<MX, BF16>, most);
+        if (e != cudaSuccess) return e;
+        allowed.fetch_or(bit, std::memory_order_relaxed);
+    }
     LayerMaps maps;
     for (int i = 0; i < 3; ++i) {
         const int K = i < 2 ? a.C : a.H, M = i < 2 ? a.H : a.C;
