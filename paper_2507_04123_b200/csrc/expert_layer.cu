@@ -352,11 +352,11 @@ struct Ring {
 //            that the row has had so far, which the sums are relative to; when it rises, they are scaled down.
 // The weights of the next step are on their way to shared memory, in boxes that the warp alone reads: registers have no room for as much as the
 // memory needs to be asked for at once (50 KB per SM and more).
-template <int STAGE, bool MX, bool BF16, int MT>
+template <int STAGE, bool MX, bool BF16, bool HALVES, int MT>
 __device__ __forceinline__ void layer_rows(const LayerArgs& a, const LayerMaps& maps, char* smem, Ring& wait, int e, int pair0, int rows, bool two) {
     constexpr int kPiece = MX ? 256 : 64;                         // elements of a step
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
-    const int split = 1 << a.split_log, per_cta = kLayerWarps >> a.split_log, part = warp & (split - 1), slot = warp >> a.split_log;
+    const int split_log = MX ? HALVES : a.split_log, split = 1 << split_log, per_cta = kLayerWarps >> split_log, part = warp & (split - 1), slot = warp >> split_log;
     const int K = STAGE == HIDDEN ? a.C : a.H, M = STAGE == HIDDEN ? a.H : a.C;
     const int unit = unit_of<STAGE>(a), tile = unit * per_cta + slot;        // of 16 hidden units, or of 32 channels
     // The third kernel's share of the hidden units, whole steps of the products; the last ones ragged.
@@ -368,7 +368,7 @@ __device__ __forceinline__ void layer_rows(const LayerArgs& a, const LayerMaps& 
     const int row = g >> 1 | (g & 1) << 2;
     uint32_t at[kRows];
 #pragma unroll
-    for (int i = 0; i < kRows; ++i) at[i] = (uint32_t)(e * M + min(r0 + row + 8 * i, M - 1)) * (uint32_t)blocks + (uint32_t)(k0 / kMxBlock + part * 8 + t);
+    for (int i = 0; i < kRows; ++i) at[i] = (uint32_t)(e * M + min(r0 + row + 8 * i, M - 1)) * (uint32_t)blocks + (uint32_t)(k0 / kMxBlock + t);
     float acc[MT][4][4];                                          // [16 rows][tile]
 #pragma unroll
     for (int m = 0; m < MT; ++m)
@@ -418,11 +418,12 @@ __device__ __forceinline__ void layer_rows(const LayerArgs& a, const LayerMaps& 
         return v;
     };
     const uint32_t ring = panels + 2 * kPanelBytes + warp * kWarpStage;
-    const uint32_t mine[2] = {ring + row * 128 + ((t ^ row) << 4), ring + row * 128 + (((t + 4) ^ row) << 4)};
-    const int stride = kPiece << a.split_log, steps = (k1 - k0 + stride - 1) / stride, panel_log = (MX ? 0 : 2) - a.split_log;       // steps of a panel
+    const uint32_t mine = ring + row * 128 + ((t ^ row) << 4);    // of the step's second half: bit 6 the other way
+    // Warps that share a tile take every such step of it, with 4 bits either half of every step (whose weights they both have copied).
+    const int stride = MX ? kPiece : kPiece << split_log, steps = (k1 - k0 + stride - 1) / stride, panel_log = MX ? 0 : 2 - split_log;      // steps of a panel
     const uint32_t lead = elected();
     auto request = [&](int s, uint32_t (&powers)[2]) {            // powers: of the lane's blocks, a byte for each of the four rows
-        const int k = k0 + s * stride + part * kPiece;
+        const int k = k0 + s * stride + (MX ? 0 : part * kPiece);
         const uint32_t to = ring + (s & 1) * kStage, bar = wait.bars + (s & 1) * 8;
         bar_expect(lead, bar, kWarpStage);
         if (STAGE == HIDDEN) {
@@ -456,7 +457,7 @@ __device__ __forceinline__ void layer_rows(const LayerArgs& a, const LayerMaps& 
         uint4 v[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v[i].x), "=r"(v[i].y), "=r"(v[i].z), "=r"(v[i].w) : "r"(mine[u] + stage + i * 1024));
+            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v[i].x), "=r"(v[i].y), "=r"(v[i].z), "=r"(v[i].w) : "r"((mine ^ u << 6) + stage + i * 1024));
         if (!MX) {
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
@@ -519,9 +520,13 @@ __device__ __forceinline__ void layer_rows(const LayerArgs& a, const LayerMaps& 
         const uint32_t stage = s & 1;
         warp_wait(wait.bars + stage * 8, wait.phases >> stage & 1u, wait.gave_up, a.status);
         wait.phases ^= 1u << stage;
+        const uint32_t at_panel = panels + (panel & 1) * kPanelBytes + lane * 16;
+        if (HALVES) {
+            multiply(stage * kStage, part, part ? powers[0][1] : powers[0][0], at_panel, 4 * part);
+        } else {
 #pragma unroll
-        for (int u = 0; u < 2; ++u)
-            multiply(stage * kStage, u, powers[0][u], panels + (panel & 1) * kPanelBytes + lane * 16, ((in_panel * stride + part * kPiece) >> 5) + (MX ? 4 : 1) * u);
+            for (int u = 0; u < 2; ++u) multiply(stage * kStage, u, powers[0][u], at_panel, ((in_panel * stride + (MX ? 0 : part * kPiece)) >> 5) + (MX ? 4 : 1) * u);
+        }
         __syncwarp();                                             // the stage is done with
         powers[0][0] = powers[1][0];
         powers[0][1] = powers[1][1];
@@ -551,42 +556,46 @@ __device__ __forceinline__ void layer_rows(const LayerArgs& a, const LayerMaps& 
                 }
             }
     __syncthreads();
-    const int width = STAGE == HIDDEN ? 16 : 32;
-    for (int s = 0; s < per_cta; ++s)
-        for (int c = tid / width; c < rows; c += kLayerThreads / width) {
-            const int u = tid % width, at = (unit * per_cta + s) * width + u;
-            if (at >= M) continue;
-            auto sum = [&](int column) {
-                float v = 0.f;
-                for (int q = 0; q < split; ++q) v += sums[sum_at(s * split + q, c / held, column, c % held)];
-                return v;
-            };
-            if (STAGE == HIDDEN) {
-                const float gate = sum(u), up = sum(16 + u);
-                const float f = a.act == EMC2_ACT_SILU ? gate / (1.0f + expf(-gate)) : 0.5f * gate * erfcf(-0.70710678f * gate);
-                const float h = f * up;
-                const size_t to = (size_t)(2 * (pair0 + c)) * a.H + (MX ? (at & ~7) + ordered_place(at & 7) : at);
-                // What the first part leaves is exact; an infinite one leaves nothing.
-                if (BF16) {
-                    __nv_bfloat16* p = static_cast<__nv_bfloat16*>(a.hidden) + to;
-                    const __nv_bfloat16 first = __float2bfloat16_rn(h);
-                    p[0] = first;
-                    p[a.H] = __float2bfloat16_rn(isinf(__bfloat162float(first)) ? 0.f : h - __bfloat162float(first));
-                } else {
-                    __half* p = static_cast<__half*>(a.hidden) + to;
-                    const __half first = __float2half_rn(h);
-                    p[0] = first;
-                    p[a.H] = __float2half_rn(isinf(__half2float(first)) ? 0.f : h - __half2float(first));
-                }
-            } else {
-                a.part[((size_t)share_of<STAGE>(a) * (a.n * a.k) + pair0 + c) * a.C + at] = sum(u);
+    auto sum = [&](int s, int c, int column) {
+        float v = 0.f;
+        for (int q = 0; q < split; ++q) v += sums[sum_at(s * split + q, c / held, column, c % held)];
+        return v;
+    };
+    if (STAGE == DOWN) {
+        for (int s = 0; s < per_cta; ++s)
+            for (int c = warp; c < rows; c += kLayerWarps) {
+                const int at = (unit * per_cta + s) * 32 + lane;
+                if (at < M) a.part[((size_t)share_of<STAGE>(a) * (a.n * a.k) + pair0 + c) * a.C + at] = sum(s, c, lane);
             }
+        __syncthreads();
+        return;
+    }
+    const uint32_t by_rows = (65536u + rows - 1) / rows;          // a quotient of fewer than 256 by it
+    for (int o = tid / 16; o < per_cta * rows; o += kLayerThreads / 16) {
+        const int s = (int)(o * by_rows >> 16), c = o - s * rows, u = tid % 16, at = (unit * per_cta + s) * 16 + u;
+        if (at >= M) continue;
+        const float gate = sum(s, c, u), up = sum(s, c, 16 + u);
+        const float f = a.act == EMC2_ACT_SILU ? gate / (1.0f + expf(-gate)) : 0.5f * gate * erfcf(-0.70710678f * gate);
+        const float h = f * up;
+        const size_t to = (size_t)(2 * (pair0 + c)) * a.H + (MX ? (at & ~7) + ordered_place(at & 7) : at);
+        // What the first part leaves is exact; an infinite one leaves nothing.
+        if (BF16) {
+            __nv_bfloat16* p = static_cast<__nv_bfloat16*>(a.hidden) + to;
+            const __nv_bfloat16 first = __float2bfloat16_rn(h);
+            p[0] = first;
+            p[a.H] = __float2bfloat16_rn(isinf(__bfloat162float(first)) ? 0.f : h - __bfloat162float(first));
+        } else {
+            __half* p = static_cast<__half*>(a.hidden) + to;
+            const __half first = __float2half_rn(h);
+            p[0] = first;
+            p[a.H] = __float2half_rn(isinf(__half2float(first)) ? 0.f : h - __half2float(first));
         }
+    }
     __syncthreads();
 }
 
 // The rows of the CTA's expert, 32 at a time, against its weights.
-template <int STAGE, bool MX, bool BF16>
+template <int STAGE, bool MX, bool BF16, bool HALVES>
 __device__ __forceinline__ void layer_unit(const LayerArgs& a, const LayerMaps& maps, char* smem) {
     __shared__ __align__(8) unsigned long long bars[kLayerWarps][2];
     __shared__ int gave_up;
@@ -602,8 +611,8 @@ __device__ __forceinline__ void layer_unit(const LayerArgs& a, const LayerMaps& 
     for (int p = a.notes->start[i]; p < a.notes->start[i + 1]; p += kRowsAtOnce) {
         const bool two = STAGE == DOWN && a.notes->start[i + 1] - a.notes->start[i] <= kTwoParts;
         const int e = a.notes->expert[i], rows = min(kRowsAtOnce, a.notes->start[i + 1] - p);
-        if ((two ? 2 * rows : rows) <= 16) layer_rows<STAGE, MX, BF16, 1>(a, maps, smem, ring, e, p, rows, two);
-        else layer_rows<STAGE, MX, BF16, 2>(a, maps, smem, ring, e, p, rows, two);
+        if ((two ? 2 * rows : rows) <= 16) layer_rows<STAGE, MX, BF16, HALVES, 1>(a, maps, smem, ring, e, p, rows, two);
+        else layer_rows<STAGE, MX, BF16, HALVES, 2>(a, maps, smem, ring, e, p, rows, two);
     }
     leave_after_timeout(&gave_up);
 }
@@ -627,22 +636,22 @@ __device__ __forceinline__ void layer_sum(const LayerArgs& a, int row, int c) {
     store_row4(a.y, ((size_t)row * a.C + c) / 4, y, BF16 ? EMC2_BF16 : EMC2_F16);
 }
 
-template <bool MX, bool BF16>
+template <bool MX, bool BF16, bool HALVES>
 __global__ void __launch_bounds__(kLayerThreads, 2) layer_hidden_kernel(LayerArgs a, const __grid_constant__ LayerMaps maps) {
     await_predecessor();
     release_successor();
     extern __shared__ __align__(128) char panels[];
-    if ((int)blockIdx.x < a.notes->active * a.tiles) layer_unit<HIDDEN, MX, BF16>(a, maps, panels);
+    if ((int)blockIdx.x < a.notes->active * a.tiles) layer_unit<HIDDEN, MX, BF16, HALVES>(a, maps, panels);
 }
 
-template <bool MX, bool BF16>
+template <bool MX, bool BF16, bool HALVES>
 __global__ void __launch_bounds__(kLayerThreads, 2) layer_down_kernel(LayerArgs a, const __grid_constant__ LayerMaps maps) {
     await_predecessor();
     release_successor();
     extern __shared__ __align__(128) char panels[];
     __shared__ int last;
     if ((int)blockIdx.x >= a.notes->active * a.tiles * a.shares) return;
-    layer_unit<DOWN, MX, BF16>(a, maps, panels);
+    layer_unit<DOWN, MX, BF16, HALVES>(a, maps, panels);
     if (!a.last_adds) return;
     const int unit = unit_of<DOWN>(a), tid = threadIdx.x;
     __syncthreads();
@@ -676,8 +685,10 @@ cudaError_t launch_layer(emc2_bridge* h, LayerArgs a, cudaStream_t st) {
     static std::atomic<uint64_t> allowed{0};                      // devices; one bound for every call, so once for each
     const uint64_t bit = h->cfg.device < 64 ? (uint64_t)1 << h->cfg.device : 0;
     if (!(allowed.load(std::memory_order_relaxed) & bit)) {
-        cudaError_t e = allow_shared(layer_hidden_kernel<MX, BF16>, most);
-        if (e == cudaSuccess) e = allow_shared(layer_down_kernel<MX, BF16>, most);
+        cudaError_t e = allow_shared(layer_hidden_kernel<MX, BF16, false>, most);
+        if (e == cudaSuccess) e = allow_shared(layer_down_kernel<MX, BF16, false>, most);
+        if (e == cudaSuccess && MX) e = allow_shared(layer_hidden_kernel<MX, BF16, MX>, most);
+        if (e == cudaSuccess && MX) e = allow_shared(layer_down_kernel<MX, BF16, MX>, most);
         if (e != cudaSuccess) return e;
         allowed.fetch_or(bit, std::memory_order_relaxed);
     }
@@ -695,13 +706,13 @@ cudaError_t launch_layer(emc2_bridge* h, LayerArgs a, cudaStream_t st) {
     }
     const int experts = std::min(a.E, a.n * a.k);
     const int step = MX ? 256 : 64;
-    // Warps that share a tile: as many as fill the SMs, and as have steps.
+    // Warps that share a tile: none where the tiles (and shares) fill the SMs, else as many as that takes, and as have steps.
     auto plan = [&](int K, int M, int width) {
-        const int steps = (K + step - 1) / step, most_log = MX ? 0 : 2;
+        const int steps = (K + step - 1) / step, most_log = MX ? 1 : 2;
         for (a.split_log = 0;; ++a.split_log) {
             const int per = (kLayerWarps >> a.split_log) * width;
             a.tiles = (M + per - 1) / per;
-            if (a.tiles * experts >= 2 * h->num_sms || a.split_log == most_log || (1 << a.split_log) >= steps) break;
+            if (a.tiles * experts * a.shares >= h->num_sms || a.split_log == most_log || (!MX && (1 << a.split_log) >= steps)) break;
         }
     };
     {
@@ -711,17 +722,17 @@ cudaError_t launch_layer(emc2_bridge* h, LayerArgs a, cudaStream_t st) {
     {
         LaunchScope ls(h, K_LAYER_HIDDEN, st);
         plan(a.C, a.H, 16);
-        launch_chained(layer_hidden_kernel<MX, BF16>, dim3((unsigned)(a.tiles * experts)), kLayerThreads, most, st, a, maps);
+        launch_chained(MX && a.split_log ? layer_hidden_kernel<MX, BF16, MX> : layer_hidden_kernel<MX, BF16, false>, dim3((unsigned)(a.tiles * experts)), kLayerThreads, most, st, a, maps);
     }
     {
         LaunchScope ls(h, K_LAYER_DOWN, st);
-        plan(a.H, a.C, 32);
-        a.shares = 1;
-        while (a.shares < kMaxShares && a.tiles * experts * a.shares < 4 * h->num_sms && a.H >= 2 * a.shares * 256 &&
-               2 * a.shares * a.n * a.k <= kPartRows)
+        // Shares of the hidden units: four CTAs per SM, of 256 units at least.
+        const int tiles = (a.C + kLayerWarps * 32 - 1) / (kLayerWarps * 32);
+        while (a.shares < kMaxShares && tiles * experts * a.shares < 4 * h->num_sms && a.H >= 2 * a.shares * 256 && 2 * a.shares * a.n * a.k <= kPartRows)
             a.shares *= 2;
+        plan(a.H / a.shares, a.C, 32);
         a.last_adds = a.n * a.k * a.shares <= kLastAdds;
-        launch_chained(layer_down_kernel<MX, BF16>, dim3((unsigned)(a.tiles * experts * a.shares)), kLayerThreads, most, st, a, maps);
+        launch_chained(MX && a.split_log ? layer_down_kernel<MX, BF16, MX> : layer_down_kernel<MX, BF16, false>, dim3((unsigned)(a.tiles * experts * a.shares)), kLayerThreads, most, st, a, maps);
     }
     if (!a.last_adds) {
         LaunchScope ls(h, K_LAYER_SUM, st);
