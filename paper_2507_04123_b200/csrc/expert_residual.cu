@@ -15,6 +15,7 @@
 #include <algorithm>
 
 #include "dropout.cuh"
+#include "umma.cuh"
 
 namespace emc2 {
 namespace {
@@ -250,6 +251,12 @@ __global__ void __launch_bounds__(kResThreads, K <= 1 ? 4 : K <= 2 ? 3 : 2) resi
     }
 }
 
+__device__ __forceinline__ uint4 lds128(uint32_t at) {
+    uint4 v;
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at));
+    return v;
+}
+
 struct ResGradArgs {
     RowSegments seg;
     const void* o;                           // the new rows; null without PRE_W
@@ -270,10 +277,10 @@ struct ResGradArgs {
 };
 
 // Sums of N values over the lanes of a row's group, `l` a lane's place in it and `base` the warp's lane of its first; every
-// lane gets them.  Any number of lanes: rows of 80 channels take ten, three of them a warp.  `even`: a power of two.
+// lane gets them.  Any number of lanes: rows of 80 channels take ten, three of them a warp.
 template <int N>
-__device__ __forceinline__ void group_sums(float (&v)[N], int lanes, bool even, int l, int base) {
-    if (even) {
+__device__ __forceinline__ void group_sums(float (&v)[N], int lanes, int l, int base) {
+    if ((lanes & (lanes - 1)) == 0) {
         for (int d = 1; d < lanes; d <<= 1) {
 #pragma unroll
             for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(0xFFFFFFFFu, v[i], d);
@@ -340,38 +347,59 @@ __device__ __forceinline__ void give_sums(const ResGradArgs& a, const float4* su
     __syncthreads();
 }
 
+// Contiguous bytes to shared memory; both on 16 bytes.
+__device__ __forceinline__ void copy_bytes(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
+}
+
 // Rows of up to 256 channels, eight per lane.  The rows are taken expert by expert, an equal run of them per CTA, which sums its rows of an
 // expert before it goes to the next; entry i + e of `part` holds those of CTA i and expert e (along the run of all rows either i or e
 // goes up, so no two share one).  The sums stay in registers; a group of lanes has two rows in work, whose waits for one another's lanes
-// and for shared memory fill each other, and the next two on their way to shared memory, for which no registers are left.
+// and for shared memory fill each other.  The warp's next rows, which lie side by side within a frame, are on their way to shared memory, for
+// which no registers are left, as one piece of every buffer (lane by lane, the copies' own way through the SM's memory pipe was what the kernel
+// waited for).  Rows of four channels more than a multiple of eight need not begin on 16 bytes: their lanes copy their own.
 constexpr int kNarrowThreads = 128;
-constexpr int kNarrowCtas = 3;               // per SM
+constexpr int narrow_ctas(bool wide) { return wide ? 3 : 2; }        // per SM, as the registers have room
 constexpr uint32_t kNarrowSlot = kNarrowThreads * 16;
 template <bool WIDE, int U, bool DROP>
-__global__ void __launch_bounds__(kNarrowThreads, kNarrowCtas) residual_grad_kernel(ResGradArgs a) {
+__global__ void __launch_bounds__(kNarrowThreads, narrow_ctas(WIDE)) residual_grad_kernel(ResGradArgs a) {
     constexpr int kWarps = kNarrowThreads / 32;
     __shared__ int bounds[kMaxBounds];
     __shared__ int start[kMaxSegments + 1];
     __shared__ int run[2];
     __shared__ float4 folded[kFolded - 1][64];                    // the expert's s w, s b and w'
-    extern __shared__ float4 sums[];         // [warps][4][nvec]; before that two stages of two rows
+    __shared__ __align__(8) unsigned long long bars[kWarps][2];
+    __shared__ int gave_up;
+    extern __shared__ float4 sums[];         // [warps][4][nvec], then two stages of two rows per group
     if (!take_run(a, bounds, start, run)) return;
     const int B = a.seg.B, E = a.seg.E;
     const int type_x = rows_type<U>(a.type_x), type_f = block_type<U>(a.type_f), type_y = block_type<U>(a.type_y);
-    const int lanes = a.lanes, warp = threadIdx.x >> 5, per_warp = 32 / lanes;
-    const int sub = (threadIdx.x & 31) / lanes, base = sub * lanes, l = (threadIdx.x & 31) - base, step = kWarps * per_warp;
+    const int lanes = a.lanes, warp = threadIdx.x >> 5, per_warp = 32 / lanes, chunk = 2 * per_warp;
+    const int sub = (threadIdx.x & 31) / lanes, base = sub * lanes, l = (threadIdx.x & 31) - base;
     const bool pre = U || a.par.p[PRE_W] != nullptr, post = U || a.par.p[POST_W] != nullptr, behind = U || a.dout, noted = U || a.stats;
-    const bool drop = U ? DROP : a.drop.any != 0, even = (lanes & (lanes - 1)) == 0, active = sub < per_warp, hi = WIDE || 2 * l + 1 < a.nvec;
+    const bool drop = U ? DROP : a.drop.any != 0, active = sub < per_warp, hi = WIDE || 2 * l + 1 < a.nvec;
     DropoutSeed seed = {};
     if (drop) seed = dropout_seed(a.drop);
-    // Where a row's places have what; all of a thread's are 16 bytes at its number.
-    const uint32_t at_y = (pre ? (type_x == EMC2_F32 ? 2u : 1u) : 0u) * kNarrowSlot;
-    const uint32_t at_d = at_y + (pre ? (type_y == EMC2_F32 ? 2u : 1u) : 0u) * kNarrowSlot;
-    const uint32_t at_f = at_d + (behind ? (type_x == EMC2_F32 ? 2u : 1u) : 0u) * kNarrowSlot;
-    const uint32_t at_s = at_f + (type_f == EMC2_F32 ? 2u : 1u) * kNarrowSlot;
-    const uint32_t at_g = at_s + (noted ? kNarrowSlot : 0u), row_bytes = at_g + (a.gate ? kNarrowSlot : 0u);
-    char* const ring = reinterpret_cast<char*>(sums) + threadIdx.x * 16;
-    const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring);
+    // Bytes of a row in each buffer, and where a stage of the warp has the buffer's rows; with copies by lanes, where it has a lane's
+    // vectors, which are 16 bytes at the thread's number.
+    auto slots = [](int type) { return type == EMC2_F32 ? 2u : 1u; };
+    const uint32_t row_x = slots(type_x) * a.nvec * 8, row_y = slots(type_y) * a.nvec * 8, row_f = slots(type_f) * a.nvec * 8;
+    const uint32_t at_y = pre ? (WIDE ? chunk * row_x : slots(type_x) * kNarrowSlot) : 0u;
+    const uint32_t at_d = at_y + (pre ? (WIDE ? chunk * row_y : slots(type_y) * kNarrowSlot) : 0u);
+    const uint32_t at_f = at_d + (behind ? (WIDE ? chunk * row_x : slots(type_x) * kNarrowSlot) : 0u);
+    const uint32_t at_s = at_f + (WIDE ? chunk * row_f : slots(type_f) * kNarrowSlot);
+    const uint32_t row_bytes = at_s + (noted ? (WIDE ? chunk * 16 : kNarrowSlot) : 0u);      // of a stage of the warp; by lanes, of a row
+    const uint32_t ring_at = smem_u32(sums + kWarps * 4 * a.nvec) + (WIDE ? warp * 2 * row_bytes : threadIdx.x * 16), bar = smem_u32(bars[warp]);
+    if (WIDE) {
+        if (threadIdx.x == 0) gave_up = 0;
+        if ((threadIdx.x & 31) == 0) { bar_init(bar, 1); bar_init(bar + 8, 1); }
+        fence_bar_init();
+        fence_async_shared();
+        __syncthreads();
+    }
+    const bool leads = (threadIdx.x & 31) == 0;
+    const int place = min(sub, per_warp - 1);                     // lanes behind the last group read its row, for nothing
+    uint32_t phases = 0;
     for (int e = segment_of(start, B * E, run[0]) / B; e < E && start[e * B] < run[1]; ++e) {
         const int from = max(run[0], start[e * B]), to = min(run[1], start[(e + 1) * B]);
         if (from >= to) continue;
@@ -390,14 +418,56 @@ __global__ void __launch_bounds__(kNarrowThreads, kNarrowCtas) residual_grad_ker
         for (int i = 0; i < 4; ++i)
 #pragma unroll
             for (int j = 0; j < 8; ++j) acc[i][j] = 0.f;
-        RowAt row_at(a, bounds, start, e);
-        uint32_t next[2];
-        auto request = [&](int p, uint32_t dst) {
+        RowAt row_at(a, bounds, start, e), ahead_at(a, bounds, start, e);
+        uint32_t next[2] = {0u, 0u};                              // rows under way; with copies by lanes
+        // The warp's rows from place p on; a lane's are p + sub and p + per_warp + sub.
+        auto request = [&](int p, uint32_t stage) {
+            uint32_t dst = ring_at + stage * (WIDE ? row_bytes : 2 * row_bytes);
+            if (WIDE) {
+                uint32_t dst_y = dst + at_y, dst_d = dst + at_d, dst_f = dst + at_f, dst_s = dst + at_s;
+                if (p >= to) return;
+                const int end = min(p + chunk, to);
+                if (end - p < chunk) {                            // places without a row are zeros, which add nothing
+                    auto clear = [&](uint32_t buffer, uint32_t bytes) {
+                        for (uint32_t o = (uint32_t)(end - p) * bytes + (threadIdx.x & 31) * 16; o < chunk * bytes; o += 512)
+                            asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(buffer + o), "r"(0u) : "memory");
+                    };
+                    if (pre) {
+                        clear(dst, row_x);
+                        clear(dst_y, row_y);
+                    }
+                    if (behind) clear(dst_d, row_x);
+                    clear(dst_f, row_f);
+                    if (noted) clear(dst_s, 16);
+                    fence_async_shared();                         // before the next expert's copies
+                    __syncwarp();
+                }
+                if (!leads) return;
+                const uint32_t full = bar + stage * 8;
+                bar_expect(1, full, (uint32_t)(end - p) * ((pre ? row_x + row_y : 0u) + (behind ? row_x : 0u) + row_f + (noted ? 16u : 0u)));
+                do {                                              // one piece of every frame
+                    const uint32_t row = ahead_at(p);
+                    const uint32_t len = (uint32_t)(min(end, ahead_at.until) - p);
+                    auto copy = [&](uint32_t to_bytes, const void* rows, uint32_t bytes) {
+                        copy_bytes(to_bytes, static_cast<const char*>(rows) + (unsigned long long)row * bytes, len * bytes, full);
+                    };
+                    if (pre) {
+                        copy(dst, a.o, row_x);
+                        copy(dst_y, a.dy, row_y);
+                    }
+                    if (behind) copy(dst_d, a.dout, row_x);
+                    copy(dst_f, a.f, row_f);
+                    if (noted) copy(dst_s, a.stats, 16);
+                    p += (int)len;
+                    dst += len * row_x; dst_y += len * row_y; dst_d += len * row_x; dst_f += len * row_f; dst_s += len * 16;
+                } while (p < end);
+                return;
+            }
 #pragma unroll
-            for (int k = 0; k < 2; ++k, p += step, dst += row_bytes) {
-                next[k] = 0;
-                if (p >= to || !active) continue;
-                const uint32_t row = next[k] = row_at(p);
+            for (int k = 0; k < 2; ++k, dst += row_bytes) {
+                const int q = p + k * per_warp + sub;
+                if (q >= to || !active) continue;
+                const uint32_t row = next[k] = ahead_at(q);
                 const uint32_t at = row * (uint32_t)a.nvec + 2 * l;             // 2^24 rows of 64 vectors at most
                 if (pre) {
                     ahead8<WIDE, kNarrowSlot>(dst, a.o, at, hi, type_x);
@@ -406,61 +476,73 @@ __global__ void __launch_bounds__(kNarrowThreads, kNarrowCtas) residual_grad_ker
                 if (behind) ahead8<WIDE, kNarrowSlot>(dst + at_d, a.dout, at, hi, type_x);
                 ahead8<WIDE, kNarrowSlot>(dst + at_f, a.f, at, hi, type_f);
                 if (noted) copy_ahead<16>(dst + at_s, a.stats + row);
-                if (a.gate) copy_ahead<4>(dst + at_g, a.gate + row);
             }
             asm volatile("cp.async.commit_group;" ::: "memory");
         };
-        const int first = from + warp * per_warp + sub;
         uint32_t stage = 0;
-        request(first, ring_at);
-        // A warp goes on while any of its groups has a row.
-        for (int p = first; p - sub < to; p += 2 * step) {
-            const bool in[2] = {active && p < to, active && p + step < to};
-            const uint32_t row[2] = {next[0], next[1]};
-            const char* at = ring + stage * 2 * row_bytes;
+        __syncwarp();
+        request(from + warp * chunk, 0);
+        for (int p = from + warp * chunk; p < to; p += kWarps * chunk) {
+            const bool in[2] = {active && p + sub < to, active && p + per_warp + sub < to};
+            uint32_t row[2];
+            float gate[2];
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                row[k] = !WIDE ? next[k] : in[k] ? row_at(p + k * per_warp + sub) : 0u;
+                gate[k] = in[k] && a.gate ? __ldg(a.gate + row[k]) : 1.0f;
+            }
+            const uint32_t now = stage;
+            const uint32_t at = ring_at + stage * (WIDE ? row_bytes : 2 * row_bytes);
             stage ^= 1;
-            request(p + 2 * step, ring_at + stage * 2 * row_bytes);
+            request(p + kWarps * chunk, stage);
             uint4 bits[2];
             if (drop) {                                           // while the rows are on their way
                 const uint32_t group[2] = {(uint32_t)l, (uint32_t)l};
                 dropout_bits(bits, seed, row, group);
             }
-            asm volatile("cp.async.wait_group 1;" ::: "memory");
-            // Lanes without a row go on with zeros, which add nothing.
-            float d[2][8], h[2][8], gate[2];
+            if (WIDE) {
+                warp_wait(bar + now * 8, phases >> now & 1u, &gave_up, a.seg.status);
+                phases ^= 1u << now;
+            } else {
+                asm volatile("cp.async.wait_group 1;" ::: "memory");
+            }
+            float d[2][8], h[2][8];
             float4 st[2];
+            auto taken = [&](float (&f)[8], int k, uint32_t buffer, uint32_t bytes, int type) {
+                Raw8 raw;
+                if (WIDE) {
+                    const uint32_t mine = at + buffer + (uint32_t)(k * per_warp + place) * bytes + (type == EMC2_F32 ? 32u : 16u) * l;
+                    raw.a = lds128(mine);
+                    if (type == EMC2_F32) raw.b = lds128(mine + 16);
+                } else {
+                    raw.a = raw.b = make_uint4(0u, 0u, 0u, 0u);
+                    if (in[k]) {
+                        raw.a = lds128(at + k * row_bytes + buffer);
+                        if (type == EMC2_F32) raw.b = lds128(at + k * row_bytes + buffer + kNarrowSlot);
+                    }
+                    if (!hi) clear_second(raw, type);
+                }
+                floats8(f, raw, type);
+            };
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
-                auto taken = [&](float (&f)[8], uint32_t slot, int type) {
-                    Raw8 raw;
-                    raw.a = raw.b = make_uint4(0u, 0u, 0u, 0u);
-                    if (in[k]) raw = slot8<kNarrowSlot>(at + k * row_bytes + slot, type);
-                    if (!WIDE && !hi) clear_second(raw, type);
-                    floats8(f, raw, type);
-                };
                 st[k] = make_float4(0.f, 1.f, 0.f, 1.f);
-                if (noted && in[k]) st[k] = *reinterpret_cast<const float4*>(at + k * row_bytes + at_s);
-                gate[k] = 1.0f;
-                if (a.gate && in[k]) gate[k] = *reinterpret_cast<const float*>(at + k * row_bytes + at_g);
+                if (noted && (WIDE || in[k])) {
+                    const uint4 v = lds128(WIDE ? at + at_s + (uint32_t)(k * per_warp + place) * 16 : at + k * row_bytes + at_s);
+                    st[k] = make_float4(__uint_as_float(v.x), __uint_as_float(v.y), __uint_as_float(v.z), __uint_as_float(v.w));
+                }
 #pragma unroll
                 for (int j = 0; j < 8; ++j) d[k][j] = 0.f;
-                if (behind) taken(d[k], at_d, type_x);
-                taken(h[k], at_f, type_f);
+                if (behind) taken(d[k], k, at_d, row_x, type_x);
+                taken(h[k], k, at_f, row_f, type_f);
             }
             if (pre) {
                 float o[2][8], g[2][8], w[8], means[4] = {0.f, 0.f, 0.f, 0.f};
                 param8(w, NEXT_W);
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
-                    auto taken = [&](float (&f)[8], uint32_t slot, int type) {
-                        Raw8 raw;
-                        raw.a = raw.b = make_uint4(0u, 0u, 0u, 0u);
-                        if (in[k]) raw = slot8<kNarrowSlot>(at + k * row_bytes + slot, type);
-                        if (!WIDE && !hi) clear_second(raw, type);
-                        floats8(f, raw, type);
-                    };
-                    taken(o[k], 0, type_x);
-                    taken(g[k], at_y, type_y);
+                    taken(o[k], k, 0, row_x, type_x);
+                    taken(g[k], k, at_y, row_y, type_y);
 #pragma unroll
                     for (int j = 0; j < 8; ++j) {
                         o[k][j] = (o[k][j] - st[k].z) * st[k].w;
@@ -472,7 +554,7 @@ __global__ void __launch_bounds__(kNarrowThreads, kNarrowCtas) residual_grad_ker
                         means[2 + k] += g[k][j] * o[k][j];
                     }
                 }
-                group_sums(means, lanes, even, l, base);
+                group_sums(means, lanes, l, base);
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
                     const float m = means[k] * a.inv_c, t = means[2 + k] * a.inv_c;
@@ -524,7 +606,7 @@ __global__ void __launch_bounds__(kNarrowThreads, kNarrowCtas) residual_grad_ker
                     means[2 + k] += d[k][j] * h[k][j];
                 }
             }
-            if (post || a.dgate) group_sums(means, lanes, even, l, base);
+            if (post || a.dgate) group_sums(means, lanes, l, base);
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
                 if (!in[k]) continue;
@@ -536,9 +618,8 @@ __global__ void __launch_bounds__(kNarrowThreads, kNarrowCtas) residual_grad_ker
                 }
                 store8<WIDE>(a.df, (size_t)row[k] * a.nvec + 2 * l, hi, d[k], type_f);
             }
+            __syncwarp();                                         // the stage has been read by all
         }
-        asm volatile("cp.async.wait_group 0;" ::: "memory");
-        __syncthreads();                                          // every thread is done with its stages
         // The groups of a warp hold the same columns at the same places.
         float4* mine = sums + warp * 4 * a.nvec + 2 * l;
 #pragma unroll
@@ -556,6 +637,8 @@ __global__ void __launch_bounds__(kNarrowThreads, kNarrowCtas) residual_grad_ker
         }
         give_sums<kNarrowThreads>(a, sums, e);
     }
+    if (WIDE) leave_after_timeout(&gave_up);
+    else asm volatile("cp.async.wait_group 0;" ::: "memory");
 }
 
 // Wider rows, K groups of eight channels per lane of a warp, whose values fill the registers: the sums are in shared memory, an entry per
@@ -645,7 +728,7 @@ __global__ void __launch_bounds__(kResThreads, 1) residual_grad_wide_kernel(ResG
                         means[1] += g[i][j] * o[i][j];
                     }
                 }
-                group_sums(means, 32, true, l, 0);
+                group_sums(means, 32, l, 0);
                 const float m = means[0] * a.inv_c, t = means[1] * a.inv_c;
 #pragma unroll
                 for (int i = 0; i < K; ++i)
@@ -698,7 +781,7 @@ __global__ void __launch_bounds__(kResThreads, 1) residual_grad_wide_kernel(ResG
                     means[1] += d[i][j] * h[i][j];
                 }
             }
-            if (post || a.dgate) group_sums(means, 32, true, l, 0);
+            if (post || a.dgate) group_sums(means, 32, l, 0);
             if (a.dgate && l == 0) a.dgate[row] = drop ? means[2] * a.drop.factor : means[2];
             const float m = means[0] * a.inv_c, t = means[1] * a.inv_c;
 #pragma unroll
@@ -792,9 +875,14 @@ cudaError_t launch_grad(F kernel, const ResGradArgs& a, int ctas, int threads, s
 cudaError_t launch_narrow(const ResGradArgs& a, bool wide, int usual, int ctas, cudaStream_t st) {
     auto slots = [](int type) { return type == EMC2_F32 ? 2 : 1; };
     const bool pre = a.par.p[PRE_W] != nullptr;
-    const int n = (pre ? slots(a.type_x) + slots(a.type_y) : 0) + (a.dout ? slots(a.type_x) : 0) + slots(a.type_f) + (a.stats ? 1 : 0) + (a.gate ? 1 : 0);
-    const size_t shared = std::max((size_t)(kNarrowThreads / 32) * 4 * a.nvec * sizeof(float4), (size_t)4 * n * kNarrowSlot);
-    constexpr size_t most = 4 * 10 * kNarrowSlot;                 // two stages of two rows of all slots; the sums need less
+    const int n = (pre ? slots(a.type_x) + slots(a.type_y) : 0) + (a.dout ? slots(a.type_x) : 0) + slots(a.type_f);
+    const size_t own = (size_t)(kNarrowThreads / 32) * 4 * a.nvec * sizeof(float4);
+    // Two stages of two rows: per warp of `chunk` rows, or per thread of its vectors and a row's statistics.
+    const size_t chunk = 2 * (32 / a.lanes);
+    const size_t stages = wide ? (size_t)(kNarrowThreads / 32) * 2 * chunk * ((size_t)n * a.nvec * 8 + (a.stats ? 16 : 0)) : (size_t)4 * (n + (a.stats ? 1 : 0)) * kNarrowSlot;
+    const size_t shared = own + stages;
+    // 16 KB of sums and the stages of four fp32 buffers: of lanes' vectors 9 slots, of rows 64 of 144 bytes per warp (eight channels) at most.
+    constexpr size_t most = 16 * 1024 + std::max<size_t>(4 * 9 * kNarrowSlot, 8 * 64 * 144);
     auto kernel = wide ? residual_grad_kernel<true, ANY, true> : residual_grad_kernel<false, ANY, true>;
     if (usual == F32_ROWS) kernel = a.drop.any ? residual_grad_kernel<true, F32_ROWS, true> : residual_grad_kernel<true, F32_ROWS, false>;
     if (usual == BF16_ROWS) kernel = a.drop.any ? residual_grad_kernel<true, BF16_ROWS, true> : residual_grad_kernel<true, BF16_ROWS, false>;
@@ -807,7 +895,7 @@ cudaError_t launch_wide(const ResGradArgs& a, bool wide, int ctas, cudaStream_t 
                        (size_t)warps * 4 * a.nvec * sizeof(float4), (size_t)warps * 4 * 64 * K * sizeof(float4), st);
 }
 
-int residual_grad_ctas(const emc2_bridge* h, int per) { return (per == 1 ? kNarrowCtas : 1) * h->num_sms; }
+int residual_grad_ctas(const emc2_bridge* h, int per, bool wide) { return (per == 1 ? narrow_ctas(wide) : 1) * h->num_sms; }
 constexpr int kShareInts = 64;               // 2 * EMC2_MAX_EXPERTS and up to a multiple of 256 bytes
 
 int check_residual(const emc2_bridge* h, int B, int N, int channels, int type_x, int type_f, int type_y, const void* f, const int32_t* offsets,
@@ -826,7 +914,7 @@ int check_residual(const emc2_bridge* h, int B, int N, int channels, int type_x,
 }  // namespace
 
 size_t residual_scratch_bytes(const emc2_bridge* h, int max_channels) {
-    return kShareInts * sizeof(int) + (size_t)(residual_grad_ctas(h, 1) + EMC2_MAX_EXPERTS) * 4 * max_channels * sizeof(float);
+    return kShareInts * sizeof(int) + (size_t)(residual_grad_ctas(h, 1, true) + EMC2_MAX_EXPERTS) * 4 * max_channels * sizeof(float);
 }
 
 }  // namespace emc2
@@ -937,7 +1025,7 @@ extern "C" int emc2_expert_residual_grad(emc2_bridge_t* h, int32_t B, int32_t N,
                       (!d_grad_out || is_wide(channels, type_x, d_grad_out)) &&
                       (!d_pre_weight || (is_wide(channels, type_x, d_out) && is_wide(channels, type_y, d_grad_y)));
     const long long rows = (long long)B * N, per_cta = per == 1 ? 2 * (kNarrowThreads / 32) * (32 / a.lanes) : kResThreads / 32;
-    const int ctas = (int)std::min<long long>((rows + per_cta - 1) / per_cta, residual_grad_ctas(h, per));
+    const int ctas = (int)std::min<long long>((rows + per_cta - 1) / per_cta, residual_grad_ctas(h, per, wide));
     const int usual = wide && d_post_weight && d_pre_weight && d_grad_out ? usual_of(type_x, type_f, type_y) : ANY;
     {
         LaunchScope ls(h, K_RESIDUAL_GRAD, st);
