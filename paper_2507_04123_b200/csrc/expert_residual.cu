@@ -21,7 +21,10 @@ namespace emc2 {
 namespace {
 
 constexpr int kResThreads = 256;
-constexpr int kResShared = 40 * 1024;        // of parameters; more are read through the L1 cache
+constexpr int kResShared = 64 * 1024;        // of parameters; more are read through the L1 cache
+// CTAs per SM.  Each stages the parameters and works out where its rows are, but few of them end unevenly.  us with 2, 4 and 8: 1.2 million rows
+// of 80 channels, fp32 209, 192 and 193; 60,000 of 1,024, bf16 117, 127 and 144; 240,000 of 36, fp32 37, 40 and 46.
+constexpr int kResGrid = 4;
 constexpr int kParams = 5;
 enum Param { POST_W = 0, POST_B, SCALE, PRE_W, PRE_B };
 
@@ -942,14 +945,16 @@ extern "C" int emc2_expert_residual(emc2_bridge_t* h, int32_t B, int32_t N, int3
     a.x = d_x; a.f = d_f; a.gate = d_gate; a.par = par; a.out = d_out; a.y = d_y; a.stats = reinterpret_cast<float4*>(d_stats);
     a.drop = make_dropout(p, d_seed);
     a.eps = eps; a.inv_c = 1.0f / (float)channels; a.nvec = channels / 4; a.type_x = type_x; a.type_f = type_f; a.type_y = type_y;
-    const RowSplit split = row_split((channels + 7) / 8, 5);
+    // Rows whose last group is half empty are accessed by 8 and 16 bytes, which few lanes that are far apart do worse: 240,000 rows of 36 fp32
+    // channels by one lane each 49 us, by two 46.
+    const RowSplit split = row_split((channels + 7) / 8, channels % 8 ? 3 : 5);
     a.log = split.log;
     const size_t staged = (size_t)kFolded * a.seg.E * channels * sizeof(float);
     a.shared = staged <= kResShared;
     const bool wide = is_wide(channels, type_x, d_x) && is_wide(channels, type_x, d_out) && is_wide(channels, type_f, d_f) &&
                       (!d_y || is_wide(channels, type_y, d_y));
     const long long rows = (long long)B * N, per_cta = kResThreads >> split.log;
-    const int ctas = (int)std::min<long long>((rows + per_cta - 1) / per_cta, 8LL * h->num_sms);
+    const int ctas = (int)std::min<long long>((rows + per_cta - 1) / per_cta, (long long)kResGrid * h->num_sms);
     LaunchScope ls(h, K_RESIDUAL, st);
     a.params_bytes = a.shared ? (uint32_t)staged : 0u;
     // Every lane of a row full, and the parameters in shared memory.
