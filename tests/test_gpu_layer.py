@@ -268,10 +268,12 @@ def test_first_call_of_a_thread_and_profile():
     thread.start()
     thread.join()
     assert all(torch.equal(got[0][i], want[i]) for i in want)
-    br.profile_read()
-    br.expert_layer(x, wr, *ws, 2)
-    counts = br.profile_read()
-    assert [counts[i][0] for i in ("layer_route", "layer_hidden", "layer_down")] == [1, 1, 1]
+    for rows, launches in ((1, [0, 1, 1]), (2, [1, 1, 1])):        # one row is routed by the kernel of its first products
+        y = x[:1].expand(rows, -1).contiguous()
+        br.profile_read()
+        br.expert_layer(y, wr, *ws, 2)
+        counts = br.profile_read()
+        assert [counts[i][0] for i in ("layer_route", "layer_hidden", "layer_down")] == launches
     br.close()
 
 
