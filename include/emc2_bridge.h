@@ -326,7 +326,8 @@ int emc2_scene_route(emc2_bridge_t* bridge, int32_t B, const int32_t* d_offsets,
 typedef enum { EMC2_F32 = 0, EMC2_BF16 = 1, EMC2_F16 = 2 } emc2_type_t;
 
 /* Allocates the scratch of the calls marked (scratch) for up to max_channels channels (4 .. 1024) and
- * any batch the handle takes; max_hidden >= 0 is the largest hidden width of emc2_expert_ffn and its gradient.  A
+ * any batch the handle takes; max_hidden >= 0 is the largest hidden width of emc2_expert_ffn, its gradient and
+ * emc2_expert_layer, which needs one.  A
  * later call can ask for more: the first area then stays allocated until the handle is destroyed, so that graphs
  * captured with it stay valid.  Call it outside any stream capture. */
 int emc2_rows_reserve(emc2_bridge_t* bridge, int32_t max_channels, int32_t max_hidden);
@@ -451,7 +452,7 @@ int emc2_mx4_quantise(emc2_bridge_t* bridge, int32_t rows, int32_t channels, int
  *                  dispatch), 1 <= choices <= 8, choices <= experts
  *   d_w_gate, d_w_up  type [experts, hidden, channels]     d_w_down  type [experts, channels, hidden]; hidden a multiple of 8 up to 8192
  *   d_ids          int32 [n, choices]     d_weights  float [n, choices]: the chosen experts and p
- * Logits are within 2^-38 of the sum of their terms' sizes; of equal ones the lower expert is first, and NaN are behind all others.
+ * Logits are within 2^-38 of the sum of their terms' sizes and 2^-138; of equal ones the lower expert is first, and NaN are behind all others.
  * Products are summed in fp32; act(g) * u goes into the last product as the sum of two numbers of the type where an expert has up to 16
  * rows of the call, else rounded to the type (in EMC2_F16 it has to stay below 65504); the result is rounded once. */
 int emc2_expert_layer(emc2_bridge_t* bridge, int32_t n, int32_t channels, int32_t hidden, int32_t experts, int32_t choices, int32_t type,

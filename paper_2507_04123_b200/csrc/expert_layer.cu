@@ -3,18 +3,21 @@
 //   l = x w_router^T + b;  the k largest;  p = softmax over these
 //   y = sum_j p_j (act(x w_gate[e_j]^T) * (x w_up[e_j]^T)) w_down[e_j]^T
 //
-// Bound by the weights of the experts that are asked for, which are read once.  The first kernel has a CTA per row; the last of them to finish
-// sorts the pairs (row, choice) by expert.  The second has a CTA per expert and tile of hidden units, the third per expert, tile of channels
-// and share of the hidden units; what they leave is added up in the order of a row's choices, by the last CTA of a tile of channels or, for more
-// rows, by a fourth kernel.  Each kernel is set up while the one before still runs.  In both products every warp streams its own rows of weights
-// from memory into the registers of m16n8k16 products, whose 16 rows are the rows at hand and whose 8 columns are the weights': a row
-// of x more costs no more reading, and there are too few of them for larger products to help.
+// Bound by the weights of the experts that are asked for, which are read once; a row alone by the kernels' starts and waits, 4-bit weights
+// by what makes numbers of them.  The first kernel has a CTA per row; the last of them to finish sorts the pairs (row, choice) by expert.  The
+// second has a CTA per expert and tile of hidden units, the third per expert, tile of channels and share of the hidden units; what they leave
+// is added up in the order of a row's choices, by the last CTA of a tile of channels or, for more rows, by a fourth kernel.  Each kernel is set
+// up while the one before still runs.  In both products every warp streams its own rows of weights from memory into the registers of m16n8k16
+// products, whose 16 rows are the rows at hand and whose 8 columns are the weights': a row of x more costs no more reading, and there are too
+// few of them for larger products to help.
+//
+// 128 rows of 1,024 channels, 4 of 32 experts of 4,096 units, bf16: 172 us, of which the weights' 805 MB take 123 at a copy's rate; in 4 bits 151
+// (33), with half of the issue slots and a third of the tensor pipe's.  One row of 256 channels, 2 of 16 experts of 1,024 units: 12.8.
 //
 // A logit is the sum of a sum in fp32 and of all that its roundings left (Ogita, Rump and Oishi, "Accurate sum and dot product", 2005), as if
 // of twice the bits, so that the choice does not depend on an order of summation; 64-bit arithmetic took six times as long.  Products are
-// summed in fp32.  act(g) * u goes into the
-// last product as the sum of two numbers of the type where an expert has up to 16 rows, whose products have columns to spare, else rounded to
-// one.  y is rounded once.
+// summed in fp32.  act(g) * u goes into the last product as the sum of two numbers of the type where an expert has up to 16 rows, whose
+// products have columns to spare, else rounded to one.  y is rounded once.
 #include <algorithm>
 #include <atomic>
 
@@ -103,6 +106,26 @@ __device__ __forceinline__ int rows_in_use(const LayerArgs& a, bool reports) {
     return min(max(used, 0), a.n);
 }
 
+// The warp's logits once more, in 64 bits: where terms or sums are past the range of fp32, or without a value.
+__device__ __forceinline__ void far_logits(const float* w, const float* bias, int C, int E, Router& r) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+#pragma unroll 1
+    for (int e = 0; e < E; ++e) {
+        if ((e >> 2) % kRouteWarps != warp) continue;
+        double l = 0.0;
+#pragma unroll 1
+        for (int c = lane; c < C; c += 32) l += (double)__ldg(w + (size_t)e * C + c) * (double)r.x[c];
+#pragma unroll
+        for (int d = 16; d; d >>= 1) l += __shfl_xor_sync(0xFFFFFFFFu, l, d);
+        if (bias) l += (double)__ldg(bias + e);
+        __syncwarp();
+        if (lane == 0) {
+            r.logit[e] = l;
+            r.key[e] = logit_key(l);
+        }
+    }
+}
+
 // A row's choices, by a whole CTA of kRouteThreads: lane j of the first warp has choice j and its weight.
 template <bool BF16>
 __device__ __forceinline__ void choose(const LayerArgs& a, int row, Router& r, int& id, float& weight) {
@@ -115,6 +138,7 @@ __device__ __forceinline__ void choose(const LayerArgs& a, int row, Router& r, i
     }
     __syncthreads();
     // Four experts at a time, so that their weights are under way together.
+    bool far = false;
     for (int e0 = warp * 4; e0 < a.E; e0 += kRouteWarps * 4) {
         float high[4] = {0.f, 0.f, 0.f, 0.f}, rest[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
@@ -133,10 +157,11 @@ __device__ __forceinline__ void choose(const LayerArgs& a, int row, Router& r, i
             }
         }
         double sum[4];
+        bool past = false;
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
             sum[q] = (double)high[q] + (double)rest[q];
-            if (!isfinite(high[q])) sum[q] = (double)high[q];            // what is left of an infinite sum is no number
+            past = past || !isfinite(high[q]);
         }
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
@@ -151,7 +176,9 @@ __device__ __forceinline__ void choose(const LayerArgs& a, int row, Router& r, i
             r.logit[e] = l;
             r.key[e] = logit_key(l);
         }
+        far = far || __any_sync(0xFFFFFFFFu, past);
     }
+    if (far) far_logits(a.w_router, a.b_router, a.C, a.E, r);
     __syncthreads();
     if (warp > 0) return;
     double chosen = 0.0, top = 0.0;                               // lane j: logit of choice j
@@ -207,9 +234,10 @@ __device__ __forceinline__ void sort_few(N& to, int e, int pairs, int k, int use
     }
 }
 
-// One CTA per row.
+// One CTA per row, and with room for few: without that bound the compiler keeps to 48 registers, too few for the weights under way, and routing
+// 128 rows of 1,024 channels to 4 of 32 experts takes 27 us instead of 17 by itself.
 template <bool BF16>
-__global__ void __launch_bounds__(kRouteThreads) layer_route_kernel(LayerArgs a) {
+__global__ void __launch_bounds__(kRouteThreads, 1) layer_route_kernel(LayerArgs a) {
     __shared__ __align__(16) Router router;
     __shared__ int last;
     const int row = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;

@@ -1,6 +1,6 @@
 """4-bit weights, and the layer for few rows with weights of 16 and of 4 bits, against the formulas in 64 bits (needs a B200).
 
-Quantisation has to be exact; the layer's choices too (its logits are summed in 64 bits); its results within the bounds of
+Quantisation has to be exact; the layer's choices too (its logits are as of a sum in 48 bits); its results within the bounds of
 layer_cases.py."""
 import pytest
 import torch
@@ -166,6 +166,33 @@ def test_choices_at_borders():
     assert torch.isnan(got["y"][2]).all() and got["ids"][2].tolist() == [0, 1, 2]
     rest = [0, 1, 3, 5]
     assert all(torch.equal(got[i][rest], want[i][rest]) for i in want)
+    br.status()
+    br.close()
+
+
+@pytest.mark.parametrize("n", [1, 2])
+def test_logits_past_fp32(n):
+    """Terms, sums on the way and results beyond fp32's range, which have values in 64 bits: 2^133, 0, 2^132, 2^131, -2^120 and an
+    infinity."""
+    C, H, E = 64, 16, 6
+    br = handle(1, 8)
+    br.reserve_rows(C, H)
+    x = torch.ones((n, C), dtype=torch.bfloat16, device=DEV)
+    x[:, 8:] = 2.0 ** 100
+    wr = torch.zeros((E, C), device=DEV)
+    wr[0, 8] = 2.0 ** 33
+    wr[1, 8], wr[1, 9] = 2.0 ** 40, -2.0 ** 40                              # infinities of both signs in 32 bits
+    wr[2, 8:16] = 2.0 ** 29                                                 # past the range by their sum
+    wr[3, 8], wr[3, 9] = 2.0 ** 32, -2.0 ** 31
+    wr[4, 8] = -2.0 ** 20
+    wr[5, 8] = -torch.inf
+    ws = [torch.zeros(s, dtype=torch.bfloat16, device=DEV) for s in ((E, H, C), (E, H, C), (E, C, H))]
+    got = br.expert_layer(x, wr, *ws, 6)
+    want = (x.double() @ wr.double().t()).sort(dim=-1, descending=True, stable=True)[1]
+    assert want[0].tolist() == [0, 2, 3, 1, 4, 5]
+    assert torch.equal(got["ids"].long(), want)
+    assert got["weights"].tolist() == [[1.0, 0.0, 0.0, 0.0, 0.0, 0.0]] * n
+    assert (got["y"] == 0).all()
     br.status()
     br.close()
 
