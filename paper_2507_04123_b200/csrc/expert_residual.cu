@@ -45,16 +45,18 @@ __device__ __forceinline__ float4 folded_param(const ResParams& par, int i, int 
 }
 
 // The usual calls have kernels of their own, without the branches on what a call can lack, which were half of the instructions: both norms, a
-// gradient from behind, bf16 blocks, rows in fp32 or bf16 of a multiple of eight channels.
-enum Usual { ANY = 0, F32_ROWS, BF16_ROWS };
+// gradient from behind, rows of a multiple of eight channels, all bf16 or fp16, or fp32 with bf16 blocks.
+enum Usual { ANY = 0, F32_ROWS, BF16_ROWS, F16_ROWS };
 inline int usual_of(int type_x, int type_f, int type_y) {
-    if (type_f != EMC2_BF16 || type_y != EMC2_BF16) return ANY;
+    if (type_f != type_y) return ANY;
+    if (type_f == EMC2_F16) return type_x == EMC2_F16 ? F16_ROWS : ANY;
+    if (type_f != EMC2_BF16) return ANY;
     return type_x == EMC2_F32 ? F32_ROWS : type_x == EMC2_BF16 ? BF16_ROWS : ANY;
 }
 template <int U>
-__device__ __forceinline__ int rows_type(int type) { return U == F32_ROWS ? EMC2_F32 : U == BF16_ROWS ? EMC2_BF16 : type; }
+__device__ __forceinline__ int rows_type(int type) { return U == F32_ROWS ? EMC2_F32 : U == BF16_ROWS ? EMC2_BF16 : U == F16_ROWS ? EMC2_F16 : type; }
 template <int U>
-__device__ __forceinline__ int block_type(int type) { return U == ANY ? type : EMC2_BF16; }
+__device__ __forceinline__ int block_type(int type) { return U == ANY ? type : U == F16_ROWS ? EMC2_F16 : EMC2_BF16; }
 
 struct ResArgs {
     RowSegments seg;
@@ -278,7 +280,7 @@ struct ResGradArgs {
     float* part;                             // [gridDim.x + E][4][C]: S2, S1, dw', db' of a CTA's rows of an expert
     int* share;                              // [E][2]: first CTA with rows of the expert and the one behind the last
     float inv_c;
-    int nvec, lanes, type_x, type_f, type_y; // lanes of a row, any number up to 32
+    int nvec, lanes, type_x, type_f, type_y; // lanes of a row, any number; more than 32 across a CTA
 };
 
 // Sums of N values over the lanes of a row's group, `l` a lane's place in it and `base` the warp's lane of its first; every
@@ -303,6 +305,27 @@ __device__ __forceinline__ void group_sums(float (&v)[N], int lanes, int l, int 
     }
 #pragma unroll
     for (int i = 0; i < N; ++i) v[i] = __shfl_sync(0xFFFFFFFFu, v[i], base);
+}
+
+// The same over a CTA, by way of `meet` [warps][N], which nobody reads behind the next barrier.
+template <int N>
+__device__ __forceinline__ void cta_sums(float (&v)[N], float (*meet)[6]) {
+#pragma unroll
+    for (int d = 16; d; d >>= 1) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(0xFFFFFFFFu, v[i], d);
+    }
+    if ((threadIdx.x & 31) == 0) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) meet[threadIdx.x >> 5][i] = v[i];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = meet[0][i];
+    for (int w = 1; w < (int)blockDim.x / 32; ++w) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] += meet[w][i];
+    }
 }
 
 // The run of rows that a CTA has, as a part of all rows expert by expert.  The first CTA notes which CTAs have rows of an expert.
@@ -357,60 +380,74 @@ __device__ __forceinline__ void copy_bytes(uint32_t dst, const void* src, uint32
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
 }
 
-// Rows of up to 256 channels, eight per lane.  The rows are taken expert by expert, an equal run of them per CTA, which sums its rows of an
+// Rows with eight channels per lane: several in a warp, or (ACROSS, more than 256 channels) one across two to four warps, a CTA, whose sums
+// meet in shared memory.  The rows are taken expert by expert, an equal run of them per CTA, which sums its rows of an
 // expert before it goes to the next; entry i + e of `part` holds those of CTA i and expert e (along the run of all rows either i or e
 // goes up, so no two share one).  The sums stay in registers; a group of lanes has two rows in work, whose waits for one another's lanes
-// and for shared memory fill each other.  The warp's next rows, which lie side by side within a frame, are on their way to shared memory, for
+// and for shared memory fill each other.  The next rows, which lie side by side within a frame, are on their way to shared memory, for
 // which no registers are left, as one piece of every buffer (lane by lane, the copies' own way through the SM's memory pipe was what the kernel
 // waited for: 147 us instead of 109).  Rows of four channels more than a multiple of eight need not begin on 16 bytes: their lanes copy their
 // own.  480,000 rows of 64 fp32 channels, a tenth dropped: 109 us, 5.2 TB/s, with half of the issue slots of few warps, which the registers of sums and
-// rows allow; 90,000 of 256 bf16 channels: 66 us.
-constexpr int kNarrowThreads = 128;
-constexpr int narrow_ctas(bool wide) { return wide ? 3 : 2; }        // per SM, as the registers have room
-constexpr uint32_t kNarrowSlot = kNarrowThreads * 16;
-template <bool WIDE, int U, bool DROP>
-__global__ void __launch_bounds__(kNarrowThreads, narrow_ctas(WIDE)) residual_grad_kernel(ResGradArgs a) {
-    constexpr int kWarps = kNarrowThreads / 32;
+// rows allow; 90,000 of 256 bf16 channels: 65 us; 28,000 of 1,024 fp32 channels 93 us, 5.6 TB/s (with a warp per row and its sums in shared memory
+// 153), 60,000 of 512 bf16 channels 87 us (164).
+constexpr int kGradThreads = 128;
+// Ragged rows, and unusual calls across a CTA, have one row in work, and the registers for four CTAs: 120,000 rows of 132 bf16 channels 169 us, with
+// two rows and two CTAs 222; 28,000 of 772, fp32, 138 and 177.  Others have two: 120,000 of 72, fp16 without kernels of its own, 64, with one 71.
+__host__ __device__ constexpr int rows_at_once(bool wide, int usual, bool across) { return usual || (wide && !across) ? 2 : 1; }
+constexpr int grad_ctas(bool wide, int usual, bool across) { return rows_at_once(wide, usual, across) == 1 ? 4 : 3; }      // per SM, as the registers have room
+constexpr uint32_t kGradSlot = kGradThreads * 16;
+template <bool WIDE, int U, bool DROP, bool ACROSS>
+__global__ void __launch_bounds__(kGradThreads, grad_ctas(WIDE, U, ACROSS)) residual_grad_kernel(ResGradArgs a) {
+    constexpr int R = rows_at_once(WIDE, U, ACROSS);
+    constexpr int kTeams = ACROSS ? 1 : kGradThreads / 32;      // that have rows of their own: warps, or the CTA
     __shared__ int bounds[kMaxBounds];
     __shared__ int start[kMaxSegments + 1];
     __shared__ int run[2];
-    __shared__ float4 folded[kFolded - 1][64];                    // the expert's s w, s b and w'
-    __shared__ __align__(8) unsigned long long bars[kWarps][2];
+    __shared__ float4 folded[kFolded - 1][ACROSS ? 256 : 64];                    // the expert's s w, s b and w'
+    __shared__ __align__(8) unsigned long long bars[kTeams][2];
+    __shared__ float meet[ACROSS ? 2 : 1][kGradThreads / 32][6];
     __shared__ int gave_up;
-    extern __shared__ float4 sums[];         // [warps][4][nvec], then two stages of two rows per group
+    extern __shared__ float4 sums[];         // [teams][4][nvec], then two stages of two rows per group; across a CTA the latter only
     if (!take_run(a, bounds, start, run)) return;
     const int B = a.seg.B, E = a.seg.E;
     const int type_x = rows_type<U>(a.type_x), type_f = block_type<U>(a.type_f), type_y = block_type<U>(a.type_y);
-    const int lanes = a.lanes, warp = threadIdx.x >> 5, per_warp = 32 / lanes, chunk = 2 * per_warp;
-    const int sub = (threadIdx.x & 31) / lanes, base = sub * lanes, l = (threadIdx.x & 31) - base;
+    const int lanes = a.lanes, team = ACROSS ? 0 : threadIdx.x >> 5, per_warp = ACROSS ? 1 : 32 / lanes, chunk = R * per_warp;
+    auto in_team = [] { return (int)(ACROSS ? threadIdx.x : threadIdx.x & 31); };
+    // Threads behind the last lane of a row that takes warps read what that one reads, and count as zeros.
+    const int sub = ACROSS ? 0 : in_team() / lanes, base = sub * lanes, l = ACROSS ? min(in_team(), lanes - 1) : in_team() - base;
+    const bool lane_in = !ACROSS || in_team() < lanes;
+    auto team_sync = [] {
+        if (ACROSS) __syncthreads();
+        else __syncwarp();
+    };
     const bool pre = U || a.par.p[PRE_W] != nullptr, post = U || a.par.p[POST_W] != nullptr, behind = U || a.dout, noted = U || a.stats;
-    const bool drop = U ? DROP : a.drop.any != 0, active = sub < per_warp, hi = WIDE || 2 * l + 1 < a.nvec;
+    const bool drop = U ? DROP : a.drop.any != 0, active = ACROSS ? lane_in : sub < per_warp, hi = WIDE || 2 * l + 1 < a.nvec;
     DropoutSeed seed = {};
     if (drop) seed = dropout_seed(a.drop);
     // Bytes of a row in each buffer, and where a stage of the warp has the buffer's rows; with copies by lanes, where it has a lane's
     // vectors, which are 16 bytes at the thread's number.
     auto slots = [](int type) { return type == EMC2_F32 ? 2u : 1u; };
     const uint32_t row_x = slots(type_x) * a.nvec * 8, row_y = slots(type_y) * a.nvec * 8, row_f = slots(type_f) * a.nvec * 8;
-    const uint32_t at_y = pre ? (WIDE ? chunk * row_x : slots(type_x) * kNarrowSlot) : 0u;
-    const uint32_t at_d = at_y + (pre ? (WIDE ? chunk * row_y : slots(type_y) * kNarrowSlot) : 0u);
-    const uint32_t at_f = at_d + (behind ? (WIDE ? chunk * row_x : slots(type_x) * kNarrowSlot) : 0u);
-    const uint32_t at_s = at_f + (WIDE ? chunk * row_f : slots(type_f) * kNarrowSlot);
-    const uint32_t row_bytes = at_s + (noted ? (WIDE ? chunk * 16 : kNarrowSlot) : 0u);      // of a stage of the warp; by lanes, of a row
-    const uint32_t ring_at = smem_u32(sums + kWarps * 4 * a.nvec) + (WIDE ? warp * 2 * row_bytes : threadIdx.x * 16), bar = smem_u32(bars[warp]);
+    const uint32_t at_y = pre ? (WIDE ? chunk * row_x : slots(type_x) * kGradSlot) : 0u;
+    const uint32_t at_d = at_y + (pre ? (WIDE ? chunk * row_y : slots(type_y) * kGradSlot) : 0u);
+    const uint32_t at_f = at_d + (behind ? (WIDE ? chunk * row_x : slots(type_x) * kGradSlot) : 0u);
+    const uint32_t at_s = at_f + (WIDE ? chunk * row_f : slots(type_f) * kGradSlot);
+    const uint32_t row_bytes = at_s + (noted ? (WIDE ? chunk * 16 : kGradSlot) : 0u);      // of a stage of the warp; by lanes, of a row
+    const uint32_t ring_at = smem_u32(sums + (ACROSS ? 0 : kTeams * 4 * a.nvec)) + (WIDE ? team * 2 * row_bytes : threadIdx.x * 16), bar = smem_u32(bars[team]);
     if (WIDE) {
         if (threadIdx.x == 0) gave_up = 0;
-        if ((threadIdx.x & 31) == 0) { bar_init(bar, 1); bar_init(bar + 8, 1); }
+        if (in_team() == 0) { bar_init(bar, 1); bar_init(bar + 8, 1); }
         fence_bar_init();
         fence_async_shared();
         __syncthreads();
     }
-    const bool leads = (threadIdx.x & 31) == 0;
+    const bool leads = in_team() == 0;
     const int place = min(sub, per_warp - 1);                     // lanes behind the last group read its row, for nothing
     uint32_t phases = 0;
     for (int e = segment_of(start, B * E, run[0]) / B; e < E && start[e * B] < run[1]; ++e) {
         const int from = max(run[0], start[e * B]), to = min(run[1], start[(e + 1) * B]);
         if (from >= to) continue;
-        for (int v = threadIdx.x; v < a.nvec; v += kNarrowThreads)
+        for (int v = threadIdx.x; v < a.nvec; v += blockDim.x)
             for (int i = SIDE_W; i <= NEXT_W; ++i) folded[i][v] = folded_param(a.par, i, e * a.nvec + v);
         __syncthreads();
         auto param8 = [&](float (&f)[8], int i) {
@@ -426,17 +463,17 @@ __global__ void __launch_bounds__(kNarrowThreads, narrow_ctas(WIDE)) residual_gr
 #pragma unroll
             for (int j = 0; j < 8; ++j) acc[i][j] = 0.f;
         RowAt row_at(a, bounds, start, e), ahead_at(a, bounds, start, e);
-        uint32_t next[2] = {0u, 0u};                              // rows under way; with copies by lanes
+        uint32_t next[R] = {};                              // rows under way; with copies by lanes
         // The warp's rows from place p on; a lane's are p + sub and p + per_warp + sub.
         auto request = [&](int p, uint32_t stage) {
-            uint32_t dst = ring_at + stage * (WIDE ? row_bytes : 2 * row_bytes);
+            uint32_t dst = ring_at + stage * (WIDE ? row_bytes : R * row_bytes);
             if (WIDE) {
                 uint32_t dst_y = dst + at_y, dst_d = dst + at_d, dst_f = dst + at_f, dst_s = dst + at_s;
                 if (p >= to) return;
                 const int end = min(p + chunk, to);
                 if (end - p < chunk) {                            // places without a row are zeros, which add nothing
                     auto clear = [&](uint32_t buffer, uint32_t bytes) {
-                        for (uint32_t o = (uint32_t)(end - p) * bytes + (threadIdx.x & 31) * 16; o < chunk * bytes; o += 512)
+                        for (uint32_t o = (uint32_t)(end - p) * bytes + in_team() * 16; o < chunk * bytes; o += (ACROSS ? blockDim.x : 32) * 16)
                             asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(buffer + o), "r"(0u) : "memory");
                     };
                     if (pre) {
@@ -447,7 +484,7 @@ __global__ void __launch_bounds__(kNarrowThreads, narrow_ctas(WIDE)) residual_gr
                     clear(dst_f, row_f);
                     if (noted) clear(dst_s, 16);
                     fence_async_shared();                         // before the next expert's copies
-                    __syncwarp();
+                    team_sync();
                 }
                 if (!leads) return;
                 const uint32_t full = bar + stage * 8;
@@ -471,40 +508,43 @@ __global__ void __launch_bounds__(kNarrowThreads, narrow_ctas(WIDE)) residual_gr
                 return;
             }
 #pragma unroll
-            for (int k = 0; k < 2; ++k, dst += row_bytes) {
+            for (int k = 0; k < R; ++k, dst += row_bytes) {
                 const int q = p + k * per_warp + sub;
                 if (q >= to || !active) continue;
                 const uint32_t row = next[k] = ahead_at(q);
                 const uint32_t at = row * (uint32_t)a.nvec + 2 * l;             // 2^24 rows of 64 vectors at most
                 if (pre) {
-                    ahead8<WIDE, kNarrowSlot>(dst, a.o, at, hi, type_x);
-                    ahead8<WIDE, kNarrowSlot>(dst + at_y, a.dy, at, hi, type_y);
+                    ahead8<WIDE, kGradSlot>(dst, a.o, at, hi, type_x);
+                    ahead8<WIDE, kGradSlot>(dst + at_y, a.dy, at, hi, type_y);
                 }
-                if (behind) ahead8<WIDE, kNarrowSlot>(dst + at_d, a.dout, at, hi, type_x);
-                ahead8<WIDE, kNarrowSlot>(dst + at_f, a.f, at, hi, type_f);
+                if (behind) ahead8<WIDE, kGradSlot>(dst + at_d, a.dout, at, hi, type_x);
+                ahead8<WIDE, kGradSlot>(dst + at_f, a.f, at, hi, type_f);
                 if (noted) copy_ahead<16>(dst + at_s, a.stats + row);
             }
             asm volatile("cp.async.commit_group;" ::: "memory");
         };
         uint32_t stage = 0;
-        __syncwarp();
-        request(from + warp * chunk, 0);
-        for (int p = from + warp * chunk; p < to; p += kWarps * chunk) {
-            const bool in[2] = {active && p + sub < to, active && p + per_warp + sub < to};
-            uint32_t row[2];
-            float gate[2];
+        team_sync();
+        request(from + team * chunk, 0);
+        for (int p = from + team * chunk; p < to; p += kTeams * chunk) {
+            bool in[R];
+            uint32_t row[R];
+            float gate[R];
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
+            for (int k = 0; k < R; ++k) {
+                in[k] = active && p + k * per_warp + sub < to;
                 row[k] = !WIDE ? next[k] : in[k] ? row_at(p + k * per_warp + sub) : 0u;
                 gate[k] = in[k] && a.gate ? __ldg(a.gate + row[k]) : 1.0f;
             }
             const uint32_t now = stage;
-            const uint32_t at = ring_at + stage * (WIDE ? row_bytes : 2 * row_bytes);
+            const uint32_t at = ring_at + stage * (WIDE ? row_bytes : R * row_bytes);
             stage ^= 1;
-            request(p + kWarps * chunk, stage);
-            uint4 bits[2];
+            request(p + kTeams * chunk, stage);
+            uint4 bits[R];
             if (drop) {                                           // while the rows are on their way
-                const uint32_t group[2] = {(uint32_t)l, (uint32_t)l};
+                uint32_t group[R];
+#pragma unroll
+                for (int k = 0; k < R; ++k) group[k] = (uint32_t)l;
                 dropout_bits(bits, seed, row, group);
             }
             if (WIDE) {
@@ -513,8 +553,8 @@ __global__ void __launch_bounds__(kNarrowThreads, narrow_ctas(WIDE)) residual_gr
             } else {
                 asm volatile("cp.async.wait_group 1;" ::: "memory");
             }
-            float d[2][8], h[2][8];
-            float4 st[2];
+            float d[R][8], h[R][8];
+            float4 st[R];
             auto taken = [&](float (&f)[8], int k, uint32_t buffer, uint32_t bytes, int type) {
                 Raw8 raw;
                 if (WIDE) {
@@ -525,14 +565,14 @@ __global__ void __launch_bounds__(kNarrowThreads, narrow_ctas(WIDE)) residual_gr
                     raw.a = raw.b = make_uint4(0u, 0u, 0u, 0u);
                     if (in[k]) {
                         raw.a = lds128(at + k * row_bytes + buffer);
-                        if (type == EMC2_F32) raw.b = lds128(at + k * row_bytes + buffer + kNarrowSlot);
+                        if (type == EMC2_F32) raw.b = lds128(at + k * row_bytes + buffer + kGradSlot);
                     }
                     if (!hi) clear_second(raw, type);
                 }
                 floats8(f, raw, type);
             };
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
+            for (int k = 0; k < R; ++k) {
                 st[k] = make_float4(0.f, 1.f, 0.f, 1.f);
                 if (noted && (WIDE || in[k])) {
                     const uint4 v = lds128(WIDE ? at + at_s + (uint32_t)(k * per_warp + place) * 16 : at + k * row_bytes + at_s);
@@ -544,35 +584,37 @@ __global__ void __launch_bounds__(kNarrowThreads, narrow_ctas(WIDE)) residual_gr
                 taken(h[k], k, at_f, row_f, type_f);
             }
             if (pre) {
-                float o[2][8], g[2][8], w[8], means[4] = {0.f, 0.f, 0.f, 0.f};
+                float o[R][8], g[R][8], w[8], means[2 * R] = {};
                 param8(w, NEXT_W);
 #pragma unroll
-                for (int k = 0; k < 2; ++k) {
+                for (int k = 0; k < R; ++k) {
                     taken(o[k], k, 0, row_x, type_x);
                     taken(g[k], k, at_y, row_y, type_y);
 #pragma unroll
                     for (int j = 0; j < 8; ++j) {
                         o[k][j] = (o[k][j] - st[k].z) * st[k].w;
                         if (!WIDE && j >= 4 && !hi) o[k][j] = 0.f;
+                        if (ACROSS && !lane_in) o[k][j] = g[k][j] = 0.f;
                         acc[2][j] += g[k][j] * o[k][j];
                         acc[3][j] += g[k][j];
                         g[k][j] *= w[j];
                         means[k] += g[k][j];
-                        means[2 + k] += g[k][j] * o[k][j];
+                        means[R + k] += g[k][j] * o[k][j];
                     }
                 }
-                group_sums(means, lanes, l, base);
+                if (ACROSS) cta_sums(means, meet[0]);
+                else group_sums(means, lanes, l, base);
 #pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    const float m = means[k] * a.inv_c, t = means[2 + k] * a.inv_c;
+                for (int k = 0; k < R; ++k) {
+                    const float m = means[k] * a.inv_c, t = means[R + k] * a.inv_c;
 #pragma unroll
                     for (int j = 0; j < 8; ++j) d[k][j] += st[k].w * ((g[k][j] - m) - o[k][j] * t);
                 }
             }
-            float w[8], means[6] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+            float w[8], means[3 * R] = {};
             param8(w, SIDE_W);
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
+            for (int k = 0; k < R; ++k) {
                 if (in[k]) store8<WIDE>(a.dx, (size_t)row[k] * a.nvec + 2 * l, hi, d[k], type_x);
                 // What is dropped passes nothing on, whatever it holds; behind a norm no element of a row with NaN or infinities has a
                 // value.
@@ -591,17 +633,21 @@ __global__ void __launch_bounds__(kNarrowThreads, narrow_ctas(WIDE)) residual_gr
 #pragma unroll
                     for (int j = 4; j < 8; ++j) d[k][j] = h[k][j] = 0.f;
                 }
+                if (ACROSS && !lane_in) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) d[k][j] = h[k][j] = 0.f;
+                }
             }
             if (a.dgate) {
                 float c[8];
                 param8(c, SIDE_B);
 #pragma unroll
-                for (int k = 0; k < 2; ++k)
+                for (int k = 0; k < R; ++k)
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) means[4 + k] += d[k][j] * (h[k][j] * w[j] + c[j]);
+                    for (int j = 0; j < 8; ++j) means[2 * R + k] += d[k][j] * (h[k][j] * w[j] + c[j]);
             }
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
+            for (int k = 0; k < R; ++k) {
                 const float through = drop ? a.drop.factor * gate[k] : gate[k];
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
@@ -610,25 +656,38 @@ __global__ void __launch_bounds__(kNarrowThreads, narrow_ctas(WIDE)) residual_gr
                     acc[0][j] += d[k][j] * h[k][j];
                     d[k][j] *= w[j];
                     means[k] += d[k][j];
-                    means[2 + k] += d[k][j] * h[k][j];
+                    means[R + k] += d[k][j] * h[k][j];
                 }
             }
-            if (post || a.dgate) group_sums(means, lanes, l, base);
+            if (post || a.dgate) {
+                if (ACROSS) cta_sums(means, meet[ACROSS]);
+                else group_sums(means, lanes, l, base);
+            }
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
+            for (int k = 0; k < R; ++k) {
                 if (!in[k]) continue;
-                if (a.dgate && l == 0) a.dgate[row[k]] = drop ? means[4 + k] * a.drop.factor : means[4 + k];
+                if (a.dgate && l == 0) a.dgate[row[k]] = drop ? means[2 * R + k] * a.drop.factor : means[2 * R + k];
                 if (post) {
-                    const float m = means[k] * a.inv_c, t = means[2 + k] * a.inv_c;
+                    const float m = means[k] * a.inv_c, t = means[R + k] * a.inv_c;
 #pragma unroll
                     for (int j = 0; j < 8; ++j) d[k][j] = st[k].y * ((d[k][j] - m) - h[k][j] * t);
                 }
                 store8<WIDE>(a.df, (size_t)row[k] * a.nvec + 2 * l, hi, d[k], type_f);
             }
-            __syncwarp();                                         // the stage has been read by all
+            team_sync();                                          // the stage has been read by all
+        }
+        if (ACROSS) {
+            float4* part = reinterpret_cast<float4*>(a.part) + (size_t)(blockIdx.x + e) * 4 * a.nvec + 2 * l;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (!lane_in) break;
+                part[i * a.nvec] = make_float4(acc[i][0], acc[i][1], acc[i][2], acc[i][3]);
+                if (hi) part[i * a.nvec + 1] = make_float4(acc[i][4], acc[i][5], acc[i][6], acc[i][7]);
+            }
+            continue;                                             // the rows of this expert are done with by all
         }
         // The groups of a warp hold the same columns at the same places.
-        float4* mine = sums + warp * 4 * a.nvec + 2 * l;
+        float4* mine = sums + team * 4 * a.nvec + 2 * l;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
 #pragma unroll
@@ -642,168 +701,10 @@ __global__ void __launch_bounds__(kNarrowThreads, narrow_ctas(WIDE)) residual_gr
                 if (hi) mine[i * a.nvec + 1] = make_float4(acc[i][4], acc[i][5], acc[i][6], acc[i][7]);
             }
         }
-        give_sums<kNarrowThreads>(a, sums, e);
+        give_sums<kGradThreads>(a, sums, e);
     }
     if (WIDE) leave_after_timeout(&gave_up);
     else asm volatile("cp.async.wait_group 0;" ::: "memory");
-}
-
-// Wider rows, K groups of eight channels per lane of a warp, whose values fill the registers: the sums are in shared memory, an entry per
-// warp and column that one lane adds to, and nothing is requested ahead: 60,000 rows of 512 bf16 channels take 167 us, of a floor of 56.
-template <int K, bool WIDE>
-__global__ void __launch_bounds__(kResThreads, 1) residual_grad_wide_kernel(ResGradArgs a) {
-    constexpr int kWarps = kResThreads / 32;
-    __shared__ int bounds[kMaxBounds];
-    __shared__ int start[kMaxSegments + 1];
-    __shared__ int run[2];
-    __shared__ float4 folded[kFolded - 1][64 * K];
-    extern __shared__ float4 sums[];         // [warps][4][nvec]
-    if (!take_run(a, bounds, start, run)) return;
-    const int B = a.seg.B, E = a.seg.E, type_x = a.type_x, type_f = a.type_f, type_y = a.type_y;
-    const int warp = threadIdx.x >> 5, l = threadIdx.x & 31;
-    const bool pre = a.par.p[PRE_W] != nullptr, post = a.par.p[POST_W] != nullptr, drop = a.drop.any != 0;
-    DropoutSeed seed = {};
-    if (drop) seed = dropout_seed(a.drop);
-    float4* mine = sums + warp * 4 * a.nvec;
-    for (int e = segment_of(start, B * E, run[0]) / B; e < E && start[e * B] < run[1]; ++e) {
-        const int from = max(run[0], start[e * B]), to = min(run[1], start[(e + 1) * B]);
-        if (from >= to) continue;
-        for (int v = threadIdx.x; v < a.nvec; v += kResThreads)
-            for (int i = SIDE_W; i <= NEXT_W; ++i) folded[i][v] = folded_param(a.par, i, e * a.nvec + v);
-        for (int v = threadIdx.x; v < kWarps * 4 * a.nvec; v += kResThreads) sums[v] = make_float4(0.f, 0.f, 0.f, 0.f);
-        __syncthreads();
-        auto param8 = [&](float (&f)[8], int i, int v, bool hi) {
-            const float4 x = folded[i][v];
-            float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (hi) y = folded[i][v + 1];
-            f[0] = x.x; f[1] = x.y; f[2] = x.z; f[3] = x.w;
-            f[4] = y.x; f[5] = y.y; f[6] = y.z; f[7] = y.w;
-        };
-        // t w to a sum, per channel.
-        auto add = [&](int plane, int v, bool hi, const float (&t)[8], const float (&w)[8]) {
-            float4* at = mine + plane * a.nvec + v;
-            float4 s = at[0];
-            at[0] = make_float4(s.x + t[0] * w[0], s.y + t[1] * w[1], s.z + t[2] * w[2], s.w + t[3] * w[3]);
-            if (!hi) return;
-            s = at[1];
-            at[1] = make_float4(s.x + t[4] * w[4], s.y + t[5] * w[5], s.z + t[6] * w[6], s.w + t[7] * w[7]);
-        };
-        const float ones[8] = {1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f};
-        RowAt row_at(a, bounds, start, e);
-        for (int p = from + warp; p < to; p += kWarps) {
-            const uint32_t row = row_at(p);
-            Raw8 ro[K], rf[K], rd[K], ry[K];
-#pragma unroll
-            for (int i = 0; i < K; ++i) {
-                const int v = 2 * (l + i * 32);
-                const bool lo = v < a.nvec, hi = v + 1 < a.nvec;
-                const size_t at = (size_t)row * a.nvec + v;
-                if (pre) {
-                    ro[i] = request8<WIDE>(a.o, at, lo, hi, type_x);
-                    ry[i] = request8<WIDE>(a.dy, at, lo, hi, type_y);
-                }
-                rd[i] = request8<WIDE>(a.dout, at, lo && a.dout, hi && a.dout, type_x);
-                rf[i] = request8<WIDE>(a.f, at, lo, hi, type_f);
-            }
-            const float4 st = a.stats ? __ldg(a.stats + row) : make_float4(0.f, 1.f, 0.f, 1.f);
-            const float gate = a.gate ? __ldg(a.gate + row) : 1.0f;
-            float d[K][8];
-#pragma unroll
-            for (int i = 0; i < K; ++i) floats8(d[i], rd[i], type_x);
-            if (pre) {
-                float o[K][8], g[K][8], means[2] = {0.f, 0.f};
-#pragma unroll
-                for (int i = 0; i < K; ++i) {
-                    const int v = 2 * (l + i * 32);
-                    floats8(o[i], ro[i], type_x);
-                    floats8(g[i], ry[i], type_y);
-                    if (v >= a.nvec) continue;
-                    const bool hi = WIDE || v + 1 < a.nvec;
-                    float w[8];
-                    param8(w, NEXT_W, v, hi);
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        o[i][j] = (o[i][j] - st.z) * st.w;
-                        if (!WIDE && j >= 4 && !hi) o[i][j] = 0.f;
-                    }
-                    add(3, v, hi, g[i], ones);
-                    add(2, v, hi, g[i], o[i]);
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        g[i][j] *= w[j];
-                        means[0] += g[i][j];
-                        means[1] += g[i][j] * o[i][j];
-                    }
-                }
-                group_sums(means, 32, l, 0);
-                const float m = means[0] * a.inv_c, t = means[1] * a.inv_c;
-#pragma unroll
-                for (int i = 0; i < K; ++i)
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) d[i][j] += st.w * ((g[i][j] - m) - o[i][j] * t);
-            }
-            float h[K][8], means[3] = {0.f, 0.f, 0.f};
-            const float through = drop ? a.drop.factor * gate : gate;
-#pragma unroll
-            for (int i = 0; i < K; ++i) {
-                const int v = 2 * (l + i * 32);
-                floats8(h[i], rf[i], type_f);
-                if (v >= a.nvec) continue;
-                const bool hi = WIDE || v + 1 < a.nvec;
-                store8<WIDE>(a.dx, (size_t)row * a.nvec + v, hi, d[i], type_x);
-                float w[8], c[8];
-                param8(w, SIDE_W, v, hi);
-                param8(c, SIDE_B, v, hi);
-                // As above.
-                if (drop) {
-                    uint4 bits[1];
-                    const uint32_t of[1] = {row}, group[1] = {(uint32_t)(l + i * 32)};
-                    dropout_bits(bits, seed, of, group);
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        d[i][j] = dropout_keeps(bits[0], j, a.drop.above) ? d[i][j] : 0.f;
-                        if (!post) h[i][j] = dropout_keeps(bits[0], j, a.drop.above) ? h[i][j] : 0.f;
-                    }
-                }
-                if (post) {
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) h[i][j] = (h[i][j] - st.x) * st.y;
-                }
-                if (!WIDE && !hi) {
-#pragma unroll
-                    for (int j = 4; j < 8; ++j) d[i][j] = h[i][j] = 0.f;
-                }
-                if (a.dgate) {
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) means[2] += d[i][j] * (h[i][j] * w[j] + c[j]);
-                }
-#pragma unroll
-                for (int j = 0; j < 8; ++j) d[i][j] *= through;
-                add(1, v, hi, d[i], ones);
-                add(0, v, hi, d[i], h[i]);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    d[i][j] *= w[j];
-                    means[0] += d[i][j];
-                    means[1] += d[i][j] * h[i][j];
-                }
-            }
-            if (post || a.dgate) group_sums(means, 32, l, 0);
-            if (a.dgate && l == 0) a.dgate[row] = drop ? means[2] * a.drop.factor : means[2];
-            const float m = means[0] * a.inv_c, t = means[1] * a.inv_c;
-#pragma unroll
-            for (int i = 0; i < K; ++i) {
-                const int v = 2 * (l + i * 32);
-                if (v >= a.nvec) continue;
-                if (post) {
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) d[i][j] = st.y * ((d[i][j] - m) - h[i][j] * t);
-                }
-                store8<WIDE>(a.df, (size_t)row * a.nvec + v, WIDE || v + 1 < a.nvec, d[i], type_f);
-            }
-        }
-        give_sums<kResThreads>(a, sums, e);
-    }
 }
 
 struct ResSumArgs {
@@ -867,11 +768,31 @@ struct Residual {
             return a.drop.any ? go(residual_kernel<K, true, F32_ROWS, true>, a, ctas, shared, st) : go(residual_kernel<K, true, F32_ROWS, false>, a, ctas, shared, st);
         if (usual == BF16_ROWS)
             return a.drop.any ? go(residual_kernel<K, true, BF16_ROWS, true>, a, ctas, shared, st) : go(residual_kernel<K, true, BF16_ROWS, false>, a, ctas, shared, st);
+        if (usual == F16_ROWS)
+            return a.drop.any ? go(residual_kernel<K, true, F16_ROWS, true>, a, ctas, shared, st) : go(residual_kernel<K, true, F16_ROWS, false>, a, ctas, shared, st);
         return wide ? go(residual_kernel<K, true, ANY, true>, a, ctas, shared, st) : go(residual_kernel<K, false, ANY, true>, a, ctas, shared, st);
     }
 };
-template <typename F>
-cudaError_t launch_grad(F kernel, const ResGradArgs& a, int ctas, int threads, size_t shared, size_t most, cudaStream_t st) {
+// Warps of a row of more than 256 channels, which a CTA then has one at a time; 1: a warp has one or more.
+int row_warps(int channels) { return (channels + 255) / 256; }
+template <bool ACROSS>
+cudaError_t launch_grad(const ResGradArgs& a, bool wide, int usual, int ctas, int threads, cudaStream_t st) {
+    auto slots = [](int type) { return type == EMC2_F32 ? 2 : 1; };
+    constexpr int teams = ACROSS ? 1 : kGradThreads / 32;
+    const bool pre = a.par.p[PRE_W] != nullptr;
+    const int n = (pre ? slots(a.type_x) + slots(a.type_y) : 0) + (a.dout ? slots(a.type_x) : 0) + slots(a.type_f);
+    const size_t own = ACROSS ? 0 : (size_t)teams * 4 * a.nvec * sizeof(float4);
+    // Two stages of two rows: per team of `chunk` rows, or per thread of its vectors and a row's statistics.
+    const size_t at_once = rows_at_once(wide, usual, ACROSS), chunk = ACROSS ? at_once : at_once * (32 / a.lanes);
+    const size_t stages = wide ? (size_t)teams * 2 * chunk * ((size_t)n * a.nvec * 8 + (a.stats ? 16 : 0)) : (size_t)2 * at_once * (n + (a.stats ? 1 : 0)) * kGradSlot;
+    const size_t shared = own + stages;
+    // 16 KB of sums and the stages of four fp32 buffers: of lanes' vectors 9 slots, of rows 64 of 144 bytes per warp (eight channels) at most;
+    // across a CTA rows of 16 KB, two at once, two stages, and no sums.
+    constexpr size_t most = 16 * 1024 + std::max<size_t>(4 * 9 * kGradSlot, 8 * 64 * 144);
+    auto kernel = wide ? residual_grad_kernel<true, ANY, true, ACROSS> : residual_grad_kernel<false, ANY, true, ACROSS>;
+    if (usual == F32_ROWS) kernel = a.drop.any ? residual_grad_kernel<true, F32_ROWS, true, ACROSS> : residual_grad_kernel<true, F32_ROWS, false, ACROSS>;
+    if (usual == BF16_ROWS) kernel = a.drop.any ? residual_grad_kernel<true, BF16_ROWS, true, ACROSS> : residual_grad_kernel<true, BF16_ROWS, false, ACROSS>;
+    if (usual == F16_ROWS) kernel = a.drop.any ? residual_grad_kernel<true, F16_ROWS, true, ACROSS> : residual_grad_kernel<true, F16_ROWS, false, ACROSS>;
     if (shared > 24 * 1024) {
         const cudaError_t e = allow_shared(kernel, most);
         if (e != cudaSuccess) return e;
@@ -879,30 +800,12 @@ cudaError_t launch_grad(F kernel, const ResGradArgs& a, int ctas, int threads, s
     kernel<<<ctas, threads, shared, st>>>(a);
     return cudaSuccess;
 }
-cudaError_t launch_narrow(const ResGradArgs& a, bool wide, int usual, int ctas, cudaStream_t st) {
-    auto slots = [](int type) { return type == EMC2_F32 ? 2 : 1; };
-    const bool pre = a.par.p[PRE_W] != nullptr;
-    const int n = (pre ? slots(a.type_x) + slots(a.type_y) : 0) + (a.dout ? slots(a.type_x) : 0) + slots(a.type_f);
-    const size_t own = (size_t)(kNarrowThreads / 32) * 4 * a.nvec * sizeof(float4);
-    // Two stages of two rows: per warp of `chunk` rows, or per thread of its vectors and a row's statistics.
-    const size_t chunk = 2 * (32 / a.lanes);
-    const size_t stages = wide ? (size_t)(kNarrowThreads / 32) * 2 * chunk * ((size_t)n * a.nvec * 8 + (a.stats ? 16 : 0)) : (size_t)4 * (n + (a.stats ? 1 : 0)) * kNarrowSlot;
-    const size_t shared = own + stages;
-    // 16 KB of sums and the stages of four fp32 buffers: of lanes' vectors 9 slots, of rows 64 of 144 bytes per warp (eight channels) at most.
-    constexpr size_t most = 16 * 1024 + std::max<size_t>(4 * 9 * kNarrowSlot, 8 * 64 * 144);
-    auto kernel = wide ? residual_grad_kernel<true, ANY, true> : residual_grad_kernel<false, ANY, true>;
-    if (usual == F32_ROWS) kernel = a.drop.any ? residual_grad_kernel<true, F32_ROWS, true> : residual_grad_kernel<true, F32_ROWS, false>;
-    if (usual == BF16_ROWS) kernel = a.drop.any ? residual_grad_kernel<true, BF16_ROWS, true> : residual_grad_kernel<true, BF16_ROWS, false>;
-    return launch_grad(kernel, a, ctas, kNarrowThreads, shared, most, st);
-}
-template <int K>
-cudaError_t launch_wide(const ResGradArgs& a, bool wide, int ctas, cudaStream_t st) {
-    constexpr int warps = kResThreads / 32;
-    return launch_grad(wide ? residual_grad_wide_kernel<K, true> : residual_grad_wide_kernel<K, false>, a, ctas, kResThreads,
-                       (size_t)warps * 4 * a.nvec * sizeof(float4), (size_t)warps * 4 * 64 * K * sizeof(float4), st);
-}
 
-int residual_grad_ctas(const emc2_bridge* h, int per, bool wide) { return (per == 1 ? narrow_ctas(wide) : 1) * h->num_sms; }
+// As many as the registers have room for.
+int residual_grad_ctas(const emc2_bridge* h, int warps, bool wide, int usual) {
+    const int full = grad_ctas(wide, usual, warps > 1);         // of kGradThreads
+    return (warps == 1 ? full : full * (kGradThreads / 32) / warps) * h->num_sms;
+}
 constexpr int kShareInts = 64;               // 2 * EMC2_MAX_EXPERTS and up to a multiple of 256 bytes
 
 int check_residual(const emc2_bridge* h, int B, int N, int channels, int type_x, int type_f, int type_y, const void* f, const int32_t* offsets,
@@ -921,7 +824,7 @@ int check_residual(const emc2_bridge* h, int B, int N, int channels, int type_x,
 }  // namespace
 
 size_t residual_scratch_bytes(const emc2_bridge* h, int max_channels) {
-    return kShareInts * sizeof(int) + (size_t)(residual_grad_ctas(h, 1, true) + EMC2_MAX_EXPERTS) * 4 * max_channels * sizeof(float);
+    return kShareInts * sizeof(int) + (size_t)(residual_grad_ctas(h, 2, true, ANY) + EMC2_MAX_EXPERTS) * 4 * max_channels * sizeof(float);
 }
 
 }  // namespace emc2
@@ -1028,23 +931,17 @@ extern "C" int emc2_expert_residual_grad(emc2_bridge_t* h, int32_t B, int32_t N,
     a.part = reinterpret_cast<float*>(a.share + kShareInts);
     a.inv_c = 1.0f / (float)channels; a.nvec = channels / 4; a.type_x = type_x; a.type_f = type_f; a.type_y = type_y;
     t.part = a.part; t.share = a.share;
-    const int groups = (channels + 7) / 8, per = (groups + 31) / 32;
-    a.lanes = std::min(groups, 32);
+    const int warps = row_warps(channels);
+    a.lanes = (channels + 7) / 8;
     const bool wide = is_wide(channels, type_x, d_grad_x) && is_wide(channels, type_f, d_f) && is_wide(channels, type_f, d_grad_f) &&
                       (!d_grad_out || is_wide(channels, type_x, d_grad_out)) &&
                       (!d_pre_weight || (is_wide(channels, type_x, d_out) && is_wide(channels, type_y, d_grad_y)));
-    const long long rows = (long long)B * N, per_cta = per == 1 ? 2 * (kNarrowThreads / 32) * (32 / a.lanes) : kResThreads / 32;
-    const int ctas = (int)std::min<long long>((rows + per_cta - 1) / per_cta, residual_grad_ctas(h, per, wide));
+    const long long rows = (long long)B * N, per_cta = warps == 1 ? 2 * (kGradThreads / 32) * (32 / a.lanes) : 4;
     const int usual = wide && d_post_weight && d_pre_weight && d_grad_out ? usual_of(type_x, type_f, type_y) : ANY;
+    const int ctas = (int)std::min<long long>((rows + per_cta - 1) / per_cta, residual_grad_ctas(h, warps, wide, usual));
     {
         LaunchScope ls(h, K_RESIDUAL_GRAD, st);
-        cudaError_t e;
-        switch (per) {
-            case 1: e = launch_narrow(a, wide, usual, ctas, st); break;
-            case 2: e = launch_wide<2>(a, wide, ctas, st); break;
-            case 3: e = launch_wide<3>(a, wide, ctas, st); break;
-            default: e = launch_wide<4>(a, wide, ctas, st);
-        }
+        const cudaError_t e = warps == 1 ? launch_grad<false>(a, wide, usual, ctas, kGradThreads, st) : launch_grad<true>(a, wide, usual, ctas, warps * 32, st);
         if (e != cudaSuccess) return check_cuda(h, e);
     }
     {
