@@ -87,7 +87,7 @@ def test_a_captured_dropout_takes_new_seeds():
 
 # ------------------------------------------------------------------ residual
 SHAPES = [(1, 1, 4, 1), (1, 130, 64, 4), (3, 777, 80, 4), (2, 300, 1024, 3), (5, 64, 36, 16), (32, 33, 256, 2), (2, 41, 516, 5), (2, 60, 772, 2), (1, 9000, 8, 3),
-          (1, 777, 264, 4), (3, 401, 512, 2), (2, 333, 640, 3)]
+          (1, 777, 264, 4), (3, 401, 512, 2), (2, 333, 640, 3), (32, 5, 264, 16), (16, 40, 996, 16)]
 KINDS = {  # tx, tf, ty, parameters, gate, p
     "all, fp32 rows": (torch.float32, torch.bfloat16, torch.bfloat16, PARAMS, True, 0.1),
     "all, bf16": (torch.bfloat16, torch.bfloat16, torch.bfloat16, PARAMS, True, 0.0),
