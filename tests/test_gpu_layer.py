@@ -80,7 +80,7 @@ def test_quantise_borders(dtype):
 
 # ------------------------------------------------------------------ the layer
 SHAPES = [(1, 8, 8, 1, 1), (1, 256, 1024, 16, 2), (3, 80, 320, 8, 2), (128, 64, 96, 4, 2), (17, 1024, 72, 64, 8), (128, 40, 264, 256, 8), (5, 136, 8192, 2, 1), (64, 72, 1032, 3, 3),
-          (33, 264, 536, 1, 1), (2, 1024, 2048, 5, 4)]
+          (33, 264, 536, 1, 1), (2, 1024, 2048, 5, 4), (128, 72, 520, 2, 2), (101, 256, 1032, 3, 1), (128, 128, 264, 8, 3)]
 
 
 def problem(g, n, C, H, E, k, dtype):
