@@ -11,7 +11,7 @@
 // products, whose 16 rows are the rows at hand and whose 8 columns are the weights': a row of x more costs no more reading, and there are too
 // few of them for larger products to help.
 //
-// 128 rows of 1,024 channels, 4 of 32 experts of 4,096 units, bf16: 172 us, of which the weights' 805 MB take 123 at a copy's rate; in 4 bits 151
+// 128 rows of 1,024 channels, 4 of 32 experts of 4,096 units, bf16: 161 us, of which the weights' 805 MB take 123 at a copy's rate; in 4 bits 147
 // (33), with half of the issue slots and a third of the tensor pipe's.  One row of 256 channels, 2 of 16 experts of 1,024 units: 12.8.
 //
 // A logit is the sum of a sum in fp32 and of all that its roundings left (Ogita, Rump and Oishi, "Accurate sum and dot product", 2005), as if
@@ -364,9 +364,6 @@ struct LayerMaps {
     CUtensorMap w[3];
 };
 
-// A CTA's place: share of the hidden units (the third kernel's) in x, tile of its rows of weights in y, active expert and, within it, of the passes
-// over its rows in z.
-
 // Panels of the rows at hand, in two buffers, as the 16-byte registers of a product's lanes: [16 rows][8 blocks of 32 elements][2 halves]
 // [32 lanes].  A lane's vector has two words of row g and, between them, those of row g + 8.
 constexpr int kPanelBytes = kRowsAtOnce / 16 * kPanel / 32 * 2 * 512;
@@ -615,7 +612,7 @@ __device__ __forceinline__ void layer_rows(const LayerArgs& a, const LayerMaps& 
         for (int s = 0; s < per_cta; ++s)
             for (int c = warp; c < rows; c += kLayerWarps) {
                 const int at = (unit * per_cta + s) * 32 + lane;
-                if (at < M) a.part[((size_t)(int)blockIdx.x * (a.n * a.k) + pair0 + c) * a.C + at] = sum(s, c, lane);
+                if (at < M) a.part[((size_t)blockIdx.x * (a.n * a.k) + pair0 + c) * a.C + at] = sum(s, c, lane);
             }
         __syncthreads();
         return;
@@ -644,7 +641,8 @@ __device__ __forceinline__ void layer_rows(const LayerArgs& a, const LayerMaps& 
     __syncthreads();
 }
 
-// The rows of the CTA's expert, 32 at a time, against its weights.
+// The rows of the CTA's expert, 32 at a time, against its weights.  A CTA's place: share of the hidden units (the third kernel's) in x,
+// tile of its rows of weights in y, active expert and, within it, of the passes over its rows in z.
 template <int STAGE, bool MX, bool BF16, bool HALVES>
 __device__ __forceinline__ void layer_unit(const LayerArgs& a, const LayerMaps& maps, const Lists& lists, char* smem) {
     __shared__ __align__(8) unsigned long long bars[kLayerWarps][2];
