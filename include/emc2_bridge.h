@@ -453,8 +453,8 @@ int emc2_mx4_quantise(emc2_bridge_t* bridge, int32_t rows, int32_t channels, int
  *   d_w_gate, d_w_up  type [experts, hidden, channels]     d_w_down  type [experts, channels, hidden]; hidden a multiple of 8 up to 8192
  *   d_ids          int32 [n, choices]     d_weights  float [n, choices]: the chosen experts and p
  * Logits are within 2^-38 of the sum of their terms' sizes and 2^-138; of equal ones the lower expert is first, and NaN are behind all others.
- * Products are summed in fp32; act(g) * u goes into the last product as the sum of two numbers of the type where an expert has up to 16
- * rows of the call, else rounded to the type (in EMC2_F16 it has to stay below 65504); the result is rounded once. */
+ * Products are summed in fp32; act(g) * u goes into the last product as the sum of two numbers of the type (in EMC2_F16 it has to stay below
+ * 65504); the result is rounded once.  A row's results do not depend on the call's other rows but for the order in which fp32 sums are taken. */
 int emc2_expert_layer(emc2_bridge_t* bridge, int32_t n, int32_t channels, int32_t hidden, int32_t experts, int32_t choices, int32_t type,
                       int32_t act, const void* d_x, const int32_t* d_count, const float* d_w_router, const float* d_b_router,
                       const void* d_w_gate, const void* d_w_up, const void* d_w_down, void* d_y, int32_t* d_ids, float* d_weights,

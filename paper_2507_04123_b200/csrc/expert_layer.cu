@@ -11,13 +11,14 @@
 // products, whose 16 rows are the rows at hand and whose 8 columns are the weights': a row of x more costs no more reading, and there are too
 // few of them for larger products to help.
 //
-// 128 rows of 1,024 channels, 4 of 32 experts of 4,096 units, bf16: 161 us, of which the weights' 805 MB take 123 at a copy's rate; in 4 bits 147
+// 128 rows of 1,024 channels, 4 of 32 experts of 4,096 units, bf16: 169 us, of which the weights' 805 MB take 123 at a copy's rate; in 4 bits 165
 // (33), with half of the issue slots and a third of the tensor pipe's.  One row of 256 channels, 2 of 16 experts of 1,024 units: 12.8.
 //
 // A logit is the sum of a sum in fp32 and of all that its roundings left (Ogita, Rump and Oishi, "Accurate sum and dot product", 2005), as if
 // of twice the bits, so that the choice does not depend on an order of summation; 64-bit arithmetic took six times as long.  Products are
-// summed in fp32.  act(g) * u goes into the last product as the sum of two numbers of the type where an expert has up to 16 rows, whose
-// products have columns to spare, else rounded to one.  y is rounded once.
+// summed in fp32.  act(g) * u goes into the last product as the sum of two numbers of the type, so that a row keeps its bits whichever rows it
+// comes with: rounded to one where an expert has more than 16 rows, the layer of 128 rows took 162 us (146), and lost what that loses.  y is
+// rounded once.
 #include <algorithm>
 #include <atomic>
 
@@ -37,10 +38,15 @@ constexpr int kMaxChoices = 8;
 constexpr int kMaxSlots = kMaxLayerRows * kMaxChoices;     // pairs (row, choice)
 constexpr int kMaxLayerHidden = 8192;
 constexpr int kPanel = 256;                  // elements of the rows at hand in shared memory at a time
-constexpr int kRowsAtOnce = 32;
+enum Stage { HIDDEN = 0, DOWN };
+// Sixteens of a product's rows in a pass, at most, and the rows at hand that they are: a row of hidden values, in two parts, takes two.  Three of
+// hidden values are what shared memory and registers have room for.  With two: 184 us instead of 169 for the layer above, whose experts
+// have 16 rows on average, 175 instead of 165 in 4 bits; 33 instead of 37 where two experts of 512 channels and 2,048 units have 128 each.
+__host__ __device__ constexpr int pass_sixteens(int stage) { return stage == DOWN ? 3 : 2; }
+__host__ __device__ constexpr int rows_of_sixteen(int stage) { return stage == DOWN ? 8 : 16; }
+__host__ __device__ constexpr int pass_rows(int stage) { return pass_sixteens(stage) * rows_of_sixteen(stage); }
 constexpr int kMaxShares = 8;                // of the hidden units in the third kernel
 constexpr int kMaxTiles = 64;                // of channels, per counter
-constexpr int kTwoParts = 16;                // rows of an expert whose hidden values are held in two parts, at most
 constexpr int kLastAdds = 64;                // partial results of an output that the third kernel adds up itself, at most
 
 // What the kernels leave one another, on the device.
@@ -65,7 +71,7 @@ struct LayerArgs {
     float* weights;
     void* y;
     LayerNotes* notes;
-    void* hidden;                            // [sorted pair][2][H]
+    void* hidden;                            // [sorted pair][H / 8][32 bytes], see hidden_place
     float* part;                             // [share][sorted pair][C]
     int* status;
     int n, C, H, E, k, act;
@@ -78,6 +84,10 @@ struct LayerArgs {
 
 // Place of element i among eight, in the order that codes come in.
 __host__ __device__ __forceinline__ int ordered_place(int i) { return (i & 3) * 2 + (i >> 2); }
+
+// A hidden value is the sum of two of the type.  Where part q of value i (whose place among its eight is i % 8) of a pair of rows lies, in
+// values: eight are two 16-byte registers of a product's lanes, the parts in rows g and g + 8.
+__device__ __forceinline__ size_t hidden_place(int i, int q) { return (size_t)(i >> 3) * 16 + (i >> 2 & 1) * 8 + (i >> 1 & 1) * 4 + q * 2 + (i & 1); }
 
 // Numbers that ascend as the logits do; NaN below all.  0 is left for what has been taken.
 __device__ __forceinline__ unsigned long long logit_key(double v) {
@@ -356,8 +366,6 @@ __device__ __forceinline__ uint32_t block_factor(int below) {
     return h * 0x00010001u;
 }
 
-enum Stage { HIDDEN = 0, DOWN };
-
 // Weights as [experts * rows][elements or bytes of codes], in boxes of 128 bytes of 16 rows (gate, up) or 32 (down), whose vectors are
 // mixed with the row's number (the copies' swizzle); what lies behind a row reads as zeros.
 struct LayerMaps {
@@ -366,13 +374,13 @@ struct LayerMaps {
 
 // Panels of the rows at hand, in two buffers, as the 16-byte registers of a product's lanes: [16 rows][8 blocks of 32 elements][2 halves]
 // [32 lanes].  A lane's vector has two words of row g and, between them, those of row g + 8.
-constexpr int kPanelBytes = kRowsAtOnce / 16 * kPanel / 32 * 2 * 512;
+__host__ __device__ constexpr uint32_t panel_bytes(int stage) { return pass_sixteens(stage) * kPanel / 32 * 2 * 512; }
 // The warps' sums take the panels' place when the products are done: [warp][16 rows][32 rows of weights][16], the last index mixed with the
 // one before, so that writers and readers meet few of the same banks.
-static_assert(kLayerWarps * kRowsAtOnce * 32 * 4 <= 2 * kPanelBytes, "sums");
-// Behind them the ring: [stage][warp][32 rows][128 bytes], on 1,024 bytes.
+static_assert(kLayerWarps * pass_sixteens(DOWN) * 16 * 32 * 4 <= 2 * panel_bytes(DOWN) && kLayerWarps * pass_sixteens(HIDDEN) * 16 * 32 * 4 <= 2 * panel_bytes(HIDDEN), "sums");
+// Behind them the ring: [stage][warp][32 rows][128 bytes], on 128 bytes.  A third kernel's CTA has 112 KB: two fit an SM's 228.
 constexpr uint32_t kWarpStage = 32 * 128, kStage = kLayerWarps * kWarpStage;
-constexpr size_t kProductShared = 1024 + 2 * kPanelBytes + 2 * kStage;
+constexpr size_t product_shared(int stage) { return 2 * panel_bytes(stage) + 2 * kStage; }
 
 // The pairs sorted by expert, where the kernel has them.
 struct Lists {
@@ -395,9 +403,11 @@ struct Ring {
 // The weights of the next step are on their way to shared memory, in boxes that the warp alone reads: registers have no room for as much as the
 // memory needs to be asked for at once (50 KB per SM and more).
 template <int STAGE, bool MX, bool BF16, bool HALVES, int MT>
-__device__ __forceinline__ void layer_rows(const LayerArgs& a, const LayerMaps& maps, const Lists& lists, char* smem, Ring& wait, int e, int pair0, int rows, bool two) {
+__device__ __forceinline__ void layer_rows(const LayerArgs& a, const LayerMaps& maps, const Lists& lists, char* smem, Ring& wait, int e, int pair0, int rows) {
     constexpr int kPiece = MX ? 256 : 64;                         // elements of a step
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
+    int tid;                                                      // anew for every pass, as what follows from it: registers are short
+    asm volatile("mov.u32 %0, %%tid.x;" : "=r"(tid));
+    const int lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
     const int split_log = MX ? HALVES : a.split_log, split = 1 << split_log, per_cta = kLayerWarps >> split_log, part = warp & (split - 1), slot = warp >> split_log;
     const int K = STAGE == HIDDEN ? a.C : a.H, M = STAGE == HIDDEN ? a.H : a.C;
     const int unit = (int)blockIdx.y, tile = unit * per_cta + slot;        // of 16 hidden units, or of 32 channels
@@ -418,44 +428,63 @@ __device__ __forceinline__ void layer_rows(const LayerArgs& a, const LayerMaps& 
         for (int i = 0; i < 4; ++i)
 #pragma unroll
             for (int c = 0; c < 4; ++c) acc[m][i][c] = 0.f;
-    // A thread brings the vectors of rows g and g + 8 for its lane number and, in every 16 rows, the warp's block of a panel, through registers:
-    // their words change places.  Two parts of a hidden value stand in rows g and g + 8, whose sums the lane adds.
+    // A thread brings the vectors of its lane number and, in every 16 rows, the warp's block of a panel: of rows g and g + 8 of x through
+    // registers, where their words change places; hidden values, which lie as the products take them, by copies past the registers.  The
+    // two parts of one stand in rows g and g + 8, whose sums the lane adds.
     const uint32_t panels = (uint32_t)__cvta_generic_to_shared(smem);
     static_assert(kLayerWarps == kPanel / 32, "a block of a panel per warp");
     const int chunk = MX ? (warp & ~3) * 4 + t * 4 + (warp & 3) : warp * 4 + t;       // vector of a panel's row
-    const char* from[MT][2];
-#pragma unroll
-    for (int m = 0; m < MT; ++m)
-#pragma unroll
-        for (int q = 0; q < 2; ++q) {
-            const int r = two ? m * 8 + g : m * 16 + q * 8 + g;
-            from[m][q] = nullptr;
-            if (r >= rows) continue;
-            if (STAGE == HIDDEN) from[m][q] = static_cast<const char*>(a.x) + ((size_t)lists.row[pair0 + r] * a.C + chunk * 8) * 2;
-            else from[m][q] = static_cast<const char*>(a.hidden) + ((size_t)(2 * (pair0 + r) + (two ? q : 0)) * a.H + chunk * 8) * 2;
-        }
-    uint4 brought[MT][2];
-    auto bring = [&](int k) {
+    const char* from[MT][2];                                      // STAGE == HIDDEN
+    const int rows_left = rows - g;
+    const uint32_t values = (uint32_t)(pair0 + g) * 4 * a.H + chunk * 32;          // 1,024 pairs of 8,192 units at most
+    if (STAGE == HIDDEN) {
 #pragma unroll
         for (int m = 0; m < MT; ++m)
 #pragma unroll
             for (int q = 0; q < 2; ++q) {
-                brought[m][q] = make_uint4(0u, 0u, 0u, 0u);
-                if (from[m][q] && k + chunk * 8 < k1) brought[m][q] = *reinterpret_cast<const uint4*>(from[m][q] + 2 * k);
-                // Eight codes come as the pairs (0, 4), (1, 5), (2, 6), (3, 7); the hidden values lie in that order.
-                if (MX && STAGE == HIDDEN) {
-                    const uint4 v = brought[m][q];
-                    brought[m][q] = make_uint4(__byte_perm(v.x, v.z, 0x5410), __byte_perm(v.x, v.z, 0x7632), __byte_perm(v.y, v.w, 0x5410), __byte_perm(v.y, v.w, 0x7632));
-                }
+                const int r = m * 16 + q * 8 + g;
+                from[m][q] = r < rows ? static_cast<const char*>(a.x) + ((size_t)lists.row[pair0 + r] * a.C + chunk * 8) * 2 : nullptr;
             }
+    }
+    uint4 brought[MT][2];
+    // The panel from element k on is on its way from `bring` on, to the buffer at `to`, and there after `put` and a barrier.
+    auto bring = [&](int k, uint32_t to) {
+        if constexpr (STAGE == DOWN) {
+#pragma unroll
+            for (int m = 0; m < MT; ++m) {
+                const bool there = m * 8 < rows_left && k + chunk * 8 < k1;
+                const char* src = static_cast<const char*>(a.hidden) + (there ? values + (uint32_t)(m * 32 * a.H + k * 4) : 0u);
+                const uint32_t dst = to + (uint32_t)((m * (kPanel / 32) + warp) * 1024 + lane * 16), bytes = there ? 16u : 0u;       // the rest of 16 is zeros
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst + 512), "l"(src + 16), "r"(bytes) : "memory");
+            }
+            asm volatile("cp.async.commit_group;" ::: "memory");
+        } else {
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int q = 0; q < 2; ++q) {
+                    brought[m][q] = make_uint4(0u, 0u, 0u, 0u);
+                    if (from[m][q] && k + chunk * 8 < k1) brought[m][q] = *reinterpret_cast<const uint4*>(from[m][q] + 2 * k);
+                    // Eight codes come as the pairs (0, 4), (1, 5), (2, 6), (3, 7); the hidden values lie in that order.
+                    if (MX) {
+                        const uint4 v = brought[m][q];
+                        brought[m][q] = make_uint4(__byte_perm(v.x, v.z, 0x5410), __byte_perm(v.x, v.z, 0x7632), __byte_perm(v.y, v.w, 0x5410), __byte_perm(v.y, v.w, 0x7632));
+                    }
+                }
+        }
     };
     auto put = [&](uint32_t to) {
+        if constexpr (STAGE == DOWN) {
+            asm volatile("cp.async.wait_group 0;" ::: "memory");
+        } else {
 #pragma unroll
-        for (int m = 0; m < MT; ++m) {
-            const uint4 &u = brought[m][0], &v = brought[m][1];
-            const uint32_t at = to + (uint32_t)((m * (kPanel / 32) + warp) * 1024 + lane * 16);
-            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(u.x), "r"(v.x), "r"(u.y), "r"(v.y) : "memory");
-            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at + 512), "r"(u.z), "r"(v.z), "r"(u.w), "r"(v.w) : "memory");
+            for (int m = 0; m < MT; ++m) {
+                const uint4 &u = brought[m][0], &v = brought[m][1];
+                const uint32_t at = to + (uint32_t)((m * (kPanel / 32) + warp) * 1024 + lane * 16);
+                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(u.x), "r"(v.x), "r"(u.y), "r"(v.y) : "memory");
+                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at + 512), "r"(u.z), "r"(v.z), "r"(u.w), "r"(v.w) : "memory");
+            }
         }
     };
     auto rows_at = [&](uint32_t panel, int block, int m, int half) {
@@ -464,8 +493,10 @@ __device__ __forceinline__ void layer_rows(const LayerArgs& a, const LayerMaps& 
                      : "r"(panel + (uint32_t)((m * (kPanel / 32) + block) * 1024 + half * 512)));
         return v;
     };
+    constexpr uint32_t kPanelBytes = panel_bytes(STAGE);
     const uint32_t ring = panels + 2 * kPanelBytes + warp * kWarpStage;
-    const uint32_t mine = ring + row * 128 + ((t ^ row) << 4);    // of the step's second half: bit 6 the other way
+    // The copies mix a vector's number with bits 7 to 9 of its row's address.  Of the step's second half: bit 6 the other way.
+    const uint32_t mine = ring + row * 128 + ((t ^ ((ring >> 7) + row & 7)) << 4);
     // Warps that share a tile take every such step of it, with 4 bits either half of every step (whose weights they both have copied).
     const int stride = MX ? kPiece : kPiece << split_log, steps = (k1 - k0 + stride - 1) / stride, panel_log = MX ? 0 : 2 - split_log;      // steps of a panel
     const uint32_t lead = elected();
@@ -554,7 +585,7 @@ __device__ __forceinline__ void layer_rows(const LayerArgs& a, const LayerMaps& 
 #pragma unroll
     for (int s = 0; s < 2; ++s)
         if (s < steps) request(s, powers[s]);
-    bring(k0);
+    bring(k0, panels);
     put(panels);
     // Not unrolled: the products of several steps do not fit the instruction cache.
 #pragma unroll 1
@@ -562,7 +593,7 @@ __device__ __forceinline__ void layer_rows(const LayerArgs& a, const LayerMaps& 
         const int panel = s >> panel_log, in_panel = s & ((1 << panel_log) - 1), next = k0 + (panel + 1) * kPanel;
         if (in_panel == 0) {
             __syncthreads();                                      // the panel is there, and the other one is done with
-            if (next < k1) bring(next);
+            if (next < k1) bring(next, panels + ((panel & 1) ^ 1) * kPanelBytes);
         }
         const uint32_t stage = s & 1;
         warp_wait(wait.bars + stage * 8, wait.phases >> stage & 1u, wait.gave_up, a.status);
@@ -586,7 +617,7 @@ __device__ __forceinline__ void layer_rows(const LayerArgs& a, const LayerMaps& 
     }
     __syncthreads();                                              // the panels are done with; the warps that share a tile are added in their order
     float* sums = reinterpret_cast<float*>(smem);
-    const int held = two ? 8 : 16;                                // rows of every 16 that there are sums of
+    constexpr int kHeld = rows_of_sixteen(STAGE);
     auto sum_at = [&](int w, int m, int column, int r) { return ((w * MT + m) * 32 + column) * 16 + (r ^ (column >> 1)); };
 #pragma unroll
     for (int m = 0; m < MT; ++m)
@@ -595,7 +626,7 @@ __device__ __forceinline__ void layer_rows(const LayerArgs& a, const LayerMaps& 
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
                 const int column = i * 8 + t + 4 * c;                // the row of lanes with g = 2t + c
-                if (two) {
+                if (STAGE == DOWN) {
                     sums[sum_at(warp, m, column, g)] = acc[m][i][c] + acc[m][i][2 + c];
                 } else {
                     sums[sum_at(warp, m, column, g)] = acc[m][i][c];
@@ -605,7 +636,7 @@ __device__ __forceinline__ void layer_rows(const LayerArgs& a, const LayerMaps& 
     __syncthreads();
     auto sum = [&](int s, int c, int column) {
         float v = 0.f;
-        for (int q = 0; q < split; ++q) v += sums[sum_at(s * split + q, c / held, column, c % held)];
+        for (int q = 0; q < split; ++q) v += sums[sum_at(s * split + q, c / kHeld, column, c % kHeld)];
         return v;
     };
     if (STAGE == DOWN) {
@@ -624,18 +655,19 @@ __device__ __forceinline__ void layer_rows(const LayerArgs& a, const LayerMaps& 
         const float gate = sum(s, c, u), up = sum(s, c, 16 + u);
         const float f = a.act == EMC2_ACT_SILU ? gate / (1.0f + expf(-gate)) : 0.5f * gate * erfcf(-0.70710678f * gate);
         const float h = f * up;
-        const size_t to = (size_t)(2 * (pair0 + c)) * a.H + (MX ? (at & ~7) + ordered_place(at & 7) : at);
+        const int i = MX ? (at & ~7) + ordered_place(at & 7) : at;
+        const size_t pair = (size_t)(pair0 + c) * 2 * a.H, to = pair + hidden_place(i, 0), rest = pair + hidden_place(i, 1);
         // What the first part leaves is exact; an infinite one leaves nothing.
         if (BF16) {
-            __nv_bfloat16* p = static_cast<__nv_bfloat16*>(a.hidden) + to;
+            __nv_bfloat16* p = static_cast<__nv_bfloat16*>(a.hidden);
             const __nv_bfloat16 first = __float2bfloat16_rn(h);
-            p[0] = first;
-            p[a.H] = __float2bfloat16_rn(isinf(__bfloat162float(first)) ? 0.f : h - __bfloat162float(first));
+            p[to] = first;
+            p[rest] = __float2bfloat16_rn(isinf(__bfloat162float(first)) ? 0.f : h - __bfloat162float(first));
         } else {
-            __half* p = static_cast<__half*>(a.hidden) + to;
+            __half* p = static_cast<__half*>(a.hidden);
             const __half first = __float2half_rn(h);
-            p[0] = first;
-            p[a.H] = __float2half_rn(isinf(__half2float(first)) ? 0.f : h - __half2float(first));
+            p[to] = first;
+            p[rest] = __float2half_rn(isinf(__half2float(first)) ? 0.f : h - __half2float(first));
         }
     }
     __syncthreads();
@@ -652,7 +684,6 @@ __device__ __forceinline__ void layer_unit(const LayerArgs& a, const LayerMaps& 
         gave_up = 0;
         at_pass = (int)blockIdx.z % a.passes;
     }
-    smem += (1024 - (smem_u32(smem) & 1023)) & 1023;
     Ring ring = {smem_u32(bars[threadIdx.x >> 5]), 0u, &gave_up};
     if ((threadIdx.x & 31) == 0)
         for (int s = 0; s < 2; ++s) bar_init(ring.bars + s * 8, 1);
@@ -663,11 +694,13 @@ __device__ __forceinline__ void layer_unit(const LayerArgs& a, const LayerMaps& 
 #pragma unroll 1
     for (;;) {
         const int pass = at_pass, i = (int)blockIdx.z / a.passes, all = lists.start[i + 1] - lists.start[i];
-        if (pass * kRowsAtOnce >= all) break;
-        const bool two = STAGE == DOWN && all <= kTwoParts;
-        const int e = lists.expert[i], p = lists.start[i] + pass * kRowsAtOnce, rows = min(kRowsAtOnce, all - pass * kRowsAtOnce);
-        if ((two ? 2 * rows : rows) <= 16) layer_rows<STAGE, MX, BF16, HALVES, 1>(a, maps, lists, smem, ring, e, p, rows, two);
-        else layer_rows<STAGE, MX, BF16, HALVES, 2>(a, maps, lists, smem, ring, e, p, rows, two);
+        constexpr int kMost = pass_rows(STAGE);
+        if (pass * kMost >= all) break;
+        const int e = lists.expert[i], p = lists.start[i] + pass * kMost, rows = min(kMost, all - pass * kMost);
+        constexpr int kEach = rows_of_sixteen(STAGE);
+        if (rows <= kEach) layer_rows<STAGE, MX, BF16, HALVES, 1>(a, maps, lists, smem, ring, e, p, rows);
+        else if (STAGE == HIDDEN || rows <= 2 * kEach) layer_rows<STAGE, MX, BF16, HALVES, 2>(a, maps, lists, smem, ring, e, p, rows);
+        else layer_rows<STAGE, MX, BF16, HALVES, STAGE == HIDDEN ? 2 : 3>(a, maps, lists, smem, ring, e, p, rows);
         if (threadIdx.x == 0) at_pass += a.passes;               // all have read it before the barriers of the products
         __syncthreads();
     }
@@ -714,7 +747,7 @@ template <bool MX, bool BF16, bool HALVES>
 __global__ void __launch_bounds__(kLayerThreads, 2) layer_one_row_kernel(LayerArgs a, const __grid_constant__ LayerMaps maps) {
     release_successor();
     extern __shared__ __align__(128) char panels[];
-    static_assert(kRouteThreads == kLayerThreads && sizeof(Router) <= 2 * kPanelBytes, "the router's place is the panels'");
+    static_assert(kRouteThreads == kLayerThreads && sizeof(Router) <= 2 * panel_bytes(HIDDEN), "the router's place is the panels'");
     __shared__ OneRow found;
     const int tid = threadIdx.x;
     const bool notes = blockIdx.y == 0 && blockIdx.z == 0;
@@ -776,16 +809,16 @@ constexpr int kPartRows = 2 * kMaxSlots;     // shares times pairs, at most
 
 template <bool MX, bool BF16>
 cudaError_t launch_layer(emc2_bridge* h, LayerArgs a, cudaStream_t st) {
-    constexpr size_t most = kProductShared;
+    constexpr size_t most_hidden = product_shared(HIDDEN), most_down = product_shared(DOWN);
     static std::atomic<uint64_t> allowed{0};                      // devices; one bound for every call, so once for each
     const uint64_t bit = h->cfg.device < 64 ? (uint64_t)1 << h->cfg.device : 0;
     if (!(allowed.load(std::memory_order_relaxed) & bit)) {
-        cudaError_t e = allow_shared(layer_hidden_kernel<MX, BF16, false>, most);
-        if (e == cudaSuccess) e = allow_shared(layer_down_kernel<MX, BF16, false>, most);
-        if (e == cudaSuccess && MX) e = allow_shared(layer_hidden_kernel<MX, BF16, MX>, most);
-        if (e == cudaSuccess) e = allow_shared(layer_one_row_kernel<MX, BF16, false>, most);
-        if (e == cudaSuccess && MX) e = allow_shared(layer_one_row_kernel<MX, BF16, MX>, most);
-        if (e == cudaSuccess && MX) e = allow_shared(layer_down_kernel<MX, BF16, MX>, most);
+        cudaError_t e = allow_shared(layer_hidden_kernel<MX, BF16, false>, most_hidden);
+        if (e == cudaSuccess) e = allow_shared(layer_down_kernel<MX, BF16, false>, most_down);
+        if (e == cudaSuccess && MX) e = allow_shared(layer_hidden_kernel<MX, BF16, MX>, most_hidden);
+        if (e == cudaSuccess) e = allow_shared(layer_one_row_kernel<MX, BF16, false>, most_hidden);
+        if (e == cudaSuccess && MX) e = allow_shared(layer_one_row_kernel<MX, BF16, MX>, most_hidden);
+        if (e == cudaSuccess && MX) e = allow_shared(layer_down_kernel<MX, BF16, MX>, most_down);
         if (e != cudaSuccess) return e;
         allowed.fetch_or(bit, std::memory_order_relaxed);
     }
@@ -811,8 +844,8 @@ cudaError_t launch_layer(emc2_bridge* h, LayerArgs a, cudaStream_t st) {
         const int per = (kLayerWarps >> a.split_log) * width;
         return (M + per - 1) / per;
     };
-    auto plan = [&](int K, int M, int width) {
-        const int steps = (K + step - 1) / step, most_log = MX ? 1 : 2, most_passes = std::min((a.n + kRowsAtOnce - 1) / kRowsAtOnce, (5 * a.n * a.k + 4 * kRowsAtOnce * a.E - 1) / (4 * kRowsAtOnce * a.E));
+    auto plan = [&](int K, int M, int width, int rows) {
+        const int steps = (K + step - 1) / step, most_log = MX ? 1 : 2, most_passes = std::min((a.n + rows - 1) / rows, (5 * a.n * a.k + 4 * rows * a.E - 1) / (4 * rows * a.E));
         a.split_log = 0;
         a.tiles = tiles_of(M, width);
         for (a.passes = 1; a.passes < most_passes && a.tiles * experts * a.shares * (a.passes + 1) <= 2 * h->num_sms;) ++a.passes;
@@ -828,7 +861,7 @@ cudaError_t launch_layer(emc2_bridge* h, LayerArgs a, cudaStream_t st) {
     }
     {
         LaunchScope ls(h, K_LAYER_HIDDEN, st);
-        plan(a.C, a.H, 16);
+        plan(a.C, a.H, 16, pass_rows(HIDDEN));
         // Two to four waves of CTAs end less unevenly as twice as many: 32 experts of 1,024 channels and 4,096 units (1,024 CTAs) 158.5 us for
         // the layer instead of 161.8.  Of 512 and 2,048 (512 CTAs) 54.1 instead of 49.2, 64 experts of 256 and 4,096 (2,048) 132.6 instead of 117.
         const int ctas = a.tiles * experts;
@@ -838,8 +871,8 @@ cudaError_t launch_layer(emc2_bridge* h, LayerArgs a, cudaStream_t st) {
         }
         const dim3 grid(1, (unsigned)a.tiles, (unsigned)(a.passes * experts));
         const bool halves = MX && a.split_log;
-        if (one) launch_kernel(false, halves ? layer_one_row_kernel<MX, BF16, MX> : layer_one_row_kernel<MX, BF16, false>, grid, kLayerThreads, most, st, a, maps);
-        else launch_chained(halves ? layer_hidden_kernel<MX, BF16, MX> : layer_hidden_kernel<MX, BF16, false>, grid, kLayerThreads, most, st, a, maps);
+        if (one) launch_kernel(false, halves ? layer_one_row_kernel<MX, BF16, MX> : layer_one_row_kernel<MX, BF16, false>, grid, kLayerThreads, most_hidden, st, a, maps);
+        else launch_chained(halves ? layer_hidden_kernel<MX, BF16, MX> : layer_hidden_kernel<MX, BF16, false>, grid, kLayerThreads, most_hidden, st, a, maps);
     }
     {
         LaunchScope ls(h, K_LAYER_DOWN, st);
@@ -848,9 +881,9 @@ cudaError_t launch_layer(emc2_bridge* h, LayerArgs a, cudaStream_t st) {
         const int tiles = (a.C + kLayerWarps * 32 - 1) / (kLayerWarps * 32);
         while (a.shares < kMaxShares && tiles * experts * a.shares < h->num_sms && a.H >= 2 * a.shares * 256 && 2 * a.shares * a.n * a.k <= kPartRows)
             a.shares *= 2;
-        plan(a.H / a.shares, a.C, 32);
+        plan(a.H / a.shares, a.C, 32, pass_rows(DOWN));
         a.last_adds = a.n * a.k * a.shares <= kLastAdds;
-        launch_chained(MX && a.split_log ? layer_down_kernel<MX, BF16, MX> : layer_down_kernel<MX, BF16, false>, dim3((unsigned)a.shares, (unsigned)a.tiles, (unsigned)(a.passes * experts)), kLayerThreads, most, st, a, maps);
+        launch_chained(MX && a.split_log ? layer_down_kernel<MX, BF16, MX> : layer_down_kernel<MX, BF16, false>, dim3((unsigned)a.shares, (unsigned)a.tiles, (unsigned)(a.passes * experts)), kLayerThreads, most_down, st, a, maps);
     }
     if (!a.last_adds) {
         LaunchScope ls(h, K_LAYER_SUM, st);
