@@ -345,7 +345,7 @@ __device__ __forceinline__ void product(float (&c)[4], uint32_t a0, uint32_t a1,
 
 // Eight codes as the pairs (0, 4), (1, 5), (2, 6), (3, 7), times the type's smallest power that is not its last: the three bits of a size
 // are put at the end of the exponent and the start of the mantissa, where they read as the element times 2^-126 (bf16) or 2^-14 (fp16),
-// its number below 1 too, and `factor` makes up for it.
+// its number below 1 too, and `factor` makes up for it.  fp16's results are twice the elements, see spare.
 template <bool BF16>
 __device__ __forceinline__ void decode8(uint32_t (&r)[4], uint32_t codes, uint32_t factor) {
     constexpr uint32_t size = BF16 ? 0x01C001C0u : 0x0E000E00u, sign = 0x80008000u;
@@ -358,11 +358,15 @@ __device__ __forceinline__ void decode8(uint32_t (&r)[4], uint32_t codes, uint32
         else asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r[i]) : "r"(v), "r"(factor));
     }
 }
-// The pair of factors for a block whose power is 2^-below of its row's.
+// Sums are relative to the largest power that a row has had so far, and `spare` powers above it, so that the next rise is seldom.  What is
+// smaller than a type's numbers reach is rounded: fp16 has one to spare and is taken twice as large, so that its elements are rounded to 2^-24 of the
+// row's largest power; with two, and as they are, to 2^-22.  bf16's reach is 2^-131.
+__host__ __device__ constexpr uint32_t spare(bool bf16) { return bf16 ? 2u : 1u; }
+// The pair of factors for a block whose power is 2^-below of what the sums are relative to.
 template <bool BF16>
 __device__ __forceinline__ uint32_t block_factor(int below) {
     if (BF16) return (uint32_t)max(253 - below, 0) * 0x00800080u;
-    const uint32_t h = below < 29 ? (uint32_t)(29 - below) << 10 : below <= 38 ? 1u << (38 - below) : 0u;
+    const uint32_t h = below < 30 ? (uint32_t)(30 - below) << 10 : below <= 39 ? 1u << (39 - below) : 0u;
     return h * 0x00010001u;
 }
 
@@ -551,8 +555,7 @@ __device__ __forceinline__ void layer_rows(const LayerArgs& a, const LayerMaps& 
         uint32_t top = __vmaxu4(power_of_block, __shfl_xor_sync(0xFFFFFFFFu, power_of_block, 1));
         top = __vmaxu4(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
         if (__any_sync(0xFFFFFFFFu, __vmaxu4(top, largest) != largest)) {
-            // With two powers to spare, so that the next rise is seldom.
-            top = __vmaxu4(__vmaxu4(__vminu4(__vaddus4(top, 0x02020202u), 0xFEFEFEFEu), top), largest);
+            top = __vmaxu4(__vmaxu4(__vminu4(__vaddus4(top, spare(BF16) * 0x01010101u), 0xFEFEFEFEu), top), largest);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int fall = (int)(top >> (8 * i) & 255u) - (int)(largest >> (8 * i) & 255u);
@@ -613,7 +616,7 @@ __device__ __forceinline__ void layer_rows(const LayerArgs& a, const LayerMaps& 
     }
     if (MX) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) scale(i, mx_power(largest >> (8 * i) & 255u));
+        for (int i = 0; i < 4; ++i) scale(i, (BF16 ? 1.0f : 0.5f) * mx_power(largest >> (8 * i) & 255u));
     }
     __syncthreads();                                              // the panels are done with; the warps that share a tile are added in their order
     float* sums = reinterpret_cast<float*>(smem);
