@@ -840,9 +840,11 @@ cudaError_t launch_layer(emc2_bridge* h, LayerArgs a, cudaStream_t st) {
     const int experts = std::min(a.E, a.n * a.k);
     const int step = MX ? 256 : 64;
     // CTAs that share an expert's rows: where its tiles leave SMs without one, so many that all fit, and as its passes are with a quarter more rows than
-    // an even choice gives it.  128 rows, both of 2 experts of 512 channels and 2,048 units: 33 us instead of 55, in 4 bits 34 instead of 75.  As many as an expert can
-    // have passes: 36 us instead of 29 for 100 rows, 2 of 16 experts.  Then warps that share a tile: none where the CTAs fill the SMs, else as many as that
-    // takes, and as have steps.
+    // an even choice gives it.  us for the layer so, with one CTA for all passes, with as many as an expert can have passes, and as an even choice gives
+    // (16-bit weights; 4-bit): 128 rows, both of 2 experts of 512 channels and 2,048 units 37.4, 65.0, 37.4, 37.3 (37.7, 79.6, 37.7, 37.7); 100 rows, 2 of
+    // 16 of 512 and 1,024 29.8, 29.9, 36.7, 29.9; 128 rows, 1 of 2 of 1,024 and 2,048 40.4, 51.0, 40.8, 39.7 (42.0, 73.6, 42.2, 50.4); 96 rows, 1 of 3 of
+    // 256 and 512 19.5, 23.3, 20.0, 20.8 (22.0, 30.1, 23.5, 27.4); 50 rows, 2 of 5 of 256 and 1,024 22.5, 24.3, 25.0, 24.4.
+    // Then warps that share a tile: none where the CTAs fill the SMs, else as many as that takes, and as have steps.
     auto tiles_of = [&](int M, int width) {
         const int per = (kLayerWarps >> a.split_log) * width;
         return (M + per - 1) / per;
@@ -865,10 +867,12 @@ cudaError_t launch_layer(emc2_bridge* h, LayerArgs a, cudaStream_t st) {
     {
         LaunchScope ls(h, K_LAYER_HIDDEN, st);
         plan(a.C, a.H, 16, pass_rows(HIDDEN));
-        // Two to four waves of CTAs end less unevenly as twice as many: 32 experts of 1,024 channels and 4,096 units (1,024 CTAs) 158.5 us for
-        // the layer instead of 161.8.  Of 512 and 2,048 (512 CTAs) 54.1 instead of 49.2, 64 experts of 256 and 4,096 (2,048) 132.6 instead of 117.
+        // Two to four waves of CTAs end less unevenly as twice as many, where there are channels enough to make up for their starts.  us for the
+        // layer with and without, at 592 to 1,183 CTAs: of 1,024 channels 167.6 and 171.6 (1,024 CTAs), 122.7 and 125.6 (640), 170.8 and 181.2
+        // (608), 144.6 and 147.8 (1,024, 20 rows); of 768 109.7 and 111.2 (896).  Of 512 105.9 and 103.4 (784), 93.9 and 92.3 (1,152), of 256 79.0
+        // and 72.8 (1,152), of 128 60.4 and 55.0 (800): no.  Of 1,024 channels in more CTAs (1,216) 195.5 and 196.6, of 512 (1,504) 159.9 and 152.
         const int ctas = a.tiles * experts;
-        if (!MX && a.split_log == 0 && ctas >= 4 * h->num_sms && ctas < 8 * h->num_sms && a.C > step) {
+        if (!MX && a.split_log == 0 && ctas >= 4 * h->num_sms && ctas < 8 * h->num_sms && a.C >= 12 * step) {
             a.split_log = 1;
             a.tiles = tiles_of(a.H, 16);
         }
