@@ -11,8 +11,8 @@
 // products, whose 16 rows are the rows at hand and whose 8 columns are the weights': a row of x more costs no more reading, and there are too
 // few of them for larger products to help.
 //
-// 128 rows of 1,024 channels, 4 of 32 experts of 4,096 units, bf16: 169 us, of which the weights' 805 MB take 123 at a copy's rate; in 4 bits 165
-// (33), with half of the issue slots and a third of the tensor pipe's.  One row of 256 channels, 2 of 16 experts of 1,024 units: 12.8.
+// 128 rows of 1,024 channels, 4 of 32 experts of 4,096 units, bf16: 167 us, of which the weights' 805 MB take 123 at a copy's rate; in 4 bits 161
+// (33), with half of the issue slots and a third of the tensor pipe's.  One row of 256 channels, 2 of 16 experts of 1,024 units: 12.7.
 //
 // A logit is the sum of a sum in fp32 and of all that its roundings left (Ogita, Rump and Oishi, "Accurate sum and dot product", 2005), as if
 // of twice the bits, so that the choice does not depend on an order of summation; 64-bit arithmetic took six times as long.  Products are
@@ -40,8 +40,8 @@ constexpr int kMaxLayerHidden = 8192;
 constexpr int kPanel = 256;                  // elements of the rows at hand in shared memory at a time
 enum Stage { HIDDEN = 0, DOWN };
 // Sixteens of a product's rows in a pass, at most, and the rows at hand that they are: a row of hidden values, in two parts, takes two.  Three of
-// hidden values are what shared memory and registers have room for.  With two: 184 us instead of 169 for the layer above, whose experts
-// have 16 rows on average, 175 instead of 165 in 4 bits; 33 instead of 37 where two experts of 512 channels and 2,048 units have 128 each.
+// hidden values are what shared memory and registers have room for.  With two: 184 us instead of 168 for the layer above, whose experts
+// have 16 rows on average, 175 instead of 164 in 4 bits; 33 instead of 37 where two experts of 512 channels and 2,048 units have 128 each.
 __host__ __device__ constexpr int pass_sixteens(int stage) { return stage == DOWN ? 3 : 2; }
 __host__ __device__ constexpr int rows_of_sixteen(int stage) { return stage == DOWN ? 8 : 16; }
 __host__ __device__ constexpr int pass_rows(int stage) { return pass_sixteens(stage) * rows_of_sixteen(stage); }
@@ -744,8 +744,8 @@ struct OneRow {
 };
 
 // The first kernel and the second in one, for one row (decoding): every CTA makes its choice for itself, the first one notes it for what
-// follows.  That is a launch and a wait less: 13.1 us against 14.5 with 8 or 32 experts of 256 channels, 28.9 against 30.6 with 256 of
-// 512.  Two rows are no faster this way (15.8 against 15.4), four are slower (19.6 against 15.6): their choices come one after the other.
+// follows.  That is a launch and a wait less: 12.9 us against 14.1 with 8 experts of 256 channels, 13.1 against 14.5 with 32, 26.0 against 27.2 with
+// 256 of 512.  Two rows are no faster this way (15.8 against 15.4), four are slower (19.6 against 15.6): their choices come one after the other.
 template <bool MX, bool BF16, bool HALVES>
 __global__ void __launch_bounds__(kLayerThreads, 2) layer_one_row_kernel(LayerArgs a, const __grid_constant__ LayerMaps maps) {
     release_successor();
@@ -883,12 +883,19 @@ cudaError_t launch_layer(emc2_bridge* h, LayerArgs a, cudaStream_t st) {
     }
     {
         LaunchScope ls(h, K_LAYER_DOWN, st);
-        // Shares of the hidden units, of 256 at least: so many that there is a CTA per SM, which then has one or two, all at once.  With four CTAs
-        // per SM there are two waves, and more to add up: 169.7 us for the larger layer above instead of 161.8, 53.3 for the smaller instead of 49.2.
+        // Shares of the hidden units, of 256 at least: so many that there is a CTA per SM, which then has one or two, all at once.  With twice as many
+        // there are two waves, and more to add up: 32 experts of 1,024 channels and 4,096 units 173.9 us instead of 167.5, of 2,560 units 128.6 instead of 121.5,
+        // of 512 and 2,048 75.1 and 75.1; in 4 bits 159.5 instead of 167.5, 118.3 instead of 115.2 and 69.3 instead of 69.7.
         const int tiles = (a.C + kLayerWarps * 32 - 1) / (kLayerWarps * 32);
         while (a.shares < kMaxShares && tiles * experts * a.shares < h->num_sms && a.H >= 2 * a.shares * 256 && 2 * a.shares * a.n * a.k <= kPartRows)
             a.shares *= 2;
         plan(a.H / a.shares, a.C, 32, pass_rows(DOWN));
+        // Where the CTAs fill the SMs, the few experts with more rows than a pass get CTAs for a second one, which the others' leave at once: one CTA
+        // with both would be the last by far.  us for the layer so and without, means of eight choices of experts: 32 of 1,024 channels and 4,096 units 167.2 and
+        // 173.5 (188 where an expert has 25 rows), in 4 bits 160.9 and 173.5; 28 experts of 512 channels and 3,584 units 95.2 and 102.3; 16 of 1,024
+        // and 4,864, of 32 rows on average, 164.0 and 171.8.  With rarer ones, up to 8 rows on average, or SMs to spare it gains nothing: 8 experts of 1,024
+        // channels and units, 64 rows, 31.6 and 30.8.
+        if (a.passes == 1 && a.split_log == 0 && a.n > pass_rows(DOWN) && 3 * a.n * a.k > pass_rows(DOWN) * a.E) a.passes = 2;
         a.last_adds = a.n * a.k * a.shares <= kLastAdds;
         launch_chained(MX && a.split_log ? layer_down_kernel<MX, BF16, MX> : layer_down_kernel<MX, BF16, false>, dim3((unsigned)a.shares, (unsigned)a.tiles, (unsigned)(a.passes * experts)), kLayerThreads, most_down, st, a, maps);
     }

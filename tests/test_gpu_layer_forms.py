@@ -37,7 +37,7 @@ def check(got, want, rows=slice(None)):
 # units; 32 rows per expert on average.  (128 and 20, 776, 2568, 32, 4): 672 CTAs, in 16 bits taken as 1,344; (96, 328, 2568, 32, 4): not.
 # (128, 1024, 1288, 40, 3): 160 CTAs of last products, all hidden units in one.  (128, 264, 8192, 2, 2): 128 rows per expert in shared passes, eight shares.
 # (5, 1000, 4104, 30, 8): few rows of each expert, filled SMs.
-SHAPES = [(128, 520, 2056, 16, 4), (128, 776, 2568, 32, 4), (20, 776, 2568, 32, 4), (128, 1024, 1288, 40, 3), (128, 264, 8192, 2, 2), (5, 1000, 4104, 30, 8), (96, 328, 2568, 32, 4)]
+SHAPES = [(128, 1024, 2048, 32, 4), (128, 520, 2056, 16, 4), (128, 776, 2568, 32, 4), (20, 776, 2568, 32, 4), (128, 1024, 1288, 40, 3), (128, 264, 8192, 2, 2), (5, 1000, 4104, 30, 8), (96, 328, 2568, 32, 4)]
 
 
 @pytest.mark.parametrize("form", ["16 bits", "4 bits"])
