@@ -407,7 +407,7 @@ __global__ void __launch_bounds__(kGradThreads, grad_ctas(WIDE, U, ACROSS)) resi
     __shared__ __align__(8) unsigned long long bars[kTeams][2];
     __shared__ float meet[ACROSS ? 2 : 1][kGradThreads / 32][6];
     __shared__ int gave_up;
-    extern __shared__ float4 sums[];         // [teams][4][nvec], then two stages of two rows per group; across a CTA the latter only
+    extern __shared__ float4 sums[];         // [teams][4][nvec], then two stages of the rows in work per group; across a CTA the latter only
     if (!take_run(a, bounds, start, run)) return;
     const int B = a.seg.B, E = a.seg.E;
     const int type_x = rows_type<U>(a.type_x), type_f = block_type<U>(a.type_f), type_y = block_type<U>(a.type_y);
@@ -782,13 +782,15 @@ cudaError_t launch_grad(const ResGradArgs& a, bool wide, int usual, int ctas, in
     const bool pre = a.par.p[PRE_W] != nullptr;
     const int n = (pre ? slots(a.type_x) + slots(a.type_y) : 0) + (a.dout ? slots(a.type_x) : 0) + slots(a.type_f);
     const size_t own = ACROSS ? 0 : (size_t)teams * 4 * a.nvec * sizeof(float4);
-    // Two stages of two rows: per team of `chunk` rows, or per thread of its vectors and a row's statistics.
+    // Two stages of the rows in work: per team of `chunk` rows, or per thread of its vectors and a row's statistics.
     const size_t at_once = rows_at_once(wide, usual, ACROSS), chunk = ACROSS ? at_once : at_once * (32 / a.lanes);
     const size_t stages = wide ? (size_t)teams * 2 * chunk * ((size_t)n * a.nvec * 8 + (a.stats ? 16 : 0)) : (size_t)2 * at_once * (n + (a.stats ? 1 : 0)) * kGradSlot;
     const size_t shared = own + stages;
-    // 16 KB of sums and the stages of four fp32 buffers: of lanes' vectors 9 slots, of rows 64 of 144 bytes per warp (eight channels) at most;
-    // across a CTA rows of 16 KB, two at once, two stages, and no sums.
-    constexpr size_t most = 16 * 1024 + std::max<size_t>(4 * 9 * kGradSlot, 8 * 64 * 144);
+    // 16 KB of sums and the two stages of four fp32 buffers and the statistics: of rows of eight channels, two in work, 64 of 144 bytes per warp.  Others
+    // need less: lanes' vectors 9 slots of one row, rows across a CTA 16 KB and 16 bytes each, two at once, and no sums.
+    constexpr size_t most = 16 * 1024 + 8 * 64 * 144;
+    static_assert(2 * 9 * kGradSlot <= 8 * 64 * 144 && 2 * 2 * (16 * 1024 + 16) <= 8 * 64 * 144, "stages");
+    static_assert(rows_at_once(false, ANY, false) == 1 && rows_at_once(false, ANY, true) == 1, "lanes' vectors of one row");
     auto kernel = wide ? residual_grad_kernel<true, ANY, true, ACROSS> : residual_grad_kernel<false, ANY, true, ACROSS>;
     if (usual == F32_ROWS) kernel = a.drop.any ? residual_grad_kernel<true, F32_ROWS, true, ACROSS> : residual_grad_kernel<true, F32_ROWS, false, ACROSS>;
     if (usual == BF16_ROWS) kernel = a.drop.any ? residual_grad_kernel<true, BF16_ROWS, true, ACROSS> : residual_grad_kernel<true, BF16_ROWS, false, ACROSS>;
