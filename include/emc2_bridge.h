@@ -463,7 +463,7 @@ int emc2_expert_layer(emc2_bridge_t* bridge, int32_t n, int32_t channels, int32_
 /* The same with weights in the form of emc2_mx4_quantise (the rows are [experts * hidden] of `channels` for the gate and the up
  * projection, [experts * channels] of `hidden` for the down projection): products with what the codes stand for, summed in fp32
  * relative to their row's largest power (sums relative to it have to stay in fp32's range); elements that are not multiples of 2^-24 of that
- * power in EMC2_F16, of 2^-131 in EMC2_BF16, are rounded to them. */
+ * power in EMC2_F16, of 2^-131 in EMC2_BF16, can be rounded to such. */
 int emc2_expert_layer_mx4(emc2_bridge_t* bridge, int32_t n, int32_t channels, int32_t hidden, int32_t experts, int32_t choices, int32_t type,
                           int32_t act, const void* d_x, const int32_t* d_count, const float* d_w_router, const float* d_b_router,
                           const uint8_t* d_gate_codes, const uint8_t* d_gate_scales, const uint8_t* d_up_codes, const uint8_t* d_up_scales,
